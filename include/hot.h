@@ -226,6 +226,111 @@ hot_status hot_select_quantizer(const hot_config* cfg, const float* g_y, int64_t
  */
 hot_status hot_lowpass_l1_rows(int32_t block, int32_t keep, int32_t* keep_idx);
 
+/* ---- the operators around the linear backward --------------------------------
+ *
+ * What a training step of a transformer block runs beside the calls above: the
+ * forward product, the activation, the layer norm, and an 8-bit form of what
+ * those keep for their backward pass (hot_compress_activation's buffer serves g_w
+ * only).  The conventions at the top of this file hold, and:
+ *   - Tensors are [rows x cols], row-major and contiguous; a `hot_type` argument
+ *     says what a tensor's elements are.  Sums, statistics and the values between a
+ *     load and a store are fp32; a bfloat16 result is rounded once, to nearest even.
+ *   - rows and cols are 1 or more; rows < 2^31, cols < 2^24 (16384 for the layer norm).
+ *   - No output may overlap an input or another output (checked: HOT_ERR_ARG).
+ *   - Kernels of one call exchange values only from one launch to the next, in
+ *     stream order: every call may be recorded into a HIP graph and replayed, without
+ *     `replayable`.  Two graphs may share a workspace if they never run at once.
+ *   - Results have the same bits in every call (no atomics).
+ *   - An infinity or a NaN in a row reaches that row's results (and the sums over
+ *     rows), never another row's.
+ */
+typedef enum { HOT_F32 = 0, HOT_BF16 = 1 } hot_type;
+
+/* RELU max(x, 0) (slope 0 at 0); GELU x Phi(x); GELU_TANH its tanh form,
+ * x / 2 (1 + tanh(sqrt(2 / pi) (x + 0.044715 x^3))); SILU x / (1 + exp(-x)). */
+typedef enum {
+  HOT_ACT_NONE = 0, HOT_ACT_RELU = 1, HOT_ACT_GELU = 2, HOT_ACT_GELU_TANH = 3, HOT_ACT_SILU = 4
+} hot_act_fn;
+
+/*
+ * 8-bit checkpoint of a tensor: 32 consecutive columns of a row (a row's last group may be
+ * shorter) share a step s = 2^(e - 133), the smallest power of two from 2^-125 on that leaves
+ * the group's largest magnitude within 127 steps after rounding; code = round(t / s), half to
+ * even, one signed byte; the value read back is code * s, exact in either type, at most s / 2 off.
+ * A group that holds an infinity or a NaN reads back as NaN.  Layout: rows x pitch codes, pitch =
+ * cols rounded up to 32 (codes past cols are 0), then, from the next multiple of 256 bytes on,
+ * rows x pitch / 32 bytes e (255: NaN).  25.8 % of fp32.
+ * hot_checkpoint_bytes: size of that buffer, 0 for a size out of range.
+ * hot_checkpoint_write: x -> ckpt.  hot_checkpoint_read: ckpt -> x.
+ */
+size_t hot_checkpoint_bytes(int64_t rows, int64_t cols);
+hot_status hot_checkpoint_write(const void* x, hot_type type, int64_t rows, int64_t cols, void* ckpt, void* stream);
+hot_status hot_checkpoint_read(const void* ckpt, int64_t rows, int64_t cols, void* x, hot_type type, void* stream);
+
+/*
+ * y = f(x) point by point, fn not HOT_ACT_NONE; ckpt: the checkpoint of x, from the same read
+ * (NULL: none is made).
+ */
+hot_status hot_activation_forward(hot_act_fn fn, const void* x, hot_type type, int64_t rows, int64_t cols, void* y,
+                                  void* ckpt, void* stream);
+
+/*
+ * g_x = g_y f'(x), with x as it was (`x`) or from its checkpoint (`ckpt`): exactly one of the
+ * two is given.  `type` is that of g_y, g_x and x; the checkpoint of either type may be used.
+ * g_bias: fp32 [cols], the sum of g_x over the rows before it is rounded (the gradient of a bias in
+ * front of the activation), or NULL; with it `ws` is at least
+ * hot_activation_backward_workspace_bytes() bytes of scratch, 256-byte aligned, otherwise ws may be
+ * NULL.  HOT_ACT_NONE is allowed here (g_x = g_y, with the sums).
+ */
+size_t hot_activation_backward_workspace_bytes(int64_t rows, int64_t cols);
+hot_status hot_activation_backward(hot_act_fn fn, const void* g_y, hot_type type, const void* x, const void* ckpt,
+                                   int64_t rows, int64_t cols, void* g_x, float* g_bias, void* ws, size_t ws_bytes,
+                                   void* stream);
+
+/*
+ * Layer norm over the columns, with the residual addition in front of it:
+ *   h = x + residual (rounded to x_type; h = x without a residual),
+ *   y = (h - mean) rstd gamma + beta,  rstd = 1 / sqrt(var + eps), var over cols (biased).
+ * residual: [rows x cols] of x_type, or NULL; h: [rows x cols] of x_type (out), required with a
+ * residual and NULL without one.  gamma, beta: fp32 [cols], or NULL (1 and 0).  y: y_type; x_type
+ * HOT_BF16 takes y_type HOT_BF16 only.  mean, rstd: fp32 [rows] (out).  eps >= 0.  ckpt: the
+ * checkpoint of h (NULL: none is made).
+ */
+hot_status hot_layer_norm_forward(const void* x, hot_type x_type, const void* residual, const float* gamma,
+                                  const float* beta, float eps, int64_t rows, int64_t cols, void* h, void* y,
+                                  hot_type y_type, float* mean, float* rstd, void* ckpt, void* stream);
+
+/*
+ * Gradients of the layer norm: with n = (h - mean) rstd and t = g_y gamma,
+ *   g_x = rstd (t - mean(t) - n mean(t n)) + g_residual,  g_gamma = sum of g_y n over the rows,
+ *   g_beta = sum of g_y.  g_x is the gradient of x and of the residual alike.
+ * g_y: y_type; h (x_type) or its checkpoint: exactly one of the two; g_residual: x_type, the gradient
+ * that reaches h past the norm, or NULL; g_x: x_type (out).  mean, rstd: what the forward call wrote.
+ * g_gamma and g_beta: fp32 [cols] (out), both or neither; with them `ws` is at least
+ * hot_layer_norm_backward_workspace_bytes() bytes of scratch, 256-byte aligned, otherwise ws may be NULL.
+ */
+size_t hot_layer_norm_backward_workspace_bytes(int64_t rows, int64_t cols);
+hot_status hot_layer_norm_backward(const void* g_y, hot_type y_type, const void* h, const void* ckpt, hot_type x_type,
+                                   const float* gamma, const float* mean, const float* rstd, const void* g_residual,
+                                   int64_t rows, int64_t cols, void* g_x, float* g_gamma, float* g_beta, void* ws,
+                                   size_t ws_bytes, void* stream);
+
+/*
+ * Forward product of a linear layer: z = x.w^T + bias, y = f(z) + residual.
+ * x: [L x I], w: [O x I] of `type`; bias: fp32 [O] or NULL; residual: [L x O] of y_type or NULL;
+ * y: [L x O] of y_type (HOT_F32 operands take y_type HOT_F32 only).  fn may be HOT_ACT_NONE.
+ * ckpt: the checkpoint of z as [L x O], for hot_activation_backward (NULL: none is made).
+ * fp32 operands: every product keeps 22 bits of each factor relative to the largest of its row, and is
+ * summed in fp32, so that the result is as near the exact one as an fp32 product's; bfloat16 operands
+ * are multiplied exactly and summed in fp32.  I < 2^24, O < 2^24.
+ * ws: at least hot_linear_forward_workspace_bytes() bytes of scratch, 256-byte aligned (where that is
+ * 0, ws may be NULL).
+ */
+size_t hot_linear_forward_workspace_bytes(hot_type type, int64_t L, int64_t O, int64_t I);
+hot_status hot_linear_forward(const void* x, const void* w, hot_type type, const float* bias, const void* residual,
+                              int64_t L, int64_t O, int64_t I, hot_act_fn fn, void* y, hot_type y_type, void* ckpt,
+                              void* ws, size_t ws_bytes, void* stream);
+
 /* ---- parity views (not on the timed path): logical forms of packed data ---- */
 
 /* Compressed activation as row-major codes [L*r/n x I] and its scale [1].  With
@@ -297,7 +402,7 @@ hot_status hot_debug_set_gemm_mode(int mode);
 /* ---- stage timing for benchmarks (off by default) ---- */
 
 /* Kernel roles timed separately; hot_debug_stage_name() gives their names. */
-#define HOT_NUM_STAGES 15
+#define HOT_NUM_STAGES 24
 
 /* From this call on, every kernel the library launches is bracketed by two HIP
  * events recorded on its stream.  Host-side state only; not thread-safe against

@@ -33,9 +33,17 @@ EXPORTS = (
     "hot_debug_gx_operands", "hot_debug_gw_operands", "hot_debug_fused_operands", "hot_debug_set_exchange_wait_us",
     "hot_debug_set_backward_strategy", "hot_debug_set_gemm_mode", "hot_debug_profile_begin", "hot_debug_profile_end", "hot_debug_profile_sequence",
     "hot_debug_stage_name", "hot_debug_probe", "hot_debug_gemm_plan",
+    "hot_checkpoint_bytes", "hot_checkpoint_write", "hot_checkpoint_read", "hot_activation_forward",
+    "hot_activation_backward_workspace_bytes", "hot_activation_backward", "hot_layer_norm_forward",
+    "hot_layer_norm_backward_workspace_bytes", "hot_layer_norm_backward", "hot_linear_forward_workspace_bytes",
+    "hot_linear_forward",
 )
-HOT_NUM_STAGES = 15
+HOT_NUM_STAGES = 24
 HOT_WS_PREFIX_BYTES = 24832
+HOT_F32, HOT_BF16 = 0, 1
+HOT_ACT_NONE, HOT_ACT_RELU, HOT_ACT_GELU, HOT_ACT_GELU_TANH, HOT_ACT_SILU = range(5)
+ACT_FNS = {"none": HOT_ACT_NONE, "relu": HOT_ACT_RELU, "gelu": HOT_ACT_GELU, "gelu_tanh": HOT_ACT_GELU_TANH,
+           "silu": HOT_ACT_SILU}
 
 
 class hot_config(C.Structure):
@@ -103,7 +111,23 @@ def lib() -> C.CDLL:
         l.hot_quantize_weight.argtypes = [cfgp, vp, i64, i64, vp, vp, sz, vp]
         l.hot_linear_backward_gx_cached.argtypes = [cfgp, vp, vp, i64, i64, i64, C.c_int, vp, vp, sz, vp]
         l.hot_debug_unpack_weight.argtypes = [cfgp, vp, i64, i64, vp, vp, vp]
+        en = C.c_int
+        l.hot_checkpoint_write.argtypes = [vp, en, i64, i64, vp, vp]
+        l.hot_checkpoint_read.argtypes = [vp, i64, i64, vp, en, vp]
+        l.hot_activation_forward.argtypes = [en, vp, en, i64, i64, vp, vp, vp]
+        l.hot_activation_backward.argtypes = [en, vp, en, vp, vp, i64, i64, vp, vp, vp, sz, vp]
+        l.hot_layer_norm_forward.argtypes = [vp, en, vp, vp, vp, C.c_float, i64, i64, vp, vp, en, vp, vp, vp, vp]
+        l.hot_layer_norm_backward.argtypes = [vp, en, vp, vp, en, vp, vp, vp, vp, i64, i64, vp, vp, vp, vp, sz, vp]
+        l.hot_linear_forward.argtypes = [vp, vp, en, vp, vp, i64, i64, i64, en, vp, en, vp, vp, sz, vp]
+        sizes = {"hot_checkpoint_bytes": [i64, i64], "hot_activation_backward_workspace_bytes": [i64, i64],
+                 "hot_layer_norm_backward_workspace_bytes": [i64, i64],
+                 "hot_linear_forward_workspace_bytes": [en, i64, i64, i64]}
+        for name, args in sizes.items():
+            getattr(l, name).argtypes = args
+            getattr(l, name).restype = sz
         for name in EXPORTS[6:]:
+            if name in sizes:
+                continue
             if name not in ("hot_debug_stage_name", "hot_debug_profile_sequence"):
                 getattr(l, name).restype = C.c_int
         l.hot_debug_profile_sequence.restype = C.c_int64
@@ -318,6 +342,185 @@ def hot_lowpass_l1_rows(block: int, keep: int):
     out = (C.c_int32 * keep)()
     _check(lib().hot_lowpass_l1_rows(int(block), int(keep), out), "hot_lowpass_l1_rows")
     return [int(k) for k in out]
+
+
+# ---- the operators around the linear backward -----------------------------------------------------------------------
+# Tensors are contiguous [rows, cols] of float32 or bfloat16 on the current device; the argument checks below hold for each.
+
+_TYPES = {torch.float32: HOT_F32, torch.bfloat16: HOT_BF16}
+
+
+def _expect(name: str, t: torch.Tensor, dtype: torch.dtype, shape: Tuple[int, ...], device: int) -> int:
+    """The tensor's address; raises unless it is a contiguous `dtype` tensor of `shape` on CUDA device `device`."""
+    if not (t.is_cuda and t.get_device() == device and t.dtype == dtype and t.shape == shape and t.is_contiguous()):
+        raise ValueError(f"{name}: expected contiguous {dtype} tensor of shape {tuple(shape)} on cuda:{device}, the current device")
+    return t.data_ptr()
+
+
+def _typed(name: str, t: torch.Tensor) -> int:
+    """hot_type of a tensor that sets the type of others; raises unless it is a matrix of a supported type on the GPU."""
+    if not (t.is_cuda and t.dim() == 2 and t.dtype in _TYPES):
+        raise ValueError(f"{name}: expected a float32 or bfloat16 device tensor of two dimensions")
+    return _TYPES[t.dtype]
+
+
+def _bytes(name: str, t: Optional[torch.Tensor], least: int, device: int) -> Optional[int]:
+    """Address of an opaque uint8 buffer of at least `least` bytes."""
+    if t is None:
+        return None
+    if not (t.is_cuda and t.get_device() == device and t.dtype == torch.uint8 and t.is_contiguous() and t.numel() >= least):
+        raise ValueError(f"{name}: expected contiguous uint8 tensor of at least {least} bytes on cuda:{device}, the current device")
+    return t.data_ptr()
+
+
+def hot_checkpoint_bytes(rows: int, cols: int) -> int:
+    return int(lib().hot_checkpoint_bytes(rows, cols))
+
+
+def hot_activation_backward_workspace_bytes(rows: int, cols: int) -> int:
+    return int(lib().hot_activation_backward_workspace_bytes(rows, cols))
+
+
+def hot_layer_norm_backward_workspace_bytes(rows: int, cols: int) -> int:
+    return int(lib().hot_layer_norm_backward_workspace_bytes(rows, cols))
+
+
+def hot_linear_forward_workspace_bytes(dtype: torch.dtype, L: int, O: int, I: int) -> int:
+    return int(lib().hot_linear_forward_workspace_bytes(_TYPES[dtype], L, O, I))
+
+
+def _alloc(n: int, where: str, device) -> torch.Tensor:
+    if n == 0:
+        raise HotError(HOT_ERR_SHAPE, where)
+    return torch.empty(n, dtype=torch.uint8, device=device)
+
+
+def alloc_checkpoint(rows: int, cols: int, device="cuda") -> torch.Tensor:
+    return _alloc(hot_checkpoint_bytes(rows, cols), "hot_checkpoint_bytes", device)
+
+
+def alloc_activation_workspace(rows: int, cols: int, device="cuda") -> torch.Tensor:
+    """Scratch of hot_activation_backward with g_bias."""
+    return _alloc(hot_activation_backward_workspace_bytes(rows, cols), "hot_activation_backward_workspace_bytes", device)
+
+
+def alloc_layer_norm_workspace(rows: int, cols: int, device="cuda") -> torch.Tensor:
+    """Scratch of hot_layer_norm_backward with parameter gradients."""
+    return _alloc(hot_layer_norm_backward_workspace_bytes(rows, cols), "hot_layer_norm_backward_workspace_bytes", device)
+
+
+def alloc_linear_workspace(dtype: torch.dtype, L: int, O: int, I: int, device="cuda") -> Optional[torch.Tensor]:
+    """Scratch of hot_linear_forward; None where it needs none."""
+    n = hot_linear_forward_workspace_bytes(dtype, L, O, I)
+    return torch.empty(n, dtype=torch.uint8, device=device) if n else None
+
+
+def hot_checkpoint_write(x: torch.Tensor, ckpt: torch.Tensor, stream=None) -> torch.Tensor:
+    """Stores x in 8 bits; returns the buffer."""
+    ty, dev = _typed("x", x), torch.cuda.current_device()
+    rows, cols = x.shape
+    st = lib().hot_checkpoint_write(_expect("x", x, x.dtype, x.shape, dev), ty, rows, cols,
+                                    _bytes("ckpt", ckpt, hot_checkpoint_bytes(rows, cols), dev), _stream(stream))
+    _check(st, "hot_checkpoint_write")
+    return ckpt
+
+
+def hot_checkpoint_read(ckpt: torch.Tensor, x: torch.Tensor, stream=None) -> torch.Tensor:
+    """Fills x [rows, cols] with the values that the checkpoint of its shape holds; returns x."""
+    ty, dev = _typed("x", x), torch.cuda.current_device()
+    rows, cols = x.shape
+    st = lib().hot_checkpoint_read(_bytes("ckpt", ckpt, hot_checkpoint_bytes(rows, cols), dev), rows, cols,
+                                   _expect("x", x, x.dtype, x.shape, dev), ty, _stream(stream))
+    _check(st, "hot_checkpoint_read")
+    return x
+
+
+def hot_activation_forward(fn: int, x: torch.Tensor, y: torch.Tensor, ckpt: Optional[torch.Tensor] = None,
+                           stream=None) -> torch.Tensor:
+    """y = f(x), and the checkpoint of x where a buffer is given; returns y."""
+    ty, dev = _typed("x", x), torch.cuda.current_device()
+    rows, cols = x.shape
+    st = lib().hot_activation_forward(int(fn), _expect("x", x, x.dtype, x.shape, dev), ty, rows, cols,
+                                      _expect("y", y, x.dtype, x.shape, dev),
+                                      None if ckpt is None else _bytes("ckpt", ckpt, hot_checkpoint_bytes(rows, cols), dev),
+                                      _stream(stream))
+    _check(st, "hot_activation_forward")
+    return y
+
+
+def hot_activation_backward(fn: int, g_y: torch.Tensor, g_x: torch.Tensor, x: Optional[torch.Tensor] = None,
+                            ckpt: Optional[torch.Tensor] = None, g_bias: Optional[torch.Tensor] = None,
+                            ws: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """g_x = g_y f'(x) with x or its checkpoint, g_bias = the sum of g_x over the rows; returns g_x."""
+    ty, dev = _typed("g_y", g_y), torch.cuda.current_device()
+    rows, cols = shape = g_y.shape
+    st = lib().hot_activation_backward(
+        int(fn), _expect("g_y", g_y, g_y.dtype, shape, dev), ty, None if x is None else _expect("x", x, g_y.dtype, shape, dev),
+        None if ckpt is None else _bytes("ckpt", ckpt, hot_checkpoint_bytes(rows, cols), dev), rows, cols,
+        _expect("g_x", g_x, g_y.dtype, shape, dev),
+        None if g_bias is None else _expect("g_bias", g_bias, torch.float32, (cols,), dev),
+        _bytes("ws", ws, 0, dev), 0 if ws is None else ws.numel(), _stream(stream))
+    _check(st, "hot_activation_backward")
+    return g_x
+
+
+def hot_layer_norm_forward(x: torch.Tensor, gamma: Optional[torch.Tensor], beta: Optional[torch.Tensor], eps: float,
+                           y: torch.Tensor, mean: torch.Tensor, rstd: torch.Tensor, residual: Optional[torch.Tensor] = None,
+                           h: Optional[torch.Tensor] = None, ckpt: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """h = x + residual, y = layer norm of h, with its mean and rstd per row, and the checkpoint of h; returns y."""
+    tx, ty, dev = _typed("x", x), _typed("y", y), torch.cuda.current_device()
+    rows, cols = shape = x.shape
+    f32 = torch.float32
+    st = lib().hot_layer_norm_forward(
+        _expect("x", x, x.dtype, shape, dev), tx, None if residual is None else _expect("residual", residual, x.dtype, shape, dev),
+        None if gamma is None else _expect("gamma", gamma, f32, (cols,), dev),
+        None if beta is None else _expect("beta", beta, f32, (cols,), dev), eps, rows, cols,
+        None if h is None else _expect("h", h, x.dtype, shape, dev), _expect("y", y, y.dtype, shape, dev), ty,
+        _expect("mean", mean, f32, (rows,), dev), _expect("rstd", rstd, f32, (rows,), dev),
+        None if ckpt is None else _bytes("ckpt", ckpt, hot_checkpoint_bytes(rows, cols), dev), _stream(stream))
+    _check(st, "hot_layer_norm_forward")
+    return y
+
+
+def hot_layer_norm_backward(g_y: torch.Tensor, gamma: Optional[torch.Tensor], mean: torch.Tensor, rstd: torch.Tensor,
+                            g_x: torch.Tensor, g_gamma: Optional[torch.Tensor] = None, g_beta: Optional[torch.Tensor] = None,
+                            ws: Optional[torch.Tensor] = None, h: Optional[torch.Tensor] = None,
+                            ckpt: Optional[torch.Tensor] = None, g_residual: Optional[torch.Tensor] = None,
+                            stream=None) -> torch.Tensor:
+    """Gradients of the layer norm of h (or of its checkpoint); g_residual is added to g_x; returns g_x."""
+    ty, tx, dev = _typed("g_y", g_y), _typed("g_x", g_x), torch.cuda.current_device()
+    rows, cols = shape = g_y.shape
+    f32 = torch.float32
+    st = lib().hot_layer_norm_backward(
+        _expect("g_y", g_y, g_y.dtype, shape, dev), ty, None if h is None else _expect("h", h, g_x.dtype, shape, dev),
+        None if ckpt is None else _bytes("ckpt", ckpt, hot_checkpoint_bytes(rows, cols), dev), tx,
+        None if gamma is None else _expect("gamma", gamma, f32, (cols,), dev),
+        _expect("mean", mean, f32, (rows,), dev), _expect("rstd", rstd, f32, (rows,), dev),
+        None if g_residual is None else _expect("g_residual", g_residual, g_x.dtype, shape, dev), rows, cols,
+        _expect("g_x", g_x, g_x.dtype, shape, dev),
+        None if g_gamma is None else _expect("g_gamma", g_gamma, f32, (cols,), dev),
+        None if g_beta is None else _expect("g_beta", g_beta, f32, (cols,), dev),
+        _bytes("ws", ws, 0, dev), 0 if ws is None else ws.numel(), _stream(stream))
+    _check(st, "hot_layer_norm_backward")
+    return g_x
+
+
+def hot_linear_forward(x: torch.Tensor, w: torch.Tensor, y: torch.Tensor, ws: Optional[torch.Tensor] = None,
+                       bias: Optional[torch.Tensor] = None, residual: Optional[torch.Tensor] = None, fn: int = HOT_ACT_NONE,
+                       ckpt: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """y = f(x.w^T + bias) + residual, and the checkpoint of x.w^T + bias; returns y."""
+    tx, ty, dev = _typed("x", x), _typed("y", y), torch.cuda.current_device()
+    _typed("w", w)
+    (L, I), O = x.shape, w.shape[0]
+    st = lib().hot_linear_forward(
+        _expect("x", x, x.dtype, (L, I), dev), _expect("w", w, x.dtype, (O, I), dev), tx,
+        None if bias is None else _expect("bias", bias, torch.float32, (O,), dev),
+        None if residual is None else _expect("residual", residual, y.dtype, (L, O), dev), L, O, I, int(fn),
+        _expect("y", y, y.dtype, (L, O), dev), ty,
+        None if ckpt is None else _bytes("ckpt", ckpt, hot_checkpoint_bytes(L, O), dev),
+        _bytes("ws", ws, 0, dev), 0 if ws is None else ws.numel(), _stream(stream))
+    _check(st, "hot_linear_forward")
+    return y
 
 
 def hot_debug_unpack_activation(cfg: Config, act_buf: torch.Tensor, L: int, I: int, stream=None):

@@ -159,7 +159,8 @@ WeightLayout weight_layout(const Config& c, int64_t O, int64_t I);
 enum Stage {
   kStGemmPair = 0, kStActAbsmax, kStActQuant, kStWAbsmax, kStWQuant, kStGyRowQuant, kStGyRowAbsmax,
   kStGyRowQuant2, kStGxGemm, kStGyTAbsmax, kStGyTQuant, kStGwGemm, kStWGyRow, kStGyFusedAbsmax,
-  kStGyFusedQuant
+  kStGyFusedQuant, kStCkptWrite, kStCkptRead, kStActForward, kStActBackward, kStNormForward, kStNormBackward,
+  kStColumnSums, kStLinearOperands, kStLinear
 };
 void stage_begin(int stage, hipStream_t s);
 void stage_end(int stage, hipStream_t s);

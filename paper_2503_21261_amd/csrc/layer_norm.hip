@@ -1,0 +1,305 @@
+// Layer norm over the columns of [rows x cols], forward and backward, up to 16384 columns.
+//
+//   h = x (+ residual), y = (h - mean) rstd gamma + beta;   with n = (h - mean) rstd, t = g_y gamma:
+//   g_h = rstd (t - mean(t) - n mean(t n)) (+ g_residual),  g_gamma = sum over rows of g_y n,  g_beta = of g_y.
+//
+// Both are bound by HBM.  A row stays in the registers of the T lanes that work on it (eight columns a
+// lane, NV times), so it is read once: the mean first, then the squares of what is left, which keeps the
+// variance of rows whose mean is large.  The backward pass keeps a lane on its columns, so that the
+// parameter gradients are sums in registers; a workgroup leaves one row of them, and column_sums adds those in order.
+#include "block_device.h"
+#include "block_host.h"
+
+namespace hot {
+
+namespace {
+
+template <int T>
+constexpr int kSlots = 256 / T;   // rows a workgroup works on at a time
+
+// Sums of two values over the T lanes of a row, in every lane.  T = 256: through LDS, whose halves
+// alternate (`turn`), so that one barrier a call is enough.
+template <int T>
+__device__ __forceinline__ void row_sums(float& a, float& b, float (*s_red)[4][2], int turn) {
+  constexpr int W = T < 64 ? T : 64;
+  a = lanes_sum<W>(a);
+  b = lanes_sum<W>(b);
+  if constexpr (T > 64) {
+    const int wave = (int)threadIdx.x >> 6;
+    if (((int)threadIdx.x & 63) == 0) {
+      s_red[turn][wave][0] = a;
+      s_red[turn][wave][1] = b;
+    }
+    __syncthreads();
+    a = (s_red[turn][0][0] + s_red[turn][1][0]) + (s_red[turn][2][0] + s_red[turn][3][0]);
+    b = (s_red[turn][0][1] + s_red[turn][1][1]) + (s_red[turn][2][1] + s_red[turn][3][1]);
+  }
+}
+
+template <int T, int NV, class TX, class TY, bool KEEP>
+__global__ __launch_bounds__(256) void layer_norm_kernel(const NormForward a, const CkptView k) {
+  __shared__ float s_red[2][4][2];
+  const int lane = (int)threadIdx.x % T, slot = (int)threadIdx.x / T;
+  const int64_t row = (int64_t)blockIdx.x * kSlots<T> + slot;
+  if (row >= a.rows) return;   // T = 256: one row a workgroup, all of it or none
+  const int cols = (int)a.cols;
+  const int64_t at = row * cols;
+  Raw8<TX> xr[NV], rr[NV];
+#pragma unroll
+  for (int j = 0; j < NV; ++j) {
+    const int c = (lane + j * T) * 8;
+    if (c < cols) {
+      xr[j] = load8((const TX*)a.x + at + c, cols - c);
+      if (a.residual) rr[j] = load8((const TX*)a.residual + at + c, cols - c);
+    }
+  }
+  float v[NV][8], sum = 0.0f, none = 0.0f;
+#pragma unroll
+  for (int j = 0; j < NV; ++j) {
+    const int c = (lane + j * T) * 8;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[j][i] = 0.0f;
+    if (c < cols) {
+      widen(xr[j], v[j]);
+      if (a.residual) {
+        float r[8];
+        widen(rr[j], r);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[j][i] = rounded(v[j][i] + r[i], TX(0.0f));
+        if (a.h) store8((TX*)a.h + at + c, v[j], cols - c);
+      }
+    }
+    if constexpr (KEEP) {
+      if (c < (int)k.pitch) ckpt_store8(k, row * k.pitch + c, v[j]);
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) sum += v[j][i];
+  }
+  row_sums<T>(sum, none, s_red, 0);
+  // Twice: what the first mean is off by (its rounding, large beside the variance where |mean| is) is the
+  // mean of what is left.
+  const float mean0 = sum / (float)cols;
+  float sq = 0.0f, left = 0.0f;
+#pragma unroll
+  for (int j = 0; j < NV; ++j) {
+    const int n = cols - (lane + j * T) * 8;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[j][i] -= mean0;
+    if (n < 8) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[j][i] = i < n ? v[j][i] : 0.0f;
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      sq = fmaf(v[j][i], v[j][i], sq);
+      left += v[j][i];
+    }
+  }
+  row_sums<T>(sq, left, s_red, 1);
+  const float off = left / (float)cols;
+  float var = fmaf(-off, off, sq / (float)cols);
+  var = var < 0.0f ? 0.0f : var;   // a constant row, by rounding
+  const float rstd = 1.0f / sqrtf(var + a.eps);
+  if (lane == 0) {
+    a.mean[row] = mean0 + off;
+    a.rstd[row] = rstd;
+  }
+#pragma unroll
+  for (int j = 0; j < NV; ++j) {
+    const int c = (lane + j * T) * 8;
+    if (c < cols) {
+      float g[8], b[8];
+      if (a.gamma) load_values(a.gamma + c, cols - c, g);
+      if (a.beta) load_values(a.beta + c, cols - c, b);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        float n = (v[j][i] - off) * rstd;
+        if (a.gamma) n *= g[i];
+        if (a.beta) n += b[i];
+        v[j][i] = n;
+      }
+      store8((TY*)a.y + at + c, v[j], cols - c);
+    }
+  }
+}
+
+template <int T, int NV, class TX, class TY, bool KEPT>
+__global__ __launch_bounds__(256) void layer_norm_grad_kernel(const NormBackward a, const CkptView k) {
+  constexpr int SPAN = T * NV * 8;    // columns the lanes of a row cover
+  __shared__ float s_red[2][4][2];
+  __shared__ float s_sum[T < 256 ? kSlots<T> * SPAN : 1];
+  const int lane = (int)threadIdx.x % T, slot = (int)threadIdx.x / T;
+  const int cols = (int)a.cols;
+  float gamma[NV][8], sg[NV][8], sb[NV][8];
+#pragma unroll
+  for (int j = 0; j < NV; ++j) {
+    const int c = (lane + j * T) * 8;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      sg[j][i] = sb[j][i] = 0.0f;
+      gamma[j][i] = a.gamma ? 0.0f : 1.0f;
+    }
+    if (a.gamma && c < cols) load_values(a.gamma + c, cols - c, gamma[j]);
+  }
+  const float inv = 1.0f / (float)cols;
+  int turn = 0;
+  for (int64_t row = (int64_t)blockIdx.x * kSlots<T> + slot; row < a.rows; row += (int64_t)gridDim.x * kSlots<T>) {
+    const int64_t at = row * cols;
+    Raw8<TY> gr[NV];
+    Raw8<TX> hr[NV], ar[NV];
+    uint2 codes[NV];
+    uint32_t e[NV];
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+      const int c = (lane + j * T) * 8;
+      if (c < cols) {
+        gr[j] = load8((const TY*)a.g_y + at + c, cols - c);
+        if constexpr (KEPT) {
+          const int64_t kat = row * k.pitch + c;
+          codes[j] = *(const uint2*)(k.codes + kat);
+          e[j] = k.exps[kat / kCkGroup];
+        } else {
+          hr[j] = load8((const TX*)a.h + at + c, cols - c);
+        }
+        if (a.g_residual) ar[j] = load8((const TX*)a.g_residual + at + c, cols - c);
+      }
+    }
+    const float mean = a.mean[row], rstd = a.rstd[row];
+    float t[NV][8], n[NV][8], s1 = 0.0f, s2 = 0.0f;
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+      const int c = (lane + j * T) * 8;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) t[j][i] = n[j][i] = 0.0f;
+      if (c < cols) {
+        widen(gr[j], t[j]);
+        if constexpr (KEPT) decode8(codes[j], ckpt_step(e[j]), n[j]);
+        else widen(hr[j], n[j]);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          n[j][i] = (n[j][i] - mean) * rstd;
+          sb[j][i] += t[j][i];
+          sg[j][i] = fmaf(t[j][i], n[j][i], sg[j][i]);
+          t[j][i] *= gamma[j][i];
+          s1 += t[j][i];
+          s2 = fmaf(t[j][i], n[j][i], s2);
+        }
+      }
+    }
+    row_sums<T>(s1, s2, s_red, turn);
+    turn ^= 1;
+    const float m1 = s1 * inv, m2 = s2 * inv;
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+      const int c = (lane + j * T) * 8;
+      if (c < cols) {
+        float r[8];
+        if (a.g_residual) widen(ar[j], r);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const float g = rstd * (t[j][i] - m1 - n[j][i] * m2);
+          t[j][i] = a.g_residual ? g + r[i] : g;
+        }
+        store8((TX*)a.g_x + at + c, t[j], cols - c);
+      }
+    }
+  }
+  if (!a.partials) return;
+  const int64_t pitch = (a.cols + 31) / 32 * 32;
+  float* const out = a.partials + (int64_t)blockIdx.x * 2 * pitch;
+  if constexpr (T == 256) {
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+      const int c = (lane + j * T) * 8;
+      if (c < (int)pitch) {
+        store8(out + c, sg[j], 8);
+        store8(out + pitch + c, sb[j], 8);
+      }
+    }
+  } else {
+    auto add_slots = [&](const float(&s)[NV][8], float* dst) {
+#pragma unroll
+      for (int j = 0; j < NV; ++j)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) s_sum[slot * SPAN + (lane + j * T) * 8 + i] = s[j][i];
+      __syncthreads();
+      for (int c = (int)threadIdx.x; c < SPAN && c < (int)pitch; c += 256) {
+        float total = 0.0f;
+#pragma unroll
+        for (int y = 0; y < kSlots<T>; ++y) total += s_sum[y * SPAN + c];
+        dst[c] = total;
+      }
+      __syncthreads();
+    };
+    add_slots(sg, out);
+    add_slots(sb, out + pitch);
+  }
+}
+
+// Lanes to a row: the fewest that hold it with eight columns (sixteen up to 1024) each.
+template <class F>
+hipError_t with_lanes(int64_t cols, F&& f) {
+  using std::integral_constant;
+  if (cols <= 128) return f(integral_constant<int, 16>{}, integral_constant<int, 1>{});
+  if (cols <= 256) return f(integral_constant<int, 32>{}, integral_constant<int, 1>{});
+  if (cols <= 512) return f(integral_constant<int, 64>{}, integral_constant<int, 1>{});
+  if (cols <= 1024) return f(integral_constant<int, 64>{}, integral_constant<int, 2>{});
+  if (cols <= 2048) return f(integral_constant<int, 256>{}, integral_constant<int, 1>{});
+  if (cols <= 4096) return f(integral_constant<int, 256>{}, integral_constant<int, 2>{});
+  if (cols <= 8192) return f(integral_constant<int, 256>{}, integral_constant<int, 4>{});
+  return f(integral_constant<int, 256>{}, integral_constant<int, 8>{});
+}
+int slots_of(int64_t cols) { return cols <= 128 ? 16 : cols <= 256 ? 8 : cols <= 1024 ? 4 : 1; }
+
+template <class F>
+hipError_t with_types(hot_type x, hot_type y, F&& f) {
+  if (x == HOT_BF16) return f(bf16(0.0f), bf16(0.0f));
+  if (y == HOT_BF16) return f(0.0f, bf16(0.0f));
+  return f(0.0f, 0.0f);
+}
+
+CkptView view(const void* ckpt, int64_t rows, int64_t cols) {
+  const CkptLayout l = ckpt_layout(rows, cols);
+  return CkptView{(uint8_t*)ckpt, (uint8_t*)ckpt + l.exps, l.pitch};
+}
+
+}  // namespace
+
+// Workgroups of the backward pass, one row of partial sums each: a compute unit's worth while rows are
+// few, four of them once every workgroup has eight turns.
+int layer_norm_sum_rows(int64_t rows, int64_t cols) {
+  const int64_t turns = ceil_div(rows, slots_of(cols));
+  int64_t g = turns < 256 ? turns : 256;
+  const int64_t many = turns / 8 < kMaxSumRows ? turns / 8 : kMaxSumRows;
+  return (int)(many > g ? many : g);
+}
+
+hipError_t launch_layer_norm(const NormForward& a, hipStream_t s) {
+  return with_lanes(a.cols, [&](auto t, auto nv) {
+    return with_types(a.x_type, a.y_type, [&](auto tx, auto ty) {
+      constexpr int T = decltype(t)::value, NV = decltype(nv)::value;
+      using TX = decltype(tx);
+      using TY = decltype(ty);
+      const dim3 grid((unsigned)ceil_div(a.rows, kSlots<T>)), block(256);
+      if (a.ckpt) layer_norm_kernel<T, NV, TX, TY, true><<<grid, block, 0, s>>>(a, view(a.ckpt, a.rows, a.cols));
+      else layer_norm_kernel<T, NV, TX, TY, false><<<grid, block, 0, s>>>(a, CkptView{});
+      return hipGetLastError();
+    });
+  });
+}
+
+hipError_t launch_layer_norm_grad(const NormBackward& a, hipStream_t s) {
+  return with_lanes(a.cols, [&](auto t, auto nv) {
+    return with_types(a.x_type, a.y_type, [&](auto tx, auto ty) {
+      constexpr int T = decltype(t)::value, NV = decltype(nv)::value;
+      using TX = decltype(tx);
+      using TY = decltype(ty);
+      const dim3 grid((unsigned)layer_norm_sum_rows(a.rows, a.cols)), block(256);
+      if (a.ckpt) layer_norm_grad_kernel<T, NV, TX, TY, true><<<grid, block, 0, s>>>(a, view(a.ckpt, a.rows, a.cols));
+      else layer_norm_grad_kernel<T, NV, TX, TY, false><<<grid, block, 0, s>>>(a, CkptView{});
+      return hipGetLastError();
+    });
+  });
+}
+
+}  // namespace hot

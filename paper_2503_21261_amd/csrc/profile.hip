@@ -49,7 +49,9 @@ void stage_end(int stage, hipStream_t s) {
 const char* const kStageNames[HOT_NUM_STAGES] = {
     "gx_and_gw_igemm", "act_col_absmax", "act_col_quant", "w_col_absmax",  "w_col_quant",
     "gy_row_quant",  "gy_row_absmax",  "gy_row_quant2", "gx_igemm",      "gyT_col_absmax",
-    "gyT_col_quant", "gw_igemm",       "w_and_gy_row_quant", "gy_fused_absmax", "gy_fused_quant"};
+    "gyT_col_quant", "gw_igemm",       "w_and_gy_row_quant", "gy_fused_absmax", "gy_fused_quant",
+    "checkpoint_write", "checkpoint_read", "activation", "activation_grad", "layer_norm", "layer_norm_grad",
+    "column_sums", "linear_operands", "linear"};
 
 }  // namespace hot
 
