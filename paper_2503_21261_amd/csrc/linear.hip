@@ -5,6 +5,9 @@
 // LDS, in order.  A lane loads 16 consecutive bytes of a row; bfloat16 rows feed v_mfma_f32_16x16x32_bf16, fp32 rows
 // four v_mfma_f32_16x16x4_f32, whose products and sums are plain fp32.  The weight is the first operand, so that a
 // lane's accumulators are four consecutive outputs of a token.
+#include <atomic>
+#include <utility>
+
 #include "block_host.h"
 #include "linear_device.h"
 
@@ -139,7 +142,9 @@ __global__ __launch_bounds__(64 * kWaves) void linear_rows_kernel(const T* x, co
         v[e + 4] += b[e];
       }
     }
-    linear_finish8<TY>(out, m0 + t, n0 + c, out.O - n0 - c, v);
+    float b[8];
+    load_bias8(out, n0 + c, out.O - n0 - c, b);
+    linear_finish8<TY>(out, m0 + t, n0 + c, out.O - n0 - c, b, v);
   }
 }
 
@@ -158,6 +163,345 @@ hipError_t rows_typed(const LinearForward& a, const LinearOut& o, hipStream_t s)
   return go(std::integral_constant<int, 4>{});
 }
 
+// ---- many rows -------------------------------------------------------------------------------------
+// linear_tile_kernel: BM tokens x BN outputs a workgroup, both operands through LDS.  Operand rows are K-contiguous
+// and a whole number of 64-byte pieces; a stage is one piece of every row of the tile:
+//   bfloat16: 32 elements (rows of x and w as they are where I % 32 == 0, else a padded copy);
+//   fp32: 16 elements as two fp16 parts, [16 high | 16 low], of the row scaled by a power of two so that its largest
+//   value lies in [2^14, 2^15): x = high + low to 22 bits (values down to 2^-17 of the row's largest keep them, smaller
+//   ones keep 2^-39 of it), and x.w = high.high + high.low + low.high with 2^-22 left out.  Three matrix instructions
+//   of fp16 in place of eight of fp32 (v_mfma_f32_32x32x2_f32) per 16 elements.
+// Pieces go from memory to LDS without registers (buffer_load ... lds), four stages deep, so that three are on their
+// way while one is worked on.  LDS holds a row's four 16-byte chunks at chunk ^ (row / 2 % 4): eight rows that read
+// the same chunk hit different banks.  As a load writes 64 consecutive chunks, it is the lanes' sources that are permuted.
+// A wave reads the fragments of a stage's second half under the first half's matrix instructions, then meets the others at a
+// barrier, behind which the next stage is complete and this stage's buffer free, and reads the next stage's first
+// half under the second's.  The weight is the matrix instructions' first operand, so that accumulators are runs of four
+// outputs of a token; they leave through LDS, a wave's 32 tokens at a time, as runs of eight outputs a lane.
+typedef float v16f __attribute__((ext_vector_type(16)));
+typedef _Float16 v8h __attribute__((ext_vector_type(8)));
+typedef int v4i __attribute__((ext_vector_type(4)));
+
+// Compile-time loop: f(integral_constant<int, 0>) ... f(integral_constant<int, N - 1>).
+template <int... Is, class F>
+__device__ __forceinline__ void static_for_impl(std::integer_sequence<int, Is...>, F&& f) {
+  (f(std::integral_constant<int, Is>{}), ...);
+}
+template <int N, class F>
+__device__ __forceinline__ void static_for(F&& f) {
+  static_for_impl(std::make_integer_sequence<int, N>{}, static_cast<F&&>(f));
+}
+
+// 16 bytes a lane, at byte offset `lane_off` + `off` of the descriptor, to 1024 consecutive bytes of LDS (`to`: the same in
+// all lanes).  Counted by vmcnt; the caller waits.
+using rsrc_t = decltype(__builtin_amdgcn_make_buffer_rsrc((void*)nullptr, 0, 0, 0));
+__device__ __forceinline__ void load_to_lds(rsrc_t from, uint8_t* to, int lane_off, int off) {
+#if defined(__HIP_DEVICE_COMPILE__)   // the host's pass does not know gfx950's 16-byte form
+  __builtin_amdgcn_raw_ptr_buffer_load_lds(from, (__attribute__((address_space(3))) void*)to, 16, lane_off, off, 0, 0);
+#endif
+}
+
+struct TileArgs {
+  const uint8_t *x, *w;       // operand rows
+  int64_t pitch;              // bytes of one, a multiple of 64
+  const int *ex, *ew;         // fp32: exponents of the rows' scales
+  int tiles_m, tiles_n;
+  LinearOut out;
+};
+
+constexpr int kStages = 4, kPiece = 64;
+
+template <int BM, int BN, int WM, int WN>
+constexpr int kTileLds = kStages * (BM + BN) * kPiece > (BM / WM) * (BN / WN) * 32 * (WN + 4) * 4
+                             ? kStages * (BM + BN) * kPiece : (BM / WM) * (BN / WN) * 32 * (WN + 4) * 4;
+
+template <int BM, int BN, int WM, int WN, bool SPLIT, class TY>
+__global__ __launch_bounds__(64 * (BM / WM) * (BN / WN), 2) void linear_tile_kernel(const TileArgs g) {
+  constexpr int WAVES_M = BM / WM, WAVES = WAVES_M * (BN / WN);
+  constexpr int TM = WM / 32, TN = WN / 32;
+  constexpr int XL = BM / 16 / WAVES, WL = BN / 16 / WAVES;   // loads of a wave and stage: 16 rows each
+  static_assert(BM % (16 * WAVES) == 0 && BN % (16 * WAVES) == 0, "loads");
+  constexpr int STAGE = (BM + BN) * kPiece;
+  extern __shared__ __align__(16) uint8_t smem[];
+  const int tid = (int)threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  int tm, tn;
+  tile_of((int)blockIdx.x, g.tiles_m, g.tiles_n, tm, tn);
+  const int64_t m0 = (int64_t)tm * BM;
+  const int n0 = tn * BN;
+  const int nk = (int)(g.pitch / kPiece);
+
+  // Sources of the wave's loads: row lane / 4 of 16, the chunk that belongs where the lane writes.
+  const int64_t rows_x = g.out.L - m0 < BM ? g.out.L - m0 : BM, rows_w = g.out.O - n0 < BN ? g.out.O - n0 : BN;
+  const auto rx = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(g.x) + m0 * g.pitch, 0, (int)(rows_x * g.pitch), 0x00027000);
+  const auto rw = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(g.w) + (int64_t)n0 * g.pitch, 0, (int)(rows_w * g.pitch), 0x00027000);
+  int off_x[XL], off_w[WL];
+  auto source = [&](int row, int64_t rows) {
+    const int chunk = (lane & 3) ^ ((row >> 1) & 3);
+    const int r = row < rows ? row : (int)rows - 1;     // rows past the last repeat it and are not stored
+    return r * (int)g.pitch + chunk * 16;
+  };
+#pragma unroll
+  for (int i = 0; i < XL; ++i) off_x[i] = source((wave * XL + i) * 16 + (lane >> 2), rows_x);
+#pragma unroll
+  for (int i = 0; i < WL; ++i) off_w[i] = source((wave * WL + i) * 16 + (lane >> 2), rows_w);
+  auto load_one = [&](int kt, auto ec) {
+    constexpr int e = decltype(ec)::value;
+    const int at = (kt < nk ? kt : nk - 1) * kPiece;    // past the end: a stage again, into a buffer that nobody reads
+    uint8_t* const b = smem + (kt & (kStages - 1)) * STAGE;
+    if constexpr (e < XL) load_to_lds(rx, b + (wave * XL + e) * 1024, off_x[e], at);
+    else load_to_lds(rw, b + BM * kPiece + (wave * WL + e - XL) * 1024, off_w[e - XL], at);
+  };
+  auto load_stage = [&](int kt) { static_for<XL + WL>([&](auto e) { load_one(kt, e); }); };
+
+  const int wm0 = wave % WAVES_M * WM, wn0 = wave / WAVES_M * WN;
+  int off_half[2];
+#pragma unroll
+  for (int h = 0; h < 2; ++h) off_half[h] = (lane & 31) * kPiece + 16 * ((2 * h + (lane >> 5)) ^ (((lane & 31) >> 1) & 3));
+  struct Frags {
+    v4i x[TM], w[TN];
+  };
+  constexpr int NM = TM * TN, NR = TM + TN, NL = XL + WL;
+  auto read_one = [&](int kt, int h, Frags& f, auto ec) {
+    constexpr int e = decltype(ec)::value;
+    const uint8_t* const b = smem + (kt & (kStages - 1)) * STAGE + off_half[h];
+    if constexpr (e < TM) f.x[e] = *(const v4i*)(b + (wm0 + e * 32) * kPiece);
+    else f.w[e - TM] = *(const v4i*)(b + (BM + wn0 + (e - TM) * 32) * kPiece);
+  };
+  v16f acc[TM][TN];
+#pragma unroll
+  for (int i = 0; i < TM; ++i)
+#pragma unroll
+    for (int j = 0; j < TN; ++j)
+#pragma unroll
+      for (int v = 0; v < 16; ++v) acc[i][j][v] = 0.0f;
+  auto multiply_one = [&](const v4i& w, const v4i& x, v16f& c) {
+    if constexpr (SPLIT) c = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(v8h, w), __builtin_bit_cast(v8h, x), c, 0, 0, 0);
+    else c = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(v8bf, w), __builtin_bit_cast(v8bf, x), c, 0, 0, 0);
+  };
+  // COUNT matrix instructions with EVENTS memory instructions pinned between the first of them: the compiler would
+  // gather the reads in front of their use.  The last SLACK matrix instructions have none, so that the reads are there
+  // when the next ones want them.
+  auto interleave = [&](auto count, auto events, auto&& mfma, auto&& event) {
+    constexpr int COUNT = decltype(count)::value, EVENTS = decltype(events)::value, SLACK = COUNT > 4 ? 3 : 1, OVER = COUNT - SLACK;
+    __builtin_amdgcn_sched_barrier(0);
+    static_for<COUNT>([&](auto qc) {
+      constexpr int q = decltype(qc)::value;
+      constexpr int E0 = q < OVER ? (q * EVENTS + OVER - 1) / OVER : EVENTS, E1 = q + 1 < OVER ? ((q + 1) * EVENTS + OVER - 1) / OVER : EVENTS;
+      static_for<E1 - E0>([&](auto dc) { event(std::integral_constant<int, E0 + decltype(dc)::value>{}); });
+      mfma(qc);
+      __builtin_amdgcn_sched_barrier(0);
+    });
+  };
+  // This wave's loads of all but the last two stages asked for have arrived, and its LDS reads are done; then everybody's.
+  auto meet = [&]() {
+    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" : : "n"(2 * NL) : "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+  };
+  // Stage kt: `a` holds its first half; `next` receives that of the stage behind it (behind the last: a repeated one, not used).
+  using std::integral_constant;
+  Frags b;
+  auto stage = [&](int kt, Frags& a, Frags& next) {
+    interleave(integral_constant<int, NM>{}, integral_constant<int, NR>{},
+               [&](auto q) { multiply_one(a.w[q % TN], a.x[q / TN], acc[q / TN][q % TN]); }, [&](auto e) { read_one(kt, 1, b, e); });
+    meet();
+    interleave(integral_constant<int, SPLIT ? 2 * NM : NM>{}, integral_constant<int, NL + NR>{},
+               [&](auto q) {
+                 constexpr int p = decltype(q)::value % NM, i = p / TN, j = p % TN;
+                 if constexpr (!SPLIT) multiply_one(b.w[j], b.x[i], acc[i][j]);
+                 else if constexpr (decltype(q)::value < NM) multiply_one(a.w[j], b.x[i], acc[i][j]);
+                 else multiply_one(b.w[j], a.x[i], acc[i][j]);
+               },
+               [&](auto e) {
+                 if constexpr (decltype(e)::value < NL) load_one(kt + 4, e);
+                 else read_one(kt + 1, 0, next, integral_constant<int, decltype(e)::value - NL>{});
+               });
+  };
+
+#pragma unroll
+  for (int k = 0; k < 3; ++k) load_stage(k);
+  meet();
+  load_stage(3);
+  Frags a, a2;
+  static_for<NR>([&](auto e) { read_one(0, 0, a, e); });
+  int kt = 0;
+  for (; kt + 1 < nk; kt += 2) {
+    stage(kt, a, a2);
+    stage(kt + 1, a2, a);
+  }
+  if (kt < nk) stage(kt, a, a2);
+  asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+
+  constexpr int PITCH = WN + 4, CH = WN / 8, RPI = 64 / CH;   // tokens a wave finishes at a time
+  float* const strip = (float*)smem + wave * 32 * PITCH;
+  const int c = n0 + wn0 + lane % CH * 8, n = g.out.O - c;
+  float bias[8];
+  load_bias8(g.out, c, n, bias);
+  int ew[8];
+  if constexpr (SPLIT) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) ew[e] = g.ew[c + e < g.out.O ? c + e : g.out.O - 1];
+  }
+#pragma unroll
+  for (int i = 0; i < TM; ++i) {
+    // accumulator register v of a 32 x 32 tile: output 8 (v / 4) + 4 (lane / 32) + v % 4, token lane % 32
+#pragma unroll
+    for (int j = 0; j < TN; ++j)
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        v4f part;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) part[r] = acc[i][j][4 * q + r];
+        *(v4f*)&strip[(lane & 31) * PITCH + j * 32 + 8 * q + 4 * (lane >> 5)] = part;
+      }
+    __builtin_amdgcn_wave_barrier();
+#pragma unroll 2
+    for (int t0 = 0; t0 < 32; t0 += RPI) {
+      const int t = t0 + lane / CH;
+      const int64_t row = m0 + wm0 + i * 32 + t;
+      const float* const p = &strip[t * PITCH + lane % CH * 8];
+      const v4f lo = *(const v4f*)p, hi = *(const v4f*)(p + 4);
+      float v[8];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        v[e] = lo[e];
+        v[e + 4] = hi[e];
+      }
+      if (row < g.out.L) {
+        if constexpr (SPLIT) {
+          const int ex = g.ex[row];
+#pragma unroll
+          for (int e = 0; e < 8; ++e) v[e] = __builtin_ldexpf(v[e], ex + ew[e]);
+        }
+        linear_finish8<TY>(g.out, row, c, n, bias, v);
+      }
+    }
+    __builtin_amdgcn_wave_barrier();
+  }
+}
+
+// Operand rows of the fp32 product: row r of the L + O rows of x and w, scaled by 2^(14 - e), e the exponent of its largest value,
+// as [16 high | 16 low] pieces; exps[r] = e - 14.  A wave takes a row, twice: the second read comes from the caches.
+// Padded columns are zero.
+__global__ __launch_bounds__(256) void linear_split_kernel(const float* x, const float* w, int64_t L, int64_t O, int64_t I, int64_t pitch,
+                                                           uint8_t* px, uint8_t* pw, int* exps) {
+  const int lane = (int)threadIdx.x & 63;
+  const int64_t r = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+  if (r >= L + O) return;
+  const float* const src = r < L ? x + r * I : w + (r - L) * I;
+  uint8_t* const dst = r < L ? px + r * pitch : pw + (r - L) * pitch;
+  uint32_t top = 0;
+#pragma unroll 4
+  for (int64_t c = lane * 8; c < I; c += 512) {
+    float v[8];
+    load_values(src + c, (int)(I - c < 8 ? I - c : 8), v);
+    top = max(top, magnitude8(v));
+  }
+#pragma unroll
+  for (int m = 1; m < 64; m *= 2) top = max(top, (uint32_t)__shfl_xor((int)top, m));
+  // frexp's exponent is right for subnormal rows too; infinities and NaNs stay what they are under any scale
+  const int e = top >= 0x7F800000u || top == 0 ? 0 : ilogbf(__uint_as_float(top));
+  if (lane == 0) exps[r] = e - 14;
+  const int64_t padded = pitch / 4;
+#pragma unroll 2
+  for (int64_t c = lane * 8; c < padded; c += 512) {
+    float v[8];
+    const int64_t n = I - c;
+    load_values(src + c, (int)(n < 0 ? 0 : n < 8 ? n : 8), v);
+    v8h hi, lo;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const float s = __builtin_ldexpf(v[i], 14 - e);
+      hi[i] = (_Float16)s;
+      lo[i] = (_Float16)(s - (float)hi[i]);
+    }
+    uint8_t* const p = dst + (c >> 4) * 64 + (c & 8) * 2;
+    *(v8h*)p = hi;
+    *(v8h*)(p + 32) = lo;
+  }
+}
+
+// Rows of bfloat16 operands whose width is no multiple of 32, padded with zeros.
+__global__ __launch_bounds__(256) void linear_pad_kernel(const bf16* x, const bf16* w, int64_t L, int64_t O, int64_t I, int64_t pitch,
+                                                         uint8_t* px, uint8_t* pw) {
+  const int lane = (int)threadIdx.x & 63;
+  const int64_t r = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+  if (r >= L + O) return;
+  const bf16* const src = r < L ? x + r * I : w + (r - L) * I;
+  uint8_t* const dst = r < L ? px + r * pitch : pw + (r - L) * pitch;
+#pragma unroll 4
+  for (int64_t c = lane * 8; c < pitch / 2; c += 512) {
+    const int64_t n = I - c;
+    const Raw8<bf16> v = load8(src + c, (int)(n < 0 ? 0 : n < 8 ? n : 8));
+    *(h8_any*)(dst + c * 2) = v.a;
+  }
+}
+
+// What the tile kernel needs besides its operands: packed rows (fp32, or a width that is no multiple of 32) and the exponents.
+struct TileLayout {
+  int64_t pitch;
+  bool packed;
+  size_t w, exps, total;     // x's rows come first
+};
+TileLayout tile_layout(hot_type type, int64_t L, int64_t O, int64_t I) {
+  TileLayout t;
+  t.packed = type == HOT_F32 || I % 32 != 0;
+  t.pitch = type == HOT_F32 ? round_up(I, 16) * 4 : round_up(I, 32) * 2;
+  t.w = t.packed ? (size_t)round_up(L * t.pitch, 256) : 0;
+  t.exps = t.w + (t.packed ? (size_t)round_up(O * t.pitch, 256) : 0);
+  t.total = t.exps + (type == HOT_F32 ? (size_t)(L + O) * 4 : 0);
+  return t;
+}
+
+bool use_tiles(hot_type type, int64_t L, int64_t, int64_t I) {
+  const int64_t pitch = type == HOT_F32 ? round_up(I, 16) * 4 : round_up(I, 32) * 2;
+  return L > 64 && pitch * 256 < (1ll << 31);     // a tile's rows within the reach of a buffer descriptor
+}
+
+template <int BM, int BN, int WM, int WN, bool SPLIT, class TY>
+hipError_t tiles_sized(TileArgs g, hipStream_t s) {
+  g.tiles_m = (int)ceil_div(g.out.L, BM);
+  g.tiles_n = (int)ceil_div(g.out.O, BN);
+  constexpr int LDS = kTileLds<BM, BN, WM, WN>;
+  auto kern = linear_tile_kernel<BM, BN, WM, WN, SPLIT, TY>;
+  static std::atomic<bool> attr_set{false};  // per instantiation; setting it twice is harmless
+  if (!attr_set.load(std::memory_order_acquire)) {
+    if (const hipError_t e = hipFuncSetAttribute((const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize, LDS); e != hipSuccess) return e;
+    attr_set.store(true, std::memory_order_release);
+  }
+  kern<<<dim3((unsigned)((int64_t)g.tiles_m * g.tiles_n)), dim3(64 * (BM / WM) * (BN / WN)), LDS, s>>>(g);
+  return hipGetLastError();
+}
+
+template <class T, class TY>
+hipError_t tiles_typed(const LinearForward& a, const LinearOut& o, hipStream_t s) {
+  constexpr bool SPLIT = sizeof(T) == 4;
+  const TileLayout t = tile_layout(a.type, a.L, a.O, a.I);
+  TileArgs g{(const uint8_t*)a.x, (const uint8_t*)a.w, t.pitch, nullptr, nullptr, 0, 0, o};
+  if (t.packed) {
+    uint8_t* const px = (uint8_t*)a.ws;
+    uint8_t* const pw = px + t.w;
+    int* const exps = (int*)(px + t.exps);
+    const dim3 grid((unsigned)ceil_div(a.L + a.O, 4)), block(256);
+    stage_begin(kStLinearOperands, s);
+    if constexpr (SPLIT) linear_split_kernel<<<grid, block, 0, s>>>((const float*)a.x, (const float*)a.w, a.L, a.O, a.I, t.pitch, px, pw, exps);
+    else linear_pad_kernel<<<grid, block, 0, s>>>((const bf16*)a.x, (const bf16*)a.w, a.L, a.O, a.I, t.pitch, px, pw);
+    stage_end(kStLinearOperands, s);
+    if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+    g.x = px;
+    g.w = pw;
+    g.ex = exps;
+    g.ew = exps + a.L;
+  }
+  stage_begin(kStLinear, s);
+  const hipError_t e = ceil_div(a.L, 256) * ceil_div(a.O, 256) >= 192 ? tiles_sized<256, 256, 64, 128, SPLIT, TY>(g, s)
+                                                                     : tiles_sized<128, 128, 64, 64, SPLIT, TY>(g, s);
+  stage_end(kStLinear, s);
+  return e;
+}
+
 template <class T, class TY>
 hipError_t linear_typed(const LinearForward& a, hipStream_t s) {
   LinearOut o{a.bias, a.residual, a.y, CkptView{}, a.L, (int)a.O, a.fn};
@@ -165,6 +509,7 @@ hipError_t linear_typed(const LinearForward& a, hipStream_t s) {
     const CkptLayout l = ckpt_layout(a.L, a.O);
     o.k = CkptView{(uint8_t*)a.ckpt, (uint8_t*)a.ckpt + l.exps, l.pitch};
   }
+  if (use_tiles(a.type, a.L, a.O, a.I)) return tiles_typed<T, TY>(a, o, s);
   // 16 outputs a workgroup where that is what fills the card; a checkpoint's groups need 32
   stage_begin(kStLinear, s);
   const hipError_t e = a.ckpt || ceil_div(a.O, 32) * ceil_div(a.L, 64) >= 512 ? rows_typed<T, TY, 2>(a, o, s) : rows_typed<T, TY, 1>(a, o, s);
@@ -174,7 +519,9 @@ hipError_t linear_typed(const LinearForward& a, hipStream_t s) {
 
 }  // namespace
 
-size_t linear_scratch_bytes(hot_type, int64_t, int64_t, int64_t) { return 0; }
+size_t linear_scratch_bytes(hot_type type, int64_t L, int64_t O, int64_t I) {
+  return use_tiles(type, L, O, I) ? tile_layout(type, L, O, I).total : 0;
+}
 
 hipError_t launch_linear(const LinearForward& a, hipStream_t s) {
   if (a.type == HOT_F32) return linear_typed<float, float>(a, s);

@@ -29,22 +29,26 @@ __device__ __forceinline__ void act_any(int fn, float (&v)[8]) {
   }
 }
 
-// v: x.w^T at (row, c .. c + 7); n = how many of the eight columns exist (may be 0 or less, for a lane of a checkpoint
-// group past the last column, whose codes are zero).  With a checkpoint the four lanes of a group call this together.
-template <class TY>
-__device__ __forceinline__ void linear_finish8(const LinearOut& o, int64_t row, int c, int n, float (&v)[8]) {
-  if (o.bias) {
-    float b[8] = {};
-    if (n > 0) load_values(o.bias + c, n, b);
+// Bias of eight outputs (0 past the last one).
+__device__ __forceinline__ void load_bias8(const LinearOut& o, int c, int n, float (&b)[8]) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] += b[i];
-  }
+  for (int i = 0; i < 8; ++i) b[i] = 0.0f;
+  if (o.bias && n > 0) load_values(o.bias + c, n, b);
+}
+
+// v: x.w^T at (row, c .. c + 7), b: its bias; n = how many of the eight columns exist (may be 0 or less, for a lane of a
+// checkpoint group past the last column, whose codes are zero).  With a checkpoint the four lanes of a group call
+// this together.
+template <class TY>
+__device__ __forceinline__ void linear_finish8(const LinearOut& o, int64_t row, int c, int n, const float (&b)[8], float (&v)[8]) {
+#pragma unroll
+  for (int i = 0; i < 8; ++i) v[i] += b[i];
   if (o.k.codes) {
     if (n < 8) {
 #pragma unroll
       for (int i = 0; i < 8; ++i) v[i] = i < n ? v[i] : 0.0f;
     }
-    ckpt_store8(o.k, row * o.k.pitch + c, v);
+    if (c < (int)o.k.pitch) ckpt_store8(o.k, row * o.k.pitch + c, v);
   }
   act_any(o.fn, v);
   if (n <= 0) return;
@@ -56,6 +60,18 @@ __device__ __forceinline__ void linear_finish8(const LinearOut& o, int64_t row, 
     for (int i = 0; i < 8; ++i) v[i] += r[i];
   }
   store8((TY*)o.y + at, v, n);
+}
+
+// Workgroup -> tile: workgroups go to the eight XCDs in turn, each with an L2 of its own.  Ids are dealt so that an XCD
+// walks a contiguous run of tiles, in bands of eight tile rows, tile row fastest: the tiles it works on at a time
+// share their operands in its L2.
+__device__ __forceinline__ void tile_of(int id, int tiles_m, int tiles_n, int& tm, int& tn) {
+  const int total = tiles_m * tiles_n, per_xcd = total / 8;
+  const int p = id < per_xcd * 8 ? (id % 8) * per_xcd + id / 8 : id;
+  const int band = 8 * tiles_n, first = p / band * 8, in = p % band;
+  const int rows = tiles_m - first < 8 ? tiles_m - first : 8;
+  tm = first + in % rows;
+  tn = in / rows;
 }
 
 }  // namespace hot

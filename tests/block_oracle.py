@@ -153,7 +153,9 @@ def product(x, w, bias):
     size = x.abs() @ w.abs().t().contiguous()
     top = x.abs().amax(1, keepdim=True), w.abs().amax(1, keepdim=True)
     tiny = 2.0 ** -38 * (top[0] * w.abs().sum(1)[None] + x.abs().sum(1, keepdim=True) * top[1].t())
-    d = size * (3 * 2.0 ** -22 + (x.shape[1] / 2 + 64) * U) + tiny
+    # no fp32 result is nearer than 2^-150, half the smallest fp32 number, however it was computed: a product and an addition for
+    # each of the I terms, and the result itself, may each be off by that where they fall below 2^-126
+    d = size * (3 * 2.0 ** -22 + (x.shape[1] / 2 + 64) * U) + tiny + (2 * x.shape[1] + 1) * 2.0 ** -150
     if bias is not None:
         z = z + bias
         d = d + U * z.abs()

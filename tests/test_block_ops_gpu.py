@@ -337,6 +337,43 @@ def test_linear_epilogues(fn, tx, ty):
                 run_linear(L, 200, 160, tx, ty, fn, True, residual, kept, seed=L)
 
 
+@pytest.mark.parametrize("tx,ty", [(F32, F32), (BF16, BF16), (BF16, F32)])
+@pytest.mark.parametrize("L,O,I", [(3500, 3600, 100), (3590, 3585, 33), (66, 70, 1), (66, 70, 16), (66, 70, 17), (66, 70, 32), (66, 70, 48),
+                                   (66, 70, 64), (129, 129, 80), (1000, 31, 96)])
+def test_linear_tiles(L, O, I, tx, ty):
+    run_linear(L, O, I, tx, ty, seed=L + I)
+    run_linear(L, O, I, tx, ty, fn="silu", bias=False, residual=True, kept=True, seed=L + I + 1)
+
+
+@pytest.mark.parametrize("L", [7, 90])
+def test_linear_rows_of_any_magnitude(L):
+    """Each row of either operand has a scale of its own, from the smallest to the largest; rows of zeros; within a row,
+    values far below its largest."""
+
+    def scale(x, w):
+        x *= (2.0 ** torch.linspace(-62, 60, x.shape[0]).round())[:, None]
+        w *= (2.0 ** torch.linspace(-62, 60, w.shape[0]).round())[:, None]
+        x[:, ::3] *= 2.0 ** -20
+        x[3], w[5] = 0.0, 0.0
+        x[4] = 0.0
+        x[4, 7] = 1e-40
+
+    run_linear(L, 77, 200, F32, F32, bias=False, scale=scale)
+
+
+def test_linear_rows_with_an_infinity_or_nan_stay_alone():
+    for tx in (F32, BF16):
+        for L in (6, 100):
+            x, w = rand((L, 96), 1, tx), rand((80, 96), 2, tx)
+            x[2, 5], x[4, 90], w[7, 1] = float("nan"), float("inf"), float("nan")
+            y = torch.empty((L, 80), dtype=tx, device="cuda")
+            hot.hot_linear_forward(x.cuda(), w.cuda(), y, hot.alloc_linear_workspace(tx, L, 80, 96))
+            bad = ~torch.isfinite(y.cpu().float())
+            want = torch.zeros(L, 80, dtype=torch.bool)
+            want[2], want[4], want[:, 7] = True, True, True
+            assert torch.equal(bad, want)
+
+
 # ---- as they are called ----------------------------------------------------------------------------------------------------
 
 def test_calls_on_another_stream_and_replayed():
