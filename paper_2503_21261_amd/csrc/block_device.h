@@ -129,11 +129,12 @@ __device__ __forceinline__ uint32_t magnitude8(const float (&v)[8]) {
   for (int i = 0; i < 8; ++i) m = max(m, __float_as_uint(v[i]) & 0x7FFFFFFFu);
   return m;
 }
-// Eight codes under 1 / step.  A largest value near the type's end (e held at 254) would round to 128.
+// Eight codes under 1 / step: the product is exact, and the addition of 1.5 x 2^23 rounds it to a whole number, half to even, in the
+// sum's low bits, whose lowest byte is the code.
 __device__ __forceinline__ uint2 encode8(const float (&v)[8], float inverse) {
   int c[8];
 #pragma unroll
-  for (int i = 0; i < 8; ++i) c[i] = (int)fminf(fmaxf(rintf(v[i] * inverse), -127.0f), 127.0f);
+  for (int i = 0; i < 8; ++i) c[i] = __float_as_int(fmaf(v[i], inverse, 12582912.0f));
   return make_uint2(pack4_codes8(c[0], c[1], c[2], c[3]), pack4_codes8(c[4], c[5], c[6], c[7]));
 }
 __device__ __forceinline__ void decode8(uint2 codes, float step, float (&v)[8]) {
@@ -153,7 +154,15 @@ struct CkptView {
 // `at`: row * pitch + column, a multiple of 8; called by all four lanes of a group together.
 __device__ __forceinline__ void ckpt_store8(const CkptView& k, int64_t at, const float (&v)[8]) {
   const uint32_t e = ckpt_exponent(quad_max(magnitude8(v)));
-  *(uint2*)(k.codes + at) = encode8(v, ckpt_inverse(e));
+  const float inverse = ckpt_inverse(e);
+  if (e == 254u) {   // at the type's end, where the next step is missing: 127.5 steps and more are held at 127
+    float w[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) w[i] = fminf(fmaxf(v[i], -0x1.fcp+127f), 0x1.fcp+127f);
+    *(uint2*)(k.codes + at) = encode8(w, inverse);
+  } else {
+    *(uint2*)(k.codes + at) = encode8(v, inverse);
+  }
   if ((at & (kCkGroup - 1)) == 0) k.exps[at / kCkGroup] = (uint8_t)e;
 }
 
@@ -188,7 +197,7 @@ __device__ __forceinline__ float act_value(float x) {
   if constexpr (FN == HOT_ACT_RELU) return x < 0.0f ? 0.0f : x;
   else if constexpr (FN == HOT_ACT_GELU) {
     const float a = fabsf(x);
-    return (x < 0.0f ? 0.0f : x) - a * normal_tail(a, gauss_of(x));
+    return fmaf(-a, normal_tail(a, gauss_of(x)), fmaxf(x, 0.0f));
   } else if constexpr (FN == HOT_ACT_GELU_TANH) {
     const float xc = clamp30(x);
     return x * sigmoid_of(gelu_tanh_arg(xc));

@@ -206,47 +206,56 @@ struct TileArgs {
   int64_t pitch;              // bytes of one, a multiple of 64
   const int *ex, *ew;         // fp32: exponents of the rows' scales
   int tiles_m, tiles_n;
+  int whole;                  // tiles with a workgroup each; every other one has `slices`, which leave their sums in
+  int slices;                 // images[tile - whole][slice], added by linear_combine_kernel
+  float* images;
   LinearOut out;
 };
 
-constexpr int kStages = 4, kPiece = 64;
+constexpr int kStages = 2, kPiece = 128;
 
 template <int BM, int BN, int WM, int WN>
 constexpr int kTileLds = kStages * (BM + BN) * kPiece > (BM / WM) * (BN / WN) * 32 * (WN + 4) * 4
                              ? kStages * (BM + BN) * kPiece : (BM / WM) * (BN / WN) * 32 * (WN + 4) * 4;
 
 template <int BM, int BN, int WM, int WN, bool SPLIT, class TY>
-__global__ __launch_bounds__(64 * (BM / WM) * (BN / WN), 2) void linear_tile_kernel(const TileArgs g) {
+__global__ __launch_bounds__(64 * (BM / WM) * (BN / WN), WM * WN > 64 * 128 ? 1 : 2) void linear_tile_kernel(const TileArgs g) {
   constexpr int WAVES_M = BM / WM, WAVES = WAVES_M * (BN / WN);
   constexpr int TM = WM / 32, TN = WN / 32;
-  constexpr int XL = BM / 16 / WAVES, WL = BN / 16 / WAVES;   // loads of a wave and stage: 16 rows each
-  static_assert(BM % (16 * WAVES) == 0 && BN % (16 * WAVES) == 0, "loads");
+  constexpr int XL = BM / 8 / WAVES, WL = BN / 8 / WAVES;   // loads of a wave and stage: 8 rows each
+  static_assert(BM % (8 * WAVES) == 0 && BN % (8 * WAVES) == 0, "loads");
   constexpr int STAGE = (BM + BN) * kPiece;
   extern __shared__ __align__(16) uint8_t smem[];
   const int tid = (int)threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  // A workgroup of a whole tile, or of a slice of one: slices of a tile are neighbours in dispatch order but for their XCD.
+  const int rest = g.tiles_m * g.tiles_n - g.whole, part = (int)blockIdx.x - g.whole;
+  const bool sliced = part >= 0;
+  const int z = sliced ? part / rest : 0, tail = sliced ? part % rest : 0;
   int tm, tn;
-  tile_of((int)blockIdx.x, g.tiles_m, g.tiles_n, tm, tn);
+  tile_at(sliced ? g.whole + tail : xcd_contiguous((int)blockIdx.x, g.whole), g.tiles_m, g.tiles_n, tm, tn);
   const int64_t m0 = (int64_t)tm * BM;
   const int n0 = tn * BN;
-  const int nk = (int)(g.pitch / kPiece);
+  const int stages = (int)(g.pitch / kPiece);
+  const int k_first = sliced ? (int)((int64_t)stages * z / g.slices) : 0;
+  const int nk = sliced ? (int)((int64_t)stages * (z + 1) / g.slices) - k_first : stages;
 
-  // Sources of the wave's loads: row lane / 4 of 16, the chunk that belongs where the lane writes.
+  // Sources of the wave's loads: row lane / 8 of 8, the chunk that belongs where the lane writes.
   const int64_t rows_x = g.out.L - m0 < BM ? g.out.L - m0 : BM, rows_w = g.out.O - n0 < BN ? g.out.O - n0 : BN;
   const auto rx = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(g.x) + m0 * g.pitch, 0, (int)(rows_x * g.pitch), 0x00027000);
   const auto rw = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(g.w) + (int64_t)n0 * g.pitch, 0, (int)(rows_w * g.pitch), 0x00027000);
   int off_x[XL], off_w[WL];
   auto source = [&](int row, int64_t rows) {
-    const int chunk = (lane & 3) ^ ((row >> 1) & 3);
+    const int chunk = (lane & 7) ^ (row & 7);
     const int r = row < rows ? row : (int)rows - 1;     // rows past the last repeat it and are not stored
     return r * (int)g.pitch + chunk * 16;
   };
 #pragma unroll
-  for (int i = 0; i < XL; ++i) off_x[i] = source((wave * XL + i) * 16 + (lane >> 2), rows_x);
+  for (int i = 0; i < XL; ++i) off_x[i] = source((wave * XL + i) * 8 + (lane >> 3), rows_x);
 #pragma unroll
-  for (int i = 0; i < WL; ++i) off_w[i] = source((wave * WL + i) * 16 + (lane >> 2), rows_w);
+  for (int i = 0; i < WL; ++i) off_w[i] = source((wave * WL + i) * 8 + (lane >> 3), rows_w);
   auto load_one = [&](int kt, auto ec) {
     constexpr int e = decltype(ec)::value;
-    const int at = (kt < nk ? kt : nk - 1) * kPiece;    // past the end: a stage again, into a buffer that nobody reads
+    const int at = (k_first + (kt < nk ? kt : nk - 1)) * kPiece;    // past the end: a stage again, into a buffer that nobody reads
     uint8_t* const b = smem + (kt & (kStages - 1)) * STAGE;
     if constexpr (e < XL) load_to_lds(rx, b + (wave * XL + e) * 1024, off_x[e], at);
     else load_to_lds(rw, b + BM * kPiece + (wave * WL + e - XL) * 1024, off_w[e - XL], at);
@@ -254,16 +263,16 @@ __global__ __launch_bounds__(64 * (BM / WM) * (BN / WN), 2) void linear_tile_ker
   auto load_stage = [&](int kt) { static_for<XL + WL>([&](auto e) { load_one(kt, e); }); };
 
   const int wm0 = wave % WAVES_M * WM, wn0 = wave / WAVES_M * WN;
-  int off_half[2];
+  int off_q[4];     // a quarter of a stage: chunks 2 q and 2 q + 1 of a row, one for each half of the lanes
 #pragma unroll
-  for (int h = 0; h < 2; ++h) off_half[h] = (lane & 31) * kPiece + 16 * ((2 * h + (lane >> 5)) ^ (((lane & 31) >> 1) & 3));
+  for (int q = 0; q < 4; ++q) off_q[q] = (lane & 31) * kPiece + 16 * ((2 * q + (lane >> 5)) ^ (lane & 7));
   struct Frags {
     v4i x[TM], w[TN];
   };
   constexpr int NM = TM * TN, NR = TM + TN, NL = XL + WL;
-  auto read_one = [&](int kt, int h, Frags& f, auto ec) {
+  auto read_one = [&](int kt, auto qc, Frags& f, auto ec) {
     constexpr int e = decltype(ec)::value;
-    const uint8_t* const b = smem + (kt & (kStages - 1)) * STAGE + off_half[h];
+    const uint8_t* const b = smem + (kt & (kStages - 1)) * STAGE + off_q[decltype(qc)::value];
     if constexpr (e < TM) f.x[e] = *(const v4i*)(b + (wm0 + e * 32) * kPiece);
     else f.w[e - TM] = *(const v4i*)(b + (BM + wn0 + (e - TM) * 32) * kPiece);
   };
@@ -292,58 +301,85 @@ __global__ __launch_bounds__(64 * (BM / WM) * (BN / WN), 2) void linear_tile_ker
       __builtin_amdgcn_sched_barrier(0);
     });
   };
-  // This wave's loads of all but the last two stages asked for have arrived, and its LDS reads are done; then everybody's.
+  // This wave's loads have arrived and its LDS reads are done; then everybody's.
   auto meet = [&]() {
-    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" : : "n"(2 * NL) : "memory");
+    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
   };
-  // Stage kt: `a` holds its first half; `next` receives that of the stage behind it (behind the last: a repeated one, not used).
   using std::integral_constant;
-  Frags b;
-  auto stage = [&](int kt, Frags& a, Frags& next) {
-    interleave(integral_constant<int, NM>{}, integral_constant<int, NR>{},
-               [&](auto q) { multiply_one(a.w[q % TN], a.x[q / TN], acc[q / TN][q % TN]); }, [&](auto e) { read_one(kt, 1, b, e); });
-    meet();
-    interleave(integral_constant<int, SPLIT ? 2 * NM : NM>{}, integral_constant<int, NL + NR>{},
+  Frags fa, fb, fc;
+  // Matrix instructions of one quarter (bfloat16) or of one half of the pair of parts (fp32), and what is fetched meanwhile.
+  auto whole = [&](Frags& f, auto events, auto&& event) {
+    interleave(integral_constant<int, NM>{}, events, [&](auto q) { multiply_one(f.w[q % TN], f.x[q / TN], acc[q / TN][q % TN]); }, event);
+  };
+  auto crossed = [&](Frags& high, Frags& low, auto events, auto&& event) {
+    interleave(integral_constant<int, 2 * NM>{}, events,
                [&](auto q) {
                  constexpr int p = decltype(q)::value % NM, i = p / TN, j = p % TN;
-                 if constexpr (!SPLIT) multiply_one(b.w[j], b.x[i], acc[i][j]);
-                 else if constexpr (decltype(q)::value < NM) multiply_one(a.w[j], b.x[i], acc[i][j]);
-                 else multiply_one(b.w[j], a.x[i], acc[i][j]);
+                 if constexpr (decltype(q)::value < NM) multiply_one(high.w[j], low.x[i], acc[i][j]);
+                 else multiply_one(low.w[j], high.x[i], acc[i][j]);
                },
-               [&](auto e) {
-                 if constexpr (decltype(e)::value < NL) load_one(kt + 4, e);
-                 else read_one(kt + 1, 0, next, integral_constant<int, decltype(e)::value - NL>{});
-               });
+               event);
   };
-
-#pragma unroll
-  for (int k = 0; k < 3; ++k) load_stage(k);
-  meet();
-  load_stage(3);
-  Frags a, a2;
-  static_for<NR>([&](auto e) { read_one(0, 0, a, e); });
-  int kt = 0;
-  for (; kt + 1 < nk; kt += 2) {
-    stage(kt, a, a2);
-    stage(kt + 1, a2, a);
+  const integral_constant<int, NR> reads;
+  const integral_constant<int, NL + NR> loads_and_reads;
+  const integral_constant<int, 0> q0;
+  const integral_constant<int, 1> q1;
+  const integral_constant<int, 2> q2;
+  const integral_constant<int, 3> q3;
+  load_stage(0);
+  load_stage(1);
+  asm volatile("s_waitcnt vmcnt(%0)" : : "n"(NL) : "memory");   // the first stage
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+  static_for<NR>([&](auto e) { read_one(0, q0, fa, e); });
+  for (int kt = 0; kt < nk; ++kt) {
+    // behind the last stage comes a repeated one, whose first quarter is read and not used
+    auto next = [&](Frags& f) {
+      return [&, kt](auto e) {
+        if constexpr (decltype(e)::value < NR) read_one(kt + 1, q0, f, e);
+        else load_one(kt + 2, integral_constant<int, decltype(e)::value - NR>{});
+      };
+    };
+    if constexpr (SPLIT) {
+      whole(fa, reads, [&](auto e) { read_one(kt, q1, fb, e); });
+      crossed(fa, fb, reads, [&](auto e) { read_one(kt, q2, fc, e); });
+      whole(fc, reads, [&](auto e) { read_one(kt, q3, fb, e); });
+      meet();
+      crossed(fc, fb, loads_and_reads, next(fa));
+    } else {
+      whole(fa, reads, [&](auto e) { read_one(kt, q1, fb, e); });
+      whole(fb, reads, [&](auto e) { read_one(kt, q2, fa, e); });
+      whole(fa, reads, [&](auto e) { read_one(kt, q3, fb, e); });
+      meet();
+      whole(fb, loads_and_reads, next(fa));
+    }
   }
-  if (kt < nk) stage(kt, a, a2);
   asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
   __builtin_amdgcn_s_barrier();
   asm volatile("" ::: "memory");
 
-  constexpr int PITCH = WN + 4, CH = WN / 8, RPI = 64 / CH;   // tokens a wave finishes at a time
-  float* const strip = (float*)smem + wave * 32 * PITCH;
-  const int c = n0 + wn0 + lane % CH * 8, n = g.out.O - c;
-  float bias[8];
-  load_bias8(g.out, c, n, bias);
-  int ew[8];
-  if constexpr (SPLIT) {
+  if (sliced) {
+    // 16 bytes a lane and quarter of an accumulator tile, as linear_combine_kernel reads them
+    float* const image = g.images + ((int64_t)tail * g.slices + z) * (BM * BN) + tid * 4;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) ew[e] = g.ew[c + e < g.out.O ? c + e : g.out.O - 1];
+    for (int i = 0; i < TM; ++i)
+#pragma unroll
+      for (int j = 0; j < TN; ++j)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          v4f part4;
+#pragma unroll
+          for (int r = 0; r < 4; ++r) part4[r] = acc[i][j][4 * q + r];
+          *(v4f*)(image + ((i * TN + j) * 4 + q) * (256 * WAVES)) = part4;
+        }
+    return;
   }
+  // CB columns of 64 / CH tokens at a time: as long runs of a row as the wave's columns divide into
+  constexpr int PITCH = WN + 4, CB = WN % 128 == 0 ? 128 : WN % 64 == 0 ? 64 : 32, CH = CB / 8, RPI = 64 / CH;
+  static_assert(WN % CB == 0, "column blocks");
+  float* const strip = (float*)smem + wave * 32 * PITCH;
 #pragma unroll
   for (int i = 0; i < TM; ++i) {
     // accumulator register v of a 32 x 32 tile: output 8 (v / 4) + 4 (lane / 32) + v % 4, token lane % 32
@@ -357,29 +393,77 @@ __global__ __launch_bounds__(64 * (BM / WM) * (BN / WN), 2) void linear_tile_ker
         *(v4f*)&strip[(lane & 31) * PITCH + j * 32 + 8 * q + 4 * (lane >> 5)] = part;
       }
     __builtin_amdgcn_wave_barrier();
-#pragma unroll 2
-    for (int t0 = 0; t0 < 32; t0 += RPI) {
-      const int t = t0 + lane / CH;
-      const int64_t row = m0 + wm0 + i * 32 + t;
-      const float* const p = &strip[t * PITCH + lane % CH * 8];
-      const v4f lo = *(const v4f*)p, hi = *(const v4f*)(p + 4);
-      float v[8];
+#pragma unroll 1
+    for (int cb = 0; cb < WN; cb += CB) {
+      const int c = n0 + wn0 + cb + lane % CH * 8, n = g.out.O - c;
+      float bias[8];
+      load_bias8(g.out, c, n, bias);
+      int ew[8];
+      if constexpr (SPLIT) {
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        v[e] = lo[e];
-        v[e + 4] = hi[e];
+        for (int e = 0; e < 8; ++e) ew[e] = g.ew[c + e < g.out.O ? c + e : g.out.O - 1];
       }
-      if (row < g.out.L) {
-        if constexpr (SPLIT) {
-          const int ex = g.ex[row];
+#pragma unroll 2
+      for (int t0 = 0; t0 < 32; t0 += RPI) {
+        const int t = t0 + lane / CH;
+        const int64_t row = m0 + wm0 + i * 32 + t;
+        const float* const p = &strip[t * PITCH + cb + lane % CH * 8];
+        const v4f lo = *(const v4f*)p, hi = *(const v4f*)(p + 4);
+        float v[8];
 #pragma unroll
-          for (int e = 0; e < 8; ++e) v[e] = __builtin_ldexpf(v[e], ex + ew[e]);
+        for (int e = 0; e < 4; ++e) {
+          v[e] = lo[e];
+          v[e + 4] = hi[e];
         }
-        linear_finish8<TY>(g.out, row, c, n, bias, v);
+        if (row < g.out.L) {
+          if constexpr (SPLIT) {
+            const int ex = g.ex[row];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] = __builtin_ldexpf(v[e], ex + ew[e]);
+          }
+          linear_finish8<TY>(g.out, row, c, n, bias, v);
+        }
       }
     }
     __builtin_amdgcn_wave_barrier();
   }
+}
+
+// The sums of a tile's slices, in slice order, and the epilogue.  A thread takes eight outputs of a token: the quarters of lanes l
+// and l + 32 of a 32 x 32 accumulator tile; four threads its 32 outputs.  Bound by the images' way through the caches.
+template <int BM, int BN, int WM, int WN, bool SPLIT, class TY>
+__global__ __launch_bounds__(256) void linear_combine_kernel(const TileArgs g) {
+  constexpr int WAVES_M = BM / WM, WAVES = WAVES_M * (BN / WN), TN = WN / 32;
+  constexpr int PER_TILE = BM * BN / 2048;    // workgroups of a tile
+  const int tail = (int)blockIdx.x / PER_TILE;
+  const int sub = (int)blockIdx.x % PER_TILE * 2 + ((int)threadIdx.x >> 7);      // 32 x 32 accumulator tile: wave fastest
+  const int q = (int)threadIdx.x & 3, l = ((int)threadIdx.x >> 2) & 31;
+  const int wave = sub % WAVES, ij = sub / WAVES;
+  int tm, tn;
+  tile_at(g.whole + tail, g.tiles_m, g.tiles_n, tm, tn);
+  const float* const image = g.images + (int64_t)tail * g.slices * (BM * BN) + (ij * 4 + q) * (256 * WAVES) + (wave * 64 + l) * 4;
+  float v[8] = {};
+#pragma unroll 4
+  for (int z = 0; z < g.slices; ++z) {
+    const float* const p = image + (int64_t)z * (BM * BN);
+    const v4f lo = *(const v4f*)p, hi = *(const v4f*)(p + 128);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      v[e] += lo[e];
+      v[e + 4] += hi[e];
+    }
+  }
+  const int64_t row = (int64_t)tm * BM + wave % WAVES_M * WM + ij / TN * 32 + l;
+  const int c = tn * BN + wave / WAVES_M * WN + ij % TN * 32 + 8 * q, n = g.out.O - c;
+  if (row >= g.out.L) return;
+  float bias[8];
+  load_bias8(g.out, c, n, bias);
+  if constexpr (SPLIT) {
+    const int ex = g.ex[row];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = __builtin_ldexpf(v[e], ex + g.ew[c + e < g.out.O ? c + e : g.out.O - 1]);
+  }
+  linear_finish8<TY>(g.out, row, c, n, bias, v);
 }
 
 // Operand rows of the fp32 product: row r of the L + O rows of x and w, scaled by 2^(14 - e), e the exponent of its largest value,
@@ -447,39 +531,103 @@ struct TileLayout {
 };
 TileLayout tile_layout(hot_type type, int64_t L, int64_t O, int64_t I) {
   TileLayout t;
-  t.packed = type == HOT_F32 || I % 32 != 0;
-  t.pitch = type == HOT_F32 ? round_up(I, 16) * 4 : round_up(I, 32) * 2;
+  t.packed = type == HOT_F32 || I % 64 != 0;
+  t.pitch = type == HOT_F32 ? round_up(I, 32) * 4 : round_up(I, 64) * 2;
   t.w = t.packed ? (size_t)round_up(L * t.pitch, 256) : 0;
   t.exps = t.w + (t.packed ? (size_t)round_up(O * t.pitch, 256) : 0);
   t.total = t.exps + (type == HOT_F32 ? (size_t)(L + O) * 4 : 0);
   return t;
 }
 
-bool use_tiles(hot_type type, int64_t L, int64_t, int64_t I) {
-  const int64_t pitch = type == HOT_F32 ? round_up(I, 16) * 4 : round_up(I, 32) * 2;
-  return L > 64 && pitch * 256 < (1ll << 31);     // a tile's rows within the reach of a buffer descriptor
+// How a product is worked on.
+struct Plan {
+  bool tiles;          // else linear_rows_kernel
+  int size;            // tile: 256 x 256, one workgroup a compute unit, or 128 x 128, two
+  int64_t tiles_m, tiles_n;
+  int64_t whole;       // tiles with a workgroup each; the rest in `slices` slices of K
+  int slices;
+};
+
+// A tile kernel's time in microseconds, from its measured parts: a stage of 128 bytes of K in a round of workgroups, what a round
+// takes besides (filling the buffers, the epilogue), the images' way to memory and back.
+double tile_time(int size, hot_type type, int64_t L, int64_t O, int64_t stages, Plan* p) {
+  const bool big = size == 256, f32 = type == HOT_F32;
+  const int64_t slots = big ? 256 : 512;
+  p->tiles = true;
+  p->size = size;
+  p->tiles_m = ceil_div(L, size);
+  p->tiles_n = ceil_div(O, size);
+  const int64_t count = p->tiles_m * p->tiles_n, rest = count % slots;
+  p->whole = count;
+  p->slices = 1;
+  const double full = big ? (f32 ? 2.27 : 1.53) : (f32 ? 1.34 : 0.97);    // every slot taken
+  const double alone = big ? full : (f32 ? 0.55 : 0.45);                  // 128 x 128, one workgroup a compute unit
+  const double round = big ? 10.0 : 5.0;
+  double t = count / slots * (stages * full + round);
+  if (rest) {
+    int64_t s = slots / rest;
+    s = s < stages / 4 ? s : stages / 4;      // four stages a slice at least
+    s = s < 16 ? s : 16;
+    double best = 1e30;
+    for (int64_t k = 1; k <= (s > 1 ? s : 1); ++k) {
+      const double sums = k > 1 ? 5.0 + k * rest * size * size * 8.0 / 4e6 : 0.0;
+      const double e = ceil_div(stages, k) * (rest * k > 256 ? full : alone) + round + sums;
+      if (e < best) {
+        best = e;
+        p->slices = (int)k;
+        p->whole = k > 1 ? count - rest : count;
+      }
+    }
+    t += best;
+  }
+  return t + 3.0;
 }
 
-template <int BM, int BN, int WM, int WN, bool SPLIT, class TY>
-hipError_t tiles_sized(TileArgs g, hipStream_t s) {
-  g.tiles_m = (int)ceil_div(g.out.L, BM);
-  g.tiles_n = (int)ceil_div(g.out.O, BN);
-  constexpr int LDS = kTileLds<BM, BN, WM, WN>;
-  auto kern = linear_tile_kernel<BM, BN, WM, WN, SPLIT, TY>;
+Plan make_plan(hot_type type, int64_t L, int64_t O, int64_t I) {
+  const TileLayout lay = tile_layout(type, L, O, I);
+  const bool f32 = type == HOT_F32;
+  Plan rows{}, a{}, b{};
+  if (lay.pitch * 256 >= (1ll << 31)) return rows;     // a tile's rows must be within the reach of a buffer descriptor
+  const double operands = lay.packed ? 4.0 + (L + O) * (double)(lay.pitch + I * (f32 ? 4 : 2)) / 4.5e6 : 0.0;
+  const int64_t stages = lay.pitch / kPiece;
+  const double ta = tile_time(128, type, L, O, stages, &a), tb = tile_time(256, type, L, O, stages, &b);
+  const int64_t mt = L <= 16 ? 16 : L <= 32 ? 32 : 64;
+  const double work = 2.0 * round_up(L, mt) * O * I / (f32 ? 55e6 : 140e6), moved = O * (double)I * (f32 ? 4 : 2) / 4.5e6;
+  const double tr = 5.0 + (work > moved ? work : moved);
+  if (tr <= operands + (ta < tb ? ta : tb)) return rows;
+  return ta < tb ? a : b;
+}
+
+size_t images_offset(const TileLayout& t) { return (size_t)round_up((int64_t)t.total, 256); }
+size_t scratch_bytes(const Plan& p, const TileLayout& t) {
+  if (!p.tiles) return 0;
+  if (p.slices == 1) return t.total;
+  return images_offset(t) + (size_t)((p.tiles_m * p.tiles_n - p.whole) * p.slices) * p.size * p.size * 4;
+}
+
+template <int SIZE, int WM, int WN, bool SPLIT, class TY>
+hipError_t tiles_sized(const TileArgs& g, hipStream_t s) {
+  constexpr int LDS = kTileLds<SIZE, SIZE, WM, WN>, THREADS = 64 * (SIZE / WM) * (SIZE / WN);
+  auto kern = linear_tile_kernel<SIZE, SIZE, WM, WN, SPLIT, TY>;
   static std::atomic<bool> attr_set{false};  // per instantiation; setting it twice is harmless
   if (!attr_set.load(std::memory_order_acquire)) {
     if (const hipError_t e = hipFuncSetAttribute((const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize, LDS); e != hipSuccess) return e;
     attr_set.store(true, std::memory_order_release);
   }
-  kern<<<dim3((unsigned)((int64_t)g.tiles_m * g.tiles_n)), dim3(64 * (BM / WM) * (BN / WN)), LDS, s>>>(g);
+  const int64_t rest = (int64_t)g.tiles_m * g.tiles_n - g.whole;
+  kern<<<dim3((unsigned)(g.whole + rest * g.slices)), dim3(THREADS), LDS, s>>>(g);
+  if (rest)
+    linear_combine_kernel<SIZE, SIZE, WM, WN, SPLIT, TY><<<dim3((unsigned)(rest * (SIZE * SIZE / 2048))), dim3(256), 0, s>>>(g);
   return hipGetLastError();
 }
 
 template <class T, class TY>
-hipError_t tiles_typed(const LinearForward& a, const LinearOut& o, hipStream_t s) {
+hipError_t tiles_typed(const LinearForward& a, const Plan& p, const LinearOut& o, hipStream_t s) {
   constexpr bool SPLIT = sizeof(T) == 4;
   const TileLayout t = tile_layout(a.type, a.L, a.O, a.I);
-  TileArgs g{(const uint8_t*)a.x, (const uint8_t*)a.w, t.pitch, nullptr, nullptr, 0, 0, o};
+  TileArgs g{(const uint8_t*)a.x, (const uint8_t*)a.w, t.pitch, nullptr, nullptr, (int)p.tiles_m, (int)p.tiles_n,
+             (int)p.whole, p.slices, nullptr, o};
+  if (p.slices > 1) g.images = (float*)((uint8_t*)a.ws + images_offset(t));
   if (t.packed) {
     uint8_t* const px = (uint8_t*)a.ws;
     uint8_t* const pw = px + t.w;
@@ -496,8 +644,7 @@ hipError_t tiles_typed(const LinearForward& a, const LinearOut& o, hipStream_t s
     g.ew = exps + a.L;
   }
   stage_begin(kStLinear, s);
-  const hipError_t e = ceil_div(a.L, 256) * ceil_div(a.O, 256) >= 192 ? tiles_sized<256, 256, 64, 128, SPLIT, TY>(g, s)
-                                                                     : tiles_sized<128, 128, 64, 64, SPLIT, TY>(g, s);
+  const hipError_t e = p.size == 256 ? tiles_sized<256, 64, 128, SPLIT, TY>(g, s) : tiles_sized<128, 64, 64, SPLIT, TY>(g, s);
   stage_end(kStLinear, s);
   return e;
 }
@@ -509,7 +656,8 @@ hipError_t linear_typed(const LinearForward& a, hipStream_t s) {
     const CkptLayout l = ckpt_layout(a.L, a.O);
     o.k = CkptView{(uint8_t*)a.ckpt, (uint8_t*)a.ckpt + l.exps, l.pitch};
   }
-  if (use_tiles(a.type, a.L, a.O, a.I)) return tiles_typed<T, TY>(a, o, s);
+  const Plan p = make_plan(a.type, a.L, a.O, a.I);
+  if (p.tiles) return tiles_typed<T, TY>(a, p, o, s);
   // 16 outputs a workgroup where that is what fills the card; a checkpoint's groups need 32
   stage_begin(kStLinear, s);
   const hipError_t e = a.ckpt || ceil_div(a.O, 32) * ceil_div(a.L, 64) >= 512 ? rows_typed<T, TY, 2>(a, o, s) : rows_typed<T, TY, 1>(a, o, s);
@@ -520,7 +668,7 @@ hipError_t linear_typed(const LinearForward& a, hipStream_t s) {
 }  // namespace
 
 size_t linear_scratch_bytes(hot_type type, int64_t L, int64_t O, int64_t I) {
-  return use_tiles(type, L, O, I) ? tile_layout(type, L, O, I).total : 0;
+  return scratch_bytes(make_plan(type, L, O, I), tile_layout(type, L, O, I));
 }
 
 hipError_t launch_linear(const LinearForward& a, hipStream_t s) {

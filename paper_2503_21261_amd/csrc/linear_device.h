@@ -63,11 +63,13 @@ __device__ __forceinline__ void linear_finish8(const LinearOut& o, int64_t row, 
 }
 
 // Workgroup -> tile: workgroups go to the eight XCDs in turn, each with an L2 of its own.  Ids are dealt so that an XCD
-// walks a contiguous run of tiles, in bands of eight tile rows, tile row fastest: the tiles it works on at a time
-// share their operands in its L2.
-__device__ __forceinline__ void tile_of(int id, int tiles_m, int tiles_n, int& tm, int& tn) {
-  const int total = tiles_m * tiles_n, per_xcd = total / 8;
-  const int p = id < per_xcd * 8 ? (id % 8) * per_xcd + id / 8 : id;
+// walks a contiguous run of positions, and positions go in bands of eight tile rows, tile row fastest: the tiles it works on
+// at a time share their operands in its L2.
+__device__ __forceinline__ int xcd_contiguous(int id, int total) {
+  const int per_xcd = total / 8;
+  return id < per_xcd * 8 ? (id % 8) * per_xcd + id / 8 : id;
+}
+__device__ __forceinline__ void tile_at(int p, int tiles_m, int tiles_n, int& tm, int& tn) {
   const int band = 8 * tiles_n, first = p / band * 8, in = p % band;
   const int rows = tiles_m - first < 8 ? tiles_m - first : 8;
   tm = first + in % rows;
