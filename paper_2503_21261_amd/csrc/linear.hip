@@ -5,6 +5,8 @@
 // LDS, in order.  A lane loads 16 consecutive bytes of a row; bfloat16 rows feed v_mfma_f32_16x16x32_bf16, fp32 rows
 // four v_mfma_f32_16x16x4_f32, whose products and sums are plain fp32.  The weight is the first operand, so that a
 // lane's accumulators are four consecutive outputs of a token.
+#include <math.h>
+
 #include <atomic>
 #include <utility>
 
@@ -59,19 +61,25 @@ __device__ __forceinline__ v4f multiply(const Frag<float>& a, const Frag<float>&
   return acc;
 }
 
+// Floats of a row of a slice's sums.
+__host__ __device__ constexpr int64_t sums_pitch(int64_t O) { return (O + 7) / 8 * 8; }
+
 constexpr int kWaves = 8;       // of a workgroup: parts of K
 constexpr int kSteps = 4;       // loads of a row on their way together: 4 x 64 bytes
 
 // NT x 16 outputs and MT x 16 tokens a workgroup.
 template <class T, class TY, int NT, int MT>
-__global__ __launch_bounds__(64 * kWaves) void linear_rows_kernel(const T* x, const T* w, int64_t I, int tiles_m, LinearOut out) {
+__global__ __launch_bounds__(64 * kWaves) void linear_rows_kernel(const T* x, const T* w, int64_t I, int tiles_m, int slices, float* sums, LinearOut out) {
   constexpr int E = Frag<T>::kElems;
   constexpr int STEP = 4 * E;               // elements of K in one matrix step (64 bytes of a row)
   constexpr int NC = NT * 16, MC = MT * 16;
   constexpr int PITCH = NC + 4;             // of a token's sums in LDS: rows apart by a multiple of 4 banks, not of 16
   __shared__ __align__(16) float s_sum[kWaves * MC * PITCH];
   const int lane = (int)threadIdx.x & 63, wave = (int)threadIdx.x >> 6;
-  const int tm = (int)blockIdx.x % tiles_m, tn = (int)blockIdx.x / tiles_m;
+  // slices of K fastest, then tokens: workgroups that share weight rows run side by side
+  const int z = (int)blockIdx.x % slices, tile = (int)blockIdx.x / slices;
+  const int tm = tile % tiles_m, tn = tile / tiles_m;
+  const int64_t k_first = I * z / slices / 16 * 16, k_end = z + 1 < slices ? I * (z + 1) / slices / 16 * 16 : I;
   const int64_t m0 = (int64_t)tm * MC;
   const int n0 = tn * NC;
   const T* wr[NT];
@@ -93,10 +101,11 @@ __global__ __launch_bounds__(64 * kWaves) void linear_rows_kernel(const T* x, co
 #pragma unroll
     for (int j = 0; j < NT; ++j) acc[i][j] = v4f{0, 0, 0, 0};
 
-  constexpr int SPAN = STEP * kSteps;       // of a wave at a time; the waves' spans follow each other
-  for (int64_t k0 = (int64_t)wave * SPAN; k0 < I; k0 += (int64_t)kWaves * SPAN) {
+  // The waves' spans of K follow each other; all loads of a span are on their way together.
+  constexpr int SPAN = STEP * kSteps;
+  for (int64_t k0 = k_first + (int64_t)wave * SPAN; k0 < k_end; k0 += (int64_t)kWaves * SPAN) {
     Frag<T> fw[kSteps][NT], fx[kSteps][MT];
-    if (k0 + SPAN <= I) {
+    if (k0 + SPAN <= k_end) {
 #pragma unroll
       for (int s = 0; s < kSteps; ++s) {
 #pragma unroll
@@ -109,9 +118,9 @@ __global__ __launch_bounds__(64 * kWaves) void linear_rows_kernel(const T* x, co
       for (int s = 0; s < kSteps; ++s) {
         const int64_t k = k0 + s * STEP + ke;
 #pragma unroll
-        for (int j = 0; j < NT; ++j) fw[s][j] = load_frag(wr[j] + k, I - k);
+        for (int j = 0; j < NT; ++j) fw[s][j] = load_frag(wr[j] + k, k_end - k);
 #pragma unroll
-        for (int i = 0; i < MT; ++i) fx[s][i] = load_frag(xr[i] + k, I - k);
+        for (int i = 0; i < MT; ++i) fx[s][i] = load_frag(xr[i] + k, k_end - k);
       }
     }
 #pragma unroll
@@ -142,25 +151,37 @@ __global__ __launch_bounds__(64 * kWaves) void linear_rows_kernel(const T* x, co
         v[e + 4] += b[e];
       }
     }
+    const int n = out.O - n0 - c;
+    if (sums) {      // a slice's: added by linear_rows_combine_kernel
+      if (n > 0) store8(sums + ((int64_t)z * out.L + m0 + t) * sums_pitch(out.O) + n0 + c, v, 8);
+      continue;
+    }
     float b[8];
-    load_bias8(out, n0 + c, out.O - n0 - c, b);
-    linear_finish8<TY>(out, m0 + t, n0 + c, out.O - n0 - c, b, v);
+    load_bias8(out, n0 + c, n, b);
+    linear_finish8<TY>(out, m0 + t, n0 + c, n, b, v);
   }
 }
 
-template <class T, class TY, int NT>
-hipError_t rows_typed(const LinearForward& a, const LinearOut& o, hipStream_t s) {
-  const int64_t tn = ceil_div(a.O, NT * 16);
-  auto go = [&](auto mt) {
-    constexpr int MT = decltype(mt)::value;
-    const int64_t tm = ceil_div(a.L, MT * 16);
-    linear_rows_kernel<T, TY, NT, MT><<<dim3((unsigned)(tm * tn)), dim3(64 * kWaves), 0, s>>>((const T*)a.x, (const T*)a.w, a.I,
-                                                                                            (int)tm, o);
-    return hipGetLastError();
-  };
-  if (a.L <= 16) return go(std::integral_constant<int, 1>{});
-  if (a.L <= 32) return go(std::integral_constant<int, 2>{});
-  return go(std::integral_constant<int, 4>{});
+// The slices' sums, in order, and the epilogue: eight outputs of a token a thread.
+template <class TY>
+__global__ __launch_bounds__(256) void linear_rows_combine_kernel(const float* sums, int slices, int chunks, LinearOut out) {
+  const int64_t q = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  const int64_t row = q / chunks;
+  const int c = (int)(q % chunks) * 8, n = out.O - c;
+  if (row >= out.L) return;
+  float v[8] = {};
+  if (n > 0) {
+#pragma unroll 4
+    for (int z = 0; z < slices; ++z) {
+      float p[8];
+      load_values(sums + ((int64_t)z * out.L + row) * sums_pitch(out.O) + c, 8, p);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[e] += p[e];
+    }
+  }
+  float b[8];
+  load_bias8(out, c, n, b);
+  linear_finish8<TY>(out, row, c, n, b, v);
 }
 
 // ---- many rows -------------------------------------------------------------------------------------
@@ -467,44 +488,99 @@ __global__ __launch_bounds__(256) void linear_combine_kernel(const TileArgs g) {
 }
 
 // Operand rows of the fp32 product: row r of the L + O rows of x and w, scaled by 2^(14 - e), e the exponent of its largest value,
-// as [16 high | 16 low] pieces; exps[r] = e - 14.  A wave takes a row, twice: the second read comes from the caches.
-// Padded columns are zero.
+// as [16 high | 16 low] pieces; exps[r] = e - 14.  Padded columns are zero.  Bound by HBM: a row stays in the registers of the T
+// lanes that work on it, NV times eight columns each, or (NV = 0: rows beyond 16384) is read a second time, from the caches.
+__device__ __forceinline__ int row_exponent(uint32_t top) {   // of the largest magnitude's bits; subnormal ones too
+  // infinities and NaNs stay what they are under any scale
+  return top >= 0x7F800000u || top == 0 ? 0 : ilogbf(__uint_as_float(top));
+}
+__device__ __forceinline__ void store_parts(uint8_t* dst, int64_t c, const float (&v)[8], int e) {
+  v8h hi, lo;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const float s = __builtin_ldexpf(v[i], 14 - e);
+    hi[i] = (_Float16)s;
+    lo[i] = (_Float16)(s - (float)hi[i]);
+  }
+  uint8_t* const p = dst + (c >> 4) * 64 + (c & 8) * 2;
+  *(v8h*)p = hi;
+  *(v8h*)(p + 32) = lo;
+}
+template <int T, int NV>
 __global__ __launch_bounds__(256) void linear_split_kernel(const float* x, const float* w, int64_t L, int64_t O, int64_t I, int64_t pitch,
                                                            uint8_t* px, uint8_t* pw, int* exps) {
-  const int lane = (int)threadIdx.x & 63;
-  const int64_t r = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-  if (r >= L + O) return;
+  __shared__ uint32_t s_top[4];
+  const int lane = (int)threadIdx.x % T;
+  const int64_t r = (int64_t)blockIdx.x * (256 / T) + (int)threadIdx.x / T;
+  if (r >= L + O) return;    // T = 256: one row a workgroup
   const float* const src = r < L ? x + r * I : w + (r - L) * I;
   uint8_t* const dst = r < L ? px + r * pitch : pw + (r - L) * pitch;
+  const int64_t padded = pitch / 4;
+  auto have = [&](int64_t c) { return (int)(I - c < 0 ? 0 : I - c < 8 ? I - c : 8); };
   uint32_t top = 0;
+  Raw8<float> raw[NV > 0 ? NV : 1];
+  if constexpr (NV > 0) {
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+      const int64_t c = (lane + j * T) * 8;
+      raw[j] = load8(src + c, have(c));
+    }
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+      float v[8];
+      widen(raw[j], v);
+      top = max(top, magnitude8(v));
+    }
+  } else {
 #pragma unroll 4
-  for (int64_t c = lane * 8; c < I; c += 512) {
-    float v[8];
-    load_values(src + c, (int)(I - c < 8 ? I - c : 8), v);
-    top = max(top, magnitude8(v));
+    for (int64_t c = lane * 8; c < I; c += T * 8) {
+      float v[8];
+      load_values(src + c, have(c), v);
+      top = max(top, magnitude8(v));
+    }
   }
 #pragma unroll
   for (int m = 1; m < 64; m *= 2) top = max(top, (uint32_t)__shfl_xor((int)top, m));
-  // frexp's exponent is right for subnormal rows too; infinities and NaNs stay what they are under any scale
-  const int e = top >= 0x7F800000u || top == 0 ? 0 : ilogbf(__uint_as_float(top));
-  if (lane == 0) exps[r] = e - 14;
-  const int64_t padded = pitch / 4;
-#pragma unroll 2
-  for (int64_t c = lane * 8; c < padded; c += 512) {
-    float v[8];
-    const int64_t n = I - c;
-    load_values(src + c, (int)(n < 0 ? 0 : n < 8 ? n : 8), v);
-    v8h hi, lo;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const float s = __builtin_ldexpf(v[i], 14 - e);
-      hi[i] = (_Float16)s;
-      lo[i] = (_Float16)(s - (float)hi[i]);
-    }
-    uint8_t* const p = dst + (c >> 4) * 64 + (c & 8) * 2;
-    *(v8h*)p = hi;
-    *(v8h*)(p + 32) = lo;
+  if constexpr (T > 64) {
+    if (((int)threadIdx.x & 63) == 0) s_top[(int)threadIdx.x >> 6] = top;
+    __syncthreads();
+    top = max(max(s_top[0], s_top[1]), max(s_top[2], s_top[3]));
   }
+  const int e = row_exponent(top);
+  if (lane == 0) exps[r] = e - 14;
+  if constexpr (NV > 0) {
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+      const int64_t c = (lane + j * T) * 8;
+      float v[8];
+      widen(raw[j], v);
+      if (c < padded) store_parts(dst, c, v, e);
+    }
+  } else {
+#pragma unroll 2
+    for (int64_t c = lane * 8; c < padded; c += T * 8) {
+      float v[8];
+      load_values(src + c, have(c), v);
+      store_parts(dst, c, v, e);
+    }
+  }
+}
+
+hipError_t launch_split(const float* x, const float* w, int64_t L, int64_t O, int64_t I, int64_t pitch, uint8_t* px, uint8_t* pw,
+                        int* exps, hipStream_t s) {
+  auto go = [&](auto t, auto nv) {
+    constexpr int T = decltype(t)::value;
+    linear_split_kernel<T, decltype(nv)::value><<<dim3((unsigned)ceil_div(L + O, 256 / T)), dim3(256), 0, s>>>(x, w, L, O, I, pitch, px, pw, exps);
+    return hipGetLastError();
+  };
+  using std::integral_constant;
+  if (I <= 512) return go(integral_constant<int, 64>{}, integral_constant<int, 1>{});
+  if (I <= 1024) return go(integral_constant<int, 64>{}, integral_constant<int, 2>{});
+  if (I <= 2048) return go(integral_constant<int, 256>{}, integral_constant<int, 1>{});
+  if (I <= 4096) return go(integral_constant<int, 256>{}, integral_constant<int, 2>{});
+  if (I <= 8192) return go(integral_constant<int, 256>{}, integral_constant<int, 4>{});
+  if (I <= 16384) return go(integral_constant<int, 256>{}, integral_constant<int, 8>{});
+  return go(integral_constant<int, 256>{}, integral_constant<int, 0>{});
 }
 
 // Rows of bfloat16 operands whose width is no multiple of 32, padded with zeros.
@@ -546,10 +622,16 @@ struct Plan {
   int64_t tiles_m, tiles_n;
   int64_t whole;       // tiles with a workgroup each; the rest in `slices` slices of K
   int slices;
+  int nt, mt;          // linear_rows_kernel: 16 nt outputs and 16 mt tokens a workgroup
 };
 
-// A tile kernel's time in microseconds, from its measured parts: a stage of 128 bytes of K in a round of workgroups, what a round
-// takes besides (filling the buffers, the epilogue), the images' way to memory and back.
+// Times in microseconds of the ways to do a product, for the choice between them.  The constants are a fit to 1900 launches of all
+// three kernels over 500 random shapes (1 to 60000 rows, widths of 64 to 11008, both types, every split below); the way they choose takes
+// 1.025 times the best one's time on average, 1.4 times at worst.  A second launch also costs the caller's thread.
+constexpr double kLaunch = 3.0;
+
+// Tiles: a stage of 128 bytes of K in a round of workgroups, what a round takes besides (filling the buffers, the epilogue), the
+// outputs, the images' way to memory and back.
 double tile_time(int size, hot_type type, int64_t L, int64_t O, int64_t stages, Plan* p) {
   const bool big = size == 256, f32 = type == HOT_F32;
   const int64_t slots = big ? 256 : 512;
@@ -560,18 +642,19 @@ double tile_time(int size, hot_type type, int64_t L, int64_t O, int64_t stages, 
   const int64_t count = p->tiles_m * p->tiles_n, rest = count % slots;
   p->whole = count;
   p->slices = 1;
-  const double full = big ? (f32 ? 2.27 : 1.53) : (f32 ? 1.34 : 0.97);    // every slot taken
-  const double alone = big ? full : (f32 ? 0.55 : 0.45);                  // 128 x 128, one workgroup a compute unit
-  const double round = big ? 10.0 : 5.0;
-  double t = count / slots * (stages * full + round);
+  const double full = big ? (f32 ? 1.34 : 1.08) : (f32 ? 1.38 : 0.96);    // a stage with every slot taken
+  const double half = big ? full : (f32 ? 0.57 : 0.54);                   // 128 x 128, one workgroup a compute unit
+  const double round = big ? (f32 ? 15.4 : 11.8) : (f32 ? 9.3 : 7.8);
+  double t = (count / slots) * (stages * full + round);
   if (rest) {
-    int64_t s = slots / rest;
-    s = s < stages / 4 ? s : stages / 4;      // four stages a slice at least
-    s = s < 16 ? s : 16;
+    int64_t most = slots / rest;                            // slices that still fill one round,
+    most = most < stages / 4 ? most : stages / 4;           // of four stages at least
+    most = most < 16 ? most : 16;
     double best = 1e30;
-    for (int64_t k = 1; k <= (s > 1 ? s : 1); ++k) {
-      const double sums = k > 1 ? 5.0 + k * rest * size * size * 8.0 / 4e6 : 0.0;
-      const double e = ceil_div(stages, k) * (rest * k > 256 ? full : alone) + round + sums;
+    for (int64_t k = 1; k <= (most > 1 ? most : 1); ++k) {
+      const int64_t n = rest * k;
+      const double stage = big || n <= 256 ? half : half + (full - half) * (double)(n - 256) / 256;
+      const double e = ceil_div(stages, k) * stage + round + (k > 1 ? kLaunch + (double)n * size * size * 8 / (big ? 6.4e6 : 3.8e6) : 0.0);
       if (e < best) {
         best = e;
         p->slices = (int)k;
@@ -580,27 +663,54 @@ double tile_time(int size, hot_type type, int64_t L, int64_t O, int64_t stages, 
     }
     t += best;
   }
-  return t + 3.0;
+  return t + (double)L * O / 3e6;
+}
+
+// linear_rows_kernel: a compute unit's matrix instructions and loads, both in units of 2000 cycles' worth a microsecond and for as many
+// rounds of workgroups as there are, beside the operands' way from HBM.  Rows of an odd number of bfloat16 elements are not
+// 4-byte aligned, which costs their loads three times the time.
+double rows_time(hot_type type, int64_t L, int64_t O, int64_t I, Plan* p) {
+  const bool f32 = type == HOT_F32;
+  const double hbm = ((double)O * I + (double)L * I) * (f32 ? 4 : 2) / (f32 ? 5.8e6 : 9e6) + (double)L * O * 4 / (f32 ? 5.8e6 : 9e6);
+  const int64_t turn = kWaves * kSteps * (f32 ? 16 : 32);    // elements of K a workgroup has on their way
+  const double odd = !f32 && I % 2 ? 3.2 : 1.0;
+  double best = 1e30;
+  for (int nt = 1; nt <= 2; ++nt)
+    for (int mt = 1; mt <= 4; mt *= 2) {
+      if (mt > 1 && (mt / 2) * 16 >= L) continue;
+      const int64_t tm = ceil_div(L, 16 * mt), tn = ceil_div(O, 16 * nt);
+      for (int s = 1; s <= 16; ++s) {
+        if (s > 1 && (tm * tn * s > 512 || I / s < turn)) break;
+        const double rounds = tm * tn * s > 256 ? tm * tn * s / 256.0 : 1.0;
+        const double k = (double)I / s * odd / 2000;
+        const double cu = rounds * (f32 ? k * (1.62 * nt * mt + 2.33 * (nt + mt)) + 0.44 * nt * mt
+                                        : k * (0.21 * nt * mt + 1.46 * (nt + mt)) + 0.39 * nt * mt);
+        const double t = 5.3 + sqrt(cu * cu + hbm * hbm) + (s > 1 ? kLaunch + 2.0 + (double)s * L * O * 8 / 4e6 : 0.0);
+        if (t < best) {
+          best = t;
+          *p = Plan{false, 0, tm, tn, 0, s, nt, mt};
+        }
+      }
+    }
+  return best;
 }
 
 Plan make_plan(hot_type type, int64_t L, int64_t O, int64_t I) {
   const TileLayout lay = tile_layout(type, L, O, I);
   const bool f32 = type == HOT_F32;
   Plan rows{}, a{}, b{};
+  const double tr = rows_time(type, L, O, I, &rows);
   if (lay.pitch * 256 >= (1ll << 31)) return rows;     // a tile's rows must be within the reach of a buffer descriptor
-  const double operands = lay.packed ? 4.0 + (L + O) * (double)(lay.pitch + I * (f32 ? 4 : 2)) / 4.5e6 : 0.0;
+  const double operands = lay.packed ? kLaunch + 2.0 + (double)(L + O) * I * (f32 ? 8 : 4) / 5.4e6 : 0.0;
   const int64_t stages = lay.pitch / kPiece;
   const double ta = tile_time(128, type, L, O, stages, &a), tb = tile_time(256, type, L, O, stages, &b);
-  const int64_t mt = L <= 16 ? 16 : L <= 32 ? 32 : 64;
-  const double work = 2.0 * round_up(L, mt) * O * I / (f32 ? 55e6 : 140e6), moved = O * (double)I * (f32 ? 4 : 2) / 4.5e6;
-  const double tr = 5.0 + (work > moved ? work : moved);
   if (tr <= operands + (ta < tb ? ta : tb)) return rows;
   return ta < tb ? a : b;
 }
 
 size_t images_offset(const TileLayout& t) { return (size_t)round_up((int64_t)t.total, 256); }
-size_t scratch_bytes(const Plan& p, const TileLayout& t) {
-  if (!p.tiles) return 0;
+size_t scratch_bytes(const Plan& p, const TileLayout& t, int64_t L, int64_t O) {
+  if (!p.tiles) return p.slices > 1 ? (size_t)p.slices * L * sums_pitch(O) * 4 : 0;
   if (p.slices == 1) return t.total;
   return images_offset(t) + (size_t)((p.tiles_m * p.tiles_n - p.whole) * p.slices) * p.size * p.size * 4;
 }
@@ -632,12 +742,17 @@ hipError_t tiles_typed(const LinearForward& a, const Plan& p, const LinearOut& o
     uint8_t* const px = (uint8_t*)a.ws;
     uint8_t* const pw = px + t.w;
     int* const exps = (int*)(px + t.exps);
-    const dim3 grid((unsigned)ceil_div(a.L + a.O, 4)), block(256);
     stage_begin(kStLinearOperands, s);
-    if constexpr (SPLIT) linear_split_kernel<<<grid, block, 0, s>>>((const float*)a.x, (const float*)a.w, a.L, a.O, a.I, t.pitch, px, pw, exps);
-    else linear_pad_kernel<<<grid, block, 0, s>>>((const bf16*)a.x, (const bf16*)a.w, a.L, a.O, a.I, t.pitch, px, pw);
+    hipError_t e;
+    if constexpr (SPLIT) {
+      e = launch_split((const float*)a.x, (const float*)a.w, a.L, a.O, a.I, t.pitch, px, pw, exps, s);
+    } else {
+      linear_pad_kernel<<<dim3((unsigned)ceil_div(a.L + a.O, 4)), dim3(256), 0, s>>>((const bf16*)a.x, (const bf16*)a.w, a.L, a.O, a.I,
+                                                                                    t.pitch, px, pw);
+      e = hipGetLastError();
+    }
     stage_end(kStLinearOperands, s);
-    if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+    if (e != hipSuccess) return e;
     g.x = px;
     g.w = pw;
     g.ex = exps;
@@ -650,17 +765,43 @@ hipError_t tiles_typed(const LinearForward& a, const Plan& p, const LinearOut& o
 }
 
 template <class T, class TY>
+hipError_t rows_typed(const LinearForward& a, const Plan& p, const LinearOut& o, hipStream_t s) {
+  auto go = [&](auto nt, auto mt) {
+    constexpr int NT = decltype(nt)::value, MT = decltype(mt)::value;
+    float* const sums = p.slices > 1 ? (float*)a.ws : nullptr;
+    linear_rows_kernel<T, TY, NT, MT><<<dim3((unsigned)(p.tiles_m * p.tiles_n * p.slices)), dim3(64 * kWaves), 0, s>>>(
+        (const T*)a.x, (const T*)a.w, a.I, (int)p.tiles_m, p.slices, sums, o);
+    if (sums) {
+      const int chunks = (int)(o.k.codes ? o.k.pitch / 8 : sums_pitch(a.O) / 8);    // a checkpoint's groups are whole
+      linear_rows_combine_kernel<TY><<<dim3((unsigned)ceil_div(a.L * chunks, 256)), dim3(256), 0, s>>>(sums, p.slices, chunks, o);
+    }
+    return hipGetLastError();
+  };
+  using std::integral_constant;
+  auto with_nt = [&](auto mt) {
+    if (p.nt == 1) return go(integral_constant<int, 1>{}, mt);
+    return go(integral_constant<int, 2>{}, mt);
+  };
+  if (p.mt == 1) return with_nt(integral_constant<int, 1>{});
+  if (p.mt == 2) return with_nt(integral_constant<int, 2>{});
+  return with_nt(integral_constant<int, 4>{});
+}
+
+template <class T, class TY>
 hipError_t linear_typed(const LinearForward& a, hipStream_t s) {
   LinearOut o{a.bias, a.residual, a.y, CkptView{}, a.L, (int)a.O, a.fn};
   if (a.ckpt) {
     const CkptLayout l = ckpt_layout(a.L, a.O);
     o.k = CkptView{(uint8_t*)a.ckpt, (uint8_t*)a.ckpt + l.exps, l.pitch};
   }
-  const Plan p = make_plan(a.type, a.L, a.O, a.I);
+  Plan p = make_plan(a.type, a.L, a.O, a.I);
+  if (a.ckpt && !p.tiles && p.slices == 1 && p.nt == 1) {   // a group is finished by one workgroup
+    p.nt = 2;
+    p.tiles_n = ceil_div(a.O, 32);
+  }
   if (p.tiles) return tiles_typed<T, TY>(a, p, o, s);
-  // 16 outputs a workgroup where that is what fills the card; a checkpoint's groups need 32
   stage_begin(kStLinear, s);
-  const hipError_t e = a.ckpt || ceil_div(a.O, 32) * ceil_div(a.L, 64) >= 512 ? rows_typed<T, TY, 2>(a, o, s) : rows_typed<T, TY, 1>(a, o, s);
+  const hipError_t e = rows_typed<T, TY>(a, p, o, s);
   stage_end(kStLinear, s);
   return e;
 }
@@ -668,7 +809,7 @@ hipError_t linear_typed(const LinearForward& a, hipStream_t s) {
 }  // namespace
 
 size_t linear_scratch_bytes(hot_type type, int64_t L, int64_t O, int64_t I) {
-  return scratch_bytes(make_plan(type, L, O, I), tile_layout(type, L, O, I));
+  return scratch_bytes(make_plan(type, L, O, I), tile_layout(type, L, O, I), L, O);
 }
 
 hipError_t launch_linear(const LinearForward& a, hipStream_t s) {
