@@ -350,27 +350,43 @@ def hot_lowpass_l1_rows(block: int, keep: int):
 _TYPES = {torch.float32: HOT_F32, torch.bfloat16: HOT_BF16}
 
 
+# The index alone; private to torch, so that a torch without it takes the public call.
+_current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
+
+
+def _stream_of(stream, device: int) -> Optional[int]:
+    """As _stream(), for the current device that the caller has asked for already."""
+    if stream is None and _raw_stream is not None:
+        return _raw_stream(device) or None
+    return _stream(stream)
+
+
 def _expect(name: str, t: torch.Tensor, dtype: torch.dtype, shape: Tuple[int, ...], device: int) -> int:
     """The tensor's address; raises unless it is a contiguous `dtype` tensor of `shape` on CUDA device `device`."""
-    if not (t.is_cuda and t.get_device() == device and t.dtype == dtype and t.shape == shape and t.is_contiguous()):
+    if t.get_device() != device or t.dtype is not dtype or t.shape != shape or not t.is_contiguous():   # a host tensor's device is -1
         raise ValueError(f"{name}: expected contiguous {dtype} tensor of shape {tuple(shape)} on cuda:{device}, the current device")
     return t.data_ptr()
 
 
 def _typed(name: str, t: torch.Tensor) -> int:
-    """hot_type of a tensor that sets the type of others; raises unless it is a matrix of a supported type on the GPU."""
-    if not (t.is_cuda and t.dim() == 2 and t.dtype in _TYPES):
+    """hot_type of a tensor that sets the type of others; raises unless it is a matrix of a supported type on a GPU."""
+    ty = _TYPES.get(t.dtype)
+    if ty is None or t.dim() != 2 or not t.is_cuda:
         raise ValueError(f"{name}: expected a float32 or bfloat16 device tensor of two dimensions")
-    return _TYPES[t.dtype]
+    return ty
 
 
-def _bytes(name: str, t: Optional[torch.Tensor], least: int, device: int) -> Optional[int]:
+def _bytes(name: str, t: torch.Tensor, least: int, device: int) -> int:
     """Address of an opaque uint8 buffer of at least `least` bytes."""
-    if t is None:
-        return None
-    if not (t.is_cuda and t.get_device() == device and t.dtype == torch.uint8 and t.is_contiguous() and t.numel() >= least):
+    if t.get_device() != device or t.dtype is not torch.uint8 or t.numel() < least or not t.is_contiguous():
         raise ValueError(f"{name}: expected contiguous uint8 tensor of at least {least} bytes on cuda:{device}, the current device")
     return t.data_ptr()
+
+
+def _ckpt(t: torch.Tensor, rows: int, cols: int, device: int) -> int:
+    """Address of a checkpoint of [rows, cols]; its size is hot_checkpoint_bytes()'s, worked out here without a call."""
+    pitch = cols + 31 & -32
+    return _bytes("ckpt", t, (rows * pitch + 255 & -256) + rows * pitch // 32, device)
 
 
 def hot_checkpoint_bytes(rows: int, cols: int) -> int:
@@ -417,34 +433,37 @@ def alloc_linear_workspace(dtype: torch.dtype, L: int, O: int, I: int, device="c
 
 def hot_checkpoint_write(x: torch.Tensor, ckpt: torch.Tensor, stream=None) -> torch.Tensor:
     """Stores x in 8 bits; returns the buffer."""
-    ty, dev = _typed("x", x), torch.cuda.current_device()
+    ty, dev = _typed("x", x), _current_device()
     rows, cols = x.shape
     st = lib().hot_checkpoint_write(_expect("x", x, x.dtype, x.shape, dev), ty, rows, cols,
-                                    _bytes("ckpt", ckpt, hot_checkpoint_bytes(rows, cols), dev), _stream(stream))
-    _check(st, "hot_checkpoint_write")
+                                    _ckpt(ckpt, rows, cols, dev), _stream_of(stream, dev))
+    if st:
+        _check(st, "hot_checkpoint_write")
     return ckpt
 
 
 def hot_checkpoint_read(ckpt: torch.Tensor, x: torch.Tensor, stream=None) -> torch.Tensor:
     """Fills x [rows, cols] with the values that the checkpoint of its shape holds; returns x."""
-    ty, dev = _typed("x", x), torch.cuda.current_device()
+    ty, dev = _typed("x", x), _current_device()
     rows, cols = x.shape
-    st = lib().hot_checkpoint_read(_bytes("ckpt", ckpt, hot_checkpoint_bytes(rows, cols), dev), rows, cols,
-                                   _expect("x", x, x.dtype, x.shape, dev), ty, _stream(stream))
-    _check(st, "hot_checkpoint_read")
+    st = lib().hot_checkpoint_read(_ckpt(ckpt, rows, cols, dev), rows, cols,
+                                   _expect("x", x, x.dtype, x.shape, dev), ty, _stream_of(stream, dev))
+    if st:
+        _check(st, "hot_checkpoint_read")
     return x
 
 
 def hot_activation_forward(fn: int, x: torch.Tensor, y: torch.Tensor, ckpt: Optional[torch.Tensor] = None,
                            stream=None) -> torch.Tensor:
     """y = f(x), and the checkpoint of x where a buffer is given; returns y."""
-    ty, dev = _typed("x", x), torch.cuda.current_device()
+    ty, dev = _typed("x", x), _current_device()
     rows, cols = x.shape
     st = lib().hot_activation_forward(int(fn), _expect("x", x, x.dtype, x.shape, dev), ty, rows, cols,
                                       _expect("y", y, x.dtype, x.shape, dev),
-                                      None if ckpt is None else _bytes("ckpt", ckpt, hot_checkpoint_bytes(rows, cols), dev),
-                                      _stream(stream))
-    _check(st, "hot_activation_forward")
+                                      None if ckpt is None else _ckpt(ckpt, rows, cols, dev),
+                                      _stream_of(stream, dev))
+    if st:
+        _check(st, "hot_activation_forward")
     return y
 
 
@@ -452,15 +471,16 @@ def hot_activation_backward(fn: int, g_y: torch.Tensor, g_x: torch.Tensor, x: Op
                             ckpt: Optional[torch.Tensor] = None, g_bias: Optional[torch.Tensor] = None,
                             ws: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
     """g_x = g_y f'(x) with x or its checkpoint, g_bias = the sum of g_x over the rows; returns g_x."""
-    ty, dev = _typed("g_y", g_y), torch.cuda.current_device()
+    ty, dev = _typed("g_y", g_y), _current_device()
     rows, cols = shape = g_y.shape
     st = lib().hot_activation_backward(
         int(fn), _expect("g_y", g_y, g_y.dtype, shape, dev), ty, None if x is None else _expect("x", x, g_y.dtype, shape, dev),
-        None if ckpt is None else _bytes("ckpt", ckpt, hot_checkpoint_bytes(rows, cols), dev), rows, cols,
+        None if ckpt is None else _ckpt(ckpt, rows, cols, dev), rows, cols,
         _expect("g_x", g_x, g_y.dtype, shape, dev),
         None if g_bias is None else _expect("g_bias", g_bias, torch.float32, (cols,), dev),
-        _bytes("ws", ws, 0, dev), 0 if ws is None else ws.numel(), _stream(stream))
-    _check(st, "hot_activation_backward")
+        *((None, 0) if ws is None else (_bytes("ws", ws, 0, dev), ws.numel())), _stream_of(stream, dev))
+    if st:
+        _check(st, "hot_activation_backward")
     return g_x
 
 
@@ -468,7 +488,7 @@ def hot_layer_norm_forward(x: torch.Tensor, gamma: Optional[torch.Tensor], beta:
                            y: torch.Tensor, mean: torch.Tensor, rstd: torch.Tensor, residual: Optional[torch.Tensor] = None,
                            h: Optional[torch.Tensor] = None, ckpt: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
     """h = x + residual, y = layer norm of h, with its mean and rstd per row, and the checkpoint of h; returns y."""
-    tx, ty, dev = _typed("x", x), _typed("y", y), torch.cuda.current_device()
+    tx, ty, dev = _typed("x", x), _typed("y", y), _current_device()
     rows, cols = shape = x.shape
     f32 = torch.float32
     st = lib().hot_layer_norm_forward(
@@ -477,8 +497,9 @@ def hot_layer_norm_forward(x: torch.Tensor, gamma: Optional[torch.Tensor], beta:
         None if beta is None else _expect("beta", beta, f32, (cols,), dev), eps, rows, cols,
         None if h is None else _expect("h", h, x.dtype, shape, dev), _expect("y", y, y.dtype, shape, dev), ty,
         _expect("mean", mean, f32, (rows,), dev), _expect("rstd", rstd, f32, (rows,), dev),
-        None if ckpt is None else _bytes("ckpt", ckpt, hot_checkpoint_bytes(rows, cols), dev), _stream(stream))
-    _check(st, "hot_layer_norm_forward")
+        None if ckpt is None else _ckpt(ckpt, rows, cols, dev), _stream_of(stream, dev))
+    if st:
+        _check(st, "hot_layer_norm_forward")
     return y
 
 
@@ -488,20 +509,21 @@ def hot_layer_norm_backward(g_y: torch.Tensor, gamma: Optional[torch.Tensor], me
                             ckpt: Optional[torch.Tensor] = None, g_residual: Optional[torch.Tensor] = None,
                             stream=None) -> torch.Tensor:
     """Gradients of the layer norm of h (or of its checkpoint); g_residual is added to g_x; returns g_x."""
-    ty, tx, dev = _typed("g_y", g_y), _typed("g_x", g_x), torch.cuda.current_device()
+    ty, tx, dev = _typed("g_y", g_y), _typed("g_x", g_x), _current_device()
     rows, cols = shape = g_y.shape
     f32 = torch.float32
     st = lib().hot_layer_norm_backward(
         _expect("g_y", g_y, g_y.dtype, shape, dev), ty, None if h is None else _expect("h", h, g_x.dtype, shape, dev),
-        None if ckpt is None else _bytes("ckpt", ckpt, hot_checkpoint_bytes(rows, cols), dev), tx,
+        None if ckpt is None else _ckpt(ckpt, rows, cols, dev), tx,
         None if gamma is None else _expect("gamma", gamma, f32, (cols,), dev),
         _expect("mean", mean, f32, (rows,), dev), _expect("rstd", rstd, f32, (rows,), dev),
         None if g_residual is None else _expect("g_residual", g_residual, g_x.dtype, shape, dev), rows, cols,
         _expect("g_x", g_x, g_x.dtype, shape, dev),
         None if g_gamma is None else _expect("g_gamma", g_gamma, f32, (cols,), dev),
         None if g_beta is None else _expect("g_beta", g_beta, f32, (cols,), dev),
-        _bytes("ws", ws, 0, dev), 0 if ws is None else ws.numel(), _stream(stream))
-    _check(st, "hot_layer_norm_backward")
+        *((None, 0) if ws is None else (_bytes("ws", ws, 0, dev), ws.numel())), _stream_of(stream, dev))
+    if st:
+        _check(st, "hot_layer_norm_backward")
     return g_x
 
 
@@ -509,7 +531,7 @@ def hot_linear_forward(x: torch.Tensor, w: torch.Tensor, y: torch.Tensor, ws: Op
                        bias: Optional[torch.Tensor] = None, residual: Optional[torch.Tensor] = None, fn: int = HOT_ACT_NONE,
                        ckpt: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
     """y = f(x.w^T + bias) + residual, and the checkpoint of x.w^T + bias; returns y."""
-    tx, ty, dev = _typed("x", x), _typed("y", y), torch.cuda.current_device()
+    tx, ty, dev = _typed("x", x), _typed("y", y), _current_device()
     _typed("w", w)
     (L, I), O = x.shape, w.shape[0]
     st = lib().hot_linear_forward(
@@ -517,9 +539,10 @@ def hot_linear_forward(x: torch.Tensor, w: torch.Tensor, y: torch.Tensor, ws: Op
         None if bias is None else _expect("bias", bias, torch.float32, (O,), dev),
         None if residual is None else _expect("residual", residual, y.dtype, (L, O), dev), L, O, I, int(fn),
         _expect("y", y, y.dtype, (L, O), dev), ty,
-        None if ckpt is None else _bytes("ckpt", ckpt, hot_checkpoint_bytes(L, O), dev),
-        _bytes("ws", ws, 0, dev), 0 if ws is None else ws.numel(), _stream(stream))
-    _check(st, "hot_linear_forward")
+        None if ckpt is None else _ckpt(ckpt, L, O, dev),
+        *((None, 0) if ws is None else (_bytes("ws", ws, 0, dev), ws.numel())), _stream_of(stream, dev))
+    if st:
+        _check(st, "hot_linear_forward")
     return y
 
 

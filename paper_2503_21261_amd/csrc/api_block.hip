@@ -127,11 +127,11 @@ hot_status hot_activation_backward(hot_act_fn fn, const void* g_y, hot_type type
   if (!b.ok()) return HOT_ERR_ARG;
   if (g_bias && ws_bytes < need) return HOT_ERR_WORKSPACE;
   hipStream_t s = (hipStream_t)stream;
-  float* const partials = g_bias ? (float*)ws : nullptr;
-  HOT_STAGE(kStActBackward, launch_activation_grad(fn, g_y, type, x, ckpt, rows, cols, g_x, partials, s));
-  if (g_bias)
-    HOT_STAGE(kStColumnSums, launch_column_sums(partials, activation_sum_rows(rows, cols), round_up(cols, 32), cols, g_bias,
-                                                nullptr, s));
+  const int64_t pitch = round_up(cols, 32);
+  const int sums = activation_sum_rows(rows, cols);
+  float* const partials = !g_bias || sums == 1 ? g_bias : (float*)ws;
+  HOT_STAGE(kStActBackward, launch_activation_grad(fn, g_y, type, x, ckpt, rows, cols, g_x, partials, pitch, s));
+  if (partials != g_bias) HOT_STAGE(kStColumnSums, launch_column_sums(partials, sums, pitch, cols, g_bias, nullptr, s));
   return HOT_OK;
 }
 
@@ -187,11 +187,17 @@ hot_status hot_layer_norm_backward(const void* g_y, hot_type y_type, const void*
   if (!b.ok()) return HOT_ERR_ARG;
   if (g_gamma && ws_bytes < need) return HOT_ERR_WORKSPACE;
   hipStream_t s = (hipStream_t)stream;
-  const NormBackward a{g_y, h, ckpt, g_residual, gamma, mean, rstd, rows, cols, x_type, y_type, g_x, g_gamma ? (float*)ws : nullptr};
+  const int64_t pitch = round_up(cols, 32);
+  const int sums = layer_norm_sum_rows(rows, cols);
+  const bool apart = g_gamma && sums > 1;
+  NormBackward a{g_y, h, ckpt, g_residual, gamma, mean, rstd, rows, cols, x_type, y_type, g_x, g_gamma, g_beta, 0};
+  if (apart) {
+    a.sum_gamma = (float*)ws;
+    a.sum_beta = a.sum_gamma + pitch;
+    a.sum_pitch = 2 * pitch;
+  }
   HOT_STAGE(kStNormBackward, launch_layer_norm_grad(a, s));
-  if (g_gamma)
-    HOT_STAGE(kStColumnSums, launch_column_sums((const float*)ws, layer_norm_sum_rows(rows, cols), 2 * round_up(cols, 32), cols,
-                                                g_gamma, g_beta, s));
+  if (apart) HOT_STAGE(kStColumnSums, launch_column_sums(a.sum_gamma, sums, 2 * pitch, cols, g_gamma, g_beta, s));
   return HOT_OK;
 }
 

@@ -18,7 +18,7 @@ inline CkptLayout ckpt_layout(int64_t rows, int64_t cols) {
 }
 
 // Rows of partial sums that a column sum over `rows` rows leaves, and its width: the gradient kernels
-// write one such row per row group, `column_sums` adds them.
+// write one such row per row group, `column_sums` adds them; a single row is the sum, and goes where that belongs.
 constexpr int kMaxSumRows = 1024;
 int activation_sum_rows(int64_t rows, int64_t cols);
 int layer_norm_sum_rows(int64_t rows, int64_t cols);
@@ -27,9 +27,9 @@ int layer_norm_sum_rows(int64_t rows, int64_t cols);
 hipError_t launch_activation(int fn, const void* x, hot_type type, int64_t rows, int64_t cols, void* y, void* ckpt,
                              hipStream_t s);
 hipError_t launch_checkpoint_read(const void* ckpt, int64_t rows, int64_t cols, void* x, hot_type type, hipStream_t s);
-// g_x = g_y f'(x), x from `x` or from `ckpt`; partials (activation_sum_rows() x pitch floats, may be null): sums of g_x.
+// g_x = g_y f'(x), x from `x` or from `ckpt`; partials (activation_sum_rows() rows, `pitch` floats apart, may be null): sums of g_x.
 hipError_t launch_activation_grad(int fn, const void* g_y, hot_type type, const void* x, const void* ckpt, int64_t rows,
-                                  int64_t cols, void* g_x, float* partials, hipStream_t s);
+                                  int64_t cols, void* g_x, float* partials, int64_t pitch, hipStream_t s);
 // out[c] = sum over r of partials[r * width + c]; the second half of a row, where there is one, goes to out2.
 hipError_t launch_column_sums(const float* partials, int rows, int64_t width, int64_t cols, float* out, float* out2,
                               hipStream_t s);
@@ -51,7 +51,9 @@ struct NormBackward {
   int64_t rows, cols;
   hot_type x_type, y_type;
   void* g_x;
-  float* partials;   // null: no parameter gradients
+  // Row b of sums of workgroup b, at sum_gamma + b * sum_pitch and sum_beta + b * sum_pitch (null: no parameter gradients)
+  float *sum_gamma, *sum_beta;
+  int64_t sum_pitch;
 };
 hipError_t launch_layer_norm_grad(const NormBackward& a, hipStream_t s);
 

@@ -204,16 +204,16 @@ __global__ __launch_bounds__(256) void layer_norm_grad_kernel(const NormBackward
       }
     }
   }
-  if (!a.partials) return;
-  const int64_t pitch = (a.cols + 31) / 32 * 32;
-  float* const out = a.partials + (int64_t)blockIdx.x * 2 * pitch;
+  if (!a.sum_gamma) return;
+  float* const to_gamma = a.sum_gamma + (int64_t)blockIdx.x * a.sum_pitch;
+  float* const to_beta = a.sum_beta + (int64_t)blockIdx.x * a.sum_pitch;
   if constexpr (T == 256) {
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
       const int c = (lane + j * T) * 8;
-      if (c < (int)pitch) {
-        store8(out + c, sg[j], 8);
-        store8(out + pitch + c, sb[j], 8);
+      if (c < cols) {
+        store8(to_gamma + c, sg[j], cols - c);
+        store8(to_beta + c, sb[j], cols - c);
       }
     }
   } else {
@@ -223,7 +223,7 @@ __global__ __launch_bounds__(256) void layer_norm_grad_kernel(const NormBackward
 #pragma unroll
         for (int i = 0; i < 8; ++i) s_sum[slot * SPAN + (lane + j * T) * 8 + i] = s[j][i];
       __syncthreads();
-      for (int c = (int)threadIdx.x; c < SPAN && c < (int)pitch; c += 256) {
+      for (int c = (int)threadIdx.x; c < SPAN && c < cols; c += 256) {
         float total = 0.0f;
 #pragma unroll
         for (int y = 0; y < kSlots<T>; ++y) total += s_sum[y * SPAN + c];
@@ -231,8 +231,8 @@ __global__ __launch_bounds__(256) void layer_norm_grad_kernel(const NormBackward
       }
       __syncthreads();
     };
-    add_slots(sg, out);
-    add_slots(sb, out + pitch);
+    add_slots(sg, to_gamma);
+    add_slots(sb, to_beta);
   }
 }
 
@@ -265,10 +265,11 @@ CkptView view(const void* ckpt, int64_t rows, int64_t cols) {
 
 }  // namespace
 
-// Workgroups of the backward pass, one row of partial sums each: a compute unit's worth while rows are
-// few, four of them once every workgroup has eight turns.
+// Workgroups of the backward pass, one row of partial sums each: one, whose sums are the gradients themselves, while its turns
+// take no longer than a second launch; a compute unit's worth while rows are few, four of them once every workgroup has eight turns.
 int layer_norm_sum_rows(int64_t rows, int64_t cols) {
   const int64_t turns = ceil_div(rows, slots_of(cols));
+  if (turns <= 2) return 1;
   int64_t g = turns < 256 ? turns : 256;
   const int64_t many = turns / 8 < kMaxSumRows ? turns / 8 : kMaxSumRows;
   return (int)(many > g ? many : g);

@@ -45,6 +45,7 @@ Walk make_walk(int64_t rows, int64_t cols) {
 // Row groups of a walk that keeps sums: at most a few workgroups per compute unit, and enough rows for
 // each that the partial sums stay small beside the tensor.
 int sum_groups(const Walk& w) {
+  if (w.batches <= 2) return 1;     // no second launch for sums that one workgroup has
   const int64_t fill = ceil_div(2048, w.col_tiles);
   int64_t g = w.batches < fill ? w.batches : fill;
   return (int)(g > kMaxSumRows ? kMaxSumRows : g);
@@ -138,7 +139,7 @@ __global__ __launch_bounds__(256) void checkpoint_read_kernel(const uint8_t* ckp
 // g_x = g_y f'(x); SUMS: a row of partial sums of g_x (in fp32, before it is rounded to T) per row group.
 template <class T, int FN, bool KEPT, bool SUMS>
 __global__ __launch_bounds__(256) void activation_grad_kernel(const T* g_y, const T* x, const uint8_t* ckpt, Walk w, T* g_x,
-                                                              float* partials) {
+                                                              float* partials, int64_t pitch) {
   __shared__ float s_sum[SUMS ? 256 * 8 : 1];
   Position p;
   int tx, ty, ct, rg;
@@ -193,10 +194,10 @@ __global__ __launch_bounds__(256) void activation_grad_kernel(const T* g_y, cons
     const int width = 8 << w.log_tx;
     for (int c = (int)threadIdx.x; c < width; c += 256) {
       const int at = ct * width + c;
-      if (at >= w.chunks * 8) break;
+      if (at >= w.cols) break;
       float total = 0.0f;
       for (int y = 0; y < step; ++y) total += s_sum[y * width + c];
-      partials[(int64_t)rg * w.chunks * 8 + at] = total;
+      partials[(int64_t)rg * pitch + at] = total;
     }
   }
 }
@@ -237,20 +238,20 @@ hipError_t activation_typed(const T* x, int64_t rows, int64_t cols, T* y, void* 
 
 template <class T, int FN>
 hipError_t grad_typed(const T* g_y, const T* x, const void* ckpt, int64_t rows, int64_t cols, T* g_x, float* partials,
-                      hipStream_t s) {
+                      int64_t pitch, hipStream_t s) {
   Walk w = make_walk(rows, cols);
   const uint8_t* k = (const uint8_t*)ckpt;
   const dim3 block(256);
   if (partials) {
     w.row_groups = sum_groups(w);
     const dim3 grid((unsigned)(w.col_tiles * w.row_groups));
-    if (k) activation_grad_kernel<T, FN, true, true><<<grid, block, 0, s>>>(g_y, x, k, w, g_x, partials);
-    else activation_grad_kernel<T, FN, false, true><<<grid, block, 0, s>>>(g_y, x, k, w, g_x, partials);
+    if (k) activation_grad_kernel<T, FN, true, true><<<grid, block, 0, s>>>(g_y, x, k, w, g_x, partials, pitch);
+    else activation_grad_kernel<T, FN, false, true><<<grid, block, 0, s>>>(g_y, x, k, w, g_x, partials, pitch);
   } else {
     w.row_groups = (int)w.batches;
     const dim3 grid((unsigned)(w.col_tiles * w.batches));
-    if (k) activation_grad_kernel<T, FN, true, false><<<grid, block, 0, s>>>(g_y, x, k, w, g_x, nullptr);
-    else activation_grad_kernel<T, FN, false, false><<<grid, block, 0, s>>>(g_y, x, k, w, g_x, nullptr);
+    if (k) activation_grad_kernel<T, FN, true, false><<<grid, block, 0, s>>>(g_y, x, k, w, g_x, nullptr, 0);
+    else activation_grad_kernel<T, FN, false, false><<<grid, block, 0, s>>>(g_y, x, k, w, g_x, nullptr, 0);
   }
   return hipGetLastError();
 }
@@ -287,11 +288,11 @@ hipError_t launch_checkpoint_read(const void* ckpt, int64_t rows, int64_t cols, 
 }
 
 hipError_t launch_activation_grad(int fn, const void* g_y, hot_type type, const void* x, const void* ckpt, int64_t rows,
-                                  int64_t cols, void* g_x, float* partials, hipStream_t s) {
+                                  int64_t cols, void* g_x, float* partials, int64_t pitch, hipStream_t s) {
   return with_fn(fn, [&](auto f) {
     if (type == HOT_BF16)
-      return grad_typed<bf16, decltype(f)::value>((const bf16*)g_y, (const bf16*)x, ckpt, rows, cols, (bf16*)g_x, partials, s);
-    return grad_typed<float, decltype(f)::value>((const float*)g_y, (const float*)x, ckpt, rows, cols, (float*)g_x, partials, s);
+      return grad_typed<bf16, decltype(f)::value>((const bf16*)g_y, (const bf16*)x, ckpt, rows, cols, (bf16*)g_x, partials, pitch, s);
+    return grad_typed<float, decltype(f)::value>((const float*)g_y, (const float*)x, ckpt, rows, cols, (float*)g_x, partials, pitch, s);
   });
 }
 
