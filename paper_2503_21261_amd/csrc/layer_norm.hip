@@ -7,6 +7,8 @@
 // lane, NV times), so it is read once: the mean first, then the squares of what is left, which keeps the
 // variance of rows whose mean is large.  The backward pass keeps a lane on its columns, so that the
 // parameter gradients are sums in registers; a workgroup leaves one row of them, and column_sums adds those in order.
+#include <type_traits>
+
 #include "block_device.h"
 #include "block_host.h"
 
@@ -15,12 +17,14 @@ namespace hot {
 namespace {
 
 template <int T>
-constexpr int kSlots = 256 / T;   // rows a workgroup works on at a time
+constexpr int kThreads = T > 256 ? T : 256;
+template <int T>
+constexpr int kSlots = kThreads<T> / T;   // rows a workgroup works on at a time
 
-// Sums of two values over the T lanes of a row, in every lane.  T = 256: through LDS, whose halves
+// Sums of two values over the T lanes of a row, in every lane.  T > 64: through LDS, whose halves
 // alternate (`turn`), so that one barrier a call is enough.
 template <int T>
-__device__ __forceinline__ void row_sums(float& a, float& b, float (*s_red)[4][2], int turn) {
+__device__ __forceinline__ void row_sums(float& a, float& b, float (*s_red)[16][2], int turn) {
   constexpr int W = T < 64 ? T : 64;
   a = lanes_sum<W>(a);
   b = lanes_sum<W>(b);
@@ -31,26 +35,32 @@ __device__ __forceinline__ void row_sums(float& a, float& b, float (*s_red)[4][2
       s_red[turn][wave][1] = b;
     }
     __syncthreads();
-    a = (s_red[turn][0][0] + s_red[turn][1][0]) + (s_red[turn][2][0] + s_red[turn][3][0]);
-    b = (s_red[turn][0][1] + s_red[turn][1][1]) + (s_red[turn][2][1] + s_red[turn][3][1]);
+    a = b = 0.0f;
+#pragma unroll
+    for (int i = 0; i < T / 64; ++i) {
+      a += s_red[turn][i][0];
+      b += s_red[turn][i][1];
+    }
   }
 }
 
-template <int T, int NV, class TX, class TY, bool KEEP>
-__global__ __launch_bounds__(256) void layer_norm_kernel(const NormForward a, const CkptView k) {
-  __shared__ float s_red[2][4][2];
+// EVEN: cols is a multiple of eight, so that a lane's chunk is whole or absent.
+template <int T, int NV, class TX, class TY, bool KEEP, bool EVEN>
+__global__ __launch_bounds__(kThreads<T>) void layer_norm_kernel(const NormForward a, const CkptView k) {
+  __shared__ float s_red[2][16][2];
   const int lane = (int)threadIdx.x % T, slot = (int)threadIdx.x / T;
   const int64_t row = (int64_t)blockIdx.x * kSlots<T> + slot;
-  if (row >= a.rows) return;   // T = 256: one row a workgroup, all of it or none
+  if (row >= a.rows) return;   // T > 64: one row a workgroup, all of it or none
   const int cols = (int)a.cols;
+  auto have = [&](int c) { return EVEN ? 8 : cols - c; };
   const int64_t at = row * cols;
   Raw8<TX> xr[NV], rr[NV];
 #pragma unroll
   for (int j = 0; j < NV; ++j) {
     const int c = (lane + j * T) * 8;
     if (c < cols) {
-      xr[j] = load8((const TX*)a.x + at + c, cols - c);
-      if (a.residual) rr[j] = load8((const TX*)a.residual + at + c, cols - c);
+      xr[j] = load8((const TX*)a.x + at + c, have(c));
+      if (a.residual) rr[j] = load8((const TX*)a.residual + at + c, have(c));
     }
   }
   float v[NV][8], sum = 0.0f, none = 0.0f;
@@ -66,7 +76,7 @@ __global__ __launch_bounds__(256) void layer_norm_kernel(const NormForward a, co
         widen(rr[j], r);
 #pragma unroll
         for (int i = 0; i < 8; ++i) v[j][i] = rounded(v[j][i] + r[i], TX(0.0f));
-        if (a.h) store8((TX*)a.h + at + c, v[j], cols - c);
+        if (a.h) store8((TX*)a.h + at + c, v[j], have(c));
       }
     }
     if constexpr (KEEP) {
@@ -83,11 +93,12 @@ __global__ __launch_bounds__(256) void layer_norm_kernel(const NormForward a, co
 #pragma unroll
   for (int j = 0; j < NV; ++j) {
     const int n = cols - (lane + j * T) * 8;
+    if constexpr (EVEN) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) v[j][i] -= mean0;
-    if (n < 8) {
+      for (int i = 0; i < 8; ++i) v[j][i] = n > 0 ? v[j][i] - mean0 : 0.0f;
+    } else {
 #pragma unroll
-      for (int i = 0; i < 8; ++i) v[j][i] = i < n ? v[j][i] : 0.0f;
+      for (int i = 0; i < 8; ++i) v[j][i] = i < n ? v[j][i] - mean0 : 0.0f;
     }
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
@@ -109,8 +120,8 @@ __global__ __launch_bounds__(256) void layer_norm_kernel(const NormForward a, co
     const int c = (lane + j * T) * 8;
     if (c < cols) {
       float g[8], b[8];
-      if (a.gamma) load_values(a.gamma + c, cols - c, g);
-      if (a.beta) load_values(a.beta + c, cols - c, b);
+      if (a.gamma) load_values(a.gamma + c, have(c), g);
+      if (a.beta) load_values(a.beta + c, have(c), b);
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
         float n = (v[j][i] - off) * rstd;
@@ -118,18 +129,19 @@ __global__ __launch_bounds__(256) void layer_norm_kernel(const NormForward a, co
         if (a.beta) n += b[i];
         v[j][i] = n;
       }
-      store8((TY*)a.y + at + c, v[j], cols - c);
+      store8((TY*)a.y + at + c, v[j], have(c));
     }
   }
 }
 
-template <int T, int NV, class TX, class TY, bool KEPT>
-__global__ __launch_bounds__(256) void layer_norm_grad_kernel(const NormBackward a, const CkptView k) {
+template <int T, int NV, class TX, class TY, bool KEPT, bool EVEN>
+__global__ __launch_bounds__(kThreads<T>) void layer_norm_grad_kernel(const NormBackward a, const CkptView k) {
   constexpr int SPAN = T * NV * 8;    // columns the lanes of a row cover
-  __shared__ float s_red[2][4][2];
+  __shared__ float s_red[2][16][2];
   __shared__ float s_sum[T < 256 ? kSlots<T> * SPAN : 1];
   const int lane = (int)threadIdx.x % T, slot = (int)threadIdx.x / T;
   const int cols = (int)a.cols;
+  auto have = [&](int c) { return EVEN ? 8 : cols - c; };
   float gamma[NV][8], sg[NV][8], sb[NV][8];
 #pragma unroll
   for (int j = 0; j < NV; ++j) {
@@ -139,7 +151,7 @@ __global__ __launch_bounds__(256) void layer_norm_grad_kernel(const NormBackward
       sg[j][i] = sb[j][i] = 0.0f;
       gamma[j][i] = a.gamma ? 0.0f : 1.0f;
     }
-    if (a.gamma && c < cols) load_values(a.gamma + c, cols - c, gamma[j]);
+    if (a.gamma && c < cols) load_values(a.gamma + c, have(c), gamma[j]);
   }
   const float inv = 1.0f / (float)cols;
   int turn = 0;
@@ -153,15 +165,15 @@ __global__ __launch_bounds__(256) void layer_norm_grad_kernel(const NormBackward
     for (int j = 0; j < NV; ++j) {
       const int c = (lane + j * T) * 8;
       if (c < cols) {
-        gr[j] = load8((const TY*)a.g_y + at + c, cols - c);
+        gr[j] = load8((const TY*)a.g_y + at + c, have(c));
         if constexpr (KEPT) {
           const int64_t kat = row * k.pitch + c;
           codes[j] = *(const uint2*)(k.codes + kat);
           e[j] = k.exps[kat / kCkGroup];
         } else {
-          hr[j] = load8((const TX*)a.h + at + c, cols - c);
+          hr[j] = load8((const TX*)a.h + at + c, have(c));
         }
-        if (a.g_residual) ar[j] = load8((const TX*)a.g_residual + at + c, cols - c);
+        if (a.g_residual) ar[j] = load8((const TX*)a.g_residual + at + c, have(c));
       }
     }
     const float mean = a.mean[row], rstd = a.rstd[row];
@@ -200,20 +212,20 @@ __global__ __launch_bounds__(256) void layer_norm_grad_kernel(const NormBackward
           const float g = rstd * (t[j][i] - m1 - n[j][i] * m2);
           t[j][i] = a.g_residual ? g + r[i] : g;
         }
-        store8((TX*)a.g_x + at + c, t[j], cols - c);
+        store8((TX*)a.g_x + at + c, t[j], have(c));
       }
     }
   }
   if (!a.sum_gamma) return;
   float* const to_gamma = a.sum_gamma + (int64_t)blockIdx.x * a.sum_pitch;
   float* const to_beta = a.sum_beta + (int64_t)blockIdx.x * a.sum_pitch;
-  if constexpr (T == 256) {
+  if constexpr (T >= 256) {
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
       const int c = (lane + j * T) * 8;
       if (c < cols) {
-        store8(to_gamma + c, sg[j], cols - c);
-        store8(to_beta + c, sb[j], cols - c);
+        store8(to_gamma + c, sg[j], have(c));
+        store8(to_beta + c, sb[j], have(c));
       }
     }
   } else {
@@ -236,7 +248,8 @@ __global__ __launch_bounds__(256) void layer_norm_grad_kernel(const NormBackward
   }
 }
 
-// Lanes to a row: the fewest that hold it with eight columns (sixteen up to 1024) each.
+// Lanes to a row: the fewest that hold it with eight or sixteen columns each.  The gradient's registers, six values a column, leave no
+// room for more: 4000 x 11008 bfloat16 takes 80 us on 1024 lanes, 95 on 256 with 64 columns each, which spill.
 template <class F>
 hipError_t with_lanes(int64_t cols, F&& f) {
   using std::integral_constant;
@@ -246,16 +259,19 @@ hipError_t with_lanes(int64_t cols, F&& f) {
   if (cols <= 1024) return f(integral_constant<int, 64>{}, integral_constant<int, 2>{});
   if (cols <= 2048) return f(integral_constant<int, 256>{}, integral_constant<int, 1>{});
   if (cols <= 4096) return f(integral_constant<int, 256>{}, integral_constant<int, 2>{});
-  if (cols <= 8192) return f(integral_constant<int, 256>{}, integral_constant<int, 4>{});
-  return f(integral_constant<int, 256>{}, integral_constant<int, 8>{});
+  if (cols <= 8192) return f(integral_constant<int, 512>{}, integral_constant<int, 2>{});
+  return f(integral_constant<int, 1024>{}, integral_constant<int, 2>{});
 }
 int slots_of(int64_t cols) { return cols <= 128 ? 16 : cols <= 256 ? 8 : cols <= 1024 ? 4 : 1; }
 
 template <class F>
-hipError_t with_types(hot_type x, hot_type y, F&& f) {
-  if (x == HOT_BF16) return f(bf16(0.0f), bf16(0.0f));
-  if (y == HOT_BF16) return f(0.0f, bf16(0.0f));
-  return f(0.0f, 0.0f);
+hipError_t with_types(hot_type x, hot_type y, bool even, F&& f) {
+  auto go = [&](auto e) {
+    if (x == HOT_BF16) return f(bf16(0.0f), bf16(0.0f), e);
+    if (y == HOT_BF16) return f(0.0f, bf16(0.0f), e);
+    return f(0.0f, 0.0f, e);
+  };
+  return even ? go(std::true_type{}) : go(std::false_type{});
 }
 
 CkptView view(const void* ckpt, int64_t rows, int64_t cols) {
@@ -266,24 +282,27 @@ CkptView view(const void* ckpt, int64_t rows, int64_t cols) {
 }  // namespace
 
 // Workgroups of the backward pass, one row of partial sums each: one, whose sums are the gradients themselves, while its turns
-// take no longer than a second launch; a compute unit's worth while rows are few, four of them once every workgroup has eight turns.
+// take no longer than a second launch; two a compute unit while rows are few; as many as are resident together (their registers:
+// 100, or 160 with sixteen columns a lane) once every workgroup has eight turns, so that none waits for another to end.
 int layer_norm_sum_rows(int64_t rows, int64_t cols) {
   const int64_t turns = ceil_div(rows, slots_of(cols));
   if (turns <= 2) return 1;
-  int64_t g = turns < 256 ? turns : 256;
-  const int64_t many = turns / 8 < kMaxSumRows ? turns / 8 : kMaxSumRows;
+  const int64_t resident = cols > 8192 ? 256 : cols > 4096 ? 512 : (cols > 512 && cols <= 1024) || cols > 2048 ? 768 : 1024;
+  const int64_t few = resident < 512 ? resident : 512;
+  const int64_t g = turns < few ? turns : few, many = turns / 8 < resident ? turns / 8 : resident;
   return (int)(many > g ? many : g);
 }
 
 hipError_t launch_layer_norm(const NormForward& a, hipStream_t s) {
   return with_lanes(a.cols, [&](auto t, auto nv) {
-    return with_types(a.x_type, a.y_type, [&](auto tx, auto ty) {
+    return with_types(a.x_type, a.y_type, a.cols % 8 == 0, [&](auto tx, auto ty, auto e) {
       constexpr int T = decltype(t)::value, NV = decltype(nv)::value;
+      constexpr bool EVEN = decltype(e)::value;
       using TX = decltype(tx);
       using TY = decltype(ty);
-      const dim3 grid((unsigned)ceil_div(a.rows, kSlots<T>)), block(256);
-      if (a.ckpt) layer_norm_kernel<T, NV, TX, TY, true><<<grid, block, 0, s>>>(a, view(a.ckpt, a.rows, a.cols));
-      else layer_norm_kernel<T, NV, TX, TY, false><<<grid, block, 0, s>>>(a, CkptView{});
+      const dim3 grid((unsigned)ceil_div(a.rows, kSlots<T>)), block(kThreads<T>);
+      if (a.ckpt) layer_norm_kernel<T, NV, TX, TY, true, EVEN><<<grid, block, 0, s>>>(a, view(a.ckpt, a.rows, a.cols));
+      else layer_norm_kernel<T, NV, TX, TY, false, EVEN><<<grid, block, 0, s>>>(a, CkptView{});
       return hipGetLastError();
     });
   });
@@ -291,13 +310,14 @@ hipError_t launch_layer_norm(const NormForward& a, hipStream_t s) {
 
 hipError_t launch_layer_norm_grad(const NormBackward& a, hipStream_t s) {
   return with_lanes(a.cols, [&](auto t, auto nv) {
-    return with_types(a.x_type, a.y_type, [&](auto tx, auto ty) {
+    return with_types(a.x_type, a.y_type, a.cols % 8 == 0, [&](auto tx, auto ty, auto e) {
       constexpr int T = decltype(t)::value, NV = decltype(nv)::value;
+      constexpr bool EVEN = decltype(e)::value;
       using TX = decltype(tx);
       using TY = decltype(ty);
-      const dim3 grid((unsigned)layer_norm_sum_rows(a.rows, a.cols)), block(256);
-      if (a.ckpt) layer_norm_grad_kernel<T, NV, TX, TY, true><<<grid, block, 0, s>>>(a, view(a.ckpt, a.rows, a.cols));
-      else layer_norm_grad_kernel<T, NV, TX, TY, false><<<grid, block, 0, s>>>(a, CkptView{});
+      const dim3 grid((unsigned)layer_norm_sum_rows(a.rows, a.cols)), block(kThreads<T>);
+      if (a.ckpt) layer_norm_grad_kernel<T, NV, TX, TY, true, EVEN><<<grid, block, 0, s>>>(a, view(a.ckpt, a.rows, a.cols));
+      else layer_norm_grad_kernel<T, NV, TX, TY, false, EVEN><<<grid, block, 0, s>>>(a, CkptView{});
       return hipGetLastError();
     });
   });
