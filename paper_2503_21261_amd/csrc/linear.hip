@@ -242,7 +242,7 @@ constexpr int kTileLds = kStages * (BM + BN) * kPiece > (BM / WM) * (BN / WN) * 
 template <int BM, int BN, int WM, int WN, bool SPLIT, class TY>
 __global__ __launch_bounds__(64 * (BM / WM) * (BN / WN), WM * WN > 64 * 128 ? 1 : 2) void linear_tile_kernel(const TileArgs g) {
   constexpr int WAVES_M = BM / WM, WAVES = WAVES_M * (BN / WN);
-  constexpr int TM = WM / 32, TN = WN / 32;
+  constexpr int TM = WM / 16, TN = WN / 16;
   constexpr int XL = BM / 8 / WAVES, WL = BN / 8 / WAVES;   // loads of a wave and stage: 8 rows each
   static_assert(BM % (8 * WAVES) == 0 && BN % (8 * WAVES) == 0, "loads");
   constexpr int STAGE = (BM + BN) * kPiece;
@@ -284,41 +284,36 @@ __global__ __launch_bounds__(64 * (BM / WM) * (BN / WN), WM * WN > 64 * 128 ? 1 
   auto load_stage = [&](int kt) { static_for<XL + WL>([&](auto e) { load_one(kt, e); }); };
 
   const int wm0 = wave % WAVES_M * WM, wn0 = wave / WAVES_M * WN;
-  int off_q[4];     // a quarter of a stage: chunks 2 q and 2 q + 1 of a row, one for each half of the lanes
+  // A fragment: 16 rows, the lane's 16 bytes of row lane % 16.  The two of a row in a stage: bfloat16, the 32 elements of its first and
+  // of its second half; fp32, the 32 high parts and the 32 low ones.
+  int off_f[2];
 #pragma unroll
-  for (int q = 0; q < 4; ++q) off_q[q] = (lane & 31) * kPiece + 16 * ((2 * q + (lane >> 5)) ^ (lane & 7));
-  struct Frags {
-    v4i x[TM], w[TN];
-  };
-  constexpr int NM = TM * TN, NR = TM + TN, NL = XL + WL;
-  auto read_one = [&](int kt, auto qc, Frags& f, auto ec) {
-    constexpr int e = decltype(ec)::value;
-    const uint8_t* const b = smem + (kt & (kStages - 1)) * STAGE + off_q[decltype(qc)::value];
-    if constexpr (e < TM) f.x[e] = *(const v4i*)(b + (wm0 + e * 32) * kPiece);
-    else f.w[e - TM] = *(const v4i*)(b + (BM + wn0 + (e - TM) * 32) * kPiece);
-  };
-  v16f acc[TM][TN];
+  for (int h = 0; h < 2; ++h) {
+    const int g = lane >> 4, chunk = SPLIT ? (g >> 1) * 4 + (g & 1) + 2 * h : 4 * h + g;
+    off_f[h] = (lane & 15) * kPiece + 16 * (chunk ^ (lane & 7));
+  }
+  using std::integral_constant;
+  auto fragment = [&](int kt, int h, int row) { return *(const v4i*)(smem + (kt & (kStages - 1)) * STAGE + off_f[h] + row * kPiece); };
+  auto read_x = [&](int kt, int h, v4i(&f)[TM], auto ic) { f[decltype(ic)::value] = fragment(kt, h, wm0 + decltype(ic)::value * 16); };
+  auto read_w = [&](int kt, int h, v4i(&f)[TN], auto jc) { f[decltype(jc)::value] = fragment(kt, h, BM + wn0 + decltype(jc)::value * 16); };
+  v4f acc[TM][TN];
 #pragma unroll
   for (int i = 0; i < TM; ++i)
 #pragma unroll
-    for (int j = 0; j < TN; ++j)
-#pragma unroll
-      for (int v = 0; v < 16; ++v) acc[i][j][v] = 0.0f;
-  auto multiply_one = [&](const v4i& w, const v4i& x, v16f& c) {
-    if constexpr (SPLIT) c = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(v8h, w), __builtin_bit_cast(v8h, x), c, 0, 0, 0);
-    else c = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(v8bf, w), __builtin_bit_cast(v8bf, x), c, 0, 0, 0);
+    for (int j = 0; j < TN; ++j) acc[i][j] = v4f{0, 0, 0, 0};
+  auto multiply_one = [&](const v4i& w, const v4i& x, v4f& c) {
+    if constexpr (SPLIT) c = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(v8h, w), __builtin_bit_cast(v8h, x), c, 0, 0, 0);
+    else c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(v8bf, w), __builtin_bit_cast(v8bf, x), c, 0, 0, 0);
   };
-  // COUNT matrix instructions with EVENTS memory instructions pinned between the first of them: the compiler would
-  // gather the reads in front of their use.  The last SLACK matrix instructions have none, so that the reads are there
-  // when the next ones want them.
-  auto interleave = [&](auto count, auto events, auto&& mfma, auto&& event) {
-    constexpr int COUNT = decltype(count)::value, EVENTS = decltype(events)::value, SLACK = COUNT > 4 ? 3 : 1, OVER = COUNT - SLACK;
+  // Products of all tiles, token tile by token tile, with event(q) pinned in front of the q-th: the compiler would gather the LDS
+  // reads in front of their use.
+  constexpr int NM = TM * TN, NL = XL + WL;
+  auto products = [&](const v4i(&w)[TN], v4i(&x)[TM], auto&& event) {
     __builtin_amdgcn_sched_barrier(0);
-    static_for<COUNT>([&](auto qc) {
-      constexpr int q = decltype(qc)::value;
-      constexpr int E0 = q < OVER ? (q * EVENTS + OVER - 1) / OVER : EVENTS, E1 = q + 1 < OVER ? ((q + 1) * EVENTS + OVER - 1) / OVER : EVENTS;
-      static_for<E1 - E0>([&](auto dc) { event(std::integral_constant<int, E0 + decltype(dc)::value>{}); });
-      mfma(qc);
+    static_for<NM>([&](auto q) {
+      constexpr int i = decltype(q)::value / TN, j = decltype(q)::value % TN;
+      event(q);
+      multiply_one(w[j], x[i], acc[i][j]);
       __builtin_amdgcn_sched_barrier(0);
     });
   };
@@ -328,73 +323,65 @@ __global__ __launch_bounds__(64 * (BM / WM) * (BN / WN), WM * WN > 64 * 128 ? 1 
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
   };
-  using std::integral_constant;
-  Frags fa, fb, fc;
-  // Matrix instructions of one quarter (bfloat16) or of one half of the pair of parts (fp32), and what is fetched meanwhile.
-  auto whole = [&](Frags& f, auto events, auto&& event) {
-    interleave(integral_constant<int, NM>{}, events, [&](auto q) { multiply_one(f.w[q % TN], f.x[q / TN], acc[q / TN][q % TN]); }, event);
+  // Events: the e-th of a list of N in front of product FIRST + e * STEP ...
+  auto at = [](auto q, auto first, auto step, auto n, auto&& f) {
+    constexpr int d = decltype(q)::value - decltype(first)::value, S = decltype(step)::value;
+    if constexpr (d >= 0 && d % S == 0 && d / S < decltype(n)::value) f(integral_constant<int, d / S>{});
   };
-  auto crossed = [&](Frags& high, Frags& low, auto events, auto&& event) {
-    interleave(integral_constant<int, 2 * NM>{}, events,
-               [&](auto q) {
-                 constexpr int p = decltype(q)::value % NM, i = p / TN, j = p % TN;
-                 if constexpr (decltype(q)::value < NM) multiply_one(high.w[j], low.x[i], acc[i][j]);
-                 else multiply_one(low.w[j], high.x[i], acc[i][j]);
-               },
-               event);
-  };
-  const integral_constant<int, NR> reads;
-  const integral_constant<int, NL + NR> loads_and_reads;
-  const integral_constant<int, 0> q0;
-  const integral_constant<int, 1> q1;
-  const integral_constant<int, 2> q2;
-  const integral_constant<int, 3> q3;
+#define HOT_INT(V) integral_constant<int, (V)>{}
   load_stage(0);
   load_stage(1);
   asm volatile("s_waitcnt vmcnt(%0)" : : "n"(NL) : "memory");   // the first stage
   __builtin_amdgcn_s_barrier();
   asm volatile("" ::: "memory");
-  static_for<NR>([&](auto e) { read_one(0, q0, fa, e); });
-  for (int kt = 0; kt < nk; ++kt) {
-    // behind the last stage comes a repeated one, whose first quarter is read and not used
-    auto next = [&](Frags& f) {
-      return [&, kt](auto e) {
-        if constexpr (decltype(e)::value < NR) read_one(kt + 1, q0, f, e);
-        else load_one(kt + 2, integral_constant<int, decltype(e)::value - NR>{});
-      };
-    };
-    if constexpr (SPLIT) {
-      whole(fa, reads, [&](auto e) { read_one(kt, q1, fb, e); });
-      crossed(fa, fb, reads, [&](auto e) { read_one(kt, q2, fc, e); });
-      whole(fc, reads, [&](auto e) { read_one(kt, q3, fb, e); });
+  v4i wa[TN], wb[TN], xa[TM];
+  static_for<TN>([&](auto j) { read_w(0, 0, wa, j); });
+  static_for<TM>([&](auto i) { read_x(0, 0, xa, i); });
+  if constexpr (!SPLIT) {
+    for (int kt = 0; kt < nk; ++kt) {
+      // a token tile's fragment is read anew once its products are issued
+      products(wa, xa, [&](auto q) {
+        at(q, HOT_INT(0), HOT_INT(NM / 2 / TN), HOT_INT(TN), [&](auto j) { read_w(kt, 1, wb, j); });
+        at(q, HOT_INT(TN), HOT_INT(TN), HOT_INT(TM - 1), [&](auto i) { read_x(kt, 1, xa, i); });
+      });
+      read_x(kt, 1, xa, HOT_INT(TM - 1));
+      // behind the last stage comes a repeated one, whose first half is read and not used
+      products(wb, xa, [&](auto q) {
+        if constexpr (decltype(q)::value == TN) meet();
+        at(q, HOT_INT(TN), HOT_INT(TN > 4 ? 2 : 1), HOT_INT(TN), [&](auto j) { read_w(kt + 1, 0, wa, j); });
+        at(q, HOT_INT(TN), HOT_INT(TN), HOT_INT(TM - 1), [&](auto i) { read_x(kt + 1, 0, xa, i); });
+        at(q, HOT_INT(TN + 1), HOT_INT(TN > 4 ? 2 : 1), HOT_INT(NL), [&](auto e) { load_one(kt + 2, e); });
+      });
+      read_x(kt + 1, 0, xa, HOT_INT(TM - 1));
+    }
+  } else {
+    v4i xb[TM];
+    for (int kt = 0; kt < nk; ++kt) {
+      products(wa, xa, [&](auto q) {
+        at(q, HOT_INT(0), HOT_INT(1), HOT_INT(TM), [&](auto i) { read_x(kt, 1, xb, i); });
+        at(q, HOT_INT(TM), HOT_INT(1), HOT_INT(TN), [&](auto j) { read_w(kt, 1, wb, j); });
+      });
       meet();
-      crossed(fc, fb, loads_and_reads, next(fa));
-    } else {
-      whole(fa, reads, [&](auto e) { read_one(kt, q1, fb, e); });
-      whole(fb, reads, [&](auto e) { read_one(kt, q2, fa, e); });
-      whole(fa, reads, [&](auto e) { read_one(kt, q3, fb, e); });
-      meet();
-      whole(fb, loads_and_reads, next(fa));
+      products(wa, xb, [&](auto q) { at(q, HOT_INT(0), HOT_INT(NM / NL), HOT_INT(NL), [&](auto e) { load_one(kt + 2, e); }); });
+      products(wb, xa, [&](auto q) {
+        at(q, HOT_INT(0), HOT_INT(NM / 2 / TN), HOT_INT(TN), [&](auto j) { read_w(kt + 1, 0, wa, j); });
+        at(q, HOT_INT(TN), HOT_INT(TN), HOT_INT(TM - 1), [&](auto i) { read_x(kt + 1, 0, xa, i); });
+      });
+      read_x(kt + 1, 0, xa, HOT_INT(TM - 1));
     }
   }
+#undef HOT_INT
   asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
   __builtin_amdgcn_s_barrier();
   asm volatile("" ::: "memory");
 
   if (sliced) {
-    // 16 bytes a lane and quarter of an accumulator tile, as linear_combine_kernel reads them
+    // 16 bytes a lane and accumulator tile, as linear_combine_kernel reads them
     float* const image = g.images + ((int64_t)tail * g.slices + z) * (BM * BN) + tid * 4;
 #pragma unroll
     for (int i = 0; i < TM; ++i)
 #pragma unroll
-      for (int j = 0; j < TN; ++j)
-#pragma unroll
-        for (int q = 0; q < 4; ++q) {
-          v4f part4;
-#pragma unroll
-          for (int r = 0; r < 4; ++r) part4[r] = acc[i][j][4 * q + r];
-          *(v4f*)(image + ((i * TN + j) * 4 + q) * (256 * WAVES)) = part4;
-        }
+      for (int j = 0; j < TN; ++j) *(v4f*)(image + (i * TN + j) * (256 * WAVES)) = acc[i][j];
     return;
   }
   // CB columns of 64 / CH tokens at a time: as long runs of a row as the wave's columns divide into
@@ -402,17 +389,12 @@ __global__ __launch_bounds__(64 * (BM / WM) * (BN / WN), WM * WN > 64 * 128 ? 1 
   static_assert(WN % CB == 0, "column blocks");
   float* const strip = (float*)smem + wave * 32 * PITCH;
 #pragma unroll
-  for (int i = 0; i < TM; ++i) {
-    // accumulator register v of a 32 x 32 tile: output 8 (v / 4) + 4 (lane / 32) + v % 4, token lane % 32
+  for (int i = 0; i < TM / 2; ++i) {
+    // accumulator register r of a 16 x 16 tile: output 4 (lane / 16) + r, token lane % 16
 #pragma unroll
-    for (int j = 0; j < TN; ++j)
+    for (int h = 0; h < 2; ++h)
 #pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        v4f part;
-#pragma unroll
-        for (int r = 0; r < 4; ++r) part[r] = acc[i][j][4 * q + r];
-        *(v4f*)&strip[(lane & 31) * PITCH + j * 32 + 8 * q + 4 * (lane >> 5)] = part;
-      }
+      for (int j = 0; j < TN; ++j) *(v4f*)&strip[(h * 16 + (lane & 15)) * PITCH + j * 16 + 4 * (lane >> 4)] = acc[2 * i + h][j];
     __builtin_amdgcn_wave_barrier();
 #pragma unroll 1
     for (int cb = 0; cb < WN; cb += CB) {
@@ -450,32 +432,32 @@ __global__ __launch_bounds__(64 * (BM / WM) * (BN / WN), WM * WN > 64 * 128 ? 1 
   }
 }
 
-// The sums of a tile's slices, in slice order, and the epilogue.  A thread takes eight outputs of a token: the quarters of lanes l
-// and l + 32 of a 32 x 32 accumulator tile; four threads its 32 outputs.  Bound by the images' way through the caches.
+// The sums of a tile's slices, in slice order, and the epilogue.  A thread takes eight outputs of a token: those of lanes l + 32 h and
+// l + 32 h + 16 of a 16 x 16 accumulator tile; four threads its 32 outputs.  Bound by the images' way through the caches.
 template <int BM, int BN, int WM, int WN, bool SPLIT, class TY>
 __global__ __launch_bounds__(256) void linear_combine_kernel(const TileArgs g) {
-  constexpr int WAVES_M = BM / WM, WAVES = WAVES_M * (BN / WN), TN = WN / 32;
+  constexpr int WAVES_M = BM / WM, WAVES = WAVES_M * (BN / WN), TN = WN / 16;
   constexpr int PER_TILE = BM * BN / 2048;    // workgroups of a tile
   const int tail = (int)blockIdx.x / PER_TILE;
-  const int sub = (int)blockIdx.x % PER_TILE * 2 + ((int)threadIdx.x >> 7);      // 32 x 32 accumulator tile: wave fastest
-  const int q = (int)threadIdx.x & 3, l = ((int)threadIdx.x >> 2) & 31;
-  const int wave = sub % WAVES, ij = sub / WAVES;
+  const int sub = (int)blockIdx.x % PER_TILE * 4 + ((int)threadIdx.x >> 6);      // 16 tokens x 32 outputs: wave fastest
+  const int q = (int)threadIdx.x & 3, l = ((int)threadIdx.x >> 2) & 15;
+  const int wave = sub % WAVES, i = sub / WAVES / (TN / 2), j = sub / WAVES % (TN / 2) * 2 + (q >> 1), h = q & 1;
   int tm, tn;
   tile_at(g.whole + tail, g.tiles_m, g.tiles_n, tm, tn);
-  const float* const image = g.images + (int64_t)tail * g.slices * (BM * BN) + (ij * 4 + q) * (256 * WAVES) + (wave * 64 + l) * 4;
+  const float* const image = g.images + (int64_t)tail * g.slices * (BM * BN) + (i * TN + j) * (256 * WAVES) + (wave * 64 + h * 32 + l) * 4;
   float v[8] = {};
 #pragma unroll 4
   for (int z = 0; z < g.slices; ++z) {
     const float* const p = image + (int64_t)z * (BM * BN);
-    const v4f lo = *(const v4f*)p, hi = *(const v4f*)(p + 128);
+    const v4f lo = *(const v4f*)p, hi = *(const v4f*)(p + 64);
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
       v[e] += lo[e];
       v[e + 4] += hi[e];
     }
   }
-  const int64_t row = (int64_t)tm * BM + wave % WAVES_M * WM + ij / TN * 32 + l;
-  const int c = tn * BN + wave / WAVES_M * WN + ij % TN * 32 + 8 * q, n = g.out.O - c;
+  const int64_t row = (int64_t)tm * BM + wave % WAVES_M * WM + i * 16 + l;
+  const int c = tn * BN + wave / WAVES_M * WN + j * 16 + 8 * h, n = g.out.O - c;
   if (row >= g.out.L) return;
   float bias[8];
   load_bias8(g.out, c, n, bias);
