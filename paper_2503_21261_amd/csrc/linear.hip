@@ -224,7 +224,7 @@ __device__ __forceinline__ void load_to_lds(rsrc_t from, uint8_t* to, int lane_o
 
 struct TileArgs {
   const uint8_t *x, *w;       // operand rows
-  int64_t pitch;              // bytes of one, a multiple of 64
+  int64_t pitch;              // bytes of one, a multiple of 128 (16 in the direct modes)
   const int *ex, *ew;         // fp32: exponents of the rows' scales
   int tiles_m, tiles_n;
   int whole;                  // tiles with a workgroup each; every other one has `slices`, which leave their sums in
@@ -239,8 +239,19 @@ template <int BM, int BN, int WM, int WN>
 constexpr int kTileLds = kStages * (BM + BN) * kPiece > (BM / WM) * (BN / WN) * 32 * (WN + 4) * 4
                              ? kStages * (BM + BN) * kPiece : (BM / WM) * (BN / WN) * 32 * (WN + 4) * 4;
 
-template <int BM, int BN, int WM, int WN, bool SPLIT, class TY>
-__global__ __launch_bounds__(64 * (BM / WM) * (BN / WN), WM * WN > 64 * 128 ? 1 : 2) void linear_tile_kernel(const TileArgs g) {
+// What a tile's operand rows are.
+enum TileMode {
+  kBf16Rows = 0,      // bfloat16, a whole number of pieces
+  kSplitRows = 1,     // fp32 in two fp16 parts, a whole number of pieces
+  // x and w as they are: rows of any whole number of 16 bytes, the last piece masked.  Small tiles, several workgroups a compute unit,
+  // for products that are over before operands could be packed; fp32 on v_mfma_f32_16x16x4_f32.
+  kBf16Direct = 2,
+  kF32Direct = 3,
+};
+
+template <int BM, int BN, int WM, int WN, int MODE, class TY>
+__global__ __launch_bounds__(64 * (BM / WM) * (BN / WN), 2) void linear_tile_kernel(const TileArgs g) {
+  constexpr bool SPLIT = MODE == kSplitRows, DIRECT = MODE >= kBf16Direct;
   constexpr int WAVES_M = BM / WM, WAVES = WAVES_M * (BN / WN);
   constexpr int TM = WM / 16, TN = WN / 16;
   constexpr int XL = BM / 8 / WAVES, WL = BN / 8 / WAVES;   // loads of a wave and stage: 8 rows each
@@ -256,7 +267,7 @@ __global__ __launch_bounds__(64 * (BM / WM) * (BN / WN), WM * WN > 64 * 128 ? 1 
   tile_at(sliced ? g.whole + tail : xcd_contiguous((int)blockIdx.x, g.whole), g.tiles_m, g.tiles_n, tm, tn);
   const int64_t m0 = (int64_t)tm * BM;
   const int n0 = tn * BN;
-  const int stages = (int)(g.pitch / kPiece);
+  const int stages = (int)((g.pitch + kPiece - 1) / kPiece);
   const int k_first = sliced ? (int)((int64_t)stages * z / g.slices) : 0;
   const int nk = sliced ? (int)((int64_t)stages * (z + 1) / g.slices) - k_first : stages;
 
@@ -303,6 +314,11 @@ __global__ __launch_bounds__(64 * (BM / WM) * (BN / WN), WM * WN > 64 * 128 ? 1 
     for (int j = 0; j < TN; ++j) acc[i][j] = v4f{0, 0, 0, 0};
   auto multiply_one = [&](const v4i& w, const v4i& x, v4f& c) {
     if constexpr (SPLIT) c = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(v8h, w), __builtin_bit_cast(v8h, x), c, 0, 0, 0);
+    else if constexpr (MODE == kF32Direct)
+      static_for<4>([&](auto e) {
+        constexpr int E = decltype(e)::value;
+        c = __builtin_amdgcn_mfma_f32_16x16x4f32(__int_as_float(w[E]), __int_as_float(x[E]), c, 0, 0, 0);
+      });
     else c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(v8bf, w), __builtin_bit_cast(v8bf, x), c, 0, 0, 0);
   };
   // Products of all tiles, token tile by token tile, with event(q) pinned in front of the q-th: the compiler would gather the LDS
@@ -337,7 +353,34 @@ __global__ __launch_bounds__(64 * (BM / WM) * (BN / WN), WM * WN > 64 * 128 ? 1 
   v4i wa[TN], wb[TN], xa[TM];
   static_for<TN>([&](auto j) { read_w(0, 0, wa, j); });
   static_for<TM>([&](auto i) { read_x(0, 0, xa, i); });
-  if constexpr (!SPLIT) {
+  if constexpr (DIRECT) {
+    v4i xb[TM];
+    // chunks past a row's end hold what follows the row: both operands' are zero
+    auto mask = [&](int kt, int h, v4i(&w)[TN], v4i(&x)[TM]) {
+      if ((int64_t)(k_first + kt + 1) * kPiece <= g.pitch) return;     // the same in all lanes
+      const bool keep = (int64_t)(k_first + kt) * kPiece + (4 * h + (lane >> 4)) * 16 < g.pitch;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+#pragma unroll
+        for (int j = 0; j < TN; ++j) w[j][e] = keep ? w[j][e] : 0;
+#pragma unroll
+        for (int i = 0; i < TM; ++i) x[i][e] = keep ? x[i][e] : 0;
+      }
+    };
+    auto nothing = [](auto) {};
+    for (int kt = 0; kt < nk; ++kt) {
+      static_for<TN>([&](auto j) { read_w(kt, 1, wb, j); });
+      static_for<TM>([&](auto i) { read_x(kt, 1, xb, i); });
+      mask(kt, 0, wa, xa);
+      products(wa, xa, nothing);
+      meet();
+      load_stage(kt + 2);
+      static_for<TN>([&](auto j) { read_w(kt + 1, 0, wa, j); });
+      static_for<TM>([&](auto i) { read_x(kt + 1, 0, xa, i); });
+      mask(kt, 1, wb, xb);
+      products(wb, xb, nothing);
+    }
+  } else if constexpr (!SPLIT) {
     for (int kt = 0; kt < nk; ++kt) {
       // a token tile's fragment is read anew once its products are issued
       products(wa, xa, [&](auto q) {
@@ -434,8 +477,9 @@ __global__ __launch_bounds__(64 * (BM / WM) * (BN / WN), WM * WN > 64 * 128 ? 1 
 
 // The sums of a tile's slices, in slice order, and the epilogue.  A thread takes eight outputs of a token: those of lanes l + 32 h and
 // l + 32 h + 16 of a 16 x 16 accumulator tile; four threads its 32 outputs.  Bound by the images' way through the caches.
-template <int BM, int BN, int WM, int WN, bool SPLIT, class TY>
+template <int BM, int BN, int WM, int WN, int MODE, class TY>
 __global__ __launch_bounds__(256) void linear_combine_kernel(const TileArgs g) {
+  constexpr bool SPLIT = MODE == kSplitRows;
   constexpr int WAVES_M = BM / WM, WAVES = WAVES_M * (BN / WN), TN = WN / 16;
   constexpr int PER_TILE = BM * BN / 2048;    // workgroups of a tile
   const int tail = (int)blockIdx.x / PER_TILE;
@@ -600,33 +644,41 @@ TileLayout tile_layout(hot_type type, int64_t L, int64_t O, int64_t I) {
 // How a product is worked on.
 struct Plan {
   bool tiles;          // else linear_rows_kernel
-  int size;            // tile: 256 x 256, one workgroup a compute unit, or 128 x 128, two
+  bool direct;         // small tiles of x and w as they are
+  int bm, bn;          // tile: 256 x 256, one workgroup a compute unit, 128 x 128, two, or, direct, 64 x 64 or 32 x 128
   int64_t tiles_m, tiles_n;
   int64_t whole;       // tiles with a workgroup each; the rest in `slices` slices of K
   int slices;
   int nt, mt;          // linear_rows_kernel: 16 nt outputs and 16 mt tokens a workgroup
 };
 
-// Times in microseconds of the ways to do a product, for the choice between them.  The constants are a fit to 1900 launches of all
-// three kernels over 500 random shapes (1 to 60000 rows, widths of 64 to 11008, both types, every split below); the way they choose takes
-// 1.025 times the best one's time on average, 1.4 times at worst.  A second launch also costs the caller's thread.
-constexpr double kLaunch = 3.0;
+// Times in microseconds of the ways to do a product, for the choice between them.  The constants are a fit to 4000 launches of all
+// kernels over 700 random shapes (1 to 60000 rows, widths of 64 to 11008, both types, every split below); the way they choose takes
+// 1.02 times the best one's time on average, 1.5 times at worst, and 0.3 us of the host's.  A second launch costs the caller's
+// thread as well.
+constexpr double kLaunch = 2.5;
+// Two resources used beside each other: little more than the longer time.
+double beside(double a, double b) { return sqrt(sqrt(a * a * a * a + b * b * b * b)); }
+
+// Workgroups that the busiest compute unit has; for many of them, as they come and go, half a workgroup more than the mean.
+double rounds_of(int64_t n) { return n <= 1024 ? (double)ceil_div(n, 256) : n / 256.0 + 0.5; }
 
 // Tiles: a stage of 128 bytes of K in a round of workgroups, what a round takes besides (filling the buffers, the epilogue), the
 // outputs, the images' way to memory and back.
 double tile_time(int size, hot_type type, int64_t L, int64_t O, int64_t stages, Plan* p) {
   const bool big = size == 256, f32 = type == HOT_F32;
   const int64_t slots = big ? 256 : 512;
+  *p = Plan{};
   p->tiles = true;
-  p->size = size;
+  p->bm = p->bn = size;
   p->tiles_m = ceil_div(L, size);
   p->tiles_n = ceil_div(O, size);
   const int64_t count = p->tiles_m * p->tiles_n, rest = count % slots;
   p->whole = count;
   p->slices = 1;
-  const double full = big ? (f32 ? 1.34 : 1.08) : (f32 ? 1.38 : 0.96);    // a stage with every slot taken
-  const double half = big ? full : (f32 ? 0.57 : 0.54);                   // 128 x 128, one workgroup a compute unit
-  const double round = big ? (f32 ? 15.4 : 11.8) : (f32 ? 9.3 : 7.8);
+  const double full = big ? (f32 ? 1.37 : 1.06) : (f32 ? 1.23 : 0.96);    // a stage with every slot taken
+  const double half = big ? full : (f32 ? 0.54 : 0.50);                   // 128 x 128, one workgroup a compute unit
+  const double round = big ? (f32 ? 11.7 : 8.9) : (f32 ? 4.1 : 3.1);
   double t = (count / slots) * (stages * full + round);
   if (rest) {
     int64_t most = slots / rest;                            // slices that still fill one round,
@@ -636,7 +688,7 @@ double tile_time(int size, hot_type type, int64_t L, int64_t O, int64_t stages, 
     for (int64_t k = 1; k <= (most > 1 ? most : 1); ++k) {
       const int64_t n = rest * k;
       const double stage = big || n <= 256 ? half : half + (full - half) * (double)(n - 256) / 256;
-      const double e = ceil_div(stages, k) * stage + round + (k > 1 ? kLaunch + (double)n * size * size * 8 / (big ? 6.4e6 : 3.8e6) : 0.0);
+      const double e = ceil_div(stages, k) * stage + round + (k > 1 ? kLaunch + (double)n * size * size * 8 / (big ? 6.9e6 : 4.6e6) : 0.0);
       if (e < best) {
         best = e;
         p->slices = (int)k;
@@ -645,7 +697,7 @@ double tile_time(int size, hot_type type, int64_t L, int64_t O, int64_t stages, 
     }
     t += best;
   }
-  return t + (double)L * O / 3e6;
+  return (big ? 2.4 : 4.5) + t + (double)L * O / 3e6;
 }
 
 // linear_rows_kernel: a compute unit's matrix instructions and loads, both in units of 2000 cycles' worth a microsecond and for as many
@@ -653,9 +705,9 @@ double tile_time(int size, hot_type type, int64_t L, int64_t O, int64_t stages, 
 // 4-byte aligned, which costs their loads three times the time.
 double rows_time(hot_type type, int64_t L, int64_t O, int64_t I, Plan* p) {
   const bool f32 = type == HOT_F32;
-  const double hbm = ((double)O * I + (double)L * I) * (f32 ? 4 : 2) / (f32 ? 5.8e6 : 9e6) + (double)L * O * 4 / (f32 ? 5.8e6 : 9e6);
+  const double hbm = ((double)O * I + (double)L * I) * (f32 ? 4 : 2) / 9e6 + (double)L * O * 4 / 9e6;
   const int64_t turn = kWaves * kSteps * (f32 ? 16 : 32);    // elements of K a workgroup has on their way
-  const double odd = !f32 && I % 2 ? 3.2 : 1.0;
+  const double odd = !f32 && I % 2 ? 3.0 : 1.0;
   double best = 1e30;
   for (int nt = 1; nt <= 2; ++nt)
     for (int mt = 1; mt <= 4; mt *= 2) {
@@ -663,44 +715,84 @@ double rows_time(hot_type type, int64_t L, int64_t O, int64_t I, Plan* p) {
       const int64_t tm = ceil_div(L, 16 * mt), tn = ceil_div(O, 16 * nt);
       for (int s = 1; s <= 16; ++s) {
         if (s > 1 && (tm * tn * s > 512 || I / s < turn)) break;
-        const double rounds = tm * tn * s > 256 ? tm * tn * s / 256.0 : 1.0;
         const double k = (double)I / s * odd / 2000;
-        const double cu = rounds * (f32 ? k * (1.62 * nt * mt + 2.33 * (nt + mt)) + 0.44 * nt * mt
-                                        : k * (0.21 * nt * mt + 1.46 * (nt + mt)) + 0.39 * nt * mt);
-        const double t = 5.3 + sqrt(cu * cu + hbm * hbm) + (s > 1 ? kLaunch + 2.0 + (double)s * L * O * 8 / 4e6 : 0.0);
+        const double cu = rounds_of(tm * tn * s) * (f32 ? k * (1.82 * nt * mt + 1.94 * (nt + mt)) + 0.38 * nt * mt
+                                        : k * (0.253 * nt * mt + 1.23 * (nt + mt)) + 0.265 * nt * mt);
+        const double t = (f32 ? 5.2 + sqrt(cu * cu + hbm * hbm) : 5.7 + beside(cu, hbm)) + (s > 1 ? kLaunch + 2.3 + (double)s * L * O * 8 / 4e6 : 0.0);
         if (t < best) {
           best = t;
-          *p = Plan{false, 0, tm, tn, 0, s, nt, mt};
+          *p = Plan{};
+          p->tiles_m = tm;
+          p->tiles_n = tn;
+          p->slices = s;
+          p->nt = nt;
+          p->mt = mt;
         }
       }
     }
   return best;
 }
 
+// Small tiles of the operands as they are: a compute unit's matrix instructions and loads, the time of a workgroup by itself.
+double direct_time(int bm, int bn, hot_type type, int64_t L, int64_t O, int64_t I, Plan* p) {
+  const bool f32 = type == HOT_F32;
+  const int64_t bytes = I * (f32 ? 4 : 2), stages = ceil_div(bytes, kPiece);
+  *p = Plan{};
+  p->tiles = p->direct = true;
+  p->bm = bm;
+  p->bn = bn;
+  p->tiles_m = ceil_div(L, bm);
+  p->tiles_n = ceil_div(O, bn);
+  p->slices = 1;
+  const int64_t count = p->tiles_m * p->tiles_n;
+  p->whole = count;
+  const double moved = (((double)L + O) * bytes + (double)L * O * 4) / (f32 ? 49e6 : 15e6);
+  double best = 1e30;
+  for (int64_t k = 1; k <= 16; ++k) {
+    if (k > 1 && (count * k > 1024 || stages / k < 4)) break;
+    const int64_t n = count * k, each = ceil_div(stages, k);
+    const double cu = rounds_of(n) * (f32 ? each * 0.484 + 0.90 : each * 0.149 + 0.39), one = each * (f32 ? 0.461 : 0.235);
+    const double t = 5.3 + beside(cu, one) + moved + (k > 1 ? kLaunch + 3.0 + (double)n * bm * bn * 8 / 5.5e6 : 0.0);
+    if (t < best) {
+      best = t;
+      p->slices = (int)k;
+      p->whole = k > 1 ? 0 : count;
+    }
+  }
+  return best;
+}
+
 Plan make_plan(hot_type type, int64_t L, int64_t O, int64_t I) {
   const TileLayout lay = tile_layout(type, L, O, I);
   const bool f32 = type == HOT_F32;
-  Plan rows{}, a{}, b{};
+  Plan rows{}, a{}, b{}, c{}, d{};
   const double tr = rows_time(type, L, O, I, &rows);
   if (lay.pitch * 256 >= (1ll << 31)) return rows;     // a tile's rows must be within the reach of a buffer descriptor
-  const double operands = lay.packed ? kLaunch + 2.0 + (double)(L + O) * I * (f32 ? 8 : 4) / 5.4e6 : 0.0;
+  const double operands = lay.packed ? kLaunch + 2.5 + (double)(L + O) * I * (f32 ? 8 : 4) / 5.2e6 : 0.0;
   const int64_t stages = lay.pitch / kPiece;
-  const double ta = tile_time(128, type, L, O, stages, &a), tb = tile_time(256, type, L, O, stages, &b);
-  if (tr <= operands + (ta < tb ? ta : tb)) return rows;
-  return ta < tb ? a : b;
+  const double ta = operands + tile_time(128, type, L, O, stages, &a), tb = operands + tile_time(256, type, L, O, stages, &b);
+  const bool direct = I * (f32 ? 4 : 2) % 16 == 0;     // 16-byte loads stay within a row or leave it whole
+  const double tc = direct ? direct_time(64, 64, type, L, O, I, &c) : 1e30, td = direct ? direct_time(32, 128, type, L, O, I, &d) : 1e30;
+  const Plan* p = &rows;
+  double t = tr;
+  if (ta < t) { t = ta; p = &a; }
+  if (tb < t) { t = tb; p = &b; }
+  if (tc < t) { t = tc; p = &c; }
+  if (td < t) { t = td; p = &d; }
+  return *p;
 }
 
-size_t images_offset(const TileLayout& t) { return (size_t)round_up((int64_t)t.total, 256); }
+size_t images_offset(const Plan& p, const TileLayout& t) { return p.direct ? 0 : (size_t)round_up((int64_t)t.total, 256); }
 size_t scratch_bytes(const Plan& p, const TileLayout& t, int64_t L, int64_t O) {
   if (!p.tiles) return p.slices > 1 ? (size_t)p.slices * L * sums_pitch(O) * 4 : 0;
-  if (p.slices == 1) return t.total;
-  return images_offset(t) + (size_t)((p.tiles_m * p.tiles_n - p.whole) * p.slices) * p.size * p.size * 4;
+  const size_t images = p.slices > 1 ? (size_t)((p.tiles_m * p.tiles_n - p.whole) * p.slices) * p.bm * p.bn * 4 : 0;
+  return images ? images_offset(p, t) + images : p.direct ? 0 : t.total;
 }
 
-template <int SIZE, int WM, int WN, bool SPLIT, class TY>
+template <int BM, int BN, int WM, int WN, int MODE, class TY>
 hipError_t tiles_sized(const TileArgs& g, hipStream_t s) {
-  constexpr int LDS = kTileLds<SIZE, SIZE, WM, WN>, THREADS = 64 * (SIZE / WM) * (SIZE / WN);
-  auto kern = linear_tile_kernel<SIZE, SIZE, WM, WN, SPLIT, TY>;
+  constexpr int LDS = kTileLds<BM, BN, WM, WN>, THREADS = 64 * (BM / WM) * (BN / WN);
+  auto kern = linear_tile_kernel<BM, BN, WM, WN, MODE, TY>;
   static std::atomic<bool> attr_set{false};  // per instantiation; setting it twice is harmless
   if (!attr_set.load(std::memory_order_acquire)) {
     if (const hipError_t e = hipFuncSetAttribute((const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize, LDS); e != hipSuccess) return e;
@@ -708,25 +800,32 @@ hipError_t tiles_sized(const TileArgs& g, hipStream_t s) {
   }
   const int64_t rest = (int64_t)g.tiles_m * g.tiles_n - g.whole;
   kern<<<dim3((unsigned)(g.whole + rest * g.slices)), dim3(THREADS), LDS, s>>>(g);
-  if (rest)
-    linear_combine_kernel<SIZE, SIZE, WM, WN, SPLIT, TY><<<dim3((unsigned)(rest * (SIZE * SIZE / 2048))), dim3(256), 0, s>>>(g);
+  if (rest) linear_combine_kernel<BM, BN, WM, WN, MODE, TY><<<dim3((unsigned)(rest * (BM * BN / 2048))), dim3(256), 0, s>>>(g);
   return hipGetLastError();
 }
 
 template <class T, class TY>
 hipError_t tiles_typed(const LinearForward& a, const Plan& p, const LinearOut& o, hipStream_t s) {
-  constexpr bool SPLIT = sizeof(T) == 4;
+  constexpr bool F32 = sizeof(T) == 4;
   const TileLayout t = tile_layout(a.type, a.L, a.O, a.I);
   TileArgs g{(const uint8_t*)a.x, (const uint8_t*)a.w, t.pitch, nullptr, nullptr, (int)p.tiles_m, (int)p.tiles_n,
              (int)p.whole, p.slices, nullptr, o};
-  if (p.slices > 1) g.images = (float*)((uint8_t*)a.ws + images_offset(t));
+  if (p.slices > 1) g.images = (float*)((uint8_t*)a.ws + images_offset(p, t));
+  if (p.direct) {
+    g.pitch = a.I * (int64_t)sizeof(T);
+    constexpr int MODE = F32 ? kF32Direct : kBf16Direct;
+    stage_begin(kStLinear, s);
+    const hipError_t e = p.bm == 64 ? tiles_sized<64, 64, 32, 32, MODE, TY>(g, s) : tiles_sized<32, 128, 32, 32, MODE, TY>(g, s);
+    stage_end(kStLinear, s);
+    return e;
+  }
   if (t.packed) {
     uint8_t* const px = (uint8_t*)a.ws;
     uint8_t* const pw = px + t.w;
     int* const exps = (int*)(px + t.exps);
     stage_begin(kStLinearOperands, s);
     hipError_t e;
-    if constexpr (SPLIT) {
+    if constexpr (F32) {
       e = launch_split((const float*)a.x, (const float*)a.w, a.L, a.O, a.I, t.pitch, px, pw, exps, s);
     } else {
       linear_pad_kernel<<<dim3((unsigned)ceil_div(a.L + a.O, 4)), dim3(256), 0, s>>>((const bf16*)a.x, (const bf16*)a.w, a.L, a.O, a.I,
@@ -740,8 +839,9 @@ hipError_t tiles_typed(const LinearForward& a, const Plan& p, const LinearOut& o
     g.ex = exps;
     g.ew = exps + a.L;
   }
+  constexpr int MODE = F32 ? kSplitRows : kBf16Rows;
   stage_begin(kStLinear, s);
-  const hipError_t e = p.size == 256 ? tiles_sized<256, 64, 128, SPLIT, TY>(g, s) : tiles_sized<128, 64, 64, SPLIT, TY>(g, s);
+  const hipError_t e = p.bm == 256 ? tiles_sized<256, 256, 64, 128, MODE, TY>(g, s) : tiles_sized<128, 128, 64, 64, MODE, TY>(g, s);
   stage_end(kStLinear, s);
   return e;
 }
