@@ -196,8 +196,8 @@ template <int FN>
 __device__ __forceinline__ float act_value(float x) {
   if constexpr (FN == HOT_ACT_RELU) return x < 0.0f ? 0.0f : x;
   else if constexpr (FN == HOT_ACT_GELU) {
-    const float a = fabsf(x);
-    return fmaf(-a, normal_tail(a, gauss_of(x)), fmaxf(x, 0.0f));
+    // the tail of +inf is zero: times a number, so that x Phi(x) is infinite there
+    return fmaf(-fabsf(fminf(x, 0x1p100f)), normal_tail(fabsf(x), gauss_of(x)), fmaxf(x, 0.0f));
   } else if constexpr (FN == HOT_ACT_GELU_TANH) {
     const float xc = clamp30(x);
     return x * sigmoid_of(gelu_tanh_arg(xc));

@@ -158,6 +158,25 @@ def test_activation_far_out_and_not_finite(fn):
     close(g[:, :14], want, torch.where(far, torch.full_like(tol, 1e-4), tol), "slope")
 
 
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("fn", FNS)
+def test_activation_of_an_infinity(fn, dtype):
+    """f(+inf) is +inf, by itself and behind a product; a NaN stays one and the values beside them finite."""
+    inf, nan = float("inf"), float("nan")
+    x = torch.tensor([[inf, 2.0, nan, 3.0] * 4], dtype=dtype)
+    y = torch.empty_like(x, device="cuda")
+    hot.hot_activation_forward(getattr(hot, "HOT_ACT_" + fn.upper()), x.cuda(), y)
+    want = torch.tensor([[inf, 0.0, nan, 0.0] * 4])
+    got = torch.where(torch.isfinite(y.cpu().float()), torch.zeros(1), y.cpu().float())
+    assert torch.equal(got.nan_to_num(7.0, posinf=9.0, neginf=-9.0), want.nan_to_num(7.0, posinf=9.0, neginf=-9.0))
+    if dtype == BF16:        # bfloat16 products are exact: an infinity is one
+        a, w = torch.full((3, 64), 1.0, dtype=dtype), torch.ones((4, 64), dtype=dtype)
+        a[1, 0] = inf
+        z = torch.empty((3, 4), dtype=dtype, device="cuda")
+        hot.hot_linear_forward(a.cuda(), w.cuda(), z, hot.alloc_linear_workspace(dtype, 3, 4, 64), fn=getattr(hot, "HOT_ACT_" + fn.upper()))
+        assert bool((z[1] == inf).all()) and bool(torch.isfinite(z[0::2]).all())
+
+
 def test_bias_sums_alone_take_no_activation():
     g = rand((500, 200), 3)
     gb, gx = torch.empty(200, device="cuda"), torch.empty((500, 200), device="cuda")
