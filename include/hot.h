@@ -322,7 +322,8 @@ hot_status hot_layer_norm_backward(const void* g_y, hot_type y_type, const void*
  * ckpt: the checkpoint of z as [L x O], for hot_activation_backward (NULL: none is made).
  * fp32 operands: every product keeps 22 bits of each factor relative to the largest of its row, and is
  * summed in fp32, so that the result is as near the exact one as an fp32 product's; bfloat16 operands
- * are multiplied exactly and summed in fp32.  I < 2^24, O < 2^24.
+ * are multiplied exactly and summed in fp32.  I < 2^24, O < 2^24.  Where a row of fp32 x or w holds an
+ * infinity, its results may be NaN instead of infinite.
  * ws: at least hot_linear_forward_workspace_bytes() bytes of scratch, 256-byte aligned (where that is
  * 0, ws may be NULL).
  */

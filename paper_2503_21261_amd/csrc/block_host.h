@@ -17,6 +17,9 @@ inline CkptLayout ckpt_layout(int64_t rows, int64_t cols) {
   return k;
 }
 
+// Lanes of one launch: a launch of 2^32 or more is refused, so the longest tensors take several.
+constexpr int64_t kMaxLaunch = 1ll << 31;
+
 // Rows of partial sums that a column sum over `rows` rows leaves, and its width: the gradient kernels
 // write one such row per row group, `column_sums` adds them; a single row is the sum, and goes where that belongs.
 constexpr int kMaxSumRows = 1024;

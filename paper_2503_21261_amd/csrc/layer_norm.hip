@@ -46,10 +46,10 @@ __device__ __forceinline__ void row_sums(float& a, float& b, float (*s_red)[16][
 
 // EVEN: cols is a multiple of eight, so that a lane's chunk is whole or absent.
 template <int T, int NV, class TX, class TY, bool KEEP, bool EVEN>
-__global__ __launch_bounds__(kThreads<T>) void layer_norm_kernel(const NormForward a, const CkptView k) {
+__global__ __launch_bounds__(kThreads<T>) void layer_norm_kernel(const NormForward a, const CkptView k, int64_t first) {
   __shared__ float s_red[2][16][2];
   const int lane = (int)threadIdx.x % T, slot = (int)threadIdx.x / T;
-  const int64_t row = (int64_t)blockIdx.x * kSlots<T> + slot;
+  const int64_t row = first + (int64_t)blockIdx.x * kSlots<T> + slot;
   if (row >= a.rows) return;   // T > 64: one row a workgroup, all of it or none
   const int cols = (int)a.cols;
   auto have = [&](int c) { return EVEN ? 8 : cols - c; };
@@ -300,10 +300,15 @@ hipError_t launch_layer_norm(const NormForward& a, hipStream_t s) {
       constexpr bool EVEN = decltype(e)::value;
       using TX = decltype(tx);
       using TY = decltype(ty);
-      const dim3 grid((unsigned)ceil_div(a.rows, kSlots<T>)), block(kThreads<T>);
-      if (a.ckpt) layer_norm_kernel<T, NV, TX, TY, true, EVEN><<<grid, block, 0, s>>>(a, view(a.ckpt, a.rows, a.cols));
-      else layer_norm_kernel<T, NV, TX, TY, false, EVEN><<<grid, block, 0, s>>>(a, CkptView{});
-      return hipGetLastError();
+      constexpr int64_t kRun = kMaxLaunch / T;     // rows of a launch
+      for (int64_t first = 0; first < a.rows; first += kRun) {
+        const int64_t rows = a.rows - first < kRun ? a.rows - first : kRun;
+        const dim3 grid((unsigned)ceil_div(rows, kSlots<T>)), block(kThreads<T>);
+        if (a.ckpt) layer_norm_kernel<T, NV, TX, TY, true, EVEN><<<grid, block, 0, s>>>(a, view(a.ckpt, a.rows, a.cols), first);
+        else layer_norm_kernel<T, NV, TX, TY, false, EVEN><<<grid, block, 0, s>>>(a, CkptView{}, first);
+        if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+      }
+      return hipSuccess;
     });
   });
 }

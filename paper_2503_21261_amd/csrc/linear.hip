@@ -534,10 +534,10 @@ __device__ __forceinline__ void store_parts(uint8_t* dst, int64_t c, const float
 }
 template <int T, int NV>
 __global__ __launch_bounds__(256) void linear_split_kernel(const float* x, const float* w, int64_t L, int64_t O, int64_t I, int64_t pitch,
-                                                           uint8_t* px, uint8_t* pw, int* exps) {
+                                                           uint8_t* px, uint8_t* pw, int* exps, int64_t first) {
   __shared__ uint32_t s_top[4];
   const int lane = (int)threadIdx.x % T;
-  const int64_t r = (int64_t)blockIdx.x * (256 / T) + (int)threadIdx.x / T;
+  const int64_t r = first + (int64_t)blockIdx.x * (256 / T) + (int)threadIdx.x / T;
   if (r >= L + O) return;    // T = 256: one row a workgroup
   const float* const src = r < L ? x + r * I : w + (r - L) * I;
   uint8_t* const dst = r < L ? px + r * pitch : pw + (r - L) * pitch;
@@ -592,12 +592,24 @@ __global__ __launch_bounds__(256) void linear_split_kernel(const float* x, const
   }
 }
 
+// f(first, rows) for the runs of rows, `lanes` lanes each, that a launch holds.
+template <class F>
+hipError_t each_run(int64_t rows, int64_t lanes, F&& f) {
+  const int64_t run = kMaxLaunch / lanes;
+  for (int64_t first = 0; first < rows; first += run)
+    if (const hipError_t e = f(first, rows - first < run ? rows - first : run); e != hipSuccess) return e;
+  return hipSuccess;
+}
+
 hipError_t launch_split(const float* x, const float* w, int64_t L, int64_t O, int64_t I, int64_t pitch, uint8_t* px, uint8_t* pw,
                         int* exps, hipStream_t s) {
   auto go = [&](auto t, auto nv) {
     constexpr int T = decltype(t)::value;
-    linear_split_kernel<T, decltype(nv)::value><<<dim3((unsigned)ceil_div(L + O, 256 / T)), dim3(256), 0, s>>>(x, w, L, O, I, pitch, px, pw, exps);
-    return hipGetLastError();
+    return each_run(L + O, T, [&](int64_t first, int64_t rows) {
+      linear_split_kernel<T, decltype(nv)::value><<<dim3((unsigned)ceil_div(rows, 256 / T)), dim3(256), 0, s>>>(x, w, L, O, I, pitch, px, pw,
+                                                                                                              exps, first);
+      return hipGetLastError();
+    });
   };
   using std::integral_constant;
   if (I <= 512) return go(integral_constant<int, 64>{}, integral_constant<int, 1>{});
@@ -611,9 +623,9 @@ hipError_t launch_split(const float* x, const float* w, int64_t L, int64_t O, in
 
 // Rows of bfloat16 operands whose width is no multiple of 32, padded with zeros.
 __global__ __launch_bounds__(256) void linear_pad_kernel(const bf16* x, const bf16* w, int64_t L, int64_t O, int64_t I, int64_t pitch,
-                                                         uint8_t* px, uint8_t* pw) {
+                                                         uint8_t* px, uint8_t* pw, int64_t first) {
   const int lane = (int)threadIdx.x & 63;
-  const int64_t r = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+  const int64_t r = first + (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
   if (r >= L + O) return;
   const bf16* const src = r < L ? x + r * I : w + (r - L) * I;
   uint8_t* const dst = r < L ? px + r * pitch : pw + (r - L) * pitch;
@@ -713,6 +725,7 @@ double rows_time(hot_type type, int64_t L, int64_t O, int64_t I, Plan* p) {
     for (int mt = 1; mt <= 4; mt *= 2) {
       if (mt > 1 && (mt / 2) * 16 >= L) continue;
       const int64_t tm = ceil_div(L, 16 * mt), tn = ceil_div(O, 16 * nt);
+      if (tm * tn > kMaxLaunch / (64 * kWaves)) continue;
       for (int s = 1; s <= 16; ++s) {
         if (s > 1 && (tm * tn * s > 512 || I / s < turn)) break;
         const double k = (double)I / s * odd / 2000;
@@ -745,6 +758,7 @@ double direct_time(int bm, int bn, hot_type type, int64_t L, int64_t O, int64_t 
   p->tiles_n = ceil_div(O, bn);
   p->slices = 1;
   const int64_t count = p->tiles_m * p->tiles_n;
+  if (count > kMaxLaunch / 256) return 1e30;
   p->whole = count;
   const double moved = (((double)L + O) * bytes + (double)L * O * 4) / (f32 ? 49e6 : 15e6);
   double best = 1e30;
@@ -828,9 +842,11 @@ hipError_t tiles_typed(const LinearForward& a, const Plan& p, const LinearOut& o
     if constexpr (F32) {
       e = launch_split((const float*)a.x, (const float*)a.w, a.L, a.O, a.I, t.pitch, px, pw, exps, s);
     } else {
-      linear_pad_kernel<<<dim3((unsigned)ceil_div(a.L + a.O, 4)), dim3(256), 0, s>>>((const bf16*)a.x, (const bf16*)a.w, a.L, a.O, a.I,
-                                                                                    t.pitch, px, pw);
-      e = hipGetLastError();
+      e = each_run(a.L + a.O, 64, [&](int64_t first, int64_t rows) {
+        linear_pad_kernel<<<dim3((unsigned)ceil_div(rows, 4)), dim3(256), 0, s>>>((const bf16*)a.x, (const bf16*)a.w, a.L, a.O, a.I, t.pitch,
+                                                                                 px, pw, first);
+        return hipGetLastError();
+      });
     }
     stage_end(kStLinearOperands, s);
     if (e != hipSuccess) return e;
@@ -870,14 +886,10 @@ hipError_t rows_typed(const LinearForward& a, const Plan& p, const LinearOut& o,
 }
 
 template <class T, class TY>
-hipError_t linear_typed(const LinearForward& a, hipStream_t s) {
-  LinearOut o{a.bias, a.residual, a.y, CkptView{}, a.L, (int)a.O, a.fn};
-  if (a.ckpt) {
-    const CkptLayout l = ckpt_layout(a.L, a.O);
-    o.k = CkptView{(uint8_t*)a.ckpt, (uint8_t*)a.ckpt + l.exps, l.pitch};
-  }
+hipError_t linear_run(const LinearForward& a, const CkptView& k, hipStream_t s) {
+  LinearOut o{a.bias, a.residual, a.y, k, a.L, (int)a.O, a.fn};
   Plan p = make_plan(a.type, a.L, a.O, a.I);
-  if (a.ckpt && !p.tiles && p.slices == 1 && p.nt == 1) {   // a group is finished by one workgroup
+  if (k.codes && !p.tiles && p.slices == 1 && p.nt == 1) {   // a group is finished by one workgroup
     p.nt = 2;
     p.tiles_n = ceil_div(a.O, 32);
   }
@@ -888,10 +900,35 @@ hipError_t linear_typed(const LinearForward& a, hipStream_t s) {
   return e;
 }
 
+// Rows of one plan: a longer x is worked on in runs, one after another on the same scratch, which bounds that and every launch.
+constexpr int64_t kRunRows = 1 << 23;
+
+template <class T, class TY>
+hipError_t linear_typed(const LinearForward& a, hipStream_t s) {
+  const CkptLayout l = ckpt_layout(a.L, a.O);
+  for (int64_t first = 0; first < a.L; first += kRunRows) {
+    LinearForward r = a;
+    r.L = a.L - first < kRunRows ? a.L - first : kRunRows;
+    r.x = (const T*)a.x + first * a.I;
+    r.y = (TY*)a.y + first * a.O;
+    if (a.residual) r.residual = (const TY*)a.residual + first * a.O;
+    CkptView k{};
+    if (a.ckpt) k = CkptView{(uint8_t*)a.ckpt + first * l.pitch, (uint8_t*)a.ckpt + l.exps + first * (l.pitch / kCkGroup), l.pitch};
+    if (const hipError_t e = linear_run<T, TY>(r, k, s); e != hipSuccess) return e;
+  }
+  return hipSuccess;
+}
+
+size_t run_scratch_bytes(hot_type type, int64_t L, int64_t O, int64_t I) {
+  return L ? scratch_bytes(make_plan(type, L, O, I), tile_layout(type, L, O, I), L, O) : 0;
+}
+
 }  // namespace
 
 size_t linear_scratch_bytes(hot_type type, int64_t L, int64_t O, int64_t I) {
-  return scratch_bytes(make_plan(type, L, O, I), tile_layout(type, L, O, I), L, O);
+  if (L <= kRunRows) return run_scratch_bytes(type, L, O, I);
+  const size_t run = run_scratch_bytes(type, kRunRows, O, I), last = run_scratch_bytes(type, L % kRunRows, O, I);
+  return run > last ? run : last;
 }
 
 hipError_t launch_linear(const LinearForward& a, hipStream_t s) {

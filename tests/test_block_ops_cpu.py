@@ -113,6 +113,16 @@ def test_linear_refusals():
     assert l.hot_linear_forward_workspace_bytes(7, 4, 4, 4) == 0
 
 
+@pytest.mark.parametrize("t", [hot.HOT_F32, hot.HOT_BF16])
+def test_linear_scratch_does_not_grow_with_long_inputs(t):
+    """Rows past one run share its scratch; a shorter last run, which may be worked on another way, fits as well."""
+    need = hot.lib().hot_linear_forward_workspace_bytes
+    for O, I in ((3, 5), (200, 33), (64, 1000)):
+        run = need(t, 1 << 23, O, I)
+        for tail in (1, 40, 700, 9000, 1 << 20):
+            assert need(t, (1 << 23) + tail, O, I) == need(t, (1 << 24) + tail, O, I) == max(run, need(t, tail, O, I))
+
+
 def test_binding_refuses_host_tensors():
     x, buf = torch.zeros(4, 64), torch.zeros(4096, dtype=torch.uint8)
     for call in (lambda: hot.hot_checkpoint_write(x, buf), lambda: hot.hot_checkpoint_read(buf, x),

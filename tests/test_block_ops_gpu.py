@@ -393,6 +393,87 @@ def test_linear_rows_with_an_infinity_or_nan_stay_alone():
             assert torch.equal(bad, want)
 
 
+# One shape for each way a product is worked on: few rows (16 or 32 outputs and 16 to 64 tokens a workgroup), operands as they are in
+# tiles of 64 x 64 and 32 x 128, packed ones in 128 x 128 and 256 x 256; each with whole tiles and in slices of K, the packed ones also
+# with slices for the last tiles alone.
+LINEAR_WAYS = [
+    (BF16, 522, 1909, 8), (BF16, 3, 112, 5000), (BF16, 50, 90, 88), (BF16, 1, 9, 4776), (BF16, 40, 600, 6000), (BF16, 9, 33, 4103),
+    (BF16, 17, 2342, 11), (BF16, 477, 17, 7907), (BF16, 4153, 38, 9), (BF16, 3017, 8, 4995), (BF16, 5, 4188, 11), (BF16, 1, 843, 7536),
+    (BF16, 7772, 21, 9), (BF16, 50, 518, 5285), (BF16, 14813, 18, 15), (BF16, 33, 1012, 7331), (BF16, 10082, 165, 9),
+    (BF16, 594, 124, 2211), (BF16, 14578, 963, 9), (BF16, 9837, 143, 7617), (BF16, 11683, 1514, 1010),
+    (F32, 203, 4471, 16), (F32, 1, 4453, 3756), (F32, 14198, 9, 8), (F32, 859, 36, 4952), (F32, 11, 24, 3004), (F32, 2140, 19, 8),
+    (F32, 536, 17, 3361), (F32, 14418, 9, 11), (F32, 1650, 8, 5097), (F32, 3, 4787, 8), (F32, 1, 1079, 3448), (F32, 3083, 56, 9),
+    (F32, 602, 17, 7289), (F32, 1880, 254, 11), (F32, 2771, 17, 4114), (F32, 6353, 238, 9), (F32, 2099, 113, 1775),
+    (F32, 6742, 1245, 2568), (F32, 6375, 2284, 40), (F32, 7329, 162, 5528), (F32, 5054, 3202, 528),
+    # operand rows of every class of width
+    (F32, 2600, 1500, 301), (F32, 2600, 1500, 513), (F32, 2600, 1500, 1030), (F32, 2600, 1500, 2501), (F32, 1200, 260, 4097),
+    (F32, 1200, 260, 9001), (F32, 1200, 260, 17001), (F32, 1200, 260, 40003)]
+
+
+@pytest.mark.parametrize("t,L,O,I", LINEAR_WAYS)
+def test_linear_ways(t, L, O, I):
+    run_linear(L, O, I, t, t, seed=L + I)
+    run_linear(L, O, I, t, F32, fn="gelu_tanh", residual=True, kept=True, seed=L + I + 1)
+
+
+def test_linear_in_runs_of_rows():
+    """More rows than one plan takes: the second run is as the first."""
+    run_linear(2 ** 23 + 5, 3, 5, F32, F32, residual=True, kept=True, seed=3)
+    run_linear(2 ** 23 + 70, 2, 9, BF16, BF16, seed=4)
+
+
+def test_linear_of_many_long_rows():
+    """Operand rows of more lanes than a launch holds, tensors past 2^32 bytes; rows from all over against 64 bits."""
+    L, O, I = 2 ** 23, 256, 1032
+    x, w = torch.empty((L, I), device="cuda"), rand((O, I), 1, std=I ** -0.5).cuda()
+    g = torch.Generator("cuda").manual_seed(2)
+    x.normal_(generator=g)
+    y = torch.full((L, O), float("nan"), device="cuda")
+    hot.hot_linear_forward(x, w, y, hot.alloc_linear_workspace(F32, L, O, I))
+    at = torch.tensor([0, 1, 2 ** 20 + 1, 2 ** 22 - 1, 2 ** 22, 2 ** 23 - 257, 2 ** 23 - 256, 2 ** 23 - 1], device="cuda")
+    wy, _ = ref.linear(ref.f64(x[at]), ref.f64(w), None, "none", None, F32)
+    close(y[at], *wy, "y")
+    assert bool(torch.isfinite(y).all())
+
+
+# ---- tensors past 32 bits ---------------------------------------------------------------------------------------------
+
+def test_pointwise_tensors_past_32_bits():
+    """Elements past 2^32: the last rows give what they give in a call of their own."""
+    rows, cols = 2 ** 17 + 6, 2 ** 15 + 32
+    x = torch.empty((rows, cols), dtype=BF16, device="cuda").normal_(generator=torch.Generator("cuda").manual_seed(1))
+    tail = x[-7:].contiguous()
+    y, kept = torch.empty_like(x), hot.alloc_checkpoint(rows, cols)
+    y7, kept7 = torch.empty_like(tail), hot.alloc_checkpoint(7, cols)
+    hot.hot_activation_forward(hot.HOT_ACT_SILU, x, y, ckpt=kept)
+    hot.hot_activation_forward(hot.HOT_ACT_SILU, tail, y7, ckpt=kept7)
+    assert torch.equal(y[-7:], y7)
+    back, back7 = torch.empty_like(x), torch.empty_like(tail)
+    hot.hot_checkpoint_read(kept, back)
+    hot.hot_checkpoint_read(kept7, back7)
+    assert torch.equal(back[-7:], back7)
+    gx, gx7 = torch.empty_like(x), torch.empty_like(tail)
+    hot.hot_activation_backward(hot.HOT_ACT_SILU, y, gx, ckpt=kept)
+    hot.hot_activation_backward(hot.HOT_ACT_SILU, y7, gx7, ckpt=kept7)
+    assert torch.equal(gx[-7:], gx7)
+    mean, rstd, mean7, rstd7 = (torch.empty(n, device="cuda") for n in (rows * 4, rows * 4, 28, 28))
+    x, tail = x.view(rows * 4, cols // 4), tail.view(28, cols // 4)
+    y, y7, gx, gx7 = y.view_as(x), y7.view_as(tail), gx.view_as(x), gx7.view_as(tail)
+    hot.hot_layer_norm_forward(x, None, None, 1e-6, y, mean, rstd)
+    hot.hot_layer_norm_forward(tail, None, None, 1e-6, y7, mean7, rstd7)
+    hot.hot_layer_norm_backward(x, None, mean, rstd, gx, h=x)
+    hot.hot_layer_norm_backward(tail, None, mean7, rstd7, gx7, h=tail)
+    assert torch.equal(y[-28:], y7) and torch.equal(mean[-28:], mean7) and torch.equal(gx[-28:], gx7)
+
+
+def test_layer_norm_of_more_lanes_than_a_launch_holds():
+    rows = 2 ** 28 + 3
+    x = torch.empty((rows, 1), device="cuda").normal_(generator=torch.Generator("cuda").manual_seed(1))
+    y, mean, rstd = torch.full_like(x, 7.0), torch.empty(rows, device="cuda"), torch.empty(rows, device="cuda")
+    hot.hot_layer_norm_forward(x, None, None, 1.0, y, mean, rstd)
+    assert torch.equal(mean, x.view(-1)) and bool((rstd == 1).all()) and not bool(y.any())
+
+
 # ---- as they are called ----------------------------------------------------------------------------------------------------
 
 def test_calls_on_another_stream_and_replayed():
@@ -438,6 +519,40 @@ def test_calls_on_another_stream_and_replayed():
         step()
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(replayed, outs)), k
+
+
+def test_two_streams_at_once():
+    """The same calls, interleaved on two streams with workspaces of their own, give what they give one after another; the stream
+    is the argument's, not the current one."""
+    L, I, O = 700, 1500, 513          # operand packing, K slices, sums over rows
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    x, w, g = [rand((L, I), k).cuda() for k in range(2)], rand((O, I), 5, std=0.03).cuda(), [rand((L, O), 7 + k).cuda() for k in range(2)]
+    make = lambda *s: [torch.zeros(s, device="cuda") for _ in range(2)]       # noqa: E731
+    y, gz, gb, n, mean, rstd, gx, gg, gbeta = (make(L, O), make(L, O), make(O), make(L, O), make(L), make(L), make(L, O), make(O), make(O))
+    kept = [hot.alloc_checkpoint(L, O) for _ in range(2)]
+    ws = [(hot.alloc_linear_workspace(F32, L, O, I), hot.alloc_activation_workspace(L, O), hot.alloc_layer_norm_workspace(L, O)) for _ in range(2)]
+    outs = [y, gz, gb, n, mean, rstd, gx, gg, gbeta]
+
+    def step(k, s):
+        hot.hot_linear_forward(x[k], w, y[k], ws[k][0], fn=hot.HOT_ACT_SILU, ckpt=kept[k], stream=s)
+        hot.hot_activation_backward(hot.HOT_ACT_SILU, g[k], gz[k], ckpt=kept[k], g_bias=gb[k], ws=ws[k][1], stream=s)
+        hot.hot_layer_norm_forward(y[k], None, None, 1e-5, n[k], mean[k], rstd[k], stream=s)
+        hot.hot_layer_norm_backward(g[k], None, mean[k], rstd[k], gx[k], gg[k], gbeta[k], ws[k][2], h=y[k], stream=s)
+
+    torch.cuda.synchronize()
+    for k in range(2):
+        step(k, streams[0])
+        torch.cuda.synchronize()
+    alone = [t.clone() for pair in outs for t in pair]
+    for pair in outs:
+        for t in pair:
+            t.zero_()
+    torch.cuda.synchronize()
+    for _ in range(4):
+        for k in range(2):
+            step(k, streams[k])
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(alone, [t for pair in outs for t in pair]))
 
 
 def test_transformer_mlp_step_with_the_linear_backward():
