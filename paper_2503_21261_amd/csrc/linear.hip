@@ -1,10 +1,11 @@
 // Forward product of a linear layer, y = f(x.w^T + bias) + residual.
 //
-// linear_rows_kernel: few rows.  The weight is read once and is what bounds it (HBM): operands go from memory to the
-// matrix instructions without LDS, every wave of a workgroup takes its part of K, and the waves' sums are added in
-// LDS, in order.  A lane loads 16 consecutive bytes of a row; bfloat16 rows feed v_mfma_f32_16x16x32_bf16, fp32 rows
-// four v_mfma_f32_16x16x4_f32, whose products and sums are plain fp32.  The weight is the first operand, so that a
-// lane's accumulators are four consecutive outputs of a token.
+// Three kernels multiply, and make_plan chooses between them by the time that each is expected to take:
+//   linear_rows_kernel            few rows: operands from memory to the matrix instructions, the weight's way from HBM is the time;
+//   linear_tile_kernel, direct    small tiles of the operands as they are: products over before operands could be packed;
+//   linear_tile_kernel, packed    large tiles, for products that the matrix cores bound; fp32 operands as two fp16 parts.
+// Each splits K where its workgroups would leave compute units idle, and a second launch adds the slices' sums in order.
+// All sums are fp32.  Sizes are given as L x O x I, times as those of a replayed graph.
 #include <math.h>
 
 #include <atomic>
@@ -67,7 +68,14 @@ __host__ __device__ constexpr int64_t sums_pitch(int64_t O) { return (O + 7) / 8
 constexpr int kWaves = 8;       // of a workgroup: parts of K
 constexpr int kSteps = 4;       // loads of a row on their way together: 4 x 64 bytes
 
-// NT x 16 outputs and MT x 16 tokens a workgroup.
+// linear_rows_kernel: NT x 16 outputs and MT x 16 tokens a workgroup, every wave on its part of K; the waves' sums are added in LDS, in
+// order.  A lane loads 16 consecutive bytes of a row; bfloat16 rows feed v_mfma_f32_16x16x32_bf16, fp32 rows four
+// v_mfma_f32_16x16x4_f32, whose products and sums are plain fp32.  The weight is the first operand, so that a lane's accumulators
+// are four consecutive outputs of a token.  Operands do not meet in LDS: a weight row serves MT tokens from registers, and with few
+// tokens nothing else would read it.  1 x 4096 x 11008 bfloat16 16.8 us, 5.4 TB/s of weight.  Both sizes are the plan's:
+// 62 x 418 x 896 fp32 8.8 us with 16 outputs and 16 tokens, 18.8 with 32 and 64, whose workgroups are too few;
+// 191 x 7833 x 8640 bfloat16 341 us against 145, as every operand byte is loaded less often.  K in slices: 18 x 216 x 8281
+// bfloat16 45 -> 14 us; 5 x 3118 x 2048 8.0 us whole, 10.6 in slices.
 template <class T, class TY, int NT, int MT>
 __global__ __launch_bounds__(64 * kWaves) void linear_rows_kernel(const T* x, const T* w, int64_t I, int tiles_m, int slices, float* sums, LinearOut out) {
   constexpr int E = Frag<T>::kElems;
@@ -162,7 +170,7 @@ __global__ __launch_bounds__(64 * kWaves) void linear_rows_kernel(const T* x, co
   }
 }
 
-// The slices' sums, in order, and the epilogue: eight outputs of a token a thread.
+// The slices' sums, in order, and the epilogue: eight outputs of a token a thread.  Bound by its launch and one way to the caches.
 template <class TY>
 __global__ __launch_bounds__(256) void linear_rows_combine_kernel(const float* sums, int slices, int chunks, LinearOut out) {
   const int64_t q = (int64_t)blockIdx.x * 256 + threadIdx.x;
@@ -185,21 +193,24 @@ __global__ __launch_bounds__(256) void linear_rows_combine_kernel(const float* s
 }
 
 // ---- many rows -------------------------------------------------------------------------------------
-// linear_tile_kernel: BM tokens x BN outputs a workgroup, both operands through LDS.  Operand rows are K-contiguous
-// and a whole number of 64-byte pieces; a stage is one piece of every row of the tile:
-//   bfloat16: 32 elements (rows of x and w as they are where I % 32 == 0, else a padded copy);
-//   fp32: 16 elements as two fp16 parts, [16 high | 16 low], of the row scaled by a power of two so that its largest
+// linear_tile_kernel: BM tokens x BN outputs a workgroup, both operands through LDS.  Operand rows are K-contiguous; a stage is
+// 128 bytes of every row of the tile:
+//   bfloat16: 64 elements (rows of x and w as they are where I % 64 == 0, else a padded copy);
+//   fp32: 32 elements as two fp16 parts, twice [16 high | 16 low], of the row scaled by a power of two so that its largest
 //   value lies in [2^14, 2^15): x = high + low to 22 bits (values down to 2^-17 of the row's largest keep them, smaller
-//   ones keep 2^-39 of it), and x.w = high.high + high.low + low.high with 2^-22 left out.  Three matrix instructions
-//   of fp16 in place of eight of fp32 (v_mfma_f32_32x32x2_f32) per 16 elements.
-// Pieces go from memory to LDS without registers (buffer_load ... lds), four stages deep, so that three are on their
-// way while one is worked on.  LDS holds a row's four 16-byte chunks at chunk ^ (row / 2 % 4): eight rows that read
-// the same chunk hit different banks.  As a load writes 64 consecutive chunks, it is the lanes' sources that are permuted.
+//   ones keep 2^-39 of it), and x.w = high.high + high.low + low.high with 2^-22 left out: a
+//   third of the fp16 rate, five times that of the fp32 instructions.
+// Pieces go from memory to LDS without registers (buffer_load ... lds), two stages deep: one arrives while one is worked on.  LDS
+// holds a row's eight 16-byte chunks at chunk ^ (row % 8): eight rows that read the same chunk hit different banks.  As a load
+// writes 64 consecutive chunks, it is the lanes' sources that are permuted.
 // A wave reads the fragments of a stage's second half under the first half's matrix instructions, then meets the others at a
-// barrier, behind which the next stage is complete and this stage's buffer free, and reads the next stage's first
-// half under the second's.  The weight is the matrix instructions' first operand, so that accumulators are runs of four
+// barrier, behind which the next stage is complete and this stage's buffer free, and reads the next stage's first half and issues
+// the loads of the one behind under the second's.  16 x 16 x 32 instructions: those of 32 x 32 x 16 move a quarter more through the
+// registers for each product, and as the chip's power holds such products down, that is time (8192^3 bfloat16 1417 TFLOP/s, 1323
+// with them; stages of 64 bytes, four deep: a tenth less).  The weight is the first operand, so that accumulators are runs of four
 // outputs of a token; they leave through LDS, a wave's 32 tokens at a time, as runs of eight outputs a lane.
-typedef float v16f __attribute__((ext_vector_type(16)));
+// Measured: 16384 x 11008 x 4096 bfloat16 with GELU and checkpoint 1240 us, 1190 TFLOP/s (its epilogue is 12 us of vector
+// instructions a round of tiles); 12608 x 2304 x 768 fp32 125 us, 1070 TFLOP/s of fp16 products, and 20 us for its operands.
 typedef _Float16 v8h __attribute__((ext_vector_type(8)));
 typedef int v4i __attribute__((ext_vector_type(4)));
 
@@ -243,8 +254,10 @@ constexpr int kTileLds = kStages * (BM + BN) * kPiece > (BM / WM) * (BN / WN) * 
 enum TileMode {
   kBf16Rows = 0,      // bfloat16, a whole number of pieces
   kSplitRows = 1,     // fp32 in two fp16 parts, a whole number of pieces
-  // x and w as they are: rows of any whole number of 16 bytes, the last piece masked.  Small tiles, several workgroups a compute unit,
-  // for products that are over before operands could be packed; fp32 on v_mfma_f32_16x16x4_f32.
+  // x and w as they are: rows of any whole number of 16 bytes, the last piece masked; fp32 on v_mfma_f32_16x16x4_f32.  Small tiles,
+  // several workgroups a compute unit, which hide each other's waits.  15774 x 64 x 128 fp32 in 64 x 64 9.2 us, packed 128 x 128
+  // 21.9; for 7383 x 1664 x 1152 259 us against 98, where the matrix instructions count.  29915 x 128 x 3920 bfloat16 83 us against
+  // 156 (a copy of x first), 3308 x 2079 x 2808 95 against 61.
   kBf16Direct = 2,
   kF32Direct = 3,
 };
@@ -516,6 +529,7 @@ __global__ __launch_bounds__(256) void linear_combine_kernel(const TileArgs g) {
 // Operand rows of the fp32 product: row r of the L + O rows of x and w, scaled by 2^(14 - e), e the exponent of its largest value,
 // as [16 high | 16 low] pieces; exps[r] = e - 14.  Padded columns are zero.  Bound by HBM: a row stays in the registers of the T
 // lanes that work on it, NV times eight columns each, or (NV = 0: rows beyond 16384) is read a second time, from the caches.
+// 8192 + 8192 rows of 8192 columns 187 us, 5.7 TB/s read and written; 250 when such rows were read twice.
 __device__ __forceinline__ int row_exponent(uint32_t top) {   // of the largest magnitude's bits; subnormal ones too
   // infinities and NaNs stay what they are under any scale
   return top >= 0x7F800000u || top == 0 ? 0 : ilogbf(__uint_as_float(top));
@@ -621,7 +635,7 @@ hipError_t launch_split(const float* x, const float* w, int64_t L, int64_t O, in
   return go(integral_constant<int, 256>{}, integral_constant<int, 0>{});
 }
 
-// Rows of bfloat16 operands whose width is no multiple of 32, padded with zeros.
+// Rows of bfloat16 operands whose width is no multiple of 64, padded with zeros to one.  Bound by HBM.
 __global__ __launch_bounds__(256) void linear_pad_kernel(const bf16* x, const bf16* w, int64_t L, int64_t O, int64_t I, int64_t pitch,
                                                          uint8_t* px, uint8_t* pw, int64_t first) {
   const int lane = (int)threadIdx.x & 63;
@@ -637,7 +651,7 @@ __global__ __launch_bounds__(256) void linear_pad_kernel(const bf16* x, const bf
   }
 }
 
-// What the tile kernel needs besides its operands: packed rows (fp32, or a width that is no multiple of 32) and the exponents.
+// What the tile kernel needs besides its operands: packed rows (fp32, or a width that is no multiple of 64) and the exponents.
 struct TileLayout {
   int64_t pitch;
   bool packed;
@@ -676,7 +690,9 @@ double beside(double a, double b) { return sqrt(sqrt(a * a * a * a + b * b * b *
 double rounds_of(int64_t n) { return n <= 1024 ? (double)ceil_div(n, 256) : n / 256.0 + 0.5; }
 
 // Tiles: a stage of 128 bytes of K in a round of workgroups, what a round takes besides (filling the buffers, the epilogue), the
-// outputs, the images' way to memory and back.
+// outputs, the images' way to memory and back.  256 x 256 moves half as much through LDS for each product, 128 x 128 fills the chip
+// with a quarter of the outputs: 3550 x 4380 x 5888 bfloat16 150 us against 214, 18 x 9042 x 1024 26 us against 14.
+// Slices of the tiles that leave compute units idle: 81 x 9536 x 320 bfloat16 88 -> 16 us, 1767 x 321 x 1728 fp32 26 us whole, 33 in slices.
 double tile_time(int size, hot_type type, int64_t L, int64_t O, int64_t stages, Plan* p) {
   const bool big = size == 256, f32 = type == HOT_F32;
   const int64_t slots = big ? 256 : 512;
@@ -746,7 +762,10 @@ double rows_time(hot_type type, int64_t L, int64_t O, int64_t I, Plan* p) {
   return best;
 }
 
-// Small tiles of the operands as they are: a compute unit's matrix instructions and loads, the time of a workgroup by itself.
+// Small tiles of the operands as they are: a compute unit's matrix instructions and loads, the time of a workgroup by itself.  32 x 128
+// reads less of a wide weight twice where tokens are few (10 x 9408 x 4352 fp32 37 us, 58 with 64 x 64), 64 x 64 less in all
+// (48 x 8704 x 9152 bfloat16 34 us, 53 with 32 x 128).  K in slices: 729 x 64 x 10240 bfloat16 69 -> 17 us; 1872 x 624 x 640 9.7 us
+// whole, 17.2 in slices.
 double direct_time(int bm, int bn, hot_type type, int64_t L, int64_t O, int64_t I, Plan* p) {
   const bool f32 = type == HOT_F32;
   const int64_t bytes = I * (f32 ? 4 : 2), stages = ceil_div(bytes, kPiece);
