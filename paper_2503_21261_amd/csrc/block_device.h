@@ -116,6 +116,14 @@ __device__ __forceinline__ uint32_t ckpt_exponent(uint32_t bits) {
 __device__ __forceinline__ float ckpt_step(uint32_t e) { return e == 255u ? __uint_as_float(0x7FC00000u) : __uint_as_float((e - 6u) << 23); }
 __device__ __forceinline__ float ckpt_inverse(uint32_t e) { return e == 255u ? 0.0f : __uint_as_float((260u - e) << 23); }
 
+// Whether any lane of the wave meets a condition that hardly ever holds: a branch around what it takes, which the compiler would
+// otherwise compute always and select from.
+__device__ __forceinline__ bool rarely(bool condition) {
+  if (__builtin_amdgcn_ballot_w64(condition) == 0) return false;
+  asm volatile("");    // not to be moved in front of the branch
+  return true;
+}
+
 // Maximum over the four lanes of a group (lane ids 4 k .. 4 k + 3) of a bit pattern.
 __device__ __forceinline__ uint32_t quad_max(uint32_t v) {
   v = max(v, (uint32_t)__builtin_amdgcn_mov_dpp((int)v, 0xB1, 0xF, 0xF, true));   // quad_perm [1,0,3,2]
@@ -155,13 +163,12 @@ struct CkptView {
 __device__ __forceinline__ void ckpt_store8(const CkptView& k, int64_t at, const float (&v)[8]) {
   const uint32_t e = ckpt_exponent(quad_max(magnitude8(v)));
   const float inverse = ckpt_inverse(e);
-  if (e == 254u) {   // at the type's end, where the next step is missing: 127.5 steps and more are held at 127
+  *(uint2*)(k.codes + at) = encode8(v, inverse);
+  if (rarely(e == 254u)) {   // at the type's end, where the next step is missing: 127.5 steps and more are held at 127
     float w[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) w[i] = fminf(fmaxf(v[i], -0x1.fcp+127f), 0x1.fcp+127f);
-    *(uint2*)(k.codes + at) = encode8(w, inverse);
-  } else {
-    *(uint2*)(k.codes + at) = encode8(v, inverse);
+    if (e == 254u) *(uint2*)(k.codes + at) = encode8(w, inverse);
   }
   if ((at & (kCkGroup - 1)) == 0) k.exps[at / kCkGroup] = (uint8_t)e;
 }
@@ -196,8 +203,11 @@ template <int FN>
 __device__ __forceinline__ float act_value(float x) {
   if constexpr (FN == HOT_ACT_RELU) return x < 0.0f ? 0.0f : x;
   else if constexpr (FN == HOT_ACT_GELU) {
-    // the tail of +inf is zero: times a number, so that x Phi(x) is infinite there
-    return fmaf(-fabsf(fminf(x, 0x1p100f)), normal_tail(fabsf(x), gauss_of(x)), fmaxf(x, 0.0f));
+    // The tail of +inf is zero: times a number, so that x Phi(x) is infinite there.  Minimum and maximum of the bit patterns, one
+    // instruction each: floats would be made quiet first.  A NaN stays one by its tail.
+    const int bits = __float_as_int(x);
+    const float held = __int_as_float(min(bits, 0x71800000)), positive = __int_as_float(max(bits, 0));
+    return fmaf(-fabsf(held), normal_tail(fabsf(x), gauss_of(x)), positive);
   } else if constexpr (FN == HOT_ACT_GELU_TANH) {
     const float xc = clamp30(x);
     return x * sigmoid_of(gelu_tanh_arg(xc));

@@ -44,7 +44,7 @@ __device__ __forceinline__ void linear_finish8(const LinearOut& o, int64_t row, 
 #pragma unroll
   for (int i = 0; i < 8; ++i) v[i] += b[i];
   if (o.k.codes) {
-    if (n < 8) {
+    if (rarely(n < 8)) {
 #pragma unroll
       for (int i = 0; i < 8; ++i) v[i] = i < n ? v[i] : 0.0f;
     }
