@@ -521,6 +521,25 @@ def test_calls_on_another_stream_and_replayed():
         assert all(torch.equal(a, b) for a, b in zip(replayed, outs)), k
 
 
+@pytest.mark.parametrize("t,L,O,I", [(F32, 700, 513, 3001), (F32, 5054, 3202, 528), (BF16, 700, 513, 1501), (BF16, 859, 36, 4952), (F32, 1, 1079, 3448)])
+def test_products_in_slices_recorded(t, L, O, I):
+    """Packed operands and the slices' images live in the workspace from launch to launch: replays between eager calls on the same
+    workspace give what eager calls give.  The first call of all may be a recorded one."""
+    x, w, b = rand((L, I), 1, t).cuda(), rand((O, I), 2, t, I ** -0.5).cuda(), rand((O,), 3).cuda()
+    y, z, ws = torch.zeros((L, O), dtype=t, device="cuda"), torch.zeros((L, O), dtype=t, device="cuda"), hot.alloc_linear_workspace(t, L, O, I)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        hot.hot_linear_forward(x, w, y, ws, bias=b, fn=hot.HOT_ACT_GELU)
+    for k in range(3):
+        x.copy_(rand((L, I), 10 + k, t))
+        y.zero_()
+        graph.replay()
+        hot.hot_linear_forward(x, w, z, ws, bias=b, fn=hot.HOT_ACT_GELU)
+        torch.cuda.synchronize()
+        assert torch.equal(y, z), k
+
+
 def test_two_streams_at_once():
     """The same calls, interleaved on two streams with workspaces of their own, give what they give one after another; the stream
     is the argument's, not the current one."""
