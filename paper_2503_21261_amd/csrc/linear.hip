@@ -195,7 +195,7 @@ __global__ __launch_bounds__(256) void linear_rows_combine_kernel(const float* s
 // ---- many rows -------------------------------------------------------------------------------------
 // linear_tile_kernel: BM tokens x BN outputs a workgroup, both operands through LDS.  Operand rows are K-contiguous; a stage is
 // 128 bytes of every row of the tile:
-//   bfloat16: 64 elements (rows of x and w as they are where I % 64 == 0, else a padded copy);
+//   bfloat16: 64 elements, of x and w as they are where I is even, else of a padded copy;
 //   fp32: 32 elements as two fp16 parts, twice [16 high | 16 low], of the row scaled by a power of two so that its largest
 //   value lies in [2^14, 2^15): x = high + low to 22 bits (values down to 2^-17 of the row's largest keep them, smaller
 //   ones keep 2^-39 of it), and x.w = high.high + high.low + low.high with 2^-22 left out: a
@@ -235,7 +235,7 @@ __device__ __forceinline__ void load_to_lds(rsrc_t from, uint8_t* to, int lane_o
 
 struct TileArgs {
   const uint8_t *x, *w;       // operand rows
-  int64_t pitch;              // bytes of one, a multiple of 128 (16 in the direct modes)
+  int64_t pitch;              // bytes of one, a multiple of 128 in the first two modes
   const int *ex, *ew;         // fp32: exponents of the rows' scales
   int tiles_m, tiles_n;
   int whole;                  // tiles with a workgroup each; every other one has `slices`, which leave their sums in
@@ -254,17 +254,19 @@ constexpr int kTileLds = kStages * (BM + BN) * kPiece > (BM / WM) * (BN / WN) * 
 enum TileMode {
   kBf16Rows = 0,      // bfloat16, a whole number of pieces
   kSplitRows = 1,     // fp32 in two fp16 parts, a whole number of pieces
-  // x and w as they are: rows of any whole number of 16 bytes, the last piece masked; fp32 on v_mfma_f32_16x16x4_f32.  Small tiles,
-  // several workgroups a compute unit, which hide each other's waits.  15774 x 64 x 128 fp32 in 64 x 64 9.2 us, packed 128 x 128
-  // 21.9; for 7383 x 1664 x 1152 259 us against 98, where the matrix instructions count.  29915 x 128 x 3920 bfloat16 83 us against
-  // 156 (a copy of x first), 3308 x 2079 x 2808 95 against 61.
-  kBf16Direct = 2,
-  kF32Direct = 3,
+  // The others are x and w as they are, of any width from 16 bytes on.  The chunk that reaches past a row's end is loaded as the row's
+  // last 16 bytes, so that nothing outside the row is read, and the bytes that belong to the chunk before it are masked.
+  kBf16Ragged = 2,    // large tiles, rows of a multiple of four bytes: no copy as kBf16Rows would need
+  // Small tiles, several workgroups a compute unit, which hide each other's waits; fp32 on v_mfma_f32_16x16x4_f32.
+  // 15774 x 64 x 128 fp32 in 64 x 64 9.2 us, packed 128 x 128 21.9; for 7383 x 1664 x 1152 259 us against 98, where the matrix
+  // instructions count.  1872 x 624 x 640 bfloat16 9.7 us, 128 x 128 12.6; 3308 x 2079 x 2808 95 against 61.
+  kBf16Direct = 3,
+  kF32Direct = 4,
 };
 
 template <int BM, int BN, int WM, int WN, int MODE, class TY>
 __global__ __launch_bounds__(64 * (BM / WM) * (BN / WN), 2) void linear_tile_kernel(const TileArgs g) {
-  constexpr bool SPLIT = MODE == kSplitRows, DIRECT = MODE >= kBf16Direct;
+  constexpr bool SPLIT = MODE == kSplitRows, DIRECT = MODE >= kBf16Direct, AS_IS = MODE >= kBf16Ragged;
   constexpr int WAVES_M = BM / WM, WAVES = WAVES_M * (BN / WN);
   constexpr int TM = WM / 16, TN = WN / 16;
   constexpr int XL = BM / 8 / WAVES, WL = BN / 8 / WAVES;   // loads of a wave and stage: 8 rows each
@@ -290,9 +292,9 @@ __global__ __launch_bounds__(64 * (BM / WM) * (BN / WN), 2) void linear_tile_ker
   const auto rw = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(g.w) + (int64_t)n0 * g.pitch, 0, (int)(rows_w * g.pitch), 0x00027000);
   int off_x[XL], off_w[WL];
   auto source = [&](int row, int64_t rows) {
-    const int chunk = (lane & 7) ^ (row & 7);
+    const int chunk = (lane & 7) ^ (row & 7);           // row & 7 is lane / 8
     const int r = row < rows ? row : (int)rows - 1;     // rows past the last repeat it and are not stored
-    return r * (int)g.pitch + chunk * 16;
+    return r * (int)g.pitch + (AS_IS ? 0 : chunk * 16);
   };
 #pragma unroll
   for (int i = 0; i < XL; ++i) off_x[i] = source((wave * XL + i) * 8 + (lane >> 3), rows_x);
@@ -302,8 +304,15 @@ __global__ __launch_bounds__(64 * (BM / WM) * (BN / WN), 2) void linear_tile_ker
     constexpr int e = decltype(ec)::value;
     const int at = (k_first + (kt < nk ? kt : nk - 1)) * kPiece;    // past the end: a stage again, into a buffer that nobody reads
     uint8_t* const b = smem + (kt & (kStages - 1)) * STAGE;
-    if constexpr (e < XL) load_to_lds(rx, b + (wave * XL + e) * 1024, off_x[e], at);
-    else load_to_lds(rw, b + BM * kPiece + (wave * WL + e - XL) * 1024, off_w[e - XL], at);
+    if constexpr (AS_IS) {
+      // the chunk that reaches past the row's end, and those behind it, are the row's last 16 bytes
+      const int in = at + ((lane & 7) ^ (lane >> 3)) * 16, last = (int)g.pitch - 16, from = in < last ? in : last;
+      if constexpr (e < XL) load_to_lds(rx, b + (wave * XL + e) * 1024, off_x[e] + from, 0);
+      else load_to_lds(rw, b + BM * kPiece + (wave * WL + e - XL) * 1024, off_w[e - XL] + from, 0);
+    } else {
+      if constexpr (e < XL) load_to_lds(rx, b + (wave * XL + e) * 1024, off_x[e], at);
+      else load_to_lds(rw, b + BM * kPiece + (wave * WL + e - XL) * 1024, off_w[e - XL], at);
+    }
   };
   auto load_stage = [&](int kt) { static_for<XL + WL>([&](auto e) { load_one(kt, e); }); };
 
@@ -346,6 +355,20 @@ __global__ __launch_bounds__(64 * (BM / WM) * (BN / WN), 2) void linear_tile_ker
       __builtin_amdgcn_sched_barrier(0);
     });
   };
+  // A row's last chunk holds bytes of the chunk before it as well, and those behind it nothing else: in both operands they are zero.
+  auto mask = [&](int kt, int h, v4i(&w)[TN], v4i(&x)[TM]) {
+    if ((int64_t)(k_first + kt + 1) * kPiece <= g.pitch) return;     // the same in all lanes
+    const int before = (k_first + kt) * kPiece + (4 * h + (lane >> 4)) * 16 - ((int)g.pitch - 16);   // bytes of the chunk that are not its own
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const int cut = before - 4 * e;
+      const uint32_t keep = cut >= 4 ? 0u : cut > 0 ? ~0u << (8 * cut) : ~0u;
+#pragma unroll
+      for (int j = 0; j < TN; ++j) w[j][e] &= keep;
+#pragma unroll
+      for (int i = 0; i < TM; ++i) x[i][e] &= keep;
+    }
+  };
   // This wave's loads have arrived and its LDS reads are done; then everybody's.
   auto meet = [&]() {
     asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
@@ -368,18 +391,6 @@ __global__ __launch_bounds__(64 * (BM / WM) * (BN / WN), 2) void linear_tile_ker
   static_for<TM>([&](auto i) { read_x(0, 0, xa, i); });
   if constexpr (DIRECT) {
     v4i xb[TM];
-    // chunks past a row's end hold what follows the row: both operands' are zero
-    auto mask = [&](int kt, int h, v4i(&w)[TN], v4i(&x)[TM]) {
-      if ((int64_t)(k_first + kt + 1) * kPiece <= g.pitch) return;     // the same in all lanes
-      const bool keep = (int64_t)(k_first + kt) * kPiece + (4 * h + (lane >> 4)) * 16 < g.pitch;
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-#pragma unroll
-        for (int j = 0; j < TN; ++j) w[j][e] = keep ? w[j][e] : 0;
-#pragma unroll
-        for (int i = 0; i < TM; ++i) x[i][e] = keep ? x[i][e] : 0;
-      }
-    };
     auto nothing = [](auto) {};
     for (int kt = 0; kt < nk; ++kt) {
       static_for<TN>([&](auto j) { read_w(kt, 1, wb, j); });
@@ -394,7 +405,8 @@ __global__ __launch_bounds__(64 * (BM / WM) * (BN / WN), 2) void linear_tile_ker
       products(wb, xb, nothing);
     }
   } else if constexpr (!SPLIT) {
-    for (int kt = 0; kt < nk; ++kt) {
+    const int scheduled = AS_IS ? nk - 1 : nk;
+    for (int kt = 0; kt < scheduled; ++kt) {
       // a token tile's fragment is read anew once its products are issued
       products(wa, xa, [&](auto q) {
         at(q, HOT_INT(0), HOT_INT(NM / 2 / TN), HOT_INT(TN), [&](auto j) { read_w(kt, 1, wb, j); });
@@ -409,6 +421,15 @@ __global__ __launch_bounds__(64 * (BM / WM) * (BN / WN), 2) void linear_tile_ker
         at(q, HOT_INT(TN + 1), HOT_INT(TN > 4 ? 2 : 1), HOT_INT(NL), [&](auto e) { load_one(kt + 2, e); });
       });
       read_x(kt + 1, 0, xa, HOT_INT(TM - 1));
+    }
+    if constexpr (AS_IS) {     // the last stage, masked
+      auto nothing = [](auto) {};
+      static_for<TN>([&](auto j) { read_w(nk - 1, 1, wb, j); });
+      mask(nk - 1, 0, wa, xa);
+      products(wa, xa, nothing);
+      static_for<TM>([&](auto i) { read_x(nk - 1, 1, xa, i); });
+      mask(nk - 1, 1, wb, xa);
+      products(wb, xa, nothing);
     }
   } else {
     v4i xb[TM];
@@ -635,7 +656,7 @@ hipError_t launch_split(const float* x, const float* w, int64_t L, int64_t O, in
   return go(integral_constant<int, 256>{}, integral_constant<int, 0>{});
 }
 
-// Rows of bfloat16 operands whose width is no multiple of 64, padded with zeros to one.  Bound by HBM.
+// Rows of bfloat16 operands of an odd width, padded with zeros to a multiple of 64.  Bound by HBM.
 __global__ __launch_bounds__(256) void linear_pad_kernel(const bf16* x, const bf16* w, int64_t L, int64_t O, int64_t I, int64_t pitch,
                                                          uint8_t* px, uint8_t* pw, int64_t first) {
   const int lane = (int)threadIdx.x & 63;
@@ -651,7 +672,8 @@ __global__ __launch_bounds__(256) void linear_pad_kernel(const bf16* x, const bf
   }
 }
 
-// What the tile kernel needs besides its operands: packed rows (fp32, or a width that is no multiple of 64) and the exponents.
+// What the large tiles need besides their operands: fp32 rows in parts with their exponents; bfloat16 rows of an odd width, or shorter than
+// 16 bytes, padded: rows that begin at odd multiples of two bytes are loaded at half the rate.
 struct TileLayout {
   int64_t pitch;
   bool packed;
@@ -659,8 +681,8 @@ struct TileLayout {
 };
 TileLayout tile_layout(hot_type type, int64_t L, int64_t O, int64_t I) {
   TileLayout t;
-  t.packed = type == HOT_F32 || I % 64 != 0;
-  t.pitch = type == HOT_F32 ? round_up(I, 32) * 4 : round_up(I, 64) * 2;
+  t.packed = type == HOT_F32 || I % 2 != 0 || I < 8;
+  t.pitch = type == HOT_F32 ? round_up(I, 32) * 4 : t.packed ? round_up(I, 64) * 2 : I * 2;
   t.w = t.packed ? (size_t)round_up(L * t.pitch, 256) : 0;
   t.exps = t.w + (t.packed ? (size_t)round_up(O * t.pitch, 256) : 0);
   t.total = t.exps + (type == HOT_F32 ? (size_t)(L + O) * 4 : 0);
@@ -693,8 +715,9 @@ double rounds_of(int64_t n) { return n <= 1024 ? (double)ceil_div(n, 256) : n / 
 // outputs, the images' way to memory and back.  256 x 256 moves half as much through LDS for each product, 128 x 128 fills the chip
 // with a quarter of the outputs: 3550 x 4380 x 5888 bfloat16 150 us against 214, 18 x 9042 x 1024 26 us against 14.
 // Slices of the tiles that leave compute units idle: 81 x 9536 x 320 bfloat16 88 -> 16 us, 1767 x 321 x 1728 fp32 26 us whole, 33 in slices.
-double tile_time(int size, hot_type type, int64_t L, int64_t O, int64_t stages, Plan* p) {
+double tile_time(int size, hot_type type, int64_t L, int64_t O, int64_t pitch, Plan* p) {
   const bool big = size == 256, f32 = type == HOT_F32;
+  const int64_t stages = ceil_div(pitch, kPiece);
   const int64_t slots = big ? 256 : 512;
   *p = Plan{};
   p->tiles = true;
@@ -704,8 +727,9 @@ double tile_time(int size, hot_type type, int64_t L, int64_t O, int64_t stages, 
   const int64_t count = p->tiles_m * p->tiles_n, rest = count % slots;
   p->whole = count;
   p->slices = 1;
-  const double full = big ? (f32 ? 1.37 : 1.06) : (f32 ? 1.23 : 0.96);    // a stage with every slot taken
-  const double half = big ? full : (f32 ? 0.54 : 0.50);                   // 128 x 128, one workgroup a compute unit
+  const double loads = pitch % kPiece ? 1.1 : 1.0;      // rows that begin anywhere (8000 x 4000 x 4000 bfloat16 229 us, x 4032 209)
+  const double full = loads * (big ? (f32 ? 1.37 : 1.06) : (f32 ? 1.23 : 0.96));    // a stage with every slot taken
+  const double half = big ? full : loads * (f32 ? 0.54 : 0.50);                     // 128 x 128, one workgroup a compute unit
   const double round = big ? (f32 ? 11.7 : 8.9) : (f32 ? 4.1 : 3.1);
   double t = (count / slots) * (stages * full + round);
   if (rest) {
@@ -779,12 +803,13 @@ double direct_time(int bm, int bn, hot_type type, int64_t L, int64_t O, int64_t 
   const int64_t count = p->tiles_m * p->tiles_n;
   if (count > kMaxLaunch / 256) return 1e30;
   p->whole = count;
+  const double odd = !f32 && I % 2 ? 1.8 : 1.0;     // as above, but for the part of a load's time that others hide
   const double moved = (((double)L + O) * bytes + (double)L * O * 4) / (f32 ? 49e6 : 15e6);
   double best = 1e30;
   for (int64_t k = 1; k <= 16; ++k) {
     if (k > 1 && (count * k > 1024 || stages / k < 4)) break;
     const int64_t n = count * k, each = ceil_div(stages, k);
-    const double cu = rounds_of(n) * (f32 ? each * 0.484 + 0.90 : each * 0.149 + 0.39), one = each * (f32 ? 0.461 : 0.235);
+    const double cu = rounds_of(n) * (f32 ? each * 0.484 + 0.90 : each * odd * 0.149 + 0.39), one = each * (f32 ? 0.461 : odd * 0.235);
     const double t = 5.3 + beside(cu, one) + moved + (k > 1 ? kLaunch + 3.0 + (double)n * bm * bn * 8 / 5.5e6 : 0.0);
     if (t < best) {
       best = t;
@@ -802,9 +827,8 @@ Plan make_plan(hot_type type, int64_t L, int64_t O, int64_t I) {
   const double tr = rows_time(type, L, O, I, &rows);
   if (lay.pitch * 256 >= (1ll << 31)) return rows;     // a tile's rows must be within the reach of a buffer descriptor
   const double operands = lay.packed ? kLaunch + 2.5 + (double)(L + O) * I * (f32 ? 8 : 4) / 5.2e6 : 0.0;
-  const int64_t stages = lay.pitch / kPiece;
-  const double ta = operands + tile_time(128, type, L, O, stages, &a), tb = operands + tile_time(256, type, L, O, stages, &b);
-  const bool direct = I * (f32 ? 4 : 2) % 16 == 0;     // 16-byte loads stay within a row or leave it whole
+  const double ta = operands + tile_time(128, type, L, O, lay.pitch, &a), tb = operands + tile_time(256, type, L, O, lay.pitch, &b);
+  const bool direct = I * (f32 ? 4 : 2) >= 16;     // a load is 16 bytes
   const double tc = direct ? direct_time(64, 64, type, L, O, I, &c) : 1e30, td = direct ? direct_time(32, 128, type, L, O, I, &d) : 1e30;
   const Plan* p = &rows;
   double t = tr;
@@ -874,11 +898,16 @@ hipError_t tiles_typed(const LinearForward& a, const Plan& p, const LinearOut& o
     g.ex = exps;
     g.ew = exps + a.L;
   }
-  constexpr int MODE = F32 ? kSplitRows : kBf16Rows;
-  stage_begin(kStLinear, s);
-  const hipError_t e = p.bm == 256 ? tiles_sized<256, 256, 64, 128, MODE, TY>(g, s) : tiles_sized<128, 128, 64, 64, MODE, TY>(g, s);
-  stage_end(kStLinear, s);
-  return e;
+  auto go = [&](auto mode) {
+    constexpr int MODE = decltype(mode)::value;
+    stage_begin(kStLinear, s);
+    const hipError_t e = p.bm == 256 ? tiles_sized<256, 256, 64, 128, MODE, TY>(g, s) : tiles_sized<128, 128, 64, 64, MODE, TY>(g, s);
+    stage_end(kStLinear, s);
+    return e;
+  };
+  if constexpr (F32) return go(std::integral_constant<int, kSplitRows>{});
+  else if (t.pitch % kPiece == 0) return go(std::integral_constant<int, kBf16Rows>{});
+  else return go(std::integral_constant<int, kBf16Ragged>{});
 }
 
 template <class T, class TY>

@@ -393,9 +393,9 @@ def test_linear_rows_with_an_infinity_or_nan_stay_alone():
             assert torch.equal(bad, want)
 
 
-# One shape for each way a product is worked on: few rows (16 or 32 outputs and 16 to 64 tokens a workgroup), operands as they are in
-# tiles of 64 x 64 and 32 x 128, packed ones in 128 x 128 and 256 x 256; each with whole tiles and in slices of K, the packed ones also
-# with slices for the last tiles alone.
+# Shapes for each way a product is worked on: few rows (16 or 32 outputs and 16 to 64 tokens a workgroup), operands as they are in
+# tiles of 64 x 64 and 32 x 128 (rows of a multiple of 16, 4 or 2 bytes), in tiles of 128 x 128 and 256 x 256 packed, as they are and as
+# they are with a last piece to mask; each with whole tiles and in slices of K, the large tiles also with slices for the last ones alone.
 LINEAR_WAYS = [
     (BF16, 522, 1909, 8), (BF16, 3, 112, 5000), (BF16, 50, 90, 88), (BF16, 1, 9, 4776), (BF16, 40, 600, 6000), (BF16, 9, 33, 4103),
     (BF16, 17, 2342, 11), (BF16, 477, 17, 7907), (BF16, 4153, 38, 9), (BF16, 3017, 8, 4995), (BF16, 5, 4188, 11), (BF16, 1, 843, 7536),
@@ -405,6 +405,14 @@ LINEAR_WAYS = [
     (F32, 536, 17, 3361), (F32, 14418, 9, 11), (F32, 1650, 8, 5097), (F32, 3, 4787, 8), (F32, 1, 1079, 3448), (F32, 3083, 56, 9),
     (F32, 602, 17, 7289), (F32, 1880, 254, 11), (F32, 2771, 17, 4114), (F32, 6353, 238, 9), (F32, 2099, 113, 1775),
     (F32, 6742, 1245, 2568), (F32, 6375, 2284, 40), (F32, 7329, 162, 5528), (F32, 5054, 3202, 528),
+    (BF16, 7, 82, 4826), (BF16, 645, 2964, 15), (BF16, 194, 4334, 12), (BF16, 11, 14, 4948), (BF16, 1, 8, 10), (BF16, 1658, 589, 3393),
+    (BF16, 18181, 4024, 9), (BF16, 1017, 2625, 6699), (BF16, 6994, 2160, 129), (BF16, 11102, 1516, 1081), (BF16, 2168, 72, 5488),
+    (BF16, 10480, 592, 8), (BF16, 2201, 3691, 5602), (BF16, 6291, 131, 9616), (BF16, 2800, 5460, 32), (BF16, 1, 8, 5818),
+    (BF16, 1, 15, 65), (BF16, 346, 17, 11102), (BF16, 4136, 8, 352), (BF16, 2685, 8, 8658), (BF16, 10985, 9, 710),
+    (BF16, 1, 4625, 272), (BF16, 1035, 18, 9792), (BF16, 17, 4153, 856), (BF16, 2508, 17, 7104), (BF16, 15606, 17, 2384),
+    (BF16, 1271, 66, 6656), (BF16, 15019, 322, 64), (BF16, 17007, 426, 10752), (BF16, 7462, 229, 9280), (BF16, 2658, 5609, 64),
+    (BF16, 3058, 5465, 896), (F32, 1, 4616, 4309), (F32, 791, 1231, 10), (F32, 1, 8, 8), (F32, 14619, 9, 40), (F32, 6262, 22, 33),
+    (F32, 9849, 17, 784),
     # operand rows of every class of width
     (F32, 2600, 1500, 301), (F32, 2600, 1500, 513), (F32, 2600, 1500, 1030), (F32, 2600, 1500, 2501), (F32, 1200, 260, 4097),
     (F32, 1200, 260, 9001), (F32, 1200, 260, 17001), (F32, 1200, 260, 40003)]
@@ -434,6 +442,18 @@ def test_linear_of_many_long_rows():
     wy, _ = ref.linear(ref.f64(x[at]), ref.f64(w), None, "none", None, F32)
     close(y[at], *wy, "y")
     assert bool(torch.isfinite(y).all())
+
+
+@pytest.mark.parametrize("t,L,O,I", [(BF16, 300, 1000, 1490), (BF16, 300, 1000, 1491), (F32, 700, 513, 301), (BF16, 2800, 5460, 34), (BF16, 700, 700, 10)])
+def test_rows_of_any_width_stay_alone(t, L, O, I):
+    """NaN at the ends of rows that begin and end inside a load reaches those rows alone."""
+    x, w = rand((L, I), 1, t), rand((O, I), 2, t)
+    x[5, 0], x[L - 2, I - 1], w[3, I - 1], w[O - 1, 0] = (float("nan"),) * 4
+    y = torch.empty((L, O), dtype=t, device="cuda")
+    hot.hot_linear_forward(x.cuda(), w.cuda(), y, hot.alloc_linear_workspace(t, L, O, I))
+    want = torch.zeros(L, O, dtype=torch.bool)
+    want[5], want[L - 2], want[:, 3], want[:, O - 1] = True, True, True, True
+    assert torch.equal(torch.isnan(y.cpu()), want)
 
 
 # ---- tensors past 32 bits ---------------------------------------------------------------------------------------------
