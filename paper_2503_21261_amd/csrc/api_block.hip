@@ -48,7 +48,7 @@ size_t activation_sums_bytes(int64_t rows, int64_t cols) {
   return (size_t)activation_sum_rows(rows, cols) * round_up(cols, 32) * 4;
 }
 size_t norm_sums_bytes(int64_t rows, int64_t cols) {
-  return (size_t)layer_norm_sum_rows(rows, cols) * 2 * round_up(cols, 32) * 4;
+  return (size_t)layer_norm_sum_rows(rows, cols, HOT_BF16) * 2 * round_up(cols, 32) * 4;
 }
 
 #define HOT_STAGE(stage, expr)                   \
@@ -188,7 +188,7 @@ hot_status hot_layer_norm_backward(const void* g_y, hot_type y_type, const void*
   if (g_gamma && ws_bytes < need) return HOT_ERR_WORKSPACE;
   hipStream_t s = (hipStream_t)stream;
   const int64_t pitch = round_up(cols, 32);
-  const int sums = layer_norm_sum_rows(rows, cols);
+  const int sums = layer_norm_sum_rows(rows, cols, x_type);
   const bool apart = g_gamma && sums > 1;
   NormBackward a{g_y, h, ckpt, g_residual, gamma, mean, rstd, rows, cols, x_type, y_type, g_x, g_gamma, g_beta, 0};
   if (apart) {

@@ -63,6 +63,8 @@ __device__ __forceinline__ void widen(const Raw8<bf16>& r, float (&v)[8]) {
 #pragma unroll
   for (int i = 0; i < 8; ++i) v[i] = bf16_to_float(r.a[i]);
 }
+// STREAM: with the hint that nothing reads the values soon.
+template <bool STREAM = false>
 __device__ __forceinline__ void store8(float* p, const float (&v)[8], int n) {
   if (n >= 8) {
     f4_any a, b;
@@ -71,21 +73,33 @@ __device__ __forceinline__ void store8(float* p, const float (&v)[8], int n) {
       a[i] = v[i];
       b[i] = v[i + 4];
     }
-    *(f4_any*)p = a;
-    *(f4_any*)(p + 4) = b;
+    if constexpr (STREAM) {
+      __builtin_nontemporal_store(a, (f4_any*)p);
+      __builtin_nontemporal_store(b, (f4_any*)(p + 4));
+      asm volatile("");   // else this store and the plain one of another branch become one plain store
+    } else {
+      *(f4_any*)p = a;
+      *(f4_any*)(p + 4) = b;
+    }
   } else {
 #pragma unroll
     for (int i = 0; i < 8; ++i)
       if (i < n) p[i] = v[i];
   }
 }
+template <bool STREAM = false>
 __device__ __forceinline__ void store8(bf16* p, const float (&v)[8], int n) {
   uint16_t* q = (uint16_t*)p;
   if (n >= 8) {
     h8_any a;
 #pragma unroll
     for (int i = 0; i < 8; ++i) a[i] = float_to_bf16(v[i]);
-    *(h8_any*)q = a;
+    if constexpr (STREAM) {
+      __builtin_nontemporal_store(a, (h8_any*)q);
+      asm volatile("");
+    } else {
+      *(h8_any*)q = a;
+    }
   } else {
 #pragma unroll
     for (int i = 0; i < 8; ++i)
@@ -160,10 +174,17 @@ struct CkptView {
   int64_t pitch;
 };
 // `at`: row * pitch + column, a multiple of 8; called by all four lanes of a group together.
+template <bool STREAM = false>
 __device__ __forceinline__ void ckpt_store8(const CkptView& k, int64_t at, const float (&v)[8]) {
   const uint32_t e = ckpt_exponent(quad_max(magnitude8(v)));
   const float inverse = ckpt_inverse(e);
-  *(uint2*)(k.codes + at) = encode8(v, inverse);
+  const uint2 c = encode8(v, inverse);
+  if constexpr (STREAM) {
+    __builtin_nontemporal_store((uint64_t)c.y << 32 | c.x, (uint64_t*)(k.codes + at));
+    asm volatile("");
+  } else {
+    *(uint2*)(k.codes + at) = c;
+  }
   if (rarely(e == 254u)) {   // at the type's end, where the next step is missing: 127.5 steps and more are held at 127
     float w[8];
 #pragma unroll

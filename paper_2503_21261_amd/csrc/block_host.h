@@ -20,11 +20,15 @@ inline CkptLayout ckpt_layout(int64_t rows, int64_t cols) {
 // Lanes of one launch: a launch of 2^32 or more is refused, so the longest tensors take several.
 constexpr int64_t kMaxLaunch = 1ll << 31;
 
+// Whether an output of `rows` rows of `pitch` bytes is stored with the streaming hint: what the L2s (32 MB) could not hold anyway, in
+// rows of whole lines.
+inline bool stream_output(int64_t rows, int64_t pitch) { return rows * pitch > (32 << 20) && pitch % 128 == 0; }
+
 // Rows of partial sums that a column sum over `rows` rows leaves, and its width: the gradient kernels
 // write one such row per row group, `column_sums` adds them; a single row is the sum, and goes where that belongs.
 constexpr int kMaxSumRows = 1024;
 int activation_sum_rows(int64_t rows, int64_t cols);
-int layer_norm_sum_rows(int64_t rows, int64_t cols);
+int layer_norm_sum_rows(int64_t rows, int64_t cols, hot_type x_type);   // bfloat16: as many as fp32 or more
 
 // x -> y = f(x) (y may be null) and the checkpoint of x (ckpt may be null).
 hipError_t launch_activation(int fn, const void* x, hot_type type, int64_t rows, int64_t cols, void* y, void* ckpt,

@@ -5,7 +5,7 @@
 //
 // Both are bound by HBM.  A row stays in the registers of the T lanes that work on it (eight columns a
 // lane, NV times), so it is read once: the mean first, then the squares of what is left, which keeps the
-// variance of rows whose mean is large.  The backward pass keeps a lane on its columns, so that the
+// variance of rows whose mean is large.  201728 x 1024 fp32 with residual and checkpoint: 660 us forward, 500 back, 5.3 TB/s.  The backward pass keeps a lane on its columns, so that the
 // parameter gradients are sums in registers; a workgroup leaves one row of them, and column_sums adds those in order.
 #include <type_traits>
 
@@ -15,6 +15,10 @@
 namespace hot {
 
 namespace {
+
+__device__ __forceinline__ void anew(Raw8<float>& r) { asm volatile("" : "+v"(r.a), "+v"(r.b)); }
+__device__ __forceinline__ void anew(Raw8<bf16>& r) { asm volatile("" : "+v"(r.a)); }
+__device__ __forceinline__ void anew(uint2& c) { asm volatile("" : "+v"(c.x), "+v"(c.y)); }
 
 template <int T>
 constexpr int kThreads = T > 256 ? T : 256;
@@ -134,7 +138,7 @@ __global__ __launch_bounds__(kThreads<T>) void layer_norm_kernel(const NormForwa
   }
 }
 
-template <int T, int NV, class TX, class TY, bool KEPT, bool EVEN>
+template <int T, int NV, class TX, class TY, bool KEPT, bool EVEN, bool STREAM>
 __global__ __launch_bounds__(kThreads<T>) void layer_norm_grad_kernel(const NormBackward a, const CkptView k) {
   constexpr int SPAN = T * NV * 8;    // columns the lanes of a row cover
   __shared__ float s_red[2][16][2];
@@ -177,24 +181,28 @@ __global__ __launch_bounds__(kThreads<T>) void layer_norm_grad_kernel(const Norm
       }
     }
     const float mean = a.mean[row], rstd = a.rstd[row];
-    float t[NV][8], n[NV][8], s1 = 0.0f, s2 = 0.0f;
+    // n and g_y of a chunk
+    auto values = [&](int j, float(&n)[8], float(&t)[8]) {
+      widen(gr[j], t);
+      if constexpr (KEPT) decode8(codes[j], ckpt_step(e[j]), n);
+      else widen(hr[j], n);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) n[i] = (n[i] - mean) * rstd;
+    };
+    float s1 = 0.0f, s2 = 0.0f;
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
       const int c = (lane + j * T) * 8;
-#pragma unroll
-      for (int i = 0; i < 8; ++i) t[j][i] = n[j][i] = 0.0f;
       if (c < cols) {
-        widen(gr[j], t[j]);
-        if constexpr (KEPT) decode8(codes[j], ckpt_step(e[j]), n[j]);
-        else widen(hr[j], n[j]);
+        float n[8], t[8];
+        values(j, n, t);
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-          n[j][i] = (n[j][i] - mean) * rstd;
-          sb[j][i] += t[j][i];
-          sg[j][i] = fmaf(t[j][i], n[j][i], sg[j][i]);
-          t[j][i] *= gamma[j][i];
-          s1 += t[j][i];
-          s2 = fmaf(t[j][i], n[j][i], s2);
+          sb[j][i] += t[i];
+          sg[j][i] = fmaf(t[i], n[i], sg[j][i]);
+          t[i] *= gamma[j][i];
+          s1 += t[i];
+          s2 = fmaf(t[i], n[i], s2);
         }
       }
     }
@@ -205,14 +213,21 @@ __global__ __launch_bounds__(kThreads<T>) void layer_norm_grad_kernel(const Norm
     for (int j = 0; j < NV; ++j) {
       const int c = (lane + j * T) * 8;
       if (c < cols) {
-        float r[8];
+        // Once more from what was loaded: to keep them takes 160 registers where 1024 lanes have 128 each (16384 x 11008 bfloat16 from
+        // a checkpoint 252 us, 898 with what spilled), and leaves fewer rows on their way.  As new values to the compiler, which
+        // would keep them all the same.
+        anew(gr[j]);
+        if constexpr (KEPT) anew(codes[j]);
+        else anew(hr[j]);
+        float n[8], t[8], r[8];
+        values(j, n, t);
         if (a.g_residual) widen(ar[j], r);
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-          const float g = rstd * (t[j][i] - m1 - n[j][i] * m2);
-          t[j][i] = a.g_residual ? g + r[i] : g;
+          const float g = rstd * (t[i] * gamma[j][i] - m1 - n[i] * m2);
+          t[i] = a.g_residual ? g + r[i] : g;
         }
-        store8((TX*)a.g_x + at + c, t[j], have(c));
+        store8<STREAM>((TX*)a.g_x + at + c, t, have(c));
       }
     }
   }
@@ -248,8 +263,8 @@ __global__ __launch_bounds__(kThreads<T>) void layer_norm_grad_kernel(const Norm
   }
 }
 
-// Lanes to a row: the fewest that hold it with eight or sixteen columns each.  The gradient's registers, six values a column, leave no
-// room for more: 4000 x 11008 bfloat16 takes 80 us on 1024 lanes, 95 on 256 with 64 columns each, which spill.
+// Lanes to a row: the fewest that hold it with eight or sixteen columns each.  The gradient's registers, three fp32 values a column and
+// what was loaded, leave no room for more.
 template <class F>
 hipError_t with_lanes(int64_t cols, F&& f) {
   using std::integral_constant;
@@ -282,12 +297,14 @@ CkptView view(const void* ckpt, int64_t rows, int64_t cols) {
 }  // namespace
 
 // Workgroups of the backward pass, one row of partial sums each: one, whose sums are the gradients themselves, while its turns
-// take no longer than a second launch; two a compute unit while rows are few; as many as are resident together (their registers:
-// 100, or 160 with sixteen columns a lane) once every workgroup has eight turns, so that none waits for another to end.
-int layer_norm_sum_rows(int64_t rows, int64_t cols) {
+// take no longer than a second launch; two a compute unit while rows are few; once every workgroup has eight turns, as many as are
+// resident together, so that none waits for another to end: four of 256 lanes a compute unit.  With sixteen columns a lane fp32 rows
+// do better with three (50432 x 1024 with g_residual 161 us, 169 with four), bfloat16 ones with four (40000 x 1000 52, 54 with three).
+int layer_norm_sum_rows(int64_t rows, int64_t cols, hot_type x_type) {
   const int64_t turns = ceil_div(rows, slots_of(cols));
   if (turns <= 2) return 1;
-  const int64_t resident = cols > 8192 ? 256 : cols > 4096 ? 512 : (cols > 512 && cols <= 1024) || cols > 2048 ? 768 : 1024;
+  const bool wide = (cols > 512 && cols <= 1024) || cols > 2048;
+  const int64_t resident = cols > 8192 ? 256 : cols > 4096 ? 512 : wide && x_type == HOT_F32 ? 768 : 1024;
   const int64_t few = resident < 512 ? resident : 512;
   const int64_t g = turns < few ? turns : few, many = turns / 8 < resident ? turns / 8 : resident;
   return (int)(many > g ? many : g);
@@ -320,10 +337,17 @@ hipError_t launch_layer_norm_grad(const NormBackward& a, hipStream_t s) {
       constexpr bool EVEN = decltype(e)::value;
       using TX = decltype(tx);
       using TY = decltype(ty);
-      const dim3 grid((unsigned)layer_norm_sum_rows(a.rows, a.cols)), block(kThreads<T>);
-      if (a.ckpt) layer_norm_grad_kernel<T, NV, TX, TY, true, EVEN><<<grid, block, 0, s>>>(a, view(a.ckpt, a.rows, a.cols));
-      else layer_norm_grad_kernel<T, NV, TX, TY, false, EVEN><<<grid, block, 0, s>>>(a, CkptView{});
-      return hipGetLastError();
+      const dim3 grid((unsigned)layer_norm_sum_rows(a.rows, a.cols, a.x_type)), block(kThreads<T>);
+      auto launch = [&](auto stream) {
+        constexpr bool STREAM = decltype(stream)::value;
+        if (a.ckpt) layer_norm_grad_kernel<T, NV, TX, TY, true, EVEN, STREAM><<<grid, block, 0, s>>>(a, view(a.ckpt, a.rows, a.cols));
+        else layer_norm_grad_kernel<T, NV, TX, TY, false, EVEN, STREAM><<<grid, block, 0, s>>>(a, CkptView{});
+        return hipGetLastError();
+      };
+      if constexpr (EVEN && sizeof(TX) == 2) {    // as for the activation's gradient: 8192 x 4096 bfloat16 42 -> 38 us
+        if (stream_output(a.rows, a.cols * (int64_t)sizeof(TX))) return launch(std::true_type{});
+      }
+      return launch(std::false_type{});
     });
   });
 }

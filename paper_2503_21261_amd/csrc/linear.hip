@@ -935,7 +935,7 @@ hipError_t rows_typed(const LinearForward& a, const Plan& p, const LinearOut& o,
 
 template <class T, class TY>
 hipError_t linear_run(const LinearForward& a, const CkptView& k, hipStream_t s) {
-  LinearOut o{a.bias, a.residual, a.y, k, a.L, (int)a.O, a.fn};
+  LinearOut o{a.bias, a.residual, a.y, k, a.L, (int)a.O, a.fn, stream_output(a.L, a.O * (int64_t)sizeof(TY))};
   Plan p = make_plan(a.type, a.L, a.O, a.I);
   if (k.codes && !p.tiles && p.slices == 1 && p.nt == 1) {   // a group is finished by one workgroup
     p.nt = 2;

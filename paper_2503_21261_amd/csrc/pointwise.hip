@@ -5,6 +5,7 @@
 // columns of a row (a 32-column group of the 8-bit form is four lanes, so its maximum is two DPP
 // permutes), TX lanes a segment of a row, 256 / TX rows a workgroup at a time.  The walk is two-dimensional
 // so that odd widths need no division per element and a lane keeps its columns for the column sums.
+// SiLU, its gradient and the bias's of 16384 x 11008 bfloat16 334 us, 5.4 TB/s; a checkpoint of 12608 x 768 fp32 written and read 20 us.
 #include <type_traits>
 
 #include "block_device.h"
@@ -86,7 +87,7 @@ __device__ __forceinline__ void whole_or_not(const Walk& w, int ct, int64_t batc
 }
 
 // y = f(x), the checkpoint of x, or both, from one read of x.
-template <class T, int FN, bool VALUE, bool KEEP>
+template <class T, int FN, bool VALUE, bool KEEP, bool STREAM>
 __global__ __launch_bounds__(256) void activation_kernel(const T* x, Walk w, T* y, void* ckpt) {
   Position p;
   int tx, ty, ct, rg;
@@ -110,18 +111,18 @@ __global__ __launch_bounds__(256) void activation_kernel(const T* x, Walk w, T* 
       if (WHOLE || row < w.rows) {
         float v[8];
         widen(raw[i], v);
-        if constexpr (KEEP) ckpt_store8(k, row * k.pitch + col, v);
+        if constexpr (KEEP) ckpt_store8<STREAM>(k, row * k.pitch + col, v);
         if constexpr (VALUE) {
 #pragma unroll
           for (int j = 0; j < 8; ++j) v[j] = act_value<FN>(v[j]);
-          store8(y + row * w.cols + col, v, n);
+          store8<STREAM>(y + row * w.cols + col, v, n);
         }
       }
     }
   });
 }
 
-template <class T>
+template <class T, bool STREAM>
 __global__ __launch_bounds__(256) void checkpoint_read_kernel(const uint8_t* ckpt, Walk w, T* x) {
   Position p;
   int tx, ty, ct, rg;
@@ -150,14 +151,14 @@ __global__ __launch_bounds__(256) void checkpoint_read_kernel(const uint8_t* ckp
       if (WHOLE || row < w.rows) {
         float v[8];
         decode8(codes[i], ckpt_step(e[i]), v);
-        store8(x + row * w.cols + col, v, n);
+        store8<STREAM>(x + row * w.cols + col, v, n);
       }
     }
   });
 }
 
 // g_x = g_y f'(x); SUMS: a row of partial sums of g_x (in fp32, before it is rounded to T) per row group.
-template <class T, int FN, bool KEPT, bool SUMS>
+template <class T, int FN, bool KEPT, bool SUMS, bool STREAM>
 __global__ __launch_bounds__(256) void activation_grad_kernel(const T* g_y, const T* x, const uint8_t* ckpt, Walk w, T* g_x,
                                                               float* partials, int64_t pitch) {
   __shared__ float s_sum[SUMS ? 256 * 8 : 1];
@@ -204,7 +205,7 @@ __global__ __launch_bounds__(256) void activation_grad_kernel(const T* g_y, cons
               g[j] *= act_slope<FN>(v[j]);
               if constexpr (SUMS) sum[j] += g[j];
             }
-            store8(g_x + row * w.cols + col, g, n);
+            store8<STREAM>(g_x + row * w.cols + col, g, n);
           }
         }
       });
@@ -250,14 +251,28 @@ __global__ __launch_bounds__(1024) void column_sums_kernel(const float* partials
   if (tx == 0 && oc < cols) dst[oc] = v;
 }
 
+// f(true_type) for outputs that are stored with the streaming hint.  Cold tensors of 16384 x 11008 bfloat16: SiLU with checkpoint 168 -> 160
+// us, its gradient 165 -> 159, checkpoint read 94 -> 89; with rows that end inside a line (100000 x 1000) the read takes 102 instead of 64.
+// Not for fp32, whose eight columns a lane are two stores that each leave half a line to the other: 201728 x 1024 350 us, 450 with it.
+template <class T, class F>
+hipError_t with_stream(int64_t rows, int64_t cols, F&& f) {
+  if constexpr (sizeof(T) == 2) {
+    if (stream_output(rows, cols * (int64_t)sizeof(T))) return f(std::true_type{});
+  }
+  return f(std::false_type{});
+}
+
 template <class T, int FN>
 hipError_t activation_typed(const T* x, int64_t rows, int64_t cols, T* y, void* ckpt, hipStream_t s) {
   const Walk w = make_walk(rows, cols);
   const dim3 grid((unsigned)(w.col_tiles * w.batches)), block(256);
-  if (y && ckpt) activation_kernel<T, FN, true, true><<<grid, block, 0, s>>>(x, w, y, ckpt);
-  else if (y) activation_kernel<T, FN, true, false><<<grid, block, 0, s>>>(x, w, y, nullptr);
-  else activation_kernel<T, HOT_ACT_NONE, false, true><<<grid, block, 0, s>>>(x, w, nullptr, ckpt);
-  return hipGetLastError();
+  return with_stream<T>(rows, cols, [&](auto stream) {
+    constexpr bool STREAM = decltype(stream)::value;
+    if (y && ckpt) activation_kernel<T, FN, true, true, STREAM><<<grid, block, 0, s>>>(x, w, y, ckpt);
+    else if (y) activation_kernel<T, FN, true, false, STREAM><<<grid, block, 0, s>>>(x, w, y, nullptr);
+    else activation_kernel<T, HOT_ACT_NONE, false, true, STREAM><<<grid, block, 0, s>>>(x, w, nullptr, ckpt);
+    return hipGetLastError();
+  });
 }
 
 template <class T, int FN>
@@ -265,19 +280,22 @@ hipError_t grad_typed(const T* g_y, const T* x, const void* ckpt, int64_t rows, 
                       int64_t pitch, hipStream_t s) {
   Walk w = make_walk(rows, cols);
   const uint8_t* k = (const uint8_t*)ckpt;
-  const dim3 block(256);
+  auto go = [&](auto sums, dim3 grid) {
+    constexpr bool SUMS = decltype(sums)::value;
+    return with_stream<T>(rows, cols, [&](auto stream) {
+      constexpr bool STREAM = decltype(stream)::value;
+      if (k) activation_grad_kernel<T, FN, true, SUMS, STREAM><<<grid, dim3(256), 0, s>>>(g_y, x, k, w, g_x, partials, pitch);
+      else activation_grad_kernel<T, FN, false, SUMS, STREAM><<<grid, dim3(256), 0, s>>>(g_y, x, k, w, g_x, partials, pitch);
+      return hipGetLastError();
+    });
+  };
   if (partials) {
     w.row_groups = sum_groups(w);
     const dim3 grid((unsigned)(w.col_tiles * w.row_groups));
-    if (k) activation_grad_kernel<T, FN, true, true><<<grid, block, 0, s>>>(g_y, x, k, w, g_x, partials, pitch);
-    else activation_grad_kernel<T, FN, false, true><<<grid, block, 0, s>>>(g_y, x, k, w, g_x, partials, pitch);
-  } else {
-    w.row_groups = (int)w.batches;
-    const dim3 grid((unsigned)(w.col_tiles * w.batches));
-    if (k) activation_grad_kernel<T, FN, true, false><<<grid, block, 0, s>>>(g_y, x, k, w, g_x, nullptr, 0);
-    else activation_grad_kernel<T, FN, false, false><<<grid, block, 0, s>>>(g_y, x, k, w, g_x, nullptr, 0);
+    return go(std::true_type{}, grid);
   }
-  return hipGetLastError();
+  w.row_groups = (int)w.batches;
+  return go(std::false_type{}, dim3((unsigned)(w.col_tiles * w.batches)));
 }
 
 template <class F>
@@ -306,8 +324,12 @@ hipError_t launch_activation(int fn, const void* x, hot_type type, int64_t rows,
 hipError_t launch_checkpoint_read(const void* ckpt, int64_t rows, int64_t cols, void* x, hot_type type, hipStream_t s) {
   const Walk w = make_walk(rows, cols);
   const dim3 grid((unsigned)(w.col_tiles * w.batches)), block(256);
-  if (type == HOT_BF16) checkpoint_read_kernel<bf16><<<grid, block, 0, s>>>((const uint8_t*)ckpt, w, (bf16*)x);
-  else checkpoint_read_kernel<float><<<grid, block, 0, s>>>((const uint8_t*)ckpt, w, (float*)x);
+  if (type == HOT_BF16)
+    return with_stream<bf16>(rows, cols, [&](auto stream) {
+      checkpoint_read_kernel<bf16, decltype(stream)::value><<<grid, block, 0, s>>>((const uint8_t*)ckpt, w, (bf16*)x);
+      return hipGetLastError();
+    });
+  checkpoint_read_kernel<float, false><<<grid, block, 0, s>>>((const uint8_t*)ckpt, w, (float*)x);
   return hipGetLastError();
 }
 
