@@ -803,13 +803,15 @@ double direct_time(int bm, int bn, hot_type type, int64_t L, int64_t O, int64_t 
   const int64_t count = p->tiles_m * p->tiles_n;
   if (count > kMaxLaunch / 256) return 1e30;
   p->whole = count;
-  const double odd = !f32 && I % 2 ? 1.8 : 1.0;     // as above, but for the part of a load's time that others hide
-  const double moved = (((double)L + O) * bytes + (double)L * O * 4) / (f32 ? 49e6 : 15e6);
+  // loads that begin at odd multiples of two bytes: the stages' share, a workgroup's by itself, what is moved (a fit to 260 shapes)
+  const bool unaligned = !f32 && I % 2;
+  const double odd = !unaligned ? 1.0 : bm == 64 ? 2.2 : 2.8, alone = unaligned ? 1.6 : 1.0, bytes_odd = unaligned ? 2.0 : 1.0;
+  const double moved = bytes_odd * (((double)L + O) * bytes + (double)L * O * 4) / (f32 ? 49e6 : 15e6);
   double best = 1e30;
   for (int64_t k = 1; k <= 16; ++k) {
     if (k > 1 && (count * k > 1024 || stages / k < 4)) break;
     const int64_t n = count * k, each = ceil_div(stages, k);
-    const double cu = rounds_of(n) * (f32 ? each * 0.484 + 0.90 : each * odd * 0.149 + 0.39), one = each * (f32 ? 0.461 : odd * 0.235);
+    const double cu = rounds_of(n) * (f32 ? each * 0.484 + 0.90 : each * odd * 0.149 + 0.39), one = each * (f32 ? 0.461 : alone * 0.235);
     const double t = 5.3 + beside(cu, one) + moved + (k > 1 ? kLaunch + 3.0 + (double)n * bm * bn * 8 / 5.5e6 : 0.0);
     if (t < best) {
       best = t;
