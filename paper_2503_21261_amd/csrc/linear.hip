@@ -209,8 +209,8 @@ __global__ __launch_bounds__(256) void linear_rows_combine_kernel(const float* s
 // registers for each product, and as the chip's power holds such products down, that is time (8192^3 bfloat16 1417 TFLOP/s, 1323
 // with them; stages of 64 bytes, four deep: a tenth less).  The weight is the first operand, so that accumulators are runs of four
 // outputs of a token; they leave through LDS, a wave's 32 tokens at a time, as runs of eight outputs a lane.
-// Measured: 16384 x 11008 x 4096 bfloat16 with GELU and checkpoint 1240 us, 1190 TFLOP/s (its epilogue is 12 us of vector
-// instructions a round of tiles); 12608 x 2304 x 768 fp32 125 us, 1070 TFLOP/s of fp16 products, and 20 us for its operands.
+// Measured: 16384 x 11008 x 4096 bfloat16 1070 us, 1380 TFLOP/s; with a checkpoint 1095, with GELU 1125 (vector instructions of the
+// epilogue, under which no matrix instruction runs), with both 1155; 12608 x 2304 x 768 fp32 125 us, 1070 TFLOP/s of fp16 products, and 20 us for its operands.
 typedef _Float16 v8h __attribute__((ext_vector_type(8)));
 typedef int v4i __attribute__((ext_vector_type(4)));
 
@@ -225,7 +225,8 @@ __device__ __forceinline__ void static_for(F&& f) {
 }
 
 // 16 bytes a lane, at byte offset `lane_off` + `off` of the descriptor, to 1024 consecutive bytes of LDS (`to`: the same in
-// all lanes).  Counted by vmcnt; the caller waits.
+// all lanes).  Counted by vmcnt; the caller waits.  The source may begin at any byte (the memory pipe runs in its unaligned mode):
+// at a multiple of four it costs a tenth at most, at an odd multiple of two as much again.
 using rsrc_t = decltype(__builtin_amdgcn_make_buffer_rsrc((void*)nullptr, 0, 0, 0));
 __device__ __forceinline__ void load_to_lds(rsrc_t from, uint8_t* to, int lane_off, int off) {
 #if defined(__HIP_DEVICE_COMPILE__)   // the host's pass does not know gfx950's 16-byte form
