@@ -210,7 +210,8 @@ __global__ __launch_bounds__(256) void linear_rows_combine_kernel(const float* s
 // with them; stages of 64 bytes, four deep: a tenth less).  The weight is the first operand, so that accumulators are runs of four
 // outputs of a token; they leave through LDS, a wave's 32 tokens at a time, as runs of eight outputs a lane.
 // Measured: 16384 x 11008 x 4096 bfloat16 1070 us, 1380 TFLOP/s; with a checkpoint 1095, with GELU 1125 (vector instructions of the
-// epilogue, under which no matrix instruction runs), with both 1155; 12608 x 2304 x 768 fp32 125 us, 1070 TFLOP/s of fp16 products, and 20 us for its operands.
+// epilogue, under which no matrix instruction runs), with both 1155; 12608 x 2304 x 768 fp32 125 us, 1070 TFLOP/s of fp16 products,
+// and 20 us for its operands.
 typedef _Float16 v8h __attribute__((ext_vector_type(8)));
 typedef int v4i __attribute__((ext_vector_type(4)));
 

@@ -69,8 +69,8 @@ __device__ __forceinline__ void linear_finish8(const LinearOut& o, int64_t row, 
   } else if (sizeof(TY) == 2 || __builtin_amdgcn_ballot_w64(n < 8)) {
     store8<true>((TY*)o.y + at, v, n);
   } else {
-    // fp32, both lanes of a pair (a streamed row is whole groups of 32 columns): they exchange halves, so that each store of theirs is 32 bytes in a row (12608 x 2304 x 768 142 us, 148
-    // with four of every eight columns a store)
+    // fp32, both lanes of a pair (a streamed row is whole groups of 32 columns): they exchange halves, so that each store of theirs is
+    // 32 bytes in a row (12608 x 2304 x 768 142 us, 148 with four of every eight columns a store)
     const bool odd = threadIdx.x & 1;
     f4_any first, second;
 #pragma unroll
