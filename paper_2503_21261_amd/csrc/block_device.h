@@ -230,8 +230,9 @@ __device__ __forceinline__ float act_value(float x) {
     const float held = __int_as_float(min(bits, 0x71800000)), positive = __int_as_float(max(bits, 0));
     return fmaf(-fabsf(held), normal_tail(fabsf(x), gauss_of(x)), positive);
   } else if constexpr (FN == HOT_ACT_GELU_TANH) {
-    const float xc = clamp30(x);
-    return x * sigmoid_of(gelu_tanh_arg(xc));
+    // the argument in powers of two; a NaN that the clamp loses is one by the last product
+    const float xc = __builtin_amdgcn_fmed3f(x, -30.0f, 30.0f);
+    return x * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(xc * fmaf(xc * xc, -0.1029432396f, -2.3022081985f)));
   } else if constexpr (FN == HOT_ACT_SILU) return x * sigmoid_of(x);
   else return x;
 }
