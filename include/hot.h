@@ -246,7 +246,7 @@ hot_status hot_lowpass_l1_rows(int32_t block, int32_t keep, int32_t* keep_idx);
  */
 typedef enum { HOT_F32 = 0, HOT_BF16 = 1 } hot_type;
 
-/* RELU max(x, 0) (slope 0 at 0); GELU x Phi(x); GELU_TANH its tanh form,
+/* RELU max(x, 0) (slope 0 at 0, NaN at a NaN); GELU x Phi(x); GELU_TANH its tanh form,
  * x / 2 (1 + tanh(sqrt(2 / pi) (x + 0.044715 x^3))); SILU x / (1 + exp(-x)). */
 typedef enum {
   HOT_ACT_NONE = 0, HOT_ACT_RELU = 1, HOT_ACT_GELU = 2, HOT_ACT_GELU_TANH = 3, HOT_ACT_SILU = 4

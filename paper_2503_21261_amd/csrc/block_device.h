@@ -238,7 +238,7 @@ __device__ __forceinline__ float act_value(float x) {
 }
 template <int FN>
 __device__ __forceinline__ float act_slope(float x) {
-  if constexpr (FN == HOT_ACT_RELU) return x <= 0.0f ? 0.0f : 1.0f;
+  if constexpr (FN == HOT_ACT_RELU) return x > 0.0f ? 1.0f : x <= 0.0f ? 0.0f : x;   // a NaN (a group that held one, too) stays one
   else if constexpr (FN == HOT_ACT_GELU) {
     const float a = fabsf(x), g = gauss_of(x), tail = normal_tail(a, g);
     return fmaf(x * g, 0.39894228040143f, x < 0.0f ? tail : 1.0f - tail);
