@@ -402,8 +402,10 @@ hot_status hot_debug_set_gemm_mode(int mode);
 
 /* ---- stage timing for benchmarks (off by default) ---- */
 
-/* Kernel roles timed separately; hot_debug_stage_name() gives their names. */
-#define HOT_NUM_STAGES 24
+/* Kernel roles timed separately; hot_debug_stage_name() gives their names.  The first HOT_NUM_STAGES are those of the
+ * linear backward, the others those of the operators around it. */
+#define HOT_NUM_STAGES 15
+#define HOT_NUM_STAGES_ALL 24
 
 /* From this call on, every kernel the library launches is bracketed by two HIP
  * events recorded on its stream.  Host-side state only; not thread-safe against
@@ -412,8 +414,12 @@ hot_status hot_debug_profile_begin(void);
 
 /* Stops recording, waits for the recorded events, and returns per stage the
  * summed elapsed milliseconds and the number of launches (host arrays of
- * HOT_NUM_STAGES entries). */
+ * HOT_NUM_STAGES entries: the stages of the linear backward alone). */
 hot_status hot_debug_profile_end(float* stage_ms, int64_t* stage_launches);
+
+/* The same for the first `count` stages of all (host arrays of `count` entries; those past
+ * HOT_NUM_STAGES_ALL become 0). */
+hot_status hot_debug_profile_end_all(float* stage_ms, int64_t* stage_launches, int32_t count);
 
 /* The stages of the recording that the last hot_debug_profile_end closed, in launch order:
  * writes up to `capacity` stage ids to `stages` (host; may be NULL) and returns how many

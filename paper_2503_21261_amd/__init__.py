@@ -31,14 +31,14 @@ EXPORTS = (
     "hot_debug_unpack_weight", "hot_compress_activation", "hot_linear_backward_gx", "hot_linear_backward_gw",
     "hot_linear_backward", "hot_linear_backward_gx_noalloc", "hot_lowpass_l1_rows", "hot_select_quantizer", "hot_debug_unpack_activation",
     "hot_debug_gx_operands", "hot_debug_gw_operands", "hot_debug_fused_operands", "hot_debug_set_exchange_wait_us",
-    "hot_debug_set_backward_strategy", "hot_debug_set_gemm_mode", "hot_debug_profile_begin", "hot_debug_profile_end", "hot_debug_profile_sequence",
+    "hot_debug_set_backward_strategy", "hot_debug_set_gemm_mode", "hot_debug_profile_begin", "hot_debug_profile_end", "hot_debug_profile_end_all", "hot_debug_profile_sequence",
     "hot_debug_stage_name", "hot_debug_probe", "hot_debug_gemm_plan",
     "hot_checkpoint_bytes", "hot_checkpoint_write", "hot_checkpoint_read", "hot_activation_forward",
     "hot_activation_backward_workspace_bytes", "hot_activation_backward", "hot_layer_norm_forward",
     "hot_layer_norm_backward_workspace_bytes", "hot_layer_norm_backward", "hot_linear_forward_workspace_bytes",
     "hot_linear_forward",
 )
-HOT_NUM_STAGES = 24
+HOT_NUM_STAGES, HOT_NUM_STAGES_ALL = 15, 24
 HOT_WS_PREFIX_BYTES = 24832
 HOT_F32, HOT_BF16 = 0, 1
 HOT_ACT_NONE, HOT_ACT_RELU, HOT_ACT_GELU, HOT_ACT_GELU_TANH, HOT_ACT_SILU = range(5)
@@ -101,6 +101,7 @@ def lib() -> C.CDLL:
         l.hot_debug_set_gemm_mode.argtypes = [C.c_int]
         l.hot_debug_profile_begin.argtypes = []
         l.hot_debug_profile_end.argtypes = [C.POINTER(C.c_float), C.POINTER(C.c_int64)]
+        l.hot_debug_profile_end_all.argtypes = [C.POINTER(C.c_float), C.POINTER(C.c_int64), C.c_int32]
         l.hot_debug_gemm_plan.argtypes = [cfgp, i64, i64, i64, C.POINTER(hot_gemm_plan)]
         l.hot_debug_probe.argtypes = [C.c_int, vp, sz, C.c_int, vp]
         l.hot_debug_profile_sequence.argtypes = [C.POINTER(C.c_int32), C.c_int64]
@@ -633,11 +634,11 @@ def hot_debug_profile_begin() -> None:
 
 def hot_debug_profile_end():
     """Returns {stage name: (total ms, launches)} for the stages that ran."""
-    ms = (C.c_float * HOT_NUM_STAGES)()
-    cnt = (C.c_int64 * HOT_NUM_STAGES)()
-    _check(lib().hot_debug_profile_end(ms, cnt), "hot_debug_profile_end")
+    ms = (C.c_float * HOT_NUM_STAGES_ALL)()
+    cnt = (C.c_int64 * HOT_NUM_STAGES_ALL)()
+    _check(lib().hot_debug_profile_end_all(ms, cnt, HOT_NUM_STAGES_ALL), "hot_debug_profile_end_all")
     return {lib().hot_debug_stage_name(i).decode(): (float(ms[i]), int(cnt[i]))
-            for i in range(HOT_NUM_STAGES) if cnt[i]}
+            for i in range(HOT_NUM_STAGES_ALL) if cnt[i]}
 
 
 def hot_debug_profile_sequence():

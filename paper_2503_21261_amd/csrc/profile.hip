@@ -46,7 +46,7 @@ void stage_end(int stage, hipStream_t s) {
   (void)hipEventRecord(g_records.back().stop, s);
 }
 
-const char* const kStageNames[HOT_NUM_STAGES] = {
+const char* const kStageNames[HOT_NUM_STAGES_ALL] = {
     "gx_and_gw_igemm", "act_col_absmax", "act_col_quant", "w_col_absmax",  "w_col_quant",
     "gy_row_quant",  "gy_row_absmax",  "gy_row_quant2", "gx_igemm",      "gyT_col_absmax",
     "gyT_col_quant", "gw_igemm",       "w_and_gy_row_quant", "gy_fused_absmax", "gy_fused_quant",
@@ -69,10 +69,14 @@ hot_status hot_debug_profile_begin(void) {
 }
 
 hot_status hot_debug_profile_end(float* stage_ms, int64_t* stage_launches) {
+  return hot_debug_profile_end_all(stage_ms, stage_launches, HOT_NUM_STAGES);
+}
+
+hot_status hot_debug_profile_end_all(float* stage_ms, int64_t* stage_launches, int32_t count) {
   std::lock_guard<std::mutex> lock(hot::g_mu);
   hot::g_on = false;
-  if (!stage_ms || !stage_launches) return HOT_ERR_ARG;
-  for (int i = 0; i < HOT_NUM_STAGES; ++i) {
+  if (!stage_ms || !stage_launches || count < 0) return HOT_ERR_ARG;
+  for (int i = 0; i < count; ++i) {
     stage_ms[i] = 0.0f;
     stage_launches[i] = 0;
   }
@@ -84,7 +88,7 @@ hot_status hot_debug_profile_end(float* stage_ms, int64_t* stage_launches) {
     if (hipEventSynchronize(r.stop) != hipSuccess ||
         hipEventElapsedTime(&ms, r.start, r.stop) != hipSuccess) {
       st = HOT_ERR_DEVICE;
-    } else if (r.stage >= 0 && r.stage < HOT_NUM_STAGES) {
+    } else if (r.stage >= 0 && r.stage < count) {
       stage_ms[r.stage] += ms;
       stage_launches[r.stage] += 1;
     }
@@ -103,7 +107,7 @@ int64_t hot_debug_profile_sequence(int32_t* stages, int64_t capacity) {
 }
 
 const char* hot_debug_stage_name(int stage) {
-  return (stage >= 0 && stage < HOT_NUM_STAGES) ? hot::kStageNames[stage] : "";
+  return (stage >= 0 && stage < HOT_NUM_STAGES_ALL) ? hot::kStageNames[stage] : "";
 }
 
 }  // extern "C"

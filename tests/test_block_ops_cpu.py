@@ -1,6 +1,8 @@
 """Host-side checks of the operators around the linear backward: sizes, refusals before any launch, and the 64-bit forms the GPU
 tests hold the kernels to."""
 import ctypes as C
+import os
+import re
 
 import numpy as np
 import pytest
@@ -162,3 +164,31 @@ def test_norm_gradients_are_those_of_its_values():
     got = ref.norm_grad(w.detach(), h.detach(), gamma.detach(), mean.detach(), rstd.detach(), None, torch.float32)
     for (value, _), at64 in zip(got, want):
         assert float((value - at64).abs().max()) < 1e-12
+
+
+# ---- the timing of stages --------------------------------------------------------------------------------------------------------
+
+def test_stage_timing_fills_the_arrays_that_its_caller_has():
+    """hot_debug_profile_end writes the linear backward's fifteen stages, as many as it always did; the others have a call of their own."""
+    l = hot.lib()
+
+    def arrays():
+        return (C.c_float * 32)(*[-1.0] * 32), (C.c_int64 * 32)(*[-1] * 32)
+
+    for call, filled in ((lambda ms, n: l.hot_debug_profile_end(ms, n), 15), (lambda ms, n: l.hot_debug_profile_end_all(ms, n, 24), 24),
+                         (lambda ms, n: l.hot_debug_profile_end_all(ms, n, 3), 3), (lambda ms, n: l.hot_debug_profile_end_all(ms, n, 0), 0)):
+        ms, n = arrays()
+        l.hot_debug_profile_begin()
+        assert call(ms, n) == hot.HOT_OK
+        assert list(ms) == [0.0] * filled + [-1.0] * (32 - filled) and list(n) == [0] * filled + [-1] * (32 - filled)
+    ms, n = arrays()
+    assert l.hot_debug_profile_end_all(ms, n, -1) == hot.HOT_ERR_ARG and l.hot_debug_profile_end_all(None, n, 4) == hot.HOT_ERR_ARG
+    names = [l.hot_debug_stage_name(i).decode() for i in range(25)]
+    assert len(set(names[:24])) == 24 and all(names[:24]) and names[24] == ""
+    assert names[14] == "gy_fused_quant" and names[15] == "checkpoint_write"
+
+
+def test_stage_numbers_are_those_of_the_header():
+    text = open(os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "include", "hot.h")).read()
+    for name in ("HOT_NUM_STAGES", "HOT_NUM_STAGES_ALL"):
+        assert int(re.search(rf"#define {name} (\d+)", text).group(1)) == getattr(hot, name)
