@@ -252,9 +252,16 @@ __device__ __forceinline__ float act_slope(float x) {
 }
 
 // ---- sums -----------------------------------------------------------------------------------------
-// Sum over T consecutive lanes (T a power of two up to 64), in every one of them.
-template <int T>
-__device__ __forceinline__ float lanes_sum(float v) {
+template <int MASK>
+__device__ __forceinline__ double lane_xor(double v) {
+  const uint64_t b = __builtin_bit_cast(uint64_t, v);
+  const uint32_t lo = __float_as_uint(lane_xor<MASK>(__uint_as_float((uint32_t)b)));
+  const uint32_t hi = __float_as_uint(lane_xor<MASK>(__uint_as_float((uint32_t)(b >> 32))));
+  return __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
+}
+// Sum over T consecutive lanes (T a power of two up to 64), in every one of them; float or double.
+template <int T, class V>
+__device__ __forceinline__ V lanes_sum(V v) {
   if constexpr (T >= 2) v += lane_xor<1>(v);
   if constexpr (T >= 4) v += lane_xor<2>(v);
   if constexpr (T >= 8) v += lane_xor<4>(v);

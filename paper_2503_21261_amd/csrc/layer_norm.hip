@@ -5,7 +5,8 @@
 //
 // Both are bound by HBM.  A row stays in the registers of the T lanes that work on it (eight columns a
 // lane, NV times), so it is read once: the mean first, then the squares of what is left, which keeps the
-// variance of rows whose mean is large.  The backward pass keeps a lane on its columns, so that the
+// variance of rows whose mean is large.  The mean is summed in 64 bits, so that it is the exact one rounded
+// once, and y takes off what that rounding left.  The backward pass keeps a lane on its columns, so that the
 // parameter gradients are sums in registers; a workgroup leaves one row of them, and column_sums adds those in order.
 // 201728 x 1024 fp32 with residual and checkpoint: 660 us forward, 500 back, 5.3 TB/s.
 #include <type_traits>
@@ -49,10 +50,25 @@ __device__ __forceinline__ void row_sums(float& a, float& b, float (*s_red)[16][
   }
 }
 
+// Sum of one value over the T lanes of a row, in every lane; s_red: the caller's own for each call.
+template <int T, class V>
+__device__ __forceinline__ V row_sum(V a, V* s_red) {
+  a = lanes_sum<(T < 64 ? T : 64)>(a);
+  if constexpr (T > 64) {
+    if (((int)threadIdx.x & 63) == 0) s_red[(int)threadIdx.x >> 6] = a;
+    __syncthreads();
+    a = V(0);
+#pragma unroll
+    for (int i = 0; i < T / 64; ++i) a += s_red[i];
+  }
+  return a;
+}
+
 // EVEN: cols is a multiple of eight, so that a lane's chunk is whole or absent.
 template <int T, int NV, class TX, class TY, bool KEEP, bool EVEN>
 __global__ __launch_bounds__(kThreads<T>) void layer_norm_kernel(const NormForward a, const CkptView k, int64_t first) {
-  __shared__ float s_red[2][16][2];
+  __shared__ double s_sum[16];
+  __shared__ float s_sq[16];
   const int lane = (int)threadIdx.x % T, slot = (int)threadIdx.x / T;
   const int64_t row = first + (int64_t)blockIdx.x * kSlots<T> + slot;
   if (row >= a.rows) return;   // T > 64: one row a workgroup, all of it or none
@@ -68,7 +84,8 @@ __global__ __launch_bounds__(kThreads<T>) void layer_norm_kernel(const NormForwa
       if (a.residual) rr[j] = load8((const TX*)a.residual + at + c, have(c));
     }
   }
-  float v[NV][8], sum = 0.0f, none = 0.0f;
+  float v[NV][8];
+  double sum = 0.0;
 #pragma unroll
   for (int j = 0; j < NV; ++j) {
     const int c = (lane + j * T) * 8;
@@ -88,13 +105,14 @@ __global__ __launch_bounds__(kThreads<T>) void layer_norm_kernel(const NormForwa
       if (c < (int)k.pitch) ckpt_store8(k, row * k.pitch + c, v[j]);
     }
 #pragma unroll
-    for (int i = 0; i < 8; ++i) sum += v[j][i];
+    for (int i = 0; i < 8; ++i) sum += (double)v[j][i];
   }
-  row_sums<T>(sum, none, s_red, 0);
-  // Twice: what the first mean is off by (its rounding, large beside the variance where |mean| is) is the
-  // mean of what is left.
-  const float mean0 = sum / (float)cols;
-  float sq = 0.0f, left = 0.0f;
+  // What the mean loses by its rounding (large beside the variance where |mean| is) is taken off the squares and off y.  Sums in
+  // 32 bits lose more, and the mean of the deviations does not bring it back: they are rounded too (rows of 768 about zero: 1.0e-7 of
+  // the mean in 32 bits, 2.4e-7 with that, 2.6e-8 in 64; 201728 x 1024 takes as long either way).
+  const double exact = row_sum<T>(sum, s_sum) / (double)cols;
+  const float mean0 = (float)exact, off = (float)(exact - (double)mean0);
+  float sq = 0.0f;
 #pragma unroll
   for (int j = 0; j < NV; ++j) {
     const int n = cols - (lane + j * T) * 8;
@@ -106,18 +124,14 @@ __global__ __launch_bounds__(kThreads<T>) void layer_norm_kernel(const NormForwa
       for (int i = 0; i < 8; ++i) v[j][i] = i < n ? v[j][i] - mean0 : 0.0f;
     }
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      sq = fmaf(v[j][i], v[j][i], sq);
-      left += v[j][i];
-    }
+    for (int i = 0; i < 8; ++i) sq = fmaf(v[j][i], v[j][i], sq);
   }
-  row_sums<T>(sq, left, s_red, 1);
-  const float off = left / (float)cols;
+  sq = row_sum<T>(sq, s_sq);
   float var = fmaf(-off, off, sq / (float)cols);
   var = var < 0.0f ? 0.0f : var;   // a constant row, by rounding
   const float rstd = 1.0f / sqrtf(var + a.eps);
   if (lane == 0) {
-    a.mean[row] = mean0 + off;
+    a.mean[row] = mean0;
     a.rstd[row] = rstd;
   }
 #pragma unroll

@@ -39,3 +39,19 @@ def test_relu_gradient_of_infinities_and_nan(dtype):
     gx = hot.hot_activation_backward(hot.HOT_ACT_RELU, g, torch.empty_like(g), x=x.cuda())
     want = torch.tensor([[3.0, 3.0, 0.0, 0.0, NAN, 0.0, 0.0, 3.0]], dtype=torch.float64)
     close(gx, want, torch.zeros_like(want), "g_x")
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("cols", [1, 100, 200, 500, 771, 1500, 4096, 5000, 11008, 16384])
+def test_layer_norm_mean_is_the_exact_one_rounded_once(cols, dtype):
+    """Rows about zero, with columns that stand out, far from zero, and of the largest numbers.  In 64 bits a lane adds 16 columns and at
+    most 25 more additions join the lanes and waves (2^-53 of mean |h| each, and the division), then the mean is rounded: half a step."""
+    x = rand((24, cols), cols, dtype)
+    x[6:12, ::100] *= 20
+    x[12:18] += 300
+    x[18:21] *= 1e-30
+    x[21:] = x[21:].abs() * 1e37
+    y, mean, rstd = torch.empty((24, cols), dtype=dtype, device="cuda"), torch.empty(24, device="cuda"), torch.empty(24, device="cuda")
+    hot.hot_layer_norm_forward(x.cuda(), None, None, 1e-6, y, mean, rstd)
+    want = ref.f64(x).mean(1)
+    close(mean, want, want.abs() * (1 + 2.0 ** -20) * ref.U + 2.0 ** -47 * ref.f64(x).abs().mean(1), "mean")
