@@ -438,6 +438,24 @@ typedef struct hot_gemm_plan {
 } hot_gemm_plan;
 hot_status hot_debug_gemm_plan(const hot_config* cfg, int64_t L, int64_t O, int64_t I, hot_gemm_plan* plan);
 
+/* How hot_linear_forward works on a product (host only, nothing is launched; of the first 2^23 rows of a longer x):
+ * rows and outputs a workgroup, how many such tiles there are, how many have a workgroup each (the others are summed in
+ * `slices` slices of the columns), whether rows end inside a 128-byte piece of the tiles that take operands as they are, and
+ * whether y is stored with the streaming hint. */
+typedef enum {
+  HOT_LINEAR_ROWS = 0,     /* few rows: operands from memory to the matrix instructions */
+  HOT_LINEAR_DIRECT = 1,   /* small tiles of the operands as they are                   */
+  HOT_LINEAR_TILES = 2,    /* large tiles of bfloat16 operands as they are              */
+  HOT_LINEAR_PACKED = 3    /* large tiles of operands that a first launch packs         */
+} hot_linear_way;
+typedef struct hot_linear_plan {
+  int32_t way, tile_rows, tile_cols;
+  int32_t tiles, whole, slices;
+  int32_t masked, streams;
+} hot_linear_plan;
+hot_status hot_debug_linear_plan(hot_type type, hot_type y_type, int64_t L, int64_t O, int64_t I, int32_t with_ckpt,
+                                 hot_linear_plan* plan);
+
 /* Machine-peak probes (context for the roofline figures, not the method): one launch of
  * kind 0 = read `bytes` of buf, 1 = write them (4 = with the streaming, non-temporal, hint the
  * GEMM epilogue uses), 2 / 3 = `iters` x 16 int8 32x32x32 matrix

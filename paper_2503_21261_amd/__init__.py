@@ -32,7 +32,7 @@ EXPORTS = (
     "hot_linear_backward", "hot_linear_backward_gx_noalloc", "hot_lowpass_l1_rows", "hot_select_quantizer", "hot_debug_unpack_activation",
     "hot_debug_gx_operands", "hot_debug_gw_operands", "hot_debug_fused_operands", "hot_debug_set_exchange_wait_us",
     "hot_debug_set_backward_strategy", "hot_debug_set_gemm_mode", "hot_debug_profile_begin", "hot_debug_profile_end", "hot_debug_profile_end_all", "hot_debug_profile_sequence",
-    "hot_debug_stage_name", "hot_debug_probe", "hot_debug_gemm_plan",
+    "hot_debug_stage_name", "hot_debug_probe", "hot_debug_gemm_plan", "hot_debug_linear_plan",
     "hot_checkpoint_bytes", "hot_checkpoint_write", "hot_checkpoint_read", "hot_activation_forward",
     "hot_activation_backward_workspace_bytes", "hot_activation_backward", "hot_layer_norm_forward",
     "hot_layer_norm_backward_workspace_bytes", "hot_layer_norm_backward", "hot_linear_forward_workspace_bytes",
@@ -54,6 +54,10 @@ class hot_config(C.Structure):
 
 class hot_gemm_plan(C.Structure):
     _fields_ = [("one_launch", C.c_int32)] + [(f, C.c_int32 * 5) for f in ("gx", "gw", "gx_alone", "gw_alone")]
+
+
+class hot_linear_plan(C.Structure):
+    _fields_ = [(f, C.c_int32) for f in ("way", "tile_rows", "tile_cols", "tiles", "whole", "slices", "masked", "streams")]
 
 
 class HotError(RuntimeError):
@@ -102,6 +106,7 @@ def lib() -> C.CDLL:
         l.hot_debug_profile_begin.argtypes = []
         l.hot_debug_profile_end.argtypes = [C.POINTER(C.c_float), C.POINTER(C.c_int64)]
         l.hot_debug_profile_end_all.argtypes = [C.POINTER(C.c_float), C.POINTER(C.c_int64), C.c_int32]
+        l.hot_debug_linear_plan.argtypes = [C.c_int, C.c_int, i64, i64, i64, C.c_int32, C.POINTER(hot_linear_plan)]
         l.hot_debug_gemm_plan.argtypes = [cfgp, i64, i64, i64, C.POINTER(hot_gemm_plan)]
         l.hot_debug_probe.argtypes = [C.c_int, vp, sz, C.c_int, vp]
         l.hot_debug_profile_sequence.argtypes = [C.POINTER(C.c_int32), C.c_int64]
@@ -657,6 +662,15 @@ def hot_debug_gemm_plan(cfg: Config, L: int, O: int, I: int) -> dict:
     names = ("gx", "gw", "gx_alone", "gw_alone")
     return dict(one_launch=bool(p.one_launch), streams={f for f in names if getattr(p, f)[4]},
                 **{f: (*list(getattr(p, f))[:3], bool(getattr(p, f)[3])) for f in names})
+
+
+def hot_debug_linear_plan(dtype: torch.dtype, L: int, O: int, I: int, y_dtype: Optional[torch.dtype] = None, ckpt: bool = False) -> dict:
+    """How hot_linear_forward works on a product: its way ("rows", "direct", "tiles", "packed"), rows and outputs a workgroup, tiles, tiles
+    with a workgroup each, slices of the others, whether row ends are masked, whether y is streamed."""
+    p = hot_linear_plan()
+    _check(lib().hot_debug_linear_plan(_TYPES[dtype], _TYPES[y_dtype or dtype], L, O, I, int(ckpt), C.byref(p)), "hot_debug_linear_plan")
+    return dict(way=("rows", "direct", "tiles", "packed")[p.way], tile=(p.tile_rows, p.tile_cols), tiles=p.tiles, whole=p.whole,
+                slices=p.slices, masked=bool(p.masked), streams=bool(p.streams))
 
 
 def hot_debug_probe(kind: int, buf: torch.Tensor, iters: int = 1, stream=None) -> None:

@@ -229,4 +229,12 @@ hot_status hot_linear_forward(const void* x, const void* w, hot_type type, const
   return HOT_OK;
 }
 
+hot_status hot_debug_linear_plan(hot_type type, hot_type y_type, int64_t L, int64_t O, int64_t I, int32_t with_ckpt,
+                                 hot_linear_plan* plan) {
+  if (!plan || !type_ok(type) || !type_ok(y_type) || (type == HOT_F32 && y_type != HOT_F32)) return HOT_ERR_ARG;
+  if (!size_ok(L, I) || !size_ok(L, O)) return HOT_ERR_SHAPE;
+  describe_linear(type, y_type, L, O, I, with_ckpt != 0, plan);
+  return HOT_OK;
+}
+
 }  // extern "C"

@@ -76,5 +76,6 @@ struct LinearForward {
 };
 size_t linear_scratch_bytes(hot_type type, int64_t L, int64_t O, int64_t I);
 hipError_t launch_linear(const LinearForward& a, hipStream_t s);
+void describe_linear(hot_type type, hot_type y_type, int64_t L, int64_t O, int64_t I, bool kept, hot_linear_plan* out);
 
 }  // namespace hot

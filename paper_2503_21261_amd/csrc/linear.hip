@@ -937,14 +937,19 @@ hipError_t rows_typed(const LinearForward& a, const Plan& p, const LinearOut& o,
   return with_nt(integral_constant<int, 4>{});
 }
 
+Plan run_plan(hot_type type, int64_t L, int64_t O, int64_t I, bool kept) {
+  Plan p = make_plan(type, L, O, I);
+  if (kept && !p.tiles && p.slices == 1 && p.nt == 1) {   // a group is finished by one workgroup
+    p.nt = 2;
+    p.tiles_n = ceil_div(O, 32);
+  }
+  return p;
+}
+
 template <class T, class TY>
 hipError_t linear_run(const LinearForward& a, const CkptView& k, hipStream_t s) {
   LinearOut o{a.bias, a.residual, a.y, k, a.L, (int)a.O, a.fn, stream_output(a.L, a.O * (int64_t)sizeof(TY))};
-  Plan p = make_plan(a.type, a.L, a.O, a.I);
-  if (k.codes && !p.tiles && p.slices == 1 && p.nt == 1) {   // a group is finished by one workgroup
-    p.nt = 2;
-    p.tiles_n = ceil_div(a.O, 32);
-  }
+  const Plan p = run_plan(a.type, a.L, a.O, a.I, k.codes != nullptr);
   if (p.tiles) return tiles_typed<T, TY>(a, p, o, s);
   stage_begin(kStLinear, s);
   const hipError_t e = rows_typed<T, TY>(a, p, o, s);
@@ -981,6 +986,21 @@ size_t linear_scratch_bytes(hot_type type, int64_t L, int64_t O, int64_t I) {
   if (L <= kRunRows) return run_scratch_bytes(type, L, O, I);
   const size_t run = run_scratch_bytes(type, kRunRows, O, I), last = run_scratch_bytes(type, L % kRunRows, O, I);
   return run > last ? run : last;
+}
+
+void describe_linear(hot_type type, hot_type y_type, int64_t L, int64_t O, int64_t I, bool kept, hot_linear_plan* out) {
+  if (L > kRunRows) L = kRunRows;
+  const Plan p = run_plan(type, L, O, I, kept);
+  const TileLayout t = tile_layout(type, L, O, I);
+  const int64_t bytes = I * (type == HOT_F32 ? 4 : 2), count = p.tiles_m * p.tiles_n;
+  out->way = !p.tiles ? HOT_LINEAR_ROWS : p.direct ? HOT_LINEAR_DIRECT : t.packed ? HOT_LINEAR_PACKED : HOT_LINEAR_TILES;
+  out->tile_rows = p.tiles ? p.bm : 16 * p.mt;
+  out->tile_cols = p.tiles ? p.bn : 16 * p.nt;
+  out->tiles = (int32_t)count;
+  out->whole = (int32_t)(p.tiles ? p.whole : p.slices > 1 ? 0 : count);
+  out->slices = p.slices;
+  out->masked = (out->way == HOT_LINEAR_DIRECT || out->way == HOT_LINEAR_TILES) && bytes % kPiece != 0;
+  out->streams = stream_output(L, O * (y_type == HOT_F32 ? 4 : 2));
 }
 
 hipError_t launch_linear(const LinearForward& a, hipStream_t s) {

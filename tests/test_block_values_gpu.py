@@ -5,7 +5,7 @@ import torch
 
 import block_oracle as ref
 import paper_2503_21261_amd as hot
-from test_block_ops_gpu import BF16, F32, FNS, close, rand
+from test_block_ops_gpu import BF16, F32, FNS, LINEAR_WAYS, close, rand
 
 pytestmark = pytest.mark.gpu
 
@@ -55,3 +55,127 @@ def test_layer_norm_mean_is_the_exact_one_rounded_once(cols, dtype):
     hot.hot_layer_norm_forward(x.cuda(), None, None, 1e-6, y, mean, rstd)
     want = ref.f64(x).mean(1)
     close(mean, want, want.abs() * (1 + 2.0 ** -20) * ref.U + 2.0 ** -47 * ref.f64(x).abs().mean(1), "mean")
+
+
+# ---- forward product ------------------------------------------------------------------------------------------------------------
+
+def product64(x, w):
+    """x.w^T and |x|.|w|^T of device tensors in 64 bits."""
+    x, w = x.double(), w.double()
+    return (x @ w.t().contiguous()).cpu(), (x.abs() @ w.abs().t().contiguous()).cpu()
+
+
+def held_to(y, z, size, I, what):
+    """The product's error for terms of random signs, in units of 2^-24 |x|.|w|: operands to 22 bits and a product left out, each 2^-22
+    at most (12), what the checks of a row's range let through (4), and the additions: partial sums of k terms are about sqrt(k) of
+    them, so that I roundings of them add up to 1.2 standard deviations (10 for eight).  No result is nearer than half the smallest
+    number in each of its terms."""
+    close(y, z, 26 * ref.U * size + (2 * I + 1) * 2.0 ** -150, what)
+
+
+def call_linear(x, w, **kw):
+    L, O, I, t = x.shape[0], w.shape[0], x.shape[1], x.dtype
+    y = torch.full((L, O), NAN, dtype=kw.pop("y_type", F32), device="cuda")
+    return hot.hot_linear_forward(x, w, y, hot.alloc_linear_workspace(t, L, O, I), **kw)
+
+
+# The large tiles of packed fp32 operands: 128 x 128 and 256 x 256, whole, in slices, and with the last ones in slices
+PACKED = [(3590, 3585, 33, (128, 128), "whole"), (2600, 1500, 1030, (128, 128), "whole"), (3500, 3600, 100, (256, 256), "whole"),
+          (1200, 260, 9001, (128, 128), "sliced"), (7329, 162, 5528, (256, 256), "sliced"), (6742, 1245, 2568, (128, 128), "last sliced"),
+          (5054, 3202, 528, (256, 256), "last sliced")]
+
+
+def packed(L, O, I, tile, cut):
+    p = hot.hot_debug_linear_plan(F32, L, O, I)
+    assert p["way"] == "packed" and p["tile"] == tile
+    assert cut == ("whole" if p["whole"] == p["tiles"] else "sliced" if p["whole"] == 0 else "last sliced")
+    print(f"[packed] {L}x{O}x{I} {p}", flush=True)
+
+
+@pytest.mark.parametrize("t,L,O,I", LINEAR_WAYS + [(F32, 500, 100, 64), (F32, 100, 500, 96), (BF16, 500, 100, 128), (BF16, 100, 500, 64)])
+def test_linear_of_whole_numbers_is_exact(t, L, O, I):
+    """Every product and sum is a whole number that fp32 holds (sums of I <= 40003 terms of +-4095 are within 4096 x 4095 by twenty
+    standard deviations), so the result has one value: a part of an operand or a piece of K that is left out shows.  fp32: twelve
+    bits, one more than an fp16 part has, against +-1, either way round."""
+    print(f"[whole numbers] {L}x{O}x{I} {t} {hot.hot_debug_linear_plan(t, L, O, I)['way']}", flush=True)
+    g = torch.Generator("cuda").manual_seed(L + O + I)
+
+    def numbers(shape, wide):
+        sign = torch.randint(0, 2, shape, generator=g, device="cuda", dtype=F32) * 2 - 1
+        if not wide:
+            return sign.to(t)
+        n = 2049 + 2 * torch.randint(0, 1024, shape, generator=g, device="cuda", dtype=F32) if t == F32 else \
+            torch.randint(1, 256, shape, generator=g, device="cuda", dtype=F32)
+        return (sign * n).to(t)
+
+    for wide_x in (True, False):
+        x, w = numbers((L, I), wide_x), numbers((O, I), not wide_x)
+        want = x.double() @ w.double().t().contiguous()
+        assert float(want.abs().max()) < 2 ** 24
+        assert torch.equal(call_linear(x, w, y_type=F32).double(), want)
+
+
+@pytest.mark.parametrize("L,O,I,tile,cut", PACKED)
+def test_packed_product_near_the_exact_one(L, O, I, tile, cut):
+    packed(L, O, I, tile, cut)
+    x, w = rand((L, I), 1).cuda(), rand((O, I), 2, std=I ** -0.5).cuda()
+    held_to(call_linear(x, w), *product64(x, w), I, "y")
+
+
+@pytest.mark.parametrize("L,O,I,tile,cut", PACKED)
+def test_packed_rows_of_any_magnitude(L, O, I, tile, cut):
+    """Each row of either operand has a scale of its own; rows of zeros, a row with one subnormal element, and within every row
+    values far below its largest."""
+    packed(L, O, I, tile, cut)
+    x, w = rand((L, I), 1), rand((O, I), 2, std=I ** -0.5)
+    x *= (2.0 ** torch.linspace(-62, 60, L).round())[torch.randperm(L, generator=torch.Generator().manual_seed(3))][:, None]
+    w *= (2.0 ** torch.linspace(-62, 60, O).round())[torch.randperm(O, generator=torch.Generator().manual_seed(4))][:, None]
+    x[:, ::3] *= 2.0 ** -20
+    x[3], w[5], x[4] = 0.0, 0.0, 0.0
+    x[4, 7] = 1e-40
+    x, w = x.cuda(), w.cuda()
+    held_to(call_linear(x, w), *product64(x, w), I, "y")
+
+
+@pytest.mark.parametrize("L,O,I,tile,cut", PACKED)
+def test_packed_rows_with_an_infinity_or_nan_stay_alone(L, O, I, tile, cut):
+    packed(L, O, I, tile, cut)
+    x, w = rand((L, I), 1), rand((O, I), 2, std=I ** -0.5)
+    x[2, 5], x[L - 2, I - 1], x[L - 1, 0], w[7, 1], w[O - 1, I - 2] = NAN, INF, -INF, NAN, INF
+    y = call_linear(x.cuda(), w.cuda())
+    bad = torch.zeros((L, O), dtype=torch.bool)
+    bad[2], bad[L - 2], bad[L - 1], bad[:, 7], bad[:, O - 1] = (True,) * 5
+    assert torch.equal(~torch.isfinite(y.cpu()), bad)
+    x[~torch.isfinite(x)], w[~torch.isfinite(w)] = 0.0, 0.0       # the rows beside them are right
+    x, w = x.cuda(), w.cuda()
+    z, size = product64(x, w)
+    held_to(y.masked_fill(bad.cuda(), 0.0), z.masked_fill(bad, 0.0), size, I, "y")
+
+
+def test_packed_products_on_two_streams_at_once():
+    """Operands packed, K in slices, epilogue and checkpoint, on two streams with workspaces of their own: as one after another."""
+    L, O, I = 7329, 162, 5528
+    packed(L, O, I, (256, 256), "sliced")
+    w, b = rand((O, I), 1, std=I ** -0.5).cuda(), rand((O,), 2).cuda()
+    x = [rand((L, I), 3 + k).cuda() for k in range(2)]
+    ws = [hot.alloc_linear_workspace(F32, L, O, I) for _ in range(2)]
+    kept = [torch.zeros_like(hot.alloc_checkpoint(L, O)) for _ in range(2)]
+    y = [torch.zeros((L, O), device="cuda") for _ in range(2)]
+    streams = [torch.cuda.Stream() for _ in range(2)]
+
+    def step(k, s):
+        hot.hot_linear_forward(x[k], w, y[k], ws[k], bias=b, fn=hot.HOT_ACT_GELU, ckpt=kept[k], stream=s)
+
+    torch.cuda.synchronize()
+    for k in range(2):
+        step(k, streams[0])
+        torch.cuda.synchronize()
+    alone = [t.clone() for t in y + kept]
+    for t in y + kept:
+        t.zero_()
+    torch.cuda.synchronize()
+    for _ in range(4):
+        for k in range(2):
+            step(k, streams[k])
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, c) for a, c in zip(alone, y + kept))
