@@ -320,10 +320,12 @@ hot_status hot_layer_norm_backward(const void* g_y, hot_type y_type, const void*
  * x: [L x I], w: [O x I] of `type`; bias: fp32 [O] or NULL; residual: [L x O] of y_type or NULL;
  * y: [L x O] of y_type (HOT_F32 operands take y_type HOT_F32 only).  fn may be HOT_ACT_NONE.
  * ckpt: the checkpoint of z as [L x O], for hot_activation_backward (NULL: none is made).
- * fp32 operands: every product keeps 22 bits of each factor relative to the largest of its row, and is
- * summed in fp32, so that the result is as near the exact one as an fp32 product's; bfloat16 operands
- * are multiplied exactly and summed in fp32.  I < 2^24, O < 2^24.  Where a row of fp32 x or w holds an
- * infinity, its results may be NaN instead of infinite.
+ * bfloat16 operands are multiplied exactly and summed in fp32.  fp32 operands: x.w^T is within 2^-20 of the sum of
+ * |x| |w| of the exact one, beside the roundings of its fp32 additions, whatever the operands and the sizes.  Small
+ * products run on the fp32 instructions; large ones on two 16-bit parts of each factor, but for the tiles whose rows
+ * hold numbers of so wide a range, or so few that are not small, that the parts could not give that (infinities
+ * and NaN too): those run on the fp32 instructions, in about three times the time.  So the last bits of a row may depend
+ * on the other rows, within that bound.  I < 2^24, O < 2^24.
  * ws: at least hot_linear_forward_workspace_bytes() bytes of scratch, 256-byte aligned (where that is
  * 0, ws may be NULL).
  */

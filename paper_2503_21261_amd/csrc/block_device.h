@@ -259,6 +259,8 @@ __device__ __forceinline__ double lane_xor(double v) {
   const uint32_t hi = __float_as_uint(lane_xor<MASK>(__uint_as_float((uint32_t)(b >> 32))));
   return __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
 }
+template <int MASK>
+__device__ __forceinline__ uint32_t lane_xor(uint32_t v) { return __float_as_uint(lane_xor<MASK>(__uint_as_float(v))); }
 // Sum over T consecutive lanes (T a power of two up to 64), in every one of them; float or double.
 template <int T, class V>
 __device__ __forceinline__ V lanes_sum(V v) {

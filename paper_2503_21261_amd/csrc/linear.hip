@@ -199,7 +199,8 @@ __global__ __launch_bounds__(256) void linear_rows_combine_kernel(const float* s
 //   fp32: 32 elements as two fp16 parts, twice [16 high | 16 low], of the row scaled by a power of two so that its largest
 //   value lies in [2^14, 2^15): x = high + low to 22 bits (values down to 2^-17 of the row's largest keep them, smaller
 //   ones keep 2^-39 of it), and x.w = high.high + high.low + low.high with 2^-22 left out: a
-//   third of the fp16 rate, five times that of the fp32 instructions.
+//   third of the fp16 rate, five times that of the fp32 instructions.  Tiles with rows of so wide a range that this is worse than
+//   an fp32 product take those instructions (wide_tile).
 // Pieces go from memory to LDS without registers (buffer_load ... lds), two stages deep: one arrives while one is worked on.  LDS
 // holds a row's eight 16-byte chunks at chunk ^ (row % 8): eight rows that read the same chunk hit different banks.  As a load
 // writes 64 consecutive chunks, it is the lanes' sources that are permuted.
@@ -238,7 +239,9 @@ __device__ __forceinline__ void load_to_lds(rsrc_t from, uint8_t* to, int lane_o
 struct TileArgs {
   const uint8_t *x, *w;       // operand rows
   int64_t pitch;              // bytes of one, a multiple of 128 in the first two modes
-  const int *ex, *ew;         // fp32: exponents of the rows' scales
+  const uint8_t *x_plain, *w_plain;   // fp32 in two parts: the rows as they are, for tiles whose rows the parts do not hold (wide_tile)
+  int64_t plain_pitch;
+  const uint32_t *ex, *ew;    // and a word for each row: its scale and range
   int tiles_m, tiles_n;
   int whole;                  // tiles with a workgroup each; every other one has `slices`, which leave their sums in
   int slices;                 // images[tile - whole][slice], added by linear_combine_kernel
@@ -264,39 +267,88 @@ enum TileMode {
   // instructions count.  1872 x 624 x 640 bfloat16 9.7 us, 128 x 128 12.6; 3308 x 2079 x 2808 95 against 61.
   kBf16Direct = 3,
   kF32Direct = 4,
+  // Large tiles of fp32 rows that two parts do not hold (wide_tile): the plain fp32 instructions, 12608 x 2304 x 768 429 us if all
+  // tiles are such, 146 in parts.
+  kF32Wide = 5,
 };
 
-template <int BM, int BN, int WM, int WN, int MODE, class TY>
-__global__ __launch_bounds__(64 * (BM / WM) * (BN / WN), 2) void linear_tile_kernel(const TileArgs g) {
-  constexpr bool SPLIT = MODE == kSplitRows, DIRECT = MODE >= kBf16Direct, AS_IS = MODE >= kBf16Ragged;
+// A row's word: the exponent of what its parts are multiplied by, and its range (linear_split_kernel) in units of 1 / 1024.
+__device__ __forceinline__ int word_exponent(uint32_t word) { return (int)(word << 22) >> 22; }
+__device__ __forceinline__ uint32_t row_word(int exponent, uint32_t large, uint32_t lossy) {
+  return ((uint32_t)exponent & 1023u) | large << 10 | lossy << 21;
+}
+
+__device__ __forceinline__ uint32_t widest_of(uint32_t a, uint32_t b) {    // of both halves
+  typedef uint16_t u2 __attribute__((ext_vector_type(2)));
+  return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(u2, a), __builtin_bit_cast(u2, b)));
+}
+// Words of ROWS rows, each lane's, of which `rows` exist (the last one repeats).
+template <int ROWS>
+struct RowRanges {
+  uint32_t words[ROWS / 64];
+  __device__ __forceinline__ RowRanges(const uint32_t* from, int rows) {
+    static_assert(ROWS % 64 == 0, "rows");
+#pragma unroll
+    for (int i = 0; i < ROWS / 64; ++i) {
+      const int r = (int)(threadIdx.x & 63) + 64 * i;
+      words[i] = from[r < rows ? r : rows - 1];
+    }
+  }
+  // The lane's widest: the largest 1024 - large above the largest lossy.
+  __device__ __forceinline__ uint32_t widest() const {
+    uint32_t m = 0;
+#pragma unroll
+    for (int i = 0; i < ROWS / 64; ++i) m = widest_of(m, (1024u - (words[i] >> 10 & 2047u)) << 16 | words[i] >> 21);
+    return m;
+  }
+};
+// Whether the two fp16 parts of a tile's rows do not give its products as near the exact ones as fp32 does.  In scaled values: a lossy
+// element is off by 2^-25 at most and meets less than 2^15, so that of the I columns those of x and w that are lossy (shares n) put
+// 2^-10 n I into a sum.  Columns that are large in both rows, a share of large_x + large_w - 1 at least, make |x|.|w| at
+// least 2^(5 + 7) I times that share: while n is no more than it, the sum is off by 2^-22 |x|.|w| at most.  All other elements are held
+// to 2^-22 each.  Every wave looks at all rows, so that none waits for another.
+// The words are asked for in front of the first stages and used behind them (12608 x 2304 x 768 143.6 -> 144.6 us with this; words
+// waited for first, their rows one after another, 146).
+template <int BM, int BN>
+__device__ __forceinline__ bool wide_tile(const RowRanges<BM>& of_x, const RowRanges<BN>& of_w) {
+  __builtin_amdgcn_sched_barrier(0);     // the words are waited for here, behind the first stages' loads
+  // x's in the lower half of the wave, w's in the upper one
+  const bool upper = (threadIdx.x & 32) != 0;
+  const uint32_t x = of_x.widest(), w = of_w.widest();
+  uint32_t m = widest_of(upper ? w : x, lane_xor<32>(upper ? x : w));
+  m = widest_of(m, lane_xor<1>(m));
+  m = widest_of(m, lane_xor<2>(m));
+  m = widest_of(m, lane_xor<4>(m));
+  m = widest_of(m, lane_xor<8>(m));
+  m = widest_of(m, lane_xor<16>(m));
+  const uint32_t mx = (uint32_t)__builtin_amdgcn_readlane((int)m, 0), mw = (uint32_t)__builtin_amdgcn_readlane((int)m, 32);
+  const int shared = 1024 - (int)(mx >> 16) - (int)(mw >> 16), lossy = (int)(mx & 0xFFFFu) + (int)(mw & 0xFFFFu);
+  return lossy > (shared > 0 ? shared : 0);
+}
+
+// acc = the products of nk stages from k_first on, of the tile at row m0 of x and n0 of w; all LDS reads and loads are over when it
+// returns.  pitch: of x and w, `rows_x` and `rows_w` of whose rows the tile has.  go(): asked while the first loads are on their way, the
+// same in all lanes; where it says no there are no products, and false is returned.
+template <int BM, int BN, int WM, int WN, int MODE, class Go>
+__device__ __forceinline__ bool tile_products(const uint8_t* x, const uint8_t* w, const int64_t pitch, const int64_t m0, const int n0,
+                                              const int64_t rows_x, const int64_t rows_w, const int k_first, const int nk,
+                                              uint8_t* const smem, v4f (&acc)[WM / 16][WN / 16], Go&& go) {
+  constexpr bool SPLIT = MODE == kSplitRows, DIRECT = MODE == kBf16Direct || MODE == kF32Direct, AS_IS = MODE >= kBf16Ragged;
   constexpr int WAVES_M = BM / WM, WAVES = WAVES_M * (BN / WN);
   constexpr int TM = WM / 16, TN = WN / 16;
   constexpr int XL = BM / 8 / WAVES, WL = BN / 8 / WAVES;   // loads of a wave and stage: 8 rows each
   static_assert(BM % (8 * WAVES) == 0 && BN % (8 * WAVES) == 0, "loads");
   constexpr int STAGE = (BM + BN) * kPiece;
-  extern __shared__ __align__(16) uint8_t smem[];
   const int tid = (int)threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  // A workgroup of a whole tile, or of a slice of one: slices of a tile are neighbours in dispatch order but for their XCD.
-  const int rest = g.tiles_m * g.tiles_n - g.whole, part = (int)blockIdx.x - g.whole;
-  const bool sliced = part >= 0;
-  const int z = sliced ? part / rest : 0, tail = sliced ? part % rest : 0;
-  int tm, tn;
-  tile_at(sliced ? g.whole + tail : xcd_contiguous((int)blockIdx.x, g.whole), g.tiles_m, g.tiles_n, tm, tn);
-  const int64_t m0 = (int64_t)tm * BM;
-  const int n0 = tn * BN;
-  const int stages = (int)((g.pitch + kPiece - 1) / kPiece);
-  const int k_first = sliced ? (int)((int64_t)stages * z / g.slices) : 0;
-  const int nk = sliced ? (int)((int64_t)stages * (z + 1) / g.slices) - k_first : stages;
 
   // Sources of the wave's loads: row lane / 8 of 8, the chunk that belongs where the lane writes.
-  const int64_t rows_x = g.out.L - m0 < BM ? g.out.L - m0 : BM, rows_w = g.out.O - n0 < BN ? g.out.O - n0 : BN;
-  const auto rx = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(g.x) + m0 * g.pitch, 0, (int)(rows_x * g.pitch), 0x00027000);
-  const auto rw = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(g.w) + (int64_t)n0 * g.pitch, 0, (int)(rows_w * g.pitch), 0x00027000);
+  const auto rx = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(x) + m0 * pitch, 0, (int)(rows_x * pitch), 0x00027000);
+  const auto rw = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(w) + (int64_t)n0 * pitch, 0, (int)(rows_w * pitch), 0x00027000);
   int off_x[XL], off_w[WL];
   auto source = [&](int row, int64_t rows) {
     const int chunk = (lane & 7) ^ (row & 7);           // row & 7 is lane / 8
     const int r = row < rows ? row : (int)rows - 1;     // rows past the last repeat it and are not stored
-    return r * (int)g.pitch + (AS_IS ? 0 : chunk * 16);
+    return r * (int)pitch + (AS_IS ? 0 : chunk * 16);
   };
 #pragma unroll
   for (int i = 0; i < XL; ++i) off_x[i] = source((wave * XL + i) * 8 + (lane >> 3), rows_x);
@@ -308,7 +360,7 @@ __global__ __launch_bounds__(64 * (BM / WM) * (BN / WN), 2) void linear_tile_ker
     uint8_t* const b = smem + (kt & (kStages - 1)) * STAGE;
     if constexpr (AS_IS) {
       // the chunk that reaches past the row's end, and those behind it, are the row's last 16 bytes
-      const int in = at + ((lane & 7) ^ (lane >> 3)) * 16, last = (int)g.pitch - 16, from = in < last ? in : last;
+      const int in = at + ((lane & 7) ^ (lane >> 3)) * 16, last = (int)pitch - 16, from = in < last ? in : last;
       if constexpr (e < XL) load_to_lds(rx, b + (wave * XL + e) * 1024, off_x[e] + from, 0);
       else load_to_lds(rw, b + BM * kPiece + (wave * WL + e - XL) * 1024, off_w[e - XL] + from, 0);
     } else {
@@ -324,21 +376,16 @@ __global__ __launch_bounds__(64 * (BM / WM) * (BN / WN), 2) void linear_tile_ker
   int off_f[2];
 #pragma unroll
   for (int h = 0; h < 2; ++h) {
-    const int g = lane >> 4, chunk = SPLIT ? (g >> 1) * 4 + (g & 1) + 2 * h : 4 * h + g;
+    const int q = lane >> 4, chunk = SPLIT ? (q >> 1) * 4 + (q & 1) + 2 * h : 4 * h + q;
     off_f[h] = (lane & 15) * kPiece + 16 * (chunk ^ (lane & 7));
   }
   using std::integral_constant;
   auto fragment = [&](int kt, int h, int row) { return *(const v4i*)(smem + (kt & (kStages - 1)) * STAGE + off_f[h] + row * kPiece); };
   auto read_x = [&](int kt, int h, v4i(&f)[TM], auto ic) { f[decltype(ic)::value] = fragment(kt, h, wm0 + decltype(ic)::value * 16); };
   auto read_w = [&](int kt, int h, v4i(&f)[TN], auto jc) { f[decltype(jc)::value] = fragment(kt, h, BM + wn0 + decltype(jc)::value * 16); };
-  v4f acc[TM][TN];
-#pragma unroll
-  for (int i = 0; i < TM; ++i)
-#pragma unroll
-    for (int j = 0; j < TN; ++j) acc[i][j] = v4f{0, 0, 0, 0};
   auto multiply_one = [&](const v4i& w, const v4i& x, v4f& c) {
     if constexpr (SPLIT) c = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(v8h, w), __builtin_bit_cast(v8h, x), c, 0, 0, 0);
-    else if constexpr (MODE == kF32Direct)
+    else if constexpr (MODE >= kF32Direct)
       static_for<4>([&](auto e) {
         constexpr int E = decltype(e)::value;
         c = __builtin_amdgcn_mfma_f32_16x16x4f32(__int_as_float(w[E]), __int_as_float(x[E]), c, 0, 0, 0);
@@ -359,8 +406,8 @@ __global__ __launch_bounds__(64 * (BM / WM) * (BN / WN), 2) void linear_tile_ker
   };
   // A row's last chunk holds bytes of the chunk before it as well, and those behind it nothing else: in both operands they are zero.
   auto mask = [&](int kt, int h, v4i(&w)[TN], v4i(&x)[TM]) {
-    if ((int64_t)(k_first + kt + 1) * kPiece <= g.pitch) return;     // the same in all lanes
-    const int before = (k_first + kt) * kPiece + (4 * h + (lane >> 4)) * 16 - ((int)g.pitch - 16);   // bytes of the chunk that are not its own
+    if ((int64_t)(k_first + kt + 1) * kPiece <= pitch) return;     // the same in all lanes
+    const int before = (k_first + kt) * kPiece + (4 * h + (lane >> 4)) * 16 - ((int)pitch - 16);   // bytes of the chunk that are not its own
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
       const int cut = before - 4 * e;
@@ -385,13 +432,35 @@ __global__ __launch_bounds__(64 * (BM / WM) * (BN / WN), 2) void linear_tile_ker
 #define HOT_INT(V) integral_constant<int, (V)>{}
   load_stage(0);
   load_stage(1);
+  if (!go()) {
+    meet();      // nothing of this is on its way to LDS any more
+    return false;
+  }
+#pragma unroll
+  for (int i = 0; i < TM; ++i)
+#pragma unroll
+    for (int j = 0; j < TN; ++j) acc[i][j] = v4f{0, 0, 0, 0};
   asm volatile("s_waitcnt vmcnt(%0)" : : "n"(NL) : "memory");   // the first stage
   __builtin_amdgcn_s_barrier();
   asm volatile("" ::: "memory");
   v4i wa[TN], wb[TN], xa[TM];
-  static_for<TN>([&](auto j) { read_w(0, 0, wa, j); });
-  static_for<TM>([&](auto i) { read_x(0, 0, xa, i); });
-  if constexpr (DIRECT) {
+  if constexpr (MODE != kF32Wide) {
+    static_for<TN>([&](auto j) { read_w(0, 0, wa, j); });
+    static_for<TM>([&](auto i) { read_x(0, 0, xa, i); });
+  }
+  if constexpr (MODE == kF32Wide) {     // a half of a stage at a time: the kernel's other path takes the registers
+    auto nothing = [](auto) {};
+    for (int kt = 0; kt < nk; ++kt) {
+      static_for<2>([&](auto h) {
+        static_for<TN>([&](auto j) { read_w(kt, decltype(h)::value, wa, j); });
+        static_for<TM>([&](auto i) { read_x(kt, decltype(h)::value, xa, i); });
+        mask(kt, decltype(h)::value, wa, xa);
+        products(wa, xa, nothing);
+      });
+      meet();
+      load_stage(kt + 2);
+    }
+  } else if constexpr (DIRECT) {
     v4i xb[TM];
     auto nothing = [](auto) {};
     for (int kt = 0; kt < nk; ++kt) {
@@ -450,11 +519,94 @@ __global__ __launch_bounds__(64 * (BM / WM) * (BN / WN), 2) void linear_tile_ker
     }
   }
 #undef HOT_INT
-  asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
-  __builtin_amdgcn_s_barrier();
-  asm volatile("" ::: "memory");
+  meet();
+  return true;
+}
+
+// The same for plain fp32 rows of fewer than four columns, which are shorter than a load: from memory, element by element.
+template <int BM, int BN, int WM, int WN>
+__device__ __forceinline__ void tile_short_rows(const float* x, const float* w, int I, int64_t L, int O, int64_t m0, int n0,
+                                                v4f (&acc)[WM / 16][WN / 16]) {
+  const int lane = (int)threadIdx.x & 63, wave = (int)threadIdx.x >> 6;
+  const int64_t row = m0 + wave % (BM / WM) * WM + (lane & 15);
+  const int col = n0 + wave / (BM / WM) * WN + 4 * (lane >> 4);
+#pragma unroll
+  for (int i = 0; i < WM / 16; ++i)
+#pragma unroll
+    for (int j = 0; j < WN / 16; ++j) acc[i][j] = v4f{0, 0, 0, 0};
+#pragma unroll 1
+  for (int k = 0; k < I; ++k) {
+    float xs[WM / 16];
+#pragma unroll
+    for (int i = 0; i < WM / 16; ++i) xs[i] = x[(row + i * 16 < L ? row + i * 16 : L - 1) * I + k];
+#pragma unroll
+    for (int j = 0; j < WN / 16; ++j)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const int c = col + j * 16 + r;
+        const float ws = w[(uint32_t)((c < O ? c : O - 1) * I + k)];     // O < 2^24, I < 4
+#pragma unroll
+        for (int i = 0; i < WM / 16; ++i) acc[i][j][r] = fmaf(xs[i], ws, acc[i][j][r]);
+      }
+  }
+}
+
+template <int BM, int BN, int WM, int WN, int MODE, class TY>
+__global__ __launch_bounds__(64 * (BM / WM) * (BN / WN), 2) void linear_tile_kernel(const TileArgs g) {
+  constexpr bool SPLIT = MODE == kSplitRows;
+  constexpr int WAVES_M = BM / WM, WAVES = WAVES_M * (BN / WN);
+  constexpr int TM = WM / 16, TN = WN / 16;
+  extern __shared__ __align__(16) uint8_t smem[];
+  const int tid = (int)threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  // A workgroup of a whole tile, or of a slice of one: slices of a tile are neighbours in dispatch order but for their XCD.
+  const int rest = g.tiles_m * g.tiles_n - g.whole, part = (int)blockIdx.x - g.whole;
+  const bool sliced = part >= 0;
+  const int z = sliced ? part / rest : 0, tail = sliced ? part % rest : 0;
+  int tm, tn;
+  tile_at(sliced ? g.whole + tail : xcd_contiguous((int)blockIdx.x, g.whole), g.tiles_m, g.tiles_n, tm, tn);
+  const int64_t m0 = (int64_t)tm * BM;
+  const int n0 = tn * BN;
+  const int stages = (int)((g.pitch + kPiece - 1) / kPiece);    // those of plain fp32 rows are as many as those of their parts
+  const int k_first = sliced ? (int)((int64_t)stages * z / g.slices) : 0;
+  const int nk = sliced ? (int)((int64_t)stages * (z + 1) / g.slices) - k_first : stages;
+  const int64_t rows_x = g.out.L - m0 < BM ? g.out.L - m0 : BM, rows_w = g.out.O - n0 < BN ? g.out.O - n0 : BN;
+  const int wm0 = wave % WAVES_M * WM, wn0 = wave / WAVES_M * WN;
+  v4f acc[TM][TN];
+  int scaled = 0;      // all bits: the sums are those of scaled rows
+  const auto always = [] { return true; };
+  if constexpr (SPLIT) {
+    const RowRanges<BM> of_x(g.ex + m0, (int)rows_x);
+    const RowRanges<BN> of_w(g.ew + n0, (int)rows_w);
+    scaled = -(int)tile_products<BM, BN, WM, WN, kSplitRows>(g.x, g.w, g.pitch, m0, n0, rows_x, rows_w, k_first, nk, smem, acc,
+                                                       [&] { return !wide_tile<BM, BN>(of_x, of_w); });
+    if (scaled) {}
+    else if (g.plain_pitch < 16) tile_short_rows<BM, BN, WM, WN>((const float*)g.x_plain, (const float*)g.w_plain, (int)g.plain_pitch / 4, g.out.L, g.out.O, m0, n0, acc);
+    else tile_products<BM, BN, WM, WN, kF32Wide>(g.x_plain, g.w_plain, g.plain_pitch, m0, n0, rows_x, rows_w, k_first, nk, smem, acc, always);
+  } else {
+    tile_products<BM, BN, WM, WN, MODE>(g.x, g.w, g.pitch, m0, n0, rows_x, rows_w, k_first, nk, smem, acc, always);
+  }
 
   if (sliced) {
+    if constexpr (SPLIT) {
+      if (scaled) {
+#pragma unroll
+        for (int j = 0; j < TN; ++j) {
+          int ew[4];
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            const int c = n0 + wn0 + j * 16 + 4 * (lane >> 4) + r;
+            ew[r] = word_exponent(g.ew[c < g.out.O ? c : g.out.O - 1]);
+          }
+#pragma unroll
+          for (int i = 0; i < TM; ++i) {
+            const int64_t row = m0 + wm0 + i * 16 + (lane & 15);
+            const int ex = word_exponent(g.ex[row < g.out.L ? row : g.out.L - 1]);
+#pragma unroll
+            for (int r = 0; r < 4; ++r) acc[i][j][r] = __builtin_ldexpf(acc[i][j][r], ex + ew[r]);
+          }
+        }
+      }
+    }
     // 16 bytes a lane and accumulator tile, as linear_combine_kernel reads them
     float* const image = g.images + ((int64_t)tail * g.slices + z) * (BM * BN) + tid * 4;
 #pragma unroll
@@ -483,7 +635,7 @@ __global__ __launch_bounds__(64 * (BM / WM) * (BN / WN), 2) void linear_tile_ker
       int ew[8];
       if constexpr (SPLIT) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) ew[e] = g.ew[c + e < g.out.O ? c + e : g.out.O - 1];
+        for (int e = 0; e < 8; ++e) ew[e] = word_exponent(g.ew[c + e < g.out.O ? c + e : g.out.O - 1]) & scaled;
       }
 #pragma unroll 2
       for (int t0 = 0; t0 < 32; t0 += RPI) {
@@ -499,7 +651,7 @@ __global__ __launch_bounds__(64 * (BM / WM) * (BN / WN), 2) void linear_tile_ker
         }
         if (row < g.out.L) {
           if constexpr (SPLIT) {
-            const int ex = g.ex[row];
+            const int ex = word_exponent(g.ex[row]) & scaled;
 #pragma unroll
             for (int e = 0; e < 8; ++e) v[e] = __builtin_ldexpf(v[e], ex + ew[e]);
           }
@@ -513,9 +665,8 @@ __global__ __launch_bounds__(64 * (BM / WM) * (BN / WN), 2) void linear_tile_ker
 
 // The sums of a tile's slices, in slice order, and the epilogue.  A thread takes eight outputs of a token: those of lanes l + 32 h and
 // l + 32 h + 16 of a 16 x 16 accumulator tile; four threads its 32 outputs.  Bound by the images' way through the caches.
-template <int BM, int BN, int WM, int WN, int MODE, class TY>
+template <int BM, int BN, int WM, int WN, class TY>
 __global__ __launch_bounds__(256) void linear_combine_kernel(const TileArgs g) {
-  constexpr bool SPLIT = MODE == kSplitRows;
   constexpr int WAVES_M = BM / WM, WAVES = WAVES_M * (BN / WN), TN = WN / 16;
   constexpr int PER_TILE = BM * BN / 2048;    // workgroups of a tile
   const int tail = (int)blockIdx.x / PER_TILE;
@@ -541,38 +692,42 @@ __global__ __launch_bounds__(256) void linear_combine_kernel(const TileArgs g) {
   if (row >= g.out.L) return;
   float bias[8];
   load_bias8(g.out, c, n, bias);
-  if constexpr (SPLIT) {
-    const int ex = g.ex[row];
-#pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] = __builtin_ldexpf(v[e], ex + g.ew[c + e < g.out.O ? c + e : g.out.O - 1]);
-  }
   linear_finish8<TY>(g.out, row, c, n, bias, v);
 }
 
 // Operand rows of the fp32 product: row r of the L + O rows of x and w, scaled by 2^(14 - e), e the exponent of its largest value,
-// as [16 high | 16 low] pieces; exps[r] = e - 14.  Padded columns are zero.  Bound by HBM: a row stays in the registers of the T
+// as [16 high | 16 low] pieces; words[r]: e - 14 and the row's range, the share of its columns that are large (a scaled value of 2^5 or
+// more in x, 2^7 in w, of at most 2^15), rounded down, and of those whose parts are off by more than 2^-22 of the value, rounded up; a row
+// of zeros is held exactly, one with an infinity or a NaN not at all.  Padded columns are zero.  Bound by HBM: a row stays in the registers of the T
 // lanes that work on it, NV times eight columns each, or (NV = 0: rows beyond 16384) is read a second time, from the caches.
-// 8192 + 8192 rows of 8192 columns 187 us, 5.7 TB/s read and written; 250 when such rows were read twice.
+// 8192 + 8192 rows of 8192 columns 177 us, 6.1 TB/s read and written; 250 when such rows were read twice.
 __device__ __forceinline__ int row_exponent(uint32_t top) {   // of the largest magnitude's bits; subnormal ones too
   // infinities and NaNs stay what they are under any scale
   return top >= 0x7F800000u || top == 0 ? 0 : ilogbf(__uint_as_float(top));
 }
-__device__ __forceinline__ void store_parts(uint8_t* dst, int64_t c, const float (&v)[8], int e) {
+// Called by all lanes of a wave; large, lossy: the wave's counts.
+__device__ __forceinline__ void store_parts(uint8_t* dst, int64_t c, bool store, const float (&v)[8], int e, float large_from, int& large, int& lossy) {
   v8h hi, lo;
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
     const float s = __builtin_ldexpf(v[i], 14 - e);
     hi[i] = (_Float16)s;
-    lo[i] = (_Float16)(s - (float)hi[i]);
+    const float rest = s - (float)hi[i];
+    lo[i] = (_Float16)rest;
+    large += __popcll(__builtin_amdgcn_ballot_w64(fabsf(s) >= large_from));
+    lossy += __popcll(__builtin_amdgcn_ballot_w64(fabsf(rest - (float)lo[i]) > 0x1p-22f * fabsf(s)));
+    if (e > 15) lossy += __popcll(__builtin_amdgcn_ballot_w64(s == 0.0f && v[i] != 0.0f));   // below the smallest number when scaled
   }
+  if (!store) return;
   uint8_t* const p = dst + (c >> 4) * 64 + (c & 8) * 2;
   *(v8h*)p = hi;
   *(v8h*)(p + 32) = lo;
 }
 template <int T, int NV>
 __global__ __launch_bounds__(256) void linear_split_kernel(const float* x, const float* w, int64_t L, int64_t O, int64_t I, int64_t pitch,
-                                                           uint8_t* px, uint8_t* pw, int* exps, int64_t first) {
+                                                           uint8_t* px, uint8_t* pw, uint32_t* words, int64_t first) {
   __shared__ uint32_t s_top[4];
+  __shared__ int s_large[4], s_lossy[4];
   const int lane = (int)threadIdx.x % T;
   const int64_t r = first + (int64_t)blockIdx.x * (256 / T) + (int)threadIdx.x / T;
   if (r >= L + O) return;    // T = 256: one row a workgroup
@@ -609,23 +764,40 @@ __global__ __launch_bounds__(256) void linear_split_kernel(const float* x, const
     __syncthreads();
     top = max(max(s_top[0], s_top[1]), max(s_top[2], s_top[3]));
   }
-  const int e = row_exponent(top);
-  if (lane == 0) exps[r] = e - 14;
+  const int e = __builtin_amdgcn_readfirstlane(row_exponent(top));    // a wave is on one row
+  const float large_from = r < L ? 0x1p5f : 0x1p7f;
+  int large = 0, lossy = 0;
   if constexpr (NV > 0) {
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
       const int64_t c = (lane + j * T) * 8;
       float v[8];
       widen(raw[j], v);
-      if (c < padded) store_parts(dst, c, v, e);
+      store_parts(dst, c, c < padded, v, e, large_from, large, lossy);
     }
   } else {
 #pragma unroll 2
-    for (int64_t c = lane * 8; c < padded; c += T * 8) {
+    for (int64_t c0 = 0; c0 < padded; c0 += T * 8) {
+      const int64_t c = c0 + lane * 8;
       float v[8];
       load_values(src + c, have(c), v);
-      store_parts(dst, c, v, e);
+      store_parts(dst, c, c < padded, v, e, large_from, large, lossy);
     }
+  }
+  if constexpr (T > 64) {
+    if (((int)threadIdx.x & 63) == 0) {
+      s_large[(int)threadIdx.x >> 6] = large;
+      s_lossy[(int)threadIdx.x >> 6] = lossy;
+    }
+    __syncthreads();
+    large = s_large[0] + s_large[1] + s_large[2] + s_large[3];
+    lossy = s_lossy[0] + s_lossy[1] + s_lossy[2] + s_lossy[3];
+  }
+  if (lane == 0) {
+    // shares of 1 / 1024, rounded down and up: the quotient is off by 2^-21 of itself at most
+    const float unit = 1024.0f * __builtin_amdgcn_rcpf((float)I);
+    const uint32_t some = (uint32_t)((float)large * unit * (1.0f - 0x1p-20f)), off = min(1024u, (uint32_t)ceilf((float)lossy * unit * (1.0f + 0x1p-20f)));
+    words[r] = top >= 0x7F800000u ? row_word(0, 0, 1024) : top == 0 ? row_word(0, 1024, 0) : row_word(e - 14, some, off);
   }
 }
 
@@ -639,12 +811,12 @@ hipError_t each_run(int64_t rows, int64_t lanes, F&& f) {
 }
 
 hipError_t launch_split(const float* x, const float* w, int64_t L, int64_t O, int64_t I, int64_t pitch, uint8_t* px, uint8_t* pw,
-                        int* exps, hipStream_t s) {
+                        uint32_t* words, hipStream_t s) {
   auto go = [&](auto t, auto nv) {
     constexpr int T = decltype(t)::value;
     return each_run(L + O, T, [&](int64_t first, int64_t rows) {
       linear_split_kernel<T, decltype(nv)::value><<<dim3((unsigned)ceil_div(rows, 256 / T)), dim3(256), 0, s>>>(x, w, L, O, I, pitch, px, pw,
-                                                                                                              exps, first);
+                                                                                                              words, first);
       return hipGetLastError();
     });
   };
@@ -674,20 +846,20 @@ __global__ __launch_bounds__(256) void linear_pad_kernel(const bf16* x, const bf
   }
 }
 
-// What the large tiles need besides their operands: fp32 rows in parts with their exponents; bfloat16 rows of an odd width, or shorter than
+// What the large tiles need besides their operands: fp32 rows in parts with their words; bfloat16 rows of an odd width, or shorter than
 // 16 bytes, padded: rows that begin at odd multiples of two bytes are loaded at half the rate.
 struct TileLayout {
   int64_t pitch;
   bool packed;
-  size_t w, exps, total;     // x's rows come first
+  size_t w, words, total;    // x's rows come first
 };
 TileLayout tile_layout(hot_type type, int64_t L, int64_t O, int64_t I) {
   TileLayout t;
   t.packed = type == HOT_F32 || I % 2 != 0 || I < 8;
   t.pitch = type == HOT_F32 ? round_up(I, 32) * 4 : t.packed ? round_up(I, 64) * 2 : I * 2;
   t.w = t.packed ? (size_t)round_up(L * t.pitch, 256) : 0;
-  t.exps = t.w + (t.packed ? (size_t)round_up(O * t.pitch, 256) : 0);
-  t.total = t.exps + (type == HOT_F32 ? (size_t)(L + O) * 4 : 0);
+  t.words = t.w + (t.packed ? (size_t)round_up(O * t.pitch, 256) : 0);
+  t.total = t.words + (type == HOT_F32 ? (size_t)(L + O) * 4 : 0);
   return t;
 }
 
@@ -861,7 +1033,7 @@ hipError_t tiles_sized(const TileArgs& g, hipStream_t s) {
   }
   const int64_t rest = (int64_t)g.tiles_m * g.tiles_n - g.whole;
   kern<<<dim3((unsigned)(g.whole + rest * g.slices)), dim3(THREADS), LDS, s>>>(g);
-  if (rest) linear_combine_kernel<BM, BN, WM, WN, MODE, TY><<<dim3((unsigned)(rest * (BM * BN / 2048))), dim3(256), 0, s>>>(g);
+  if (rest) linear_combine_kernel<BM, BN, WM, WN, TY><<<dim3((unsigned)(rest * (BM * BN / 2048))), dim3(256), 0, s>>>(g);
   return hipGetLastError();
 }
 
@@ -869,7 +1041,8 @@ template <class T, class TY>
 hipError_t tiles_typed(const LinearForward& a, const Plan& p, const LinearOut& o, hipStream_t s) {
   constexpr bool F32 = sizeof(T) == 4;
   const TileLayout t = tile_layout(a.type, a.L, a.O, a.I);
-  TileArgs g{(const uint8_t*)a.x, (const uint8_t*)a.w, t.pitch, nullptr, nullptr, (int)p.tiles_m, (int)p.tiles_n,
+  TileArgs g{(const uint8_t*)a.x, (const uint8_t*)a.w, t.pitch, (const uint8_t*)a.x, (const uint8_t*)a.w, a.I * (int64_t)sizeof(T), nullptr, nullptr,
+             (int)p.tiles_m, (int)p.tiles_n,
              (int)p.whole, p.slices, nullptr, o};
   if (p.slices > 1) g.images = (float*)((uint8_t*)a.ws + images_offset(p, t));
   if (p.direct) {
@@ -883,11 +1056,11 @@ hipError_t tiles_typed(const LinearForward& a, const Plan& p, const LinearOut& o
   if (t.packed) {
     uint8_t* const px = (uint8_t*)a.ws;
     uint8_t* const pw = px + t.w;
-    int* const exps = (int*)(px + t.exps);
+    uint32_t* const words = (uint32_t*)(px + t.words);
     stage_begin(kStLinearOperands, s);
     hipError_t e;
     if constexpr (F32) {
-      e = launch_split((const float*)a.x, (const float*)a.w, a.L, a.O, a.I, t.pitch, px, pw, exps, s);
+      e = launch_split((const float*)a.x, (const float*)a.w, a.L, a.O, a.I, t.pitch, px, pw, words, s);
     } else {
       e = each_run(a.L + a.O, 64, [&](int64_t first, int64_t rows) {
         linear_pad_kernel<<<dim3((unsigned)ceil_div(rows, 4)), dim3(256), 0, s>>>((const bf16*)a.x, (const bf16*)a.w, a.L, a.O, a.I, t.pitch,
@@ -899,8 +1072,8 @@ hipError_t tiles_typed(const LinearForward& a, const Plan& p, const LinearOut& o
     if (e != hipSuccess) return e;
     g.x = px;
     g.w = pw;
-    g.ex = exps;
-    g.ew = exps + a.L;
+    g.ex = words;
+    g.ew = words + a.L;
   }
   auto go = [&](auto mode) {
     constexpr int MODE = decltype(mode)::value;

@@ -179,3 +179,92 @@ def test_packed_products_on_two_streams_at_once():
             step(k, streams[k])
     torch.cuda.synchronize()
     assert all(torch.equal(a, c) for a, c in zip(alone, y + kept))
+
+
+def spread_columns(x, w):
+    """Columns that are large in x are small in w: their products are alike, and every one counts."""
+    x *= torch.logspace(-8, 0, x.shape[1], device="cuda")
+    w *= torch.logspace(0, -8, w.shape[1], device="cuda")
+
+
+def large_column(size):
+    def scale(x, w):
+        x[:, x.shape[1] // 2] *= size
+        w[:, x.shape[1] // 2] = 0.0
+    return scale
+
+
+def large_against_small(x, w):
+    x[:, 1] *= 1e6
+    w[:, 1] *= 1e-7
+
+
+def one_wide_row(x, w):
+    x[-1] *= 10.0 ** torch.linspace(-30, 6, x.shape[1], device="cuda")
+
+
+def one_wide_weight(x, w):
+    w[w.shape[0] // 2] *= 10.0 ** torch.linspace(5, -25, x.shape[1], device="cuda")
+
+
+def one_column_rows(x, w):
+    """Rows with one element: each result is one product."""
+    at = torch.arange(x.shape[0], device="cuda") % x.shape[1]
+    kept = x[torch.arange(x.shape[0], device="cuda"), at].clone()
+    x.zero_()
+    x[torch.arange(x.shape[0], device="cuda"), at] = kept
+
+
+def from_end_to_end(x, w):
+    """Beside the row's largest the others vanish even as they are scaled."""
+    x *= 2.0 ** -100
+    w *= 2.0 ** 90
+    x[:, 0], w[:, 0] = 2.0 ** 100, 0.0
+
+
+RANGES = {"columns": spread_columns, "2^24": large_column(2.0 ** 24), "2^30": large_column(2.0 ** 30), "1e6 by 1e-7": large_against_small,
+          "a row": one_wide_row, "a weight": one_wide_weight, "one column": one_column_rows,
+          "2^200": from_end_to_end}
+
+
+@pytest.mark.parametrize("name", RANGES)
+@pytest.mark.parametrize("L,O,I,tile,cut", PACKED + [(3590, 3585, 3, (128, 128), "whole"), (3590, 3585, 2, (128, 128), "whole"),
+                                                     (3590, 3585, 5, (128, 128), "whole")])
+def test_packed_rows_of_a_wide_range(L, O, I, tile, cut, name):
+    """A row's two 16-bit parts hold an element to 2^-39 of the row's largest.  Where that is not enough for the product, whatever w is,
+    the result is no worse than on any other way."""
+    packed(L, O, I, tile, cut)
+    x, w = rand((L, I), 1).cuda(), rand((O, I), 2, std=I ** -0.5).cuda()
+    RANGES[name](x, w)
+    held_to(call_linear(x, w), *product64(x, w), I, "y")
+
+
+@pytest.mark.parametrize("L,O,I,tile,cut", PACKED)
+def test_packed_rows_of_a_wide_range_through_the_epilogue(L, O, I, tile, cut):
+    packed(L, O, I, tile, cut)
+    x, w, b, r = rand((L, I), 1).cuda(), rand((O, I), 2, std=I ** -0.5).cuda(), rand((O,), 3), rand((L, O), 4)
+    x[L // 2:, 0] *= 2.0 ** 24
+    w[:, 0] = 0.0
+    kept = hot.alloc_checkpoint(L, O)
+    y = call_linear(x, w, bias=b.cuda(), residual=r.cuda(), fn=hot.HOT_ACT_SILU, ckpt=kept)
+    z, size = product64(x, w)
+    z = z + ref.f64(b)
+    dz = 27 * ref.U * size + ref.U * z.abs()
+    want, dy = ref.act("silu", z)
+    close(y, want + ref.f64(r), dy + 1.2 * dz + 2 * ref.U * (want.abs() + ref.f64(r).abs()), "y")
+    back = ref.f64(hot.hot_checkpoint_read(kept, torch.empty((L, O), device="cuda")))
+    pad = torch.zeros(L, -(-O // 32) * 32, dtype=torch.float64)
+    pad[:, :O] = z.abs() + dz
+    step = pad.view(L, -1, 32).amax(-1).clamp(min=2.0 ** -118) / 63.75      # the largest is 63.75 steps or more
+    close(back, z, dz + step.repeat_interleave(32, 1)[:, :O] / 2, "z of the checkpoint")
+
+
+@pytest.mark.parametrize("L,O,I,tile,cut", PACKED)
+def test_packed_infinities_are_infinite(L, O, I, tile, cut):
+    packed(L, O, I, tile, cut)
+    x, w = rand((L, I), 1), rand((O, I), 2, std=I ** -0.5)
+    x[5, 3], x[L - 1, I - 1] = INF, -INF
+    y = call_linear(x.cuda(), w.cuda()).cpu()
+    assert torch.equal(y[5], w[:, 3].sign() * INF) and torch.equal(y[L - 1], w[:, I - 1].sign() * -INF)
+    y[5], y[L - 1] = 0.0, 0.0
+    assert bool(torch.isfinite(y).all())
