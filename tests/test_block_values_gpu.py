@@ -268,3 +268,180 @@ def test_packed_infinities_are_infinite(L, O, I, tile, cut):
     assert torch.equal(y[5], w[:, 3].sign() * INF) and torch.equal(y[L - 1], w[:, I - 1].sign() * -INF)
     y[5], y[L - 1] = 0.0, 0.0
     assert bool(torch.isfinite(y).all())
+
+
+# ---- outputs stored with the streaming hint ---------------------------------------------------------------------------------------
+# Those past 32 MB with rows of whole 128-byte lines.
+
+def streams(rows, cols, size):
+    return rows * cols * size > 2 ** 25 and cols * size % 128 == 0
+
+
+def pieces(rows, cols, size):
+    """Runs of rows that are not streamed."""
+    step = 2 ** 25 // (cols * size)
+    return [slice(a, min(a + step, rows)) for a in range(0, rows, step)]
+
+
+def large_input(rows, cols, seed):
+    """bfloat16 of unit spread; a group at the end of the type, whose values past 127 steps are held there, one past it, and a NaN."""
+    x = torch.empty((rows, cols), device="cuda").normal_(generator=torch.Generator("cuda").manual_seed(seed)).bfloat16()
+    x[rows // 2, :32] = torch.linspace(-1.9921875, 1.9921875, 32).mul(2.0 ** 127).bfloat16().cuda()
+    x[rows - 1, cols - 32] = 3.3e38
+    x[1, 40], x[rows - 2, 5] = NAN, INF
+    return x
+
+
+def same(a, b):
+    """Equal bits, or a NaN in both."""
+    return torch.equal(a.isnan(), b.isnan()) and torch.equal(a.nan_to_num(7.0, 3.0e38, -3.0e38), b.nan_to_num(7.0, 3.0e38, -3.0e38))
+
+
+@pytest.mark.parametrize("fn", FNS)
+def test_streamed_activation(fn):
+    """Value, checkpoint, its reading, gradient and bias sums of a large bfloat16 tensor: every row as in a call too small to be
+    streamed, and rows from all over against 64 bits."""
+    rows, cols, code = 8200, 2112, hot.ACT_FNS[fn]
+    assert streams(rows, cols, 2) and not any(streams(p.stop - p.start, cols, 2) for p in pieces(rows, cols, 2))
+    x, g = large_input(rows, cols, 1), torch.empty((rows, cols), device="cuda").normal_(generator=torch.Generator("cuda").manual_seed(2)).bfloat16()
+    y, back, gx, gx2, alone = (torch.full_like(x, 7.0) for _ in range(5))
+    kept, gb, gb2, ws = hot.alloc_checkpoint(rows, cols), *(torch.empty(cols, device="cuda") for _ in range(2)), hot.alloc_activation_workspace(rows, cols)
+    only = torch.zeros_like(kept)
+    hot.hot_activation_forward(code, x, y, ckpt=kept)
+    hot.hot_activation_forward(code, x, alone)
+    hot.hot_checkpoint_write(x, only)
+    hot.hot_checkpoint_read(kept, back)
+    hot.hot_activation_backward(code, g, gx, ckpt=kept, g_bias=gb, ws=ws)
+    hot.hot_activation_backward(code, g, gx2, x=x, g_bias=gb2, ws=ws)
+    no_sums = hot.hot_activation_backward(code, g, torch.empty_like(g), ckpt=kept)
+    assert torch.equal(only, kept) and same(alone, y) and same(no_sums, gx)
+    sums, sums2 = torch.zeros(cols, dtype=torch.float64, device="cuda"), torch.zeros(cols, dtype=torch.float64, device="cuda")
+    for p in pieces(rows, cols, 2):
+        n = p.stop - p.start
+        part, ckpt = torch.empty((n, cols), dtype=BF16, device="cuda"), hot.alloc_checkpoint(n, cols)
+        xs, gs, half = x[p].contiguous(), g[p].contiguous(), torch.empty(cols, device="cuda")
+        assert same(hot.hot_activation_forward(code, xs, part, ckpt=ckpt), y[p])
+        assert same(hot.hot_checkpoint_read(ckpt, part), back[p])
+        small = hot.alloc_activation_workspace(n, cols)
+        assert same(hot.hot_activation_backward(code, gs, part, ckpt=ckpt, g_bias=half, ws=small), gx[p])
+        sums += half.double()
+        assert same(hot.hot_activation_backward(code, gs, part, x=xs, g_bias=half, ws=small), gx2[p])
+        sums2 += half.double()
+    # each side adds 8200 values of a column in fp32, at most 64 + 64 one after the other; |g_x| <= 1.13 |g_y|
+    size = 1.13 * g.double().abs().sum(0).cpu()
+    for got, want in ((gb, sums), (gb2, sums2)):
+        close(got, want.cpu(), 2 * 128 * ref.U * size, "g_bias")
+    at = torch.tensor([0, 1, 2, rows // 2, rows - 2, rows - 1] + list(range(17, rows, 400)))
+    xs, gs = x[at.cuda()].cpu(), g[at.cuda()].cpu()
+    values = ref.checkpoint(xs)[2]
+    assert torch.equal(torch.isnan(ref.f64(back[at.cuda()])), torch.isnan(values))
+    assert torch.equal(ref.f64(back[at.cuda()]).nan_to_num(7.0), values.nan_to_num(7.0))
+    plain = (xs.float().abs() < 1e4).all(1)       # the formulas of the tolerances end far out
+    want, tol = ref.act(fn, ref.f64(xs[plain]))
+    close(y[at.cuda()][plain.cuda()], want, tol + 2.0 ** -8 * (want.abs() + tol), "y")
+    want, tol, _, _ = ref.act_grad(fn, ref.f64(gs[plain]), values[plain], BF16)
+    close(gx[at.cuda()][plain.cuda()], want, tol, "g_x")
+
+
+@pytest.mark.parametrize("kept", [False, True])
+@pytest.mark.parametrize("rows,cols", [(140000, 128), (70000, 256), (33000, 512), (17000, 1024), (8200, 2112), (4200, 4096), (2100, 8192), (1600, 11008)])
+def test_streamed_layer_norm_gradient(rows, cols, kept):
+    """Every width of the kernel: rows as in calls too small to be streamed, sums and some rows against 64 bits."""
+    assert streams(rows, cols, 2)
+    g = torch.Generator("cuda").manual_seed(cols)
+    make = lambda *s: torch.empty(s, device="cuda").normal_(generator=g)          # noqa: E731
+    x, gy, gr, gamma, beta = make(rows, cols).bfloat16(), make(rows, cols).bfloat16(), make(rows, cols).bfloat16(), 1 + 0.2 * make(cols), make(cols)
+    y, mean, rstd, buf = torch.empty_like(x), torch.empty(rows, device="cuda"), torch.empty(rows, device="cuda"), hot.alloc_checkpoint(rows, cols)
+    hot.hot_layer_norm_forward(x, gamma, beta, 1e-6, y, mean, rstd, ckpt=buf)
+    gx, gg, gb = torch.full_like(x, 7.0), torch.empty(cols, device="cuda"), torch.empty(cols, device="cuda")
+    args = dict(h=None if kept else x, ckpt=buf if kept else None)
+    hot.hot_layer_norm_backward(gy, gamma, mean, rstd, gx, gg, gb, hot.alloc_layer_norm_workspace(rows, cols), g_residual=gr, **args)
+    held = hot.hot_checkpoint_read(buf, torch.empty_like(x)) if kept else x
+    n = (held.double() - mean.double()[:, None]) * rstd.double()[:, None]
+    # at most 1024 rows one after the other in a workgroup's sum, 32 + 5 of those; three roundings an element
+    for got, terms in ((gg, gy.double() * n), (gb, gy.double())):
+        close(got, terms.sum(0).cpu(), 1100 * ref.U * terms.abs().sum(0).cpu(), "sums")
+    for p in pieces(rows, cols, 2):
+        m = p.stop - p.start
+        some = dict(h=None if kept else x[p].contiguous(), ckpt=None)
+        if kept:
+            some["ckpt"] = hot.hot_checkpoint_write(x[p].contiguous(), hot.alloc_checkpoint(m, cols))
+        part = hot.hot_layer_norm_backward(gy[p].contiguous(), gamma, mean[p].clone(), rstd[p].clone(), torch.empty((m, cols), dtype=BF16, device="cuda"),
+                                           g_residual=gr[p].contiguous(), **some)
+        assert torch.equal(part, gx[p])
+    at = torch.arange(0, rows, rows // 13, device="cuda")
+    wx, _, _ = ref.norm_grad(ref.f64(gy[at]), ref.f64(held[at]), ref.f64(gamma), ref.f64(mean[at]), ref.f64(rstd[at]), ref.f64(gr[at]), BF16)
+    close(gx[at], *wx, "g_x")
+
+
+STREAMED = [
+    (BF16, "direct", 8344, 2048, 64), (BF16, "direct", 26637, 640, 8), (BF16, "direct", 267070, 64, 64), (BF16, "direct", 16570, 1024, 8),
+    (BF16, "packed", 65757, 320, 773), (BF16, "packed", 2130, 8192, 9), (BF16, "packed", 33352, 512, 707), (BF16, "packed", 128623, 192, 79),
+    (BF16, "tiles", 26606, 640, 1074), (BF16, "tiles", 177597, 128, 64), (BF16, "tiles", 195187, 128, 10), (BF16, "tiles", 22519, 768, 1088),
+    (BF16, "tiles", 66646, 256, 712), (BF16, "tiles", 123516, 192, 256), (BF16, "tiles", 131018, 192, 186),
+    (F32, "direct", 1051, 8192, 32), (F32, "direct", 11037, 768, 8), (F32, "direct", 265528, 32, 32), (F32, "direct", 16560, 512, 8),
+    (F32, "packed", 16634, 512, 1663), (F32, "packed", 1541, 8192, 8), (F32, "packed", 65543, 192, 482), (F32, "packed", 64792, 192, 33)]
+
+
+@pytest.mark.parametrize("t,way,L,O,I", STREAMED)
+def test_streamed_linear(t, way, L, O, I):
+    """Bias, activation, residual and checkpoint behind a large product, one row of which reaches the end of the type."""
+    p = hot.hot_debug_linear_plan(t, L, O, I, ckpt=True)
+    print(f"[streamed] {L}x{O}x{I} {t} {p}", flush=True)
+    assert p["streams"] and p["way"] == way
+    g = torch.Generator("cuda").manual_seed(L + O)
+    make = lambda *s: torch.empty(s, device="cuda").normal_(generator=g)          # noqa: E731
+    x, w, b, r = make(L, I).to(t), (make(O, I) * I ** -0.5).to(t), make(O), make(L, O).to(t)
+    far = L - 3                              # its first 32 outputs are +-255 x 2^120, 127.5 steps; no other row has its column
+    x[:, 0], x[far], w[:, 0] = 0.0, 0.0, 0.0
+    x[far, 0] = 2.0 ** 64
+    w[:32, 0] = (torch.arange(32, device="cuda") % 2 * 2.0 - 1).to(t) * 1.9921875 * 2.0 ** 63
+    kept, y, y0 = hot.alloc_checkpoint(L, O), torch.full((L, O), NAN, dtype=t, device="cuda"), torch.full((L, O), NAN, dtype=t, device="cuda")
+    ws = hot.alloc_linear_workspace(t, L, O, I)
+    hot.hot_linear_forward(x, w, y, ws, bias=b, residual=r, fn=hot.HOT_ACT_SILU, ckpt=kept)
+    hot.hot_linear_forward(x, w, y0, ws)
+    z, size = product64(x, w)
+    half = ref.HALF[t]
+    d0 = 26 * ref.U * size + (2 * I + 1) * 2.0 ** -150
+    close(y0, z, d0 + half * (z.abs() + d0), "bare y")
+    z = z + ref.f64(b)
+    dz = d0 + ref.U * z.abs()
+    want, dy = ref.act("silu", z)
+    dy = dy + 1.2 * dz
+    want, dy = want + ref.f64(r), dy + 2 * ref.U * (want.abs() + ref.f64(r).abs())
+    # far out the formula of the activation's error has infinity times zero: the value is z or 0 there
+    far_out = z.abs() > 1e4
+    dy = torch.where(far_out, dz + 4 * ref.U * z.abs(), dy)
+    close(y, want, dy + half * (want.abs() + dy), "y")
+    back = torch.empty((L, O), device="cuda")
+    back = ref.f64(hot.hot_checkpoint_read(kept, back))
+    step = (z.abs() + dz).view(L, -1, 32).amax(-1).clamp(min=2.0 ** -118) / 63.75
+    close(back, z, dz + step.repeat_interleave(32, 1) / 2, "z of the checkpoint")
+    assert torch.equal(back[far, :32], (torch.arange(32) % 2 * 2.0 - 1).double() * 127 * 2.0 ** 121)
+
+
+def test_streamed_tensors_past_32_bits():
+    """Elements past 2^32 in rows of whole lines: the last rows give what they give in a call of their own."""
+    rows, cols = 2 ** 17 + 6, 2 ** 15 + 256
+    assert streams(rows, cols, 2) and streams(rows * 4, cols // 4, 2) and rows * cols > 2 ** 32
+    x = torch.empty((rows, cols), dtype=BF16, device="cuda").normal_(generator=torch.Generator("cuda").manual_seed(1))
+    tail = x[-7:].contiguous()
+    y, kept, y7, kept7 = torch.empty_like(x), hot.alloc_checkpoint(rows, cols), torch.empty_like(tail), hot.alloc_checkpoint(7, cols)
+    hot.hot_activation_forward(hot.HOT_ACT_GELU, x, y, ckpt=kept)
+    hot.hot_activation_forward(hot.HOT_ACT_GELU, tail, y7, ckpt=kept7)
+    assert torch.equal(y[-7:], y7)
+    back, back7 = torch.empty_like(x), torch.empty_like(tail)
+    hot.hot_checkpoint_read(kept, back)
+    hot.hot_checkpoint_read(kept7, back7)
+    assert torch.equal(back[-7:], back7)
+    hot.hot_activation_backward(hot.HOT_ACT_GELU, y, back, ckpt=kept)
+    hot.hot_activation_backward(hot.HOT_ACT_GELU, y7, back7, ckpt=kept7)
+    assert torch.equal(back[-7:], back7)
+    mean, rstd, mean7, rstd7 = (torch.empty(n, device="cuda") for n in (rows * 4, rows * 4, 28, 28))
+    x, tail = x.view(rows * 4, cols // 4), tail.view(28, cols // 4)
+    y, y7, gx, gx7 = y.view_as(x), y7.view_as(tail), back.view_as(x), back7.view_as(tail)
+    hot.hot_layer_norm_forward(x, None, None, 1e-6, y, mean, rstd)
+    hot.hot_layer_norm_forward(tail, None, None, 1e-6, y7, mean7, rstd7)
+    hot.hot_layer_norm_backward(y, None, mean, rstd, gx, h=x)
+    hot.hot_layer_norm_backward(y7, None, mean7, rstd7, gx7, h=tail)
+    assert torch.equal(y[-28:], y7) and torch.equal(mean[-28:], mean7) and torch.equal(gx[-28:], gx7)
