@@ -327,7 +327,8 @@ hot_status hot_layer_norm_backward(const void* g_y, hot_type y_type, const void*
  * and NaN too): those run on the fp32 instructions, in about three times the time.  So the last bits of a row may depend
  * on the other rows, within that bound.  I < 2^24, O < 2^24.
  * ws: at least hot_linear_forward_workspace_bytes() bytes of scratch, 256-byte aligned (where that is
- * 0, ws may be NULL).
+ * 0, ws may be NULL).  A smaller product may need more than a larger one, whose tiles need no slices: a workspace
+ * for several sizes is as large as the largest of theirs (a smaller one is refused).
  */
 size_t hot_linear_forward_workspace_bytes(hot_type type, int64_t L, int64_t O, int64_t I);
 hot_status hot_linear_forward(const void* x, const void* w, hot_type type, const float* bias, const void* residual,

@@ -407,8 +407,14 @@ def hot_layer_norm_backward_workspace_bytes(rows: int, cols: int) -> int:
     return int(lib().hot_layer_norm_backward_workspace_bytes(rows, cols))
 
 
+def _type_of(name: str, dtype: torch.dtype) -> int:
+    if dtype not in _TYPES:
+        raise ValueError(f"{name}: expected torch.float32 or torch.bfloat16, not {dtype}")
+    return _TYPES[dtype]
+
+
 def hot_linear_forward_workspace_bytes(dtype: torch.dtype, L: int, O: int, I: int) -> int:
-    return int(lib().hot_linear_forward_workspace_bytes(_TYPES[dtype], L, O, I))
+    return int(lib().hot_linear_forward_workspace_bytes(_type_of("dtype", dtype), L, O, I))
 
 
 def _alloc(n: int, where: str, device) -> torch.Tensor:
@@ -432,8 +438,10 @@ def alloc_layer_norm_workspace(rows: int, cols: int, device="cuda") -> torch.Ten
 
 
 def alloc_linear_workspace(dtype: torch.dtype, L: int, O: int, I: int, device="cuda") -> Optional[torch.Tensor]:
-    """Scratch of hot_linear_forward; None where it needs none."""
+    """Scratch of hot_linear_forward for these sizes (others may need more, smaller ones too); None where it needs none."""
     n = hot_linear_forward_workspace_bytes(dtype, L, O, I)
+    if not (0 < L < 1 << 31 and 0 < O < 1 << 24 and 0 < I < 1 << 24):
+        raise HotError(HOT_ERR_SHAPE, "hot_linear_forward_workspace_bytes")
     return torch.empty(n, dtype=torch.uint8, device=device) if n else None
 
 
@@ -668,7 +676,7 @@ def hot_debug_linear_plan(dtype: torch.dtype, L: int, O: int, I: int, y_dtype: O
     """How hot_linear_forward works on a product: its way ("rows", "direct", "tiles", "packed"), rows and outputs a workgroup, tiles, tiles
     with a workgroup each, slices of the others, whether row ends are masked, whether y is streamed."""
     p = hot_linear_plan()
-    _check(lib().hot_debug_linear_plan(_TYPES[dtype], _TYPES[y_dtype or dtype], L, O, I, int(ckpt), C.byref(p)), "hot_debug_linear_plan")
+    _check(lib().hot_debug_linear_plan(_type_of("dtype", dtype), _type_of("y_dtype", y_dtype or dtype), L, O, I, int(ckpt), C.byref(p)), "hot_debug_linear_plan")
     return dict(way=("rows", "direct", "tiles", "packed")[p.way], tile=(p.tile_rows, p.tile_cols), tiles=p.tiles, whole=p.whole,
                 slices=p.slices, masked=bool(p.masked), streams=bool(p.streams))
 

@@ -166,6 +166,23 @@ def test_norm_gradients_are_those_of_its_values():
         assert float((value - at64).abs().max()) < 1e-12
 
 
+# ---- sizes asked for from Python ----------------------------------------------------------------------------------------------
+
+def test_linear_workspace_refuses_other_types_and_sizes():
+    for call in (hot.hot_linear_forward_workspace_bytes, hot.alloc_linear_workspace, hot.hot_debug_linear_plan):
+        for dtype in (torch.float16, torch.float64, torch.int8):
+            with pytest.raises(ValueError):
+                call(dtype, 64, 64, 64)
+    for bad in ((0, 4, 4), (4, 0, 4), (4, 4, 0), (-1, 4, 4), (1 << 31, 4, 4), (4, 1 << 24, 4), (4, 4, 1 << 24)):
+        with pytest.raises(hot.HotError):
+            hot.alloc_linear_workspace(torch.float32, *bad, device="cpu")
+        with pytest.raises(hot.HotError):
+            hot.hot_debug_linear_plan(torch.float32, *bad)
+    assert hot.alloc_linear_workspace(torch.float32, 1, 1, 1, device="cpu") is None
+    assert hot.alloc_linear_workspace(torch.float32, 12608, 2304, 768, device="cpu").numel() == \
+        hot.hot_linear_forward_workspace_bytes(torch.float32, 12608, 2304, 768) > 0
+
+
 # ---- the timing of stages --------------------------------------------------------------------------------------------------------
 
 def test_stage_timing_fills_the_arrays_that_its_caller_has():
