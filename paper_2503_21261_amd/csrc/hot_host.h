@@ -5,6 +5,8 @@
 #include <stddef.h>
 #include <stdint.h>
 
+#include <atomic>
+
 #include "hot.h"
 
 namespace hot {
@@ -162,6 +164,18 @@ enum Stage {
   kStGyFusedQuant, kStCkptWrite, kStCkptRead, kStActForward, kStActBackward, kStNormForward, kStNormBackward,
   kStColumnSums, kStLinearOperands, kStLinear
 };
+// A kernel's limit of dynamic LDS is each device's own: raised on the current one, once (again does no harm).  `done`: the kernel's,
+// a bit a device.
+inline hipError_t raise_lds_limit(const void* kernel, int bytes, std::atomic<uint64_t>& done) {
+  int device = 0;
+  if (const hipError_t e = hipGetDevice(&device); e != hipSuccess) return e;
+  const uint64_t bit = device < 64 ? 1ull << device : 0;
+  if (done.load(std::memory_order_acquire) & bit) return hipSuccess;
+  if (const hipError_t e = hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, bytes); e != hipSuccess) return e;
+  done.fetch_or(bit, std::memory_order_release);
+  return hipSuccess;
+}
+
 void stage_begin(int stage, hipStream_t s);
 void stage_end(int stage, hipStream_t s);
 

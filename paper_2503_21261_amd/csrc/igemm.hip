@@ -288,12 +288,8 @@ hipError_t launch_kernel(const GemmArgs& g, unsigned grid, hipStream_t s, int ge
   const size_t lds = 2 * (size_t)(BM + BN) * BKB;
   constexpr int WM = gemm_waves_m<BM, INT4, BF16>();
   auto kern = igemm_kernel<BM, BN, WM, 2, BKB, INT4, BF16, SPLIT>;
-  static std::atomic<bool> attr_set{false};  // per instantiation; setting it twice is harmless
-  if (!attr_set.load(std::memory_order_acquire)) {
-    hipError_t e = hipFuncSetAttribute((const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
-    if (e != hipSuccess) return e;
-    attr_set.store(true, std::memory_order_release);
-  }
+  static std::atomic<uint64_t> raised{0};
+  if (const hipError_t e = raise_lds_limit((const void*)kern, (int)lds, raised); e != hipSuccess) return e;
   if (gemm_stage >= 0) stage_begin(gemm_stage, s);
   kern<<<dim3(grid), dim3(64 * WM * 2), lds, s>>>(g);
   if (gemm_stage >= 0) stage_end(gemm_stage, s);
@@ -425,12 +421,8 @@ hipError_t launch_pair_kernel(const GemmArgs& gw, const GemmArgs& gx, int gw_wgs
   constexpr size_t lds_w = 2 * (128 + 128) * 128, lds_x = 2 * (128 + BN) * (INT4 ? 64 : 128);
   constexpr size_t lds = lds_w > lds_x ? lds_w : lds_x;
   auto kern = gemm_pair_kernel<BN, INT4, BF16, SPLIT>;
-  static std::atomic<bool> attr_set{false};
-  if (!attr_set.load(std::memory_order_acquire)) {
-    hipError_t e = hipFuncSetAttribute((const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
-    if (e != hipSuccess) return e;
-    attr_set.store(true, std::memory_order_release);
-  }
+  static std::atomic<uint64_t> raised{0};
+  if (const hipError_t e = raise_lds_limit((const void*)kern, (int)lds, raised); e != hipSuccess) return e;
   kern<<<dim3((unsigned)(gw_wgs + gx_wgs)), dim3(256), lds, s>>>(gw, gx, gw_wgs);
   return hipGetLastError();
 }

@@ -1026,11 +1026,8 @@ template <int BM, int BN, int WM, int WN, int MODE, class TY>
 hipError_t tiles_sized(const TileArgs& g, hipStream_t s) {
   constexpr int LDS = kTileLds<BM, BN, WM, WN>, THREADS = 64 * (BM / WM) * (BN / WN);
   auto kern = linear_tile_kernel<BM, BN, WM, WN, MODE, TY>;
-  static std::atomic<bool> attr_set{false};  // per instantiation; setting it twice is harmless
-  if (!attr_set.load(std::memory_order_acquire)) {
-    if (const hipError_t e = hipFuncSetAttribute((const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize, LDS); e != hipSuccess) return e;
-    attr_set.store(true, std::memory_order_release);
-  }
+  static std::atomic<uint64_t> raised{0};
+  if (const hipError_t e = raise_lds_limit((const void*)kern, LDS, raised); e != hipSuccess) return e;
   const int64_t rest = (int64_t)g.tiles_m * g.tiles_n - g.whole;
   kern<<<dim3((unsigned)(g.whole + rest * g.slices)), dim3(THREADS), LDS, s>>>(g);
   if (rest) linear_combine_kernel<BM, BN, WM, WN, TY><<<dim3((unsigned)(rest * (BM * BN / 2048))), dim3(256), 0, s>>>(g);

@@ -445,3 +445,14 @@ def test_streamed_tensors_past_32_bits():
     hot.hot_layer_norm_backward(y, None, mean, rstd, gx, h=x)
     hot.hot_layer_norm_backward(y7, None, mean7, rstd7, gx7, h=tail)
     assert torch.equal(y[-28:], y7) and torch.equal(mean[-28:], mean7) and torch.equal(gx[-28:], gx7)
+
+
+@pytest.mark.skipif(torch.cuda.device_count() < 2, reason="needs a second device")
+def test_large_tiles_on_a_second_device():
+    """Kernels that take more LDS than a launch may by itself, on one device of a process after another."""
+    x, w = rand((3500, 100), 1), rand((3600, 100), 2)
+    for device in ("cuda:0", "cuda:1"):
+        with torch.cuda.device(device):
+            y = torch.empty((3500, 3600), device=device)
+            hot.hot_linear_forward(x.to(device), w.to(device), y, hot.alloc_linear_workspace(F32, 3500, 3600, 100, device=device))
+            held_to(y, *product64(x.to(device), w.to(device)), 100, device)
