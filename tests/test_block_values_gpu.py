@@ -115,6 +115,12 @@ def test_linear_of_whole_numbers_is_exact(t, L, O, I):
         assert torch.equal(call_linear(x, w, y_type=F32).double(), want)
 
 
+@pytest.mark.parametrize("t,L,O,I", LINEAR_WAYS)
+def test_every_way_near_the_exact_one(t, L, O, I):
+    x, w = rand((L, I), 1, t).cuda(), rand((O, I), 2, t, I ** -0.5).cuda()
+    held_to(call_linear(x, w), *product64(x, w), I, "y")
+
+
 @pytest.mark.parametrize("L,O,I,tile,cut", PACKED)
 def test_packed_product_near_the_exact_one(L, O, I, tile, cut):
     packed(L, O, I, tile, cut)
