@@ -256,7 +256,8 @@ typedef enum {
  * 8-bit checkpoint of a tensor: 32 consecutive columns of a row (a row's last group may be
  * shorter) share a step s = 2^(e - 133), the smallest power of two from 2^-125 on that leaves
  * the group's largest magnitude within 127 steps after rounding; code = round(t / s), half to
- * even, one signed byte; the value read back is code * s, exact in either type, at most s / 2 off.
+ * even, one signed byte; the value read back is code * s, exact in either type, at most s / 2 off
+ * (at the type's end, where there is no larger step, 127.5 steps and more are held at 127: up to s off).
  * A group that holds an infinity or a NaN reads back as NaN.  Layout: rows x pitch codes, pitch =
  * cols rounded up to 32 (codes past cols are 0), then, from the next multiple of 256 bytes on,
  * rows x pitch / 32 bytes e (255: NaN).  25.8 % of fp32.

@@ -146,6 +146,17 @@ def test_checkpoint_form_keeps_half_a_step():
     assert not codes[:, 100:].any()
 
 
+def test_checkpoint_form_at_the_end_of_the_type():
+    """The largest step there is, 2^121: half of it off up to 127.5 steps, a whole one at most beyond."""
+    t = torch.cat([torch.linspace(2.0, 255.0 / 128, 4096).mul(2.0 ** 126), torch.linspace(255.0 / 128, 2 - 2.0 ** -23, 4096).mul(2.0 ** 127)]).view(-1, 32)
+    t[:, 0] = 255.0 / 128 * 2.0 ** 127             # every group has the largest step
+    codes, exps, values = ref.checkpoint(t)
+    assert (exps == 254).all() and np.abs(codes).max() == 127
+    off = (values - t.double()).abs()
+    far = t.double() > 127.5 * 2.0 ** 121
+    assert bool((off[~far] <= 2.0 ** 120).all()) and bool((off[far] <= 2.0 ** 121).all()) and float(off.max()) > 0.99 * 2.0 ** 121
+
+
 @pytest.mark.parametrize("fn", ["relu", "gelu", "gelu_tanh", "silu"])
 def test_slopes_are_the_differences_of_the_values(fn):
     x = torch.linspace(-8, 8, 4001, dtype=torch.float64) + 1e-4
