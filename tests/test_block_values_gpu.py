@@ -462,3 +462,16 @@ def test_large_tiles_on_a_second_device():
             y = torch.empty((3500, 3600), device=device)
             hot.hot_linear_forward(x.to(device), w.to(device), y, hot.alloc_linear_workspace(F32, 3500, 3600, 100, device=device))
             held_to(y, *product64(x.to(device), w.to(device)), 100, device)
+
+
+def test_gelu_tanh_slope_keeps_its_tail():
+    """1 - sigmoid is small beside 1 from x = 3 on and meets a large factor.  In units u = 2^-24: the argument and its exponential are off by
+    4 u |arg|, which the sigmoid s takes times s (1 - s), the product x s (1 - s) arg' relative to itself; three roundings of s (a reciprocal
+    and a sum), eight of the product, one of each sum."""
+    x = torch.linspace(-9.9, 9.9, 20000).view(20, 1000)
+    got = hot.hot_activation_backward(hot.HOT_ACT_GELU_TANH, torch.ones_like(x).cuda(), torch.empty_like(x, device="cuda"), x=x.cuda())
+    X = ref.f64(x)
+    arg, up = ref._tanh_arg(X)
+    s, r = torch.sigmoid(arg), torch.sigmoid(-arg)
+    want, product = ref.act_slope("gelu_tanh", X)[0], (X * up * s * r).abs()
+    close(got, want, ref.U * (4 * arg.abs() * s * r + 3 * s + product * (4 * arg.abs() + 8) + 2 * want.abs()) + 2.0 ** -100, "slope")
