@@ -475,3 +475,33 @@ def test_gelu_tanh_slope_keeps_its_tail():
     s, r = torch.sigmoid(arg), torch.sigmoid(-arg)
     want, product = ref.act_slope("gelu_tanh", X)[0], (X * up * s * r).abs()
     close(got, want, ref.U * (4 * arg.abs() * s * r + 3 * s + product * (4 * arg.abs() + 8) + 2 * want.abs()) + 2.0 ** -100, "slope")
+
+
+@pytest.mark.parametrize("L,O,I,tile,cut", PACKED)
+def test_packed_product_recorded_on_rows_of_other_ranges(L, O, I, tile, cut):
+    """Which instructions a tile takes is decided anew on every replay: ordinary rows, wide ones, infinities, ordinary ones again, each as
+    eager calls give them and near the exact product."""
+    packed(L, O, I, tile, cut)
+    x, w, ws = rand((L, I), 1).cuda(), rand((O, I), 2, std=I ** -0.5).cuda(), hot.alloc_linear_workspace(F32, L, O, I)
+    w[:, 0] = 0.0
+    first, y, eager = x.clone(), torch.empty((L, O), device="cuda"), torch.empty((L, O), device="cuda")
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        hot.hot_linear_forward(x, w, y, ws)
+    seen = []
+    for scale in (1.0, 2.0 ** 24, INF, 1.0):
+        x.copy_(first)
+        if scale == INF:
+            x[L // 2, 1] = INF
+        else:
+            x[L // 3:, 0] *= scale
+        y.fill_(NAN)
+        graph.replay()
+        hot.hot_linear_forward(x, w, eager, ws)
+        torch.cuda.synchronize()
+        assert same(y, eager), scale
+        if scale != INF:
+            held_to(y, *product64(x, w), I, f"scale {scale}")
+        seen.append(y.clone())
+    assert torch.equal(seen[0], seen[3]) and not torch.equal(seen[0], seen[1])
