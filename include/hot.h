@@ -242,7 +242,7 @@ hot_status hot_lowpass_l1_rows(int32_t block, int32_t keep, int32_t* keep_idx);
  *     `replayable`.  Two graphs may share a workspace if they never run at once.
  *   - Results have the same bits in every call (no atomics).
  *   - An infinity or a NaN in a row reaches that row's results (and the sums over
- *     rows), never another row's.
+ *     rows) as the formulas have it, never another row's.
  */
 typedef enum { HOT_F32 = 0, HOT_BF16 = 1 } hot_type;
 

@@ -210,9 +210,10 @@ __global__ __launch_bounds__(256) void linear_rows_combine_kernel(const float* s
 // registers for each product, and as the chip's power holds such products down, that is time (8192^3 bfloat16 1417 TFLOP/s, 1323
 // with them; stages of 64 bytes, four deep: a tenth less).  The weight is the first operand, so that accumulators are runs of four
 // outputs of a token; they leave through LDS, a wave's 32 tokens at a time, as runs of eight outputs a lane.
-// Measured: 16384 x 11008 x 4096 bfloat16 1070 us, 1380 TFLOP/s; with a checkpoint 1095, with GELU 1125 (vector instructions of the
-// epilogue, under which no matrix instruction runs), with both 1155; 12608 x 2304 x 768 fp32 125 us, 1070 TFLOP/s of fp16 products,
-// and 20 us for its operands.
+// Measured, in a graph by itself: 16384 x 11008 x 4096 bfloat16 1060 us, 1390 TFLOP/s; with a checkpoint 1080, with GELU 1105 (vector
+// instructions of the epilogue, under which no matrix instruction runs), with both 1150, and 1210 to 1260 where its gradient runs between
+// its calls; 12608 x 2304 x 768 fp32 126 to 147 us from run to run, 128 at best in each, 1060 to 910 TFLOP/s of fp16 products, and 18 us
+// for its operands.
 typedef _Float16 v8h __attribute__((ext_vector_type(8)));
 typedef int v4i __attribute__((ext_vector_type(4)));
 
@@ -874,10 +875,10 @@ struct Plan {
   int nt, mt;          // linear_rows_kernel: 16 nt outputs and 16 mt tokens a workgroup
 };
 
-// Times in microseconds of the ways to do a product, for the choice between them.  The constants are a fit to 4000 launches of all
-// kernels over 700 random shapes (1 to 60000 rows, widths of 64 to 11008, both types, every split below); the way they choose takes
-// 1.02 times the best one's time on average, 1.5 times at worst, and 0.3 us of the host's.  A second launch costs the caller's
-// thread as well.
+// Times in microseconds of the ways to do a product, for the choice between them.  The constants are a fit to launches of all
+// kernels over random shapes (1 to 60000 rows, widths of 64 to 11008, both types, every split below); over 597 others the way they
+// choose takes 1.03 times the fastest one's time on average, 1.41 times at worst (profiles/linear_plan_shapes.txt), and 0.3 us of the
+// host's.  A second launch costs the caller's thread as well.
 constexpr double kLaunch = 2.5;
 // Two resources used beside each other: little more than the longer time.
 double beside(double a, double b) { return sqrt(sqrt(a * a * a * a + b * b * b * b)); }
@@ -977,7 +978,7 @@ double direct_time(int bm, int bn, hot_type type, int64_t L, int64_t O, int64_t 
   const int64_t count = p->tiles_m * p->tiles_n;
   if (count > kMaxLaunch / 256) return 1e30;
   p->whole = count;
-  // loads that begin at odd multiples of two bytes: the stages' share, a workgroup's by itself, what is moved (a fit to 260 shapes)
+  // loads that begin at odd multiples of two bytes: the stages' share, a workgroup's by itself, what is moved (fitted apart)
   const bool unaligned = !f32 && I % 2;
   const double odd = !unaligned ? 1.0 : bm == 64 ? 2.2 : 2.8, alone = unaligned ? 1.6 : 1.0, bytes_odd = unaligned ? 2.0 : 1.0;
   const double moved = bytes_odd * (((double)L + O) * bytes + (double)L * O * 4) / (f32 ? 49e6 : 15e6);
