@@ -65,12 +65,13 @@ def product64(x, w):
     return (x @ w.t().contiguous()).cpu(), (x.abs() @ w.abs().t().contiguous()).cpu()
 
 
-def held_to(y, z, size, I, what):
+def held_to(y, z, size, I, what, units=26):
     """The product's error for terms of random signs, in units of 2^-24 |x|.|w|: operands to 22 bits and a product left out, each 2^-22
     at most (12), what the checks of a row's range let through (4), and the additions: partial sums of k terms are about sqrt(k) of
-    them, so that I roundings of them add up to 1.2 standard deviations (10 for eight).  No result is nearer than half the smallest
-    number in each of its terms."""
-    close(y, z, 26 * ref.U * size + (2 * I + 1) * 2.0 ** -150, what)
+    them, so that I roundings of them add up to 1.2 standard deviations (10 for eight).  Of factors that are multiplied as they are: a
+    rounding of each product at most and the additions (12).  No result is nearer than half the smallest number in each of its
+    terms."""
+    close(y, z, units * ref.U * size + (2 * I + 1) * 2.0 ** -150, what)
 
 
 def call_linear(x, w, **kw):
@@ -118,7 +119,8 @@ def test_linear_of_whole_numbers_is_exact(t, L, O, I):
 @pytest.mark.parametrize("t,L,O,I", LINEAR_WAYS)
 def test_every_way_near_the_exact_one(t, L, O, I):
     x, w = rand((L, I), 1, t).cuda(), rand((O, I), 2, t, I ** -0.5).cuda()
-    held_to(call_linear(x, w), *product64(x, w), I, "y")
+    in_parts = t == F32 and hot.hot_debug_linear_plan(t, L, O, I)["way"] == "packed"
+    held_to(call_linear(x, w), *product64(x, w), I, "y", units=26 if in_parts else 12)
 
 
 @pytest.mark.parametrize("L,O,I,tile,cut", PACKED)
@@ -505,3 +507,48 @@ def test_packed_product_recorded_on_rows_of_other_ranges(L, O, I, tile, cut):
             held_to(y, *product64(x, w), I, f"scale {scale}")
         seen.append(y.clone())
     assert torch.equal(seen[0], seen[3]) and not torch.equal(seen[0], seen[1])
+
+
+@pytest.mark.parametrize("wide_x", [True, False])
+@pytest.mark.parametrize("L,O,I,tile,cut", PACKED)
+def test_packed_whole_numbers_far_below_their_rows_largest(L, O, I, tile, cut, wide_x):
+    """Twelve bits beside a column of 2^30, whose factor is zero: the low part of each is a subnormal 16-bit number, and all of them count.
+    Products and sums are whole and within 2^24 (twenty standard deviations), so there is one result."""
+    packed(L, O, I, tile, cut)
+    g = torch.Generator("cuda").manual_seed(I)
+    sign = lambda *s: torch.randint(0, 2, s, generator=g, device="cuda", dtype=F32) * 2 - 1          # noqa: E731
+    x, w = sign(L, I), sign(O, I)
+    far, near = (x, w) if wide_x else (w, x)
+    far *= 2049 + 2 * torch.randint(0, 1024, far.shape, generator=g, device="cuda", dtype=F32)
+    far[:, I // 3], near[:, I // 3] = 2.0 ** 30, 0.0
+    want = x.double() @ w.double().t().contiguous()
+    assert float(want.abs().max()) < 2 ** 24
+    assert torch.equal(call_linear(x, w).double(), want)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("kept", [False, True])
+@pytest.mark.parametrize("cols", [40, 100, 200, 500, 771, 1500, 4096, 5000, 11008])
+def test_layer_norm_rows_with_an_infinity_or_nan_stay_alone(cols, kept, dtype):
+    """Rows that share a workgroup with them give the bits that they give beside rows of zeros; theirs are NaN, and so are the sums over rows."""
+    rows, bad = 50, [2, 17, 49]
+    x, g = rand((rows, cols), cols, dtype), rand((rows, cols), 1, dtype)
+    x[2, 0], x[17, cols - 1], x[49, cols // 2] = NAN, INF, -INF
+    clean = x.clone()
+    clean[bad] = 0.0
+    outs = []
+    for t in (x.cuda(), clean.cuda()):
+        y, mean, rstd, gx = torch.empty_like(t), torch.empty(rows, device="cuda"), torch.empty(rows, device="cuda"), torch.empty_like(t)
+        gg, gb, buf = torch.empty(cols, device="cuda"), torch.empty(cols, device="cuda"), hot.alloc_checkpoint(rows, cols)
+        hot.hot_layer_norm_forward(t, None, None, 1e-5, y, mean, rstd, ckpt=buf)
+        hot.hot_layer_norm_backward(g.cuda(), None, mean, rstd, gx, gg, gb, hot.alloc_layer_norm_workspace(rows, cols),
+                                    h=None if kept else t, ckpt=buf if kept else None)
+        outs.append((y, mean, rstd, gx, hot.hot_checkpoint_read(buf, torch.empty_like(t)), gg, gb))
+    fine = torch.ones(rows, dtype=torch.bool, device="cuda")
+    fine[bad] = False
+    for a, b in zip(outs[0][:5], outs[1][:5]):
+        assert torch.equal(a[fine], b[fine]) and bool(torch.isfinite(b).all())
+    y, mean, rstd, gx, back, gg, gb = outs[0]
+    assert bool(y[bad].isnan().all()) and bool(gx[bad].isnan().all()) and not bool(torch.isfinite(mean[bad]).any())
+    assert int(back.isnan().sum()) == sum(min(32, cols - c // 32 * 32) for c in (0, cols - 1, cols // 2))
+    assert bool(gg.isnan().all()) and torch.equal(gb, outs[1][6])
