@@ -234,7 +234,8 @@ hot_status hot_lowpass_l1_rows(int32_t block, int32_t keep, int32_t* keep_idx);
  * only).  The conventions at the top of this file hold, and:
  *   - Tensors are [rows x cols], row-major and contiguous; a `hot_type` argument
  *     says what a tensor's elements are.  Sums, statistics and the values between a
- *     load and a store are fp32 (the layer norm's mean is summed in 64 bits); a bfloat16 result is rounded once, to nearest even.
+ *     load and a store are fp32 (the layer norm's mean is summed in 64 bits); a bfloat16
+ *     result is rounded once, to nearest even.
  *   - rows and cols are 1 or more; rows < 2^31, cols < 2^24 (16384 for the layer norm).
  *   - No output may overlap an input or another output (checked: HOT_ERR_ARG).
  *   - Kernels of one call exchange values only from one launch to the next, in

@@ -579,10 +579,13 @@ __global__ __launch_bounds__(64 * (BM / WM) * (BN / WN), 2) void linear_tile_ker
     const RowRanges<BM> of_x(g.ex + m0, (int)rows_x);
     const RowRanges<BN> of_w(g.ew + n0, (int)rows_w);
     scaled = -(int)tile_products<BM, BN, WM, WN, kSplitRows>(g.x, g.w, g.pitch, m0, n0, rows_x, rows_w, k_first, nk, smem, acc,
-                                                       [&] { return !wide_tile<BM, BN>(of_x, of_w); });
-    if (scaled) {}
-    else if (g.plain_pitch < 16) tile_short_rows<BM, BN, WM, WN>((const float*)g.x_plain, (const float*)g.w_plain, (int)g.plain_pitch / 4, g.out.L, g.out.O, m0, n0, acc);
-    else tile_products<BM, BN, WM, WN, kF32Wide>(g.x_plain, g.w_plain, g.plain_pitch, m0, n0, rows_x, rows_w, k_first, nk, smem, acc, always);
+                                                             [&] { return !wide_tile<BM, BN>(of_x, of_w); });
+    if (!scaled) {
+      if (g.plain_pitch >= 16)
+        tile_products<BM, BN, WM, WN, kF32Wide>(g.x_plain, g.w_plain, g.plain_pitch, m0, n0, rows_x, rows_w, k_first, nk, smem, acc, always);
+      else
+        tile_short_rows<BM, BN, WM, WN>((const float*)g.x_plain, (const float*)g.w_plain, (int)g.plain_pitch / 4, g.out.L, g.out.O, m0, n0, acc);
+    }
   } else {
     tile_products<BM, BN, WM, WN, MODE>(g.x, g.w, g.pitch, m0, n0, rows_x, rows_w, k_first, nk, smem, acc, always);
   }
@@ -699,15 +702,16 @@ __global__ __launch_bounds__(256) void linear_combine_kernel(const TileArgs g) {
 // Operand rows of the fp32 product: row r of the L + O rows of x and w, scaled by 2^(14 - e), e the exponent of its largest value,
 // as [16 high | 16 low] pieces; words[r]: e - 14 and the row's range, the share of its columns that are large (a scaled value of 2^5 or
 // more in x, 2^7 in w, of at most 2^15), rounded down, and of those whose parts are off by more than 2^-22 of the value, rounded up; a row
-// of zeros is held exactly, one with an infinity or a NaN not at all.  Padded columns are zero.  Bound by HBM: a row stays in the registers of the T
-// lanes that work on it, NV times eight columns each, or (NV = 0: rows beyond 16384) is read a second time, from the caches.
-// 8192 + 8192 rows of 8192 columns 177 us, 6.1 TB/s read and written; 250 when such rows were read twice.
+// of zeros is held exactly, one with an infinity or a NaN not at all.  Padded columns are zero.  Bound by HBM: a row stays in the
+// registers of the T lanes that work on it, NV times eight columns each, or (NV = 0: rows beyond 16384) is read a second time, from the
+// caches.  8192 + 8192 rows of 8192 columns 177 us, 6.1 TB/s read and written; 250 when such rows were read twice.
 __device__ __forceinline__ int row_exponent(uint32_t top) {   // of the largest magnitude's bits; subnormal ones too
   // infinities and NaNs stay what they are under any scale
   return top >= 0x7F800000u || top == 0 ? 0 : ilogbf(__uint_as_float(top));
 }
 // Called by all lanes of a wave; large, lossy: the wave's counts.
-__device__ __forceinline__ void store_parts(uint8_t* dst, int64_t c, bool store, const float (&v)[8], int e, float large_from, int& large, int& lossy) {
+__device__ __forceinline__ void store_parts(uint8_t* dst, int64_t c, bool store, const float (&v)[8], int e, float large_from, int& large,
+                                            int& lossy) {
   v8h hi, lo;
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
@@ -797,7 +801,8 @@ __global__ __launch_bounds__(256) void linear_split_kernel(const float* x, const
   if (lane == 0) {
     // shares of 1 / 1024, rounded down and up: the quotient is off by 2^-21 of itself at most
     const float unit = 1024.0f * __builtin_amdgcn_rcpf((float)I);
-    const uint32_t some = (uint32_t)((float)large * unit * (1.0f - 0x1p-20f)), off = min(1024u, (uint32_t)ceilf((float)lossy * unit * (1.0f + 0x1p-20f)));
+    const uint32_t some = (uint32_t)((float)large * unit * (1.0f - 0x1p-20f));
+    const uint32_t off = min(1024u, (uint32_t)ceilf((float)lossy * unit * (1.0f + 0x1p-20f)));
     words[r] = top >= 0x7F800000u ? row_word(0, 0, 1024) : top == 0 ? row_word(0, 1024, 0) : row_word(e - 14, some, off);
   }
 }
