@@ -1,0 +1,509 @@
+"""Performance cases of the operators of a fine-tuning step with frozen weights: what runs beside
+``hot_linear_backward_gx_cached`` when only low-rank adapters are trained, and when they are served.
+
+A case is one pass through one of them:
+
+- ``adapter``: y = base + scale (x.A^T).B^T, the rows of a ragged batch each with the adapter of their request
+  (``hot_adapter_forward``), and in training the gradients of x, A and B (``hot_adapter_backward``);
+- ``logprob``: log probabilities of given tokens with the entropy of their distributions, in serving with the likeliest
+  tokens beside them (``hot_token_logprobs``), in training with the gradient of the logits
+  (``hot_token_logprobs_backward``);
+- ``adamw``: one optimiser step over all tensors of a model at once, moments in fp32 or in 8 bits (``hot_adamw_step``;
+  with 8 bits the moments are read back too, ``hot_adamw_state_read``).
+
+Sizes are those of the benchmark's layers and of the tests, or lie between them; ``draw`` spreads over the same ranges.
+"""
+import math
+import zlib
+
+import torch
+
+own = False
+
+DEVICE = "cuda"
+TYPES = {"f32": torch.float32, "bf16": torch.bfloat16}
+SIZE = {"f32": 4, "bf16": 2}
+BLOCK, GROUP = 1024, 32          # elements of an 8-bit moment's block, and those that share an exponent
+LR, BETA1, BETA2, EPS, DECAY, STEP = 3e-4, 0.9, 0.999, 1e-8, 0.01, 37
+
+
+def _adapter(rows, cols, out, rank, x="bf16", segments=0, adapters=1, train=False, behind=0):
+    return dict(kind="adapter", rows=rows, cols=cols, out=out, rank=rank, x=x, segments=segments, adapters=adapters, train=train,
+                behind=behind)
+
+
+def _logprob(rows, vocab, x="bf16", top=0, train=False, masked=0):
+    return dict(kind="logprob", rows=rows, vocab=vocab, x=x, top=top, train=train, masked=masked)
+
+
+def _adamw(tensors, layers, width, hidden, rank=0, p="f32", g="f32", state="f32", copy=False):
+    return dict(kind="adamw", tensors=tensors, layers=layers, width=width, hidden=hidden, rank=rank, p=p, g=g, state=state, copy=copy)
+
+
+def listed():
+    return [
+        # One new token of one request: bound by launches and latencies.
+        dict(_adapter(1, 4096, 4096, 16), name="adapter_1_token"),
+        # A serving step: 64 requests with one new token each, 24 adapters, the LLM MLP's up-projection.
+        dict(_adapter(64, 4096, 11008, 16, segments=64, adapters=24), name="adapter_64_requests"),
+        # Prompts of 14 requests, ragged, beside padding rows; an odd rank and odd widths.
+        dict(_adapter(3330, 771, 2307, 12, segments=14, adapters=5, behind=97), name="adapter_ragged_prompts"),
+        # Fine-tuning ViT-B's qkv at batch 64 in fp32, one adapter.
+        dict(_adapter(64 * 197, 768, 2304, 16, x="f32", train=True), name="adapter_64_images_f32_trained"),
+        # Fine-tuning the LLM MLP's up-projection, 8 x 2048 tokens, a large rank.
+        dict(_adapter(16384, 4096, 11008, 64, train=True), name="adapter_16384_tokens_trained"),
+        # One new token: its log probability and the 20 likeliest ones.
+        dict(_logprob(1, 32000, top=20), name="logprob_1_token_top_20"),
+        # A batch of new tokens over a large vocabulary of odd size in fp32.
+        dict(_logprob(96, 50257, x="f32", top=8), name="logprob_96_tokens_f32_top_8"),
+        # A training step's loss: 8 x 2048 tokens, entropy and its gradient among the results, a padded vocabulary.
+        dict(_logprob(16384, 32000, train=True, masked=64), name="logprob_16384_tokens_trained"),
+        # The adapters of four blocks: sixteen small tensors, bound by the launch.
+        dict(_adamw("adapters", 4, 768, 0, rank=16), name="adamw_16_adapters"),
+        # All of a ViT-L in fp32: matrices, biases and norms.
+        dict(_adamw("blocks", 24, 1024, 4096), name="adamw_vitl_f32"),
+        # Four layers of the LLM MLP: bfloat16 gradients, fp32 weights with a bfloat16 copy for the products, 8-bit moments.
+        dict(_adamw("mlps", 4, 4096, 11008, g="bf16", state="8bit", copy=True), name="adamw_llm_mlp_8bit"),
+        # Odd sizes, bfloat16 weights alone, 8-bit moments.
+        dict(_adamw("blocks", 3, 771, 2307, p="bf16", g="bf16", state="8bit"), name="adamw_odd_bf16_8bit"),
+    ]
+
+
+def _sizes(case):
+    """(elements, weight decay) of each tensor of an optimiser step."""
+    w, h, r = case["width"], case["hidden"], case["rank"]
+    if case["tensors"] == "adapters":
+        layer = [(r * w, DECAY), (w * r, DECAY), (r * w, DECAY), (3 * w * r, DECAY)]
+    elif case["tensors"] == "mlps":
+        layer = [(h * w, DECAY), (w * h, DECAY)]
+    else:
+        layer = 4 * [(w * w, DECAY), (w, 0.0)] + [(h * w, DECAY), (h, 0.0), (w * h, DECAY), (w, 0.0)] + 4 * [(w, 0.0)]
+    return case["layers"] * layer
+
+
+def work(case):
+    """What each call of a pass reads and writes once, and its arithmetic."""
+    kind = case["kind"]
+    if kind == "adapter":
+        L, I, O, r, s, k = case["rows"] - case["behind"], case["cols"], case["out"], case["rank"], SIZE[case["x"]], case["adapters"]
+        k = min(k, case["segments"] or 1)
+        weights = k * r * (I + O)
+        moved = (L * I + weights + 2 * L * O) * s + 4 * L * r * case["train"]
+        if case["train"]:
+            moved += (L * O + weights + 3 * L * I) * s + 4 * L * r + 4 * weights
+        return {"bytes": moved, "flops": 2 * L * r * (I + O) * (3 if case["train"] else 1)}
+    if kind == "logprob":
+        L, V, s = case["rows"], case["vocab"], SIZE[case["x"]]
+        return {"bytes": L * V * s * (3 if case["train"] else 1) + L * (16 + 8 * case["top"]), "flops": L * V * (14 if case["train"] else 6)}
+    n = sum(size for size, _ in _sizes(case))
+    each = 2 * SIZE[case["p"]] + SIZE[case["g"]] + (16 if case["state"] == "f32" else 4 * 33 / 32 + 2 * 33 / 32 + 4) + 2 * case["copy"]
+    return {"bytes": n * each, "flops": 14 * n}
+
+
+def draw(rng):
+    limit = {k: max(work(c)["bytes"] for c in listed() if c["kind"] == k) for k in ("adapter", "logprob", "adamw")}
+    flops = max(work(c)["flops"] for c in listed() if c["kind"] == "adapter")
+
+    def spread(lo, hi):
+        return int(round(lo * (hi / lo) ** rng.random()))
+
+    def width():
+        n = spread(64, 11008)
+        return max(64, n // 64 * 64) if rng.random() < 0.6 else n
+
+    while True:
+        kind = rng.choice(["adapter", "adapter", "adapter", "logprob", "logprob", "adamw", "adamw"])
+        if kind == "adapter":
+            rows, train = spread(1, 16384), rng.random() < 0.5
+            segments = 0 if rng.random() < 0.3 else rng.choice([rows, spread(1, rows)]) if rows <= 512 else spread(1, min(rows, 256))
+            adapters = 1 if segments == 0 else spread(1, 32)
+            behind = rng.choice([0, rows // 7]) if 0 < segments < rows // 2 else 0
+            rank = rng.choice([4, 8, 8, 16, 16, 16, 32, 64, rng.randint(1, 64)])
+            case = _adapter(rows, width(), width(), rank, rng.choice(["f32", "bf16", "bf16"]), segments, adapters, train, behind)
+        elif kind == "logprob":
+            rows, vocab, train = spread(1, 16384), spread(1000, 131072), rng.random() < 0.5
+            vocab = max(1000, vocab // 64 * 64) if rng.random() < 0.5 else vocab
+            top = 0 if train else rng.choice([0, 1, 5, 20, 32]) if rows <= 512 else 0
+            case = _logprob(rows, vocab, rng.choice(["f32", "bf16", "bf16"]), top, train, rng.choice([0, 0, 64]))
+        else:
+            tensors, layers = rng.choice(["adapters", "blocks", "mlps"]), spread(1, 24)
+            w = spread(64, 4096)
+            w = max(64, w // 64 * 64) if rng.random() < 0.6 else w
+            p, state = rng.choice(["f32", "f32", "bf16"]), rng.choice(["f32", "8bit"])
+            case = _adamw(tensors, layers, w, 0 if tensors == "adapters" else spread(64, 11008), rng.choice([4, 8, 16, 64]) if tensors == "adapters" else 0,
+                          p, "bf16" if p == "bf16" else rng.choice(["f32", "bf16"]), state, p == "f32" and rng.random() < 0.4)
+        w = work(case)
+        if w["bytes"] <= limit[kind] and (kind != "adapter" or w["flops"] <= flops):
+            return case
+
+
+# ---- inputs ---------------------------------------------------------------------------------------------------------
+
+def _generator(seed, name, device=None):
+    g = torch.Generator(device=device or DEVICE)
+    g.manual_seed((int(seed) * 1_000_003 + zlib.crc32(name.encode())) & 0x7FFF_FFFF_FFFF)
+    return g
+
+
+def _normal(shape, std, seed, name, dtype=torch.float32):
+    t = torch.randn(shape, generator=_generator(seed, name), device=DEVICE, dtype=torch.float32)
+    return t.mul_(std).to(dtype)
+
+
+def _whole(low, high, shape, seed, name, dtype=torch.int64):
+    return torch.randint(low, high, shape, generator=_generator(seed, name), device=DEVICE, dtype=dtype)
+
+
+def _requests(case, seed):
+    """Where each request's rows begin, the last one's end behind them, and the adapter of each; one in nine has none."""
+    n, rows = case["segments"], case["rows"] - case["behind"]
+    g = _generator(seed, "requests", "cpu")
+    cuts = torch.arange(rows + 1) if n == rows else torch.cat([torch.tensor([0, rows]), torch.randint(0, rows + 1, (n - 1,), generator=g)]).sort()[0]
+    index = torch.randint(0, case["adapters"], (n,), generator=g)
+    index[torch.randint(0, 9, (n,), generator=g) == 0] = -1
+    return cuts.to(torch.int32).to(DEVICE), index.to(torch.int32).to(DEVICE)
+
+
+def _prepare_adapter(case, seed, s, out):
+    L, I, O, r, K, t = case["rows"], case["cols"], case["out"], case["rank"], case["adapters"], TYPES[case["x"]]
+    s["x"] = _normal((L, I), 1.0, seed, "x", t)
+    s["a"] = _normal((K, r, I), 1.0 / math.sqrt(I), seed, "a", t)
+    s["b"] = _normal((K, O, r), 0.05, seed, "b", t)
+    s["scale"] = _normal((K,), 0.5, seed, "scale").abs_().add_(1.0)
+    s["base"] = _normal((L, O), 1.0, seed, "base", t)
+    s["offsets"], s["index"] = _requests(case, seed) if case["segments"] else (None, None)
+    out("y", L, O, dtype=t)
+    if case["train"]:
+        s["g_y"] = _normal((L, O), 1e-3, seed, "g_y", t)
+        s["g_base"] = _normal((L, I), 1e-3, seed, "g_base", t)
+        out("u", L, r)
+        out("g_x", L, I, dtype=t)
+        out("g_a", K, r, I)
+        out("g_b", K, O, r)
+
+
+def _prepare_logprob(case, seed, s, out):
+    L, V, t = case["rows"], case["vocab"], TYPES[case["x"]]
+    z = _normal((L, V), 2.0, seed, "logits")
+    used = V - case["masked"]
+    likely = _whole(0, used, (L, 1), seed, "likely")
+    z.scatter_(1, likely, _normal((L, 1), 4.0, seed, "peak").add_(10.0))
+    z[:, used:] = -math.inf
+    s["logits"] = z.to(t)
+    other, kind = _whole(0, used, (L,), seed, "other"), _whole(0, 10, (L,), seed, "kind")
+    s["targets"] = torch.where(kind < 6, likely[:, 0], torch.where(kind < 9, other, -1))     # one row in ten is not scored
+    out("logp", L)
+    out("entropy", L)
+    if case["top"]:
+        out("top_logp", L, case["top"])
+        out("top_ids", L, case["top"], dtype=torch.int32)
+    if case["train"]:
+        out("stats", L, 2)
+        out("g_logits", L, V, dtype=t)
+        s["g_logp"] = _normal((L,), 1.0 / L, seed, "g_logp")
+        s["g_entropy"] = _normal((L,), 0.01 / L, seed, "g_entropy")
+
+
+def _blocks(n):
+    return -(-n // BLOCK)
+
+
+def _prepare_adamw(case, seed, s, out):
+    """Tensors one after the other in one allocation, each from a block's beginning on; zeros between them."""
+    sizes = _sizes(case)
+    first, blocks = [], 0
+    for n, _ in sizes:
+        first.append(blocks)
+        blocks += _blocks(n)
+    s["layout"] = [(f * BLOCK, n, decay) for f, (n, decay) in zip(first, sizes)]
+    N, tp, tg = blocks * BLOCK, TYPES[case["p"]], TYPES[case["g"]]
+    counts = torch.tensor([_blocks(n) for n, _ in sizes])
+    in_tensor = torch.arange(blocks) - torch.repeat_interleave(torch.tensor(first), counts)
+    left = (torch.repeat_interleave(torch.tensor([n for n, _ in sizes]), counts) - in_tensor * BLOCK).clamp(max=BLOCK).to(DEVICE)
+    held = torch.arange(BLOCK, device=DEVICE) < left[:, None]                                 # not padding
+    s["decay"] = torch.repeat_interleave(torch.tensor([d for _, d in sizes]), counts).to(DEVICE)[:, None]
+
+    def values(name, std, dtype=torch.float32):
+        return _normal((blocks, BLOCK), std, seed, name).mul_(held).to(dtype)
+
+    s["param"], s["grad"] = values("param", 0.02, tp), values("grad", 1e-3, tg)
+    s["param_out"] = torch.zeros(blocks, BLOCK, device=DEVICE, dtype=tp)
+    s["copy"] = torch.zeros(blocks, BLOCK, device=DEVICE, dtype=torch.bfloat16) if case["copy"] else None
+    if case["state"] == "f32":
+        s["m"], s["v"] = values("m", 3e-4), values("v", 1e-3).square_()
+        s["m_out"], s["v_out"] = torch.zeros_like(s["m"]), torch.zeros_like(s["v"])
+    else:                                                                                     # 1024 codes, 32 exponents
+        m = _normal((blocks, BLOCK), 45.0, seed, "m").round_().clamp_(-127, 127).mul_(held).to(torch.int8).view(torch.uint8)
+        v = _whole(150, 256, (blocks, BLOCK), seed, "v").mul_(held).to(torch.uint8)
+        e = [_whole(lo, lo + 4, (blocks, BLOCK // GROUP), seed, "e%d" % lo).to(torch.uint8) for lo in (112, 106)]
+        s["m"], s["v"] = torch.cat([m, e[0]], 1), torch.cat([v, e[1]], 1)
+        s["m_out"], s["v_out"] = torch.zeros_like(s["m"]), torch.zeros_like(s["v"])
+        out("m_read", N, dtype=torch.bfloat16)
+        out("v_read", N, dtype=torch.bfloat16)
+
+
+def prepare(case, seed):
+    """Inputs, and the output buffers that the caller owns: rows that belong to no request stay zero."""
+    s = {"case": case, "scratch": {}}
+
+    def out(name, *shape, dtype=torch.float32):
+        s[name] = torch.zeros(shape, device=DEVICE, dtype=dtype)
+
+    {"adapter": _prepare_adapter, "logprob": _prepare_logprob, "adamw": _prepare_adamw}[case["kind"]](case, seed, s, out)
+    return s
+
+
+# ---- the plain forms ------------------------------------------------------------------------------------------------
+
+def _plain_adapter(s):
+    case, t = s["case"], s["x"].dtype
+    L, I, O, r, K = case["rows"], case["cols"], case["out"], case["rank"], case["adapters"]
+    x, a, b = s["x"].float(), s["a"].float().view(K * r, I), s["b"].float().transpose(1, 2).reshape(K * r, O)
+    row = torch.arange(L, device=DEVICE)
+    if s["offsets"] is None:
+        inside, k = row >= 0, torch.zeros_like(row)
+    else:
+        inside = row < s["offsets"][-1]
+        at = torch.searchsorted(s["offsets"], row.to(torch.int32), right=True).clamp(max=case["segments"]) - 1
+        k = torch.where(inside, s["index"][at], -1)
+    mine = (k[:, None] == torch.arange(K, device=DEVICE))                     # [L, K]
+    scaled = (mine * s["scale"])[:, :, None]
+    u = (x @ a.t()).view(L, K, r) * mine[:, :, None]                          # zero but for the row's own adapter
+    y = s["base"].float() + (u * scaled).view(L, K * r) @ b
+    result = {"y": torch.where(inside[:, None], y, 0.0).to(t)}
+    if case["train"]:
+        g_y, x = s["g_y"].float() * inside[:, None], x * inside[:, None]
+        g_u = ((g_y @ b.t()).view(L, K, r) * scaled).view(L, K * r)
+        g_x = s["g_base"].float() + g_u @ a
+        result["u"] = u.sum(1)
+        result["g_x"] = torch.where(inside[:, None], g_x, 0.0).to(t)
+        result["g_a"] = (g_u.t() @ x).view(K, r, I)
+        result["g_b"] = ((u * scaled).view(L, K * r).t() @ g_y).view(K, r, O).transpose(1, 2).contiguous()
+    return result
+
+
+def _plain_logprob(s):
+    case, z, target = s["case"], s["logits"].float(), s["targets"]
+    top = z.amax(1, keepdim=True)
+    d = z - top
+    e = torch.exp(d)
+    d = torch.where(e > 0, d, 0.0)                     # a masked token adds nothing
+    total = e.sum(1, keepdim=True)
+    log_total = torch.log(total)
+    scored = target >= 0
+    at = target.clamp(min=0)[:, None]
+    logp = torch.where(scored, (z.gather(1, at) - top - log_total)[:, 0], 0.0)
+    entropy = log_total - (e * d).sum(1, keepdim=True) / total
+    result = {"logp": logp, "entropy": entropy[:, 0]}
+    if case["top"]:
+        value, ids = torch.sort(z, dim=1, descending=True, stable=True)
+        result["top_logp"] = value[:, :case["top"]] - top - log_total
+        result["top_ids"] = ids[:, :case["top"]].to(torch.int32)
+    if case["train"]:
+        p = e / total
+        g_logp = torch.where(scored, s["g_logp"], 0.0)[:, None]
+        g = p * (-g_logp - s["g_entropy"][:, None] * (d - log_total + entropy))
+        g.scatter_add_(1, at, g_logp)
+        result["stats"] = torch.cat([top, log_total], 1)
+        result["g_logits"] = g.to(s["logits"].dtype)
+    return result
+
+
+def _decoded(s, name):
+    """fp32 values of an 8-bit moment: m is a signed code times 2^(e - 133); v is 0, or 1.fff x 2^(x + e - 158) with the code's five upper
+    bits x and its three lower ones f (e: the group's byte)."""
+    codes, e = s[name][:, :BLOCK], s[name][:, BLOCK:].to(torch.int32).repeat_interleave(GROUP, dim=1)
+    if name == "m":
+        return codes.view(torch.int8).float() * ((e - 6) << 23).view(torch.float32)
+    bits = (codes.to(torch.int32) + (e - 31) * 8) << 20
+    return torch.where(codes > 0, bits.view(torch.float32), 0.0)
+
+
+def _held_m(t):
+    """m as 8 bits hold it: steps of the smallest power of two that leaves the group's largest within 127 of them; rounded up where the
+    fraction is more than the low 11 bits of the number of steps are of 2^11."""
+    t = t.view(-1, GROUP)
+    e = ((t.abs().amax(1, keepdim=True).view(torch.int32) + 0x10000) >> 23).clamp(8, 254)
+    steps = t * ((260 - e) << 23).view(torch.float32)
+    low = torch.floor(steps)
+    up = (steps - low) > (steps.view(torch.int32) & 0x7FF).float() / 2048
+    return ((low + up).clamp(-127, 127) * ((e - 6) << 23).view(torch.float32)).view(-1, BLOCK)
+
+
+def _held_v(t):
+    """v as 8 bits hold it: three bits behind the leading one, rounded up where the rest is more than the low 11 bits are of 2^11; 2^-31 of
+    the group's largest power of two, and the next of the 8 values there, is the least but zero."""
+    bits = t.view(-1, GROUP).view(torch.int32)
+    kept = (bits >> 20) + ((bits & 0xFFFFF) > ((bits & 0x7FF) << 9))
+    e = (kept >> 3).amax(1, keepdim=True).clamp(32, 254)
+    code = torch.where(bits == 0, 0, (kept - (e - 31) * 8).clamp(1, 255))
+    held = ((code + (e - 31) * 8) << 20).view(torch.float32)
+    return torch.where(code > 0, held, 0.0).view(-1, BLOCK)
+
+
+def _plain_adamw(s):
+    case, eight = s["case"], s["case"]["state"] == "8bit"
+    p, g = s["param"].float(), s["grad"].float()
+    m, v = (_decoded(s, "m"), _decoded(s, "v")) if eight else (s["m"], s["v"])
+    m = m * BETA1 + g * (1 - BETA1)
+    v = v * BETA2 + (g * (1 - BETA2)) * g
+    move = m / (torch.sqrt(v) / math.sqrt(1 - BETA2 ** STEP) + EPS)
+    p = p - (p * (s["decay"] * LR) + move * (LR / (1 - BETA1 ** STEP)))
+    result = {"param": p.to(s["param"].dtype)}
+    if case["copy"]:
+        result["copy"] = p.to(torch.bfloat16)
+    if eight:
+        result["m"], result["v"] = _held_m(m).view(-1).to(torch.bfloat16), _held_v(v).view(-1).to(torch.bfloat16)
+    else:
+        result["m"], result["v"] = m, v
+    return result
+
+
+# ---- the framework's calls ------------------------------------------------------------------------------------------
+
+def _kernels(s):
+    import paper_2503_21261_amd as hot
+
+    case, keep = s["case"], s["scratch"]
+
+    def scratch(name, make):     # what a user's program allocates once for its shapes
+        if name not in keep:
+            keep[name] = make()
+        return keep[name]
+
+    if case["kind"] == "adapter":
+        more = dict(scale=s["scale"], offsets=s["offsets"], index=s["index"])
+        ws = scratch("ws", lambda: hot.alloc_adapter_workspace(s["x"], s["a"], s["b"], segments=case["segments"], backward=case["train"]))
+        hot.hot_adapter_forward(s["x"], s["a"], s["b"], s["y"], ws, base=s["base"], u=s.get("u"), **more)
+        if not case["train"]:
+            return {"y": s["y"]}
+        hot.hot_adapter_backward(s["g_y"], s["x"], s["u"], s["a"], s["b"], ws, g_base=s["g_base"], g_x=s["g_x"], g_a=s["g_a"],
+                                 g_b=s["g_b"], **more)
+        return {k: s[k] for k in ("y", "u", "g_x", "g_a", "g_b")}
+    if case["kind"] == "logprob":
+        ws = scratch("ws", lambda: hot.alloc_logprobs_workspace(s["logits"], case["top"]))
+        hot.hot_token_logprobs(s["logits"], s["targets"], s["logp"], ws, entropy=s["entropy"], stats=s.get("stats"),
+                               top_logp=s.get("top_logp"), top_ids=s.get("top_ids"))
+        names = ["logp", "entropy"] + (["top_logp", "top_ids"] if case["top"] else [])
+        if case["train"]:
+            hot.hot_token_logprobs_backward(s["logits"], s["targets"], s["stats"], s["g_logits"], g_logp=s["g_logp"],
+                                            entropy=s["entropy"], g_entropy=s["g_entropy"])
+            names += ["stats", "g_logits"]
+        return {k: s[k] for k in names}
+    eight = case["state"] == "8bit"
+
+    def table():
+        def part(name, first, n):
+            if s[name] is None:
+                return None
+            if eight and name[:2] in ("m", "v", "m_", "v_"):
+                return s[name].view(-1)[first // BLOCK * (BLOCK + GROUP):][:_blocks(n) * (BLOCK + GROUP)]
+            return s[name].view(-1)[first:first + n]
+
+        return hot.AdamWTensors([dict(weight_decay=decay, **{k: part(k, first, n) for k in (
+            "param", "grad", "m", "v", "param_out", "m_out", "v_out", "copy")}) for first, n, decay in s["layout"]], state=case["state"])
+
+    hot.hot_adamw_step(scratch("table", table), lr=LR, beta1=BETA1, beta2=BETA2, eps=EPS, step=STEP)
+    result = {"param": s["param_out"], "m": s["m_out"], "v": s["v_out"]}
+    if eight:
+        result["m"] = hot.hot_adamw_state_read(s["m_out"].view(-1), "m", s["m_read"])
+        result["v"] = hot.hot_adamw_state_read(s["v_out"].view(-1), "v", s["v_read"])
+    if case["copy"]:
+        result["copy"] = s["copy"]
+    return result
+
+
+def run(state):
+    if own:
+        return _kernels(state)
+    return {"adapter": _plain_adapter, "logprob": _plain_logprob, "adamw": _plain_adamw}[state["case"]["kind"]](state)
+
+
+# ---- 64 bits --------------------------------------------------------------------------------------------------------
+
+def _exact_adapter(case, s):
+    L, K = case["rows"], case["adapters"]
+    x, y = s["x"].double(), s["base"].double()
+    last = L if s["offsets"] is None else int(s["offsets"][-1])
+    owner = [0] * L if s["offsets"] is None else [-1] * L
+    if s["offsets"] is not None:
+        cuts = s["offsets"].tolist()
+        for i, k in enumerate(s["index"].tolist()):
+            owner[cuts[i]:cuts[i + 1]] = [k] * (cuts[i + 1] - cuts[i])
+    owner = torch.tensor(owner, device=DEVICE)
+    y[last:] = 0
+    r = {"y": y}
+    if case["train"]:
+        g_y, g_x = s["g_y"].double(), s["g_base"].double()
+        g_x[last:] = 0
+        r.update(u=torch.zeros_like(s["u"], dtype=torch.float64), g_x=g_x, g_a=torch.zeros_like(s["g_a"], dtype=torch.float64),
+                 g_b=torch.zeros_like(s["g_b"], dtype=torch.float64))
+    for k in range(K):
+        rows = torch.nonzero(owner == k)[:, 0]
+        a, b, c = s["a"][k].double(), s["b"][k].double(), float(s["scale"][k])
+        u = torch.matmul(x[rows], a.t().contiguous())
+        y[rows] += c * torch.matmul(u, b.t().contiguous())
+        if case["train"]:
+            g = g_y[rows]
+            g_u = c * torch.matmul(g, b)
+            g_x[rows] += torch.matmul(g_u, a)
+            r["u"][rows] = u
+            r["g_a"][k] = torch.matmul(g_u.t().contiguous(), x[rows])
+            r["g_b"][k] = c * torch.matmul(g.t().contiguous(), u)
+    return r
+
+
+def _exact_logprob(case, s):
+    """Row by row in parts, from log p = log_softmax and entropy = -sum p log p."""
+    parts = []
+    for first in range(0, case["rows"], 1024):
+        z = s["logits"][first:first + 1024].double()
+        t = s["targets"][first:first + 1024]
+        lp = z - torch.logsumexp(z, 1, keepdim=True)
+        p = torch.exp(lp)
+        plp = torch.special.entr(p).neg()                                      # p log p, 0 at 0
+        H = -plp.sum(1)
+        hit = t >= 0
+        rows = torch.nonzero(hit)[:, 0]
+        logp = torch.zeros(len(t), dtype=torch.float64, device=DEVICE)
+        logp[rows] = lp[rows, t[rows]]
+        r = {"logp": logp, "entropy": H}
+        if case["top"]:
+            key = torch.argsort(-z, dim=1, stable=True)[:, :case["top"]]
+            r["top_logp"], r["top_ids"] = lp.gather(1, key), key.to(torch.int32)
+        if case["train"]:
+            g_l = s["g_logp"][first:first + 1024].double() * hit
+            g_e = s["g_entropy"][first:first + 1024].double()
+            g = -p * g_l[:, None] - g_e[:, None] * (plp + p * H[:, None])
+            g[rows, t[rows]] += g_l[rows]
+            top = z.max(1).values
+            r["stats"], r["g_logits"] = torch.stack([top, torch.logsumexp(z - top[:, None], 1)], 1), g
+        parts.append(r)
+    return {k: torch.cat([q[k] for q in parts]) for k in parts[0]}
+
+
+def _exact_adamw(case, s):
+    """The weights alone where the moments are held in 8 bits: which way their rounding goes is up to bits that 64 have otherwise."""
+    g = s["grad"].double()
+    if case["state"] == "f32":
+        m, v = s["m"].double(), s["v"].double()
+    else:
+        e = {k: s[k][:, BLOCK:].double().repeat_interleave(GROUP, dim=1) for k in "mv"}
+        code = s["m"][:, :BLOCK].double()
+        m = torch.where(code > 127, code - 256, code) * torch.exp2(e["m"] - 133)
+        code = s["v"][:, :BLOCK].long()
+        v = torch.where(code > 0, (8 + code % 8).double() / 8 * torch.exp2(code.div(8, rounding_mode="floor").double() + e["v"] - 158), 0.0)
+    m = torch.lerp(g, m, BETA1)
+    v = torch.lerp(g * g, v, BETA2)
+    p = s["param"].double()
+    step = (m / (1 - BETA1 ** STEP)) / (torch.sqrt(v / (1 - BETA2 ** STEP)) + EPS)
+    p = p - LR * (s["decay"].double() * p + step)
+    r = {"param": p, "m": m, "v": v} if case["state"] == "f32" else {"param": p, "m": None, "v": None}
+    if case["copy"]:
+        r["copy"] = p
+    return r
+
+
+def exact(case, seed):
+    s = prepare(case, seed)
+    return {"adapter": _exact_adapter, "logprob": _exact_logprob, "adamw": _exact_adamw}[case["kind"]](case, s)
