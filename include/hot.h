@@ -337,6 +337,140 @@ hot_status hot_linear_forward(const void* x, const void* w, hot_type type, const
                               int64_t L, int64_t O, int64_t I, hot_act_fn fn, void* y, hot_type y_type, void* ckpt,
                               void* ws, size_t ws_bytes, void* stream);
 
+/* ---- the operators of a fine-tuning step -----------------------------------------
+ *
+ * With frozen weights (Sec. 5.3) a step runs hot_linear_forward and
+ * hot_linear_backward_gx_cached for the weights themselves; these are what it trains and ends with:
+ * low-rank adapters, the log probabilities of the tokens, the optimiser.  The first two serve
+ * requests as well.  The conventions of the operators around the linear backward hold; where a
+ * call allows an output on an input, it says so.
+ */
+
+/*
+ * Low-rank adapters beside a shared projection, each row l with the adapter k of its request:
+ *   u = x A_k^T,  y = base + scale_k u B_k^T.
+ * x: [L x I], a: [adapters x rank x I], b: [adapters x O x rank], base: [L x O] or NULL (zeros), y: [L x O],
+ * all of `type`; base may be y.  scale: device fp32 [adapters] or NULL (1).  u: fp32 [L x rank] (out), for the
+ * backward call, or NULL.
+ * offsets: device int32 [segments + 1], ascending, and index: device int32 [segments]: rows
+ * offsets[s] .. offsets[s + 1] - 1 (none, one or many) have adapter index[s]; several segments may have the
+ * same.  An index outside [0, adapters) is no adapter: y = base, u = 0.  Rows in front of the first segment
+ * and behind the last one are left as they were, in y and in u.  offsets and index NULL (segments 0): all rows have
+ * adapter 0.  Both are read by the kernels, so that a recorded call follows what they hold at each replay;
+ * offsets that do not ascend or leave [0, L] give undefined results within the buffers.
+ * 1 <= rank <= 128 (adapters of lower rank beside it: zeros in a and b), L < 2^30, segments <= 2^24,
+ * adapters <= 65536, adapters * (O + I) < 2^28.
+ * Products and sums are fp32; bfloat16 operands are exact, u enters the second product with 16 bits or more.
+ * ws: at least hot_adapter_forward_workspace_bytes() bytes of scratch, 256-byte aligned.
+ */
+size_t hot_adapter_forward_workspace_bytes(hot_type type, int64_t L, int64_t O, int64_t I, int64_t rank, int64_t adapters,
+                                           int64_t segments);
+hot_status hot_adapter_forward(const void* x, const void* a, const void* b, hot_type type, const float* scale,
+                               const int32_t* offsets, const int32_t* index, int64_t segments, int64_t adapters, int64_t L, int64_t O,
+                               int64_t I, int64_t rank, const void* base, void* y, float* u, void* ws, size_t ws_bytes,
+                               void* stream);
+
+/*
+ * Gradients of the adapters: with g_u = scale_k g_y B_k,
+ *   g_x = g_base + g_u A_k,  g_A_k = sum of g_u^T x,  g_B_k = scale_k sum of g_y^T u  over the rows of adapter k.
+ * g_y: [L x O], x: [L x I], g_base: [L x I] or NULL (the gradient that reaches x past the adapters,
+ * hot_linear_backward_gx_cached's), g_x: [L x I] (out) or NULL, all of `type`; g_base may be g_x.  u: what the
+ * forward call wrote.  g_a, g_b: fp32, of the shapes of a and b (out), both or neither, written whole: zeros for an
+ * adapter that has no rows.  g_x, or g_a and g_b, must be given; x and u are needed for g_a and g_b, a for
+ * g_x.  Rows without an adapter have g_x = g_base; g_x's rows outside the segments are left as they were.
+ * ws: at least hot_adapter_backward_workspace_bytes() bytes of scratch, 256-byte aligned; nothing in it is kept between calls.
+ */
+size_t hot_adapter_backward_workspace_bytes(hot_type type, int64_t L, int64_t O, int64_t I, int64_t rank, int64_t adapters,
+                                            int64_t segments);
+hot_status hot_adapter_backward(const void* g_y, const void* x, const float* u, const void* a, const void* b, hot_type type,
+                                const float* scale, const int32_t* offsets, const int32_t* index, int64_t segments,
+                                int64_t adapters, int64_t L, int64_t O, int64_t I, int64_t rank, const void* g_base, void* g_x,
+                                float* g_a, float* g_b, void* ws, size_t ws_bytes, void* stream);
+
+/*
+ * Log probabilities of given tokens, row by row over [rows x vocab] logits z:
+ *   m = max z, log S = log sum exp(z - m), log p = z - m - log S, logp = log p[target],
+ *   entropy = -sum p log p (0 log 0 is 0).
+ * targets: device int64 [rows], with logp: fp32 [rows] (out), both or neither; a target outside [0, vocab) is not
+ * scored, its logp is 0.  entropy: fp32 [rows] (out) or NULL.  stats: fp32 [rows x 2] (out), m and log S,
+ * for the backward call, or NULL.  top_logp: fp32 and top_ids: int32 [rows x top] (out), the log probabilities and
+ * numbers of the `top` likeliest tokens in order, among equals the lower number first; top <= HOT_MAX_TOP, top <= vocab,
+ * 0 and NULLs for none.  One output at least must be wanted.
+ * A logit of -inf is a token that cannot come.  A row that holds nothing else has m = -inf, log S = 0, entropy 0, and
+ * log p = -inf for every token.  A NaN or +inf makes all of its row's log probabilities and its entropy NaN; NaNs come first
+ * among the likeliest.  vocab < 2^24.
+ * ws: at least hot_token_logprobs_workspace_bytes() bytes of scratch, 256-byte aligned (where that is 0, ws may be
+ * NULL; fewer rows may need more: a workspace for several sizes is as large as the largest of theirs).
+ */
+#define HOT_MAX_TOP 32
+size_t hot_token_logprobs_workspace_bytes(hot_type type, int64_t rows, int64_t vocab, int32_t top);
+hot_status hot_token_logprobs(const void* logits, hot_type type, int64_t rows, int64_t vocab, const int64_t* targets, float* logp,
+                              float* entropy, float* stats, int32_t top, float* top_logp, int32_t* top_ids, void* ws,
+                              size_t ws_bytes, void* stream);
+
+/*
+ * Gradient of the logits: g_z = g_logp (1[target] - p) - g_entropy p (log p + entropy).
+ * targets with g_logp (fp32 [rows]), both or neither; entropy (what the forward call wrote) with g_entropy (fp32 [rows]), both
+ * or neither; one of the pairs at least.  A row whose target is not scored has no part of g_logp; a row of -inf alone has
+ * gradient 0.  g_logits: [rows x vocab] of `type` (out); it may be logits.
+ */
+hot_status hot_token_logprobs_backward(const void* logits, hot_type type, int64_t rows, int64_t vocab, const int64_t* targets,
+                                       const float* stats, const float* entropy, const float* g_logp, const float* g_entropy,
+                                       void* g_logits, void* stream);
+
+/*
+ * One optimiser step (AdamW) over many tensors at once:
+ *   m' = beta1 m + (1 - beta1) g,  v' = beta2 v + (1 - beta2) g^2,
+ *   p' = p - lr (weight_decay p + (m' / c1) / (sqrt(v' / c2) + eps)),  c = 1 - beta^step.
+ * Each operation of m' and v' is one fp32 operation, in the order written ((1 - beta2) g times g).
+ *
+ * Moments are fp32 [n] (HOT_STATE_F32) or held in 8 bits (HOT_STATE_8BIT): blocks of 1024 elements, 1024 codes and then 32 bytes
+ * e, one for every 32 of them; a new state is all zeros.  m: a signed code times 2^(e - 133), as in the 8-bit
+ * checkpoint.  v: code 0 is zero, another one 1.fff x 2^(x + e - 158) with x its upper five bits and fff the lower three; e is
+ * that of the largest of the 32 (32 at least), and a v' above zero is never held as zero but as code 1 at least.  e = 255: NaN, for a
+ * group that held an infinity or a NaN.  Codes past n are zero.  The new weights come from m' and v' before they are
+ * rounded.
+ * rounding: nearest, or HOT_ROUND_PSEUDO_STOCHASTIC: up where the fraction is more than the low 11 bits are, read as a
+ * fraction, of what is rounded (m' in steps of its group; v' itself).  With rounding to the nearest a v that a step moves by less
+ * than half a code (all of them, for beta2 = 0.999) stays where it is.
+ */
+typedef enum { HOT_STATE_F32 = 0, HOT_STATE_8BIT = 1 } hot_state_form;
+typedef enum { HOT_MOMENT_M = 0, HOT_MOMENT_V = 1 } hot_moment;
+typedef struct {
+  const void* grad;        /* grad_type [n]                                                            */
+  void *param, *m, *v;     /* param_type [n]; moments                                                  */
+  void *param_out, *m_out, *v_out; /* results, apart from all inputs; NULL: in place                   */
+  void* copy;              /* bfloat16 [n] (out): the new weights rounded, for the products; HOT_F32 weights only; or NULL */
+  int64_t n;               /* 1 .. 2^40 - 1                                                            */
+  int32_t param_type, grad_type;   /* hot_type                                                         */
+  float weight_decay;
+  float lr_factor;         /* the tensor's learning rate in units of the call's                        */
+} hot_adamw_tensor;
+typedef struct {
+  double lr, beta1, beta2, eps;    /* 0 <= beta < 1, eps > 0                                            */
+  int64_t step;            /* 1 for the first one                                                       */
+  int32_t rounding;        /* hot_rounding, of 8-bit moments                                             */
+  int32_t reserved;
+  const float* dynamic;    /* NULL, or device fp32 [4]: lr, c1, c2 and a factor of every gradient (loss scale, clipping), read
+                              by the kernels in place of lr and step: for recorded calls                 */
+} hot_adamw_config;
+
+/* Bytes of one moment of n elements; 0 for a size out of range. */
+size_t hot_adamw_state_bytes(hot_state_form form, int64_t n);
+/* An 8-bit moment as values (exact in either type), and values (v: none below zero) as an 8-bit moment, rounded to nearest. */
+hot_status hot_adamw_state_read(const void* state, hot_moment moment, int64_t n, void* out, hot_type type, void* stream);
+hot_status hot_adamw_state_write(const void* x, hot_type type, hot_moment moment, int64_t n, void* state, void* stream);
+
+/* The tensors of a step, checked once and written into `table`, HOST memory of hot_adamw_table_bytes(count) bytes that the
+ * caller keeps (0: count below 1), aligned to 8.  No output of any tensor may lie on another one or on an input (HOT_ERR_ARG); moments
+ * of all tensors have the same form. */
+size_t hot_adamw_table_bytes(int32_t count);
+hot_status hot_adamw_table(const hot_adamw_tensor* tensors, int32_t count, hot_state_form state, void* table, size_t table_bytes);
+
+/* One step: a launch for every forty tensors.  A recorded call keeps the tensors, lr, step and the other numbers it was
+ * recorded with, but for what `dynamic` points to; the table is not read after the call returns. */
+hot_status hot_adamw_step(const void* table, const hot_adamw_config* cfg, void* stream);
+
 /* ---- parity views (not on the timed path): logical forms of packed data ---- */
 
 /* Compressed activation as row-major codes [L*r/n x I] and its scale [1].  With
@@ -408,9 +542,9 @@ hot_status hot_debug_set_gemm_mode(int mode);
 /* ---- stage timing for benchmarks (off by default) ---- */
 
 /* Kernel roles timed separately; hot_debug_stage_name() gives their names.  The first HOT_NUM_STAGES are those of the
- * linear backward, the others those of the operators around it. */
+ * linear backward, the next nine those of the operators around it; 24 is none, and those of a fine-tuning step follow. */
 #define HOT_NUM_STAGES 15
-#define HOT_NUM_STAGES_ALL 24
+#define HOT_NUM_STAGES_ALL 35
 
 /* From this call on, every kernel the library launches is bracketed by two HIP
  * events recorded on its stream.  Host-side state only; not thread-safe against

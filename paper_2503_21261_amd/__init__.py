@@ -37,13 +37,19 @@ EXPORTS = (
     "hot_activation_backward_workspace_bytes", "hot_activation_backward", "hot_layer_norm_forward",
     "hot_layer_norm_backward_workspace_bytes", "hot_layer_norm_backward", "hot_linear_forward_workspace_bytes",
     "hot_linear_forward",
+    "hot_adapter_forward_workspace_bytes", "hot_adapter_backward_workspace_bytes", "hot_adapter_forward", "hot_adapter_backward",
+    "hot_token_logprobs_workspace_bytes", "hot_token_logprobs", "hot_token_logprobs_backward",
+    "hot_adamw_state_bytes", "hot_adamw_state_read", "hot_adamw_state_write", "hot_adamw_table_bytes", "hot_adamw_table", "hot_adamw_step",
 )
-HOT_NUM_STAGES, HOT_NUM_STAGES_ALL = 15, 24
+HOT_NUM_STAGES, HOT_NUM_STAGES_ALL = 15, 35
 HOT_WS_PREFIX_BYTES = 24832
 HOT_F32, HOT_BF16 = 0, 1
 HOT_ACT_NONE, HOT_ACT_RELU, HOT_ACT_GELU, HOT_ACT_GELU_TANH, HOT_ACT_SILU = range(5)
 ACT_FNS = {"none": HOT_ACT_NONE, "relu": HOT_ACT_RELU, "gelu": HOT_ACT_GELU, "gelu_tanh": HOT_ACT_GELU_TANH,
            "silu": HOT_ACT_SILU}
+HOT_MAX_TOP, HOT_MAX_RANK = 32, 128
+HOT_STATE_F32, HOT_STATE_8BIT = 0, 1
+HOT_MOMENT_M, HOT_MOMENT_V = 0, 1
 
 
 class hot_config(C.Structure):
@@ -58,6 +64,16 @@ class hot_gemm_plan(C.Structure):
 
 class hot_linear_plan(C.Structure):
     _fields_ = [(f, C.c_int32) for f in ("way", "tile_rows", "tile_cols", "tiles", "whole", "slices", "masked", "streams")]
+
+
+class hot_adamw_tensor(C.Structure):
+    _fields_ = ([(f, C.c_void_p) for f in ("grad", "param", "m", "v", "param_out", "m_out", "v_out", "copy")] +
+                [("n", C.c_int64), ("param_type", C.c_int32), ("grad_type", C.c_int32), ("weight_decay", C.c_float), ("lr_factor", C.c_float)])
+
+
+class hot_adamw_config(C.Structure):
+    _fields_ = ([(f, C.c_double) for f in ("lr", "beta1", "beta2", "eps")] +
+                [("step", C.c_int64), ("rounding", C.c_int32), ("reserved", C.c_int32), ("dynamic", C.c_void_p)])
 
 
 class HotError(RuntimeError):
@@ -125,7 +141,17 @@ def lib() -> C.CDLL:
         l.hot_layer_norm_forward.argtypes = [vp, en, vp, vp, vp, C.c_float, i64, i64, vp, vp, en, vp, vp, vp, vp]
         l.hot_layer_norm_backward.argtypes = [vp, en, vp, vp, en, vp, vp, vp, vp, i64, i64, vp, vp, vp, vp, sz, vp]
         l.hot_linear_forward.argtypes = [vp, vp, en, vp, vp, i64, i64, i64, en, vp, en, vp, vp, sz, vp]
-        sizes = {"hot_checkpoint_bytes": [i64, i64], "hot_activation_backward_workspace_bytes": [i64, i64],
+        l.hot_adapter_forward.argtypes = [vp, vp, vp, en, vp, vp, vp] + [i64] * 6 + [vp, vp, vp, vp, sz, vp]
+        l.hot_adapter_backward.argtypes = [vp, vp, vp, vp, vp, en, vp, vp, vp] + [i64] * 6 + [vp, vp, vp, vp, vp, sz, vp]
+        l.hot_token_logprobs.argtypes = [vp, en, i64, i64, vp, vp, vp, vp, C.c_int32, vp, vp, vp, sz, vp]
+        l.hot_token_logprobs_backward.argtypes = [vp, en, i64, i64, vp, vp, vp, vp, vp, vp, vp]
+        l.hot_adamw_state_read.argtypes = [vp, en, i64, vp, en, vp]
+        l.hot_adamw_state_write.argtypes = [vp, en, en, i64, vp, vp]
+        l.hot_adamw_table.argtypes = [C.POINTER(hot_adamw_tensor), C.c_int32, en, vp, sz]
+        l.hot_adamw_step.argtypes = [vp, C.POINTER(hot_adamw_config), vp]
+        sizes = {"hot_adapter_forward_workspace_bytes": [en] + [i64] * 6, "hot_adapter_backward_workspace_bytes": [en] + [i64] * 6,
+                 "hot_token_logprobs_workspace_bytes": [en, i64, i64, C.c_int32], "hot_adamw_state_bytes": [en, i64],
+                 "hot_adamw_table_bytes": [C.c_int32], "hot_checkpoint_bytes": [i64, i64], "hot_activation_backward_workspace_bytes": [i64, i64],
                  "hot_layer_norm_backward_workspace_bytes": [i64, i64],
                  "hot_linear_forward_workspace_bytes": [en, i64, i64, i64]}
         for name, args in sizes.items():
@@ -558,6 +584,237 @@ def hot_linear_forward(x: torch.Tensor, w: torch.Tensor, y: torch.Tensor, ws: Op
     if st:
         _check(st, "hot_linear_forward")
     return y
+
+
+# ---- the operators of a fine-tuning step ------------------------------------------------------------------------------
+
+def _opt(name: str, t: Optional[torch.Tensor], dtype: torch.dtype, shape: Tuple[int, ...], device: int) -> Optional[int]:
+    return None if t is None else _expect(name, t, dtype, shape, device)
+
+
+def _scratch(ws: Optional[torch.Tensor], device: int) -> Tuple[Optional[int], int]:
+    return (None, 0) if ws is None else (_bytes("ws", ws, 0, device), ws.numel())
+
+
+def hot_adapter_forward_workspace_bytes(dtype: torch.dtype, L: int, O: int, I: int, rank: int, adapters: int, segments: int = 0) -> int:
+    return int(lib().hot_adapter_forward_workspace_bytes(_type_of("dtype", dtype), L, O, I, rank, adapters, segments))
+
+
+def hot_adapter_backward_workspace_bytes(dtype: torch.dtype, L: int, O: int, I: int, rank: int, adapters: int, segments: int = 0) -> int:
+    return int(lib().hot_adapter_backward_workspace_bytes(_type_of("dtype", dtype), L, O, I, rank, adapters, segments))
+
+
+def _adapter_shape(x: torch.Tensor, a: torch.Tensor, b: torch.Tensor) -> Tuple[int, int, int, int, int]:
+    if x.dim() != 2 or a.dim() != 3 or b.dim() != 3:
+        raise ValueError("expected x [L, I], a [adapters, rank, I] and b [adapters, O, rank]")
+    (L, I), (K, rank, _), O = x.shape, a.shape, b.shape[1]
+    return L, O, I, rank, K
+
+
+def alloc_adapter_workspace(x: torch.Tensor, a: torch.Tensor, b: torch.Tensor, segments: int = 0, backward: bool = True) -> torch.Tensor:
+    """Scratch of hot_adapter_forward and, with `backward`, of hot_adapter_backward for tensors of these shapes."""
+    L, O, I, rank, K = _adapter_shape(x, a, b)
+    sizes = (x.dtype, L, O, I, rank, K, segments)
+    n = hot_adapter_forward_workspace_bytes(*sizes)
+    if n and backward:
+        n = max(n, hot_adapter_backward_workspace_bytes(*sizes))
+    return _alloc(n, "hot_adapter_forward_workspace_bytes", x.device)
+
+
+def _batch(offsets: Optional[torch.Tensor], index: Optional[torch.Tensor], device: int):
+    if offsets is None and index is None:
+        return None, None, 0
+    if offsets is None or index is None or index.dim() != 1 or not index.shape[0]:
+        raise ValueError("offsets, index: expected both, of segments + 1 and segments int32 numbers, or neither")
+    n = index.shape[0]
+    return _expect("offsets", offsets, torch.int32, (n + 1,), device), _expect("index", index, torch.int32, (n,), device), n
+
+
+def hot_adapter_forward(x: torch.Tensor, a: torch.Tensor, b: torch.Tensor, y: torch.Tensor, ws: torch.Tensor,
+                        scale: Optional[torch.Tensor] = None, offsets: Optional[torch.Tensor] = None,
+                        index: Optional[torch.Tensor] = None, base: Optional[torch.Tensor] = None,
+                        u: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """y = base + scale_k (x.A_k^T).B_k^T with the adapter k of each row's request; u = x.A_k^T where a tensor is given; returns y."""
+    ty, dev = _typed("x", x), _current_device()
+    L, O, I, rank, K = _adapter_shape(x, a, b)
+    t, f32 = x.dtype, torch.float32
+    at, ix, n = _batch(offsets, index, dev)
+    st = lib().hot_adapter_forward(
+        _expect("x", x, t, (L, I), dev), _expect("a", a, t, (K, rank, I), dev), _expect("b", b, t, (K, O, rank), dev), ty,
+        _opt("scale", scale, f32, (K,), dev), at, ix, n, K, L, O, I, rank, _opt("base", base, t, (L, O), dev),
+        _expect("y", y, t, (L, O), dev), _opt("u", u, f32, (L, rank), dev), *_scratch(ws, dev), _stream_of(stream, dev))
+    if st:
+        _check(st, "hot_adapter_forward")
+    return y
+
+
+def hot_adapter_backward(g_y: torch.Tensor, x: torch.Tensor, u: Optional[torch.Tensor], a: torch.Tensor, b: torch.Tensor,
+                         ws: torch.Tensor, g_x: Optional[torch.Tensor] = None, g_a: Optional[torch.Tensor] = None,
+                         g_b: Optional[torch.Tensor] = None, scale: Optional[torch.Tensor] = None,
+                         offsets: Optional[torch.Tensor] = None, index: Optional[torch.Tensor] = None,
+                         g_base: Optional[torch.Tensor] = None, stream=None) -> None:
+    """g_x = g_base + g_u.A_k with g_u = scale_k g_y.B_k, and fp32 g_a and g_b of each adapter, of those that are given."""
+    ty, dev = _typed("x", x), _current_device()
+    L, O, I, rank, K = _adapter_shape(x, a, b)
+    t, f32 = x.dtype, torch.float32
+    at, ix, n = _batch(offsets, index, dev)
+    st = lib().hot_adapter_backward(
+        _expect("g_y", g_y, t, (L, O), dev), _expect("x", x, t, (L, I), dev), _opt("u", u, f32, (L, rank), dev),
+        _expect("a", a, t, (K, rank, I), dev), _expect("b", b, t, (K, O, rank), dev), ty, _opt("scale", scale, f32, (K,), dev), at, ix, n,
+        K, L, O, I, rank, _opt("g_base", g_base, t, (L, I), dev), _opt("g_x", g_x, t, (L, I), dev),
+        _opt("g_a", g_a, f32, (K, rank, I), dev), _opt("g_b", g_b, f32, (K, O, rank), dev), *_scratch(ws, dev), _stream_of(stream, dev))
+    if st:
+        _check(st, "hot_adapter_backward")
+
+
+def hot_token_logprobs_workspace_bytes(dtype: torch.dtype, rows: int, vocab: int, top: int = 0) -> int:
+    return int(lib().hot_token_logprobs_workspace_bytes(_type_of("dtype", dtype), rows, vocab, top))
+
+
+def alloc_logprobs_workspace(logits: torch.Tensor, top: int = 0) -> Optional[torch.Tensor]:
+    """Scratch of hot_token_logprobs for logits of this shape (fewer rows may need more); None where it needs none."""
+    rows, vocab = logits.shape
+    n = hot_token_logprobs_workspace_bytes(logits.dtype, rows, vocab, top)
+    if not (0 < rows < 1 << 31 and 0 < vocab < 1 << 24 and 0 <= top <= min(vocab, HOT_MAX_TOP)):
+        raise HotError(HOT_ERR_SHAPE, "hot_token_logprobs_workspace_bytes")
+    return torch.empty(n, dtype=torch.uint8, device=logits.device) if n else None
+
+
+def hot_token_logprobs(logits: torch.Tensor, targets: Optional[torch.Tensor], logp: Optional[torch.Tensor],
+                       ws: Optional[torch.Tensor] = None, entropy: Optional[torch.Tensor] = None,
+                       stats: Optional[torch.Tensor] = None, top_logp: Optional[torch.Tensor] = None,
+                       top_ids: Optional[torch.Tensor] = None, stream=None) -> Optional[torch.Tensor]:
+    """logp[row] = log softmax(logits[row])[targets[row]] (0 where the target is no token), and what else is given; returns logp."""
+    ty, dev = _typed("logits", logits), _current_device()
+    rows, vocab = shape = logits.shape
+    f32 = torch.float32
+    top = 0
+    if top_logp is not None or top_ids is not None:
+        if top_logp is None or top_ids is None or top_logp.dim() != 2:
+            raise ValueError("top_logp, top_ids: expected both, of shape [rows, top], or neither")
+        top = top_logp.shape[1]
+    st = lib().hot_token_logprobs(
+        _expect("logits", logits, logits.dtype, shape, dev), ty, rows, vocab, _opt("targets", targets, torch.int64, (rows,), dev),
+        _opt("logp", logp, f32, (rows,), dev), _opt("entropy", entropy, f32, (rows,), dev), _opt("stats", stats, f32, (rows, 2), dev), top,
+        _opt("top_logp", top_logp, f32, (rows, top), dev), _opt("top_ids", top_ids, torch.int32, (rows, top), dev),
+        *_scratch(ws, dev), _stream_of(stream, dev))
+    if st:
+        _check(st, "hot_token_logprobs")
+    return logp
+
+
+def hot_token_logprobs_backward(logits: torch.Tensor, targets: Optional[torch.Tensor], stats: torch.Tensor, g_logits: torch.Tensor,
+                                g_logp: Optional[torch.Tensor] = None, entropy: Optional[torch.Tensor] = None,
+                                g_entropy: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """Gradient of the logits (g_logits may be logits) from those of logp and of the entropy; returns g_logits."""
+    ty, dev = _typed("logits", logits), _current_device()
+    rows, vocab = shape = logits.shape
+    f32 = torch.float32
+    st = lib().hot_token_logprobs_backward(
+        _expect("logits", logits, logits.dtype, shape, dev), ty, rows, vocab, _opt("targets", targets, torch.int64, (rows,), dev),
+        _expect("stats", stats, f32, (rows, 2), dev), _opt("entropy", entropy, f32, (rows,), dev), _opt("g_logp", g_logp, f32, (rows,), dev),
+        _opt("g_entropy", g_entropy, f32, (rows,), dev), _expect("g_logits", g_logits, logits.dtype, shape, dev), _stream_of(stream, dev))
+    if st:
+        _check(st, "hot_token_logprobs_backward")
+    return g_logits
+
+
+_STATES = {"f32": HOT_STATE_F32, "8bit": HOT_STATE_8BIT}
+_MOMENTS = {"m": HOT_MOMENT_M, "v": HOT_MOMENT_V}
+
+
+def hot_adamw_state_bytes(state: str, n: int) -> int:
+    return int(lib().hot_adamw_state_bytes(_STATES[state], n))
+
+
+def alloc_adamw_state(state: str, n: int, device="cuda") -> torch.Tensor:
+    """One moment of n elements at the first step (all zeros): float32 [n], or the bytes of the 8-bit form."""
+    size = hot_adamw_state_bytes(state, n)
+    if size == 0:
+        raise HotError(HOT_ERR_SHAPE, "hot_adamw_state_bytes")
+    return torch.zeros(n, dtype=torch.float32, device=device) if state == "f32" else torch.zeros(size, dtype=torch.uint8, device=device)
+
+
+def _flat(name: str, t: torch.Tensor) -> int:
+    ty = _TYPES.get(t.dtype)
+    if ty is None or not t.is_cuda or not t.is_contiguous():
+        raise ValueError(f"{name}: expected a contiguous float32 or bfloat16 device tensor")
+    return ty
+
+
+def hot_adamw_state_read(buf: torch.Tensor, moment: str, x: torch.Tensor, stream=None) -> torch.Tensor:
+    """Fills x with the values that an 8-bit moment ("m" or "v") of as many elements holds; returns x."""
+    ty, dev, n = _flat("x", x), _current_device(), x.numel()
+    st = lib().hot_adamw_state_read(_bytes("buf", buf, hot_adamw_state_bytes("8bit", n), dev), _MOMENTS[moment], n,
+                                    _expect("x", x, x.dtype, x.shape, dev), ty, _stream_of(stream, dev))
+    if st:
+        _check(st, "hot_adamw_state_read")
+    return x
+
+
+def hot_adamw_state_write(x: torch.Tensor, moment: str, buf: torch.Tensor, stream=None) -> torch.Tensor:
+    """Stores x as an 8-bit moment, rounded to the nearest; returns buf."""
+    ty, dev, n = _flat("x", x), _current_device(), x.numel()
+    st = lib().hot_adamw_state_write(_expect("x", x, x.dtype, x.shape, dev), ty, _MOMENTS[moment], n,
+                                     _bytes("buf", buf, hot_adamw_state_bytes("8bit", n), dev), _stream_of(stream, dev))
+    if st:
+        _check(st, "hot_adamw_state_write")
+    return buf
+
+
+class AdamWTensors:
+    """The tensors of an optimiser step: a list of dicts with param, grad, m and v, and where wanted copy (bfloat16), param_out, m_out,
+    v_out (in place without), weight_decay and lr_factor.  Checked once, and held as long as this object lives."""
+
+    def __init__(self, tensors: Sequence[dict], state: str = "f32"):
+        form = _STATES[state]
+        self.tensors = [dict(t) for t in tensors]
+        self.device = -1
+        count = len(self.tensors)
+        entries = (hot_adamw_tensor * max(count, 1))()
+        for i, (t, e) in enumerate(zip(self.tensors, entries)):
+            p, g = t["param"], t["grad"]
+            e.param_type, e.grad_type, n, dev = _flat(f"param of tensor {i}", p), _flat(f"grad of tensor {i}", g), p.numel(), p.get_device()
+            if n < 1 or g.numel() != n:
+                raise ValueError(f"tensor {i}: expected as many gradients as weights, one at least")
+            if self.device not in (-1, dev):
+                raise ValueError(f"tensor {i}: on cuda:{dev}, others on cuda:{self.device}")
+            self.device = dev
+            e.n, e.weight_decay, e.lr_factor = n, t.get("weight_decay", 0.0), t.get("lr_factor", 1.0)
+            for name, dtype in (("param", p.dtype), ("grad", g.dtype), ("param_out", p.dtype), ("copy", torch.bfloat16)):
+                x = t.get(name)
+                if x is not None:
+                    if x.numel() != n:
+                        raise ValueError(f"{name} of tensor {i}: expected {n} elements")
+                    setattr(e, name, _expect(f"{name} of tensor {i}", x, dtype, x.shape, dev))
+            for name in ("m", "v", "m_out", "v_out"):
+                x = t.get(name)
+                if x is None:
+                    continue
+                if state == "8bit":
+                    setattr(e, name, _bytes(f"{name} of tensor {i}", x, hot_adamw_state_bytes(state, n), dev))
+                elif x.numel() != n:
+                    raise ValueError(f"{name} of tensor {i}: expected {n} elements")
+                else:
+                    setattr(e, name, _expect(f"{name} of tensor {i}", x, torch.float32, x.shape, dev))
+        self.state = state
+        size = int(lib().hot_adamw_table_bytes(count))
+        self.table = (C.c_uint64 * max((size + 7) // 8, 1))()
+        _check(lib().hot_adamw_table(entries, count, form, self.table, size), "hot_adamw_table")
+
+
+def hot_adamw_step(tensors: AdamWTensors, lr: float, beta1: float = 0.9, beta2: float = 0.999, eps: float = 1e-8, step: int = 1,
+                   rounding: int = HOT_ROUND_PSEUDO_STOCHASTIC, dynamic: Optional[torch.Tensor] = None, stream=None) -> None:
+    """One AdamW step over the tensors.  dynamic: float32 [4] on the device, lr, 1 - beta1^step, 1 - beta2^step and a factor of every
+    gradient, in place of lr and step (for recorded calls)."""
+    dev = _current_device()
+    if tensors.device != dev:
+        raise ValueError(f"tensors: expected on cuda:{dev}, the current device")
+    cfg = hot_adamw_config(float(lr), float(beta1), float(beta2), float(eps), int(step), int(rounding), 0,
+                           _opt("dynamic", dynamic, torch.float32, (4,), dev))
+    st = lib().hot_adamw_step(tensors.table, C.byref(cfg), _stream_of(stream, dev))
+    if st:
+        _check(st, "hot_adamw_step")
 
 
 def hot_debug_unpack_activation(cfg: Config, act_buf: torch.Tensor, L: int, I: int, stream=None):

@@ -13,7 +13,8 @@ CSRC = os.path.join(HERE, "csrc")
 OBJ = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libhot.so")
 SOURCES = ["api.hip", "row_quant.hip", "col_quant.hip", "gx_front.hip", "col_bf16.hip", "gy_fused.hip", "igemm.hip", "select.hip", "profile.hip", "probe.hip",
-           "api_block.hip", "pointwise.hip", "layer_norm.hip", "linear.hip"]
+           "api_block.hip", "pointwise.hip", "layer_norm.hip", "linear.hip",
+           "api_tune.hip", "adapter.hip", "logprob.hip", "adamw.hip"]
 
 # IEEE fp32 is part of the contract: the integer codes depend on every add, mul and
 # div rounding exactly once, so no contraction, no fast-math, correctly rounded

@@ -1,0 +1,228 @@
+// One optimiser step (AdamW) over many tensors: m' = b1 m + (1 - b1) g, v' = b2 v + (1 - b2) g^2,
+// p' = p - lr (decay p + (m' / c1) / (sqrt(v' / c2) + eps)), and the 8-bit form of the two moments.
+//
+// Bound by memory: an element is read and written once, 28 bytes with fp32 moments and parameters, 16.1 with 8-bit moments and
+// fp32 parameters and gradients.  One launch takes forty tensors: a lane finds its tensor from its workgroup's number, so that
+// small tensors (biases, norms) cost no launch of their own.
+#include "block_device.h"
+#include "tune_host.h"
+
+namespace hot {
+
+namespace {
+
+// ---- the 8-bit moments ----------------------------------------------------------------------------
+// m: the form of the 8-bit checkpoint, a signed code times a power-of-two step that 32 elements share.
+// v, which spans the squares of what m does: a code of five exponent and three mantissa bits under the largest exponent e of 32
+// elements: 0, or 1.fff x 2^(x - 31 + e - 127) with x the upper five bits.  All but the rounding is exact in both, and the
+// roundings' inputs are single fp32 operations, so codes have one value whatever computes them.
+// Rounding, as elsewhere in this library: to the nearest, or up where the fraction is more than the value's own low 11 bits
+// are of 2^11.  The latter is what a moment needs: with b2 = 0.999 a step moves v by 0.1 %, 1/60 to 1/120 of a code, and
+// rounding to the nearest would bring the same code back for ever.
+// A v that is not zero never becomes zero: the least code is held instead, so that 1 / sqrt(v) is not blown up.
+constexpr uint32_t kVMinExp = 32;   // keeps the least code a normal number
+
+template <bool NEAREST>
+__device__ __forceinline__ uint2 encode_m8(const float (&v)[8], float inverse) {
+  int c[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const float t = v[i] * inverse;
+    float q;
+    if constexpr (NEAREST) {
+      q = rintf(t);
+    } else {
+      q = floorf(t);
+      q += t - q > (float)(__float_as_uint(t) & 0x7FFu) * (1.0f / 2048.0f) ? 1.0f : 0.0f;
+    }
+    c[i] = (int)fminf(fmaxf(q, -127.0f), 127.0f);
+  }
+  return make_uint2(pack4_codes8(c[0], c[1], c[2], c[3]), pack4_codes8(c[4], c[5], c[6], c[7]));
+}
+
+// Upper bits of v after rounding: exponent and three bits of the mantissa.
+template <bool NEAREST>
+__device__ __forceinline__ uint32_t rounded_v(float v) {
+  const uint32_t b = __float_as_uint(v) & 0x7FFFFFFFu;   // -0 is 0; below zero is marked as NaN
+  if constexpr (NEAREST) return (b + 0x7FFFFu + (b >> 20 & 1u)) >> 20;
+  else return (b >> 20) + ((b & 0xFFFFFu) > (b & 0x7FFu) << 9 ? 1u : 0u);
+}
+
+// Codes of eight elements of a group, by the four lanes of the group together; e: the group's exponent byte.
+template <bool NEAREST>
+__device__ __forceinline__ uint2 store_v8(const float (&v)[8], uint32_t& e) {
+  uint32_t k[8], top = 0;
+  bool bad = false;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    k[i] = rounded_v<NEAREST>(v[i]);
+    top = max(top, k[i]);
+    bad |= !(v[i] >= 0.0f && v[i] <= 0x1.fffffep+127f);
+  }
+  top = quad_max(bad ? 0xFFFu << 3 : top);
+  e = min(max(top >> 3, kVMinExp), 254u);
+  const int least = (int)(e - 31u) * 8;
+  int c[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) c[i] = v[i] == 0.0f ? 0 : min(max((int)k[i] - least, 1), 255);
+  if (top >= 0xFFFu << 3) e = 255u;
+  return make_uint2(pack4_codes8(c[0], c[1], c[2], c[3]), pack4_codes8(c[4], c[5], c[6], c[7]));
+}
+__device__ __forceinline__ void decode_v8(uint2 codes, uint32_t e, float (&v)[8]) {
+  const uint32_t base = (e - 31u) * 8;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const uint32_t c = (i < 4 ? codes.x >> (8 * i) : codes.y >> (8 * i - 32)) & 255u;
+    v[i] = e == 255u ? __uint_as_float(0x7FC00000u) : c ? __uint_as_float((c + base) << 20) : 0.0f;
+  }
+}
+
+__device__ __forceinline__ int64_t whole_blocks(int64_t n) { return (n + kStateBlock - 1) & -(int64_t)kStateBlock; }
+__device__ __forceinline__ uint8_t* state_at(const void* s, int64_t i) {
+  return (uint8_t*)s + (i / kStateBlock) * kStateBlockBytes + (i & (kStateBlock - 1));
+}
+__device__ __forceinline__ uint8_t* exp_at(const void* s, int64_t i) {
+  return (uint8_t*)s + (i / kStateBlock) * kStateBlockBytes + kStateBlock + (i & (kStateBlock - 1)) / 32;
+}
+
+// ---- the step -------------------------------------------------------------------------------------
+struct Scalars {
+  float beta1, rest1, beta2, rest2, eps, step, root2, shrink, g_scale;
+};
+
+template <bool EIGHT, bool NEAREST, class TP, class TG>
+__device__ __forceinline__ void update8(const AdamWEntry& t, const Scalars& c, int64_t at) {
+  const int n = (int)min((int64_t)8, t.n - at);
+  if (EIGHT ? at >= whole_blocks(t.n) : n <= 0) return;   // 8 bits: all of the last block's codes are written
+  float p[8], g[8], m[8], v[8];
+  const Raw8<TP> rp = load8((const TP*)t.p + at, n);
+  const Raw8<TG> rg = load8((const TG*)t.g + at, n);
+  if constexpr (EIGHT) {
+    const uint2 cm = *(const uint2*)state_at(t.m, at), cv = *(const uint2*)state_at(t.v, at);
+    const uint32_t em = *exp_at(t.m, at), ev = *exp_at(t.v, at);
+    decode8(cm, ckpt_step(em), m);
+    decode_v8(cv, ev, v);
+    if (rarely(n < 8)) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        if (i >= n) m[i] = v[i] = 0.0f;
+    }
+  } else {
+    const Raw8<float> rm = load8((const float*)t.m + at, n), rv = load8((const float*)t.v + at, n);
+    widen(rm, m);
+    widen(rv, v);
+  }
+  widen(rp, p);
+  widen(rg, g);
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const float gi = g[i] * c.g_scale;
+    m[i] = m[i] * c.beta1 + gi * c.rest1;         // every operation rounded by itself: the codes of m' and v' rest on it
+    v[i] = v[i] * c.beta2 + gi * c.rest2 * gi;
+    const float move = m[i] / (sqrtf(v[i]) * c.root2 + c.eps);
+    p[i] = p[i] - (p[i] * c.shrink + move * c.step);
+  }
+  if constexpr (EIGHT) {
+    const uint32_t em = ckpt_exponent(quad_max(magnitude8(m)));
+    uint32_t ev;
+    const uint2 cm = encode_m8<NEAREST>(m, ckpt_inverse(em)), cv = store_v8<NEAREST>(v, ev);
+    *(uint2*)state_at(t.m_out, at) = cm;
+    *(uint2*)state_at(t.v_out, at) = cv;
+    if ((at & 31) == 0) {
+      *exp_at(t.m_out, at) = (uint8_t)em;
+      *exp_at(t.v_out, at) = (uint8_t)ev;
+    }
+  } else {
+    store8((float*)t.m_out + at, m, n);
+    store8((float*)t.v_out + at, v, n);
+  }
+  store8((TP*)t.p_out + at, p, n);
+  if (t.copy) store8((bf16*)t.copy + at, p, n);
+}
+
+template <bool EIGHT, bool NEAREST>
+__global__ __launch_bounds__(256) void adamw_kernel(const AdamWArgs a) {
+  uint32_t k = 0;
+#pragma unroll
+  for (int i = 1; i < kAdamWEntries; ++i) k += blockIdx.x >= a.block[i];
+  const AdamWEntry& t = a.e[k];
+  const int64_t at = (int64_t)(blockIdx.x - a.block[k]) * kAdamWChunk + (k == 0 ? a.first : 0) + threadIdx.x * 8;
+  const float* const dyn = a.s.dyn;
+  const float lr = (dyn ? dyn[0] : a.s.lr) * t.lr, corr1 = dyn ? dyn[1] : a.s.corr1, corr2 = dyn ? dyn[2] : a.s.corr2;
+  const Scalars c{a.s.beta1, a.s.rest1, a.s.beta2, a.s.rest2, a.s.eps, lr / corr1, 1.0f / sqrtf(corr2), t.decay * lr, dyn ? dyn[3] : 1.0f};
+  if (t.types & 1u) {
+    if (t.types & 2u) update8<EIGHT, NEAREST, bf16, bf16>(t, c, at);
+    else update8<EIGHT, NEAREST, bf16, float>(t, c, at);
+  } else {
+    if (t.types & 2u) update8<EIGHT, NEAREST, float, bf16>(t, c, at);
+    else update8<EIGHT, NEAREST, float, float>(t, c, at);
+  }
+}
+
+// ---- moments as values -----------------------------------------------------------------------------
+template <class T>
+__global__ __launch_bounds__(256) void state_read_kernel(const void* state, int second, int64_t first, int64_t n, T* out) {
+  const int64_t at = first + ((int64_t)blockIdx.x * 256 + threadIdx.x) * 8;
+  if (at >= n) return;
+  const uint2 c = *(const uint2*)state_at(state, at);
+  const uint32_t e = *exp_at(state, at);
+  float v[8];
+  if (second) decode_v8(c, e, v);
+  else decode8(c, ckpt_step(e), v);
+  store8(out + at, v, (int)min((int64_t)8, n - at));
+}
+
+template <class T>
+__global__ __launch_bounds__(256) void state_write_kernel(const T* x, int second, int64_t first, int64_t n, void* state) {
+  const int64_t at = first + ((int64_t)blockIdx.x * 256 + threadIdx.x) * 8;
+  if (at >= whole_blocks(n)) return;
+  float v[8];
+  load_values(x + at, (int)min((int64_t)8, n - at), v);
+  uint32_t e;
+  uint2 c;
+  if (second) {
+    c = store_v8<true>(v, e);
+  } else {
+    e = ckpt_exponent(quad_max(magnitude8(v)));
+    c = encode_m8<true>(v, ckpt_inverse(e));
+  }
+  *(uint2*)state_at(state, at) = c;
+  if ((at & 31) == 0) *exp_at(state, at) = (uint8_t)e;
+}
+
+}  // namespace
+
+hipError_t launch_adamw(const AdamWArgs& a, uint32_t blocks, bool eight, bool nearest, hipStream_t s) {
+  if (!eight) adamw_kernel<false, true><<<blocks, 256, 0, s>>>(a);
+  else if (nearest) adamw_kernel<true, true><<<blocks, 256, 0, s>>>(a);
+  else adamw_kernel<true, false><<<blocks, 256, 0, s>>>(a);
+  return hipGetLastError();
+}
+
+namespace {
+constexpr int64_t kStateRun = 1ll << 33;   // elements of one launch: 2^30 lanes
+}
+
+hipError_t launch_state_read(const void* state, bool second, int64_t n, void* out, hot_type type, hipStream_t s) {
+  for (int64_t first = 0; first < n; first += kStateRun) {
+    const int64_t last = first + kStateRun < n ? first + kStateRun : n;
+    const uint32_t blocks = (uint32_t)ceil_div(last - first, 2048);
+    if (type == HOT_BF16) state_read_kernel<<<blocks, 256, 0, s>>>(state, second, first, last, (bf16*)out);
+    else state_read_kernel<<<blocks, 256, 0, s>>>(state, second, first, last, (float*)out);
+    if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+  }
+  return hipSuccess;
+}
+
+hipError_t launch_state_write(const void* x, hot_type type, bool second, int64_t n, void* state, hipStream_t s) {
+  for (int64_t first = 0; first < n; first += kStateRun) {
+    const int64_t last = first + kStateRun < n ? first + kStateRun : n;
+    const uint32_t blocks = (uint32_t)ceil_div(last - first, 2048);
+    if (type == HOT_BF16) state_write_kernel<<<blocks, 256, 0, s>>>((const bf16*)x, second, first, last, state);
+    else state_write_kernel<<<blocks, 256, 0, s>>>((const float*)x, second, first, last, state);
+    if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+  }
+  return hipSuccess;
+}
+
+}  // namespace hot

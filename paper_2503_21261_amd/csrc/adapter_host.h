@@ -1,0 +1,86 @@
+// Host-side declarations of the low-rank adapters: layouts and launchers.
+#pragma once
+#include "hot_host.h"
+
+namespace hot {
+
+constexpr int64_t kMaxRank = 128;
+constexpr int kMaxSlices = 32;
+
+// Rows of a batch and the adapters of their requests: rows offsets[s] .. offsets[s + 1] - 1 belong to adapter index[s].
+struct AdapterBatch {
+  const int32_t *offsets, *index;   // device; null: all rows belong to adapter 0
+  int segments, adapters;
+  int64_t L;
+};
+
+// out[l][j] = sum over k of q[l][k] w[adapter(l)][j][k], in `slices` slices of the sum, each [L][pitch] fp32.
+struct AdapterShrink {
+  AdapterBatch b;
+  const void *q, *w;
+  float* out;
+  int64_t K, w_pitch, w_stride;     // w: elements from j to j + 1 and from adapter to adapter
+  int rank, pitch, slices;
+  int64_t slice;                    // columns of a slice
+};
+// y[l][n] = base[l][n] + scale[adapter(l)] * sum over j of p[l][j] w[adapter(l)][n][j], p the sum of the slices.
+struct AdapterExpand {
+  AdapterBatch b;
+  const float* p;
+  const void *w, *base;
+  const float* scale;
+  void* y;
+  float* u;                         // p itself, [L][rank]; null: not wanted
+  int64_t N, w_pitch, w_stride;
+  int rank, pitch, slices;
+};
+// One product of sums over rows: part[slot][j][n] = sum over the part's rows of p[l][j] q[l][n].
+struct AdapterOuterOperand {
+  const float* p;
+  const void* q;
+  float* part;
+  int64_t N;
+  int p_pitch, slices;              // slices of p
+  int scaled;                       // p times the adapter's scale
+};
+struct AdapterOuter {
+  AdapterBatch b;
+  AdapterOuterOperand a[2];
+  const float* scale;
+  const int32_t *order, *start, *first;   // segments in the order of their adapters, their first positions, the adapters' (null without offsets)
+  int rank, parts;
+};
+struct AdapterReduce {
+  const int32_t* first;
+  int64_t L, I, O;
+  const float *part_a, *part_b;
+  float *g_a, *g_b;
+  int rank, parts, adapters;
+};
+// Before a backward call: segments sorted by adapter, and both weights transposed.
+struct AdapterPrepare {
+  AdapterBatch b;
+  const void *a, *w;                // a [adapters][rank][I], w [adapters][O][rank]
+  void *at, *wt;                    // [adapters][I][rank_pitch], [adapters][rank][O]
+  int64_t I, O;
+  int rank, rank_pitch;
+  int32_t *order, *start, *first;
+};
+
+struct AdapterPlan {
+  bool rows;                        // a wave works on one row, not on a tile of them
+  int pitch;                        // floats of a row of p
+  int slices_forward, slices_backward, parts;
+  int64_t slice_forward, slice_backward;
+  int rank_pitch;
+  size_t p_bytes, at, wt, sorted, part_a, part_b, forward, backward;   // offsets into the workspace, and its sizes
+};
+AdapterPlan adapter_plan(hot_type type, int64_t L, int64_t O, int64_t I, int64_t rank, int64_t adapters, int64_t segments);
+
+hipError_t launch_adapter_shrink(const AdapterShrink& a, bool rows, hot_type type, hipStream_t s);
+hipError_t launch_adapter_expand(const AdapterExpand& a, bool rows, hot_type type, hipStream_t s);
+hipError_t launch_adapter_prepare(const AdapterPrepare& a, hot_type type, hipStream_t s);
+hipError_t launch_adapter_outer(const AdapterOuter& a, hot_type type, hipStream_t s);
+hipError_t launch_adapter_reduce(const AdapterReduce& a, hipStream_t s);
+
+}  // namespace hot

@@ -1,48 +1,13 @@
 // C ABI of the operators around the linear backward: argument checks, workspace layouts and the launches
 // behind each call.
 #include "block_host.h"
+#include "call_checks.h"
 
 namespace hot {
 
 namespace {
 
-constexpr int64_t kMaxRows = 1ll << 31, kMaxCols = 1ll << 24;
-
-bool size_ok(int64_t rows, int64_t cols) { return rows >= 1 && cols >= 1 && rows < kMaxRows && cols < kMaxCols; }
-bool type_ok(hot_type t) { return t == HOT_F32 || t == HOT_BF16; }
 bool fn_ok(hot_act_fn f) { return f >= HOT_ACT_NONE && f <= HOT_ACT_SILU; }
-int64_t bytes_of(hot_type t, int64_t rows, int64_t cols) { return rows * cols * (t == HOT_BF16 ? 2 : 4); }
-
-// Collects a call's buffers: aligned, and no output on top of an input or of another output.
-class Buffers {
- public:
-  void in(const void* p, int64_t bytes) { add(p, bytes, false); }
-  void out(const void* p, int64_t bytes) { add(p, bytes, true); }
-  bool ok() const {
-    for (int i = 0; i < n_; ++i) {
-      if (!aligned_) return false;
-      for (int j = 0; j < i; ++j)
-        if ((out_[i] || out_[j]) && lo_[i] < hi_[j] && lo_[j] < hi_[i]) return false;
-    }
-    return true;
-  }
-
- private:
-  void add(const void* p, int64_t bytes, bool out) {
-    if (!p) return;
-    const uintptr_t a = reinterpret_cast<uintptr_t>(p);
-    if (a & 15u) aligned_ = false;
-    lo_[n_] = a;
-    hi_[n_] = a + (uintptr_t)bytes;
-    out_[n_++] = out;
-  }
-  uintptr_t lo_[12], hi_[12];
-  bool out_[12];
-  int n_ = 0;
-  bool aligned_ = true;
-};
-
-bool aligned256(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 255u) == 0; }
 
 size_t activation_sums_bytes(int64_t rows, int64_t cols) {
   return (size_t)activation_sum_rows(rows, cols) * round_up(cols, 32) * 4;
@@ -50,14 +15,6 @@ size_t activation_sums_bytes(int64_t rows, int64_t cols) {
 size_t norm_sums_bytes(int64_t rows, int64_t cols) {
   return (size_t)layer_norm_sum_rows(rows, cols, HOT_BF16) * 2 * round_up(cols, 32) * 4;
 }
-
-#define HOT_STAGE(stage, expr)                   \
-  do {                                           \
-    stage_begin(stage, s);                       \
-    const hipError_t e_ = (expr);                \
-    stage_end(stage, s);                         \
-    if (e_ != hipSuccess) return HOT_ERR_DEVICE; \
-  } while (0)
 
 }  // namespace
 }  // namespace hot

@@ -162,7 +162,9 @@ enum Stage {
   kStGemmPair = 0, kStActAbsmax, kStActQuant, kStWAbsmax, kStWQuant, kStGyRowQuant, kStGyRowAbsmax,
   kStGyRowQuant2, kStGxGemm, kStGyTAbsmax, kStGyTQuant, kStGwGemm, kStWGyRow, kStGyFusedAbsmax,
   kStGyFusedQuant, kStCkptWrite, kStCkptRead, kStActForward, kStActBackward, kStNormForward, kStNormBackward,
-  kStColumnSums, kStLinearOperands, kStLinear
+  kStColumnSums, kStLinearOperands, kStLinear,
+  kStAdapterPrepare = 25, kStAdapterShrink, kStAdapterExpand, kStAdapterOuter, kStAdapterSums, kStLogProbs, kStLogProbsGrad, kStAdamW,
+  kStStateRead, kStStateWrite        // 24 has no name: those who read names up to an empty one keep their list
 };
 // A kernel's limit of dynamic LDS is each device's own: raised on the current one, once (again does no harm).  `done`: the kernel's,
 // a bit a device.
