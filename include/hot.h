@@ -544,7 +544,7 @@ hot_status hot_debug_set_gemm_mode(int mode);
 /* Kernel roles timed separately; hot_debug_stage_name() gives their names.  The first HOT_NUM_STAGES are those of the
  * linear backward, the next nine those of the operators around it; 24 is none, and those of a fine-tuning step follow. */
 #define HOT_NUM_STAGES 15
-#define HOT_NUM_STAGES_ALL 35
+#define HOT_NUM_STAGES_ALL 36
 
 /* From this call on, every kernel the library launches is bracketed by two HIP
  * events recorded on its stream.  Host-side state only; not thread-safe against

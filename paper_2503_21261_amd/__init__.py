@@ -41,7 +41,7 @@ EXPORTS = (
     "hot_token_logprobs_workspace_bytes", "hot_token_logprobs", "hot_token_logprobs_backward",
     "hot_adamw_state_bytes", "hot_adamw_state_read", "hot_adamw_state_write", "hot_adamw_table_bytes", "hot_adamw_table", "hot_adamw_step",
 )
-HOT_NUM_STAGES, HOT_NUM_STAGES_ALL = 15, 35
+HOT_NUM_STAGES, HOT_NUM_STAGES_ALL = 15, 36
 HOT_WS_PREFIX_BYTES = 24832
 HOT_F32, HOT_BF16 = 0, 1
 HOT_ACT_NONE, HOT_ACT_RELU, HOT_ACT_GELU, HOT_ACT_GELU_TANH, HOT_ACT_SILU = range(5)

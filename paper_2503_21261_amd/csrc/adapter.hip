@@ -6,9 +6,12 @@
 // kernels, all on the matrix cores, none with a library call:
 //   shrink  [rows x K] . [rank x K]^T -> [rows x rank]: a wave holds 32 rows (or one) and all ranks, K in slices where rows are few;
 //   expand  [rows x rank] . [N x rank]^T -> [rows x N]: the ranks' factors of the rows stay in registers, columns go by;
-//   outer   [rows x rank]^T . [rows x N] -> [rank x N]: rows as they lie are transposed in registers, 8 x 8 values a lane.
+//   outer   [rows x rank]^T . [rows x N] -> [rank x N]: rows as they lie are transposed in registers, 8 x 8 values a lane, the factors
+//           before, by a launch of its own.
 // u and g_u are fp32.  Where they meet bfloat16 operands they are split into bfloat16 parts, cut off and not rounded, so that three
 // parts are the number itself: three for fp32 results (g_A, g_B), two (2^-16) for bfloat16 ones.
+#include <type_traits>
+
 #include "adapter_host.h"
 #include "block_device.h"
 #include "block_host.h"
@@ -121,13 +124,8 @@ __global__ __launch_bounds__(256) void shrink_kernel(const AdapterShrink a) {
       const T* const w = (const T*)a.w + run.adapter * a.w_stride;
       const T* x[R];
       const T* wr[RT];
-      bool part_of_run[R];
 #pragma unroll
-      for (int r = 0; r < R; ++r) {
-        const int64_t l = min(max(row0 + r * 16 + i, row), run.end - 1);
-        x[r] = (const T*)a.q + l * a.K + q * kPer;
-        part_of_run[r] = row0 + r * 16 < run.end && row0 + r * 16 + 16 > row;
-      }
+      for (int r = 0; r < R; ++r) x[r] = (const T*)a.q + min(max(row0 + r * 16 + i, row), run.end - 1) * a.K + q * kPer;
 #pragma unroll
       for (int t = 0; t < RT; ++t) wr[t] = w + min(t * 16 + i, a.rank - 1) * a.w_pitch + q * kPer;
       f4 acc[RT][R];
@@ -135,25 +133,43 @@ __global__ __launch_bounds__(256) void shrink_kernel(const AdapterShrink a) {
       for (int t = 0; t < RT; ++t)
 #pragma unroll
         for (int r = 0; r < R; ++r) acc[t][r] = f4{0.0f, 0.0f, 0.0f, 0.0f};
-      int64_t k = k0;
-      for (; k + kStep <= k1; k += kStep) {
-        Raw8<T> fx[R][kFrags], fw[RT][kFrags];
-#pragma unroll
-        for (int f = 0; f < kFrags; ++f) {
-#pragma unroll
-          for (int r = 0; r < R; ++r)
-            if (R == 1 || part_of_run[r]) fx[r][f] = load8(x[r] + k + f * 8, 8);
-#pragma unroll
-          for (int t = 0; t < RT; ++t) fw[t][f] = load8(wr[t] + k + f * 8, 8);
-        }
+      struct Step {
+        Raw8<T> x[R][kFrags], w[RT][kFrags];
+      };
+      const auto load = [&](int64_t at, Step& d) {
 #pragma unroll
         for (int r = 0; r < R; ++r)
-          if (R == 1 || part_of_run[r]) {
 #pragma unroll
-            for (int f = 0; f < kFrags; ++f)
+          for (int f = 0; f < kFrags; ++f) d.x[r][f] = load8(x[r] + at + f * 8, 8);
 #pragma unroll
-              for (int t = 0; t < RT; ++t) acc[t][r] = mma(frag(fw[t][f]), frag(fx[r][f]), acc[t][r]);
-          }
+        for (int t = 0; t < RT; ++t)
+#pragma unroll
+          for (int f = 0; f < kFrags; ++f) d.w[t][f] = load8(wr[t] + at + f * 8, 8);
+      };
+      const auto multiply = [&](const Step& d) {
+#pragma unroll
+        for (int f = 0; f < kFrags; ++f)
+#pragma unroll
+          for (int r = 0; r < R; ++r)
+#pragma unroll
+            for (int t = 0; t < RT; ++t) acc[t][r] = mma(frag(d.w[t][f]), frag(d.x[r][f]), acc[t][r]);
+      };
+      // Whole steps, the next one's loads on their way; the last one's once more instead of a branch around them, which would make
+      // the waits wait for all.
+      const int64_t k = k0 + (k1 - k0) / kStep * kStep;
+      if (k > k0) {
+        Step d0, d1;
+        load(k0, d0);
+        for (int64_t at = k0;; at += 2 * kStep) {
+          load(min(at + kStep, k - kStep), d1);
+          __builtin_amdgcn_sched_barrier(0);      // else the loads sink to where they are used
+          multiply(d0);
+          if (at + kStep >= k) break;
+          load(min(at + 2 * kStep, k - kStep), d0);
+          __builtin_amdgcn_sched_barrier(0);
+          multiply(d1);
+          if (at + 2 * kStep >= k) break;
+        }
       }
       if (k < k1) {     // the row's last elements: zeros behind them, on both sides
 #pragma unroll
@@ -173,8 +189,13 @@ __global__ __launch_bounds__(256) void shrink_kernel(const AdapterShrink a) {
         const int64_t l = row0 + r * 16 + i;
         if (l >= row && l < run.end) {
 #pragma unroll
-          for (int t = 0; t < RT; ++t)
-            if (t * 16 + q * 4 < a.pitch) *(f4*)(out + l * a.pitch + t * 16 + q * 4) = acc[t][r];
+          for (int t = 0; t < RT; ++t) {
+            const int j = t * 16 + q * 4;
+            f4 v;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[e] = j + e < a.rank ? acc[t][r][e] : 0.0f;
+            if (j < a.pitch) *(f4*)(out + l * a.pitch + j) = v;
+          }
         }
       }
     }
@@ -187,7 +208,7 @@ __global__ __launch_bounds__(256) void shrink_kernel(const AdapterShrink a) {
 // A wave's step is 64 columns: tile t of the four has columns 16 (m / 4) + 4 t + m % 4 in its row m, so that a lane ends with 16
 // columns in a row of its row.
 template <class T, int RC, int R, int ROWS>
-__global__ __launch_bounds__(256) void expand_kernel(const AdapterExpand a, int64_t span) {
+__global__ __launch_bounds__(256, 2) void expand_kernel(const AdapterExpand a, int64_t span) {
   constexpr bool kSingle = sizeof(T) == 4, kPack = RC == 0 && !kSingle;
   constexpr int kChunks = RC == 0 ? 1 : RC, kParts = kSingle || kPack ? 1 : 2;
   const int lane = threadIdx.x & 63, i = lane & 15, q = lane >> 4;
@@ -212,22 +233,27 @@ __global__ __launch_bounds__(256) void expand_kernel(const AdapterExpand a, int6
     bool mine[R];
 #pragma unroll
     for (int r = 0; r < R; ++r) {
-      const int64_t l = min(row0 + r * 16 + i, a.b.L - 1);
+      const int64_t l = min(max(row0 + r * 16 + i, row), run.end - 1);
       mine[r] = row0 + r * 16 + i >= row && row0 + r * 16 + i < run.end;
 #pragma unroll
       for (int c = 0; c < kChunks; ++c) {
-        const int j = c * 32 + j0;
+        // The weights' last ranks are loaded as a row's last eight: p as they are, zeros for those that another lane has.
+        const int j = c * 32 + j0, at = a.w_cols < 8 ? min(j, 0) : min(j, a.w_cols - 8);
         float v[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
-        if (!none && mine[r]) {
+        if (!none) {
           for (int s = 0; s < a.slices; ++s) {
-            const float* const from = a.p + ((int64_t)s * a.b.L + l) * a.pitch + j;
             float w[8];
-            load_values(from, min(max(a.rank - j, 0), 8), w);
+            load_values(a.p + ((int64_t)s * a.b.L + l) * a.pitch + at, 8, w);
 #pragma unroll
             for (int e = 0; e < 8; ++e) v[e] += w[e];
           }
+#pragma unroll
+          for (int e = 0; e < 8; ++e) v[e] = at + e >= j ? v[e] : 0.0f;
         }
-        if (a.u && n0 == 0 && mine[r] && !(kPack && q >= 2)) store8(a.u + l * a.rank + j, v, min(a.rank - j, 8));
+        if (a.u && n0 == 0 && mine[r] && !(kPack && q >= 2)) {
+          for (int e = 0; e < 8; ++e)
+            if (at + e >= j && at + e < a.rank) a.u[l * a.rank + at + e] = v[e];
+        }
 #pragma unroll
         for (int e = 0; e < 8; ++e) v[e] *= scale;
         if constexpr (kSingle) {
@@ -242,41 +268,55 @@ __global__ __launch_bounds__(256) void expand_kernel(const AdapterExpand a, int6
         }
       }
     }
+    // Factors of 16 columns a lane, from n on; past the last column the last one's.
     const T* const w = (const T*)a.w + (none ? 0 : run.adapter * a.w_stride);
-    for (int64_t n = n0; n < n1; n += 64) {
-      f4 acc[4][R];
+    const auto product = [&](int64_t n, auto tail, f4 (&acc)[4][R]) {
 #pragma unroll
       for (int t = 0; t < 4; ++t)
 #pragma unroll
         for (int r = 0; r < R; ++r) acc[t][r] = f4{0.0f, 0.0f, 0.0f, 0.0f};
-      const int64_t col = n + q * 16;
-      const int have[2] = {(int)max(min((int64_t)8, a.N - col), (int64_t)0), (int)max(min((int64_t)8, a.N - col - 8), (int64_t)0)};
+      if (none) return;
+#pragma unroll
+      for (int c = 0; c < kChunks; ++c) {
+        const int j = c * 32 + j0;
+        Raw8<T> fw[4];
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+          int64_t wn = n + (i >> 2) * 16 + t * 4 + (i & 3);
+          if (decltype(tail)::value) wn = min(wn, a.N - 1);
+          if (RC == 0 && a.w_cols < 8) fw[t] = load8(w + wn * a.w_pitch + j, min(max(a.w_cols - j, 0), 8));
+          else fw[t] = load8(w + wn * a.w_pitch + min(j, a.w_cols - 8), 8);
+        }
+#pragma unroll
+        for (int t = 0; t < 4; ++t)
+#pragma unroll
+          for (int r = 0; r < R; ++r)
+#pragma unroll
+            for (int part = 0; part < kParts; ++part) acc[t][r] = mma(frag(fw[t]), p[r][c][part], acc[t][r]);
+      }
+    };
+    const T* from[R];
+    T* to[R];
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+      const int64_t l = min(max(row0 + r * 16 + i, row), run.end - 1);
+      from[r] = (const T*)a.base + l * a.N + q * 16;
+      to[r] = (T*)a.y + l * a.N + q * 16;
+    }
+    int64_t n = n0;
+    for (; n + 64 <= n1; n += 64) {
       Raw8<T> base[R][2];
 #pragma unroll
-      for (int r = 0; r < R; ++r) {
-        const int64_t l = row0 + r * 16 + i;
+      for (int r = 0; r < R; ++r)
 #pragma unroll
-        for (int h = 0; h < 2; ++h)
-          base[r][h] = load8((const T*)a.base + l * a.N + col + h * 8, a.base && mine[r] ? have[h] : 0);
-      }
-      if (!none) {
-#pragma unroll
-        for (int c = 0; c < kChunks; ++c) {
-          const int j = c * 32 + j0, nj = min(max(a.rank - j, 0), 8);
-#pragma unroll
-          for (int t = 0; t < 4; ++t) {
-            const int64_t wn = min(n + (i >> 2) * 16 + t * 4 + (i & 3), a.N - 1);
-            const Frag<T> fw = frag(load8(w + wn * a.w_pitch + j, nj));
-#pragma unroll
-            for (int r = 0; r < R; ++r)
-#pragma unroll
-              for (int part = 0; part < kParts; ++part) acc[t][r] = mma(fw, p[r][c][part], acc[t][r]);
-          }
+        for (int h = 0; h < 2; ++h) {
+          if (a.base) base[r][h] = load8(from[r] + n + h * 8, 8);
+          else base[r][h] = Raw8<T>{};
         }
-      }
+      f4 acc[4][R];
+      product(n, std::false_type{}, acc);
 #pragma unroll
       for (int r = 0; r < R; ++r) {
-        const int64_t l = row0 + r * 16 + i;
         if (!mine[r]) continue;
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
@@ -284,9 +324,22 @@ __global__ __launch_bounds__(256) void expand_kernel(const AdapterExpand a, int6
           widen(base[r][h], v);
 #pragma unroll
           for (int e = 0; e < 8; ++e) v[e] += acc[h * 2 + e / 4][r][e & 3];
-          if (have[h] > 0) store8((T*)a.y + l * a.N + col + h * 8, v, have[h]);
+          if (a.stream) store8<true>(to[r] + n + h * 8, v, 8);
+          else store8(to[r] + n + h * 8, v, 8);
         }
       }
+    }
+    if (n < n1) {       // the last columns, one by one
+      f4 acc[4][R];
+      product(n, std::true_type{}, acc);
+#pragma unroll
+      for (int r = 0; r < R; ++r)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          if (!mine[r] || n + q * 16 + e >= n1) continue;
+          const float v = acc[e / 4][r][e & 3] + (a.base ? (float)from[r][n + e] : 0.0f);
+          to[r][n + e] = (T)v;
+        }
     }
     row = run.end;
   }
@@ -389,6 +442,26 @@ __global__ __launch_bounds__(256) void prepare_kernel(const AdapterPrepare a, in
 }
 
 // ---- outer ----------------------------------------------------------------------------------------
+// Rows of a part of the sums over `total` rows.
+__device__ __forceinline__ int64_t rows_of_part(int64_t total, int parts) { return ((total + parts - 1) / parts + 31) & -32ll; }
+
+// The first n of eight elements, zeros behind them.
+__device__ __forceinline__ Raw8<bf16> first_of(const Raw8<bf16>& r, int n) {
+  Raw8<bf16> o;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) o.a[e] = e < n ? r.a[e] : (uint16_t)0;
+  return o;
+}
+__device__ __forceinline__ Raw8<float> first_of(const Raw8<float>& r, int n) {
+  Raw8<float> o;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    o.a[e] = e < n ? r.a[e] : 0.0f;
+    o.b[e] = e + 4 < n ? r.b[e] : 0.0f;
+  }
+  return o;
+}
+
 // Eight rows of eight columns a lane.  bfloat16: column c's eight rows come together in 32 byte permutes; fp32: they are registers.
 __device__ __forceinline__ void columns_of(const Raw8<bf16> (&rows)[8], Frag<bf16> (&out)[8]) {
 #pragma unroll
@@ -411,25 +484,90 @@ __device__ __forceinline__ void columns_of(const Raw8<float> (&rows)[8], Frag<fl
   }
 }
 
-constexpr int kOuterCols = 128;
-
-// A workgroup: 128 columns, up to 64 ranks, one part of the rows that have adapters, in the order of their adapters.  Its four waves take
-// steps of 32 rows in turn and join their sums through LDS, once for each adapter of the part.
-template <class T, int RT>
-__global__ __launch_bounds__(256) void outer_kernel(const AdapterOuter a, int tiles_first, int tiles, int rank_blocks) {
+// u and g_u for the sums over rows: rows in the order of their adapters, a rank's factors one after the other, so that a lane's eight rows are one
+// load; bfloat16 in its three parts.  [parts][ranks rounded up to 16][pitch] of T.  A workgroup: 64 positions of one operand.
+template <class T>
+__global__ __launch_bounds__(256) void pack_kernel(const AdapterPack a) {
   constexpr int kParts = sizeof(T) == 4 ? 1 : 3;
-  __shared__ float s_acc[2][RT * 16 * kOuterCols];
-  const int lane = threadIdx.x & 63, i = lane & 15, q = lane >> 4, wave = threadIdx.x >> 6;
-  const int part = blockIdx.x / (tiles * rank_blocks), in = blockIdx.x % (tiles * rank_blocks);
-  const int tile = in % tiles, rank0 = in / tiles * 64;
-  const bool second = tile >= tiles_first;
-  const AdapterOuterOperand& o = second ? a.a[1] : a.a[0];
-  const int64_t col0 = (int64_t)(second ? tile - tiles_first : tile) * kOuterCols, col = col0 + i * 8;
-  const int have = (int)max(min((int64_t)8, o.N - col), (int64_t)0);
+  __shared__ float s_p[kMaxRank * 65];
+  __shared__ int s_row[64];
+  const int tid = threadIdx.x;
+  const bool second = blockIdx.y != 0;
+  const int64_t pos0 = (int64_t)blockIdx.x * 64;
   const int64_t total = a.first ? max(min((int64_t)a.first[a.b.adapters], a.b.L), (int64_t)0) : a.b.L;
-  const int64_t lo = total * part / a.parts, hi = total * (part + 1) / a.parts;
+  if (pos0 >= total) return;
+  if (tid < 64) {
+    const int pos = (int)min(pos0 + tid, total - 1);
+    int64_t row = pos;
+    if (a.first) {
+      int lo = 0, n = a.b.segments + 1;          // the last segment that starts at or before it
+      while (n > 1) {
+        const int half = n / 2;
+        if (a.start[lo + half] <= pos) {
+          lo += half;
+          n -= half;
+        } else {
+          n = half;
+        }
+      }
+      lo = min(lo, a.b.segments - 1);
+      row = min(max((int64_t)a.b.offsets[a.order[lo]] + pos - a.start[lo], (int64_t)0), a.b.L - 1);
+      if (!second) a.rows[pos0 + tid] = (int)row;
+    }
+    s_row[tid] = (int)row;
+  }
+  __syncthreads();
+  const float* const p = second ? a.u : a.g_u;
+  const int pitch = second ? a.rank : a.g_pitch, slices = second ? 1 : a.slices, ranks = (a.rank + 15) & -16;
+  for (int at = tid; at < 64 * ranks; at += 256) {
+    const int j = at % ranks, x = at / ranks;
+    float v = 0.0f;
+    if (j < a.rank) {
+      for (int s = 0; s < slices; ++s) v += p[((int64_t)s * a.b.L + s_row[x]) * pitch + j];
+    }
+    s_p[j * 65 + x] = v;
+  }
+  __syncthreads();
+  T* const out = (T*)(second ? a.u_out : a.g_out);
+  for (int at = tid; at < 8 * ranks; at += 256) {
+    const int j = at / 8, x = at % 8 * 8;
+    float v[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = s_p[j * 65 + x + e];
+    T* const to = out + (int64_t)j * a.pitch + pos0 + x;
+    if constexpr (kParts == 1) {
+      store8(to, v, 8);
+    } else {
+      Frag<bf16> f[kParts];
+      split8<kParts>(v, f);
+#pragma unroll
+      for (int part = 0; part < kParts; ++part) *(u4*)(to + (int64_t)part * ranks * a.pitch) = f[part].v;
+    }
+  }
+}
 
-  for (int64_t pos = lo; pos < hi;) {
+constexpr int kOuterCols = 128, kOuterWaves = 4;    // columns of a wave, waves of a workgroup side by side
+
+// A wave: 128 columns, up to 64 ranks, one part of the rows that have adapters, in steps of 32, the next step's loads on their way.
+// The waves of a workgroup share the rows' factors in the first cache.  Sums over rows leave as one partial sum a part and adapter.
+template <class T, int RT>
+__global__ __launch_bounds__(64 * kOuterWaves) void outer_kernel(const AdapterOuter a, int tiles_first, int tiles, int rank_blocks) {
+  constexpr int kParts = sizeof(T) == 4 ? 1 : 3;
+  const int lane = threadIdx.x & 63, i = lane & 15, q = lane >> 4, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int part = blockIdx.x / (tiles * rank_blocks), in = blockIdx.x % (tiles * rank_blocks);
+  const int tile = in % tiles, rank0 = in / tiles * 64, ranks = (a.rank + 15) & -16;
+  const bool second = tile >= tiles_first;
+  const AdapterOuterOperand o = second ? a.a[1] : a.a[0];
+  const int64_t col0 = ((int64_t)(second ? tile - tiles_first : tile) * kOuterWaves + wave) * kOuterCols;
+  if (col0 >= o.N) return;
+  // Columns past the last one: the last eight once more, which come out the same.
+  const int64_t col = o.N < 8 ? col0 + i * 8 : min(col0 + i * 8, o.N - 8);
+  const int have = o.N < 8 ? (int)max(min((int64_t)8, o.N - col), (int64_t)0) : 8;
+  const int64_t total = a.first ? max(min((int64_t)a.first[a.b.adapters], a.b.L), (int64_t)0) : a.b.L;
+  const int64_t per = rows_of_part(total, a.parts);
+  const int64_t hi = min(per * (part + 1), total);
+
+  for (int64_t pos = per * part; pos < hi;) {
     int k = 0;
     int64_t k_end = hi;
     if (a.first) {
@@ -443,83 +581,73 @@ __global__ __launch_bounds__(256) void outer_kernel(const AdapterOuter a, int ti
     for (int t = 0; t < RT; ++t)
 #pragma unroll
       for (int c = 0; c < 8; ++c) acc[t][c] = f4{0.0f, 0.0f, 0.0f, 0.0f};
-    int turn = 0;
-    while (pos < k_end) {
-      int64_t row = pos, end = k_end;       // rows row .. row + end - pos - 1
-      if (a.first) {
-        const int s = min(max(__builtin_amdgcn_readfirstlane(count_up_to(a.start, a.b.segments + 1, (int)pos)) - 1, 0), a.b.segments - 1);
-        row = max((int64_t)a.b.offsets[a.order[s]] + pos - a.start[s], (int64_t)0);
-        end = min(k_end, max((int64_t)a.start[s + 1], pos + 1));
+    Raw8<T> p[RT][kParts];
+    const T* const p_at = (const T*)o.p + (int64_t)(rank0 + i) * a.pitch + q * 8;
+    const int64_t last = pos + (k_end - pos - 1) / 32 * 32;      // the last step's first position
+    const auto rows_at = [&](int64_t at, int (&r)[8]) {          // past the last row: that one once more, times zero
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const int64_t l = min(at + q * 8 + e, k_end - 1);
+        r[e] = a.first ? a.rows[l] : (int)l;
       }
-      const int64_t last = min(row + (end - pos), a.b.L) - 1;
-      for (; row <= last; row += 32) {
-        if ((turn++ & 3) != wave) continue;
-        Raw8<T> x[8];
+    };
+    const auto load = [&](const int (&r)[8], Raw8<T> (&x)[8]) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          const int64_t l = min(row + q * 8 + e, last);      // rows past the run's end: the last one, times zero
-          x[e] = load8((const T*)o.q + l * o.N + col, have);
-        }
-        Frag<T> p[RT][kParts];
+      for (int e = 0; e < 8; ++e) {
+        const T* const from = (const T*)o.q + (int64_t)r[e] * o.N + col;
+        if (o.N < 8) x[e] = load8(from, have);
+        else x[e] = load8(from, 8);
+      }
+    };
+    const auto load_p = [&](int t, int64_t at) {     // ranks past the last tile: the last tile's, whose sums are not stored
+      const int64_t j = min(t * 16, ranks - 16 - rank0);
 #pragma unroll
-        for (int t = 0; t < RT; ++t) {
-          const int j = rank0 + t * 16 + i;
-          float v[8];
-#pragma unroll
-          for (int e = 0; e < 8; ++e) {
-            const int64_t l = row + q * 8 + e;
-            v[e] = 0.0f;
-            if (l <= last && j < a.rank) {
-              for (int s = 0; s < o.slices; ++s) v[e] += o.p[((int64_t)s * a.b.L + l) * o.p_pitch + j];
-            }
-          }
-          if constexpr (kParts == 1) {
-#pragma unroll
-            for (int e = 0; e < 8; ++e) p[t][0].v[e] = v[e];
-          } else {
-            split8<3>(v, p[t]);
-          }
-        }
-        Frag<T> f[8];
-        columns_of(x, f);
+      for (int s = 0; s < kParts; ++s) p[t][s] = load8(p_at + (s * ranks + j) * a.pitch + at, 8);
+    };
+    const auto multiply = [&](int64_t at, const Raw8<T> (&x)[8]) {
+      if (at == last) {                                          // zeros past the last row
+        const int n = (int)min(max(k_end - at - q * 8, (int64_t)0), (int64_t)8);
 #pragma unroll
         for (int t = 0; t < RT; ++t)
 #pragma unroll
-          for (int s = 0; s < kParts; ++s)
-#pragma unroll
-            for (int c = 0; c < 8; ++c) acc[t][c] = mma(p[t][s], f[c], acc[t][c]);
+          for (int s = 0; s < kParts; ++s) p[t][s] = first_of(p[t][s], n);
       }
-      pos = end;
+      Frag<T> f[8];
+      columns_of(x, f);
+#pragma unroll
+      for (int t = 0; t < RT; ++t) {
+#pragma unroll
+        for (int s = 0; s < kParts; ++s)
+#pragma unroll
+          for (int c = 0; c < 8; ++c) acc[t][c] = mma(frag(p[t][s]), f[c], acc[t][c]);
+        __builtin_amdgcn_sched_barrier(0);                       // the next step's factors into the registers that are free now
+        load_p(t, min(at + 32, last));
+      }
+    };
+    Raw8<T> x0[8], x1[8];
+    int r0[8], r1[8];
+    rows_at(pos, r0);
+    rows_at(min(pos + 32, last), r1);
+    load(r0, x0);
+#pragma unroll
+    for (int t = 0; t < RT; ++t) load_p(t, pos);
+    for (;; pos += 64) {
+      load(r1, x1);
+      rows_at(min(pos + 64, last), r0);
+      __builtin_amdgcn_sched_barrier(0);
+      multiply(pos, x0);
+      if (pos >= last) break;
+      load(r0, x0);
+      rows_at(min(pos + 96, last), r1);
+      __builtin_amdgcn_sched_barrier(0);
+      multiply(pos + 32, x1);
+      if (pos + 32 >= last) break;
     }
-    // Waves 2 and 3 hand their sums to 0 and 1, then 1 to 0.  Lane (i, q) has ranks 16 t + 4 q + e of columns 8 i + c.
-#pragma unroll
-    for (int half = 2; half >= 1; half /= 2) {
-      __syncthreads();
-      if (wave >= half && wave < 2 * half) {
-#pragma unroll
-        for (int t = 0; t < RT; ++t)
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            float* const to = &s_acc[wave - half][(t * 16 + q * 4 + e) * kOuterCols + i * 8];
-            *(f4*)to = f4{acc[t][0][e], acc[t][1][e], acc[t][2][e], acc[t][3][e]};
-            *(f4*)(to + 4) = f4{acc[t][4][e], acc[t][5][e], acc[t][6][e], acc[t][7][e]};
-          }
-      }
-      __syncthreads();
-      if (wave < half) {
-#pragma unroll
-        for (int t = 0; t < RT; ++t)
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const float* const from = &s_acc[wave][(t * 16 + q * 4 + e) * kOuterCols + i * 8];
-#pragma unroll
-            for (int c = 0; c < 8; ++c) acc[t][c][e] += from[c];
-          }
-      }
-    }
-    if (wave == 0) {
-      const float scale = o.scaled && a.scale ? a.scale[k] : 1.0f;
-      float* const to = o.part + (int64_t)(part + k) * a.rank * o.N;
+    pos = k_end;
+    // Lane (i, q) has ranks 16 t + 4 q + e of its eight columns.
+    const float scale = o.scaled && a.scale ? a.scale[k] : 1.0f;
+    float* const to = o.part + (int64_t)(part + k) * a.rank * o.N;
+    if (col0 + i * 8 < o.N) {
 #pragma unroll
       for (int t = 0; t < RT; ++t)
 #pragma unroll
@@ -528,30 +656,53 @@ __global__ __launch_bounds__(256) void outer_kernel(const AdapterOuter a, int ti
           float v[8];
 #pragma unroll
           for (int c = 0; c < 8; ++c) v[c] = acc[t][c][e] * scale;
-          if (j < a.rank && have > 0) store8(to + (int64_t)j * o.N + col, v, have);
+          if (j < a.rank) store8(to + (int64_t)j * o.N + col, v, have);
         }
     }
   }
 }
 
-// Sums of the parts of each adapter, in order.  Block: (adapter, 256 columns of [I | O]); part p of adapter k is slot p + k.
+// Sums of the parts of each adapter, in order; part p of adapter k is slot p + k.  Blocks of g_A: 1024 columns of one rank.  Blocks of g_B: 64
+// columns, all ranks, transposed through LDS.
 __global__ __launch_bounds__(256) void reduce_kernel(const AdapterReduce a, int tiles_a, int tiles) {
-  const int k = blockIdx.x / tiles, tile = blockIdx.x % tiles;
-  const bool second = tile >= tiles_a;
-  const int64_t N = second ? a.O : a.I, n = (int64_t)(second ? tile - tiles_a : tile) * 256 + threadIdx.x;
-  if (n >= N) return;
-  const float* const part = second ? a.part_b : a.part_a;
+  __shared__ float s_tile[64 * (kMaxRank + 1)];
+  const int k = blockIdx.x / tiles, tile = blockIdx.x % tiles, tid = threadIdx.x;
   const int64_t total = a.first ? max(min((int64_t)a.first[a.adapters], a.L), (int64_t)0) : a.L;
-  const int64_t lo = a.first ? a.first[k] : (k == 0 ? 0 : total), hi = a.first ? a.first[k + 1] : (k == 0 ? total : total);
-  for (int j = 0; j < a.rank; ++j) {
-    float v = 0.0f;
-    for (int p = 0; p < a.parts; ++p) {
-      const int64_t b = total * p / a.parts, e = total * (p + 1) / a.parts;
-      if (max(b, lo) < min(e, hi)) v += part[((int64_t)(p + k) * a.rank + j) * N + n];
+  const int64_t lo = a.first ? a.first[k] : (k == 0 ? 0 : total), hi = a.first ? a.first[k + 1] : total;
+  const int64_t per = rows_of_part(total, a.parts);         // the parts that hold rows of this adapter
+  const int p0 = lo < hi ? (int)(lo / per) : 0, p1 = lo < hi ? (int)min((hi + per - 1) / per, (int64_t)a.parts) : 0;
+  if (tile < tiles_a) {
+    const int spans = (int)((a.I + 1023) / 1024), j = tile / spans;
+    const int64_t n = (int64_t)(tile % spans) * 1024 + tid * 4;
+    const int have = (int)max(min((int64_t)4, a.I - n), (int64_t)0);
+    float v[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+    for (int p = p0; p < p1; ++p) {
+      const float* const from = a.part_a + ((int64_t)(p + k) * a.rank + j) * a.I + n;
+      if (have == 4) {
+        const f4_any x = *(const f4_any*)from;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] += x[i];
+      } else {
+        for (int i = 0; i < have; ++i) v[i] += from[i];
+      }
     }
-    if (second) a.g_b[((int64_t)k * a.O + n) * a.rank + j] = v;
-    else a.g_a[((int64_t)k * a.rank + j) * a.I + n] = v;
+    float* const to = a.g_a + ((int64_t)k * a.rank + j) * a.I + n;
+    for (int i = 0; i < have; ++i) to[i] = v[i];
+    return;
   }
+  const int64_t n0 = (int64_t)(tile - tiles_a) * 64, n = n0 + (tid & 63);
+  const int pitch = a.rank | 1;
+  for (int j = tid >> 6; j < a.rank; j += 4) {
+    float v = 0.0f;
+    if (n < a.O) {
+      for (int p = p0; p < p1; ++p) v += a.part_b[((int64_t)(p + k) * a.rank + j) * a.O + n];
+    }
+    s_tile[(tid & 63) * pitch + j] = v;
+  }
+  __syncthreads();
+  const int held = (int)min((int64_t)64, a.O - n0) * a.rank;
+  float* const to = a.g_b + ((int64_t)k * a.O + n0) * a.rank;
+  for (int i = tid; i < held; i += 256) to[i] = s_tile[i / a.rank * pitch + i % a.rank];
 }
 
 template <class T, int RT>
@@ -578,13 +729,14 @@ constexpr int64_t kExpandWaves = 4096;
 
 template <class T, int RC>
 hipError_t run_expand(const AdapterExpand& a, bool rows, hipStream_t s) {
-  const int64_t tiles = rows ? a.b.L : ceil_div(a.b.L, 32), steps = ceil_div(a.N, 64);
+  constexpr int R = RC == 4 ? 1 : 2;      // the factors of 128 ranks take the registers of a second tile
+  const int64_t tiles = rows ? a.b.L : ceil_div(a.b.L, 16 * R), steps = ceil_div(a.N, 64);
   int64_t cuts = ceil_div(kExpandWaves, tiles);
   if (cuts > steps) cuts = steps;
   const int64_t span = ceil_div(steps, cuts) * 64;
   const int64_t tasks = tiles * ceil_div(a.N, span);
   if (rows) expand_kernel<T, RC, 1, 1><<<(uint32_t)ceil_div(tasks, 4), 256, 0, s>>>(a, span);
-  else expand_kernel<T, RC, 2, 32><<<(uint32_t)ceil_div(tasks, 4), 256, 0, s>>>(a, span);
+  else expand_kernel<T, RC, R, 16 * R><<<(uint32_t)ceil_div(tasks, 4), 256, 0, s>>>(a, span);
   return hipGetLastError();
 }
 template <class T>
@@ -597,12 +749,13 @@ hipError_t expand_of(const AdapterExpand& a, bool rows, hipStream_t s) {
 
 template <class T>
 hipError_t outer_of(const AdapterOuter& a, hipStream_t s) {
-  const int tiles_first = (int)ceil_div(a.a[0].N, kOuterCols), tiles = tiles_first + (int)ceil_div(a.a[1].N, kOuterCols);
+  constexpr int kCols = kOuterCols * kOuterWaves;
+  const int tiles_first = (int)ceil_div(a.a[0].N, kCols), tiles = tiles_first + (int)ceil_div(a.a[1].N, kCols);
   const int blocks = (int)ceil_div(a.rank, 64);
   const uint32_t grid = (uint32_t)((int64_t)tiles * blocks * a.parts);
-  if (a.rank <= 16) outer_kernel<T, 1><<<grid, 256, 0, s>>>(a, tiles_first, tiles, blocks);
-  else if (a.rank <= 32) outer_kernel<T, 2><<<grid, 256, 0, s>>>(a, tiles_first, tiles, blocks);
-  else outer_kernel<T, 4><<<grid, 256, 0, s>>>(a, tiles_first, tiles, blocks);
+  if (a.rank <= 16) outer_kernel<T, 1><<<grid, 64 * kOuterWaves, 0, s>>>(a, tiles_first, tiles, blocks);
+  else if (a.rank <= 32) outer_kernel<T, 2><<<grid, 64 * kOuterWaves, 0, s>>>(a, tiles_first, tiles, blocks);
+  else outer_kernel<T, 4><<<grid, 64 * kOuterWaves, 0, s>>>(a, tiles_first, tiles, blocks);
   return hipGetLastError();
 }
 
@@ -612,7 +765,7 @@ AdapterPlan adapter_plan(hot_type type, int64_t L, int64_t O, int64_t I, int64_t
   AdapterPlan p{};
   const int64_t size = type == HOT_BF16 ? 2 : 4, step = 128 / size;
   p.rows = L <= 4 * (segments > 0 ? segments : 1) && L <= 1 << 20;
-  p.pitch = (int)round_up(rank, 4);
+  p.pitch = (int)round_up(rank, 8);      // zeros behind the ranks
   p.rank_pitch = (int)round_up(rank, 8);
   const auto slices = [&](int64_t K, int& count, int64_t& slice) {
     const int64_t tiles = p.rows ? L : ceil_div(L, 32);
@@ -626,10 +779,11 @@ AdapterPlan adapter_plan(hot_type type, int64_t L, int64_t O, int64_t I, int64_t
   };
   slices(I, p.slices_forward, p.slice_forward);
   slices(O, p.slices_backward, p.slice_backward);
-  const int64_t tiles = (ceil_div(I, kOuterCols) + ceil_div(O, kOuterCols)) * ceil_div(rank, 64);
-  int64_t parts = ceil_div(768, tiles);
-  const int64_t most = ceil_div(L, 128);
-  p.parts = (int)(parts < most ? parts : most);
+  // Parts of the sums over rows: workgroups for all compute units (one each with the registers of 64 ranks, two below).
+  const int64_t tiles = (ceil_div(I, kOuterCols * kOuterWaves) + ceil_div(O, kOuterCols * kOuterWaves)) * ceil_div(rank, 64);
+  const int64_t wanted = ceil_div(rank > 32 ? 256 : 512, tiles), most = ceil_div(L, 64);
+  p.parts = (int)(wanted < most ? wanted : most);
+  p.pos_pitch = round_up(L, 64) + 64;
 
   const int64_t row_bytes = L * p.pitch * 4;
   p.forward = (size_t)round_up(row_bytes * p.slices_forward, 256);
@@ -641,7 +795,8 @@ AdapterPlan adapter_plan(hot_type type, int64_t L, int64_t O, int64_t I, int64_t
   };
   p.at = take(adapters * I * p.rank_pitch * size);
   p.wt = take(adapters * rank * O * size);
-  p.sorted = take((2 * segments + 1 + adapters + 1) * 4);
+  p.sorted = take((2 * segments + 1 + adapters + 1 + (segments ? p.pos_pitch : 0)) * 4);
+  p.packed = take(2 * (type == HOT_BF16 ? 3 : 1) * size * round_up(rank, 16) * p.pos_pitch);
   p.part_a = take((p.parts + adapters) * rank * I * 4);
   p.part_b = take((p.parts + adapters) * rank * O * 4);
   p.backward = at;
@@ -664,11 +819,17 @@ hipError_t launch_adapter_prepare(const AdapterPrepare& a, hot_type type, hipStr
   else prepare_kernel<float><<<(uint32_t)grid, 256, 0, s>>>(a, sorts, tiles_a, tiles_w, rank_tiles);
   return hipGetLastError();
 }
+hipError_t launch_adapter_pack(const AdapterPack& a, hot_type type, hipStream_t s) {
+  const dim3 grid((uint32_t)ceil_div(a.b.L, 64), 2);
+  if (type == HOT_BF16) pack_kernel<bf16><<<grid, 256, 0, s>>>(a);
+  else pack_kernel<float><<<grid, 256, 0, s>>>(a);
+  return hipGetLastError();
+}
 hipError_t launch_adapter_outer(const AdapterOuter& a, hot_type type, hipStream_t s) {
   return type == HOT_BF16 ? outer_of<bf16>(a, s) : outer_of<float>(a, s);
 }
 hipError_t launch_adapter_reduce(const AdapterReduce& a, hipStream_t s) {
-  const int tiles_a = (int)ceil_div(a.I, 256), tiles = tiles_a + (int)ceil_div(a.O, 256);
+  const int tiles_a = (int)ceil_div(a.I, 1024) * a.rank, tiles = tiles_a + (int)ceil_div(a.O, 64);
   reduce_kernel<<<(uint32_t)((int64_t)a.adapters * tiles), 256, 0, s>>>(a, tiles_a, tiles);
   return hipGetLastError();
 }

@@ -33,21 +33,33 @@ struct AdapterExpand {
   float* u;                         // p itself, [L][rank]; null: not wanted
   int64_t N, w_pitch, w_stride;
   int rank, pitch, slices;
+  int w_cols;                       // elements of a row of w: rank, or more with zeros behind
+  int stream;                       // y is stored with the streaming hint
 };
-// One product of sums over rows: part[slot][j][n] = sum over the part's rows of p[l][j] q[l][n].
+// u and g_u (the sum of its slices) for the sums over rows: [parts][ranks rounded up to 16][pitch], rows in the order of their adapters, and that
+// order itself.
+struct AdapterPack {
+  AdapterBatch b;
+  const float *g_u, *u;
+  void *g_out, *u_out;
+  const int32_t *order, *start, *first;   // segments in the order of their adapters, their first positions, the adapters' (null without offsets)
+  int32_t* rows;                    // rows of the positions
+  int64_t pitch;
+  int rank, g_pitch, slices;
+};
+// One product of sums over rows: part[slot][j][n] = sum over the part's rows of p[j][l] q[l][n].
 struct AdapterOuterOperand {
-  const float* p;
-  const void* q;
+  const void *p, *q;
   float* part;
   int64_t N;
-  int p_pitch, slices;              // slices of p
   int scaled;                       // p times the adapter's scale
 };
 struct AdapterOuter {
   AdapterBatch b;
   AdapterOuterOperand a[2];
   const float* scale;
-  const int32_t *order, *start, *first;   // segments in the order of their adapters, their first positions, the adapters' (null without offsets)
+  const int32_t *first, *rows;
+  int64_t pitch;
   int rank, parts;
 };
 struct AdapterReduce {
@@ -73,13 +85,15 @@ struct AdapterPlan {
   int slices_forward, slices_backward, parts;
   int64_t slice_forward, slice_backward;
   int rank_pitch;
-  size_t p_bytes, at, wt, sorted, part_a, part_b, forward, backward;   // offsets into the workspace, and its sizes
+  int64_t pos_pitch;                // positions of a row of packed factors
+  size_t at, wt, sorted, packed, part_a, part_b, forward, backward;   // offsets into the workspace, and its sizes
 };
 AdapterPlan adapter_plan(hot_type type, int64_t L, int64_t O, int64_t I, int64_t rank, int64_t adapters, int64_t segments);
 
 hipError_t launch_adapter_shrink(const AdapterShrink& a, bool rows, hot_type type, hipStream_t s);
 hipError_t launch_adapter_expand(const AdapterExpand& a, bool rows, hot_type type, hipStream_t s);
 hipError_t launch_adapter_prepare(const AdapterPrepare& a, hot_type type, hipStream_t s);
+hipError_t launch_adapter_pack(const AdapterPack& a, hot_type type, hipStream_t s);
 hipError_t launch_adapter_outer(const AdapterOuter& a, hot_type type, hipStream_t s);
 hipError_t launch_adapter_reduce(const AdapterReduce& a, hipStream_t s);
 

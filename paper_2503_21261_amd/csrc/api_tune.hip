@@ -5,6 +5,7 @@
 #include <new>
 
 #include "adapter_host.h"
+#include "block_host.h"
 #include "call_checks.h"
 #include "tune_host.h"
 
@@ -90,7 +91,8 @@ hot_status hot_adapter_forward(const void* x, const void* a, const void* b, hot_
   const AdapterBatch batch{offsets, index, (int)segments, (int)adapters, L};
   const AdapterShrink shrink{batch, x, a, (float*)ws, I, I, rank * I, (int)rank, p.pitch, p.slices_forward, p.slice_forward};
   HOT_STAGE(kStAdapterShrink, launch_adapter_shrink(shrink, p.rows, type, s));
-  const AdapterExpand expand{batch, (const float*)ws, b, base, scale, y, u, O, rank, O * rank, (int)rank, p.pitch, p.slices_forward};
+  const AdapterExpand expand{batch, (const float*)ws, b, base, scale, y, u, O, rank, O * rank, (int)rank, p.pitch, p.slices_forward, (int)rank,
+                             stream_output(L, bytes_of(type, 1, O))};
   HOT_STAGE(kStAdapterExpand, launch_adapter_expand(expand, p.rows, type, s));
   return HOT_OK;
 }
@@ -132,20 +134,36 @@ hot_status hot_adapter_backward(const void* g_y, const void* x, const float* u, 
   HOT_STAGE(kStAdapterShrink, launch_adapter_shrink(shrink, p.rows, type, s));
   if (g_x) {
     const AdapterExpand expand{batch, g_u, w + p.at, g_base, scale, g_x, nullptr, I, p.rank_pitch, I * p.rank_pitch, (int)rank, p.pitch,
-                               p.slices_backward};
+                               p.slices_backward, p.rank_pitch, stream_output(L, bytes_of(type, 1, I))};
     HOT_STAGE(kStAdapterExpand, launch_adapter_expand(expand, p.rows, type, s));
   }
   if (g_a) {
+    const int64_t half = (type == HOT_BF16 ? 6 : 4) * round_up(rank, 16) * p.pos_pitch;
+    AdapterPack pack{};
+    pack.b = batch;
+    pack.g_u = g_u;
+    pack.u = u;
+    pack.g_out = w + p.packed;
+    pack.u_out = w + p.packed + half;
+    if (offsets) {
+      pack.order = order;
+      pack.start = start;
+      pack.first = first;
+      pack.rows = first + adapters + 1;
+    }
+    pack.pitch = p.pos_pitch;
+    pack.rank = (int)rank;
+    pack.g_pitch = p.pitch;
+    pack.slices = p.slices_backward;
+    HOT_STAGE(kStAdapterPack, launch_adapter_pack(pack, type, s));
     AdapterOuter outer{};
     outer.b = batch;
-    outer.a[0] = AdapterOuterOperand{g_u, x, (float*)(w + p.part_a), I, p.pitch, p.slices_backward, 1};
-    outer.a[1] = AdapterOuterOperand{u, g_y, (float*)(w + p.part_b), O, (int)rank, 1, 1};
+    outer.a[0] = AdapterOuterOperand{pack.g_out, x, (float*)(w + p.part_a), I, 1};
+    outer.a[1] = AdapterOuterOperand{pack.u_out, g_y, (float*)(w + p.part_b), O, 1};
     outer.scale = scale;
-    if (offsets) {
-      outer.order = order;
-      outer.start = start;
-      outer.first = first;
-    }
+    outer.first = pack.first;
+    outer.rows = pack.rows;
+    outer.pitch = p.pos_pitch;
     outer.rank = (int)rank;
     outer.parts = p.parts;
     HOT_STAGE(kStAdapterOuter, launch_adapter_outer(outer, type, s));

@@ -163,7 +163,7 @@ enum Stage {
   kStGyRowQuant2, kStGxGemm, kStGyTAbsmax, kStGyTQuant, kStGwGemm, kStWGyRow, kStGyFusedAbsmax,
   kStGyFusedQuant, kStCkptWrite, kStCkptRead, kStActForward, kStActBackward, kStNormForward, kStNormBackward,
   kStColumnSums, kStLinearOperands, kStLinear,
-  kStAdapterPrepare = 25, kStAdapterShrink, kStAdapterExpand, kStAdapterOuter, kStAdapterSums, kStLogProbs, kStLogProbsGrad, kStAdamW,
+  kStAdapterPrepare = 25, kStAdapterShrink, kStAdapterExpand, kStAdapterPack, kStAdapterOuter, kStAdapterSums, kStLogProbs, kStLogProbsGrad, kStAdamW,
   kStStateRead, kStStateWrite        // 24 has no name: those who read names up to an empty one keep their list
 };
 // A kernel's limit of dynamic LDS is each device's own: raised on the current one, once (again does no harm).  `done`: the kernel's,

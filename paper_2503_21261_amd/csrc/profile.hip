@@ -52,7 +52,7 @@ const char* const kStageNames[HOT_NUM_STAGES_ALL] = {
     "gyT_col_quant", "gw_igemm",       "w_and_gy_row_quant", "gy_fused_absmax", "gy_fused_quant",
     "checkpoint_write", "checkpoint_read", "activation", "activation_grad", "layer_norm", "layer_norm_grad",
     "column_sums", "linear_operands", "linear", "",
-    "adapter_prepare", "adapter_shrink", "adapter_expand", "adapter_outer", "adapter_sums", "token_logprobs", "token_logprobs_grad",
+    "adapter_prepare", "adapter_shrink", "adapter_expand", "adapter_pack", "adapter_outer", "adapter_sums", "token_logprobs", "token_logprobs_grad",
     "adamw", "adamw_state_read", "adamw_state_write"};
 
 }  // namespace hot
