@@ -30,6 +30,24 @@ template <class T> struct Frag;
 template <> struct Frag<bf16> { u4 v; };
 template <> struct Frag<float> { float v[8]; };
 
+// Eight elements of a row for each of four lanes, in loads of 64 consecutive bytes of it: bfloat16 as they lie, fp32 in two pieces of
+// four, 16 elements apart (the order of the reduced elements is free).
+template <class T> struct Piece;
+template <> struct Piece<bf16> { h8_any v; };
+template <> struct Piece<float> { f4_any v[2]; };
+__device__ __forceinline__ Piece<bf16> load_piece(const bf16* p) { return Piece<bf16>{*(const h8_any*)p}; }
+__device__ __forceinline__ Piece<float> load_piece(const float* p) { return Piece<float>{{*(const f4_any*)p, *(const f4_any*)(p + 16)}}; }
+__device__ __forceinline__ Frag<bf16> frag(const Piece<bf16>& r) { return Frag<bf16>{__builtin_bit_cast(u4, r.v)}; }
+__device__ __forceinline__ Frag<float> frag(const Piece<float>& r) {
+  Frag<float> f;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    f.v[e] = r.v[0][e];
+    f.v[4 + e] = r.v[1][e];
+  }
+  return f;
+}
+
 __device__ __forceinline__ f4 mma(const Frag<bf16>& a, const Frag<bf16>& b, f4 c) {
   return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(b8, a.v), __builtin_bit_cast(b8, b.v), c, 0, 0, 0);
 }
@@ -104,19 +122,20 @@ __device__ __forceinline__ Run run_at(const AdapterBatch& b, int64_t row, int64_
 }
 
 // ---- shrink ---------------------------------------------------------------------------------------
-// RT tiles of 16 ranks, R tiles of 16 rows; ROWS: rows that a wave takes (1, or 16 R).  A step is 128 bytes of each row.
-template <class T, int RT, int R, int ROWS>
+// RT tiles of 16 ranks, R tiles of 16 rows; ROWS: rows that a workgroup takes (1, or 16 R).  A step is 128 bytes of each row; the four waves
+// take steps in turn, DEPTH of them on their way, and join their sums through LDS.
+template <class T, int RT, int R, int ROWS, int DEPTH>
 __global__ __launch_bounds__(256) void shrink_kernel(const AdapterShrink a) {
-  constexpr int kStep = 128 / sizeof(T), kPer = kStep / 4, kFrags = kPer / 8;   // a lane's elements of a step, in fragments of 8
-  const int lane = threadIdx.x & 63, i = lane & 15, q = lane >> 4;
+  constexpr int kStep = 128 / sizeof(T), kFrags = kStep / 32, kPer = 16 / sizeof(T);
+  __shared__ f4 s_acc[3][RT * R][64];
+  const int lane = threadIdx.x & 63, i = lane & 15, q = lane >> 4, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int64_t tiles = (a.b.L + ROWS - 1) / ROWS;
-  const int64_t task = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-  const int slice = __builtin_amdgcn_readfirstlane((int)(task / tiles));
-  if (slice >= a.slices) return;
-  const int64_t row0 = (task - slice * tiles) * ROWS;
+  const int slice = (int)(blockIdx.x / tiles);
+  const int64_t row0 = (blockIdx.x - slice * tiles) * ROWS;
   const int64_t row1 = min(row0 + ROWS, a.b.L);
   const int64_t k0 = slice * a.slice, k1 = min(k0 + a.slice, a.K);
   float* const out = a.out + (int64_t)slice * a.b.L * a.pitch;
+  const int64_t first = k0 + wave * kStep, whole = k0 + (k1 - k0) / kStep * kStep;      // this wave's first step, the end of the whole ones
 
   for (int64_t row = row0; row < row1;) {
     const Run run = run_at(a.b, row, row1);
@@ -134,17 +153,16 @@ __global__ __launch_bounds__(256) void shrink_kernel(const AdapterShrink a) {
 #pragma unroll
         for (int r = 0; r < R; ++r) acc[t][r] = f4{0.0f, 0.0f, 0.0f, 0.0f};
       struct Step {
-        Raw8<T> x[R][kFrags], w[RT][kFrags];
+        Piece<T> x[R][kFrags], w[RT][kFrags];
       };
       const auto load = [&](int64_t at, Step& d) {
 #pragma unroll
-        for (int r = 0; r < R; ++r)
+        for (int f = 0; f < kFrags; ++f) {
 #pragma unroll
-          for (int f = 0; f < kFrags; ++f) d.x[r][f] = load8(x[r] + at + f * 8, 8);
+          for (int r = 0; r < R; ++r) d.x[r][f] = load_piece(x[r] + at + f * 32);
 #pragma unroll
-        for (int t = 0; t < RT; ++t)
-#pragma unroll
-          for (int f = 0; f < kFrags; ++f) d.w[t][f] = load8(wr[t] + at + f * 8, 8);
+          for (int t = 0; t < RT; ++t) d.w[t][f] = load_piece(wr[t] + at + f * 32);
+        }
       };
       const auto multiply = [&](const Step& d) {
 #pragma unroll
@@ -154,71 +172,174 @@ __global__ __launch_bounds__(256) void shrink_kernel(const AdapterShrink a) {
 #pragma unroll
             for (int t = 0; t < RT; ++t) acc[t][r] = mma(frag(d.w[t][f]), frag(d.x[r][f]), acc[t][r]);
       };
-      // Whole steps, the next one's loads on their way; the last one's once more instead of a branch around them, which would make
-      // the waits wait for all.
-      const int64_t k = k0 + (k1 - k0) / kStep * kStep;
-      if (k > k0) {
-        Step d0, d1;
-        load(k0, d0);
-        for (int64_t at = k0;; at += 2 * kStep) {
-          load(min(at + kStep, k - kStep), d1);
-          __builtin_amdgcn_sched_barrier(0);      // else the loads sink to where they are used
-          multiply(d0);
-          if (at + kStep >= k) break;
-          load(min(at + 2 * kStep, k - kStep), d0);
-          __builtin_amdgcn_sched_barrier(0);
-          multiply(d1);
-          if (at + 2 * kStep >= k) break;
-        }
-      }
-      if (k < k1) {     // the row's last elements: zeros behind them, on both sides
+      if (first < whole) {
+        // The last step's loads are made once more instead of a branch around them, which would make the waits wait for all.
+        constexpr int kTurn = 4 * kStep;
+        const int64_t last = first + (whole - 1 - first) / kTurn * kTurn;
+        Step d[DEPTH];
 #pragma unroll
-        for (int f = 0; f < kFrags; ++f) {
-          const int n = (int)max(min((int64_t)8, k1 - k - q * kPer - f * 8), (int64_t)0);
+        for (int s = 0; s < DEPTH - 1; ++s) load(min(first + s * kTurn, last), d[s]);
+        // Rounds of DEPTH steps without a way out of their middle, which would have the buffers copied at each round's end; what is left is
+        // loaded already.
+        int64_t at = first;
+        for (; at + (DEPTH - 1) * kTurn <= last; at += DEPTH * kTurn) {
+#pragma unroll
+          for (int s = 0; s < DEPTH; ++s) {
+            load(min(at + (s + DEPTH - 1) * kTurn, last), d[(s + DEPTH - 1) % DEPTH]);
+            __builtin_amdgcn_sched_barrier(0);      // else the loads sink to where they are used
+            multiply(d[s]);
+            __builtin_amdgcn_sched_barrier(0);
+          }
+        }
+#pragma unroll
+        for (int s = 0; s < DEPTH - 1; ++s)
+          if (at + s * kTurn <= last) multiply(d[s]);
+      }
+      if (whole < k1 && wave == 3) {              // the row's last elements: zeros behind them, on both sides
+        for (int64_t at = whole; at < k1; at += 32) {
+          const int n = (int)max(min((int64_t)8, k1 - at - q * 8), (int64_t)0);
+          const int64_t by = at + q * (8 - kPer);
 #pragma unroll
           for (int r = 0; r < R; ++r) {
-            const Frag<T> fx = frag(load8(x[r] + k + f * 8, n));
+            const Frag<T> fx = frag(load8(x[r] + by, n));
 #pragma unroll
-            for (int t = 0; t < RT; ++t) acc[t][r] = mma(frag(load8(wr[t] + k + f * 8, n)), fx, acc[t][r]);
+            for (int t = 0; t < RT; ++t) acc[t][r] = mma(frag(load8(wr[t] + by, n)), fx, acc[t][r]);
           }
         }
       }
-      // Lane (i, q) has ranks 16 t + 4 q .. + 3 of row i.
+      if (wave > 0) {
 #pragma unroll
-      for (int r = 0; r < R; ++r) {
-        const int64_t l = row0 + r * 16 + i;
-        if (l >= row && l < run.end) {
+        for (int t = 0; t < RT; ++t)
+#pragma unroll
+          for (int r = 0; r < R; ++r) s_acc[wave - 1][t * R + r][lane] = acc[t][r];
+      }
+      __syncthreads();
+      // Lane (i, q) has ranks 16 t + 4 q .. + 3 of row i.
+      if (wave == 0) {
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+          const int64_t l = row0 + r * 16 + i;
 #pragma unroll
           for (int t = 0; t < RT; ++t) {
             const int j = t * 16 + q * 4;
-            f4 v;
+            f4 v = acc[t][r];
 #pragma unroll
-            for (int e = 0; e < 4; ++e) v[e] = j + e < a.rank ? acc[t][r][e] : 0.0f;
-            if (j < a.pitch) *(f4*)(out + l * a.pitch + j) = v;
+            for (int o = 0; o < 3; ++o) {
+              const f4 other = s_acc[o][t * R + r][lane];
+#pragma unroll
+              for (int e = 0; e < 4; ++e) v[e] += other[e];
+            }
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[e] = j + e < a.rank ? v[e] : 0.0f;
+            if (l >= row && l < run.end && j < a.pitch) *(f4*)(out + l * a.pitch + j) = v;
+            if (a.u && l >= row && l < run.end) {
+#pragma unroll
+              for (int e = 0; e < 4; ++e)
+                if (j + e < a.rank) a.u[l * a.rank + j + e] = v[e];
+            }
           }
         }
       }
+      __syncthreads();
+    } else if (run.adapter == -1 && a.u) {
+      for (int64_t at = row * a.rank + threadIdx.x; at < run.end * a.rank; at += 256) a.u[at] = 0.0f;
     }
     row = run.end;
   }
 }
 
+// 16 bytes of a row, and their sums with the factors of a lane's columns.
+template <class T> struct Vec16;
+template <> struct Vec16<bf16> { h8_any v; };
+template <> struct Vec16<float> { f4_any v; };
+__device__ __forceinline__ Vec16<bf16> load16(const bf16* p) { return Vec16<bf16>{*(const h8_any*)p}; }
+__device__ __forceinline__ Vec16<float> load16(const float* p) { return Vec16<float>{*(const f4_any*)p}; }
+__device__ __forceinline__ Vec16<bf16> sum16(const Vec16<bf16>& b, f4 lo, f4 hi) {
+  Vec16<bf16> r;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) r.v[e] = float_to_bf16(bf16_to_float(b.v[e]) + (e < 4 ? lo[e & 3] : hi[e & 3]));
+  return r;
+}
+__device__ __forceinline__ Vec16<float> sum16(const Vec16<float>& b, f4 lo, f4) {
+  Vec16<float> r;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) r.v[e] = b.v[e] + lo[e];
+  return r;
+}
+template <class T>
+__device__ __forceinline__ void store16(T* p, const Vec16<T>& v) { *(std::remove_cv_t<decltype(v.v)>*)p = v.v; }
+
+// Rows row .. end - 1 of one adapter and 64 columns from n on: tiles of 16 rows, DEPTH of them on their way.  Nothing here branches but the
+// loop, so that a wait is for one tile and not for all.  (The streaming hint on y: 140 us for 130, reading and writing 16384 x 11008.)
+template <class T, int PIECES, int CHUNKS, int DEPTH, bool BASE, class F>
+__device__ __forceinline__ void expand_rows(const AdapterExpand& a, int64_t end, int64_t row, int64_t n, const int (&jw)[CHUNKS], const F& product) {
+  constexpr bool kSingle = sizeof(T) == 4;
+  constexpr int kPer = 16 / sizeof(T);
+  typedef Vec16<T> V;
+  const int lane = threadIdx.x & 63, i = lane & 15, q = lane >> 4;
+  struct Tile {
+    V base[PIECES];
+    Raw8<float> p[CHUNKS];
+  };
+  const auto load = [&](int64_t at, Tile& d) {
+    const int64_t l = min(at + i, end - 1);
+    if constexpr (BASE) {
+#pragma unroll
+      for (int h = 0; h < PIECES; ++h) d.base[h] = load16((const T*)a.base + l * a.N + n + q * kPer + h * 4 * kPer);
+    }
+#pragma unroll
+    for (int c = 0; c < CHUNKS; ++c) d.p[c] = load8(a.p + l * a.pitch + jw[c], 8);
+  };
+  // Rows past the end are the last one's once more, the same sums, stored by several lanes.
+  const auto finish = [&](int64_t at, const Tile& d) {
+    const int64_t l = min(at + i, end - 1);
+    f4 acc[4];
+#pragma unroll
+    for (int t = 0; t < 4; ++t) acc[t] = f4{0.0f, 0.0f, 0.0f, 0.0f};
+    product(d.p, acc);
+    T* const to = (T*)a.y + l * a.N + n + q * kPer;
+#pragma unroll
+    for (int h = 0; h < PIECES; ++h)
+      store16(to + h * 4 * kPer, sum16(BASE ? d.base[h] : V{}, acc[kSingle ? h : 2 * h], acc[kSingle ? h : 2 * h + 1]));
+  };
+  // The tile that is loaded again past the last one is never used, so that y may be base.
+  const int64_t last = row + (end - 1 - row) / 16 * 16;
+  Tile d[DEPTH];
+#pragma unroll
+  for (int s = 0; s < DEPTH - 1; ++s) load(min(row + s * 16, last), d[s]);
+  int64_t at = row;
+  for (; at + (DEPTH - 1) * 16 <= last; at += DEPTH * 16) {
+#pragma unroll
+    for (int s = 0; s < DEPTH; ++s) {
+      load(min(at + (s + DEPTH - 1) * 16, last), d[(s + DEPTH - 1) % DEPTH]);
+      __builtin_amdgcn_sched_barrier(0);
+      finish(at + s * 16, d[s]);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+  }
+#pragma unroll
+  for (int s = 0; s < DEPTH - 1; ++s)
+    if (at + s * 16 <= last) finish(at + s * 16, d[s]);
+}
+
 // ---- expand ---------------------------------------------------------------------------------------
 // RC chunks of 32 ranks (0: at most 16 ranks; the chunk's second half is the second part of the same ranks).
-// A wave's step is 64 columns: tile t of the four has columns 16 (m / 4) + 4 t + m % 4 in its row m, so that a lane ends with 16
-// columns in a row of its row.
-template <class T, int RC, int R, int ROWS>
-__global__ __launch_bounds__(256, 2) void expand_kernel(const AdapterExpand a, int64_t span) {
+// A wave holds the factors of 64 columns and goes over the rows, DEPTH tiles of 16 of them on their way; the four waves of a workgroup are
+// side by side.  A lane has its columns in pieces of 16 bytes, four lanes 64 bytes in a row: fp32 in the order of the four tiles of
+// 16; bfloat16 with the columns 8 (m / 4) + 4 (t % 2) + m % 4 of half t / 2 in row m of tile t, so that two tiles make a piece.
+template <class T, int RC, int DEPTH>
+__global__ __launch_bounds__(256) void expand_kernel(const AdapterExpand a, int col_groups, int64_t chunk) {
   constexpr bool kSingle = sizeof(T) == 4, kPack = RC == 0 && !kSingle;
   constexpr int kChunks = RC == 0 ? 1 : RC, kParts = kSingle || kPack ? 1 : 2;
-  const int lane = threadIdx.x & 63, i = lane & 15, q = lane >> 4;
-  const int64_t tiles = (a.b.L + ROWS - 1) / ROWS;
-  const int64_t task = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-  const int64_t cut = task / tiles;
-  const int64_t n0 = cut * span, n1 = min(n0 + span, a.N);
-  if (n0 >= a.N) return;
-  const int64_t row0 = (task - cut * tiles) * ROWS;
-  const int64_t row1 = min(row0 + ROWS, a.b.L);
+  constexpr int kPer = 16 / sizeof(T), kPieces = sizeof(T);       // a lane's pieces of 16 bytes of 64 columns: 4 or 2
+  typedef Vec16<T> V;
+  const int lane = threadIdx.x & 63, i = lane & 15, q = lane >> 4, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int group = (int)(blockIdx.x % col_groups);
+  const int64_t n = (int64_t)group * 256 + wave * 64;
+  if (n >= a.N) return;
+  const bool whole = n + 64 <= a.N;
+  const int64_t row0 = (int64_t)(blockIdx.x / col_groups) * chunk, row1 = min(row0 + chunk, a.b.L);
+  const bool writes_u = a.u && group == 0 && wave == 0;
   const int j0 = kPack ? (q & 1) * 8 : q * 8;      // this lane's ranks within a chunk
 
   for (int64_t row = row0; row < row1;) {
@@ -229,117 +350,104 @@ __global__ __launch_bounds__(256, 2) void expand_kernel(const AdapterExpand a, i
     }
     const bool none = run.adapter < 0;
     const float scale = none ? 0.0f : a.scale ? a.scale[run.adapter] : 1.0f;
-    Frag<T> p[R][kChunks][kParts];
-    bool mine[R];
+    // A row's last ranks are loaded as its last eight: p as they are, with zeros for those that another lane has.
+    int jw[kChunks];
 #pragma unroll
-    for (int r = 0; r < R; ++r) {
-      const int64_t l = min(max(row0 + r * 16 + i, row), run.end - 1);
-      mine[r] = row0 + r * 16 + i >= row && row0 + r * 16 + i < run.end;
+    for (int c = 0; c < kChunks; ++c) jw[c] = a.w_cols < 8 ? 0 : min(c * 32 + j0, a.w_cols - 8);
+    Frag<T> fw[4][kChunks];
+    if (!none) {
+      const T* const w = (const T*)a.w + run.adapter * a.w_stride;
+#pragma unroll
+      for (int t = 0; t < 4; ++t) {
+        const int64_t wn = min(n + (kSingle ? t * 16 + i : t / 2 * 32 + (i >> 2) * 8 + t % 2 * 4 + (i & 3)), a.N - 1);
+#pragma unroll
+        for (int c = 0; c < kChunks; ++c) fw[t][c] = frag(load8(w + wn * a.w_pitch + jw[c], RC == 0 ? min(a.w_cols, 8) : 8));
+      }
+    }
+    const auto product = [&](const Raw8<float> (&p)[kChunks], f4 (&acc)[4]) {
 #pragma unroll
       for (int c = 0; c < kChunks; ++c) {
-        // The weights' last ranks are loaded as a row's last eight: p as they are, zeros for those that another lane has.
-        const int j = c * 32 + j0, at = a.w_cols < 8 ? min(j, 0) : min(j, a.w_cols - 8);
-        float v[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
-        if (!none) {
-          for (int s = 0; s < a.slices; ++s) {
-            float w[8];
-            load_values(a.p + ((int64_t)s * a.b.L + l) * a.pitch + at, 8, w);
+        float v[8];
+        widen(p[c], v);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) v[e] += w[e];
-          }
-#pragma unroll
-          for (int e = 0; e < 8; ++e) v[e] = at + e >= j ? v[e] : 0.0f;
-        }
-        if (a.u && n0 == 0 && mine[r] && !(kPack && q >= 2)) {
-          for (int e = 0; e < 8; ++e)
-            if (at + e >= j && at + e < a.rank) a.u[l * a.rank + at + e] = v[e];
-        }
-#pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] *= scale;
+        for (int e = 0; e < 8; ++e) v[e] = (jw[c] + e >= c * 32 + j0 ? v[e] : 0.0f) * scale;
+        Frag<T> f[kParts];
         if constexpr (kSingle) {
 #pragma unroll
-          for (int e = 0; e < 8; ++e) p[r][c][0].v[e] = v[e];
+          for (int e = 0; e < 8; ++e) f[0].v[e] = v[e];
         } else if constexpr (kPack) {
           Frag<bf16> two[2];
           split8<2>(v, two);
-          p[r][c][0] = q < 2 ? two[0] : two[1];
+          f[0] = q < 2 ? two[0] : two[1];
         } else {
-          split8<2>(v, p[r][c]);
-        }
-      }
-    }
-    // Factors of 16 columns a lane, from n on; past the last column the last one's.
-    const T* const w = (const T*)a.w + (none ? 0 : run.adapter * a.w_stride);
-    const auto product = [&](int64_t n, auto tail, f4 (&acc)[4][R]) {
-#pragma unroll
-      for (int t = 0; t < 4; ++t)
-#pragma unroll
-        for (int r = 0; r < R; ++r) acc[t][r] = f4{0.0f, 0.0f, 0.0f, 0.0f};
-      if (none) return;
-#pragma unroll
-      for (int c = 0; c < kChunks; ++c) {
-        const int j = c * 32 + j0;
-        Raw8<T> fw[4];
-#pragma unroll
-        for (int t = 0; t < 4; ++t) {
-          int64_t wn = n + (i >> 2) * 16 + t * 4 + (i & 3);
-          if (decltype(tail)::value) wn = min(wn, a.N - 1);
-          if (RC == 0 && a.w_cols < 8) fw[t] = load8(w + wn * a.w_pitch + j, min(max(a.w_cols - j, 0), 8));
-          else fw[t] = load8(w + wn * a.w_pitch + min(j, a.w_cols - 8), 8);
+          split8<2>(v, f);
         }
 #pragma unroll
-        for (int t = 0; t < 4; ++t)
+        for (int part = 0; part < kParts; ++part)
 #pragma unroll
-          for (int r = 0; r < R; ++r)
-#pragma unroll
-            for (int part = 0; part < kParts; ++part) acc[t][r] = mma(frag(fw[t]), p[r][c][part], acc[t][r]);
+          for (int t = 0; t < 4; ++t) acc[t] = mma(fw[t][c], f[part], acc[t]);
       }
     };
-    const T* from[R];
-    T* to[R];
-#pragma unroll
-    for (int r = 0; r < R; ++r) {
-      const int64_t l = min(max(row0 + r * 16 + i, row), run.end - 1);
-      from[r] = (const T*)a.base + l * a.N + q * 16;
-      to[r] = (T*)a.y + l * a.N + q * 16;
+    if (whole && !none && a.slices == 1 && run.end - row >= 16 * DEPTH) {
+      if (a.base) expand_rows<T, kPieces, kChunks, DEPTH, true>(a, run.end, row, n, jw, product);
+      else expand_rows<T, kPieces, kChunks, DEPTH, false>(a, run.end, row, n, jw, product);
+      row = run.end;
+      continue;
     }
-    int64_t n = n0;
-    for (; n + 64 <= n1; n += 64) {
-      Raw8<T> base[R][2];
+    for (int64_t at = row; at < run.end; at += 16) {       // few rows, rows without an adapter, the last columns
+      const int64_t l = min(at + i, run.end - 1);
+      f4 acc[4];
 #pragma unroll
-      for (int r = 0; r < R; ++r)
+      for (int t = 0; t < 4; ++t) acc[t] = f4{0.0f, 0.0f, 0.0f, 0.0f};
+      V have[kPieces];
+      if (whole && a.base) {
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          if (a.base) base[r][h] = load8(from[r] + n + h * 8, 8);
-          else base[r][h] = Raw8<T>{};
-        }
-      f4 acc[4][R];
-      product(n, std::false_type{}, acc);
+        for (int h = 0; h < kPieces; ++h) have[h] = load16((const T*)a.base + l * a.N + n + q * kPer + h * 4 * kPer);
+      } else {
 #pragma unroll
-      for (int r = 0; r < R; ++r) {
-        if (!mine[r]) continue;
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          float v[8];
-          widen(base[r][h], v);
-#pragma unroll
-          for (int e = 0; e < 8; ++e) v[e] += acc[h * 2 + e / 4][r][e & 3];
-          if (a.stream) store8<true>(to[r] + n + h * 8, v, 8);
-          else store8(to[r] + n + h * 8, v, 8);
-        }
+        for (int h = 0; h < kPieces; ++h) have[h] = V{};
       }
-    }
-    if (n < n1) {       // the last columns, one by one
-      f4 acc[4][R];
-      product(n, std::true_type{}, acc);
+      if (!none) {
+        Raw8<float> p[kChunks];
 #pragma unroll
-      for (int r = 0; r < R; ++r)
+        for (int c = 0; c < kChunks; ++c) p[c] = load8(a.p + l * a.pitch + jw[c], 8);
+#pragma unroll 4
+        for (int s = 1; s < a.slices; ++s) {
+#pragma unroll
+          for (int c = 0; c < kChunks; ++c) {
+            const Raw8<float> more = load8(a.p + ((int64_t)s * a.b.L + l) * a.pitch + jw[c], 8);
+            p[c].a += more.a;
+            p[c].b += more.b;
+          }
+        }
+        product(p, acc);
+        if (writes_u && at + i < run.end && !(kPack && q >= 2)) {
+#pragma unroll
+          for (int c = 0; c < kChunks; ++c) {
+            float v[8];
+            widen(p[c], v);
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+              if (jw[c] + e >= c * 32 + j0 && jw[c] + e < a.rank) a.u[l * a.rank + jw[c] + e] = v[e];
+          }
+        }
+      } else if (writes_u && at + i < run.end) {
+        for (int j = q; j < a.rank; j += 4) a.u[l * a.rank + j] = 0.0f;
+      }
+      if (at + i >= run.end) continue;
+      T* const to = (T*)a.y + l * a.N + n + q * kPer;
+      if (whole) {
+#pragma unroll
+        for (int h = 0; h < kPieces; ++h)
+          store16(to + h * 4 * kPer, sum16(have[h], acc[kSingle ? h : 2 * h], acc[kSingle ? h : 2 * h + 1]));
+      } else {                // one by one
+        const T* const from = (const T*)a.base + l * a.N + n + q * kPer;
 #pragma unroll
         for (int e = 0; e < 16; ++e) {
-          if (!mine[r] || n + q * 16 + e >= n1) continue;
-          const float v = acc[e / 4][r][e & 3] + (a.base ? (float)from[r][n + e] : 0.0f);
-          to[r][n + e] = (T)v;
+          const int c = kSingle ? e / 4 * 16 + e % 4 : e / 8 * 32 + e % 8;
+          if (n + q * kPer + c < a.N) to[c] = (T)(acc[e / 4][e & 3] + (a.base ? (float)from[c] : 0.0f));
         }
+      }
     }
     row = run.end;
   }
@@ -512,8 +620,8 @@ __global__ __launch_bounds__(256) void pack_kernel(const AdapterPack a) {
       }
       lo = min(lo, a.b.segments - 1);
       row = min(max((int64_t)a.b.offsets[a.order[lo]] + pos - a.start[lo], (int64_t)0), a.b.L - 1);
-      if (!second) a.rows[pos0 + tid] = (int)row;
     }
+    if (!second) a.rows[pos0 + tid] = (int)row;
     s_row[tid] = (int)row;
   }
   __syncthreads();
@@ -550,7 +658,8 @@ constexpr int kOuterCols = 128, kOuterWaves = 4;    // columns of a wave, waves 
 
 // A wave: 128 columns, up to 64 ranks, one part of the rows that have adapters, in steps of 32, the next step's loads on their way.
 // The waves of a workgroup share the rows' factors in the first cache.  Sums over rows leave as one partial sum a part and adapter.
-template <class T, int RT>
+// MODE: 0 all rows as they lie, 1 in the order of a.rows, 2 too, with fewer than eight columns in one of the products.
+template <class T, int RT, int MODE>
 __global__ __launch_bounds__(64 * kOuterWaves) void outer_kernel(const AdapterOuter a, int tiles_first, int tiles, int rank_blocks) {
   constexpr int kParts = sizeof(T) == 4 ? 1 : 3;
   const int lane = threadIdx.x & 63, i = lane & 15, q = lane >> 4, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -561,8 +670,9 @@ __global__ __launch_bounds__(64 * kOuterWaves) void outer_kernel(const AdapterOu
   const int64_t col0 = ((int64_t)(second ? tile - tiles_first : tile) * kOuterWaves + wave) * kOuterCols;
   if (col0 >= o.N) return;
   // Columns past the last one: the last eight once more, which come out the same.
-  const int64_t col = o.N < 8 ? col0 + i * 8 : min(col0 + i * 8, o.N - 8);
-  const int have = o.N < 8 ? (int)max(min((int64_t)8, o.N - col), (int64_t)0) : 8;
+  const bool narrow = MODE == 2 && o.N < 8;
+  const int64_t col = narrow ? col0 + i * 8 : min(col0 + i * 8, o.N - 8);
+  const int have = narrow ? (int)max(min((int64_t)8, o.N - col), (int64_t)0) : 8;
   const int64_t total = a.first ? max(min((int64_t)a.first[a.b.adapters], a.b.L), (int64_t)0) : a.b.L;
   const int64_t per = rows_of_part(total, a.parts);
   const int64_t hi = min(per * (part + 1), total);
@@ -588,14 +698,14 @@ __global__ __launch_bounds__(64 * kOuterWaves) void outer_kernel(const AdapterOu
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
         const int64_t l = min(at + q * 8 + e, k_end - 1);
-        r[e] = a.first ? a.rows[l] : (int)l;
+        r[e] = MODE ? a.rows[l] : (int)l;
       }
     };
     const auto load = [&](const int (&r)[8], Raw8<T> (&x)[8]) {
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
         const T* const from = (const T*)o.q + (int64_t)r[e] * o.N + col;
-        if (o.N < 8) x[e] = load8(from, have);
+        if (narrow) x[e] = load8(from, have);
         else x[e] = load8(from, 8);
       }
     };
@@ -631,18 +741,18 @@ __global__ __launch_bounds__(64 * kOuterWaves) void outer_kernel(const AdapterOu
     load(r0, x0);
 #pragma unroll
     for (int t = 0; t < RT; ++t) load_p(t, pos);
-    for (;; pos += 64) {
+    int64_t at = pos;
+    for (; at + 32 <= last; at += 64) {
       load(r1, x1);
-      rows_at(min(pos + 64, last), r0);
+      rows_at(min(at + 64, last), r0);
       __builtin_amdgcn_sched_barrier(0);
-      multiply(pos, x0);
-      if (pos >= last) break;
+      multiply(at, x0);
       load(r0, x0);
-      rows_at(min(pos + 96, last), r1);
+      rows_at(min(at + 96, last), r1);
       __builtin_amdgcn_sched_barrier(0);
-      multiply(pos + 32, x1);
-      if (pos + 32 >= last) break;
+      multiply(at + 32, x1);
     }
+    if (at <= last) multiply(at, x0);
     pos = k_end;
     // Lane (i, q) has ranks 16 t + 4 q + e of its eight columns.
     const float scale = o.scaled && a.scale ? a.scale[k] : 1.0f;
@@ -662,81 +772,73 @@ __global__ __launch_bounds__(64 * kOuterWaves) void outer_kernel(const AdapterOu
   }
 }
 
-// Sums of the parts of each adapter, in order; part p of adapter k is slot p + k.  Blocks of g_A: 1024 columns of one rank.  Blocks of g_B: 64
-// columns, all ranks, transposed through LDS.
-__global__ __launch_bounds__(256) void reduce_kernel(const AdapterReduce a, int tiles_a, int tiles) {
-  __shared__ float s_tile[64 * (kMaxRank + 1)];
-  const int k = blockIdx.x / tiles, tile = blockIdx.x % tiles, tid = threadIdx.x;
+// Sums of the parts of each adapter, in order; part p of adapter k is slot p + k.  A workgroup: 64 columns of 4 / G ranks, the parts of
+// each in G runs of lanes that are joined through LDS.
+template <int G>
+__global__ __launch_bounds__(256) void reduce_kernel(const AdapterReduce a, int tiles_a, int tiles, int ranks) {
+  constexpr int kRanks = 4 / G;
+  __shared__ float s_sum[4][64];
+  const int tid = threadIdx.x, x = tid & 63, y = tid >> 6;
+  const int k = blockIdx.x / (tiles * ranks), in = blockIdx.x % (tiles * ranks), tile = in / ranks;
+  const int j0 = in % ranks * kRanks, j = j0 + y / G;
   const int64_t total = a.first ? max(min((int64_t)a.first[a.adapters], a.L), (int64_t)0) : a.L;
   const int64_t lo = a.first ? a.first[k] : (k == 0 ? 0 : total), hi = a.first ? a.first[k + 1] : total;
   const int64_t per = rows_of_part(total, a.parts);         // the parts that hold rows of this adapter
   const int p0 = lo < hi ? (int)(lo / per) : 0, p1 = lo < hi ? (int)min((hi + per - 1) / per, (int64_t)a.parts) : 0;
-  if (tile < tiles_a) {
-    const int spans = (int)((a.I + 1023) / 1024), j = tile / spans;
-    const int64_t n = (int64_t)(tile % spans) * 1024 + tid * 4;
-    const int have = (int)max(min((int64_t)4, a.I - n), (int64_t)0);
-    float v[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-    for (int p = p0; p < p1; ++p) {
-      const float* const from = a.part_a + ((int64_t)(p + k) * a.rank + j) * a.I + n;
-      if (have == 4) {
-        const f4_any x = *(const f4_any*)from;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) v[i] += x[i];
-      } else {
-        for (int i = 0; i < have; ++i) v[i] += from[i];
-      }
-    }
-    float* const to = a.g_a + ((int64_t)k * a.rank + j) * a.I + n;
-    for (int i = 0; i < have; ++i) to[i] = v[i];
-    return;
+  const int run = (p1 - p0 + G - 1) / G, b = p0 + y % G * run, e = min(b + run, p1);
+  const bool second = tile >= tiles_a;
+  const int64_t N = second ? a.O : a.I, n0 = (int64_t)(second ? tile - tiles_a : tile) * 64, n = n0 + x;
+  float v = 0.0f;
+  if (n < N && j < a.rank) {
+    const float* from = (second ? a.part_b : a.part_a) + ((int64_t)(b + k) * a.rank + j) * N + n;
+#pragma unroll 8
+    for (int p = b; p < e; ++p, from += a.rank * N) v += *from;
   }
-  const int64_t n0 = (int64_t)(tile - tiles_a) * 64, n = n0 + (tid & 63);
-  const int pitch = a.rank | 1;
-  for (int j = tid >> 6; j < a.rank; j += 4) {
-    float v = 0.0f;
-    if (n < a.O) {
-      for (int p = p0; p < p1; ++p) v += a.part_b[((int64_t)(p + k) * a.rank + j) * a.O + n];
-    }
-    s_tile[(tid & 63) * pitch + j] = v;
-  }
+  s_sum[y][x] = v;
   __syncthreads();
-  const int held = (int)min((int64_t)64, a.O - n0) * a.rank;
-  float* const to = a.g_b + ((int64_t)k * a.O + n0) * a.rank;
-  for (int i = tid; i < held; i += 256) to[i] = s_tile[i / a.rank * pitch + i % a.rank];
+  if (second) {             // [n][rank]: a column's ranks side by side
+    const int c = tid / kRanks, r = tid % kRanks;
+    if (tid < 64 * kRanks && n0 + c < N && j0 + r < a.rank) {
+      float t = 0.0f;
+#pragma unroll
+      for (int g = 0; g < G; ++g) t += s_sum[r * G + g][c];
+      a.g_b[((int64_t)k * N + n0 + c) * a.rank + j0 + r] = t;
+    }
+  } else if (y < kRanks && n < N && j0 + y < a.rank) {
+    float t = 0.0f;
+#pragma unroll
+    for (int g = 0; g < G; ++g) t += s_sum[y * G + g][x];
+    a.g_a[((int64_t)k * a.rank + j0 + y) * N + n] = t;
+  }
 }
 
 template <class T, int RT>
-hipError_t run_shrink(const AdapterShrink& a, bool rows, hipStream_t s) {
-  if (rows) {
-    const int64_t tasks = a.b.L * a.slices;
-    shrink_kernel<T, RT, 1, 1><<<(uint32_t)ceil_div(tasks, 4), 256, 0, s>>>(a);
-  } else {
-    const int64_t tasks = ceil_div(a.b.L, 32) * a.slices;
-    shrink_kernel<T, RT, 2, 32><<<(uint32_t)ceil_div(tasks, 4), 256, 0, s>>>(a);
-  }
+hipError_t run_shrink(const AdapterShrink& a, int tile, hipStream_t s) {
+  constexpr int kDepth = RT <= 2 ? 4 : RT == 4 ? 3 : 2;     // as the registers of two waves allow
+  const uint32_t grid = (uint32_t)(ceil_div(a.b.L, tile) * a.slices);
+  if (tile == 1) shrink_kernel<T, RT, 1, 1, kDepth><<<grid, 256, 0, s>>>(a);
+  else if (tile == 16 || RT == 8) shrink_kernel<T, RT, 1, 16, kDepth><<<grid, 256, 0, s>>>(a);
+  else shrink_kernel<T, RT, 2, 32, kDepth><<<grid, 256, 0, s>>>(a);
   return hipGetLastError();
 }
 template <class T>
-hipError_t shrink_of(const AdapterShrink& a, bool rows, hipStream_t s) {
-  if (a.rank <= 16) return run_shrink<T, 1>(a, rows, s);
-  if (a.rank <= 32) return run_shrink<T, 2>(a, rows, s);
-  if (a.rank <= 64) return run_shrink<T, 4>(a, rows, s);
-  return run_shrink<T, 8>(a, rows, s);
+hipError_t shrink_of(const AdapterShrink& a, int tile, hipStream_t s) {
+  if (a.rank <= 16) return run_shrink<T, 1>(a, tile, s);
+  if (a.rank <= 32) return run_shrink<T, 2>(a, tile, s);
+  if (a.rank <= 64) return run_shrink<T, 4>(a, tile, s);
+  return run_shrink<T, 8>(a, tile, s);
 }
 
-// Waves that an expansion is cut into where its rows alone are fewer.
-constexpr int64_t kExpandWaves = 4096;
+// Workgroups of an expansion of many rows.
+constexpr int64_t kExpandGroups = 1024;
 
 template <class T, int RC>
 hipError_t run_expand(const AdapterExpand& a, bool rows, hipStream_t s) {
-  constexpr int R = RC == 4 ? 1 : 2;      // the factors of 128 ranks take the registers of a second tile
-  const int64_t tiles = rows ? a.b.L : ceil_div(a.b.L, 16 * R), steps = ceil_div(a.N, 64);
-  int64_t cuts = ceil_div(kExpandWaves, tiles);
-  if (cuts > steps) cuts = steps;
-  const int64_t span = ceil_div(steps, cuts) * 64;
-  const int64_t tasks = tiles * ceil_div(a.N, span);
-  if (rows) expand_kernel<T, RC, 1, 1><<<(uint32_t)ceil_div(tasks, 4), 256, 0, s>>>(a, span);
-  else expand_kernel<T, RC, R, 16 * R><<<(uint32_t)ceil_div(tasks, 4), 256, 0, s>>>(a, span);
+  constexpr int kDepth = RC <= 2 ? 3 : 2;
+  const int64_t groups = ceil_div(a.N, 256);
+  const int64_t chunk = rows ? 1 : round_up(ceil_div(a.b.L * groups, kExpandGroups), 16);
+  const uint32_t grid = (uint32_t)(groups * ceil_div(a.b.L, chunk));
+  expand_kernel<T, RC, kDepth><<<grid, 256, 0, s>>>(a, (int)groups, chunk);
   return hipGetLastError();
 }
 template <class T>
@@ -753,9 +855,10 @@ hipError_t outer_of(const AdapterOuter& a, hipStream_t s) {
   const int tiles_first = (int)ceil_div(a.a[0].N, kCols), tiles = tiles_first + (int)ceil_div(a.a[1].N, kCols);
   const int blocks = (int)ceil_div(a.rank, 64);
   const uint32_t grid = (uint32_t)((int64_t)tiles * blocks * a.parts);
-  if (a.rank <= 16) outer_kernel<T, 1><<<grid, 64 * kOuterWaves, 0, s>>>(a, tiles_first, tiles, blocks);
-  else if (a.rank <= 32) outer_kernel<T, 2><<<grid, 64 * kOuterWaves, 0, s>>>(a, tiles_first, tiles, blocks);
-  else outer_kernel<T, 4><<<grid, 64 * kOuterWaves, 0, s>>>(a, tiles_first, tiles, blocks);
+  const auto run = [&](auto kernel) { kernel<<<grid, 64 * kOuterWaves, 0, s>>>(a, tiles_first, tiles, blocks); };
+  if (a.a[0].N < 8 || a.a[1].N < 8) run(outer_kernel<T, 4, 2>);
+  else if (a.first) a.rank <= 16 ? run(outer_kernel<T, 1, 1>) : a.rank <= 32 ? run(outer_kernel<T, 2, 1>) : run(outer_kernel<T, 4, 1>);
+  else a.rank <= 16 ? run(outer_kernel<T, 1, 0>) : a.rank <= 32 ? run(outer_kernel<T, 2, 0>) : run(outer_kernel<T, 4, 0>);
   return hipGetLastError();
 }
 
@@ -767,14 +870,15 @@ AdapterPlan adapter_plan(hot_type type, int64_t L, int64_t O, int64_t I, int64_t
   p.rows = L <= 4 * (segments > 0 ? segments : 1) && L <= 1 << 20;
   p.pitch = (int)round_up(rank, 8);      // zeros behind the ranks
   p.rank_pitch = (int)round_up(rank, 8);
+  // Rows of a workgroup: as many as leave workgroups for all compute units without slices, 16 at least.
+  p.tile = p.rows ? 1 : L >= 64 * 32 && rank <= 64 ? 32 : 16;
   const auto slices = [&](int64_t K, int& count, int64_t& slice) {
-    const int64_t tiles = p.rows ? L : ceil_div(L, 32);
-    int64_t n = 2048 / tiles;
-    const int64_t most = ceil_div(K, 4 * step);
+    int64_t n = 512 / ceil_div(L, p.tile);
+    const int64_t most = ceil_div(K, 4 * step);      // a step for each wave
     if (n > most) n = most;
     if (n > kMaxSlices) n = kMaxSlices;
     if (n < 1) n = 1;
-    slice = round_up(ceil_div(K, n), step);
+    slice = round_up(ceil_div(K, n), 4 * step);
     count = (int)ceil_div(K, slice);
   };
   slices(I, p.slices_forward, p.slice_forward);
@@ -795,7 +899,7 @@ AdapterPlan adapter_plan(hot_type type, int64_t L, int64_t O, int64_t I, int64_t
   };
   p.at = take(adapters * I * p.rank_pitch * size);
   p.wt = take(adapters * rank * O * size);
-  p.sorted = take((2 * segments + 1 + adapters + 1 + (segments ? p.pos_pitch : 0)) * 4);
+  p.sorted = take((2 * segments + 1 + adapters + 1 + p.pos_pitch) * 4);
   p.packed = take(2 * (type == HOT_BF16 ? 3 : 1) * size * round_up(rank, 16) * p.pos_pitch);
   p.part_a = take((p.parts + adapters) * rank * I * 4);
   p.part_b = take((p.parts + adapters) * rank * O * 4);
@@ -803,8 +907,8 @@ AdapterPlan adapter_plan(hot_type type, int64_t L, int64_t O, int64_t I, int64_t
   return p;
 }
 
-hipError_t launch_adapter_shrink(const AdapterShrink& a, bool rows, hot_type type, hipStream_t s) {
-  return type == HOT_BF16 ? shrink_of<bf16>(a, rows, s) : shrink_of<float>(a, rows, s);
+hipError_t launch_adapter_shrink(const AdapterShrink& a, int tile, hot_type type, hipStream_t s) {
+  return type == HOT_BF16 ? shrink_of<bf16>(a, tile, s) : shrink_of<float>(a, tile, s);
 }
 hipError_t launch_adapter_expand(const AdapterExpand& a, bool rows, hot_type type, hipStream_t s) {
   return type == HOT_BF16 ? expand_of<bf16>(a, rows, s) : expand_of<float>(a, rows, s);
@@ -829,8 +933,11 @@ hipError_t launch_adapter_outer(const AdapterOuter& a, hot_type type, hipStream_
   return type == HOT_BF16 ? outer_of<bf16>(a, s) : outer_of<float>(a, s);
 }
 hipError_t launch_adapter_reduce(const AdapterReduce& a, hipStream_t s) {
-  const int tiles_a = (int)ceil_div(a.I, 1024) * a.rank, tiles = tiles_a + (int)ceil_div(a.O, 64);
-  reduce_kernel<<<(uint32_t)((int64_t)a.adapters * tiles), 256, 0, s>>>(a, tiles_a, tiles);
+  const bool runs = a.parts >= 16;
+  const int tiles_a = (int)ceil_div(a.I, 64), tiles = tiles_a + (int)ceil_div(a.O, 64), ranks = (int)ceil_div(a.rank, runs ? 1 : 4);
+  const uint32_t grid = (uint32_t)((int64_t)a.adapters * tiles * ranks);
+  if (runs) reduce_kernel<4><<<grid, 256, 0, s>>>(a, tiles_a, tiles, ranks);
+  else reduce_kernel<1><<<grid, 256, 0, s>>>(a, tiles_a, tiles, ranks);
   return hipGetLastError();
 }
 

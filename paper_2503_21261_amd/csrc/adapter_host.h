@@ -22,6 +22,7 @@ struct AdapterShrink {
   int64_t K, w_pitch, w_stride;     // w: elements from j to j + 1 and from adapter to adapter
   int rank, pitch, slices;
   int64_t slice;                    // columns of a slice
+  float* u;                         // the sums again, [L][rank] (zeros where a row has no adapter), without slices; or null
 };
 // y[l][n] = base[l][n] + scale[adapter(l)] * sum over j of p[l][j] w[adapter(l)][n][j], p the sum of the slices.
 struct AdapterExpand {
@@ -34,7 +35,6 @@ struct AdapterExpand {
   int64_t N, w_pitch, w_stride;
   int rank, pitch, slices;
   int w_cols;                       // elements of a row of w: rank, or more with zeros behind
-  int stream;                       // y is stored with the streaming hint
 };
 // u and g_u (the sum of its slices) for the sums over rows: [parts][ranks rounded up to 16][pitch], rows in the order of their adapters, and that
 // order itself.
@@ -81,6 +81,7 @@ struct AdapterPrepare {
 
 struct AdapterPlan {
   bool rows;                        // a wave works on one row, not on a tile of them
+  int tile;                         // rows of a workgroup of the first product
   int pitch;                        // floats of a row of p
   int slices_forward, slices_backward, parts;
   int64_t slice_forward, slice_backward;
@@ -90,7 +91,7 @@ struct AdapterPlan {
 };
 AdapterPlan adapter_plan(hot_type type, int64_t L, int64_t O, int64_t I, int64_t rank, int64_t adapters, int64_t segments);
 
-hipError_t launch_adapter_shrink(const AdapterShrink& a, bool rows, hot_type type, hipStream_t s);
+hipError_t launch_adapter_shrink(const AdapterShrink& a, int tile, hot_type type, hipStream_t s);
 hipError_t launch_adapter_expand(const AdapterExpand& a, bool rows, hot_type type, hipStream_t s);
 hipError_t launch_adapter_prepare(const AdapterPrepare& a, hot_type type, hipStream_t s);
 hipError_t launch_adapter_pack(const AdapterPack& a, hot_type type, hipStream_t s);

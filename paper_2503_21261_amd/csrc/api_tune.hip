@@ -89,10 +89,11 @@ hot_status hot_adapter_forward(const void* x, const void* a, const void* b, hot_
   if (ws_bytes < p.forward) return HOT_ERR_WORKSPACE;
   hipStream_t s = (hipStream_t)stream;
   const AdapterBatch batch{offsets, index, (int)segments, (int)adapters, L};
-  const AdapterShrink shrink{batch, x, a, (float*)ws, I, I, rank * I, (int)rank, p.pitch, p.slices_forward, p.slice_forward};
-  HOT_STAGE(kStAdapterShrink, launch_adapter_shrink(shrink, p.rows, type, s));
-  const AdapterExpand expand{batch, (const float*)ws, b, base, scale, y, u, O, rank, O * rank, (int)rank, p.pitch, p.slices_forward, (int)rank,
-                             stream_output(L, bytes_of(type, 1, O))};
+  const AdapterShrink shrink{batch, x, a, (float*)ws, I, I, rank * I, (int)rank, p.pitch, p.slices_forward, p.slice_forward,
+                             p.slices_forward == 1 ? u : nullptr};
+  HOT_STAGE(kStAdapterShrink, launch_adapter_shrink(shrink, p.tile, type, s));
+  const AdapterExpand expand{batch, (const float*)ws, b, base, scale, y, p.slices_forward == 1 ? nullptr : u, O, rank, O * rank, (int)rank, p.pitch,
+                             p.slices_forward, (int)rank};
   HOT_STAGE(kStAdapterExpand, launch_adapter_expand(expand, p.rows, type, s));
   return HOT_OK;
 }
@@ -130,11 +131,11 @@ hot_status hot_adapter_backward(const void* g_y, const void* x, const float* u, 
   const AdapterBatch batch{offsets, index, (int)segments, (int)adapters, L};
   const AdapterPrepare prepare{batch, a, b, g_x ? w + p.at : nullptr, w + p.wt, I, O, (int)rank, p.rank_pitch, order, start, first};
   HOT_STAGE(kStAdapterPrepare, launch_adapter_prepare(prepare, type, s));
-  const AdapterShrink shrink{batch, g_y, w + p.wt, g_u, O, O, rank * O, (int)rank, p.pitch, p.slices_backward, p.slice_backward};
-  HOT_STAGE(kStAdapterShrink, launch_adapter_shrink(shrink, p.rows, type, s));
+  const AdapterShrink shrink{batch, g_y, w + p.wt, g_u, O, O, rank * O, (int)rank, p.pitch, p.slices_backward, p.slice_backward, nullptr};
+  HOT_STAGE(kStAdapterShrink, launch_adapter_shrink(shrink, p.tile, type, s));
   if (g_x) {
     const AdapterExpand expand{batch, g_u, w + p.at, g_base, scale, g_x, nullptr, I, p.rank_pitch, I * p.rank_pitch, (int)rank, p.pitch,
-                               p.slices_backward, p.rank_pitch, stream_output(L, bytes_of(type, 1, I))};
+                               p.slices_backward, p.rank_pitch};
     HOT_STAGE(kStAdapterExpand, launch_adapter_expand(expand, p.rows, type, s));
   }
   if (g_a) {
@@ -149,8 +150,8 @@ hot_status hot_adapter_backward(const void* g_y, const void* x, const float* u, 
       pack.order = order;
       pack.start = start;
       pack.first = first;
-      pack.rows = first + adapters + 1;
     }
+    pack.rows = first + adapters + 1;
     pack.pitch = p.pos_pitch;
     pack.rank = (int)rank;
     pack.g_pitch = p.pitch;
