@@ -125,7 +125,7 @@ __device__ __forceinline__ Run run_at(const AdapterBatch& b, int64_t row, int64_
 // RT tiles of 16 ranks, R tiles of 16 rows; ROWS: rows that a workgroup takes (1, or 16 R).  A step is 128 bytes of each row; the four waves
 // take steps in turn, DEPTH of them on their way, and join their sums through LDS.
 template <class T, int RT, int R, int ROWS, int DEPTH>
-__global__ __launch_bounds__(256) void shrink_kernel(const AdapterShrink a) {
+__global__ __launch_bounds__(256, RT <= 4 ? 2 : 1) void shrink_kernel(const AdapterShrink a) {
   constexpr int kStep = 128 / sizeof(T), kFrags = kStep / 32, kPer = 16 / sizeof(T);
   __shared__ f4 s_acc[3][RT * R][64];
   const int lane = threadIdx.x & 63, i = lane & 15, q = lane >> 4, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -161,7 +161,7 @@ __global__ __launch_bounds__(256) void shrink_kernel(const AdapterShrink a) {
 #pragma unroll
           for (int r = 0; r < R; ++r) d.x[r][f] = load_piece(x[r] + at + f * 32);
 #pragma unroll
-          for (int t = 0; t < RT; ++t) d.w[t][f] = load_piece(wr[t] + at + f * 32);
+          for (int t = 0; t < RT; ++t) d.w[t][f] = load_piece(wr[t] + at * a.w_step + f * 32);
         }
       };
       const auto multiply = [&](const Step& d) {
@@ -173,19 +173,25 @@ __global__ __launch_bounds__(256) void shrink_kernel(const AdapterShrink a) {
             for (int t = 0; t < RT; ++t) acc[t][r] = mma(frag(d.w[t][f]), frag(d.x[r][f]), acc[t][r]);
       };
       if (first < whole) {
-        // The last step's loads are made once more instead of a branch around them, which would make the waits wait for all.
+        // Each workgroup begins its walk elsewhere: side by side they would all ask the same few channels of the caches for the same
+        // columns of rows that are a power of two apart.
         constexpr int kTurn = 4 * kStep;
-        const int64_t last = first + (whole - 1 - first) / kTurn * kTurn;
+        const int n = (int)((whole - 1 - first) / kTurn) + 1, from = (int)(blockIdx.x % (uint32_t)n);
+        // The last step's loads are made once more instead of a branch around them, which would make the waits wait for all.
+        const auto step_at = [&](int s) {
+          const int k = min(s, n - 1) + from;
+          return first + (int64_t)(k < n ? k : k - n) * kTurn;
+        };
         Step d[DEPTH];
 #pragma unroll
-        for (int s = 0; s < DEPTH - 1; ++s) load(min(first + s * kTurn, last), d[s]);
+        for (int s = 0; s < DEPTH - 1; ++s) load(step_at(s), d[s]);
         // Rounds of DEPTH steps without a way out of their middle, which would have the buffers copied at each round's end; what is left is
         // loaded already.
-        int64_t at = first;
-        for (; at + (DEPTH - 1) * kTurn <= last; at += DEPTH * kTurn) {
+        int at = 0;
+        for (; at + DEPTH <= n; at += DEPTH) {
 #pragma unroll
           for (int s = 0; s < DEPTH; ++s) {
-            load(min(at + (s + DEPTH - 1) * kTurn, last), d[(s + DEPTH - 1) % DEPTH]);
+            load(step_at(at + s + DEPTH - 1), d[(s + DEPTH - 1) % DEPTH]);
             __builtin_amdgcn_sched_barrier(0);      // else the loads sink to where they are used
             multiply(d[s]);
             __builtin_amdgcn_sched_barrier(0);
@@ -193,7 +199,7 @@ __global__ __launch_bounds__(256) void shrink_kernel(const AdapterShrink a) {
         }
 #pragma unroll
         for (int s = 0; s < DEPTH - 1; ++s)
-          if (at + s * kTurn <= last) multiply(d[s]);
+          if (at + s < n) multiply(d[s]);
       }
       if (whole < k1 && wave == 3) {              // the row's last elements: zeros behind them, on both sides
         for (int64_t at = whole; at < k1; at += 32) {
@@ -203,7 +209,7 @@ __global__ __launch_bounds__(256) void shrink_kernel(const AdapterShrink a) {
           for (int r = 0; r < R; ++r) {
             const Frag<T> fx = frag(load8(x[r] + by, n));
 #pragma unroll
-            for (int t = 0; t < RT; ++t) acc[t][r] = mma(frag(load8(wr[t] + by, n)), fx, acc[t][r]);
+            for (int t = 0; t < RT; ++t) acc[t][r] = mma(frag(load8(wr[t] + whole * (a.w_step - 1) + by, n)), fx, acc[t][r]);
           }
         }
       }
@@ -521,15 +527,18 @@ __device__ void sort_segments(const AdapterPrepare& a, int k) {
   }
 }
 
+// to[c][r] of `from` [rows x cols]: at c * c_pitch + r, in groups of `group` r's that are g_pitch apart; r up to `held`, zeros past the rows.
 template <class T>
-__device__ void transpose_tile(const T* from, int64_t rows, int64_t cols, T* to, int64_t to_pitch, int64_t r0, int64_t c0) {
+__device__ void transpose_tile(const T* from, int64_t rows, int64_t cols, T* to, int64_t c_pitch, int64_t group, int64_t g_pitch, int64_t held,
+                               int64_t r0, int64_t c0) {
   __shared__ T s_tile[64][65];
   const int x = threadIdx.x & 63, y = threadIdx.x >> 6;
   for (int r = y; r < 64; r += 4)
     s_tile[r][x] = r0 + r < rows && c0 + x < cols ? from[(r0 + r) * cols + c0 + x] : (T)0.0f;
   __syncthreads();
+  const int64_t r = r0 + x, at = r / group * g_pitch + r % group;
   for (int c = y; c < 64; c += 4)
-    if (c0 + c < cols && r0 + x < to_pitch) to[(c0 + c) * to_pitch + r0 + x] = s_tile[x][c];   // the pitch past the rows: zeros
+    if (c0 + c < cols && r < held) to[(c0 + c) * c_pitch + at] = s_tile[x][c];
 }
 
 template <class T>
@@ -543,29 +552,30 @@ __global__ __launch_bounds__(256) void prepare_kernel(const AdapterPrepare a, in
   const int per = tiles_a + tiles_w, k = b / per, t = b % per;
   if (t < tiles_a)
     transpose_tile((const T*)a.a + (int64_t)k * a.rank * a.I, a.rank, a.I, (T*)a.at + (int64_t)k * a.I * a.rank_pitch, a.rank_pitch,
-                   (int64_t)(t % rank_tiles) * 64, (int64_t)(t / rank_tiles) * 64);
+                   (int64_t)a.rank_pitch, 0, a.rank_pitch, (int64_t)(t % rank_tiles) * 64, (int64_t)(t / rank_tiles) * 64);
   else
-    transpose_tile((const T*)a.w + (int64_t)k * a.O * a.rank, a.O, a.rank, (T*)a.wt + (int64_t)k * a.rank * a.O, a.O,
-                   (int64_t)((t - tiles_a) / rank_tiles) * 64, (int64_t)((t - tiles_a) % rank_tiles) * 64);
+    transpose_tile((const T*)a.w + (int64_t)k * a.O * a.rank, a.O, a.rank, (T*)a.wt + k * a.wt_stride, 128 / (int64_t)sizeof(T),
+                   128 / (int64_t)sizeof(T), a.rank * (128 / (int64_t)sizeof(T)), a.wt_stride / a.rank, (int64_t)((t - tiles_a) / rank_tiles) * 64,
+                   (int64_t)((t - tiles_a) % rank_tiles) * 64);
 }
 
 // ---- outer ----------------------------------------------------------------------------------------
 // Rows of a part of the sums over `total` rows.
 __device__ __forceinline__ int64_t rows_of_part(int64_t total, int parts) { return ((total + parts - 1) / parts + 31) & -32ll; }
 
-// The first n of eight elements, zeros behind them.
-__device__ __forceinline__ Raw8<bf16> first_of(const Raw8<bf16>& r, int n) {
+// Elements m .. n - 1 of eight, zeros beside them.
+__device__ __forceinline__ Raw8<bf16> between(const Raw8<bf16>& r, int m, int n) {
   Raw8<bf16> o;
 #pragma unroll
-  for (int e = 0; e < 8; ++e) o.a[e] = e < n ? r.a[e] : (uint16_t)0;
+  for (int e = 0; e < 8; ++e) o.a[e] = e >= m && e < n ? r.a[e] : (uint16_t)0;
   return o;
 }
-__device__ __forceinline__ Raw8<float> first_of(const Raw8<float>& r, int n) {
+__device__ __forceinline__ Raw8<float> between(const Raw8<float>& r, int m, int n) {
   Raw8<float> o;
 #pragma unroll
   for (int e = 0; e < 4; ++e) {
-    o.a[e] = e < n ? r.a[e] : 0.0f;
-    o.b[e] = e + 4 < n ? r.b[e] : 0.0f;
+    o.a[e] = e >= m && e < n ? r.a[e] : 0.0f;
+    o.b[e] = e + 4 >= m && e + 4 < n ? r.b[e] : 0.0f;
   }
   return o;
 }
@@ -592,8 +602,9 @@ __device__ __forceinline__ void columns_of(const Raw8<float> (&rows)[8], Frag<fl
   }
 }
 
-// u and g_u for the sums over rows: rows in the order of their adapters, a rank's factors one after the other, so that a lane's eight rows are one
-// load; bfloat16 in its three parts.  [parts][ranks rounded up to 16][pitch] of T.  A workgroup: 64 positions of one operand.
+// u and g_u for the sums over rows: rows in the order of their adapters, a rank's factors of 32 rows one after the other, so that a lane's eight
+// rows are one load; bfloat16 in its three parts.  [steps of 32 rows][parts][ranks rounded up to 16][32] of T: what a wave loads at a time
+// lies together (ranks a long row apart meet in a few channels of the caches).  A workgroup: 64 positions of one operand.
 template <class T>
 __global__ __launch_bounds__(256) void pack_kernel(const AdapterPack a) {
   constexpr int kParts = sizeof(T) == 4 ? 1 : 3;
@@ -642,14 +653,14 @@ __global__ __launch_bounds__(256) void pack_kernel(const AdapterPack a) {
     float v[8];
 #pragma unroll
     for (int e = 0; e < 8; ++e) v[e] = s_p[j * 65 + x + e];
-    T* const to = out + (int64_t)j * a.pitch + pos0 + x;
+    T* const to = out + (((pos0 + x) / 32 * kParts) * ranks + j) * 32 + x % 32;
     if constexpr (kParts == 1) {
       store8(to, v, 8);
     } else {
       Frag<bf16> f[kParts];
       split8<kParts>(v, f);
 #pragma unroll
-      for (int part = 0; part < kParts; ++part) *(u4*)(to + (int64_t)part * ranks * a.pitch) = f[part].v;
+      for (int part = 0; part < kParts; ++part) *(u4*)(to + part * ranks * 32) = f[part].v;
     }
   }
 }
@@ -692,12 +703,12 @@ __global__ __launch_bounds__(64 * kOuterWaves) void outer_kernel(const AdapterOu
 #pragma unroll
       for (int c = 0; c < 8; ++c) acc[t][c] = f4{0.0f, 0.0f, 0.0f, 0.0f};
     Raw8<T> p[RT][kParts];
-    const T* const p_at = (const T*)o.p + (int64_t)(rank0 + i) * a.pitch + q * 8;
-    const int64_t last = pos + (k_end - pos - 1) / 32 * 32;      // the last step's first position
-    const auto rows_at = [&](int64_t at, int (&r)[8]) {          // past the last row: that one once more, times zero
+    const T* const p_at = (const T*)o.p + (rank0 + i) * 32 + q * 8;
+    const int64_t begin = pos & -32ll, last = (k_end - 1) & -32ll;          // the first and the last step
+    const auto rows_at = [&](int64_t at, int (&r)[8]) {          // beside the rows: the nearest one, times zero
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        const int64_t l = min(at + q * 8 + e, k_end - 1);
+        const int64_t l = max(min(at + q * 8 + e, k_end - 1), pos);
         r[e] = MODE ? a.rows[l] : (int)l;
       }
     };
@@ -712,15 +723,15 @@ __global__ __launch_bounds__(64 * kOuterWaves) void outer_kernel(const AdapterOu
     const auto load_p = [&](int t, int64_t at) {     // ranks past the last tile: the last tile's, whose sums are not stored
       const int64_t j = min(t * 16, ranks - 16 - rank0);
 #pragma unroll
-      for (int s = 0; s < kParts; ++s) p[t][s] = load8(p_at + (s * ranks + j) * a.pitch + at, 8);
+      for (int s = 0; s < kParts; ++s) p[t][s] = load8(p_at + at * kParts * ranks + (s * ranks + j) * 32, 8);
     };
     const auto multiply = [&](int64_t at, const Raw8<T> (&x)[8]) {
-      if (at == last) {                                          // zeros past the last row
-        const int n = (int)min(max(k_end - at - q * 8, (int64_t)0), (int64_t)8);
+      if (at == last || at < pos) {                              // zeros beside the rows
+        const int n = (int)min(max(k_end - at - q * 8, (int64_t)0), (int64_t)8), m = (int)max(pos - at - q * 8, (int64_t)0);
 #pragma unroll
         for (int t = 0; t < RT; ++t)
 #pragma unroll
-          for (int s = 0; s < kParts; ++s) p[t][s] = first_of(p[t][s], n);
+          for (int s = 0; s < kParts; ++s) p[t][s] = between(p[t][s], m, n);
       }
       Frag<T> f[8];
       columns_of(x, f);
@@ -736,12 +747,12 @@ __global__ __launch_bounds__(64 * kOuterWaves) void outer_kernel(const AdapterOu
     };
     Raw8<T> x0[8], x1[8];
     int r0[8], r1[8];
-    rows_at(pos, r0);
-    rows_at(min(pos + 32, last), r1);
+    rows_at(begin, r0);
+    rows_at(min(begin + 32, last), r1);
     load(r0, x0);
 #pragma unroll
-    for (int t = 0; t < RT; ++t) load_p(t, pos);
-    int64_t at = pos;
+    for (int t = 0; t < RT; ++t) load_p(t, begin);
+    int64_t at = begin;
     for (; at + 32 <= last; at += 64) {
       load(r1, x1);
       rows_at(min(at + 64, last), r0);
@@ -887,7 +898,7 @@ AdapterPlan adapter_plan(hot_type type, int64_t L, int64_t O, int64_t I, int64_t
   const int64_t tiles = (ceil_div(I, kOuterCols * kOuterWaves) + ceil_div(O, kOuterCols * kOuterWaves)) * ceil_div(rank, 64);
   const int64_t wanted = ceil_div(rank > 32 ? 256 : 512, tiles), most = ceil_div(L, 64);
   p.parts = (int)(wanted < most ? wanted : most);
-  p.pos_pitch = round_up(L, 64) + 64;
+  p.positions = round_up(L, 64);
 
   const int64_t row_bytes = L * p.pitch * 4;
   p.forward = (size_t)round_up(row_bytes * p.slices_forward, 256);
@@ -898,9 +909,9 @@ AdapterPlan adapter_plan(hot_type type, int64_t L, int64_t O, int64_t I, int64_t
     return here;
   };
   p.at = take(adapters * I * p.rank_pitch * size);
-  p.wt = take(adapters * rank * O * size);
-  p.sorted = take((2 * segments + 1 + adapters + 1 + p.pos_pitch) * 4);
-  p.packed = take(2 * (type == HOT_BF16 ? 3 : 1) * size * round_up(rank, 16) * p.pos_pitch);
+  p.wt = take(adapters * rank * round_up(O, step) * size);
+  p.sorted = take((2 * segments + 1 + adapters + 1 + p.positions) * 4);
+  p.packed = take(2 * (type == HOT_BF16 ? 3 : 1) * size * round_up(rank, 16) * p.positions);
   p.part_a = take((p.parts + adapters) * rank * I * 4);
   p.part_b = take((p.parts + adapters) * rank * O * 4);
   p.backward = at;

@@ -19,7 +19,7 @@ struct AdapterShrink {
   AdapterBatch b;
   const void *q, *w;
   float* out;
-  int64_t K, w_pitch, w_stride;     // w: elements from j to j + 1 and from adapter to adapter
+  int64_t K, w_pitch, w_stride, w_step;   // w: elements from j to j + 1, from adapter to adapter, and a step's distance in units of its length
   int rank, pitch, slices;
   int64_t slice;                    // columns of a slice
   float* u;                         // the sums again, [L][rank] (zeros where a row has no adapter), without slices; or null
@@ -36,15 +36,14 @@ struct AdapterExpand {
   int rank, pitch, slices;
   int w_cols;                       // elements of a row of w: rank, or more with zeros behind
 };
-// u and g_u (the sum of its slices) for the sums over rows: [parts][ranks rounded up to 16][pitch], rows in the order of their adapters, and that
-// order itself.
+// u and g_u (the sum of its slices) for the sums over rows: [steps of 32 rows][parts][ranks rounded up to 16][32], rows in the order of their
+// adapters, and that order itself.
 struct AdapterPack {
   AdapterBatch b;
   const float *g_u, *u;
   void *g_out, *u_out;
   const int32_t *order, *start, *first;   // segments in the order of their adapters, their first positions, the adapters' (null without offsets)
   int32_t* rows;                    // rows of the positions
-  int64_t pitch;
   int rank, g_pitch, slices;
 };
 // One product of sums over rows: part[slot][j][n] = sum over the part's rows of p[j][l] q[l][n].
@@ -59,7 +58,6 @@ struct AdapterOuter {
   AdapterOuterOperand a[2];
   const float* scale;
   const int32_t *first, *rows;
-  int64_t pitch;
   int rank, parts;
 };
 struct AdapterReduce {
@@ -73,9 +71,10 @@ struct AdapterReduce {
 struct AdapterPrepare {
   AdapterBatch b;
   const void *a, *w;                // a [adapters][rank][I], w [adapters][O][rank]
-  void *at, *wt;                    // [adapters][I][rank_pitch], [adapters][rank][O]
+  void *at, *wt;                    // [adapters][I][rank_pitch], [adapters][steps of 128 bytes of O][rank][step]
   int64_t I, O;
   int rank, rank_pitch;
+  int64_t wt_stride;
   int32_t *order, *start, *first;
 };
 
@@ -86,7 +85,7 @@ struct AdapterPlan {
   int slices_forward, slices_backward, parts;
   int64_t slice_forward, slice_backward;
   int rank_pitch;
-  int64_t pos_pitch;                // positions of a row of packed factors
+  int64_t positions;                // of the packed factors
   size_t at, wt, sorted, packed, part_a, part_b, forward, backward;   // offsets into the workspace, and its sizes
 };
 AdapterPlan adapter_plan(hot_type type, int64_t L, int64_t O, int64_t I, int64_t rank, int64_t adapters, int64_t segments);

@@ -89,7 +89,7 @@ hot_status hot_adapter_forward(const void* x, const void* a, const void* b, hot_
   if (ws_bytes < p.forward) return HOT_ERR_WORKSPACE;
   hipStream_t s = (hipStream_t)stream;
   const AdapterBatch batch{offsets, index, (int)segments, (int)adapters, L};
-  const AdapterShrink shrink{batch, x, a, (float*)ws, I, I, rank * I, (int)rank, p.pitch, p.slices_forward, p.slice_forward,
+  const AdapterShrink shrink{batch, x, a, (float*)ws, I, I, rank * I, 1, (int)rank, p.pitch, p.slices_forward, p.slice_forward,
                              p.slices_forward == 1 ? u : nullptr};
   HOT_STAGE(kStAdapterShrink, launch_adapter_shrink(shrink, p.tile, type, s));
   const AdapterExpand expand{batch, (const float*)ws, b, base, scale, y, p.slices_forward == 1 ? nullptr : u, O, rank, O * rank, (int)rank, p.pitch,
@@ -129,9 +129,10 @@ hot_status hot_adapter_backward(const void* g_y, const void* x, const float* u, 
   int32_t* const start = order + segments;
   int32_t* const first = start + segments + 1;
   const AdapterBatch batch{offsets, index, (int)segments, (int)adapters, L};
-  const AdapterPrepare prepare{batch, a, b, g_x ? w + p.at : nullptr, w + p.wt, I, O, (int)rank, p.rank_pitch, order, start, first};
+  const int64_t step = type == HOT_BF16 ? 64 : 32, wt_stride = rank * round_up(O, step);
+  const AdapterPrepare prepare{batch, a, b, g_x ? w + p.at : nullptr, w + p.wt, I, O, (int)rank, p.rank_pitch, wt_stride, order, start, first};
   HOT_STAGE(kStAdapterPrepare, launch_adapter_prepare(prepare, type, s));
-  const AdapterShrink shrink{batch, g_y, w + p.wt, g_u, O, O, rank * O, (int)rank, p.pitch, p.slices_backward, p.slice_backward, nullptr};
+  const AdapterShrink shrink{batch, g_y, w + p.wt, g_u, O, step, wt_stride, rank, (int)rank, p.pitch, p.slices_backward, p.slice_backward, nullptr};
   HOT_STAGE(kStAdapterShrink, launch_adapter_shrink(shrink, p.tile, type, s));
   if (g_x) {
     const AdapterExpand expand{batch, g_u, w + p.at, g_base, scale, g_x, nullptr, I, p.rank_pitch, I * p.rank_pitch, (int)rank, p.pitch,
@@ -139,7 +140,7 @@ hot_status hot_adapter_backward(const void* g_y, const void* x, const float* u, 
     HOT_STAGE(kStAdapterExpand, launch_adapter_expand(expand, p.rows, type, s));
   }
   if (g_a) {
-    const int64_t half = (type == HOT_BF16 ? 6 : 4) * round_up(rank, 16) * p.pos_pitch;
+    const int64_t half = (type == HOT_BF16 ? 6 : 4) * round_up(rank, 16) * p.positions;
     AdapterPack pack{};
     pack.b = batch;
     pack.g_u = g_u;
@@ -152,7 +153,6 @@ hot_status hot_adapter_backward(const void* g_y, const void* x, const float* u, 
       pack.first = first;
     }
     pack.rows = first + adapters + 1;
-    pack.pitch = p.pos_pitch;
     pack.rank = (int)rank;
     pack.g_pitch = p.pitch;
     pack.slices = p.slices_backward;
@@ -164,7 +164,6 @@ hot_status hot_adapter_backward(const void* g_y, const void* x, const float* u, 
     outer.scale = scale;
     outer.first = pack.first;
     outer.rows = pack.rows;
-    outer.pitch = p.pos_pitch;
     outer.rank = (int)rank;
     outer.parts = p.parts;
     HOT_STAGE(kStAdapterOuter, launch_adapter_outer(outer, type, s));
