@@ -30,13 +30,40 @@ template <class T> struct Frag;
 template <> struct Frag<bf16> { u4 v; };
 template <> struct Frag<float> { float v[8]; };
 
-// Eight elements of a row for each of four lanes, in loads of 64 consecutive bytes of it: bfloat16 as they lie, fp32 in two pieces of
-// four, 16 elements apart (the order of the reduced elements is free).
+// Eight elements for a lane, of 32 that four lanes share: bfloat16 those from 8 q on; fp32 in two loads of four, those from 4 q and from 16 + 4 q
+// on (the order of the reduced elements is free), which are APART elements apart in memory.
 template <class T> struct Piece;
 template <> struct Piece<bf16> { h8_any v; };
 template <> struct Piece<float> { f4_any v[2]; };
+template <int APART>
 __device__ __forceinline__ Piece<bf16> load_piece(const bf16* p) { return Piece<bf16>{*(const h8_any*)p}; }
-__device__ __forceinline__ Piece<float> load_piece(const float* p) { return Piece<float>{{*(const f4_any*)p, *(const f4_any*)(p + 16)}}; }
+template <int APART>
+__device__ __forceinline__ Piece<float> load_piece(const float* p) { return Piece<float>{{*(const f4_any*)p, *(const f4_any*)(p + APART)}}; }
+// Of the 32 elements from p on, of which `left` exist; zeros for the others.
+__device__ __forceinline__ Piece<bf16> load_piece_of(const bf16* p, int q, int left) {
+  return Piece<bf16>{load8(p + q * 8, min(max(left - q * 8, 0), 8)).a};
+}
+__device__ __forceinline__ Piece<float> load_piece_of(const float* p, int q, int left) {
+  Piece<float> r;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    const int at = e / 4 * 16 + q * 4 + e % 4;
+    r.v[e / 4][e % 4] = at < left ? p[at] : 0.0f;
+  }
+  return r;
+}
+// fp32 numbers in the places that a piece of T has them.
+template <class T>
+__device__ __forceinline__ Piece<float> load_piece_as(const float* p, int q, int left) {
+  if constexpr (sizeof(T) == 4) {
+    return load_piece_of(p, q, left);
+  } else {
+    const Raw8<float> r = load8(p + q * 8, min(max(left - q * 8, 0), 8));
+    return Piece<float>{{r.a, r.b}};
+  }
+}
+// Elements that a wave's 64 lanes have of 16 rows and 32 reduced elements: a packed tile.
+constexpr int kTile = 512;
 __device__ __forceinline__ Frag<bf16> frag(const Piece<bf16>& r) { return Frag<bf16>{__builtin_bit_cast(u4, r.v)}; }
 __device__ __forceinline__ Frag<float> frag(const Piece<float>& r) {
   Frag<float> f;
@@ -89,6 +116,31 @@ __device__ __forceinline__ void split8(const float (&v)[8], Frag<bf16> (&out)[PA
   }
 }
 
+// Factors of the expansion in the order of its lanes: for 16 rows and 32 ranks a tile (bfloat16: two, the two parts), [rows / 16][chunks].  Up to 16
+// ranks in bfloat16 are one tile: the second half of its 32 elements is the second part of the first.  Ranks j .. j + 3 of row l.
+__device__ __forceinline__ void store_factors(float* p, int64_t l, int j, int chunks, f4 v) {
+  const int in = j & 31, q = (in & 15) / 4;
+  *(f4*)(p + ((l >> 4) * chunks + (j >> 5)) * kTile + in / 16 * 256 + (q * 16 + (l & 15)) * 4) = v;
+}
+__device__ __forceinline__ void store_factors(bf16* p, int64_t l, int j, int chunks, f4 v) {
+  uint32_t part[2][4];
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    const uint32_t b = __float_as_uint(v[e]);
+    const bool finite = (b & 0x7F800000u) != 0x7F800000u;
+    part[0][e] = (b & 0x7FFFFFFFu) > 0x7F800000u ? b | 0x400000u : b;      // as split8()
+    part[1][e] = finite ? __float_as_uint(v[e] - __uint_as_float(b & 0xFFFF0000u)) : 0u;
+  }
+#pragma unroll
+  for (int s = 0; s < 2; ++s) {
+    const uint2 x = make_uint2(__builtin_amdgcn_perm(part[s][1], part[s][0], 0x07060302u), __builtin_amdgcn_perm(part[s][3], part[s][2], 0x07060302u));
+    const int in = j & 31;
+    bf16* const at = chunks == 0 ? p + (l >> 4) * kTile + ((s * 2 + in / 8) * 16 + (l & 15)) * 8
+                                 : p + (((l >> 4) * chunks + (j >> 5)) * 2 + s) * kTile + (in / 8 * 16 + (l & 15)) * 8;
+    *(uint2*)(at + (j & 4)) = x;
+  }
+}
+
 // How many of the n ascending numbers at t are at most x, by the wave together: each trip narrows the range to a 64th.
 __device__ __forceinline__ int count_up_to(const int32_t* t, int n, int x) {
   const int lane = threadIdx.x & 63;
@@ -122,9 +174,14 @@ __device__ __forceinline__ Run run_at(const AdapterBatch& b, int64_t row, int64_
 }
 
 // ---- shrink ---------------------------------------------------------------------------------------
+// The memory pipe takes the 64 bytes of four neighbouring lanes at a time, where they lie together; lanes of a matrix instruction's operand are
+// rows, so that a load of 16 rows takes four times as long as one of 1024 bytes in a row.  Rows that are read once can bear that (half the
+// pipe's time at 5 TB/s), what is read again cannot: weights are packed in the order of the lanes first, where that pays or they have to
+// be transposed anyway, and the sums are left in that order for the expansion.
+//
 // RT tiles of 16 ranks, R tiles of 16 rows; ROWS: rows that a workgroup takes (1, or 16 R).  A step is 128 bytes of each row; the four waves
 // take steps in turn, DEPTH of them on their way, and join their sums through LDS.
-template <class T, int RT, int R, int ROWS, int DEPTH>
+template <class T, int RT, int R, int ROWS, int DEPTH, bool PACKED>
 __global__ __launch_bounds__(256, RT <= 4 ? 2 : 1) void shrink_kernel(const AdapterShrink a) {
   constexpr int kStep = 128 / sizeof(T), kFrags = kStep / 32, kPer = 16 / sizeof(T);
   __shared__ f4 s_acc[3][RT * R][64];
@@ -136,6 +193,7 @@ __global__ __launch_bounds__(256, RT <= 4 ? 2 : 1) void shrink_kernel(const Adap
   const int64_t k0 = slice * a.slice, k1 = min(k0 + a.slice, a.K);
   float* const out = a.out + (int64_t)slice * a.b.L * a.pitch;
   const int64_t first = k0 + wave * kStep, whole = k0 + (k1 - k0) / kStep * kStep;      // this wave's first step, the end of the whole ones
+  const int rank_tiles = (a.rank + 15) / 16;
 
   for (int64_t row = row0; row < row1;) {
     const Run run = run_at(a.b, row, row1);
@@ -144,9 +202,10 @@ __global__ __launch_bounds__(256, RT <= 4 ? 2 : 1) void shrink_kernel(const Adap
       const T* x[R];
       const T* wr[RT];
 #pragma unroll
-      for (int r = 0; r < R; ++r) x[r] = (const T*)a.q + min(max(row0 + r * 16 + i, row), run.end - 1) * a.K + q * kPer;
+      for (int r = 0; r < R; ++r) x[r] = (const T*)a.q + min(max(row0 + r * 16 + i, row), run.end - 1) * a.K;
 #pragma unroll
-      for (int t = 0; t < RT; ++t) wr[t] = w + min(t * 16 + i, a.rank - 1) * a.w_pitch + q * kPer;
+      for (int t = 0; t < RT; ++t)      // ranks past the last: the last one's, whose sums are not kept
+        wr[t] = PACKED ? w + min(t, rank_tiles - 1) * kTile + lane * kPer : w + min(t * 16 + i, a.rank - 1) * a.K;
       f4 acc[RT][R];
 #pragma unroll
       for (int t = 0; t < RT; ++t)
@@ -159,9 +218,12 @@ __global__ __launch_bounds__(256, RT <= 4 ? 2 : 1) void shrink_kernel(const Adap
 #pragma unroll
         for (int f = 0; f < kFrags; ++f) {
 #pragma unroll
-          for (int r = 0; r < R; ++r) d.x[r][f] = load_piece(x[r] + at + f * 32);
+          for (int r = 0; r < R; ++r) d.x[r][f] = load_piece<16>(x[r] + at + f * 32 + q * kPer);
 #pragma unroll
-          for (int t = 0; t < RT; ++t) d.w[t][f] = load_piece(wr[t] + at * a.w_step + f * 32);
+          for (int t = 0; t < RT; ++t) {
+            if constexpr (PACKED) d.w[t][f] = load_piece<256>(wr[t] + (at / 32 + f) * rank_tiles * kTile);
+            else d.w[t][f] = load_piece<16>(wr[t] + at + f * 32 + q * kPer);
+          }
         }
       };
       const auto multiply = [&](const Step& d) {
@@ -173,8 +235,7 @@ __global__ __launch_bounds__(256, RT <= 4 ? 2 : 1) void shrink_kernel(const Adap
             for (int t = 0; t < RT; ++t) acc[t][r] = mma(frag(d.w[t][f]), frag(d.x[r][f]), acc[t][r]);
       };
       if (first < whole) {
-        // Each workgroup begins its walk elsewhere: side by side they would all ask the same few channels of the caches for the same
-        // columns of rows that are a power of two apart.
+        // Each workgroup begins its walk elsewhere: side by side they would all ask for the same columns of the weights.
         constexpr int kTurn = 4 * kStep;
         const int n = (int)((whole - 1 - first) / kTurn) + 1, from = (int)(blockIdx.x % (uint32_t)n);
         // The last step's loads are made once more instead of a branch around them, which would make the waits wait for all.
@@ -203,13 +264,15 @@ __global__ __launch_bounds__(256, RT <= 4 ? 2 : 1) void shrink_kernel(const Adap
       }
       if (whole < k1 && wave == 3) {              // the row's last elements: zeros behind them, on both sides
         for (int64_t at = whole; at < k1; at += 32) {
-          const int n = (int)max(min((int64_t)8, k1 - at - q * 8), (int64_t)0);
-          const int64_t by = at + q * (8 - kPer);
+          const int left = (int)min(k1 - at, (int64_t)32);
 #pragma unroll
           for (int r = 0; r < R; ++r) {
-            const Frag<T> fx = frag(load8(x[r] + by, n));
+            const Frag<T> fx = frag(load_piece_of(x[r] + at, q, left));
 #pragma unroll
-            for (int t = 0; t < RT; ++t) acc[t][r] = mma(frag(load8(wr[t] + whole * (a.w_step - 1) + by, n)), fx, acc[t][r]);
+            for (int t = 0; t < RT; ++t) {
+              if constexpr (PACKED) acc[t][r] = mma(frag(load_piece<256>(wr[t] + at / 32 * rank_tiles * kTile)), fx, acc[t][r]);
+              else acc[t][r] = mma(frag(load_piece_of(wr[t] + at, q, left)), fx, acc[t][r]);
+            }
           }
         }
       }
@@ -222,6 +285,7 @@ __global__ __launch_bounds__(256, RT <= 4 ? 2 : 1) void shrink_kernel(const Adap
       __syncthreads();
       // Lane (i, q) has ranks 16 t + 4 q .. + 3 of row i.
       if (wave == 0) {
+        const float scale = a.scale ? a.scale[run.adapter] : 1.0f;
 #pragma unroll
         for (int r = 0; r < R; ++r) {
           const int64_t l = row0 + r * 16 + i;
@@ -237,13 +301,17 @@ __global__ __launch_bounds__(256, RT <= 4 ? 2 : 1) void shrink_kernel(const Adap
             }
 #pragma unroll
             for (int e = 0; e < 4; ++e) v[e] = j + e < a.rank ? v[e] : 0.0f;
-            if (l >= row && l < run.end && j < a.pitch) *(f4*)(out + l * a.pitch + j) = v;
-            if (a.u && l >= row && l < run.end) {
+            if (l < row || l >= run.end) continue;
+            if (j < a.pitch) *(f4*)(out + l * a.pitch + j) = v;
+            if (a.u) {
 #pragma unroll
               for (int e = 0; e < 4; ++e)
                 if (j + e < a.rank) a.u[l * a.rank + j + e] = v[e];
             }
+            if (a.packed) store_factors((T*)a.packed, l, j, a.chunks, v * scale);
           }
+          if (a.packed && RT == 1 && sizeof(T) == 4 && l >= row && l < run.end)    // the other half of a chunk of 32 ranks
+            store_factors((T*)a.packed, l, 16 + q * 4, a.chunks, f4{0.0f, 0.0f, 0.0f, 0.0f});
         }
       }
       __syncthreads();
@@ -254,91 +322,89 @@ __global__ __launch_bounds__(256, RT <= 4 ? 2 : 1) void shrink_kernel(const Adap
   }
 }
 
-// 16 bytes of a row, and their sums with the factors of a lane's columns.
-template <class T> struct Vec16;
-template <> struct Vec16<bf16> { h8_any v; };
-template <> struct Vec16<float> { f4_any v; };
-__device__ __forceinline__ Vec16<bf16> load16(const bf16* p) { return Vec16<bf16>{*(const h8_any*)p}; }
-__device__ __forceinline__ Vec16<float> load16(const float* p) { return Vec16<float>{*(const f4_any*)p}; }
-__device__ __forceinline__ Vec16<bf16> sum16(const Vec16<bf16>& b, f4 lo, f4 hi) {
-  Vec16<bf16> r;
-#pragma unroll
-  for (int e = 0; e < 8; ++e) r.v[e] = float_to_bf16(bf16_to_float(b.v[e]) + (e < 4 ? lo[e & 3] : hi[e & 3]));
-  return r;
-}
-__device__ __forceinline__ Vec16<float> sum16(const Vec16<float>& b, f4 lo, f4) {
-  Vec16<float> r;
-#pragma unroll
-  for (int e = 0; e < 4; ++e) r.v[e] = b.v[e] + lo[e];
-  return r;
-}
+// ---- expand ---------------------------------------------------------------------------------------
+// Four consecutive columns of a row.
+template <class T> struct Four;
+template <> struct Four<bf16> { typedef uint16_t V __attribute__((ext_vector_type(4), aligned(2))); V v; };
+template <> struct Four<float> { typedef f4_any V; V v; };
 template <class T>
-__device__ __forceinline__ void store16(T* p, const Vec16<T>& v) { *(std::remove_cv_t<decltype(v.v)>*)p = v.v; }
+__device__ __forceinline__ Four<T> load4(const T* p) { return Four<T>{*(const typename Four<T>::V*)p}; }
+__device__ __forceinline__ Four<bf16> sum4(const Four<bf16>& b, f4 x) {
+  Four<bf16> r;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) r.v[e] = float_to_bf16(bf16_to_float(b.v[e]) + x[e]);
+  return r;
+}
+__device__ __forceinline__ Four<float> sum4(const Four<float>& b, f4 x) {
+  Four<float> r;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) r.v[e] = b.v[e] + x[e];
+  return r;
+}
 
-// Rows row .. end - 1 of one adapter and 64 columns from n on: tiles of 16 rows, DEPTH of them on their way.  Nothing here branches but the
-// loop, so that a wait is for one tile and not for all.  (The streaming hint on y: 140 us for 130, reading and writing 16384 x 11008.)
-template <class T, int PIECES, int CHUNKS, int DEPTH, bool BASE, class F>
-__device__ __forceinline__ void expand_rows(const AdapterExpand& a, int64_t end, int64_t row, int64_t n, const int (&jw)[CHUNKS], const F& product) {
-  constexpr bool kSingle = sizeof(T) == 4;
-  constexpr int kPer = 16 / sizeof(T);
-  typedef Vec16<T> V;
+// Whole tiles of 16 rows, first to last, and 64 columns from n on: the rows' factors as they were packed, DEPTH tiles on their way.  Rows are the
+// product's rows here: lane (i, q) ends with columns 4 i .. + 3 (tile t of the four has columns 4 m + t) of rows 4 q .. + 3, 16 lanes a row.
+// Nothing here branches but the loop, so that a wait is for one tile and not for all.  (The streaming hint on y: 140 us for 130,
+// reading and writing 16384 x 11008 bfloat16.)
+template <class T, int PIECES, int CHUNKS, int PARTS, int DEPTH, bool BASE>
+__device__ __forceinline__ void expand_tiles(const AdapterExpand& a, int64_t first, int64_t last, int64_t n, const Frag<T> (&fw)[4][CHUNKS]) {
   const int lane = threadIdx.x & 63, i = lane & 15, q = lane >> 4;
   struct Tile {
-    V base[PIECES];
-    Raw8<float> p[CHUNKS];
+    Four<T> base[4];
+    Piece<T> p[PIECES];
   };
-  const auto load = [&](int64_t at, Tile& d) {
-    const int64_t l = min(at + i, end - 1);
+  const int64_t from = (first + q * 4) * a.N + n + i * 4;
+  const T* const factors = (const T*)a.packed + (first >> 4) * PIECES * kTile + lane * (16 / (int)sizeof(T));
+  const int count = (int)((last - first) / 16) + 1;
+  const auto load = [&](int tile, Tile& d) {
+    const int t = min(tile, count - 1);
     if constexpr (BASE) {
 #pragma unroll
-      for (int h = 0; h < PIECES; ++h) d.base[h] = load16((const T*)a.base + l * a.N + n + q * kPer + h * 4 * kPer);
+      for (int e = 0; e < 4; ++e) d.base[e] = load4((const T*)a.base + from + (t * 16 + e) * a.N);
     }
 #pragma unroll
-    for (int c = 0; c < CHUNKS; ++c) d.p[c] = load8(a.p + l * a.pitch + jw[c], 8);
+    for (int c = 0; c < PIECES; ++c) d.p[c] = load_piece<256>(factors + ((int64_t)t * PIECES + c) * kTile);
   };
-  // Rows past the end are the last one's once more, the same sums, stored by several lanes.
-  const auto finish = [&](int64_t at, const Tile& d) {
-    const int64_t l = min(at + i, end - 1);
+  const auto finish = [&](int tile, const Tile& d) {
     f4 acc[4];
 #pragma unroll
     for (int t = 0; t < 4; ++t) acc[t] = f4{0.0f, 0.0f, 0.0f, 0.0f};
-    product(d.p, acc);
-    T* const to = (T*)a.y + l * a.N + n + q * kPer;
 #pragma unroll
-    for (int h = 0; h < PIECES; ++h)
-      store16(to + h * 4 * kPer, sum16(BASE ? d.base[h] : V{}, acc[kSingle ? h : 2 * h], acc[kSingle ? h : 2 * h + 1]));
+    for (int c = 0; c < CHUNKS; ++c)
+#pragma unroll
+      for (int part = 0; part < PARTS; ++part)
+#pragma unroll
+        for (int t = 0; t < 4; ++t) acc[t] = mma(frag(d.p[c * PARTS + part]), fw[t][c], acc[t]);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const f4 v = {acc[0][e], acc[1][e], acc[2][e], acc[3][e]};
+      *(typename Four<T>::V*)((T*)a.y + from + (tile * 16 + e) * a.N) = sum4(BASE ? d.base[e] : Four<T>{}, v).v;
+    }
   };
-  // The tile that is loaded again past the last one is never used, so that y may be base.
-  const int64_t last = row + (end - 1 - row) / 16 * 16;
   Tile d[DEPTH];
 #pragma unroll
-  for (int s = 0; s < DEPTH - 1; ++s) load(min(row + s * 16, last), d[s]);
-  int64_t at = row;
-  for (; at + (DEPTH - 1) * 16 <= last; at += DEPTH * 16) {
+  for (int s = 0; s < DEPTH - 1; ++s) load(s, d[s]);
+  int at = 0;
+  for (; at + DEPTH <= count; at += DEPTH) {
 #pragma unroll
     for (int s = 0; s < DEPTH; ++s) {
-      load(min(at + (s + DEPTH - 1) * 16, last), d[(s + DEPTH - 1) % DEPTH]);
+      load(at + s + DEPTH - 1, d[(s + DEPTH - 1) % DEPTH]);
       __builtin_amdgcn_sched_barrier(0);
-      finish(at + s * 16, d[s]);
+      finish(at + s, d[s]);
       __builtin_amdgcn_sched_barrier(0);
     }
   }
 #pragma unroll
   for (int s = 0; s < DEPTH - 1; ++s)
-    if (at + s * 16 <= last) finish(at + s * 16, d[s]);
+    if (at + s < count) finish(at + s, d[s]);
 }
 
-// ---- expand ---------------------------------------------------------------------------------------
-// RC chunks of 32 ranks (0: at most 16 ranks; the chunk's second half is the second part of the same ranks).
-// A wave holds the factors of 64 columns and goes over the rows, DEPTH tiles of 16 of them on their way; the four waves of a workgroup are
-// side by side.  A lane has its columns in pieces of 16 bytes, four lanes 64 bytes in a row: fp32 in the order of the four tiles of
-// 16; bfloat16 with the columns 8 (m / 4) + 4 (t % 2) + m % 4 of half t / 2 in row m of tile t, so that two tiles make a piece.
+// RC chunks of 32 ranks (0: at most 16 ranks; in bfloat16 the chunk's second half is the second part of the same ranks).  A wave holds the
+// factors of 64 columns and goes over the rows; the four waves of a workgroup are side by side.
 template <class T, int RC, int DEPTH>
 __global__ __launch_bounds__(256) void expand_kernel(const AdapterExpand a, int col_groups, int64_t chunk) {
   constexpr bool kSingle = sizeof(T) == 4, kPack = RC == 0 && !kSingle;
   constexpr int kChunks = RC == 0 ? 1 : RC, kParts = kSingle || kPack ? 1 : 2;
-  constexpr int kPer = 16 / sizeof(T), kPieces = sizeof(T);       // a lane's pieces of 16 bytes of 64 columns: 4 or 2
-  typedef Vec16<T> V;
   const int lane = threadIdx.x & 63, i = lane & 15, q = lane >> 4, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int group = (int)(blockIdx.x % col_groups);
   const int64_t n = (int64_t)group * 256 + wave * 64;
@@ -346,7 +412,6 @@ __global__ __launch_bounds__(256) void expand_kernel(const AdapterExpand a, int 
   const bool whole = n + 64 <= a.N;
   const int64_t row0 = (int64_t)(blockIdx.x / col_groups) * chunk, row1 = min(row0 + chunk, a.b.L);
   const bool writes_u = a.u && group == 0 && wave == 0;
-  const int j0 = kPack ? (q & 1) * 8 : q * 8;      // this lane's ranks within a chunk
 
   for (int64_t row = row0; row < row1;) {
     const Run run = run_at(a.b, row, row1);
@@ -356,104 +421,91 @@ __global__ __launch_bounds__(256) void expand_kernel(const AdapterExpand a, int 
     }
     const bool none = run.adapter < 0;
     const float scale = none ? 0.0f : a.scale ? a.scale[run.adapter] : 1.0f;
-    // A row's last ranks are loaded as its last eight: p as they are, with zeros for those that another lane has.
-    int jw[kChunks];
-#pragma unroll
-    for (int c = 0; c < kChunks; ++c) jw[c] = a.w_cols < 8 ? 0 : min(c * 32 + j0, a.w_cols - 8);
+    // Ranks of this lane: bfloat16 8 q .. + 7 of a chunk (of its half, where that is all), fp32 4 q .. + 3 and 16 + 4 q .. + 3.
     Frag<T> fw[4][kChunks];
     if (!none) {
       const T* const w = (const T*)a.w + run.adapter * a.w_stride;
 #pragma unroll
       for (int t = 0; t < 4; ++t) {
-        const int64_t wn = min(n + (kSingle ? t * 16 + i : t / 2 * 32 + (i >> 2) * 8 + t % 2 * 4 + (i & 3)), a.N - 1);
+        const T* const at = w + min(n + i * 4 + t, a.N - 1) * a.w_pitch;
 #pragma unroll
-        for (int c = 0; c < kChunks; ++c) fw[t][c] = frag(load8(w + wn * a.w_pitch + jw[c], RC == 0 ? min(a.w_cols, 8) : 8));
+        for (int c = 0; c < kChunks; ++c) fw[t][c] = frag(load_piece_of(at + c * 32, kPack ? q & 1 : q, a.rank - c * 32));
       }
     }
-    const auto product = [&](const Raw8<float> (&p)[kChunks], f4 (&acc)[4]) {
-#pragma unroll
-      for (int c = 0; c < kChunks; ++c) {
-        float v[8];
-        widen(p[c], v);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = (jw[c] + e >= c * 32 + j0 ? v[e] : 0.0f) * scale;
-        Frag<T> f[kParts];
-        if constexpr (kSingle) {
-#pragma unroll
-          for (int e = 0; e < 8; ++e) f[0].v[e] = v[e];
-        } else if constexpr (kPack) {
-          Frag<bf16> two[2];
-          split8<2>(v, two);
-          f[0] = q < 2 ? two[0] : two[1];
-        } else {
-          split8<2>(v, f);
-        }
-#pragma unroll
-        for (int part = 0; part < kParts; ++part)
-#pragma unroll
-          for (int t = 0; t < 4; ++t) acc[t] = mma(fw[t][c], f[part], acc[t]);
-      }
-    };
-    if (whole && !none && a.slices == 1 && run.end - row >= 16 * DEPTH) {
-      if (a.base) expand_rows<T, kPieces, kChunks, DEPTH, true>(a, run.end, row, n, jw, product);
-      else expand_rows<T, kPieces, kChunks, DEPTH, false>(a, run.end, row, n, jw, product);
-      row = run.end;
-      continue;
+    const int64_t first = (row + 15) & -16ll, last = (run.end & -16ll) - 16;      // whole tiles
+    const bool tiles = whole && !none && a.packed && first <= last;
+    if (tiles) {
+      if (a.base) expand_tiles<T, kChunks * kParts, kChunks, kParts, DEPTH, true>(a, first, last, n, fw);
+      else expand_tiles<T, kChunks * kParts, kChunks, kParts, DEPTH, false>(a, first, last, n, fw);
     }
-    for (int64_t at = row; at < run.end; at += 16) {       // few rows, rows without an adapter, the last columns
-      const int64_t l = min(at + i, run.end - 1);
+    // The rows beside whole tiles; all of them where there are slices of the factors, no adapter, or not 64 columns.  Columns are the
+    // product's rows here: lane (i, q) ends with columns 16 q + 4 e + t of row i.
+    for (int64_t at = row; at < run.end; at += 16) {
+      if (tiles && at >= first && at <= last) {
+        at = last;
+        continue;
+      }
+      const int64_t end = tiles && at < first ? first : run.end;
+      const int64_t l = min(at + i, end - 1);
+      const bool mine = at + i < end;
       f4 acc[4];
 #pragma unroll
       for (int t = 0; t < 4; ++t) acc[t] = f4{0.0f, 0.0f, 0.0f, 0.0f};
-      V have[kPieces];
-      if (whole && a.base) {
-#pragma unroll
-        for (int h = 0; h < kPieces; ++h) have[h] = load16((const T*)a.base + l * a.N + n + q * kPer + h * 4 * kPer);
-      } else {
-#pragma unroll
-        for (int h = 0; h < kPieces; ++h) have[h] = V{};
-      }
       if (!none) {
-        Raw8<float> p[kChunks];
 #pragma unroll
-        for (int c = 0; c < kChunks; ++c) p[c] = load8(a.p + l * a.pitch + jw[c], 8);
+        for (int c = 0; c < kChunks; ++c) {
+          const int jq = kPack ? q & 1 : q, left = a.rank - c * 32;
+          Piece<float> p = load_piece_as<T>(a.p + l * a.pitch + c * 32, jq, left);
 #pragma unroll 4
-        for (int s = 1; s < a.slices; ++s) {
-#pragma unroll
-          for (int c = 0; c < kChunks; ++c) {
-            const Raw8<float> more = load8(a.p + ((int64_t)s * a.b.L + l) * a.pitch + jw[c], 8);
-            p[c].a += more.a;
-            p[c].b += more.b;
+          for (int s = 1; s < a.slices; ++s) {
+            const Piece<float> more = load_piece_as<T>(a.p + ((int64_t)s * a.b.L + l) * a.pitch + c * 32, jq, left);
+            p.v[0] += more.v[0];
+            p.v[1] += more.v[1];
           }
-        }
-        product(p, acc);
-        if (writes_u && at + i < run.end && !(kPack && q >= 2)) {
+          if (writes_u && mine && !(kPack && q >= 2)) {
 #pragma unroll
-          for (int c = 0; c < kChunks; ++c) {
-            float v[8];
-            widen(p[c], v);
-#pragma unroll
-            for (int e = 0; e < 8; ++e)
-              if (jw[c] + e >= c * 32 + j0 && jw[c] + e < a.rank) a.u[l * a.rank + jw[c] + e] = v[e];
+            for (int e = 0; e < 8; ++e) {
+              const int j = kSingle ? e / 4 * 16 + q * 4 + e % 4 : q * 8 + e;
+              if (j < left) a.u[l * a.rank + c * 32 + j] = p.v[e / 4][e % 4];
+            }
           }
+          float v[8];
+#pragma unroll
+          for (int e = 0; e < 8; ++e) v[e] = p.v[e / 4][e % 4] * scale;
+          Frag<T> f[kParts];
+          if constexpr (kSingle) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) f[0].v[e] = v[e];
+          } else if constexpr (kPack) {
+            Frag<bf16> two[2];
+            split8<2>(v, two);
+            f[0] = q < 2 ? two[0] : two[1];
+          } else {
+            split8<2>(v, f);
+          }
+#pragma unroll
+          for (int part = 0; part < kParts; ++part)
+#pragma unroll
+            for (int t = 0; t < 4; ++t) acc[t] = mma(fw[t][c], f[part], acc[t]);
         }
-      } else if (writes_u && at + i < run.end) {
+      } else if (writes_u && mine) {
         for (int j = q; j < a.rank; j += 4) a.u[l * a.rank + j] = 0.0f;
       }
-      if (at + i >= run.end) continue;
-      T* const to = (T*)a.y + l * a.N + n + q * kPer;
-      if (whole) {
+      const int64_t to = l * a.N + n + q * 16;
+      if (mine && whole) {
 #pragma unroll
-        for (int h = 0; h < kPieces; ++h)
-          store16(to + h * 4 * kPer, sum16(have[h], acc[kSingle ? h : 2 * h], acc[kSingle ? h : 2 * h + 1]));
-      } else {                // one by one
-        const T* const from = (const T*)a.base + l * a.N + n + q * kPer;
-#pragma unroll
-        for (int e = 0; e < 16; ++e) {
-          const int c = kSingle ? e / 4 * 16 + e % 4 : e / 8 * 32 + e % 8;
-          if (n + q * kPer + c < a.N) to[c] = (T)(acc[e / 4][e & 3] + (a.base ? (float)from[c] : 0.0f));
+        for (int e = 0; e < 4; ++e) {
+          const f4 v = {acc[0][e], acc[1][e], acc[2][e], acc[3][e]};
+          const Four<T> base = a.base ? load4((const T*)a.base + to + e * 4) : Four<T>{};
+          *(typename Four<T>::V*)((T*)a.y + to + e * 4) = sum4(base, v).v;
         }
+      } else if (mine) {
+        for (int e = 0; e < 4; ++e)
+          for (int t = 0; t < 4; ++t)
+            if (n + q * 16 + e * 4 + t < a.N)
+              ((T*)a.y)[to + e * 4 + t] = (T)(acc[t][e] + (a.base ? (float)((const T*)a.base)[to + e * 4 + t] : 0.0f));
       }
+      if (tiles && at < first) at = first - 16;
     }
     row = run.end;
   }
@@ -527,18 +579,35 @@ __device__ void sort_segments(const AdapterPrepare& a, int k) {
   }
 }
 
-// to[c][r] of `from` [rows x cols]: at c * c_pitch + r, in groups of `group` r's that are g_pitch apart; r up to `held`, zeros past the rows.
+// Rows `j` and reduced elements `k` of weights, at j * by_j + k * by_k, in the order of the lanes: [K / 32][tiles of 16 rows] packed tiles, zeros past
+// the last ones.  A lane: eight of them.
 template <class T>
-__device__ void transpose_tile(const T* from, int64_t rows, int64_t cols, T* to, int64_t c_pitch, int64_t group, int64_t g_pitch, int64_t held,
-                               int64_t r0, int64_t c0) {
+__device__ void pack_weights(const T* w, int64_t by_j, int64_t by_k, int rows, int64_t K, T* out, int64_t block) {
+  const int lane = threadIdx.x & 63, i = lane & 15, q = lane >> 4, tiles = (rows + 15) / 16;
+  const int64_t tile = block * 4 + (threadIdx.x >> 6), k0 = tile / tiles * 32;
+  if (k0 >= ((K + 63) & -64ll)) return;
+  const int j = (int)(tile % tiles) * 16 + i;
+  T v[8];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    const int64_t k = k0 + (sizeof(T) == 4 ? e / 4 * 16 + q * 4 + e % 4 : q * 8 + e);
+    v[e] = j < rows && k < K ? w[j * by_j + k * by_k] : (T)0.0f;
+  }
+  T* const to = out + tile * kTile;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) to[sizeof(T) == 4 ? e / 4 * 256 + lane * 4 + e % 4 : lane * 8 + e] = v[e];
+}
+
+// at[n][j] of a [rank x I].
+template <class T>
+__device__ void transpose_tile(const T* from, int64_t rows, int64_t cols, T* to, int64_t r0, int64_t c0) {
   __shared__ T s_tile[64][65];
   const int x = threadIdx.x & 63, y = threadIdx.x >> 6;
   for (int r = y; r < 64; r += 4)
-    s_tile[r][x] = r0 + r < rows && c0 + x < cols ? from[(r0 + r) * cols + c0 + x] : (T)0.0f;
+    if (r0 + r < rows && c0 + x < cols) s_tile[r][x] = from[(r0 + r) * cols + c0 + x];
   __syncthreads();
-  const int64_t r = r0 + x, at = r / group * g_pitch + r % group;
   for (int c = y; c < 64; c += 4)
-    if (c0 + c < cols && r < held) to[(c0 + c) * c_pitch + at] = s_tile[x][c];
+    if (c0 + c < cols && r0 + x < rows) to[(c0 + c) * rows + r0 + x] = s_tile[x][c];
 }
 
 template <class T>
@@ -551,33 +620,28 @@ __global__ __launch_bounds__(256) void prepare_kernel(const AdapterPrepare a, in
   b -= sorts;
   const int per = tiles_a + tiles_w, k = b / per, t = b % per;
   if (t < tiles_a)
-    transpose_tile((const T*)a.a + (int64_t)k * a.rank * a.I, a.rank, a.I, (T*)a.at + (int64_t)k * a.I * a.rank_pitch, a.rank_pitch,
-                   (int64_t)a.rank_pitch, 0, a.rank_pitch, (int64_t)(t % rank_tiles) * 64, (int64_t)(t / rank_tiles) * 64);
+    transpose_tile((const T*)a.a + (int64_t)k * a.rank * a.I, a.rank, a.I, (T*)a.at + (int64_t)k * a.I * a.rank, (int64_t)(t % rank_tiles) * 64,
+                   (int64_t)(t / rank_tiles) * 64);
   else
-    transpose_tile((const T*)a.w + (int64_t)k * a.O * a.rank, a.O, a.rank, (T*)a.wt + k * a.wt_stride, 128 / (int64_t)sizeof(T),
-                   128 / (int64_t)sizeof(T), a.rank * (128 / (int64_t)sizeof(T)), a.wt_stride / a.rank, (int64_t)((t - tiles_a) / rank_tiles) * 64,
-                   (int64_t)((t - tiles_a) % rank_tiles) * 64);
+    pack_weights((const T*)a.w + (int64_t)k * a.rank * a.K, a.by_j, a.by_k, a.rank, a.K, (T*)a.wt + k * a.wt_stride, t - tiles_a);
 }
 
 // ---- outer ----------------------------------------------------------------------------------------
 // Rows of a part of the sums over `total` rows.
 __device__ __forceinline__ int64_t rows_of_part(int64_t total, int parts) { return ((total + parts - 1) / parts + 31) & -32ll; }
 
-// Elements m .. n - 1 of eight, zeros beside them.
-__device__ __forceinline__ Raw8<bf16> between(const Raw8<bf16>& r, int m, int n) {
-  Raw8<bf16> o;
+// Row e of lane quarter q in a step of 32 rows, in the order that pieces have.
+template <class T>
+__device__ __forceinline__ int row_in_step(int q, int e) { return sizeof(T) == 4 ? e / 4 * 16 + q * 4 + e % 4 : q * 8 + e; }
+// Rows m .. n - 1 of a step, zeros beside them.
+__device__ __forceinline__ void keep_rows(Piece<bf16>& p, int q, int m, int n) {
 #pragma unroll
-  for (int e = 0; e < 8; ++e) o.a[e] = e >= m && e < n ? r.a[e] : (uint16_t)0;
-  return o;
+  for (int e = 0; e < 8; ++e) p.v[e] = row_in_step<bf16>(q, e) >= m && row_in_step<bf16>(q, e) < n ? p.v[e] : (uint16_t)0;
 }
-__device__ __forceinline__ Raw8<float> between(const Raw8<float>& r, int m, int n) {
-  Raw8<float> o;
+__device__ __forceinline__ void keep_rows(Piece<float>& p, int q, int m, int n) {
 #pragma unroll
-  for (int e = 0; e < 4; ++e) {
-    o.a[e] = e >= m && e < n ? r.a[e] : 0.0f;
-    o.b[e] = e + 4 >= m && e + 4 < n ? r.b[e] : 0.0f;
-  }
-  return o;
+  for (int e = 0; e < 8; ++e)
+    p.v[e / 4][e % 4] = row_in_step<float>(q, e) >= m && row_in_step<float>(q, e) < n ? p.v[e / 4][e % 4] : 0.0f;
 }
 
 // Eight rows of eight columns a lane.  bfloat16: column c's eight rows come together in 32 byte permutes; fp32: they are registers.
@@ -603,8 +667,8 @@ __device__ __forceinline__ void columns_of(const Raw8<float> (&rows)[8], Frag<fl
 }
 
 // u and g_u for the sums over rows: rows in the order of their adapters, a rank's factors of 32 rows one after the other, so that a lane's eight
-// rows are one load; bfloat16 in its three parts.  [steps of 32 rows][parts][ranks rounded up to 16][32] of T: what a wave loads at a time
-// lies together (ranks a long row apart meet in a few channels of the caches).  A workgroup: 64 positions of one operand.
+// rows are one load; bfloat16 in its three parts.  packed tiles of 16 ranks and 32 rows, [steps of 32 rows][parts][tiles]: what a wave loads lies
+// together, in the order of its lanes.  A workgroup: 64 positions of one operand.
 template <class T>
 __global__ __launch_bounds__(256) void pack_kernel(const AdapterPack a) {
   constexpr int kParts = sizeof(T) == 4 ? 1 : 3;
@@ -653,14 +717,17 @@ __global__ __launch_bounds__(256) void pack_kernel(const AdapterPack a) {
     float v[8];
 #pragma unroll
     for (int e = 0; e < 8; ++e) v[e] = s_p[j * 65 + x + e];
-    T* const to = out + (((pos0 + x) / 32 * kParts) * ranks + j) * 32 + x % 32;
+    T* const to = out + ((pos0 + x) / 32 * kParts * (ranks / 16) + j / 16) * kTile;
+    const int q = x % 32 / 8;
     if constexpr (kParts == 1) {
-      store8(to, v, 8);
+#pragma unroll
+      for (int e = 0; e < 2; ++e)       // rows 8 q + 4 e .. + 3 of 32: piece x % 32 / 16, of lane (j, x / 4 % 4)
+        *(f4_any*)((float*)to + (x % 32 / 16) * 256 + (((x / 4 + e) & 3) * 16 + j % 16) * 4) = f4_any{v[4 * e], v[4 * e + 1], v[4 * e + 2], v[4 * e + 3]};
     } else {
       Frag<bf16> f[kParts];
       split8<kParts>(v, f);
 #pragma unroll
-      for (int part = 0; part < kParts; ++part) *(u4*)(to + part * ranks * 32) = f[part].v;
+      for (int part = 0; part < kParts; ++part) *(u4*)(to + part * (ranks / 16) * kTile + (q * 16 + j % 16) * 8) = f[part].v;
     }
   }
 }
@@ -702,13 +769,13 @@ __global__ __launch_bounds__(64 * kOuterWaves) void outer_kernel(const AdapterOu
     for (int t = 0; t < RT; ++t)
 #pragma unroll
       for (int c = 0; c < 8; ++c) acc[t][c] = f4{0.0f, 0.0f, 0.0f, 0.0f};
-    Raw8<T> p[RT][kParts];
-    const T* const p_at = (const T*)o.p + (rank0 + i) * 32 + q * 8;
+    Piece<T> p[RT][kParts];
+    const T* const p_at = (const T*)o.p + rank0 * 32 + lane * (16 / (int)sizeof(T));
     const int64_t begin = pos & -32ll, last = (k_end - 1) & -32ll;          // the first and the last step
     const auto rows_at = [&](int64_t at, int (&r)[8]) {          // beside the rows: the nearest one, times zero
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        const int64_t l = max(min(at + q * 8 + e, k_end - 1), pos);
+        const int64_t l = max(min(at + row_in_step<T>(q, e), k_end - 1), pos);
         r[e] = MODE ? a.rows[l] : (int)l;
       }
     };
@@ -721,17 +788,17 @@ __global__ __launch_bounds__(64 * kOuterWaves) void outer_kernel(const AdapterOu
       }
     };
     const auto load_p = [&](int t, int64_t at) {     // ranks past the last tile: the last tile's, whose sums are not stored
-      const int64_t j = min(t * 16, ranks - 16 - rank0);
+      const int64_t tile = min(t, (ranks - rank0) / 16 - 1);
 #pragma unroll
-      for (int s = 0; s < kParts; ++s) p[t][s] = load8(p_at + at * kParts * ranks + (s * ranks + j) * 32, 8);
+      for (int s = 0; s < kParts; ++s) p[t][s] = load_piece<256>(p_at + at * kParts * ranks + (s * (ranks / 16) + tile) * kTile);
     };
     const auto multiply = [&](int64_t at, const Raw8<T> (&x)[8]) {
       if (at == last || at < pos) {                              // zeros beside the rows
-        const int n = (int)min(max(k_end - at - q * 8, (int64_t)0), (int64_t)8), m = (int)max(pos - at - q * 8, (int64_t)0);
+        const int n = (int)min(k_end - at, (int64_t)32), m = (int)max(pos - at, (int64_t)0);
 #pragma unroll
         for (int t = 0; t < RT; ++t)
 #pragma unroll
-          for (int s = 0; s < kParts; ++s) p[t][s] = between(p[t][s], m, n);
+          for (int s = 0; s < kParts; ++s) keep_rows(p[t][s], q, m, n);
       }
       Frag<T> f[8];
       columns_of(x, f);
@@ -827,9 +894,10 @@ template <class T, int RT>
 hipError_t run_shrink(const AdapterShrink& a, int tile, hipStream_t s) {
   constexpr int kDepth = RT <= 2 ? 4 : RT == 4 ? 3 : 2;     // as the registers of two waves allow
   const uint32_t grid = (uint32_t)(ceil_div(a.b.L, tile) * a.slices);
-  if (tile == 1) shrink_kernel<T, RT, 1, 1, kDepth><<<grid, 256, 0, s>>>(a);
-  else if (tile == 16 || RT == 8) shrink_kernel<T, RT, 1, 16, kDepth><<<grid, 256, 0, s>>>(a);
-  else shrink_kernel<T, RT, 2, 32, kDepth><<<grid, 256, 0, s>>>(a);
+  const auto run = [&](auto kernel) { kernel<<<grid, 256, 0, s>>>(a); };
+  if (tile == 1) a.w_packed ? run(shrink_kernel<T, RT, 1, 1, kDepth, true>) : run(shrink_kernel<T, RT, 1, 1, kDepth, false>);
+  else if (tile == 16 || RT == 8) a.w_packed ? run(shrink_kernel<T, RT, 1, 16, kDepth, true>) : run(shrink_kernel<T, RT, 1, 16, kDepth, false>);
+  else a.w_packed ? run(shrink_kernel<T, RT, 2, 32, kDepth, true>) : run(shrink_kernel<T, RT, 2, 32, kDepth, false>);
   return hipGetLastError();
 }
 template <class T>
@@ -880,7 +948,6 @@ AdapterPlan adapter_plan(hot_type type, int64_t L, int64_t O, int64_t I, int64_t
   const int64_t size = type == HOT_BF16 ? 2 : 4, step = 128 / size;
   p.rows = L <= 4 * (segments > 0 ? segments : 1) && L <= 1 << 20;
   p.pitch = (int)round_up(rank, 8);      // zeros behind the ranks
-  p.rank_pitch = (int)round_up(rank, 8);
   // Rows of a workgroup: as many as leave workgroups for all compute units without slices, 16 at least.
   p.tile = p.rows ? 1 : L >= 64 * 32 && rank <= 64 ? 32 : 16;
   const auto slices = [&](int64_t K, int& count, int64_t& slice) {
@@ -900,16 +967,27 @@ AdapterPlan adapter_plan(hot_type type, int64_t L, int64_t O, int64_t I, int64_t
   p.parts = (int)(wanted < most ? wanted : most);
   p.positions = round_up(L, 64);
 
+  // Packed weights of the forward call: 2 to 4 us for a launch, against 48 cycles of a compute unit's memory pipe for each kilobyte of
+  // weights and 32 rows (16384 x 4096, rank 64: 53 us without).
+  p.pack_forward = !p.rows && ceil_div(L, 32) * (rank * I * size / 1024) > 60000;
+  p.chunks = rank <= 16 && type == HOT_BF16 ? 0 : rank <= 32 ? 1 : rank <= 64 ? 2 : 4;    // as the expansion's kernels have them
+  p.wt_stride = round_up(rank, 16) * round_up(I > O ? I : O, 64);
   const int64_t row_bytes = L * p.pitch * 4;
-  p.forward = (size_t)round_up(row_bytes * p.slices_forward, 256);
-  size_t at = (size_t)round_up(row_bytes * p.slices_backward, 256);
+  const int64_t factors = ceil_div(L, 16) * kTile * size * (type == HOT_BF16 ? (p.chunks ? 2 * p.chunks : 1) : p.chunks);
+  size_t at = 0;
   const auto take = [&](int64_t bytes) {
     const size_t here = at;
     at += (size_t)round_up(bytes, 256);
     return here;
   };
-  p.at = take(adapters * I * p.rank_pitch * size);
-  p.wt = take(adapters * rank * round_up(O, step) * size);
+  const int slices_most = p.slices_forward > p.slices_backward ? p.slices_forward : p.slices_backward;
+  take(row_bytes * slices_most);
+  p.factors = take(factors);
+  p.wt = take(p.pack_forward ? adapters * p.wt_stride * size : 0);
+  p.forward = at;
+  at = p.wt;
+  take(adapters * p.wt_stride * size);
+  p.at = take(adapters * I * rank * size);
   p.sorted = take((2 * segments + 1 + adapters + 1 + p.positions) * 4);
   p.packed = take(2 * (type == HOT_BF16 ? 3 : 1) * size * round_up(rank, 16) * p.positions);
   p.part_a = take((p.parts + adapters) * rank * I * 4);
@@ -925,13 +1003,12 @@ hipError_t launch_adapter_expand(const AdapterExpand& a, bool rows, hot_type typ
   return type == HOT_BF16 ? expand_of<bf16>(a, rows, s) : expand_of<float>(a, rows, s);
 }
 hipError_t launch_adapter_prepare(const AdapterPrepare& a, hot_type type, hipStream_t s) {
-  const int sorts = a.b.offsets ? a.b.adapters : 0;
-  const int rank_tiles = (int)ceil_div(a.rank_pitch, 64);
-  const int tiles_a = a.at ? (int)ceil_div(a.I, 64) * rank_tiles : 0, tiles_w = a.wt ? (int)ceil_div(a.O, 64) * rank_tiles : 0;
-  const int64_t grid = sorts + (int64_t)a.b.adapters * (tiles_a + tiles_w);
-  if (grid == 0) return hipSuccess;
-  if (type == HOT_BF16) prepare_kernel<bf16><<<(uint32_t)grid, 256, 0, s>>>(a, sorts, tiles_a, tiles_w, rank_tiles);
-  else prepare_kernel<float><<<(uint32_t)grid, 256, 0, s>>>(a, sorts, tiles_a, tiles_w, rank_tiles);
+  const int sorts = a.order ? a.b.adapters : 0;
+  const int rank_tiles = (int)ceil_div(a.rank, 64);
+  const int tiles_a = a.at ? (int)ceil_div(a.I, 64) * rank_tiles : 0, tiles_w = (int)ceil_div(round_up(a.K, 64) / 32 * ceil_div(a.rank, 16), 4);
+  const uint32_t grid = (uint32_t)(sorts + (int64_t)a.b.adapters * (tiles_a + tiles_w));
+  if (type == HOT_BF16) prepare_kernel<bf16><<<grid, 256, 0, s>>>(a, sorts, tiles_a, tiles_w, rank_tiles);
+  else prepare_kernel<float><<<grid, 256, 0, s>>>(a, sorts, tiles_a, tiles_w, rank_tiles);
   return hipGetLastError();
 }
 hipError_t launch_adapter_pack(const AdapterPack& a, hot_type type, hipStream_t s) {

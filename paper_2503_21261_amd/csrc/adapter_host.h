@@ -19,10 +19,14 @@ struct AdapterShrink {
   AdapterBatch b;
   const void *q, *w;
   float* out;
-  int64_t K, w_pitch, w_stride, w_step;   // w: elements from j to j + 1, from adapter to adapter, and a step's distance in units of its length
-  int rank, pitch, slices;
+  int64_t K, w_stride;              // w: [rank][K], or packed tiles; elements from adapter to adapter
+  int w_packed, rank, pitch, slices;
   int64_t slice;                    // columns of a slice
-  float* u;                         // the sums again, [L][rank] (zeros where a row has no adapter), without slices; or null
+  // Without slices: the sums again, [L][rank] (zeros where a row has no adapter); and scaled, as the expansion takes them; or null.
+  float* u;
+  void* packed;
+  const float* scale;
+  int chunks;                       // chunks of 32 ranks of those; 0: one that holds 16 ranks and their second parts
 };
 // y[l][n] = base[l][n] + scale[adapter(l)] * sum over j of p[l][j] w[adapter(l)][n][j], p the sum of the slices.
 struct AdapterExpand {
@@ -32,9 +36,9 @@ struct AdapterExpand {
   const float* scale;
   void* y;
   float* u;                         // p itself, [L][rank]; null: not wanted
+  const void* packed;               // scale * p in the order of the lanes; null: there are slices
   int64_t N, w_pitch, w_stride;
   int rank, pitch, slices;
-  int w_cols;                       // elements of a row of w: rank, or more with zeros behind
 };
 // u and g_u (the sum of its slices) for the sums over rows: [steps of 32 rows][parts][ranks rounded up to 16][32], rows in the order of their
 // adapters, and that order itself.
@@ -67,26 +71,27 @@ struct AdapterReduce {
   float *g_a, *g_b;
   int rank, parts, adapters;
 };
-// Before a backward call: segments sorted by adapter, and both weights transposed.
+// Before the first product: weights packed in the order of its lanes; in a backward call also segments sorted by adapter, and the transpose
+// of the second product's weights.
 struct AdapterPrepare {
   AdapterBatch b;
-  const void *a, *w;                // a [adapters][rank][I], w [adapters][O][rank]
-  void *at, *wt;                    // [adapters][I][rank_pitch], [adapters][steps of 128 bytes of O][rank][step]
-  int64_t I, O;
-  int rank, rank_pitch;
-  int64_t wt_stride;
-  int32_t *order, *start, *first;
+  const void *a, *w;                // a [adapters][rank][I]; w [adapters][rank * K], element (j, k) at j * by_j + k * by_k
+  void *at, *wt;                    // [adapters][I][rank] (null: not wanted), [adapters][wt_stride]
+  int64_t I, K, by_j, by_k, wt_stride;
+  int rank;
+  int32_t *order, *start, *first;   // null: not wanted
 };
 
 struct AdapterPlan {
   bool rows;                        // a wave works on one row, not on a tile of them
+  bool pack_forward;                // the forward call packs its weights
   int tile;                         // rows of a workgroup of the first product
   int pitch;                        // floats of a row of p
+  int chunks;
   int slices_forward, slices_backward, parts;
-  int64_t slice_forward, slice_backward;
-  int rank_pitch;
-  int64_t positions;                // of the packed factors
-  size_t at, wt, sorted, packed, part_a, part_b, forward, backward;   // offsets into the workspace, and its sizes
+  int64_t slice_forward, slice_backward, wt_stride;
+  int64_t positions;                // of the packed factors of the sums over rows
+  size_t factors, wt, at, sorted, packed, part_a, part_b, forward, backward;   // offsets into the workspace, and its sizes
 };
 AdapterPlan adapter_plan(hot_type type, int64_t L, int64_t O, int64_t I, int64_t rank, int64_t adapters, int64_t segments);
 

@@ -89,11 +89,20 @@ hot_status hot_adapter_forward(const void* x, const void* a, const void* b, hot_
   if (ws_bytes < p.forward) return HOT_ERR_WORKSPACE;
   hipStream_t s = (hipStream_t)stream;
   const AdapterBatch batch{offsets, index, (int)segments, (int)adapters, L};
-  const AdapterShrink shrink{batch, x, a, (float*)ws, I, I, rank * I, 1, (int)rank, p.pitch, p.slices_forward, p.slice_forward,
-                             p.slices_forward == 1 ? u : nullptr};
+  char* const w = (char*)ws;
+  const bool sliced = p.slices_forward > 1;
+  AdapterShrink shrink{batch, x, a, (float*)ws, I, rank * I, 0, (int)rank, p.pitch, p.slices_forward, p.slice_forward,
+                       sliced ? nullptr : u, sliced ? nullptr : w + p.factors, scale, p.chunks};
+  if (p.pack_forward) {
+    const AdapterPrepare prepare{batch, nullptr, a, nullptr, w + p.wt, I, I, I, 1, p.wt_stride, (int)rank, nullptr, nullptr, nullptr};
+    HOT_STAGE(kStAdapterPrepare, launch_adapter_prepare(prepare, type, s));
+    shrink.w = w + p.wt;
+    shrink.w_stride = p.wt_stride;
+    shrink.w_packed = 1;
+  }
   HOT_STAGE(kStAdapterShrink, launch_adapter_shrink(shrink, p.tile, type, s));
-  const AdapterExpand expand{batch, (const float*)ws, b, base, scale, y, p.slices_forward == 1 ? nullptr : u, O, rank, O * rank, (int)rank, p.pitch,
-                             p.slices_forward, (int)rank};
+  const AdapterExpand expand{batch, (const float*)ws, b, base, scale, y, sliced ? u : nullptr, shrink.packed, O, rank, O * rank, (int)rank,
+                             p.pitch, p.slices_forward};
   HOT_STAGE(kStAdapterExpand, launch_adapter_expand(expand, p.rows, type, s));
   return HOT_OK;
 }
@@ -129,14 +138,17 @@ hot_status hot_adapter_backward(const void* g_y, const void* x, const float* u, 
   int32_t* const start = order + segments;
   int32_t* const first = start + segments + 1;
   const AdapterBatch batch{offsets, index, (int)segments, (int)adapters, L};
-  const int64_t step = type == HOT_BF16 ? 64 : 32, wt_stride = rank * round_up(O, step);
-  const AdapterPrepare prepare{batch, a, b, g_x ? w + p.at : nullptr, w + p.wt, I, O, (int)rank, p.rank_pitch, wt_stride, order, start, first};
+  const bool sort = offsets && g_a;
+  const AdapterPrepare prepare{batch, a, b, g_x ? w + p.at : nullptr, w + p.wt, I, O, 1, rank, p.wt_stride, (int)rank,
+                               sort ? order : nullptr, start, first};
   HOT_STAGE(kStAdapterPrepare, launch_adapter_prepare(prepare, type, s));
-  const AdapterShrink shrink{batch, g_y, w + p.wt, g_u, O, step, wt_stride, rank, (int)rank, p.pitch, p.slices_backward, p.slice_backward, nullptr};
+  const bool sliced = p.slices_backward > 1;
+  const AdapterShrink shrink{batch, g_y, w + p.wt, g_u, O, p.wt_stride, 1, (int)rank, p.pitch, p.slices_backward, p.slice_backward,
+                             nullptr, sliced || !g_x ? nullptr : w + p.factors, scale, p.chunks};
   HOT_STAGE(kStAdapterShrink, launch_adapter_shrink(shrink, p.tile, type, s));
   if (g_x) {
-    const AdapterExpand expand{batch, g_u, w + p.at, g_base, scale, g_x, nullptr, I, p.rank_pitch, I * p.rank_pitch, (int)rank, p.pitch,
-                               p.slices_backward, p.rank_pitch};
+    const AdapterExpand expand{batch, g_u, w + p.at, g_base, scale, g_x, nullptr, shrink.packed, I, rank, I * rank, (int)rank, p.pitch,
+                               p.slices_backward};
     HOT_STAGE(kStAdapterExpand, launch_adapter_expand(expand, p.rows, type, s));
   }
   if (g_a) {
