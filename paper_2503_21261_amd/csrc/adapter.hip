@@ -52,6 +52,40 @@ __device__ __forceinline__ Piece<float> load_piece_of(const float* p, int q, int
   }
   return r;
 }
+// The same where the elements from p on are a row's last `left`, of `row` in all: a row of eight (four) or more is loaded as its last ones, and
+// they are moved down.
+__device__ __forceinline__ Piece<bf16> load_piece_end(const bf16* p, int q, int left, int row) {
+  const int n = min(max(left - q * 8, 0), 8);
+  if (row < 8) return load_piece_of(p, q, left);
+  const int by = n > 0 ? 8 - n : 0;
+  u4 v = __builtin_bit_cast(u4, *(const h8_any*)(p + (n > 0 ? q * 8 - by : left - 8)));
+  uint64_t lo = (uint64_t)v[1] << 32 | v[0], hi = (uint64_t)v[3] << 32 | v[2];
+  if (by & 4) {
+    lo = hi;
+    hi = 0;
+  }
+  const int bits = (by & 3) * 16;
+  if (bits) lo = lo >> bits | hi << (64 - bits);
+  hi >>= bits;
+  if (n == 0) lo = hi = 0;
+  v = u4{(uint32_t)lo, (uint32_t)(lo >> 32), (uint32_t)hi, (uint32_t)(hi >> 32)};
+  return Piece<bf16>{__builtin_bit_cast(h8_any, v)};
+}
+__device__ __forceinline__ Piece<float> load_piece_end(const float* p, int q, int left, int row) {
+  if (row < 4) return load_piece_of(p, q, left);
+  Piece<float> r;
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    const int at = h * 16 + q * 4, n = min(max(left - at, 0), 4), by = n > 0 ? 4 - n : 0;
+    const f4_any v = *(const f4_any*)(p + (n > 0 ? at - by : left - 4));
+    const float a = v[0], b = v[1], c = v[2], d = v[3];
+    r.v[h][0] = n == 0 ? 0.0f : by == 0 ? a : by == 1 ? b : by == 2 ? c : d;
+    r.v[h][1] = n <= 1 ? 0.0f : by == 0 ? b : by == 1 ? c : d;
+    r.v[h][2] = n <= 2 ? 0.0f : by == 0 ? c : d;
+    r.v[h][3] = n <= 3 ? 0.0f : d;
+  }
+  return r;
+}
 // fp32 numbers in the places that a piece of T has them.
 template <class T>
 __device__ __forceinline__ Piece<float> load_piece_as(const float* p, int q, int left) {
@@ -163,14 +197,21 @@ struct Run {
 };
 __device__ __forceinline__ Run run_at(const AdapterBatch& b, int64_t row, int64_t limit) {
   if (!b.offsets) return Run{0, limit};
-  const int c = __builtin_amdgcn_readfirstlane(count_up_to(b.offsets, b.segments + 1, (int)row));
-  if (c == 0 || c > b.segments) {
-    const int64_t end = c == 0 ? (int64_t)b.offsets[0] : limit;
-    return Run{-2, end > row && end < limit ? end : limit};
+  int c, k;
+  int64_t end;
+  if (b.segments < 64) {        // all in one load of the wave
+    const int lane = threadIdx.x & 63;
+    const int at = b.offsets[min(lane, b.segments)], own = b.index[min(lane, b.segments - 1)];
+    c = __popcll(__builtin_amdgcn_ballot_w64(lane <= b.segments && at <= row));
+    end = __builtin_amdgcn_readlane(at, c <= b.segments ? c : 0);
+    k = __builtin_amdgcn_readlane(own, c > 0 && c <= b.segments ? c - 1 : 0);
+  } else {
+    c = __builtin_amdgcn_readfirstlane(count_up_to(b.offsets, b.segments + 1, (int)row));
+    end = c <= b.segments ? b.offsets[c] : 0;
+    k = c > 0 && c <= b.segments ? b.index[c - 1] : -1;
   }
-  const int64_t end = b.offsets[c];
-  const int k = b.index[c - 1];
-  return Run{k >= 0 && k < b.adapters ? k : -1, end > row && end < limit ? end : (end > row ? limit : row + 1)};
+  if (c == 0 || c > b.segments) return Run{-2, c == 0 && end > row && end < limit ? end : limit};
+  return Run{k >= 0 && k < b.adapters ? k : -1, end > row ? (end < limit ? end : limit) : row + 1};
 }
 
 // ---- shrink ---------------------------------------------------------------------------------------
@@ -322,64 +363,67 @@ __global__ __launch_bounds__(256, RT <= 4 ? 2 : 1) void shrink_kernel(const Adap
   }
 }
 
+__device__ __forceinline__ int64_t ceil_of(int64_t a, int64_t b) { return (a + b - 1) / b; }
+
 // ---- expand ---------------------------------------------------------------------------------------
-// Four consecutive columns of a row.
-template <class T> struct Four;
-template <> struct Four<bf16> { typedef uint16_t V __attribute__((ext_vector_type(4), aligned(2))); V v; };
-template <> struct Four<float> { typedef f4_any V; V v; };
+// The consecutive columns of a row that a lane has: 16 bytes.
+template <class T> struct Cols;
+template <> struct Cols<bf16> { typedef h8_any V; V v; };
+template <> struct Cols<float> { typedef f4_any V; V v; };
 template <class T>
-__device__ __forceinline__ Four<T> load4(const T* p) { return Four<T>{*(const typename Four<T>::V*)p}; }
-__device__ __forceinline__ Four<bf16> sum4(const Four<bf16>& b, f4 x) {
-  Four<bf16> r;
+constexpr int kCols = 16 / sizeof(T);
+template <class T>
+__device__ __forceinline__ Cols<T> load_cols(const T* p) { return Cols<T>{*(const typename Cols<T>::V*)p}; }
+__device__ __forceinline__ Cols<bf16> sum_cols(const Cols<bf16>& b, const f4 (&x)[8], int e) {
+  Cols<bf16> r;
 #pragma unroll
-  for (int e = 0; e < 4; ++e) r.v[e] = float_to_bf16(bf16_to_float(b.v[e]) + x[e]);
+  for (int t = 0; t < 8; ++t) r.v[t] = float_to_bf16(bf16_to_float(b.v[t]) + x[t][e]);
   return r;
 }
-__device__ __forceinline__ Four<float> sum4(const Four<float>& b, f4 x) {
-  Four<float> r;
+__device__ __forceinline__ Cols<float> sum_cols(const Cols<float>& b, const f4 (&x)[4], int e) {
+  Cols<float> r;
 #pragma unroll
-  for (int e = 0; e < 4; ++e) r.v[e] = b.v[e] + x[e];
+  for (int t = 0; t < 4; ++t) r.v[t] = b.v[t] + x[t][e];
   return r;
 }
 
-// Whole tiles of 16 rows, first to last, and 64 columns from n on: the rows' factors as they were packed, DEPTH tiles on their way.  Rows are the
-// product's rows here: lane (i, q) ends with columns 4 i .. + 3 (tile t of the four has columns 4 m + t) of rows 4 q .. + 3, 16 lanes a row.
+// Whole tiles of 16 rows, first to last, and 16 lanes' columns from n on: the rows' factors as they were packed, DEPTH tiles on their way.  Rows are
+// the product's rows here: tile t of NT has columns NT m + t, so that lane (i, q) ends with columns NT i .. of rows 4 q .. + 3, 16 lanes a row.
 // Nothing here branches but the loop, so that a wait is for one tile and not for all.  (The streaming hint on y: 140 us for 130,
 // reading and writing 16384 x 11008 bfloat16.)
 template <class T, int PIECES, int CHUNKS, int PARTS, int DEPTH, bool BASE>
-__device__ __forceinline__ void expand_tiles(const AdapterExpand& a, int64_t first, int64_t last, int64_t n, const Frag<T> (&fw)[4][CHUNKS]) {
+__device__ __forceinline__ void expand_tiles(const AdapterExpand& a, int64_t first, int64_t last, int64_t n, const Frag<T> (&fw)[kCols<T>][CHUNKS]) {
+  constexpr int NT = kCols<T>;
   const int lane = threadIdx.x & 63, i = lane & 15, q = lane >> 4;
   struct Tile {
-    Four<T> base[4];
+    Cols<T> base[4];
     Piece<T> p[PIECES];
   };
-  const int64_t from = (first + q * 4) * a.N + n + i * 4;
+  const int64_t from = (first + q * 4) * a.N + n + i * NT;
   const T* const factors = (const T*)a.packed + (first >> 4) * PIECES * kTile + lane * (16 / (int)sizeof(T));
   const int count = (int)((last - first) / 16) + 1;
   const auto load = [&](int tile, Tile& d) {
     const int t = min(tile, count - 1);
     if constexpr (BASE) {
 #pragma unroll
-      for (int e = 0; e < 4; ++e) d.base[e] = load4((const T*)a.base + from + (t * 16 + e) * a.N);
+      for (int e = 0; e < 4; ++e) d.base[e] = load_cols((const T*)a.base + from + (t * 16 + e) * a.N);
     }
 #pragma unroll
     for (int c = 0; c < PIECES; ++c) d.p[c] = load_piece<256>(factors + ((int64_t)t * PIECES + c) * kTile);
   };
   const auto finish = [&](int tile, const Tile& d) {
-    f4 acc[4];
+    f4 acc[NT];
 #pragma unroll
-    for (int t = 0; t < 4; ++t) acc[t] = f4{0.0f, 0.0f, 0.0f, 0.0f};
+    for (int t = 0; t < NT; ++t) acc[t] = f4{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
     for (int c = 0; c < CHUNKS; ++c)
 #pragma unroll
       for (int part = 0; part < PARTS; ++part)
 #pragma unroll
-        for (int t = 0; t < 4; ++t) acc[t] = mma(frag(d.p[c * PARTS + part]), fw[t][c], acc[t]);
+        for (int t = 0; t < NT; ++t) acc[t] = mma(frag(d.p[c * PARTS + part]), fw[t][c], acc[t]);
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const f4 v = {acc[0][e], acc[1][e], acc[2][e], acc[3][e]};
-      *(typename Four<T>::V*)((T*)a.y + from + (tile * 16 + e) * a.N) = sum4(BASE ? d.base[e] : Four<T>{}, v).v;
-    }
+    for (int e = 0; e < 4; ++e)
+      *(typename Cols<T>::V*)((T*)a.y + from + (tile * 16 + e) * a.N) = sum_cols(BASE ? d.base[e] : Cols<T>{}, acc, e).v;
   };
   Tile d[DEPTH];
 #pragma unroll
@@ -400,16 +444,16 @@ __device__ __forceinline__ void expand_tiles(const AdapterExpand& a, int64_t fir
 }
 
 // RC chunks of 32 ranks (0: at most 16 ranks; in bfloat16 the chunk's second half is the second part of the same ranks).  A wave holds the
-// factors of 64 columns and goes over the rows; the four waves of a workgroup are side by side.
+// factors of 128 columns (fp32: 64) and goes over the rows; the four waves of a workgroup are side by side.
 template <class T, int RC, int DEPTH>
-__global__ __launch_bounds__(256) void expand_kernel(const AdapterExpand a, int col_groups, int64_t chunk) {
+__global__ __launch_bounds__(256, RC <= 2 ? 2 : 1) void expand_kernel(const AdapterExpand a, int col_groups, int64_t chunk) {
   constexpr bool kSingle = sizeof(T) == 4, kPack = RC == 0 && !kSingle;
-  constexpr int kChunks = RC == 0 ? 1 : RC, kParts = kSingle || kPack ? 1 : 2;
+  constexpr int kChunks = RC == 0 ? 1 : RC, kParts = kSingle || kPack ? 1 : 2, NT = kCols<T>;
   const int lane = threadIdx.x & 63, i = lane & 15, q = lane >> 4, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int group = (int)(blockIdx.x % col_groups);
-  const int64_t n = (int64_t)group * 256 + wave * 64;
+  const int64_t n = ((int64_t)group * 4 + wave) * (16 * NT);
   if (n >= a.N) return;
-  const bool whole = n + 64 <= a.N;
+  const bool whole = n + 16 * NT <= a.N;
   const int64_t row0 = (int64_t)(blockIdx.x / col_groups) * chunk, row1 = min(row0 + chunk, a.b.L);
   const bool writes_u = a.u && group == 0 && wave == 0;
 
@@ -422,14 +466,14 @@ __global__ __launch_bounds__(256) void expand_kernel(const AdapterExpand a, int 
     const bool none = run.adapter < 0;
     const float scale = none ? 0.0f : a.scale ? a.scale[run.adapter] : 1.0f;
     // Ranks of this lane: bfloat16 8 q .. + 7 of a chunk (of its half, where that is all), fp32 4 q .. + 3 and 16 + 4 q .. + 3.
-    Frag<T> fw[4][kChunks];
+    Frag<T> fw[NT][kChunks];
     if (!none) {
       const T* const w = (const T*)a.w + run.adapter * a.w_stride;
 #pragma unroll
-      for (int t = 0; t < 4; ++t) {
-        const T* const at = w + min(n + i * 4 + t, a.N - 1) * a.w_pitch;
+      for (int t = 0; t < NT; ++t) {
+        const T* const at = w + min(n + i * NT + t, a.N - 1) * a.w_pitch;
 #pragma unroll
-        for (int c = 0; c < kChunks; ++c) fw[t][c] = frag(load_piece_of(at + c * 32, kPack ? q & 1 : q, a.rank - c * 32));
+        for (int c = 0; c < kChunks; ++c) fw[t][c] = frag(load_piece_end(at + c * 32, kPack ? q & 1 : q, a.rank - c * 32, a.rank));
       }
     }
     const int64_t first = (row + 15) & -16ll, last = (run.end & -16ll) - 16;      // whole tiles
@@ -438,8 +482,8 @@ __global__ __launch_bounds__(256) void expand_kernel(const AdapterExpand a, int 
       if (a.base) expand_tiles<T, kChunks * kParts, kChunks, kParts, DEPTH, true>(a, first, last, n, fw);
       else expand_tiles<T, kChunks * kParts, kChunks, kParts, DEPTH, false>(a, first, last, n, fw);
     }
-    // The rows beside whole tiles; all of them where there are slices of the factors, no adapter, or not 64 columns.  Columns are the
-    // product's rows here: lane (i, q) ends with columns 16 q + 4 e + t of row i.
+    // The rows beside whole tiles; all of them where there are slices of the factors, no adapter, or fewer columns.  Columns are the
+    // product's rows here: lane (i, q) ends with columns NT (4 q + e) + t of row i.
     for (int64_t at = row; at < run.end; at += 16) {
       if (tiles && at >= first && at <= last) {
         at = last;
@@ -448,9 +492,9 @@ __global__ __launch_bounds__(256) void expand_kernel(const AdapterExpand a, int 
       const int64_t end = tiles && at < first ? first : run.end;
       const int64_t l = min(at + i, end - 1);
       const bool mine = at + i < end;
-      f4 acc[4];
+      f4 acc[NT];
 #pragma unroll
-      for (int t = 0; t < 4; ++t) acc[t] = f4{0.0f, 0.0f, 0.0f, 0.0f};
+      for (int t = 0; t < NT; ++t) acc[t] = f4{0.0f, 0.0f, 0.0f, 0.0f};
       if (!none) {
 #pragma unroll
         for (int c = 0; c < kChunks; ++c) {
@@ -486,28 +530,87 @@ __global__ __launch_bounds__(256) void expand_kernel(const AdapterExpand a, int 
 #pragma unroll
           for (int part = 0; part < kParts; ++part)
 #pragma unroll
-            for (int t = 0; t < 4; ++t) acc[t] = mma(fw[t][c], f[part], acc[t]);
+            for (int t = 0; t < NT; ++t) acc[t] = mma(fw[t][c], f[part], acc[t]);
         }
       } else if (writes_u && mine) {
         for (int j = q; j < a.rank; j += 4) a.u[l * a.rank + j] = 0.0f;
       }
-      const int64_t to = l * a.N + n + q * 16;
+      const int64_t to = l * a.N + n + q * (4 * NT);
       if (mine && whole) {
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          const f4 v = {acc[0][e], acc[1][e], acc[2][e], acc[3][e]};
-          const Four<T> base = a.base ? load4((const T*)a.base + to + e * 4) : Four<T>{};
-          *(typename Four<T>::V*)((T*)a.y + to + e * 4) = sum4(base, v).v;
+          const Cols<T> base = a.base ? load_cols((const T*)a.base + to + e * NT) : Cols<T>{};
+          *(typename Cols<T>::V*)((T*)a.y + to + e * NT) = sum_cols(base, acc, e).v;
         }
       } else if (mine) {
+#pragma unroll
         for (int e = 0; e < 4; ++e)
-          for (int t = 0; t < 4; ++t)
-            if (n + q * 16 + e * 4 + t < a.N)
-              ((T*)a.y)[to + e * 4 + t] = (T)(acc[t][e] + (a.base ? (float)((const T*)a.base)[to + e * 4 + t] : 0.0f));
+#pragma unroll
+          for (int t = 0; t < NT; ++t)
+            if (n + q * (4 * NT) + e * NT + t < a.N)
+              ((T*)a.y)[to + e * NT + t] = (T)(acc[t][e] + (a.base ? (float)((const T*)a.base)[to + e * NT + t] : 0.0f));
       }
       if (tiles && at < first) at = first - 16;
     }
     row = run.end;
+  }
+}
+
+// One row a workgroup and `span` columns of it: a row of weights is dealt to its rank / 8 lanes (a power of two, from 1 to 16), so that a wave
+// reads 1024 bytes in a row.  For rows that have an adapter each there is nothing that a matrix instruction could share.
+template <class T>
+__global__ __launch_bounds__(256) void expand_row_kernel(const AdapterExpand a, int cuts, int64_t span) {
+  __shared__ float s_p[kMaxRank];
+  const int tid = threadIdx.x, per = a.rank / 8;                // lanes of a column
+  const int64_t row = blockIdx.x / cuts, n0 = (int64_t)(blockIdx.x % cuts) * span, n1 = min(n0 + span, a.N);
+  const Run run = run_at(a.b, row, row + 1);
+  if (run.adapter == -2) return;
+  const int step = 256 / per, j0 = tid % per * 8;
+  if (run.adapter < 0) {
+    for (int64_t n = n0 + tid; n < n1; n += 256)
+      ((T*)a.y)[row * a.N + n] = a.base ? ((const T*)a.base)[row * a.N + n] : (T)0.0f;
+    if (a.u && n0 == 0 && tid < a.rank) a.u[row * a.rank + tid] = 0.0f;
+    return;
+  }
+  constexpr int kAhead = 4;
+  const T* const w = (const T*)a.w + run.adapter * a.w_stride + j0;
+  const int64_t first = n0 + tid / per;
+  Raw8<T> next[kAhead];
+#pragma unroll
+  for (int s = 0; s < kAhead; ++s) next[s] = load8(w + min(first + s * step, a.N - 1) * a.w_pitch, 8);
+  if (tid < a.rank) {
+    float v = 0.0f;
+#pragma unroll 8
+    for (int s = 0; s < a.slices; ++s) v += a.p[((int64_t)s * a.b.L + row) * a.pitch + tid];
+    if (a.u && n0 == 0) a.u[row * a.rank + tid] = v;
+    s_p[tid] = v * (a.scale ? a.scale[run.adapter] : 1.0f);
+  }
+  __syncthreads();
+  float p[8];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) p[e] = s_p[j0 + e];
+  for (int64_t n = first, left = ceil_of(n1 - n0, kAhead * step); left > 0; --left, n += kAhead * step) {
+    Raw8<T> now[kAhead];
+#pragma unroll
+    for (int s = 0; s < kAhead; ++s) now[s] = next[s];
+#pragma unroll
+    for (int s = 0; s < kAhead; ++s) next[s] = load8(w + min(n + (kAhead + s) * step, a.N - 1) * a.w_pitch, 8);
+#pragma unroll
+    for (int s = 0; s < kAhead; ++s) {
+      float x[8], sum = 0.0f;
+      widen(now[s], x);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) sum = fmaf(x[e], p[e], sum);
+      if (per >= 2) sum += lane_xor<1>(sum);
+      if (per >= 4) sum += lane_xor<2>(sum);
+      if (per >= 8) sum += lane_xor<4>(sum);
+      if (per >= 16) sum += lane_xor<8>(sum);
+      const int64_t c = n + s * step;
+      if (tid % per == 0 && c < n1) {
+        const int64_t at = row * a.N + c;
+        ((T*)a.y)[at] = (T)(sum + (a.base ? (float)((const T*)a.base)[at] : 0.0f));
+      }
+    }
   }
 }
 
@@ -914,7 +1017,7 @@ constexpr int64_t kExpandGroups = 1024;
 template <class T, int RC>
 hipError_t run_expand(const AdapterExpand& a, bool rows, hipStream_t s) {
   constexpr int kDepth = RC <= 2 ? 3 : 2;
-  const int64_t groups = ceil_div(a.N, 256);
+  const int64_t groups = ceil_div(a.N, 64 * kCols<T>);
   const int64_t chunk = rows ? 1 : round_up(ceil_div(a.b.L * groups, kExpandGroups), 16);
   const uint32_t grid = (uint32_t)(groups * ceil_div(a.b.L, chunk));
   expand_kernel<T, RC, kDepth><<<grid, 256, 0, s>>>(a, (int)groups, chunk);
@@ -922,6 +1025,16 @@ hipError_t run_expand(const AdapterExpand& a, bool rows, hipStream_t s) {
 }
 template <class T>
 hipError_t expand_of(const AdapterExpand& a, bool rows, hipStream_t s) {
+  const int per = a.rank / 8;
+  if (rows && a.rank % 8 == 0 && (per & (per - 1)) == 0) {
+    const int64_t step = 256 / per, steps = ceil_div(a.N, step);
+    int64_t cuts = ceil_div(kExpandGroups, a.b.L);
+    if (cuts > steps) cuts = steps;
+    const int64_t span = ceil_div(steps, cuts) * step;
+    cuts = ceil_div(a.N, span);
+    expand_row_kernel<T><<<(uint32_t)(a.b.L * cuts), 256, 0, s>>>(a, (int)cuts, span);
+    return hipGetLastError();
+  }
   if (a.rank <= 16) return run_expand<T, 0>(a, rows, s);
   if (a.rank <= 32) return run_expand<T, 1>(a, rows, s);
   if (a.rank <= 64) return run_expand<T, 2>(a, rows, s);

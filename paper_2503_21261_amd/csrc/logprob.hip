@@ -50,6 +50,25 @@ __device__ __forceinline__ uint32_t order_key(float z) {
 }
 __device__ __forceinline__ bool before(uint32_t ka, int ia, uint32_t kb, int ib) { return ka > kb || (ka == kb && ia < ib); }
 
+// The first of a wave's lanes' (key, token), in its first N lanes: permutes on the vector pipe for up to 16.
+template <int MASK>
+__device__ __forceinline__ void first_with(uint32_t& key, int& id) {
+  const uint32_t k = lane_xor<MASK>(key);
+  const int i = (int)lane_xor<MASK>((uint32_t)id);
+  if (before(k, i, key, id)) {
+    key = k;
+    id = i;
+  }
+}
+__device__ __forceinline__ void first_of_lanes(uint32_t& key, int& id, int n) {
+  first_with<1>(key, id);
+  first_with<2>(key, id);
+  first_with<4>(key, id);
+  first_with<8>(key, id);
+  if (n > 16) first_with<16>(key, id);
+  if (n > 32) first_with<32>(key, id);
+}
+
 // What leaves the sums of a whole row.
 struct RowResult {
   float m, log_s, entropy;
@@ -113,8 +132,9 @@ __device__ void part_top(const T* row, int64_t first, int64_t end, int top, floa
   if (wave == 0) {
     const float mine = s_group[lane];
     int rank = 0;
+#pragma unroll
     for (int i = 0; i < 64; ++i) {
-      const float other = s_group[i];
+      const float other = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(mine), i));
       rank += other > mine || (other == mine && i < lane);
     }
     if (rank == top - 1) s_border = mine;
@@ -173,15 +193,7 @@ __device__ void part_top(const T* row, int64_t first, int64_t end, int top, floa
         }
       }
     }
-#pragma unroll
-    for (int mask = 1; mask < 64; mask *= 2) {
-      const uint32_t k2 = (uint32_t)__shfl_xor((int)key, mask);
-      const int i2 = __shfl_xor(id, mask);
-      if (before(k2, i2, key, id)) {
-        key = k2;
-        id = i2;
-      }
-    }
+    first_of_lanes(key, id, 64);
     __syncthreads();
     if (lane == 0) {
       s_key[wave] = key;
@@ -332,16 +344,8 @@ __global__ __launch_bounds__(64) void logprob_join_kernel(const LogProbArgs a) {
     const float z = there ? s_z[at] : -INFINITY;
     uint32_t key = mine == 0x7FFFFFFF ? 0u : order_key(z);
     int id = mine;
-#pragma unroll
-    for (int mask = 1; mask < 64; mask *= 2) {
-      const uint32_t k2 = (uint32_t)__shfl_xor((int)key, mask);
-      const int i2 = __shfl_xor(id, mask);
-      if (before(k2, i2, key, id)) {
-        key = k2;
-        id = i2;
-      }
-    }
-    if (mine == id) {       // one lane: tokens differ, and there are `top` of them at least
+    first_of_lanes(key, id, a.parts);
+    if (mine == id && there) {       // one lane: tokens differ, and there are `top` of them at least
       a.top_logp[r * a.top + k] = log_prob(z, f);
       a.top_ids[r * a.top + k] = id;
       ++head;
