@@ -837,19 +837,22 @@ __global__ __launch_bounds__(256) void pack_kernel(const AdapterPack a) {
 
 constexpr int kOuterCols = 128, kOuterWaves = 4;    // columns of a wave, waves of a workgroup side by side
 
-// A wave: 128 columns, up to 64 ranks, one part of the rows that have adapters, in steps of 32, the next step's loads on their way.
-// The waves of a workgroup share the rows' factors in the first cache.  Sums over rows leave as one partial sum a part and adapter.
+// A wave: 128 columns, up to 64 ranks, one part of the rows that have adapters, in steps of 32, DEPTH of them on their way.  The four waves
+// of a workgroup are side by side and share the rows' factors through LDS: each loads a quarter, with its rows, so that both are as far
+// ahead (a wait for factors loaded later than rows is one for the rows).  Sums over rows leave as one partial sum a part and adapter.
 // MODE: 0 all rows as they lie, 1 in the order of a.rows, 2 too, with fewer than eight columns in one of the products.
-template <class T, int RT, int MODE>
+template <class T, int RT, int MODE, int DEPTH>
 __global__ __launch_bounds__(64 * kOuterWaves) void outer_kernel(const AdapterOuter a, int tiles_first, int tiles, int rank_blocks) {
-  constexpr int kParts = sizeof(T) == 4 ? 1 : 3;
+  constexpr int kParts = sizeof(T) == 4 ? 1 : 3, kHeld = 16;       // steps whose rows' numbers are held
+  constexpr int kFactors = kParts * RT, kOwn = (kFactors + kOuterWaves - 1) / kOuterWaves;   // packed tiles of a step, of a wave
+  __shared__ int s_rows[kOuterWaves][MODE ? kHeld * 32 : 1];
+  __shared__ Piece<T> s_p[2][kFactors][64];
   const int lane = threadIdx.x & 63, i = lane & 15, q = lane >> 4, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int part = blockIdx.x / (tiles * rank_blocks), in = blockIdx.x % (tiles * rank_blocks);
   const int tile = in % tiles, rank0 = in / tiles * 64, ranks = (a.rank + 15) & -16;
   const bool second = tile >= tiles_first;
   const AdapterOuterOperand o = second ? a.a[1] : a.a[0];
   const int64_t col0 = ((int64_t)(second ? tile - tiles_first : tile) * kOuterWaves + wave) * kOuterCols;
-  if (col0 >= o.N) return;
   // Columns past the last one: the last eight once more, which come out the same.
   const bool narrow = MODE == 2 && o.N < 8;
   const int64_t col = narrow ? col0 + i * 8 : min(col0 + i * 8, o.N - 8);
@@ -872,68 +875,74 @@ __global__ __launch_bounds__(64 * kOuterWaves) void outer_kernel(const AdapterOu
     for (int t = 0; t < RT; ++t)
 #pragma unroll
       for (int c = 0; c < 8; ++c) acc[t][c] = f4{0.0f, 0.0f, 0.0f, 0.0f};
-    Piece<T> p[RT][kParts];
     const T* const p_at = (const T*)o.p + rank0 * 32 + lane * (16 / (int)sizeof(T));
     const int64_t begin = pos & -32ll, last = (k_end - 1) & -32ll;          // the first and the last step
-    const auto rows_at = [&](int64_t at, int (&r)[8]) {          // beside the rows: the nearest one, times zero
+    const int steps = (int)((last - begin) / 32) + 1;
+    struct Step {
+      Raw8<T> x[8];
+      Piece<T> p[kOwn];
+    };
+    const auto load = [&](int step, Step& d) {
+      const int64_t at = begin + min(step, steps - 1) * 32;
+      if (MODE && step < steps && step % kHeld == 0) {          // the rows' numbers, for many steps at once: a wait for them is one for all
+        const int64_t l = at + lane * 8;
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const int64_t l = max(min(at + row_in_step<T>(q, e), k_end - 1), pos);
-        r[e] = MODE ? a.rows[l] : (int)l;
+        for (int e = 0; e < 8; ++e) s_rows[wave][lane * 8 + e] = a.rows[max(min(l + e, k_end - 1), pos)];
+        __builtin_amdgcn_wave_barrier();
+      }
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {     // beside the adapter's rows: its nearest one, times zero
+        const int64_t r = MODE ? s_rows[wave][min(step, steps - 1) % kHeld * 32 + row_in_step<T>(q, e)] : max(min(at + row_in_step<T>(q, e), k_end - 1), pos);
+        const T* const from = (const T*)o.q + r * o.N + col;
+        if (narrow) d.x[e] = load8(from, have);
+        else d.x[e] = load8(from, 8);
+      }
+#pragma unroll
+      for (int k = 0; k < kOwn; ++k) {  // ranks past the last tile: the last tile's, whose sums are not stored
+        const int tile = min(wave + k * kOuterWaves, kFactors - 1), t = min(tile % RT, (ranks - rank0) / 16 - 1);
+        d.p[k] = load_piece<256>(p_at + at * kParts * ranks + (tile / RT * (ranks / 16) + t) * kTile);
       }
     };
-    const auto load = [&](const int (&r)[8], Raw8<T> (&x)[8]) {
+    const auto multiply = [&](int step, Step& d) {
+      const int64_t at = begin + step * 32;
+      const int n = (int)min(k_end - at, (int64_t)32), m = (int)max(pos - at, (int64_t)0);
+      Piece<T>(&slot)[kFactors][64] = s_p[step & 1];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const T* const from = (const T*)o.q + (int64_t)r[e] * o.N + col;
-        if (narrow) x[e] = load8(from, have);
-        else x[e] = load8(from, 8);
+      for (int k = 0; k < kOwn; ++k) {
+        keep_rows(d.p[k], q, m, n);
+        slot[min(wave + k * kOuterWaves, kFactors - 1)][lane] = d.p[k];
       }
-    };
-    const auto load_p = [&](int t, int64_t at) {     // ranks past the last tile: the last tile's, whose sums are not stored
-      const int64_t tile = min(t, (ranks - rank0) / 16 - 1);
-#pragma unroll
-      for (int s = 0; s < kParts; ++s) p[t][s] = load_piece<256>(p_at + at * kParts * ranks + (s * (ranks / 16) + tile) * kTile);
-    };
-    const auto multiply = [&](int64_t at, const Raw8<T> (&x)[8]) {
-      if (at == last || at < pos) {                              // zeros beside the rows
-        const int n = (int)min(k_end - at, (int64_t)32), m = (int)max(pos - at, (int64_t)0);
-#pragma unroll
-        for (int t = 0; t < RT; ++t)
-#pragma unroll
-          for (int s = 0; s < kParts; ++s) keep_rows(p[t][s], q, m, n);
-      }
+      // The waves are done with this slot's last content: they have passed the barrier of the step between.
+      asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
       Frag<T> f[8];
-      columns_of(x, f);
+      columns_of(d.x, f);
 #pragma unroll
-      for (int t = 0; t < RT; ++t) {
+      for (int t = 0; t < RT; ++t)
 #pragma unroll
-        for (int s = 0; s < kParts; ++s)
+        for (int s = 0; s < kParts; ++s) {
+          const Frag<T> p = frag(slot[s * RT + t][lane]);
 #pragma unroll
-          for (int c = 0; c < 8; ++c) acc[t][c] = mma(frag(p[t][s]), f[c], acc[t][c]);
-        __builtin_amdgcn_sched_barrier(0);                       // the next step's factors into the registers that are free now
-        load_p(t, min(at + 32, last));
-      }
+          for (int c = 0; c < 8; ++c) acc[t][c] = mma(p, f[c], acc[t][c]);
+        }
     };
-    Raw8<T> x0[8], x1[8];
-    int r0[8], r1[8];
-    rows_at(begin, r0);
-    rows_at(min(begin + 32, last), r1);
-    load(r0, x0);
+    // DEPTH steps on their way, as in the first product; every wave takes every step, for the barriers.
+    Step d[DEPTH];
 #pragma unroll
-    for (int t = 0; t < RT; ++t) load_p(t, begin);
-    int64_t at = begin;
-    for (; at + 32 <= last; at += 64) {
-      load(r1, x1);
-      rows_at(min(at + 64, last), r0);
-      __builtin_amdgcn_sched_barrier(0);
-      multiply(at, x0);
-      load(r0, x0);
-      rows_at(min(at + 96, last), r1);
-      __builtin_amdgcn_sched_barrier(0);
-      multiply(at + 32, x1);
+    for (int s = 0; s < DEPTH - 1; ++s) load(s, d[s]);
+    int at = 0;
+    for (; at + DEPTH <= steps; at += DEPTH) {
+#pragma unroll
+      for (int s = 0; s < DEPTH; ++s) {
+        load(at + s + DEPTH - 1, d[(s + DEPTH - 1) % DEPTH]);
+        __builtin_amdgcn_sched_barrier(0);
+        multiply(at + s, d[s]);
+        __builtin_amdgcn_sched_barrier(0);
+      }
     }
-    if (at <= last) multiply(at, x0);
+#pragma unroll
+    for (int s = 0; s < DEPTH - 1; ++s)
+      if (at + s < steps) multiply(at + s, d[s]);
+    __syncthreads();          // the next adapter begins with the first slot again
     pos = k_end;
     // Lane (i, q) has ranks 16 t + 4 q + e of its eight columns.
     const float scale = o.scaled && a.scale ? a.scale[k] : 1.0f;
@@ -1018,7 +1027,7 @@ template <class T, int RC>
 hipError_t run_expand(const AdapterExpand& a, bool rows, hipStream_t s) {
   constexpr int kDepth = RC <= 2 ? 3 : 2;
   const int64_t groups = ceil_div(a.N, 64 * kCols<T>);
-  const int64_t chunk = rows ? 1 : round_up(ceil_div(a.b.L * groups, kExpandGroups), 16);
+  const int64_t chunk = rows ? 1 : round_up(ceil_div(a.b.L, groups < kExpandGroups ? kExpandGroups / groups : 1), 16);
   const uint32_t grid = (uint32_t)(groups * ceil_div(a.b.L, chunk));
   expand_kernel<T, RC, kDepth><<<grid, 256, 0, s>>>(a, (int)groups, chunk);
   return hipGetLastError();
@@ -1048,9 +1057,10 @@ hipError_t outer_of(const AdapterOuter& a, hipStream_t s) {
   const int blocks = (int)ceil_div(a.rank, 64);
   const uint32_t grid = (uint32_t)((int64_t)tiles * blocks * a.parts);
   const auto run = [&](auto kernel) { kernel<<<grid, 64 * kOuterWaves, 0, s>>>(a, tiles_first, tiles, blocks); };
-  if (a.a[0].N < 8 || a.a[1].N < 8) run(outer_kernel<T, 4, 2>);
-  else if (a.first) a.rank <= 16 ? run(outer_kernel<T, 1, 1>) : a.rank <= 32 ? run(outer_kernel<T, 2, 1>) : run(outer_kernel<T, 4, 1>);
-  else a.rank <= 16 ? run(outer_kernel<T, 1, 0>) : a.rank <= 32 ? run(outer_kernel<T, 2, 0>) : run(outer_kernel<T, 4, 0>);
+  constexpr int kMost = sizeof(T) == 4 ? 2 : 4;      // steps on their way that the registers hold with 64 ranks
+  if (a.a[0].N < 8 || a.a[1].N < 8) run(outer_kernel<T, 4, 2, 2>);
+  else if (a.first) a.rank <= 16 ? run(outer_kernel<T, 1, 1, 3>) : a.rank <= 32 ? run(outer_kernel<T, 2, 1, 3>) : run(outer_kernel<T, 4, 1, kMost>);
+  else a.rank <= 16 ? run(outer_kernel<T, 1, 0, 3>) : a.rank <= 32 ? run(outer_kernel<T, 2, 0, 3>) : run(outer_kernel<T, 4, 0, kMost>);
   return hipGetLastError();
 }
 
@@ -1076,8 +1086,8 @@ AdapterPlan adapter_plan(hot_type type, int64_t L, int64_t O, int64_t I, int64_t
   slices(O, p.slices_backward, p.slice_backward);
   // Parts of the sums over rows: workgroups for all compute units (one each with the registers of 64 ranks, two below).
   const int64_t tiles = (ceil_div(I, kOuterCols * kOuterWaves) + ceil_div(O, kOuterCols * kOuterWaves)) * ceil_div(rank, 64);
-  const int64_t wanted = ceil_div(rank > 32 ? 256 : 512, tiles), most = ceil_div(L, 64);
-  p.parts = (int)(wanted < most ? wanted : most);
+  const int64_t wanted = 256 / tiles, most = ceil_div(L, 64);
+  p.parts = (int)(wanted < 1 ? 1 : wanted < most ? wanted : most);
   p.positions = round_up(L, 64);
 
   // Packed weights of the forward call: 2 to 4 us for a launch, against 48 cycles of a compute unit's memory pipe for each kilobyte of
