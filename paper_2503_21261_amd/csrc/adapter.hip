@@ -175,6 +175,19 @@ __device__ __forceinline__ void store_factors(bf16* p, int64_t l, int j, int chu
   }
 }
 
+// A row's 128 bytes of a step as fragments, from a lane's pieces of the first and the second half.
+__device__ __forceinline__ void frags_of(u4 lo, u4 hi, Frag<bf16> (&f)[2]) {
+  f[0].v = lo;
+  f[1].v = hi;
+}
+__device__ __forceinline__ void frags_of(u4 lo, u4 hi, Frag<float> (&f)[1]) {
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    f[0].v[e] = __uint_as_float(lo[e]);
+    f[0].v[4 + e] = __uint_as_float(hi[e]);
+  }
+}
+
 // How many of the n ascending numbers at t are at most x, by the wave together: each trip narrows the range to a 64th.
 __device__ __forceinline__ int count_up_to(const int32_t* t, int n, int x) {
   const int lane = threadIdx.x & 63;
@@ -214,18 +227,30 @@ __device__ __forceinline__ Run run_at(const AdapterBatch& b, int64_t row, int64_
   return Run{k >= 0 && k < b.adapters ? k : -1, end > row ? (end < limit ? end : limit) : row + 1};
 }
 
+// The consecutive columns of a row that a lane has: 16 bytes.
+template <class T> struct Cols;
+template <> struct Cols<bf16> { typedef h8_any V; V v; };
+template <> struct Cols<float> { typedef f4_any V; V v; };
+template <class T>
+constexpr int kCols = 16 / sizeof(T);
+template <class T>
+__device__ __forceinline__ Cols<T> load_cols(const T* p) { return Cols<T>{*(const typename Cols<T>::V*)p}; }
+
 // ---- shrink ---------------------------------------------------------------------------------------
 // The memory pipe takes the 64 bytes of four neighbouring lanes at a time, where they lie together; lanes of a matrix instruction's operand are
-// rows, so that a load of 16 rows takes four times as long as one of 1024 bytes in a row.  Rows that are read once can bear that (half the
-// pipe's time at 5 TB/s), what is read again cannot: weights are packed in the order of the lanes first, where that pays or they have to
-// be transposed anyway, and the sums are left in that order for the expansion.
+// rows, so that a load of 16 rows takes four times as long as one of 1024 bytes in a row.  So rows are loaded eight lanes a row and change
+// lanes through LDS (16384 x 11008 bfloat16, rank 64: 113 us without, which MEASURED); weights are packed in the order of the lanes first, where
+// that pays or they have to be transposed anyway; and the sums are left in that order for the expansion.
 //
 // RT tiles of 16 ranks, R tiles of 16 rows; ROWS: rows that a workgroup takes (1, or 16 R).  A step is 128 bytes of each row; the four waves
 // take steps in turn, DEPTH of them on their way, and join their sums through LDS.
 template <class T, int RT, int R, int ROWS, int DEPTH, bool PACKED>
-__global__ __launch_bounds__(256, RT <= 4 ? 2 : 1) void shrink_kernel(const AdapterShrink a) {
+__global__ __launch_bounds__(256, RT <= 4 && R <= 2 ? 2 : 1) void shrink_kernel(const AdapterShrink a) {
   constexpr int kStep = 128 / sizeof(T), kFrags = kStep / 32, kPer = 16 / sizeof(T);
+  constexpr bool kTurned = ROWS > 1;         // rows through LDS
+  constexpr int kLoads = kTurned ? 2 * R : 0;
   __shared__ f4 s_acc[3][RT * R][64];
+  __shared__ u4 s_x[4][kTurned ? R * 16 : 1][8];
   const int lane = threadIdx.x & 63, i = lane & 15, q = lane >> 4, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int64_t tiles = (a.b.L + ROWS - 1) / ROWS;
   const int slice = (int)(blockIdx.x / tiles);
@@ -240,10 +265,17 @@ __global__ __launch_bounds__(256, RT <= 4 ? 2 : 1) void shrink_kernel(const Adap
     const Run run = run_at(a.b, row, row1);
     if (run.adapter >= 0) {
       const T* const w = (const T*)a.w + run.adapter * a.w_stride;
-      const T* x[R];
+      const auto row_at = [&](int r) { return (const T*)a.q + min(max(row0 + r, row), run.end - 1) * a.K; };
+      const T* x[kTurned ? kLoads : 1];
       const T* wr[RT];
+      // Row 8 g + lane / 8, of its eight pieces of 16 bytes the one that lies in place lane % 8: they are dealt so that reads of 16 rows meet
+      // all banks.
+      if constexpr (kTurned) {
 #pragma unroll
-      for (int r = 0; r < R; ++r) x[r] = (const T*)a.q + min(max(row0 + r * 16 + i, row), run.end - 1) * a.K;
+        for (int g = 0; g < kLoads; ++g) x[g] = row_at(g * 8 + lane / 8) + ((lane & 7) ^ (lane / 8)) * kPer;
+      } else {
+        x[0] = row_at(0) + q * kPer;
+      }
 #pragma unroll
       for (int t = 0; t < RT; ++t)      // ranks past the last: the last one's, whose sums are not kept
         wr[t] = PACKED ? w + min(t, rank_tiles - 1) * kTile + lane * kPer : w + min(t * 16 + i, a.rank - 1) * a.K;
@@ -253,13 +285,19 @@ __global__ __launch_bounds__(256, RT <= 4 ? 2 : 1) void shrink_kernel(const Adap
 #pragma unroll
         for (int r = 0; r < R; ++r) acc[t][r] = f4{0.0f, 0.0f, 0.0f, 0.0f};
       struct Step {
-        Piece<T> x[R][kFrags], w[RT][kFrags];
+        Cols<T> rows[kTurned ? kLoads : 1];
+        Piece<T> x[kTurned ? 1 : kFrags], w[RT][kFrags];
       };
       const auto load = [&](int64_t at, Step& d) {
+        if constexpr (kTurned) {
+#pragma unroll
+          for (int g = 0; g < kLoads; ++g) d.rows[g] = load_cols(x[g] + at);
+        } else {
+#pragma unroll
+          for (int f = 0; f < kFrags; ++f) d.x[f] = load_piece<16>(x[0] + at + f * 32);
+        }
 #pragma unroll
         for (int f = 0; f < kFrags; ++f) {
-#pragma unroll
-          for (int r = 0; r < R; ++r) d.x[r][f] = load_piece<16>(x[r] + at + f * 32 + q * kPer);
 #pragma unroll
           for (int t = 0; t < RT; ++t) {
             if constexpr (PACKED) d.w[t][f] = load_piece<256>(wr[t] + (at / 32 + f) * rank_tiles * kTile);
@@ -268,12 +306,28 @@ __global__ __launch_bounds__(256, RT <= 4 ? 2 : 1) void shrink_kernel(const Adap
         }
       };
       const auto multiply = [&](const Step& d) {
+        Frag<T> fx[R][kFrags];
+        if constexpr (kTurned) {      // in order within the wave: no barrier
+          u4(&place)[R * 16][8] = s_x[wave];
+#pragma unroll
+          for (int g = 0; g < kLoads; ++g) place[g * 8 + lane / 8][lane & 7] = __builtin_bit_cast(u4, d.rows[g].v);
+          __builtin_amdgcn_wave_barrier();
+#pragma unroll
+          for (int r = 0; r < R; ++r) {
+            const u4 lo = place[r * 16 + i][q ^ (i & 7)], hi = place[r * 16 + i][(4 + q) ^ (i & 7)];
+            frags_of(lo, hi, fx[r]);
+          }
+          __builtin_amdgcn_wave_barrier();
+        } else {
+#pragma unroll
+          for (int f = 0; f < kFrags; ++f) fx[0][f] = frag(d.x[f]);
+        }
 #pragma unroll
         for (int f = 0; f < kFrags; ++f)
 #pragma unroll
           for (int r = 0; r < R; ++r)
 #pragma unroll
-            for (int t = 0; t < RT; ++t) acc[t][r] = mma(frag(d.w[t][f]), frag(d.x[r][f]), acc[t][r]);
+            for (int t = 0; t < RT; ++t) acc[t][r] = mma(frag(d.w[t][f]), fx[r][f], acc[t][r]);
       };
       if (first < whole) {
         // Each workgroup begins its walk elsewhere: side by side they would all ask for the same columns of the weights.
@@ -308,7 +362,7 @@ __global__ __launch_bounds__(256, RT <= 4 ? 2 : 1) void shrink_kernel(const Adap
           const int left = (int)min(k1 - at, (int64_t)32);
 #pragma unroll
           for (int r = 0; r < R; ++r) {
-            const Frag<T> fx = frag(load_piece_of(x[r] + at, q, left));
+            const Frag<T> fx = frag(load_piece_of(row_at(r * 16 + i) + at, q, left));
 #pragma unroll
             for (int t = 0; t < RT; ++t) {
               if constexpr (PACKED) acc[t][r] = mma(frag(load_piece<256>(wr[t] + at / 32 * rank_tiles * kTile)), fx, acc[t][r]);
@@ -366,14 +420,6 @@ __global__ __launch_bounds__(256, RT <= 4 ? 2 : 1) void shrink_kernel(const Adap
 __device__ __forceinline__ int64_t ceil_of(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
 // ---- expand ---------------------------------------------------------------------------------------
-// The consecutive columns of a row that a lane has: 16 bytes.
-template <class T> struct Cols;
-template <> struct Cols<bf16> { typedef h8_any V; V v; };
-template <> struct Cols<float> { typedef f4_any V; V v; };
-template <class T>
-constexpr int kCols = 16 / sizeof(T);
-template <class T>
-__device__ __forceinline__ Cols<T> load_cols(const T* p) { return Cols<T>{*(const typename Cols<T>::V*)p}; }
 __device__ __forceinline__ Cols<bf16> sum_cols(const Cols<bf16>& b, const f4 (&x)[8], int e) {
   Cols<bf16> r;
 #pragma unroll
@@ -1009,7 +1055,8 @@ hipError_t run_shrink(const AdapterShrink& a, int tile, hipStream_t s) {
   const auto run = [&](auto kernel) { kernel<<<grid, 256, 0, s>>>(a); };
   if (tile == 1) a.w_packed ? run(shrink_kernel<T, RT, 1, 1, kDepth, true>) : run(shrink_kernel<T, RT, 1, 1, kDepth, false>);
   else if (tile == 16 || RT == 8) a.w_packed ? run(shrink_kernel<T, RT, 1, 16, kDepth, true>) : run(shrink_kernel<T, RT, 1, 16, kDepth, false>);
-  else a.w_packed ? run(shrink_kernel<T, RT, 2, 32, kDepth, true>) : run(shrink_kernel<T, RT, 2, 32, kDepth, false>);
+  else if (tile == 32 || RT == 1) a.w_packed ? run(shrink_kernel<T, RT, 2, 32, kDepth, true>) : run(shrink_kernel<T, RT, 2, 32, kDepth, false>);
+  else if constexpr (RT == 2 || RT == 4) run(shrink_kernel<T, RT, 4, 64, 3, true>);
   return hipGetLastError();
 }
 template <class T>
@@ -1072,9 +1119,9 @@ AdapterPlan adapter_plan(hot_type type, int64_t L, int64_t O, int64_t I, int64_t
   p.rows = L <= 4 * (segments > 0 ? segments : 1) && L <= 1 << 20;
   p.pitch = (int)round_up(rank, 8);      // zeros behind the ranks
   // Rows of a workgroup: as many as leave workgroups for all compute units without slices, 16 at least.
-  p.tile = p.rows ? 1 : L >= 64 * 32 && rank <= 64 ? 32 : 16;
+  p.tile = p.rows ? 1 : L >= 64 * 224 && rank > 16 && rank <= 64 ? 64 : L >= 64 * 32 && rank <= 64 ? 32 : 16;
   const auto slices = [&](int64_t K, int& count, int64_t& slice) {
-    int64_t n = 512 / ceil_div(L, p.tile);
+    int64_t n = (p.tile == 64 ? 256 : 512) / ceil_div(L, p.tile);      // workgroups that are resident
     const int64_t most = ceil_div(K, 4 * step);      // a step for each wave
     if (n > most) n = most;
     if (n > kMaxSlices) n = kMaxSlices;
@@ -1092,7 +1139,7 @@ AdapterPlan adapter_plan(hot_type type, int64_t L, int64_t O, int64_t I, int64_t
 
   // Packed weights of the forward call: 2 to 4 us for a launch, against 48 cycles of a compute unit's memory pipe for each kilobyte of
   // weights and 32 rows (16384 x 4096, rank 64: 53 us without).
-  p.pack_forward = !p.rows && ceil_div(L, 32) * (rank * I * size / 1024) > 60000;
+  p.pack_forward = p.tile == 64 || (!p.rows && ceil_div(L, 32) * (rank * I * size / 1024) > 60000);
   p.chunks = rank <= 16 && type == HOT_BF16 ? 0 : rank <= 32 ? 1 : rank <= 64 ? 2 : 4;    // as the expansion's kernels have them
   p.wt_stride = round_up(rank, 16) * round_up(I > O ? I : O, 64);
   const int64_t row_bytes = L * p.pitch * 4;

@@ -83,6 +83,26 @@ def test_adapter_lengths(L, O, I, rank, dtype):
     check_pass(t, kind, run_pass(t))
 
 
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("L,O,I,rank,batch", [(2100, 264, 200, 16, None), (2500, 77, 133, 30, None), (4096, 40, 2080, 64, None), (14400, 136, 200, 40, None),
+                                              (14500, 72, 100, 20, ([0, 33, 5000, 5001, 14499], [1, 0, 1, 0], 2)), (3000, 520, 96, 100, None)])
+def test_adapter_many_rows(L, O, I, rank, batch, dtype):
+    """Larger tiles of rows, packed weights, rounds of steps on their way."""
+    t, kind = make(L, O, I, rank, batch or (None, None, 1), dtype, seed=25)
+    check_pass(t, kind, run_pass(t))
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
+def test_adapter_rows_of_their_own(dtype):
+    """A token a request at every rank that has a kernel of its own, and at some that have not; more segments than one load of a wave."""
+    for L, rank, O, I in ((5, 8, 1030, 300), (100, 16, 333, 500), (64, 32, 200, 96), (3, 64, 4100, 4100), (200, 128, 65, 130), (30, 24, 100, 77), (30, 7, 90, 64)):
+        batch = (list(range(L + 1)), [(i * 3) % 5 - (i % 7 == 0) for i in range(L)], 4)
+        t, kind = make(L, O, I, rank, batch, dtype, seed=27)
+        check_pass(t, kind, run_pass(t))
+        plain = {k: v for k, v in t.items() if k not in ("scale", "base", "g_base")}
+        check_pass(plain, kind, run_pass(plain))
+
+
 def test_adapter_many_segments():
     """More segments than the widest step of their search, of lengths from zero on, adapters in no order."""
     rng = np.random.default_rng(5)
