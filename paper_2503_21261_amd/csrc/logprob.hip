@@ -42,31 +42,62 @@ __device__ __forceinline__ float lane_max64(float v) {
   return fmaxf(v, lane_xor<32>(v));
 }
 
-// Values in the order of the likeliest tokens: a NaN first, then by value (-0 is 0).  Among equals the lower token comes first.
-__device__ __forceinline__ uint32_t order_key(float z) {
+// Values in the order of the likeliest tokens, the first the largest number: a NaN first, then by value (-0 is 0), among equals the lower token.
+__device__ __forceinline__ uint64_t order_of(float z, int token) {
   const uint32_t b = __float_as_uint(z + 0.0f);
-  if (z != z) return 0xFFFFFFFFu;
-  return b & 0x80000000u ? ~b : b | 0x80000000u;
+  const uint32_t key = z != z ? 0xFFFFFFFFu : b & 0x80000000u ? ~b : b | 0x80000000u;
+  return (uint64_t)key << 32 | (uint32_t)~token;
 }
-__device__ __forceinline__ bool before(uint32_t ka, int ia, uint32_t kb, int ib) { return ka > kb || (ka == kb && ia < ib); }
+__device__ __forceinline__ float value_of(uint64_t order) {
+  const uint32_t key = (uint32_t)(order >> 32);
+  return key == 0xFFFFFFFFu ? __uint_as_float(0x7FC00000u) : __uint_as_float(key & 0x80000000u ? key & 0x7FFFFFFFu : ~key);
+}
+__device__ __forceinline__ int token_of(uint64_t order) { return (int)~(uint32_t)order; }
 
-// The first of a wave's lanes' (key, token), in its first N lanes: permutes on the vector pipe for up to 16.
-template <int MASK>
-__device__ __forceinline__ void first_with(uint32_t& key, int& id) {
-  const uint32_t k = lane_xor<MASK>(key);
-  const int i = (int)lane_xor<MASK>((uint32_t)id);
-  if (before(k, i, key, id)) {
-    key = k;
-    id = i;
-  }
+// A wave's values sorted, the largest in lane 0 (bitonic: 21 exchanges of neighbours at powers of two).
+template <int RUN, int MASK>
+__device__ __forceinline__ void sort_step(float& v) {
+  const int lane = threadIdx.x & 63;
+  const float o = lane_xor<MASK>(v);
+  v = ((lane & MASK) == 0) == ((lane & RUN) == 0) ? fmaxf(v, o) : fminf(v, o);
+  if constexpr (MASK > 1) sort_step<RUN, MASK / 2>(v);
 }
-__device__ __forceinline__ void first_of_lanes(uint32_t& key, int& id, int n) {
-  first_with<1>(key, id);
-  first_with<2>(key, id);
-  first_with<4>(key, id);
-  first_with<8>(key, id);
-  if (n > 16) first_with<16>(key, id);
-  if (n > 32) first_with<32>(key, id);
+__device__ __forceinline__ void sort_wave(float& v) {
+  sort_step<2, 1>(v);
+  sort_step<4, 2>(v);
+  sort_step<8, 4>(v);
+  sort_step<16, 8>(v);
+  sort_step<32, 16>(v);
+  sort_step<64, 32>(v);
+}
+
+// How many of the n orders at t come before `mine` (t is held to a multiple of eight, zeros behind the n, which come last).
+__device__ __forceinline__ int rank_among(const uint64_t* t, int n, uint64_t mine) {
+  int rank = 0;
+#pragma unroll 1
+  for (int i = 0; i < n; i += 8) {
+    uint64_t x[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) x[e] = t[i + e];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) rank += x[e] > mine;
+  }
+  return rank;
+}
+template <int MASK>
+__device__ __forceinline__ uint64_t max_with(uint64_t v) {
+  const uint64_t o = (uint64_t)lane_xor<MASK>((uint32_t)(v >> 32)) << 32 | lane_xor<MASK>((uint32_t)v);
+  return o > v ? o : v;
+}
+// The largest of the first n lanes' (their number rounded up to a power of two, 16 at least), in all of them.
+__device__ __forceinline__ uint64_t max_of_lanes(uint64_t v, int n) {
+  v = max_with<1>(v);
+  v = max_with<2>(v);
+  v = max_with<4>(v);
+  v = max_with<8>(v);
+  if (n > 16) v = max_with<16>(v);
+  if (n > 32) v = max_with<32>(v);
+  return v;
 }
 
 // What leaves the sums of a whole row.
@@ -96,8 +127,7 @@ struct LogProbArgs {
   float *logp, *entropy, *stats, *top_logp;
   int32_t* top_ids;
   float* part_sums;        // [rows][parts][4]
-  float* part_top;         // [rows][parts][top] values, then tokens
-  int32_t* part_ids;
+  uint64_t* part_top;      // [rows][parts][top] orders
   int64_t vocab, first_row;
   int part, parts, top;    // elements of a part (a multiple of kSpan), parts of a row
 };
@@ -113,114 +143,88 @@ __device__ __forceinline__ void load_logits(const T* row, int64_t at, int64_t en
   }
 }
 
-// The first `top` of a part in order: values and tokens to out_z, out_id (LDS).  tmax: the lane's largest value but for NaNs;
+// The first `top` of a part in order, to out (LDS); zeros where a short part holds fewer.  v: the lane's values, those of 4 spans from `first` on (a part has
+// no more, but for vocabularies that 64 parts of 4 spans do not hold: they are read again); tmax: the lane's largest of all but NaNs;
 // nan: whether the part holds one.
 template <class T>
-__device__ void part_top(const T* row, int64_t first, int64_t end, int top, float tmax, bool nan, float* out_z, int* out_id) {
+__device__ void part_top(const T* row, int64_t first, int64_t end, int top, const float (&v)[4][8], float tmax, bool nan, uint64_t* out) {
   __shared__ float s_group[64];
-  __shared__ uint32_t s_key[kCandidates];
-  __shared__ int s_id[kCandidates];
+  __shared__ uint64_t s_order[kCandidates];
   __shared__ int s_count;
-  __shared__ float s_border;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   // The `top`-th largest of the maxima of 64 groups of lanes is at most the `top`-th largest value: a border that few values pass.
   float g = fmaxf(tmax, lane_xor<1>(tmax));
   g = fmaxf(g, lane_xor<2>(g));
   if ((lane & 3) == 0) s_group[wave * 16 + lane / 4] = g;
+  s_order[tid] = 0;
   if (tid == 0) s_count = 0;
   __syncthreads();
-  if (wave == 0) {
-    const float mine = s_group[lane];
-    int rank = 0;
-#pragma unroll
-    for (int i = 0; i < 64; ++i) {
-      const float other = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(mine), i));
-      rank += other > mine || (other == mine && i < lane);
-    }
-    if (rank == top - 1) s_border = mine;
-  }
-  __syncthreads();
-  const float border = s_border;
+  float sorted = s_group[lane];
+  sort_wave(sorted);            // every wave for itself
+  const float border = __uint_as_float((uint32_t)__builtin_amdgcn_readlane(__float_as_int(sorted), top - 1));
   if (!nan && border != -INFINITY) {
     if (tmax >= border) {
-      for (int64_t at = first + tid * 8; at < end; at += kSpan) {
-        float v[8];
-        load_logits(row, at, end, v);
+      const auto take = [&](const float (&x)[8], int64_t at) {
+        int mine = 0;
 #pragma unroll
-        for (int i = 0; i < 8; ++i)
-          if (v[i] >= border) {
-            const int k = atomicAdd(&s_count, 1);
-            if (k < kCandidates) {
-              s_key[k] = order_key(v[i]);
-              s_id[k] = (int)(at + i);
-            }
-          }
+        for (int i = 0; i < 8; ++i) mine += x[i] >= border;
+        if (mine == 0) return;
+        int k = atomicAdd(&s_count, mine);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          if (x[i] >= border && k < kCandidates) s_order[k] = order_of(x[i], (int)at + i);
+          k += x[i] >= border;
+        }
+      };
+#pragma unroll
+      for (int u = 0; u < 4; ++u) take(v[u], first + u * kSpan + tid * 8);
+      for (int64_t at = first + 4 * kSpan + tid * 8; at < end; at += kSpan) {
+        float x[8];
+        load_logits(row, at, end, x);
+        take(x, at);
       }
     }
     __syncthreads();
     const int count = s_count;
     if (count <= kCandidates) {     // uniform; the order in which lanes came does not show in the ranks
       if (tid < count) {
-        const uint32_t key = s_key[tid];
-        const int id = s_id[tid];
-        int rank = 0;
-        for (int i = 0; i < count; ++i) rank += before(s_key[i], s_id[i], key, id);
-        if (rank < top) {
-          out_z[rank] = (float)row[id];
-          out_id[rank] = id;
-        }
+        const uint64_t mine = s_order[tid];
+        const int rank = rank_among(s_order, count, mine);
+        if (rank < top) out[rank] = mine;
       }
       __syncthreads();
       return;
     }
   }
   // Many values at the border, rows with few finite values or NaNs: one after the other, each the first behind the last one.
-  uint32_t last_key = 0xFFFFFFFFu;
-  int last_id = -1;
+  uint64_t last = ~0ull;
   for (int k = 0; k < top; ++k) {
-    uint32_t key = 0;
-    int id = 0x7FFFFFFF;
+    uint64_t best = 0;
     for (int64_t at = first + tid * 8; at < end; at += kSpan) {
       float v[8];
       load_logits(row, at, end, v);
       const int n = (int)min((int64_t)8, end - at);
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        const uint32_t c = order_key(v[i]);
-        if (i < n && before(last_key, last_id, c, (int)at + i) && before(c, (int)at + i, key, id)) {
-          key = c;
-          id = (int)at + i;
-        }
+        const uint64_t c = order_of(v[i], (int)at + i);
+        if (i < n && c < last && c > best) best = c;
       }
     }
-    first_of_lanes(key, id, 64);
+    best = max_of_lanes(best, 64);
     __syncthreads();
-    if (lane == 0) {
-      s_key[wave] = key;
-      s_id[wave] = id;
-    }
+    if (lane == 0) s_order[wave] = best;
     __syncthreads();
-    for (int i = 0; i < kLanes / 64; ++i)
-      if (before(s_key[i], s_id[i], key, id)) {
-        key = s_key[i];
-        id = s_id[i];
-      }
-    last_key = key;
-    last_id = id;
-    if (tid == 0) {
-      const bool there = id != 0x7FFFFFFF;     // a short part holds fewer than `top`
-      out_z[k] = there ? (float)row[id] : -INFINITY;
-      out_id[k] = id;
-    }
+    for (int i = 0; i < kLanes / 64; ++i) best = s_order[i] > best ? s_order[i] : best;
+    last = best;
+    if (tid == 0) out[k] = best;
   }
   __syncthreads();
 }
 
-template <class T, bool ENTROPY>
+template <class T, bool ENTROPY, bool TOP>
 __global__ __launch_bounds__(kLanes) void logprob_kernel(const LogProbArgs a) {
   __shared__ Sums s_sums[kLanes / 64];
-  __shared__ float s_z[kMaxTop];
-  __shared__ int s_token[kMaxTop];
+  __shared__ uint64_t s_top[kMaxTop];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int64_t r = a.first_row + blockIdx.x / a.parts;
   const int p = blockIdx.x % a.parts;
@@ -249,20 +253,28 @@ __global__ __launch_bounds__(kLanes) void logprob_kernel(const LogProbArgs a) {
         if (ENTROPY) t.w = fmaf(e, fmaxf(d, kFloor), t.w);
       }
   };
+  const auto load = [&](int64_t at, float (&v)[4][8]) {
+    if (at + 3 * kSpan + 8 <= end) {
+      Raw8<T> raw[4];
+#pragma unroll
+      for (int u = 0; u < 4; ++u) raw[u] = load8(row + at + u * kSpan, 8);
+#pragma unroll
+      for (int u = 0; u < 4; ++u) widen(raw[u], v[u]);
+    } else {
+#pragma unroll
+      for (int u = 0; u < 4; ++u) load_logits(row, at + u * kSpan, end, v[u]);
+    }
+  };
   int64_t at = first + tid * 8;
-  for (; at + 3 * kSpan + 8 <= end; at += 4 * kSpan) {
-    Raw8<T> raw[4];
-    float v[4][8];
-#pragma unroll
-    for (int u = 0; u < 4; ++u) raw[u] = load8(row + at + u * kSpan, 8);
-#pragma unroll
-    for (int u = 0; u < 4; ++u) widen(raw[u], v[u]);
-    add(v);
+  float held[4][8];                // the first ones, for the likeliest tokens
+  if constexpr (TOP) {
+    load(at, held);
+    add(held);
+    at += 4 * kSpan;
   }
-  if (at < end) {
+  for (; at < end; at += 4 * kSpan) {
     float v[4][8];
-#pragma unroll
-    for (int u = 0; u < 4; ++u) load_logits(row, at + u * kSpan, end, v[u]);
+    load(at, v);
     add(v);
   }
   const float m = lane_max64(t.m);
@@ -282,14 +294,11 @@ __global__ __launch_bounds__(kLanes) void logprob_kernel(const LogProbArgs a) {
     q.s += o.s;
     q.w += o.w;
   }
-  if (a.top) part_top(row, first, end, a.top, tmax, q.s != q.s, s_z, s_token);
+  if constexpr (TOP) part_top(row, first, end, a.top, held, tmax, q.s != q.s, s_top);
   if (a.parts > 1) {
     const int64_t at = r * a.parts + p;
     if (tid == 0) *(float4*)(a.part_sums + at * 4) = make_float4(q.m, q.s, q.w, 0.0f);
-    if (tid < a.top) {
-      a.part_top[at * a.top + tid] = s_z[tid];
-      a.part_ids[at * a.top + tid] = s_token[tid];
-    }
+    if (tid < a.top) a.part_top[at * a.top + tid] = s_top[tid];
     return;
   }
   const RowResult f = finish(q);
@@ -299,8 +308,8 @@ __global__ __launch_bounds__(kLanes) void logprob_kernel(const LogProbArgs a) {
     if (a.stats) *(float2*)(a.stats + 2 * r) = make_float2(f.m, f.log_s);
   }
   if (tid < a.top) {
-    a.top_logp[r * a.top + tid] = log_prob(s_z[tid], f);
-    a.top_ids[r * a.top + tid] = s_token[tid];
+    a.top_logp[r * a.top + tid] = log_prob(value_of(s_top[tid]), f);
+    a.top_ids[r * a.top + tid] = token_of(s_top[tid]);
   }
 }
 
@@ -308,8 +317,8 @@ __global__ __launch_bounds__(kLanes) void logprob_kernel(const LogProbArgs a) {
 // lists' heads, `top` times.
 template <class T>
 __global__ __launch_bounds__(64) void logprob_join_kernel(const LogProbArgs a) {
-  __shared__ float s_z[kMaxParts * kMaxTop];
-  __shared__ int s_token[kMaxParts * kMaxTop];
+  __shared__ uint64_t s_list[kMaxParts * kMaxTop];
+  __shared__ uint64_t s_order[64];
   const int lane = threadIdx.x;
   const int64_t r = a.first_row + blockIdx.x;
   const int64_t target = a.targets ? a.targets[r] : -1;
@@ -321,10 +330,8 @@ __global__ __launch_bounds__(64) void logprob_join_kernel(const LogProbArgs a) {
     t = Sums{x.x, x.y, x.z};
   }
   const int held = a.parts * a.top;
-  for (int i = lane; i < held; i += 64) {
-    s_z[i] = a.part_top[r * held + i];
-    s_token[i] = a.part_ids[r * held + i];
-  }
+#pragma unroll 8
+  for (int i = lane; i < held; i += 64) s_list[i] = a.part_top[r * held + i];
   const float m = lane_max64(t.m);
   rescale(t, m);
   t.s = lanes_sum<64>(t.s);
@@ -335,19 +342,50 @@ __global__ __launch_bounds__(64) void logprob_join_kernel(const LogProbArgs a) {
     if (a.entropy) a.entropy[r] = f.entropy;
     if (a.stats) *(float2*)(a.stats + 2 * r) = make_float2(f.m, f.log_s);
   }
+  if (a.top == 0) return;
   __syncthreads();
+  // Each list's `depth` first ones come no later than its entry at depth - 1, so that `top` or more come no later than the border below, and
+  // mostly not many more.
+  const int depth = min((2 * a.top + a.parts - 1) / a.parts, a.top), wanted = (a.top + depth - 1) / depth;
+  const uint64_t mine = lane < a.parts ? s_list[lane * a.top + depth - 1] : 0ull;
+  s_order[lane] = mine;
+  __syncthreads();
+  const bool chosen = mine != 0 && rank_among(s_order, a.parts, mine) == wanted - 1;
+  const uint64_t vote = __builtin_amdgcn_ballot_w64(chosen);
+  int count = 0;
+  if (vote) {
+    const int at = __ffsll((unsigned long long)vote) - 1;
+    const uint64_t border = (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(mine >> 32), at) << 32 |
+                            (uint32_t)__builtin_amdgcn_readlane((int)mine, at);
+    __syncthreads();
+    s_order[lane] = 0;
+    __syncthreads();
+    for (int j = 0; j < a.top; ++j) {
+      const uint64_t x = lane < a.parts ? s_list[lane * a.top + j] : 0ull;
+      const uint64_t passing = __builtin_amdgcn_ballot_w64(x >= border);
+      if (passing == 0) break;
+      const int place = count + __popcll(passing & ((1ull << lane) - 1));
+      if (x >= border && place < 64) s_order[place] = x;
+      count += __popcll(passing);
+    }
+    __syncthreads();
+  }
+  if (vote && count <= 64) {
+    const uint64_t x = s_order[lane];
+    const int rank = rank_among(s_order, count, x);
+    if (lane < count && rank < a.top) {
+      a.top_logp[r * a.top + rank] = log_prob(value_of(x), f);
+      a.top_ids[r * a.top + rank] = token_of(x);
+    }
+    return;
+  }
   int head = 0;
   for (int k = 0; k < a.top; ++k) {
-    const int at = lane * a.top + head;
-    const bool there = lane < a.parts && head < a.top;
-    const int mine = there ? s_token[at] : 0x7FFFFFFF;
-    const float z = there ? s_z[at] : -INFINITY;
-    uint32_t key = mine == 0x7FFFFFFF ? 0u : order_key(z);
-    int id = mine;
-    first_of_lanes(key, id, a.parts);
-    if (mine == id && there) {       // one lane: tokens differ, and there are `top` of them at least
-      a.top_logp[r * a.top + k] = log_prob(z, f);
-      a.top_ids[r * a.top + k] = id;
+    const uint64_t own = lane < a.parts && head < a.top ? s_list[lane * a.top + head] : 0ull;
+    const uint64_t best = max_of_lanes(own, a.parts);
+    if (own == best && own != 0) {       // one lane: there are `top` of them at least
+      a.top_logp[r * a.top + k] = log_prob(value_of(own), f);
+      a.top_ids[r * a.top + k] = token_of(own);
       ++head;
     }
   }
@@ -412,8 +450,9 @@ hipError_t run_forward(LogProbArgs k, int64_t rows, hipStream_t s) {
   const bool entropy = k.entropy != nullptr;
   for (k.first_row = 0; k.first_row < rows; k.first_row += run) {
     const int64_t n = rows - k.first_row < run ? rows - k.first_row : run;
-    if (entropy) logprob_kernel<T, true><<<(uint32_t)(n * k.parts), kLanes, 0, s>>>(k);
-    else logprob_kernel<T, false><<<(uint32_t)(n * k.parts), kLanes, 0, s>>>(k);
+    const auto go = [&](auto kernel) { kernel<<<(uint32_t)(n * k.parts), kLanes, 0, s>>>(k); };
+    if (k.top) entropy ? go(logprob_kernel<T, true, true>) : go(logprob_kernel<T, false, true>);
+    else entropy ? go(logprob_kernel<T, true, false>) : go(logprob_kernel<T, false, false>);
     if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
     if (k.parts > 1) logprob_join_kernel<T><<<(uint32_t)n, 64, 0, s>>>(k);
     if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
@@ -435,15 +474,17 @@ hipError_t run_grad(GradArgs k, int64_t rows, hipStream_t s) {
 
 }  // namespace
 
-// Few rows are cut into parts, so that there are workgroups for all compute units; a part is one span at least.
-int logprob_parts(hot_type, int64_t rows, int64_t vocab) {
+// Few rows are cut into parts, so that there are workgroups for all compute units; a part is one span at least, and with likeliest tokens what a
+// workgroup holds in registers at most.
+int logprob_parts(hot_type, int64_t rows, int64_t vocab, int top) {
   const int64_t most = ceil_div(vocab, kSpan), wanted = ceil_div(2048, rows);
   int64_t parts = most < wanted ? most : wanted;
+  if (top && parts < ceil_div(vocab, 4 * kSpan)) parts = ceil_div(vocab, 4 * kSpan);
   if (parts > kMaxParts) parts = kMaxParts;
   return (int)ceil_div(vocab, (int64_t)spans_of_part(vocab, (int)parts) * kSpan);
 }
 size_t logprob_scratch_bytes(hot_type type, int64_t rows, int64_t vocab, int top) {
-  const int parts = logprob_parts(type, rows, vocab);
+  const int parts = logprob_parts(type, rows, vocab, top);
   return parts == 1 ? 0 : (size_t)(rows * parts) * (16 + 8 * (size_t)top);
 }
 
@@ -458,12 +499,11 @@ hipError_t launch_logprobs(const LogProbs& a, hipStream_t s) {
   k.top_ids = a.top_ids;
   k.vocab = a.vocab;
   k.top = a.top;
-  k.parts = logprob_parts(a.type, a.rows, a.vocab);
+  k.parts = logprob_parts(a.type, a.rows, a.vocab, a.top);
   k.part = spans_of_part(a.vocab, k.parts) * kSpan;
   if (k.parts > 1) {
     k.part_sums = (float*)a.ws;
-    k.part_top = k.part_sums + a.rows * k.parts * 4;
-    k.part_ids = (int32_t*)(k.part_top + a.rows * k.parts * a.top);
+    k.part_top = (uint64_t*)(k.part_sums + a.rows * k.parts * 4);
   }
   return a.type == HOT_BF16 ? run_forward<bf16>(k, a.rows, s) : run_forward<float>(k, a.rows, s);
 }
