@@ -769,35 +769,38 @@ class AdamWTensors:
     def __init__(self, tensors: Sequence[dict], state: str = "f32"):
         form = _STATES[state]
         self.tensors = [dict(t) for t in tensors]
-        self.device = -1
+        self.state, self.device = state, -1
         count = len(self.tensors)
         entries = (hot_adamw_tensor * max(count, 1))()
-        for i, (t, e) in enumerate(zip(self.tensors, entries)):
-            p, g = t["param"], t["grad"]
-            e.param_type, e.grad_type, n, dev = _flat(f"param of tensor {i}", p), _flat(f"grad of tensor {i}", g), p.numel(), p.get_device()
-            if n < 1 or g.numel() != n:
-                raise ValueError(f"tensor {i}: expected as many gradients as weights, one at least")
+
+        def address(name: str, i: int, x: torch.Tensor, dtype: torch.dtype, n: int) -> int:
+            if x.numel() != n or x.dtype is not dtype or x.get_device() != self.device or not x.is_contiguous():
+                raise ValueError(f"{name} of tensor {i}: expected {n} contiguous {dtype} elements on cuda:{self.device}")
+            return x.data_ptr()
+
+        for i, t in enumerate(self.tensors):
+            p, g, e, get = t["param"], t["grad"], entries[i], t.get
+            n, dev = p.numel(), p.get_device()
+            e.param_type, e.grad_type = _flat(f"param of tensor {i}", p), _flat(f"grad of tensor {i}", g)
             if self.device not in (-1, dev):
                 raise ValueError(f"tensor {i}: on cuda:{dev}, others on cuda:{self.device}")
             self.device = dev
-            e.n, e.weight_decay, e.lr_factor = n, t.get("weight_decay", 0.0), t.get("lr_factor", 1.0)
-            for name, dtype in (("param", p.dtype), ("grad", g.dtype), ("param_out", p.dtype), ("copy", torch.bfloat16)):
-                x = t.get(name)
-                if x is not None:
-                    if x.numel() != n:
-                        raise ValueError(f"{name} of tensor {i}: expected {n} elements")
-                    setattr(e, name, _expect(f"{name} of tensor {i}", x, dtype, x.shape, dev))
+            e.n, e.weight_decay, e.lr_factor = n, get("weight_decay", 0.0), get("lr_factor", 1.0)
+            e.param, e.grad = p.data_ptr(), address("grad", i, g, g.dtype, n)
+            x = get("param_out")
+            if x is not None:
+                e.param_out = address("param_out", i, x, p.dtype, n)
+            x = get("copy")
+            if x is not None:
+                e.copy = address("copy", i, x, torch.bfloat16, n)
             for name in ("m", "v", "m_out", "v_out"):
-                x = t.get(name)
+                x = get(name)
                 if x is None:
                     continue
-                if state == "8bit":
-                    setattr(e, name, _bytes(f"{name} of tensor {i}", x, hot_adamw_state_bytes(state, n), dev))
-                elif x.numel() != n:
-                    raise ValueError(f"{name} of tensor {i}: expected {n} elements")
-                else:
-                    setattr(e, name, _expect(f"{name} of tensor {i}", x, torch.float32, x.shape, dev))
-        self.state = state
+                if form == HOT_STATE_F32:
+                    setattr(e, name, address(name, i, x, torch.float32, n))
+                else:      # blocks of 1024 codes and 32 exponents
+                    setattr(e, name, _bytes(f"{name} of tensor {i}", x, (n + 1023) // 1024 * 1056, dev))
         size = int(lib().hot_adamw_table_bytes(count))
         self.table = (C.c_uint64 * max((size + 7) // 8, 1))()
         _check(lib().hot_adamw_table(entries, count, form, self.table, size), "hot_adamw_table")
