@@ -358,9 +358,10 @@ hot_status hot_linear_forward(const void* x, const void* w, hot_type type, const
  * and behind the last one are left as they were, in y and in u.  offsets and index NULL (segments 0): all rows have
  * adapter 0.  Both are read by the kernels, so that a recorded call follows what they hold at each replay;
  * offsets that do not ascend or leave [0, L] give undefined results within the buffers.
- * 1 <= rank <= 128 (adapters of lower rank beside it: zeros in a and b), L < 2^30, segments <= 2^24,
- * adapters <= 65536, adapters * (O + I) < 2^28.
- * Products and sums are fp32; bfloat16 operands are exact, u enters the second product with 16 bits or more.
+ * 1 <= rank <= 128 (adapters of lower rank beside it: zeros in a and b), L < 2^27, segments <= 2^24,
+ * adapters <= 65536, adapters * (O + I) < 2^27.
+ * Products and sums are fp32; bfloat16 operands are exact, u enters the second product with 16 bits or more.  An infinity or
+ * a NaN in a row stays in it; one in an adapter makes infinities or NaNs in the outputs that its elements have a part in.
  * ws: at least hot_adapter_forward_workspace_bytes() bytes of scratch, 256-byte aligned.
  */
 size_t hot_adapter_forward_workspace_bytes(hot_type type, int64_t L, int64_t O, int64_t I, int64_t rank, int64_t adapters,

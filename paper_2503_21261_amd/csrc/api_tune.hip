@@ -14,7 +14,7 @@ namespace hot {
 namespace {
 
 // ---- adapters ----
-constexpr int64_t kMaxBatchRows = 1ll << 30, kMaxSegments = 1ll << 24, kMaxAdapters = 1ll << 16, kMaxAdapterCols = 1ll << 28;
+constexpr int64_t kMaxBatchRows = 1ll << 27, kMaxSegments = 1ll << 24, kMaxAdapters = 1ll << 16, kMaxAdapterCols = 1ll << 27;   // fewer than 2^32 lanes a launch
 
 bool adapter_size_ok(int64_t L, int64_t O, int64_t I, int64_t rank, int64_t adapters, int64_t segments) {
   return size_ok(L, O) && size_ok(L, I) && L < kMaxBatchRows && rank >= 1 && rank <= kMaxRank && adapters >= 1 &&

@@ -69,6 +69,8 @@ def test_adapter_workspace_sizes():
         for bad in ((0, 4, 4, 4, 1, 0), (4, 0, 4, 4, 1, 0), (4, 4, 0, 4, 1, 0), (4, 4, 4, 0, 1, 0), (4, 4, 4, 129, 1, 0), (4, 4, 4, 4, 0, 0), (4, 4, 4, 4, 1, -1),
                     (1 << 30, 4, 4, 4, 1, 0)):
             assert f(torch.float32, *bad) == 0
+        assert f(torch.float32, (1 << 27) - 1, 4, 4, 4, 1, 0) > 0 and f(torch.float32, 1 << 27, 4, 4, 4, 1, 0) == 0
+        assert f(torch.float32, 4, 1024, 1023, 4, 65536, 1) > 0 and f(torch.float32, 4, 1024, 1024, 4, 65536, 1) == 0
     with pytest.raises(ValueError):
         hot.hot_adapter_forward_workspace_bytes(torch.float16, 4, 4, 4, 4, 1, 0)
     x, a, b = torch.empty(4, 8), torch.empty(2, 3, 8), torch.empty(2, 5, 3)
@@ -93,7 +95,7 @@ def test_logprob_refusals():
         assert logprobs(**bad) == hot.HOT_ERR_SHAPE, bad
     assert logprobs(vocab=9000, n=0) == hot.HOT_ERR_WORKSPACE
     size = hot.hot_token_logprobs_workspace_bytes
-    assert size(torch.float32, 4, 9000, 5) > 0 and size(torch.float32, 4, 100, 5) == 0 and size(torch.float32, 4096, 9000, 5) == 0
+    assert size(torch.float32, 4, 9000, 5) > 0 and size(torch.float32, 4, 100, 5) == 0 and size(torch.float32, 4096, 8192, 5) == 0
     assert size(torch.float32, 4, 9000, 33) == 0 and size(torch.float32, 4, 4, 5) == 0 and size(torch.float32, 0, 9000, 0) == 0
     with pytest.raises(hot.HotError):
         hot.alloc_logprobs_workspace(torch.empty(3, 9), 10)

@@ -210,6 +210,49 @@ def test_adapter_recorded_calls_follow_the_batch():
             assert torch.equal(d[name], want), (cuts, name)
 
 
+def test_recorded_calls_share_a_workspace():
+    """Two recorded passes of adapters and one of log probabilities, all with one workspace, replayed in turn."""
+    sizes = ((96, 130, 200, 16), (40, 520, 264, 24))
+    made = [make(L, O, I, rank, ([0, 20, L - 3], [1, 0], 2), BF16, seed=87 + L)[0] for L, O, I, rank in sizes]
+    want = [run_pass(t) for t in made]
+    z = logits(2, 9000, BF16, 88).cuda()
+    need = max([hot.hot_token_logprobs_workspace_bytes(BF16, 2, 9000, 5)] + [max(hot.hot_adapter_forward_workspace_bytes(BF16, *s, 2, 2),
+                                                                                 hot.hot_adapter_backward_workspace_bytes(BF16, *s, 2, 2)) for s in sizes])
+    ws = torch.full((need,), 255, device="cuda", dtype=torch.uint8)
+    top_logp, top_ids = torch.empty(2, 5, device="cuda"), torch.empty(2, 5, device="cuda", dtype=torch.int32)
+    hot.hot_token_logprobs(z, None, None, ws, top_logp=top_logp, top_ids=top_ids)
+    want_top = top_logp.clone(), top_ids.clone()
+    device = [{k: v.cuda() for k, v in t.items()} for t in made]
+
+    def call(d):
+        more = dict(scale=d["scale"], offsets=d["offsets"], index=d["index"])
+        hot.hot_adapter_forward(d["x"], d["a"], d["b"], d["y"], ws, base=d["base"], u=d["u"], **more)
+        hot.hot_adapter_backward(d["g_y"], d["x"], d["u"], d["a"], d["b"], ws, g_base=d["g_base"], g_x=d["g_x"], g_a=d["g_a"], g_b=d["g_b"], **more)
+
+    graphs = [torch.cuda.CUDAGraph() for _ in range(3)]
+    for graph, d in zip(graphs, device):
+        with torch.cuda.graph(graph):
+            call(d)
+    with torch.cuda.graph(graphs[2]):
+        hot.hot_token_logprobs(z, None, None, ws, top_logp=top_logp, top_ids=top_ids)
+    for turn in ((0, 1, 2), (2, 1, 0), (1, 2, 0)):
+        for d, t in zip(device, made):
+            for name in ("g_a", "g_b"):
+                d[name].fill_(math.nan)
+            for name in ("y", "u", "g_x"):
+                d[name].copy_(t[name])
+        top_logp.zero_()
+        top_ids.zero_()
+        torch.cuda.synchronize()
+        for g in turn:
+            graphs[g].replay()
+        torch.cuda.synchronize()
+        for k in range(2):
+            for name, value in want[k].items():
+                assert torch.equal(device[k][name], value), (turn, k, name)
+        assert torch.equal(top_logp, want_top[0]) and torch.equal(top_ids, want_top[1]), turn
+
+
 def test_adapter_past_32_bits():
     """Rows whose elements lie past 2^31 of the tensors' beginning."""
     L, O, I, rank = (1 << 20) + 40, 8, 2056, 4
