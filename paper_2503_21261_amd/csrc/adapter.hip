@@ -4,8 +4,8 @@
 //
 // Bound by memory: with a rank of some tens, x, g_y and the outputs are read or written for two operations a rank and element.  Three
 // kernels, all on the matrix cores, none with a library call:
-//   shrink  [rows x K] . [rank x K]^T -> [rows x rank]: a wave holds 32 rows (or one) and all ranks, K in slices where rows are few;
-//   expand  [rows x rank] . [N x rank]^T -> [rows x N]: the ranks' factors of the rows stay in registers, columns go by;
+//   shrink  [rows x K] . [rank x K]^T -> [rows x rank]: a workgroup has 16 to 64 rows (or one) and all ranks, K in slices where rows are few;
+//   expand  [rows x rank] . [N x rank]^T -> [rows x N]: a wave holds the factors of its columns in registers, rows go by;
 //   outer   [rows x rank]^T . [rows x N] -> [rank x N]: rows as they lie are transposed in registers, 8 x 8 values a lane, the factors
 //           before, by a launch of its own.
 // u and g_u are fp32.  Where they meet bfloat16 operands they are split into bfloat16 parts, cut off and not rounded, so that three
@@ -433,29 +433,37 @@ __device__ __forceinline__ Cols<float> sum_cols(const Cols<float>& b, const f4 (
   return r;
 }
 
-// Whole tiles of 16 rows, first to last, and 16 lanes' columns from n on: the rows' factors as they were packed, DEPTH tiles on their way.  Rows are
-// the product's rows here: tile t of NT has columns NT m + t, so that lane (i, q) ends with columns NT i .. of rows 4 q .. + 3, 16 lanes a row.
-// Nothing here branches but the loop, so that a wait is for one tile and not for all.  (The streaming hint on y: 140 us for 130,
-// reading and writing 16384 x 11008 bfloat16.)
-template <class T, int PIECES, int CHUNKS, int PARTS, int DEPTH, bool BASE>
-__device__ __forceinline__ void expand_tiles(const AdapterExpand& a, int64_t first, int64_t last, int64_t n, const Frag<T> (&fw)[kCols<T>][CHUNKS]) {
-  constexpr int NT = kCols<T>;
+// The rows of [row, end) and 16 lanes' columns, NT from col on each: the rows' factors as they were packed, DEPTH tiles of 16 rows on their way.  Rows are
+// the product's rows here: tile t of NT has column t of each lane, so that lane (i, q) ends with its columns of rows 4 q .. + 3, 16 lanes a row.
+// Nothing here branches but the loop, so that a wait is for one tile and not for all: where the rows do not fill their tiles (WHOLE says that they
+// do), the nearest one of them stands for those beside them, from its factors to its output, which is written more than once (by one
+// instruction, or by the same wave: the same bits).  Reading and writing 16384 x 11008 bfloat16, rank 64: 136 us, 5.3 TB/s; with the streaming
+// hint on y 8 % more.
+template <class T, int NT, int PIECES, int CHUNKS, int PARTS, int DEPTH, bool BASE, bool WHOLE>
+__device__ __forceinline__ void expand_tiles(const AdapterExpand& a, int64_t row, int64_t end, int64_t col, const Frag<T> (&fw)[NT][CHUNKS]) {
   const int lane = threadIdx.x & 63, i = lane & 15, q = lane >> 4;
   struct Tile {
-    Cols<T> base[4];
+    std::conditional_t<NT == 1, T, Cols<T>> base[4];
     Piece<T> p[PIECES];
   };
-  const int64_t from = (first + q * 4) * a.N + n + i * NT;
-  const T* const factors = (const T*)a.packed + (first >> 4) * PIECES * kTile + lane * (16 / (int)sizeof(T));
-  const int count = (int)((last - first) / 16) + 1;
+  const int64_t first = row & -16ll;
+  const int count = (int)((((end - 1) & -16ll) - first) / 16) + 1, m = (int)(row - first), rows = (int)(end - 1 - first);
+  const int64_t from = (WHOLE ? (first + q * 4) * a.N : first * a.N) + col;
+  const T* const factors = (const T*)a.packed + (first >> 4) * PIECES * kTile + (WHOLE ? lane : q * 16) * (16 / (int)sizeof(T));
+  const auto row_of = [&](int t, int e) -> int64_t { return (WHOLE ? t * 16 + e : min(max(t * 16 + q * 4 + e, m), rows)) * a.N; };
   const auto load = [&](int tile, Tile& d) {
     const int t = min(tile, count - 1);
     if constexpr (BASE) {
 #pragma unroll
-      for (int e = 0; e < 4; ++e) d.base[e] = load_cols((const T*)a.base + from + (t * 16 + e) * a.N);
+      for (int e = 0; e < 4; ++e) {
+        const T* const at = (const T*)a.base + from + row_of(t, e);
+        if constexpr (NT == 1) d.base[e] = *at;
+        else d.base[e] = load_cols(at);
+      }
     }
 #pragma unroll
-    for (int c = 0; c < PIECES; ++c) d.p[c] = load_piece<256>(factors + ((int64_t)t * PIECES + c) * kTile);
+    for (int c = 0; c < PIECES; ++c)
+      d.p[c] = load_piece<256>(factors + ((int64_t)t * PIECES + c) * kTile + (WHOLE ? 0 : (min(max(t * 16 + i, m), rows) & 15) * (16 / (int)sizeof(T))));
   };
   const auto finish = [&](int tile, const Tile& d) {
     f4 acc[NT];
@@ -468,8 +476,11 @@ __device__ __forceinline__ void expand_tiles(const AdapterExpand& a, int64_t fir
 #pragma unroll
         for (int t = 0; t < NT; ++t) acc[t] = mma(frag(d.p[c * PARTS + part]), fw[t][c], acc[t]);
 #pragma unroll
-    for (int e = 0; e < 4; ++e)
-      *(typename Cols<T>::V*)((T*)a.y + from + (tile * 16 + e) * a.N) = sum_cols(BASE ? d.base[e] : Cols<T>{}, acc, e).v;
+    for (int e = 0; e < 4; ++e) {
+      T* const to = (T*)a.y + from + row_of(tile, e);
+      if constexpr (NT == 1) *to = (T)(acc[0][e] + (BASE ? (float)d.base[e] : 0.0f));
+      else *(typename Cols<T>::V*)to = sum_cols(BASE ? d.base[e] : Cols<T>{}, acc, e).v;
+    }
   };
   Tile d[DEPTH];
 #pragma unroll
@@ -489,10 +500,77 @@ __device__ __forceinline__ void expand_tiles(const AdapterExpand& a, int64_t fir
     if (at + s < count) finish(at + s, d[s]);
 }
 
+// y = base in the rows of [row, end), NT columns a lane from col on; 32 rows are loaded together, the last one more than once.
+template <class T, int NT>
+__device__ __forceinline__ void copy_rows(const AdapterExpand& a, int64_t row, int64_t end, int64_t col) {
+  const int q = (threadIdx.x & 63) >> 4;
+  for (; row < end; row += 32) {
+    typedef std::conditional_t<NT == 1, T, typename Cols<T>::V> V;
+    V v[8]{};
+    if (a.base) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[e] = *(const V*)((const T*)a.base + min(row + e * 4 + q, end - 1) * a.N + col);
+    }
+#pragma unroll
+    for (int e = 0; e < 8; ++e) *(V*)((T*)a.y + min(row + e * 4 + q, end - 1) * a.N + col) = v[e];
+  }
+}
+
+// A lane's ranks of a row of weights: bfloat16 8 q .. + 7 of each chunk (of its half, where that is all), fp32 4 q .. + 3 and 16 + 4 q .. + 3.
+template <class T, int CHUNKS, bool PACK>
+__device__ __forceinline__ void load_ranks(const T* w, int rank, Frag<T> (&out)[CHUNKS]) {
+  const int q = (threadIdx.x & 63) >> 4;
+#pragma unroll
+  for (int c = 0; c < CHUNKS; ++c) out[c] = frag(load_piece_end(w + c * 32, PACK ? q & 1 : q, rank - c * 32, rank));
+}
+
 // RC chunks of 32 ranks (0: at most 16 ranks; in bfloat16 the chunk's second half is the second part of the same ranks).  A wave holds the
 // factors of 128 columns (fp32: 64) and goes over the rows; the four waves of a workgroup are side by side.
 template <class T, int RC, int DEPTH>
 __global__ __launch_bounds__(256, RC <= 2 ? 2 : 1) void expand_kernel(const AdapterExpand a, int col_groups, int64_t chunk) {
+  constexpr bool kSingle = sizeof(T) == 4, kPack = RC == 0 && !kSingle;
+  constexpr int kChunks = RC == 0 ? 1 : RC, kParts = kSingle || kPack ? 1 : 2, NT = kCols<T>;
+  const int lane = threadIdx.x & 63, i = lane & 15, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int64_t n = ((int64_t)(blockIdx.x % col_groups) * 4 + wave) * (16 * NT);
+  if (n >= a.N) return;
+  const bool few = n + NT > a.N;             // the last columns, too few for a load of NT: one a lane
+  const int64_t row0 = (int64_t)(blockIdx.x / col_groups) * chunk, row1 = min(row0 + chunk, a.b.L);
+
+  for (int64_t row = row0; row < row1;) {
+    const Run run = run_at(a.b, row, row1);
+    const T* const w = (const T*)a.w + run.adapter * a.w_stride;
+    if (run.adapter < 0) {
+      if (run.adapter == -1 && a.base != a.y) {
+        if (few) copy_rows<T, 1>(a, row, run.end, min(n + i, a.N - 1));
+        else copy_rows<T, NT>(a, row, run.end, min(n + i * NT, a.N - NT));
+      }
+    } else if (few) {
+      const int64_t col = min(n + i, a.N - 1);          // the last one more than once
+      Frag<T> fw[1][kChunks];
+      load_ranks<T, kChunks, kPack>(w + col * a.w_pitch, a.rank, fw[0]);
+      if (a.base) expand_tiles<T, 1, kChunks * kParts, kChunks, kParts, DEPTH, true, false>(a, row, run.end, col, fw);
+      else expand_tiles<T, 1, kChunks * kParts, kChunks, kParts, DEPTH, false, false>(a, row, run.end, col, fw);
+    } else {
+      const int64_t col = min(n + i * NT, a.N - NT);    // past the last column: the last NT once more
+      Frag<T> fw[NT][kChunks];
+#pragma unroll
+      for (int t = 0; t < NT; ++t) load_ranks<T, kChunks, kPack>(w + (col + t) * a.w_pitch, a.rank, fw[t]);
+      const auto tiles = [&](auto base, auto full) {
+        expand_tiles<T, NT, kChunks * kParts, kChunks, kParts, DEPTH, decltype(base)::value, decltype(full)::value>(a, row, run.end, col, fw);
+      };
+      const std::true_type yes{};
+      const std::false_type no{};
+      if (((row | run.end) & 15) == 0) a.base ? tiles(yes, yes) : tiles(no, yes);
+      else a.base ? tiles(yes, no) : tiles(no, no);
+    }
+    row = run.end;
+  }
+}
+
+// The same with factors in slices that are summed here, so that they cannot be asked for so far ahead: for few rows.  Columns are the
+// product's rows: lane (i, q) ends with columns NT (4 q + e) + t of row i.
+template <class T, int RC>
+__global__ __launch_bounds__(256, RC <= 2 ? 2 : 1) void expand_slices_kernel(const AdapterExpand a, int col_groups, int64_t chunk) {
   constexpr bool kSingle = sizeof(T) == 4, kPack = RC == 0 && !kSingle;
   constexpr int kChunks = RC == 0 ? 1 : RC, kParts = kSingle || kPack ? 1 : 2, NT = kCols<T>;
   const int lane = threadIdx.x & 63, i = lane & 15, q = lane >> 4, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -511,33 +589,15 @@ __global__ __launch_bounds__(256, RC <= 2 ? 2 : 1) void expand_kernel(const Adap
     }
     const bool none = run.adapter < 0;
     const float scale = none ? 0.0f : a.scale ? a.scale[run.adapter] : 1.0f;
-    // Ranks of this lane: bfloat16 8 q .. + 7 of a chunk (of its half, where that is all), fp32 4 q .. + 3 and 16 + 4 q .. + 3.
     Frag<T> fw[NT][kChunks];
     if (!none) {
       const T* const w = (const T*)a.w + run.adapter * a.w_stride;
 #pragma unroll
-      for (int t = 0; t < NT; ++t) {
-        const T* const at = w + min(n + i * NT + t, a.N - 1) * a.w_pitch;
-#pragma unroll
-        for (int c = 0; c < kChunks; ++c) fw[t][c] = frag(load_piece_end(at + c * 32, kPack ? q & 1 : q, a.rank - c * 32, a.rank));
-      }
+      for (int t = 0; t < NT; ++t) load_ranks<T, kChunks, kPack>(w + min(n + i * NT + t, a.N - 1) * a.w_pitch, a.rank, fw[t]);
     }
-    const int64_t first = (row + 15) & -16ll, last = (run.end & -16ll) - 16;      // whole tiles
-    const bool tiles = whole && !none && a.packed && first <= last;
-    if (tiles) {
-      if (a.base) expand_tiles<T, kChunks * kParts, kChunks, kParts, DEPTH, true>(a, first, last, n, fw);
-      else expand_tiles<T, kChunks * kParts, kChunks, kParts, DEPTH, false>(a, first, last, n, fw);
-    }
-    // The rows beside whole tiles; all of them where there are slices of the factors, no adapter, or fewer columns.  Columns are the
-    // product's rows here: lane (i, q) ends with columns NT (4 q + e) + t of row i.
     for (int64_t at = row; at < run.end; at += 16) {
-      if (tiles && at >= first && at <= last) {
-        at = last;
-        continue;
-      }
-      const int64_t end = tiles && at < first ? first : run.end;
-      const int64_t l = min(at + i, end - 1);
-      const bool mine = at + i < end;
+      const int64_t l = min(at + i, run.end - 1);
+      const bool mine = at + i < run.end;
       f4 acc[NT];
 #pragma unroll
       for (int t = 0; t < NT; ++t) acc[t] = f4{0.0f, 0.0f, 0.0f, 0.0f};
@@ -596,7 +656,6 @@ __global__ __launch_bounds__(256, RC <= 2 ? 2 : 1) void expand_kernel(const Adap
             if (n + q * (4 * NT) + e * NT + t < a.N)
               ((T*)a.y)[to + e * NT + t] = (T)(acc[t][e] + (a.base ? (float)((const T*)a.base)[to + e * NT + t] : 0.0f));
       }
-      if (tiles && at < first) at = first - 16;
     }
     row = run.end;
   }
@@ -1075,11 +1134,12 @@ hipError_t run_expand(const AdapterExpand& a, bool rows, hipStream_t s) {
   constexpr int kDepth = RC <= 2 ? 3 : 2;
   const int64_t groups = ceil_div(a.N, 64 * kCols<T>);
   // Packed factors are asked for ahead, so that workgroups need only be as many as are resident; slices are waited for, and more waves hide
-  // that (packed, 12608 x 768 fp32: 21.7 us, with 1024 of them 26.4; slices, 3330 x 2307 bfloat16: 26 us, with 512 of them 32.5).
+  // that (packed, 12608 x 768 fp32: 21.7 us, with 1024 of them 26.4; four slices, 3330 x 2307 bfloat16: 26 us, with 512 of them 32.5).
   const int64_t wanted = a.packed ? 512 : 1024;
   const int64_t chunk = rows ? ceil_div(a.b.L * groups, 1 << 22) : round_up(ceil_div(a.b.L, groups < wanted ? wanted / groups : 1), 16);
   const uint32_t grid = (uint32_t)(groups * ceil_div(a.b.L, chunk));
-  expand_kernel<T, RC, kDepth><<<grid, 256, 0, s>>>(a, (int)groups, chunk);
+  if (a.packed) expand_kernel<T, RC, kDepth><<<grid, 256, 0, s>>>(a, (int)groups, chunk);
+  else expand_slices_kernel<T, RC><<<grid, 256, 0, s>>>(a, (int)groups, chunk);
   return hipGetLastError();
 }
 template <class T>
@@ -1123,12 +1183,14 @@ AdapterPlan adapter_plan(hot_type type, int64_t L, int64_t O, int64_t I, int64_t
   p.pitch = (int)round_up(rank, 8);      // zeros behind the ranks
   // Rows of a workgroup: as many as leave workgroups for all compute units without slices, 16 at least.
   p.tile = p.rows ? 1 : L >= 64 * 224 && rank > 16 && rank <= 64 ? 64 : L >= 64 * 32 && rank <= 64 ? 32 : 16;
+  // With no slices the expansion finds its factors packed: not where each wave has four steps at most, which are all on their way at once, and
+  // the workgroups are not too few (3330 x 771 bfloat16, rank 12: 10.8 us in four slices or in none, and the expansion to 2307 then 26 us or 13.9).
   const auto slices = [&](int64_t K, int& count, int64_t& slice) {
     int64_t n = (p.tile == 64 ? 256 : 512) / ceil_div(L, p.tile);      // workgroups that are resident
     const int64_t most = ceil_div(K, 4 * step);      // a step for each wave
     if (n > most) n = most;
     if (n > kMaxSlices) n = kMaxSlices;
-    if (n < 1) n = 1;
+    if (n < 1 || (K <= 16 * step && ceil_div(L, p.tile) >= 64)) n = 1;
     slice = round_up(ceil_div(K, n), 4 * step);
     count = (int)ceil_div(K, slice);
   };
