@@ -138,6 +138,28 @@ def test_adapter_without_base_and_scale_and_in_place(dtype):
 
 
 @pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("O,I,rank", [(131, 259, 12), (139, 75, 40), (3, 7, 5), (264, 132, 100)])
+def test_adapter_borders_inside_tiles_of_many_rows(O, I, rank, dtype):
+    """Requests, rows without an adapter among them, that begin and end anywhere in tiles of many rows; last columns that fill no load; beside
+    base, without it, and in place."""
+    batch = ([3, 5, 700, 1407, 1407, 1441, 2140], [1, 0, -1, 1, 0, 1], 2)
+    t, kind = make(2150, O, I, rank, batch, dtype, seed=64)
+    got = run_pass(t)
+    check_pass(t, kind, got)
+    plain = {k: v for k, v in t.items() if k not in ("scale", "base", "g_base")}
+    check_pass(plain, kind, run_pass(plain))
+    d = {k: v.cuda() for k, v in t.items()}
+    ws = hot.alloc_adapter_workspace(d["x"], d["a"], d["b"], segments=len(batch[1]))
+    more = dict(scale=d["scale"], offsets=d["offsets"], index=d["index"])
+    hot.hot_adapter_forward(d["x"], d["a"], d["b"], d["base"], ws, base=d["base"], u=d["u"], **more)
+    hot.hot_adapter_backward(d["g_y"], d["x"], d["u"], d["a"], d["b"], ws, g_base=d["g_base"], g_x=d["g_base"], g_a=d["g_a"], g_b=d["g_b"], **more)
+    inside = slice(batch[0][0], batch[0][-1])
+    assert torch.equal(d["base"][inside], got["y"][inside]) and torch.equal(d["g_base"][inside], got["g_x"][inside])
+    for name in ("u", "g_a", "g_b"):
+        assert torch.equal(d[name], got[name]), name
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
 def test_adapter_keeps_infinities_and_nans_in_their_rows(dtype):
     for batch in ("ragged", "single", "one"):
         t, kind = make(70, 96, 70, 20, batch, dtype, seed=60)
