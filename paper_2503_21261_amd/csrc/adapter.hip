@@ -665,12 +665,13 @@ __global__ __launch_bounds__(256, RC <= 2 ? 2 : 1) void expand_slices_kernel(con
 
 // One row a workgroup and `span` columns of it: a row of weights is dealt to its rank / 8 lanes (a power of two, from 1 to 16), so that a wave
 // reads 1024 bytes in a row.  For rows that have an adapter each there is nothing that a matrix instruction could share (64 requests, 11008 columns,
-// rank 16: 9.8 us, 21.5 in tiles of 16 rows).
+// rank 16: 8.4 us, 21.5 in tiles of 16 rows).
 template <class T>
 __global__ __launch_bounds__(256) void expand_row_kernel(const AdapterExpand a, int cuts, int64_t span) {
   __shared__ float s_p[kMaxRank];
   const int tid = threadIdx.x, per = a.rank / 8;                // lanes of a column
   const int64_t row = blockIdx.x / cuts, n0 = (int64_t)(blockIdx.x % cuts) * span, n1 = min(n0 + span, a.N);
+  if (n0 >= a.N) return;
   const Run run = run_at(a.b, row, row + 1);
   if (run.adapter == -2) return;
   const int step = 256 / per, j0 = tid % per * 8;
@@ -1154,9 +1155,14 @@ hipError_t expand_of(const AdapterExpand& a, bool rows, hipStream_t s) {
   if (rows && a.rank % 8 == 0 && (per & (per - 1)) == 0) {
     const int64_t step = 256 / per, steps = ceil_div(a.N, step);
     int64_t cuts = ceil_div(1024, a.b.L);
+    if (a.b.L > 1 && cuts < 8 && steps >= 64) cuts = 8;
     if (cuts > steps) cuts = steps;
     const int64_t span = ceil_div(steps, cuts) * step;
     cuts = ceil_div(a.N, span);
+    // The eight XCDs take workgroups in turn: with eight cuts or a multiple of them an adapter's cut is read by one of them, for all of its rows
+    // (24 adapters, 11008 columns, rank 16: 64 rows 8.4 us, with 15 cuts 9.8; 1000 rows 46.5, with two cuts 50.7).  Cuts of few steps wait more than
+    // they read (1000 x 2304: 14.8 us in two, 23 in eight).
+    if (cuts > 4 && a.b.L > 1) cuts = round_up(cuts, 8);
     expand_row_kernel<T><<<(uint32_t)(a.b.L * cuts), 256, 0, s>>>(a, (int)cuts, span);
     return hipGetLastError();
   }
