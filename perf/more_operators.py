@@ -403,7 +403,8 @@ def _kernels(s):
         return hot.AdamWTensors([dict(weight_decay=decay, **{k: part(k, first, n) for k in (
             "param", "grad", "m", "v", "param_out", "m_out", "v_out", "copy")}) for first, n, decay in s["layout"]], state=case["state"])
 
-    hot.hot_adamw_step(scratch("table", table), lr=LR, beta1=BETA1, beta2=BETA2, eps=EPS, step=STEP)
+    # The plain form's rounding, which goes by the moments alone: by their own low bits.
+    hot.hot_adamw_step(scratch("table", table), lr=LR, beta1=BETA1, beta2=BETA2, eps=EPS, step=STEP, rounding=hot.HOT_ROUND_PSEUDO_STOCHASTIC)
     result = {"param": s["param_out"], "m": s["m_out"], "v": s["v_out"]}
     if eight:
         result["m"] = hot.hot_adamw_state_read(s["m_out"].view(-1), "m", s["m_read"])
