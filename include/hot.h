@@ -61,7 +61,11 @@ typedef enum { HOT_Q_PER_TENSOR = 0, HOT_Q_PER_TOKEN = 1 } hot_quantizer;
 
 /* Sec. 5.1: the paper's quantiser rounds pseudo-stochastically; nearest-even is
  * offered so the half-step round-trip bound can be checked. */
-typedef enum { HOT_ROUND_NEAREST_EVEN = 0, HOT_ROUND_PSEUDO_STOCHASTIC = 1 } hot_rounding;
+typedef enum {
+  HOT_ROUND_NEAREST_EVEN = 0,
+  HOT_ROUND_PSEUDO_STOCHASTIC = 1,
+  HOT_ROUND_DRAWN = 3      /* 8-bit moments of hot_adamw_step alone (below)                        */
+} hot_rounding;
 
 typedef struct {
   int32_t block;           /* n: WHT tile, 16 (paper, Supp. D) | 32 | 64                */
@@ -431,9 +435,18 @@ hot_status hot_token_logprobs_backward(const void* logits, hot_type type, int64_
  * that of the largest of the 32 (32 at least), and a v' above zero is never held as zero but as code 1 at least.  e = 255: NaN, for a
  * group that held an infinity or a NaN.  Codes past n are zero.  The new weights come from m' and v' before they are
  * rounded.
- * rounding: nearest, or HOT_ROUND_PSEUDO_STOCHASTIC: up where the fraction is more than the low 11 bits are, read as a
- * fraction, of what is rounded (m' in steps of its group; v' itself).  With rounding to the nearest a v that a step moves by less
- * than half a code (all of them, for beta2 = 0.999) stays where it is.
+ * rounding: HOT_ROUND_DRAWN is the one to train with: up with the probability that the fraction is, so that moments are right on
+ * average over the steps, to 2^-20 of a code of v and 2^-17 of one of m (a v that swings by a fifth, for beta2 = 0.999).  An
+ * element's 32 bits R, from its place i in its block, the step's seed and m' and v' themselves, all modulo 2^32:
+ *   R = f(seed + i / 8) + (i % 8) 0x9E379E37 + bits(m') + bits(v'),  f(x): x ^= x >> 16, x *= 0x6A09E667, x ^= x >> 15,
+ *   x *= 0xBB67AE85, x ^= x >> 16;  v' is held as (bits(v') + (R >> 12)) >> 20, m' as floor(m' / step + ((R & 0xFFFF) + 0.5) / 2^16).
+ *   seed: from 0, x -> f(seed ^ x ^ 0x9E3779B9) for the bits of lr, c1 and c2 in fp32 and a last word: step where c1 and c2 are those
+ *   of the step before, 0 otherwise; with `dynamic`, its fifth number's bits, 0 where there are four.
+ * So the same call gives the same bits, and a step number must not be used twice.
+ * The other two are for comparing a step's results and not for training: with HOT_ROUND_NEAREST_EVEN a v that a step moves by less than
+ * half a code (all of them, for beta2 = 0.999) stays where it is; HOT_ROUND_PSEUDO_STOCHASTIC, up where the fraction is more than the low 11
+ * bits are, read as a fraction, of what is rounded (m' in steps of its group; v' itself), takes the same way in every step whose gradient
+ * does not change those bits: with gradients of zero, constant or rare ones v does not follow.
  */
 typedef enum { HOT_STATE_F32 = 0, HOT_STATE_8BIT = 1 } hot_state_form;
 typedef enum { HOT_MOMENT_M = 0, HOT_MOMENT_V = 1 } hot_moment;
@@ -450,10 +463,12 @@ typedef struct {
 typedef struct {
   double lr, beta1, beta2, eps;    /* 0 <= beta < 1, eps > 0                                            */
   int64_t step;            /* 1 for the first one                                                       */
-  int32_t rounding;        /* hot_rounding, of 8-bit moments                                             */
-  int32_t reserved;
+  int32_t rounding;        /* hot_rounding, of 8-bit moments: HOT_ROUND_DRAWN to train with              */
+  int32_t dynamic_count;   /* numbers at `dynamic`: 4 (or 0, the same), or 5                             */
   const float* dynamic;    /* NULL, or device fp32 [4]: lr, c1, c2 and a factor of every gradient (loss scale, clipping), read
-                              by the kernels in place of lr and step: for recorded calls                 */
+                              by the kernels in place of lr and step: for recorded calls; apart from the tensors.  A fifth one
+                              for HOT_ROUND_DRAWN, which has to differ from step to step (the step, say): without it, steps whose lr,
+                              c1 and c2 are alike (from some thousand steps on, where lr does not change) round alike */
 } hot_adamw_config;
 
 /* Bytes of one moment of n elements; 0 for a size out of range. */

@@ -23,7 +23,7 @@ HOT_ERR_ARG, HOT_ERR_SHAPE, HOT_ERR_WORKSPACE, HOT_ERR_DEVICE, HOT_ERR_UNIMPLEME
 HOT_ERR_SCRATCH_LIMIT = 6
 HOT_NOALLOC_SCRATCH_BYTES = 64 << 20
 HOT_Q_PER_TENSOR, HOT_Q_PER_TOKEN = 0, 1
-HOT_ROUND_NEAREST_EVEN, HOT_ROUND_PSEUDO_STOCHASTIC = 0, 1
+HOT_ROUND_NEAREST_EVEN, HOT_ROUND_PSEUDO_STOCHASTIC, HOT_ROUND_DRAWN = 0, 1, 3
 
 EXPORTS = (
     "hot_default_config", "hot_status_string", "hot_act_buffer_bytes", "hot_workspace_bytes",
@@ -73,7 +73,7 @@ class hot_adamw_tensor(C.Structure):
 
 class hot_adamw_config(C.Structure):
     _fields_ = ([(f, C.c_double) for f in ("lr", "beta1", "beta2", "eps")] +
-                [("step", C.c_int64), ("rounding", C.c_int32), ("reserved", C.c_int32), ("dynamic", C.c_void_p)])
+                [("step", C.c_int64), ("rounding", C.c_int32), ("dynamic_count", C.c_int32), ("dynamic", C.c_void_p)])
 
 
 class HotError(RuntimeError):
@@ -807,14 +807,16 @@ class AdamWTensors:
 
 
 def hot_adamw_step(tensors: AdamWTensors, lr: float, beta1: float = 0.9, beta2: float = 0.999, eps: float = 1e-8, step: int = 1,
-                   rounding: int = HOT_ROUND_PSEUDO_STOCHASTIC, dynamic: Optional[torch.Tensor] = None, stream=None) -> None:
+                   rounding: int = HOT_ROUND_DRAWN, dynamic: Optional[torch.Tensor] = None, stream=None) -> None:
     """One AdamW step over the tensors.  dynamic: float32 [4] on the device, lr, 1 - beta1^step, 1 - beta2^step and a factor of every
-    gradient, in place of lr and step (for recorded calls)."""
+    gradient, in place of lr and step (for recorded calls); [5] with a number that no two steps share (the step, say), which goes
+    into the rounding of 8-bit moments where the first three no longer change."""
     dev = _current_device()
     if tensors.device != dev:
         raise ValueError(f"tensors: expected on cuda:{dev}, the current device")
-    cfg = hot_adamw_config(float(lr), float(beta1), float(beta2), float(eps), int(step), int(rounding), 0,
-                           _opt("dynamic", dynamic, torch.float32, (4,), dev))
+    count = 5 if dynamic is not None and tuple(dynamic.shape) == (5,) else 4
+    cfg = hot_adamw_config(float(lr), float(beta1), float(beta2), float(eps), int(step), int(rounding), count,
+                           _opt("dynamic", dynamic, torch.float32, (count,), dev))
     st = lib().hot_adamw_step(tensors.table, C.byref(cfg), _stream_of(stream, dev))
     if st:
         _check(st, "hot_adamw_step")

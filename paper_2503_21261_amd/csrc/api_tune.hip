@@ -322,8 +322,9 @@ hot_status hot_adamw_step(const void* table, const hot_adamw_config* cfg, void* 
   const TableHead* const head = (const TableHead*)table;
   const AdamWEntry* const e = (const AdamWEntry*)(head + 1);
   if (head->mark != kTableMark) return HOT_ERR_ARG;
-  const bool nearest = cfg->rounding == HOT_ROUND_NEAREST_EVEN;
-  if (!nearest && cfg->rounding != HOT_ROUND_PSEUDO_STOCHASTIC) return HOT_ERR_ARG;
+  const hot_rounding rounding = (hot_rounding)cfg->rounding;
+  if (rounding != HOT_ROUND_NEAREST_EVEN && rounding != HOT_ROUND_PSEUDO_STOCHASTIC && rounding != HOT_ROUND_DRAWN) return HOT_ERR_ARG;
+  if (cfg->dynamic_count != 0 && cfg->dynamic_count != 4 && cfg->dynamic_count != 5) return HOT_ERR_ARG;
   if (!(cfg->beta1 >= 0 && cfg->beta1 < 1) || !(cfg->beta2 >= 0 && cfg->beta2 < 1) || !((float)cfg->eps > 0) || !std::isfinite(cfg->eps) ||
       !std::isfinite(cfg->lr) || (!cfg->dynamic && cfg->step < 1))
     return HOT_ERR_ARG;
@@ -338,6 +339,12 @@ hot_status hot_adamw_step(const void* table, const hot_adamw_config* cfg, void* 
   a.s.corr1 = (float)(1.0 - std::pow(cfg->beta1, (double)cfg->step));
   a.s.corr2 = (float)(1.0 - std::pow(cfg->beta2, (double)cfg->step));
   a.s.dyn = cfg->dynamic;
+  a.s.words = cfg->dynamic_count == 5;
+  // The step's number is in the seed only where the corrections no longer tell the step from the one before, so that until then recorded
+  // calls, which have lr and the corrections, round as this one does.
+  const double before = (double)cfg->step - 1;
+  if (a.s.corr1 == (float)(1.0 - std::pow(cfg->beta1, before)) && a.s.corr2 == (float)(1.0 - std::pow(cfg->beta2, before)))
+    a.s.word = (uint32_t)cfg->step;
   int32_t next = 0;
   int64_t from = 0;                       // first block of tensor `next` that is still to be done
   while (next < head->count) {
@@ -356,7 +363,7 @@ hot_status hot_adamw_step(const void* table, const hot_adamw_config* cfg, void* 
     }
     a.count = (uint32_t)in;
     for (int i = in; i <= kAdamWEntries; ++i) a.block[i] = 0xFFFFFFFFu;
-    HOT_STAGE(kStAdamW, launch_adamw(a, (uint32_t)blocks, head->state == HOT_STATE_8BIT, nearest, s));
+    HOT_STAGE(kStAdamW, launch_adamw(a, (uint32_t)blocks, head->state == HOT_STATE_8BIT, rounding, s));
   }
   return HOT_OK;
 }

@@ -28,7 +28,8 @@ struct AdamWEntry {
 struct AdamWStep {
   float beta1, rest1, beta2, rest2;   // rest = 1 - beta
   float eps, lr, corr1, corr2;        // corr = 1 - beta^step
-  const float* dyn;                   // device: lr, corr1, corr2, factor of the gradients; or null
+  const float* dyn;                   // device: lr, corr1, corr2, factor of the gradients, and (`words`) a word of the seed; or null
+  uint32_t word, words;               // the seed's last word, where dyn has none
 };
 // `count` entries; the first one from element `first` on (a multiple of the chunk), the last one to element `last`.
 struct AdamWArgs {
@@ -39,7 +40,7 @@ struct AdamWArgs {
   AdamWEntry e[kAdamWEntries];
 };
 static_assert(sizeof(AdamWArgs) <= 4096, "kernel arguments");
-hipError_t launch_adamw(const AdamWArgs& a, uint32_t blocks, bool eight, bool nearest, hipStream_t s);
+hipError_t launch_adamw(const AdamWArgs& a, uint32_t blocks, bool eight, hot_rounding rounding, hipStream_t s);
 hipError_t launch_state_read(const void* state, bool second, int64_t n, void* out, hot_type type, hipStream_t s);
 hipError_t launch_state_write(const void* x, hot_type type, bool second, int64_t n, void* state, hipStream_t s);
 
