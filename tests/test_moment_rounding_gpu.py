@@ -120,3 +120,39 @@ def test_recorded_steps_draw_anew():
     want = drawn.held(m2, v2, drawn.step_seed(lr, 1.0, 1.0))
     got = values(four, n)
     assert np.array_equal(got[0], ref.read_m(*want[0])) and np.array_equal(got[1], ref.read_v(*want[1]))
+
+
+@pytest.mark.parametrize("form", ["f32", "8bit"])
+@pytest.mark.parametrize("rounding", [hot.HOT_ROUND_NEAREST_EVEN, hot.HOT_ROUND_PSEUDO_STOCHASTIC, hot.HOT_ROUND_DRAWN])
+def test_largest_numbers_are_held_and_what_overflows_is_marked(form, rounding):
+    """A gradient of 3e19, whose v' is 9e35: its group is held, to the bit.  One of 1e21, whose square is none: v's group is NaN, m's is not, and
+    the weight does not move, since m' / inf is 0."""
+    n, lr, b1, b2, eps = 2100, 1e-3, 0.9, 0.999, 1e-8
+    m, v, mb, vb = moments_of(n, 7, form)
+    p, g = rand((n,), 0.5, 1), rand((n,), 1e-2, 2)
+    g[70], g[1100] = 3e19, 1e21
+    d = dict(param=p.cuda(), grad=g.cuda(), m=mb.cuda(), v=vb.cuda())
+    hot.hot_adamw_step(hot.AdamWTensors([d], state=form), lr, b1, b2, eps, 1, rounding=rounding)
+    with np.errstate(over="ignore"):
+        m2, v2 = ref.moments(m, v, g.numpy(), b1, b2)
+    assert np.isfinite(m2).all() and np.isinf(v2[1100]) and np.isfinite(np.delete(v2, 1100)).all() and 8e35 < v2[70] < 1e36
+    fine = np.arange(n) != 1100
+    weights = d["param"].cpu()
+    w, err = ref.weights(p.numpy(), m2, np.where(fine, v2, 1), lr, 0.0, 1 - b1, 1 - b2, eps)
+    within("param", weights[fine], torch.from_numpy(w[fine]), torch.from_numpy(err[fine]))
+    assert weights[1100] == p[1100]
+    if form == "f32":
+        assert torch.equal(d["m"].cpu(), torch.from_numpy(m2)) and torch.equal(d["v"].cpu(), torch.from_numpy(v2))
+        return
+    pad = (0, -n % 1024)
+    mp, vp = np.pad(m2, pad), np.pad(np.where(fine, v2, 0), pad).astype(np.float32)
+    if rounding == hot.HOT_ROUND_DRAWN:
+        cm, cv = drawn.held(mp, vp, drawn.seed_of(lr, b1, b2, 1))
+        cm = drawn.held_m(mp, drawn.draws(mp, np.pad(v2, pad), drawn.seed_of(lr, b1, b2, 1)))
+    else:
+        cm, cv = (hold(x, rounding == hot.HOT_ROUND_NEAREST_EVEN) for hold, x in ((ref.held_m, mp), (ref.held_v, vp)))
+    got_m, got_v = values(d, n)
+    assert np.array_equal(got_m, ref.read_m(*cm)[:n])
+    marked = np.arange(n) // 32 == 1100 // 32
+    assert np.isnan(got_v[marked]).all() and np.array_equal(got_v[~marked], ref.read_v(*cv)[:n][~marked])
+    assert abs(float(got_v[70]) / float(v2[70]) - 1) <= 2.0 ** -3           # one of the two neighbours
