@@ -724,7 +724,7 @@ __global__ __launch_bounds__(256) void expand_row_kernel(const AdapterExpand a, 
 }
 
 // ---- what a backward call needs first -------------------------------------------------------------
-// Workgroups of the first `adapters` blocks: the segments of adapter k, in the order they have, behind those of the lower ones.  The others:
+// Workgroups of the first blocks: the segments of a range of adapters each, in the order they have, behind those of the lower ones.  The others:
 // 64 x 64 tiles of the two transposes.
 __device__ __forceinline__ int64_t block_sum(int64_t v, int64_t* s_sum) {
   const int lane = threadIdx.x & 63;
@@ -736,56 +736,115 @@ __device__ __forceinline__ int64_t block_sum(int64_t v, int64_t* s_sum) {
   return s_sum[0] + s_sum[1] + s_sum[2] + s_sum[3];
 }
 
-__device__ void sort_segments(const AdapterPrepare& a, int k) {
+// A workgroup reads every segment twice, so there are at most kSorts of them, whatever the adapters are: 65536 adapters are ranges of 256
+// (262144 segments: 0.67 ms, with a workgroup for each adapter 32.4).  2^20 segments of 16 adapters: 6.5 ms, all in the order of the waves.
+constexpr int kSorts = 256, kSortRange = 256;
+__device__ void sort_segments(const AdapterPrepare& a, int k0, int k1) {
   __shared__ int64_t s_sum[4];
-  __shared__ int s_len[4], s_cnt[4];
+  __shared__ uint32_t s_rows[kSortRange], s_count[kSortRange];      // of each adapter's segments; then where its next one goes
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int L = (int)a.b.L;
-  const auto length = [&](int s) {
-    const int b = min(max(a.b.offsets[s], 0), L);
-    return min(max(a.b.offsets[s + 1], b), L) - b;
+  const int L = (int)a.b.L, range = k1 - k0;
+  // Four segments' adapters (-1 past the last one) and lengths, 64 apart, in loads that wait together.
+  struct Four {
+    int x[4];
+    uint32_t len[4];
   };
+  const auto load = [&](int s, Four& f) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const int at = min(s + e * 64, a.b.segments - 1);
+      const int b = min(max(a.b.offsets[at], 0), L);
+      f.len[e] = (uint32_t)(min(max(a.b.offsets[at + 1], b), L) - b);
+      f.x[e] = s + e * 64 < a.b.segments ? a.b.index[at] : -1;
+    }
+  };
+  s_rows[tid] = s_count[tid] = 0;
+  __syncthreads();
   int64_t before = 0;                       // rows, and (upper half) segments, of lower adapters
-  for (int s = tid; s < a.b.segments; s += 256) {
-    const int x = a.b.index[s];
-    if (x >= 0 && x < k) before += (int64_t)1 << 32 | (int64_t)length(s);
+  for (int s0 = wave * 256 + lane; s0 < a.b.segments; s0 += 1024) {
+    Four f;
+    load(s0, f);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      if (f.x[e] >= 0 && f.x[e] < k0) before += (int64_t)1 << 32 | (int64_t)f.len[e];
+      if (range > 1 && f.x[e] >= k0 && f.x[e] < k1) {
+        atomicAdd(&s_rows[f.x[e] - k0], f.len[e]);
+        atomicAdd(&s_count[f.x[e] - k0], 1u);
+      }
+    }
   }
   before = block_sum(before, s_sum);
-  int rows = (int)(before & 0x7FFFFFFF), count = (int)(before >> 32 & 0x7FFFFFFF);
-  if (tid == 0) a.first[k] = rows;
-  for (int s0 = 0; s0 < a.b.segments; s0 += 256) {
-    const int s = s0 + tid;
-    const bool mine = s < a.b.segments && a.b.index[s] == k;
-    int len = mine ? length(s) : 0;
-    const int own = len;
-    const uint64_t votes = __builtin_amdgcn_ballot_w64(mine);
+  uint32_t rows = (uint32_t)before & 0x7FFFFFFFu, count = (uint32_t)(before >> 32) & 0x7FFFFFFFu;
+  if (range > 1) {                          // those of the range's lower ones too
+    const uint32_t own_rows = s_rows[tid], own_count = s_count[tid];
+    uint32_t r = own_rows, c = own_count;
 #pragma unroll
     for (int m = 1; m < 64; m *= 2) {
-      const int other = __shfl_up(len, m);
-      if (lane >= m) len += other;
+      const uint32_t r_other = __shfl_up(r, m), c_other = __shfl_up(c, m);
+      if (lane >= m) {
+        r += r_other;
+        c += c_other;
+      }
     }
     __syncthreads();
-    if (lane == 63) s_len[wave] = len;
-    if (lane == 0) s_cnt[wave] = __popcll(votes);
+    if (lane == 63) s_sum[wave] = (int64_t)c << 32 | r;
     __syncthreads();
-    int at = rows + len - own, place = count + __popcll(votes & ((1ull << lane) - 1));
+    rows += r - own_rows;
+    count += c - own_count;
     for (int w = 0; w < wave; ++w) {
-      at += s_len[w];
-      place += s_cnt[w];
-    }
-    if (mine && place < a.b.segments) {      // always, but for offsets that do not ascend
-      a.order[place] = s;
-      a.start[place] = at;
-    }
-    for (int w = 0; w < 4; ++w) {
-      rows += s_len[w];
-      count += s_cnt[w];
+      rows += (uint32_t)s_sum[w];
+      count += (uint32_t)(s_sum[w] >> 32);
     }
   }
-  if (k == a.b.adapters - 1) {              // behind the last one: all that no adapter has, past every row
-    if (tid == 0) a.first[k + 1] = rows;
-    for (int s = count + tid; s <= a.b.segments; s += 256) {
-      a.start[s] = rows;
+  s_rows[tid] = rows;
+  s_count[tid] = count;
+  if (tid < range) a.first[k0 + tid] = (int)rows;
+  __syncthreads();
+  Four next;
+  load(wave * 256 + lane, next);
+  for (int s0 = 0; s0 < a.b.segments; s0 += 1024) {
+    const int first = s0 + wave * 256 + lane;
+    const Four f = next;
+    load(min(first, a.b.segments) + 1024, next);      // on their way meanwhile
+    for (int w = 0; w < 4; ++w) {           // the waves in turn, in each one adapter after the other
+      if (wave == w) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const int s = first + e * 64, x = f.x[e];
+          const bool mine = x >= k0 && x < k1;
+          for (uint64_t left = __builtin_amdgcn_ballot_w64(mine); left;) {
+            const int k = __builtin_amdgcn_readlane(x, __ffsll((unsigned long long)left) - 1);
+            const uint64_t same = __builtin_amdgcn_ballot_w64(mine && x == k);
+            const bool here = same >> lane & 1;
+            const uint32_t own = here ? f.len[e] : 0;
+            uint32_t len = own;
+#pragma unroll
+            for (int m = 1; m < 64; m *= 2) {
+              const uint32_t other = __shfl_up(len, m);
+              if (lane >= m) len += other;
+            }
+            const uint32_t at = s_rows[k - k0], place = s_count[k - k0] + __popcll(same & ((1ull << lane) - 1));
+            if (here && place < (uint32_t)a.b.segments) {      // always, but for offsets that do not ascend
+              a.order[place] = s;
+              a.start[place] = (int)(at + len - own);
+            }
+            if (lane == 63) {
+              s_rows[k - k0] = at + len;
+              s_count[k - k0] = place + (here ? 1 : 0);
+            }
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");    // the next of these may be read in the next trip
+            left &= ~same;
+          }
+        }
+      }
+      __syncthreads();
+    }
+  }
+  if (k1 == a.b.adapters) {                 // behind the last one: all that no adapter has, past every row
+    const int end = (int)s_rows[range - 1], done = (int)s_count[range - 1];
+    if (tid == 0) a.first[k1] = end;
+    for (int s = done + tid; s <= a.b.segments; s += 256) {
+      a.start[s] = end;
       if (s < a.b.segments) a.order[s] = 0;
     }
   }
@@ -823,10 +882,10 @@ __device__ void transpose_tile(const T* from, int64_t rows, int64_t cols, T* to,
 }
 
 template <class T>
-__global__ __launch_bounds__(256) void prepare_kernel(const AdapterPrepare a, int sorts, int tiles_a, int tiles_w, int rank_tiles) {
+__global__ __launch_bounds__(256) void prepare_kernel(const AdapterPrepare a, int sorts, int range, int tiles_a, int tiles_w, int rank_tiles) {
   int b = blockIdx.x;
   if (b < sorts) {
-    sort_segments(a, b);
+    sort_segments(a, b * range, min((b + 1) * range, a.b.adapters));
     return;
   }
   b -= sorts;
@@ -1250,12 +1309,12 @@ hipError_t launch_adapter_expand(const AdapterExpand& a, bool rows, hot_type typ
   return type == HOT_BF16 ? expand_of<bf16>(a, rows, s) : expand_of<float>(a, rows, s);
 }
 hipError_t launch_adapter_prepare(const AdapterPrepare& a, hot_type type, hipStream_t s) {
-  const int sorts = a.order ? a.b.adapters : 0;
+  const int range = (int)ceil_div(a.b.adapters, kSorts), sorts = a.order ? (int)ceil_div(a.b.adapters, range) : 0;      // 256 of 256 at most
   const int rank_tiles = (int)ceil_div(a.rank, 64);
   const int tiles_a = a.at ? (int)ceil_div(a.I, 64) * rank_tiles : 0, tiles_w = (int)ceil_div(round_up(a.K, 64) / 32 * ceil_div(a.rank, 16), 4);
   const uint32_t grid = (uint32_t)(sorts + (int64_t)a.b.adapters * (tiles_a + tiles_w));
-  if (type == HOT_BF16) prepare_kernel<bf16><<<grid, 256, 0, s>>>(a, sorts, tiles_a, tiles_w, rank_tiles);
-  else prepare_kernel<float><<<grid, 256, 0, s>>>(a, sorts, tiles_a, tiles_w, rank_tiles);
+  if (type == HOT_BF16) prepare_kernel<bf16><<<grid, 256, 0, s>>>(a, sorts, range, tiles_a, tiles_w, rank_tiles);
+  else prepare_kernel<float><<<grid, 256, 0, s>>>(a, sorts, range, tiles_a, tiles_w, rank_tiles);
   return hipGetLastError();
 }
 hipError_t launch_adapter_pack(const AdapterPack& a, hot_type type, hipStream_t s) {
