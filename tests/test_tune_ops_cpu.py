@@ -268,3 +268,19 @@ def test_eight_bit_moments_round_trip_and_round_as_said():
     v = rng.uniform(1.0, 2.0, 1 << 16).astype(np.float32)
     c, e = ref.held_v(v, False)
     assert abs((ref.read_v(c, e).astype(np.float64) - v).mean()) < 4 * 0.125 / math.sqrt(12 * (1 << 16)) + 0.125 / 2048
+
+
+# ---- the timing of stages ----------------------------------------------------------------------------------------------
+
+def test_every_stage_but_the_gap_has_a_name_of_its_own():
+    """24 is none, so that a list read up to the first number without a name is the one that it was; the last ones end at HOT_NUM_STAGES_ALL."""
+    l, n = hot.lib(), hot.HOT_NUM_STAGES_ALL
+    names = [l.hot_debug_stage_name(i).decode() for i in range(-1, n + 2)][1:]
+    assert names[24] == names[n] == names[n + 1] == "" and l.hot_debug_stage_name(-1) == b""
+    named = [s for i, s in enumerate(names[:n]) if i != 24]
+    assert all(named) and len(set(named)) == n - 1
+    assert names[25] == "adapter_prepare" and names[31:] == ["token_logprobs", "token_logprobs_grad", "adamw", "adamw_state_read", "adamw_state_write", "", ""]
+    ms, launches = (C.c_float * (n + 2))(*[-1.0] * (n + 2)), (C.c_int64 * (n + 2))(*[-1] * (n + 2))
+    l.hot_debug_profile_begin()
+    assert l.hot_debug_profile_end_all(ms, launches, n + 1) == hot.HOT_OK
+    assert list(ms) == [0.0] * (n + 1) + [-1.0] and list(launches) == [0] * (n + 1) + [-1]
