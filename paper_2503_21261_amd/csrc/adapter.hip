@@ -117,12 +117,6 @@ __device__ __forceinline__ f4 mma(const Frag<float>& a, const Frag<float>& b, f4
   for (int t = 0; t < 8; ++t) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a.v[t], b.v[t], c, 0, 0, 0);
   return c;
 }
-__device__ __forceinline__ Frag<bf16> frag(const Raw8<bf16>& r) { return Frag<bf16>{__builtin_bit_cast(u4, r.a)}; }
-__device__ __forceinline__ Frag<float> frag(const Raw8<float>& r) {
-  Frag<float> f;
-  widen(r, f.v);
-  return f;
-}
 
 // Parts of eight fp32 numbers as bfloat16: the upper 16 bits, then those of what is left.  An infinity or a NaN is whole in the first.
 template <int PARTS>
@@ -1116,7 +1110,7 @@ __global__ __launch_bounds__(64 * kOuterWaves) void outer_kernel(const AdapterOu
     __syncthreads();          // the next adapter begins with the first slot again
     pos = k_end;
     // Lane (i, q) has ranks 16 t + 4 q + e of its eight columns.
-    const float scale = o.scaled && a.scale ? a.scale[k] : 1.0f;
+    const float scale = a.scale ? a.scale[k] : 1.0f;
     float* const to = o.part + (int64_t)(part + k) * a.rank * o.N;
     if (col0 + i * 8 < o.N) {
 #pragma unroll

@@ -50,12 +50,11 @@ struct AdapterPack {
   int32_t* rows;                    // rows of the positions
   int rank, g_pitch, slices;
 };
-// One product of sums over rows: part[slot][j][n] = sum over the part's rows of p[j][l] q[l][n].
+// One product of sums over rows: part[slot][j][n] = scale[adapter] times the sum over the part's rows of p[j][l] q[l][n].
 struct AdapterOuterOperand {
   const void *p, *q;
   float* part;
   int64_t N;
-  int scaled;                       // p times the adapter's scale
 };
 struct AdapterOuter {
   AdapterBatch b;

@@ -171,8 +171,8 @@ hot_status hot_adapter_backward(const void* g_y, const void* x, const float* u, 
     HOT_STAGE(kStAdapterPack, launch_adapter_pack(pack, type, s));
     AdapterOuter outer{};
     outer.b = batch;
-    outer.a[0] = AdapterOuterOperand{pack.g_out, x, (float*)(w + p.part_a), I, 1};
-    outer.a[1] = AdapterOuterOperand{pack.u_out, g_y, (float*)(w + p.part_b), O, 1};
+    outer.a[0] = AdapterOuterOperand{pack.g_out, x, (float*)(w + p.part_a), I};
+    outer.a[1] = AdapterOuterOperand{pack.u_out, g_y, (float*)(w + p.part_b), O};
     outer.scale = scale;
     outer.first = pack.first;
     outer.rows = pack.rows;
@@ -187,7 +187,7 @@ hot_status hot_adapter_backward(const void* g_y, const void* x, const float* u, 
 
 size_t hot_token_logprobs_workspace_bytes(hot_type type, int64_t rows, int64_t vocab, int32_t top) {
   if (!type_ok(type) || !size_ok(rows, vocab) || top < 0 || top > HOT_MAX_TOP || top > vocab) return 0;
-  return logprob_scratch_bytes(type, rows, vocab, top);
+  return logprob_scratch_bytes(rows, vocab, top);
 }
 
 hot_status hot_token_logprobs(const void* logits, hot_type type, int64_t rows, int64_t vocab, const int64_t* targets, float* logp,
@@ -196,7 +196,7 @@ hot_status hot_token_logprobs(const void* logits, hot_type type, int64_t rows, i
   if (!logits || !type_ok(type) || !targets != !logp || !top_logp != !top_ids || !top_logp != (top == 0)) return HOT_ERR_ARG;
   if (!logp && !entropy && !stats && !top) return HOT_ERR_ARG;
   if (!size_ok(rows, vocab) || top < 0 || top > HOT_MAX_TOP || top > vocab) return HOT_ERR_SHAPE;
-  const size_t need = logprob_scratch_bytes(type, rows, vocab, top);
+  const size_t need = logprob_scratch_bytes(rows, vocab, top);
   if (need && (!ws || !aligned256(ws))) return HOT_ERR_ARG;
   Buffers b;
   b.in(logits, bytes_of(type, rows, vocab));

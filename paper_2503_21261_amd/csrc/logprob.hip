@@ -479,15 +479,15 @@ hipError_t run_grad(GradArgs k, int64_t rows, hipStream_t s) {
 
 // Few rows are cut into parts, so that there are workgroups for all compute units; a part is one span at least, and with likeliest tokens what a
 // workgroup holds in registers at most.
-int logprob_parts(hot_type, int64_t rows, int64_t vocab, int top) {
+static int logprob_parts(int64_t rows, int64_t vocab, int top) {
   const int64_t most = ceil_div(vocab, kSpan), wanted = ceil_div(2048, rows);
   int64_t parts = most < wanted ? most : wanted;
   if (top && parts < ceil_div(vocab, 4 * kSpan)) parts = ceil_div(vocab, 4 * kSpan);
   if (parts > kMaxParts) parts = kMaxParts;
   return (int)ceil_div(vocab, (int64_t)spans_of_part(vocab, (int)parts) * kSpan);
 }
-size_t logprob_scratch_bytes(hot_type type, int64_t rows, int64_t vocab, int top) {
-  const int parts = logprob_parts(type, rows, vocab, top);
+size_t logprob_scratch_bytes(int64_t rows, int64_t vocab, int top) {
+  const int parts = logprob_parts(rows, vocab, top);
   return parts == 1 ? 0 : (size_t)(rows * parts) * (16 + 8 * (size_t)top);
 }
 
@@ -502,7 +502,7 @@ hipError_t launch_logprobs(const LogProbs& a, hipStream_t s) {
   k.top_ids = a.top_ids;
   k.vocab = a.vocab;
   k.top = a.top;
-  k.parts = logprob_parts(a.type, a.rows, a.vocab, a.top);
+  k.parts = logprob_parts(a.rows, a.vocab, a.top);
   k.part = spans_of_part(a.vocab, k.parts) * kSpan;
   if (k.parts > 1) {
     k.part_sums = (float*)a.ws;

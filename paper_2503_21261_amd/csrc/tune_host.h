@@ -56,8 +56,7 @@ struct LogProbs {
   int32_t* top_ids;
   void* ws;
 };
-int logprob_parts(hot_type type, int64_t rows, int64_t vocab, int top);
-size_t logprob_scratch_bytes(hot_type type, int64_t rows, int64_t vocab, int top);
+size_t logprob_scratch_bytes(int64_t rows, int64_t vocab, int top);
 hipError_t launch_logprobs(const LogProbs& a, hipStream_t s);
 struct LogProbGrad {
   const void* logits;
