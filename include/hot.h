@@ -366,6 +366,7 @@ hot_status hot_linear_forward(const void* x, const void* w, hot_type type, const
  * adapters <= 65536, adapters * (O + I) < 2^27.
  * Products and sums are fp32; bfloat16 operands are exact, u enters the second product with 16 bits or more.  An infinity or
  * a NaN in a row stays in it; one in an adapter makes infinities or NaNs in the outputs that its elements have a part in.
+ * The same call gives the same bits; the same row at another place of a batch may differ in its last ones (the order of its sums).
  * ws: at least hot_adapter_forward_workspace_bytes() bytes of scratch, 256-byte aligned.
  */
 size_t hot_adapter_forward_workspace_bytes(hot_type type, int64_t L, int64_t O, int64_t I, int64_t rank, int64_t adapters,
@@ -383,7 +384,8 @@ hot_status hot_adapter_forward(const void* x, const void* a, const void* b, hot_
  * forward call wrote.  g_a, g_b: fp32, of the shapes of a and b (out), both or neither, written whole: zeros for an
  * adapter that has no rows.  g_x, or g_a and g_b, must be given; x and u are needed for g_a and g_b, a for
  * g_x.  Rows without an adapter have g_x = g_base; g_x's rows outside the segments are left as they were.
- * ws: at least hot_adapter_backward_workspace_bytes() bytes of scratch, 256-byte aligned; nothing in it is kept between calls.
+ * ws: at least hot_adapter_backward_workspace_bytes() bytes of scratch, 256-byte aligned; nothing in it is kept between calls.  It
+ * grows with adapters * rank * (O + I), whether they have rows or not.
  */
 size_t hot_adapter_backward_workspace_bytes(hot_type type, int64_t L, int64_t O, int64_t I, int64_t rank, int64_t adapters,
                                             int64_t segments);
@@ -478,7 +480,8 @@ hot_status hot_adamw_state_read(const void* state, hot_moment moment, int64_t n,
 hot_status hot_adamw_state_write(const void* x, hot_type type, hot_moment moment, int64_t n, void* state, void* stream);
 
 /* The tensors of a step, checked once and written into `table`, HOST memory of hot_adamw_table_bytes(count) bytes that the
- * caller keeps (0: count below 1), aligned to 8.  No output of any tensor may lie on another one or on an input (HOT_ERR_ARG); moments
+ * caller keeps (0: count below 1), aligned to 8: it holds addresses, so that other gradients, ones allocated anew for each step among
+ * them, need another table.  No output of any tensor may lie on another one or on an input (HOT_ERR_ARG); moments
  * of all tensors have the same form. */
 size_t hot_adamw_table_bytes(int32_t count);
 hot_status hot_adamw_table(const hot_adamw_tensor* tensors, int32_t count, hot_state_form state, void* table, size_t table_bytes);

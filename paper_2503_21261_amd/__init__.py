@@ -764,7 +764,8 @@ def hot_adamw_state_write(x: torch.Tensor, moment: str, buf: torch.Tensor, strea
 
 class AdamWTensors:
     """The tensors of an optimiser step: a list of dicts with param, grad, m and v, and where wanted copy (bfloat16), param_out, m_out,
-    v_out (in place without), weight_decay and lr_factor.  Checked once, and held as long as this object lives."""
+    v_out (in place without), weight_decay and lr_factor.  Checked once, and held as long as this object lives: zero or write the gradients
+    where they are (gradients allocated anew need another object, some microseconds a tensor)."""
 
     def __init__(self, tensors: Sequence[dict], state: str = "f32"):
         form = _STATES[state]

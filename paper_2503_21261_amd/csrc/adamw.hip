@@ -4,8 +4,9 @@
 // Bound by memory: an element is read and written once, 28 bytes with fp32 moments and parameters, 16.1 with 8-bit moments and
 // fp32 parameters and gradients.  One launch takes forty tensors: a lane finds its tensor from its workgroup's number, so that
 // small tensors (biases, norms) cost no launch of their own.  302 million fp32 elements: 1518 us, 5.6 TB/s; 361 million with 8-bit
-// moments, bfloat16 gradients and copies: 1147 us, 5.1 TB/s; 18 million bfloat16 ones with 8-bit moments: 53 us, 3.5 TB/s, bound by the
-// hundred vector instructions of an element (quotient and root rounded once, two codes), which fill 88 % of the cycles there.  Both with moments
+// moments, bfloat16 gradients and copies: 1134 us, 5.1 TB/s; 18 million bfloat16 ones with 8-bit moments: 53 us, 3.5 TB/s, bound by the
+// hundred vector instructions of an element (quotient and root rounded once, two codes), which come at the same rate in the larger one: 1.1 to 1.2
+// of them in four cycles of a SIMD.  Both with moments
 // rounded by their own low bits; by draws (below) 1114 us, for 1095 in the same process, and 57.
 #include "block_device.h"
 #include "tune_host.h"

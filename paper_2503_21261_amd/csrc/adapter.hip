@@ -1003,7 +1003,7 @@ constexpr int kOuterCols = 128, kOuterWaves = 4;    // columns of a wave, waves 
 // of a workgroup are side by side and share the rows' factors through LDS: each loads a quarter, with its rows, so that both are as far
 // ahead (a wait for factors loaded later than rows is one for the rows).  Sums over rows leave as one partial sum a part and adapter.
 // 16384 x (4096 + 11008) bfloat16, rank 64: 130 to 145 us for 495 MB of rows (each wave loading all factors: 175), 4.1 TB/s with the factors; matrix and
-// vector pipes are busy for a third of it each, and the one wave a SIMD that 64 ranks leave room for waits with the others at every step's
+// vector pipes are busy for 31 and 30 % of it, and the one wave a SIMD that 64 ranks leave room for waits with the others at every step's
 // barrier.  12608 x (768 + 2304) fp32, rank 16: 32.7 us for 155 MB, 4.7 TB/s.
 // MODE: 0 all rows as they lie, 1 in the order of a.rows, 2 too, with fewer than eight columns in one of the products.
 template <class T, int RT, int MODE, int DEPTH>
@@ -1246,7 +1246,10 @@ AdapterPlan adapter_plan(hot_type type, int64_t L, int64_t O, int64_t I, int64_t
   const int64_t size = type == HOT_BF16 ? 2 : 4, step = 128 / size;
   p.rows = L <= 4 * (segments > 0 ? segments : 1) && L <= 1 << 20;
   p.pitch = (int)round_up(rank, 8);      // zeros behind the ranks
-  // Rows of a workgroup: as many as leave workgroups for all compute units without slices, 16 at least.
+  // Rows of a workgroup: 16 to 64.  First product and expansion of a bfloat16 pass 4096 -> 11008, in us with 16 and with 32 rows: rank 16, 1024 rows 30 and
+  // 36, 2048 54 and 57, 5000 66 and 100; rank 64 67 and 99, 71 and 92, 82 and 132; fp32, rank 64: 213 and 378, 239 and 401, 187 and 433.  The first
+  // product itself is the faster with 32 (5000 rows, fp32, rank 64: 41 for 60), but in slices up to 8192 rows, with 16 up to 4096, which the expansion
+  // adds.  So 32 rows pay from where they need no slices; the border here is lower than that.
   p.tile = p.rows ? 1 : L >= 64 * 224 && rank > 16 && rank <= 64 ? 64 : L >= 64 * 32 && rank <= 64 ? 32 : 16;
   // With no slices the expansion finds its factors packed: not where each wave has four steps at most, which are all on their way at once, and
   // the workgroups are not too few (3330 x 771 bfloat16, rank 12: 10.8 us in four slices or in none, and the expansion to 2307 then 26 us or 13.9).
@@ -1261,7 +1264,9 @@ AdapterPlan adapter_plan(hot_type type, int64_t L, int64_t O, int64_t I, int64_t
   };
   slices(I, p.slices_forward, p.slice_forward);
   slices(O, p.slices_backward, p.slice_backward);
-  // Parts of the sums over rows: workgroups for all compute units (one each with the registers of 64 ranks, two below).
+  // Parts of the sums over rows: workgroups for all compute units (one each with the registers of 64 ranks, two below), and no more, since each part's
+  // sums are written and added (8192 rows 4096 -> 11008, rank 64: 67 us and 11 for the parts, with twice as many 81 and 35).  That leaves compute units
+  // idle where tiles are just more than half of them (136 tiles, 4096 rows, rank 128: 219 us and 28, in four parts 183 and 38).
   const int64_t tiles = (ceil_div(I, kOuterCols * kOuterWaves) + ceil_div(O, kOuterCols * kOuterWaves)) * ceil_div(rank, 64);
   const int64_t wanted = 256 / tiles, most = ceil_div(L, 64);
   p.parts = (int)(wanted < 1 ? 1 : wanted < most ? wanted : most);
