@@ -364,7 +364,7 @@ hot_status hot_linear_forward(const void* x, const void* w, hot_type type, const
  * offsets that do not ascend or leave [0, L] give undefined results within the buffers.
  * 1 <= rank <= 128 (adapters of lower rank beside it: zeros in a and b), L < 2^27, segments <= 2^24,
  * adapters <= 65536, adapters * (O + I) < 2^27.
- * Products and sums are fp32; bfloat16 operands are exact, u enters the second product with 16 bits or more.  An infinity or
+ * Products and sums are fp32; bfloat16 operands are exact, u enters the second product within 2^-16 of itself.  An infinity or
  * a NaN in a row stays in it; one in an adapter makes infinities or NaNs in the outputs that its elements have a part in.
  * The same call gives the same bits; the same row at another place of a batch may differ in its last ones (the order of its sums).
  * ws: at least hot_adapter_forward_workspace_bytes() bytes of scratch, 256-byte aligned.

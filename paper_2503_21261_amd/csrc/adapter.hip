@@ -9,7 +9,8 @@
 //   outer   [rows x rank]^T . [rows x N] -> [rank x N]: rows as they lie are transposed in registers, 8 x 8 values a lane, the factors
 //           before, by a launch of its own.
 // u and g_u are fp32.  Where they meet bfloat16 operands they are split into bfloat16 parts, cut off and not rounded, so that three
-// parts are the number itself: three for fp32 results (g_A, g_B), two (2^-16) for bfloat16 ones.
+// parts are the number itself: three for fp32 results (g_A, g_B), two for bfloat16 ones, the second of which is rounded: 16 bits, within 2^-16
+// of the number (cut off as well it would be within 2^-15).
 #include <type_traits>
 
 #include "adapter_host.h"
@@ -118,7 +119,11 @@ __device__ __forceinline__ f4 mma(const Frag<float>& a, const Frag<float>& b, f4
   return c;
 }
 
-// Parts of eight fp32 numbers as bfloat16: the upper 16 bits, then those of what is left.  An infinity or a NaN is whole in the first.
+// Parts of eight fp32 numbers as bfloat16: the upper 16 bits, then those of what is left, rounded to nearest in the second of two.  An infinity
+// or a NaN is whole in the first.
+__device__ __forceinline__ uint32_t rounded_pair(uint32_t a, uint32_t b) {
+  return (uint32_t)float_to_bf16(__uint_as_float(b)) << 16 | float_to_bf16(__uint_as_float(a));
+}
 template <int PARTS>
 __device__ __forceinline__ void split8(const float (&v)[8], Frag<bf16> (&out)[PARTS]) {
   float left[8];
@@ -140,7 +145,8 @@ __device__ __forceinline__ void split8(const float (&v)[8], Frag<bf16> (&out)[PA
       }
     }
 #pragma unroll
-    for (int i = 0; i < 4; ++i) out[p].v[i] = __builtin_amdgcn_perm(bits[2 * i + 1], bits[2 * i], 0x07060302u);
+    for (int i = 0; i < 4; ++i)
+      out[p].v[i] = PARTS == 2 && p == 1 ? rounded_pair(bits[2 * i], bits[2 * i + 1]) : __builtin_amdgcn_perm(bits[2 * i + 1], bits[2 * i], 0x07060302u);
   }
 }
 
@@ -161,7 +167,8 @@ __device__ __forceinline__ void store_factors(bf16* p, int64_t l, int j, int chu
   }
 #pragma unroll
   for (int s = 0; s < 2; ++s) {
-    const uint2 x = make_uint2(__builtin_amdgcn_perm(part[s][1], part[s][0], 0x07060302u), __builtin_amdgcn_perm(part[s][3], part[s][2], 0x07060302u));
+    const auto pair = [&](uint32_t a, uint32_t b) { return s == 0 ? __builtin_amdgcn_perm(b, a, 0x07060302u) : rounded_pair(a, b); };
+    const uint2 x = make_uint2(pair(part[s][0], part[s][1]), pair(part[s][2], part[s][3]));
     const int in = j & 31;
     bf16* const at = chunks == 0 ? p + (l >> 4) * kTile + ((s * 2 + in / 8) * 16 + (l & 15)) * 8
                                  : p + (((l >> 4) * chunks + (j >> 5)) * 2 + s) * kTile + (in / 8 * 16 + (l & 15)) * 8;

@@ -6,7 +6,7 @@
 // gradient reads them and writes as much.  16384 x 32000 bfloat16 with entropy: 213 us (4.9 TB/s) and 378 us (5.6).
 //
 // A row is a workgroup's where there are rows for all compute units, so that nothing is joined; few rows are cut into parts, which a launch of
-// one wave a row joins: 96 x 50257 fp32, 8 likeliest: 11.5 and 4.0 us; 1 x 32000, 20 likeliest: 7.9 and 4.9, latencies.
+// one wave a row joins: 96 x 50257 fp32, 8 likeliest: 11.5 and 4.1 us; 1 x 32000, 20 likeliest: 7.3 and 5.0, latencies.
 #include "block_device.h"
 #include "block_host.h"
 #include "tune_host.h"
