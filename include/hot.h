@@ -419,7 +419,7 @@ hot_status hot_token_logprobs(const void* logits, hot_type type, int64_t rows, i
  * Gradient of the logits: g_z = g_logp (1[target] - p) - g_entropy p (log p + entropy).
  * targets with g_logp (fp32 [rows]), both or neither; entropy (what the forward call wrote) with g_entropy (fp32 [rows]), both
  * or neither; one of the pairs at least.  A row whose target is not scored has no part of g_logp; a row of -inf alone has
- * gradient 0.  g_logits: [rows x vocab] of `type` (out); it may be logits.
+ * gradient 0.  A p below 2^-126 counts as 0, here and in the entropy.  g_logits: [rows x vocab] of `type` (out); it may be logits.
  */
 hot_status hot_token_logprobs_backward(const void* logits, hot_type type, int64_t rows, int64_t vocab, const int64_t* targets,
                                        const float* stats, const float* entropy, const float* g_logp, const float* g_entropy,

@@ -21,6 +21,7 @@ constexpr float kLog2e = 1.44269504088896341f, kLn2 = 0.693147180559945309f;
 constexpr float kLowest = -3.402823466e+38f;
 constexpr float kFloor = -300.0f;                    // e^-300 is 0: keeps 0 x -inf out of a sum
 
+// 0 where the power is below 2^-126 (the instruction's way), which is 2^-126 |log p| of a gradient at most.
 __device__ __forceinline__ float exp_of(float d) { return __builtin_amdgcn_exp2f(d * kLog2e); }
 
 // Sums of a part of a row: m = max z, s = sum e^(z - m), w = sum e^(z - m) (z - m).  An infinity or a NaN makes s and w NaN.

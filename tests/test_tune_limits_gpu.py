@@ -44,6 +44,21 @@ def test_ties_and_rows_without_tokens_in_parts_that_are_read_again():
 
 
 @pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("rows,V", [(5, 300), (70, 9000), (2100, 40)])
+@pytest.mark.parametrize("std,shift", [(40.0, 0.0), (100.0, -300.0), (1e-3, 50.0)])
+def test_logits_far_apart(std, shift, rows, V, dtype):
+    """Probabilities down to where they are none: those below 2^-126 count as 0, which is 2^-126 |log p + H| of the entropy's gradient."""
+    z = (rand((rows, V), std, rows + V) + shift).to(dtype)
+    targets, gl, ge = torch.randint(0, V, (rows,), generator=torch.Generator().manual_seed(1)), rand((rows,), 1.0, 2), rand((rows,), 1.0, 3)
+    want, got = ref.logprobs(z, targets, 0, gl, ge), run_logprobs(z, targets, 0, gl, ge)
+    for name in ("logp", "entropy", "stats"):
+        within(name, got[name], *want[name])
+    lp = torch.log_softmax(z.double(), 1)
+    none = torch.where(lp < -87, 2.0 ** -126 * ge.double().abs()[:, None] * torch.exp(lp + 126 * math.log(2)).clamp(max=1.0) * (lp.abs() + want["entropy"][0][:, None]), 0.0)
+    within("g_logits", got["g_logits"], want["g_logits"][0], want["g_logits"][1] + none)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
 @pytest.mark.parametrize("L", [1, 3, 70, 300])
 def test_rows_without_offsets_have_the_first_of_several_adapters(L, dtype):
     t, kind = make(L, 72, 100, 12, (None, None, 3), dtype, seed=9)
